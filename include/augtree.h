@@ -431,6 +431,72 @@ typedef struct {
 int augtree_plan_tree(const augtree_tree_t *tree, const augtree_profile_t *profile, augtree_choice_t *choice,
                       int32_t *round_out, int32_t *lane_out);
 
+/*
+ * The vocabulary ends of a model on the tree: the embedding lookup and the softmax cross entropy over the vocabulary,
+ * each with its gradient.  (The paper has no counterpart: its loss and its parameters are the base trainer's, Sec. 4.)
+ * Both work on a [vocab, hidden] matrix, which may be the same one (tied weights): table or weight, row-major, no padding.
+ *
+ * A handle holds the sizes, the scales and a status word; it does not depend on the number of tokens, so one handle
+ * serves a whole run, from single tokens to whole micro-batches.  It is immutable after creation and belongs to a
+ * device exactly as a plan does (same rule for the current device, streams and concurrent calls: each call that may
+ * overlap another needs a workspace of its own).  Token ids are int64 or int32 (id_bytes 8 or 4) device arrays.
+ *   id < 0       padding: a zero row of the embedding, a row that is not scored; whatever its hidden state holds (NaN
+ *                included) enters no result, and its work is saved
+ *   id >= vocab  is treated like padding, and AUGTREE_ERR_INVALID_ARG with the position of the token as detail is
+ *                recorded in the status word
+ * No atomics on floating-point values: results are bitwise repeatable.
+ */
+enum { AUGTREE_BF16 = 0, AUGTREE_F16 = 1, AUGTREE_F32 = 2 };
+typedef struct {
+  uint32_t struct_size;        /* sizeof(augtree_lm_desc_t)                                          */
+  uint32_t version;            /* AUGTREE_VERSION                                                    */
+  int32_t vocab, hidden;       /* hidden: a multiple of 8                                            */
+  float embed_scale;           /* out = embed_scale * table[id]; 0 => 1                              */
+  float logit_scale;           /* logits = logit_scale * (h . W): an inverse temperature; 0 => 1     */
+  uint32_t flags;              /* AUGTREE_FLAG_TEST_SHORT_WAIT, AUGTREE_FLAG_TEST_SKIP_FWD_LOAD      */
+  int32_t n_lanes;             /* persistent CTAs; 0 => SM count of device                           */
+  int64_t piece_bytes;         /* bound on the scratch that holds a piece of the logit gradient in the backward
+                                  pass (bf16, rows x piece of the vocabulary); 0 => 512 MiB, more if that were
+                                  under 4096 columns                                                 */
+} augtree_lm_desc_t;
+typedef struct augtree_lm augtree_lm_t;
+
+/* As augtree_plan_create: device < 0 makes a host-only handle (n_lanes must be given) for workspace queries.  This call
+ * and augtree_lm_destroy are the only ones that allocate or free device memory. */
+int augtree_lm_create(const augtree_lm_desc_t *desc, int device, augtree_lm_t **out);
+int augtree_lm_destroy(augtree_lm_t *lm);
+
+/* Scratch (16-byte aligned) that the calls need for n_tokens tokens; any of the pointers may be NULL. */
+int augtree_lm_workspace_bytes(const augtree_lm_t *lm, int64_t n_tokens, size_t *loss_fwd, size_t *loss_bwd, size_t *embed_bwd);
+
+/* out[t] = embed_scale * table[id_t], rounded once.  table and out: any of the three types each, 16-byte aligned. */
+int augtree_embed_fwd(const augtree_lm_t *lm, const void *table, int table_dtype, const void *ids, int id_bytes,
+                      int64_t n_tokens, void *out, int out_dtype, void *stream);
+
+/* d_table[v] = embed_scale * sum of d_out[t] over the tokens with id_t = v, summed in fp32 in an order that depends on
+ * the ids alone.  Every row of d_table is written (zeros where no token falls).  With accumulate != 0 (fp32 d_table
+ * only, else AUGTREE_ERR_UNSUPPORTED) the sums are ADDED instead and rows without tokens are left alone. */
+int augtree_embed_bwd(const augtree_lm_t *lm, const void *d_out, int out_dtype, const void *ids, int id_bytes,
+                      int64_t n_tokens, void *d_table, int table_dtype, int accumulate, void *ws, size_t ws_bytes, void *stream);
+
+/* Cross entropy of every token without its logits in memory:
+ *   lse[t] = ln sum_v exp(logit_scale h_t . W_v),   loss[t] = lse[t] - logit_scale h_t . W_target     (fp32; zeros for padding)
+ * hidden [n_tokens, hidden], weight [vocab, hidden]: bf16, 16-byte aligned.  -loss[t] is the token's log-probability. */
+int augtree_lm_loss_fwd(const augtree_lm_t *lm, const void *hidden, const void *weight, const void *targets, int id_bytes,
+                        int64_t n_tokens, float *loss, float *lse, void *ws, size_t ws_bytes, void *stream);
+
+/* Its gradient under the seed d_loss [n_tokens] (fp32): the logits are made again, a piece of the vocabulary at a time,
+ * and their gradient (bf16) is multiplied at once with weight and hidden:
+ *   d_hidden [n_tokens, hidden] bf16 (zeros for padding),   d_weight [vocab, hidden] bf16 or fp32.
+ * lse is the forward's.  Either output may be NULL: its product is then not computed.  With accumulate != 0 (fp32
+ * d_weight only, else AUGTREE_ERR_UNSUPPORTED) d_weight is ADDED to. */
+int augtree_lm_loss_bwd(const augtree_lm_t *lm, const void *hidden, const void *weight, const void *targets, int id_bytes,
+                        const float *lse, const float *d_loss, int64_t n_tokens, void *d_hidden, void *d_weight,
+                        int weight_dtype, int accumulate, void *ws, size_t ws_bytes, void *stream);
+
+/* As augtree_last_device_status, for a handle. */
+int augtree_lm_last_device_status(const augtree_lm_t *lm, int *status, int *detail);
+
 const char *augtree_status_string(int status);
 
 #ifdef __cplusplus

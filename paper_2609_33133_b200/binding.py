@@ -34,7 +34,9 @@ EXPORTS = ["augtree_plan_create", "augtree_plan_destroy", "augtree_plan_workspac
            "augtree_last_device_status", "augtree_launch_count", "augtree_status_string",
            "augtree_set_timing", "augtree_get_kernel_time", "augtree_replay_fwd_static", "augtree_assign_grid",
            "augtree_items_completed", "augtree_plan_tree", "augtree_replay_fwd_state", "augtree_merge_states",
-           "augtree_replay_bwd_state", "augtree_plan_bwd_handoff_bytes"]
+           "augtree_replay_bwd_state", "augtree_plan_bwd_handoff_bytes", "augtree_lm_create", "augtree_lm_destroy",
+           "augtree_lm_workspace_bytes", "augtree_embed_fwd", "augtree_embed_bwd", "augtree_lm_loss_fwd", "augtree_lm_loss_bwd",
+           "augtree_lm_last_device_status"]
 
 
 class Desc(C.Structure):
@@ -93,6 +95,20 @@ class ChoiceC(C.Structure):
                 ("lanes", C.c_int32), ("solved_exactly", C.c_int32), ("n_candidates", C.c_int32)]
 
 
+class LmDescC(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("version", C.c_uint32), ("vocab", C.c_int32), ("hidden", C.c_int32),
+                ("embed_scale", C.c_float), ("logit_scale", C.c_float), ("flags", C.c_uint32), ("n_lanes", C.c_int32),
+                ("piece_bytes", C.c_int64)]
+
+
+lib.augtree_lm_create.argtypes = [C.POINTER(LmDescC), C.c_int, C.POINTER(_vp)]
+lib.augtree_lm_destroy.argtypes = [_vp]
+lib.augtree_lm_workspace_bytes.argtypes = [_vp, C.c_int64, C.POINTER(_sz), C.POINTER(_sz), C.POINTER(_sz)]
+lib.augtree_embed_fwd.argtypes = [_vp, _vp, C.c_int, _vp, C.c_int, C.c_int64, _vp, C.c_int, _vp]
+lib.augtree_embed_bwd.argtypes = [_vp, _vp, C.c_int, _vp, C.c_int, C.c_int64, _vp, C.c_int, C.c_int, _vp, _sz, _vp]
+lib.augtree_lm_loss_fwd.argtypes = [_vp, _vp, _vp, _vp, C.c_int, C.c_int64, _vp, _vp, _vp, _sz, _vp]
+lib.augtree_lm_loss_bwd.argtypes = [_vp, _vp, _vp, _vp, C.c_int, _vp, _vp, C.c_int64, _vp, _vp, C.c_int, C.c_int, _vp, _sz, _vp]
+lib.augtree_lm_last_device_status.argtypes = [_vp, C.POINTER(C.c_int), C.POINTER(C.c_int)]
 lib.augtree_plan_tree.argtypes = [C.POINTER(TreeC), C.POINTER(ProfileC), C.POINTER(ChoiceC), _i32p, _i32p]
 
 
@@ -255,6 +271,94 @@ class Plan:
     def device_status(self):
         s, d = C.c_int(), C.c_int()
         _check(lib.augtree_last_device_status(self._h, C.byref(s), C.byref(d)), "last_device_status")
+        return s.value, d.value
+
+
+_DTYPE_CODE = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+_ID_BYTES = {torch.int64: 8, torch.int32: 4}
+
+
+class LM:
+    """Owns an augtree_lm_t: the embedding lookup and the vocabulary cross entropy of a [vocab, hidden] matrix, with their
+    gradients.  device=None builds a host-only handle (workspace queries only).  Every method checks its tensors, launches on
+    the current stream of the handle's device, which must be the current device, and returns without waiting."""
+
+    def __init__(self, vocab, hidden, *, device=0, embed_scale=0.0, logit_scale=0.0, flags=0, n_lanes=0, piece_bytes=0):
+        self.vocab, self.hidden, self.device = int(vocab), int(hidden), device
+        d = LmDescC(C.sizeof(LmDescC), 1, vocab, hidden, embed_scale, logit_scale, flags, n_lanes, piece_bytes)
+        self._h = C.c_void_p()
+        _check(lib.augtree_lm_create(C.byref(d), -1 if device is None else int(device), C.byref(self._h)), "lm_create")
+
+    def __del__(self):
+        h = getattr(self, "_h", None)
+        if h is not None and h.value and lib is not None:
+            lib.augtree_lm_destroy(h)
+            self._h = None
+
+    def workspace_parts(self, n_tokens):
+        """Scratch bytes of (loss_fwd, loss_bwd, embed_bwd) for n_tokens tokens."""
+        f, b, e = _sz(), _sz(), _sz()
+        _check(lib.augtree_lm_workspace_bytes(self._h, int(n_tokens), C.byref(f), C.byref(b), C.byref(e)), "lm_workspace_bytes")
+        return f.value, b.value, e.value
+
+    def workspace_bytes(self, n_tokens) -> int:
+        """Scratch for any call on up to n_tokens tokens."""
+        return max(self.workspace_parts(n_tokens))
+
+    def _arg(self, t, name, dtypes, shape):
+        if t.dtype not in dtypes or tuple(t.shape) != shape or not t.is_cuda or t.device.index != self.device or not t.is_contiguous():
+            raise ValueError(f"{name}: expected a contiguous tensor on cuda:{self.device} of shape {shape} and one of {list(dtypes)}, "
+                             f"got {tuple(t.shape)} {t.dtype} on {t.device}")
+        return t.data_ptr()
+
+    def _ids(self, t):
+        if t.dim() != 1:
+            raise ValueError("token ids: expected one dimension")
+        return self._arg(t, "token ids", _ID_BYTES, (t.shape[0],)), _ID_BYTES[t.dtype], t.shape[0]
+
+    def _ws(self, ws):
+        if not ws.is_cuda or ws.device.index != self.device or not ws.is_contiguous():
+            raise ValueError(f"ws: expected a contiguous tensor on cuda:{self.device}")
+        return ws.data_ptr(), ws.numel() * ws.element_size()
+
+    def embed_fwd(self, table, ids, out):
+        """out[t] = embed_scale * table[ids[t]]; zeros for a negative id."""
+        i, ib, n = self._ids(ids)
+        _check(lib.augtree_embed_fwd(self._h, self._arg(table, "table", _DTYPE_CODE, (self.vocab, self.hidden)), _DTYPE_CODE[table.dtype], i, ib,
+                                     n, self._arg(out, "out", _DTYPE_CODE, (n, self.hidden)), _DTYPE_CODE[out.dtype], Plan._stream()), "embed_fwd")
+
+    def embed_bwd(self, d_out, ids, d_table, ws, accumulate=False):
+        """d_table[v] = embed_scale * sum of d_out over the tokens of id v (added to an fp32 d_table with accumulate)."""
+        i, ib, n = self._ids(ids)
+        w, wb = self._ws(ws)
+        _check(lib.augtree_embed_bwd(self._h, self._arg(d_out, "d_out", _DTYPE_CODE, (n, self.hidden)), _DTYPE_CODE[d_out.dtype], i, ib, n,
+                                     self._arg(d_table, "d_table", _DTYPE_CODE, (self.vocab, self.hidden)), _DTYPE_CODE[d_table.dtype],
+                                     int(bool(accumulate)), w, wb, Plan._stream()), "embed_bwd")
+
+    def loss_fwd(self, hidden, weight, targets, loss, lse, ws):
+        """Cross entropy and log-sum-exp of every token; zeros where the target is negative."""
+        i, ib, n = self._ids(targets)
+        w, wb = self._ws(ws)
+        bf, f32 = (torch.bfloat16,), (torch.float32,)
+        _check(lib.augtree_lm_loss_fwd(self._h, self._arg(hidden, "hidden", bf, (n, self.hidden)),
+                                       self._arg(weight, "weight", bf, (self.vocab, self.hidden)), i, ib, n,
+                                       self._arg(loss, "loss", f32, (n,)), self._arg(lse, "lse", f32, (n,)), w, wb, Plan._stream()), "lm_loss_fwd")
+
+    def loss_bwd(self, hidden, weight, targets, lse, d_loss, d_hidden, d_weight, ws, accumulate=False):
+        """Gradients of sum(d_loss * loss); d_hidden or d_weight may be None, and is then not computed."""
+        i, ib, n = self._ids(targets)
+        w, wb = self._ws(ws)
+        bf, f32 = (torch.bfloat16,), (torch.float32,)
+        dh = None if d_hidden is None else self._arg(d_hidden, "d_hidden", bf, (n, self.hidden))
+        dw = None if d_weight is None else self._arg(d_weight, "d_weight", bf + f32, (self.vocab, self.hidden))
+        _check(lib.augtree_lm_loss_bwd(self._h, self._arg(hidden, "hidden", bf, (n, self.hidden)),
+                                       self._arg(weight, "weight", bf, (self.vocab, self.hidden)), i, ib, self._arg(lse, "lse", f32, (n,)),
+                                       self._arg(d_loss, "d_loss", f32, (n,)), n, dh, dw, 0 if dw is None else _DTYPE_CODE[d_weight.dtype],
+                                       int(bool(accumulate)), w, wb, Plan._stream()), "lm_loss_bwd")
+
+    def device_status(self):
+        s, d = C.c_int(), C.c_int()
+        _check(lib.augtree_lm_last_device_status(self._h, C.byref(s), C.byref(d)), "lm_last_device_status")
         return s.value, d.value
 
 

@@ -8,8 +8,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libaugtree.so")
-SOURCES = ["augtree.cu", "plan.cpp", "planner.cpp"]
-HEADERS = ["ptx.cuh", "fwd_kernel.cuh", "bwd_kernel.cuh", "dq_kernel.cuh", "dql_kernel.cuh", "plan.h", os.path.join("..", "..", "include", "augtree.h")]
+SOURCES = ["augtree.cu", "lm.cu", "plan.cpp", "planner.cpp"]
+HEADERS = ["ptx.cuh", "fwd_kernel.cuh", "bwd_kernel.cuh", "dq_kernel.cuh", "dql_kernel.cuh", "lm_tile_kernel.cuh", "lm_kernels.cuh", "launch.h", "plan.h", os.path.join("..", "..", "include", "augtree.h")]
 
 
 def _stale() -> bool:

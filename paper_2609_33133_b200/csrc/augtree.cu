@@ -12,6 +12,7 @@
 #include "dq_kernel.cuh"
 #include "dql_kernel.cuh"
 #include "fwd_kernel.cuh"
+#include "launch.h"
 #include "plan.h"
 
 using namespace augtree;
@@ -20,17 +21,9 @@ using namespace augtree;
 // each GPU that loads this library holds it until the process exits.
 static __device__ __align__(256) unsigned char g_static_scratch[AUGTREE_STATIC_SCRATCH_BYTES];
 
-namespace {
-
-constexpr int kMaxStaticDevices = 64;
-void *g_static_ptr[kMaxStaticDevices] = {};  // device address of g_static_scratch, per device
-std::mutex g_static_mutex;
+namespace augtree {
 
 std::atomic<long long> g_launches{0};
-
-typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
-                                  const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
 EncodeTiledFn get_encode() {
   static EncodeTiledFn fn = nullptr;
@@ -44,6 +37,14 @@ EncodeTiledFn get_encode() {
   });
   return fn;
 }
+
+}  // namespace augtree
+
+namespace {
+
+constexpr int kMaxStaticDevices = 64;
+void *g_static_ptr[kMaxStaticDevices] = {};  // device address of g_static_scratch, per device
+std::mutex g_static_mutex;
 
 // Tensor map over a packed [tokens, heads, d] bf16 tensor; one box = 128 tokens
 // of one head, 64 elements (128 bytes) wide, written to shared memory with the

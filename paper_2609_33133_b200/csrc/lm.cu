@@ -1,0 +1,413 @@
+// C-ABI entry points of a model's vocabulary ends: embedding lookup and vocabulary cross entropy, with their gradients.
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <new>
+
+#include "launch.h"
+#include "lm_kernels.cuh"
+#include "lm_tile_kernel.cuh"
+#include "../../include/augtree.h"
+
+using namespace augtree;
+
+struct augtree_lm {
+  int32_t vocab = 0, hidden = 0;
+  float embed_scale = 1.f, logit_scale = 1.f;
+  uint32_t flags = 0;
+  int32_t n_lanes = 0;
+  int64_t piece_bytes = 0;
+  int device = -1;
+  int *d_status = nullptr;  // status, detail
+};
+
+namespace {
+
+bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+constexpr int64_t kMaxTokens = (1ll << 31) - 4096;
+
+int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
+
+// Scratch of one call, cut from the caller's block: every part starts on 256 bytes.
+struct Cursor {
+  uint8_t *base;
+  size_t off = 0;
+  template <typename T>
+  T *take(int64_t n) {
+    T *p = base ? reinterpret_cast<T *>(base + off) : nullptr;
+    off += (size_t)up((int64_t)sizeof(T) * std::max<int64_t>(n, 1), 256);
+    return p;
+  }
+};
+
+struct LossWs {
+  LmRows rows;
+  __nv_bfloat16 *h;       // [rows_pad][hidden] scored rows
+  float *tlogit;          // forward
+  float2 *part;           // forward: [n_part][rows_pad]
+  __nv_bfloat16 *grad;    // backward: [rows_pad][piece]
+  float *dh_part;         // backward: [splits][rows_pad][hidden]
+};
+
+int n_part(const augtree_lm *lm) { return 2 * (int)((lm->vocab + kLmTile - 1) / kLmTile); }
+
+// Columns of a piece of the vocabulary in the backward pass: as many as fit the scratch bound for G, in equal pieces.
+// With the default bound a piece has 4096 columns at least, so that the additions into dH's partial sums, one per
+// piece, stay a small part of the piece's products however many rows there are.
+int64_t piece_cols(const augtree_lm *lm, int64_t rows_pad) {
+  const int64_t bound = lm->piece_bytes > 0 ? lm->piece_bytes : (int64_t)512 << 20, least = lm->piece_bytes > 0 ? kLmTile : 4096;
+  const int64_t cols = std::max<int64_t>(bound / (rows_pad * 2) / kLmTile * kLmTile, least);
+  const int64_t pieces = (lm->vocab + cols - 1) / cols;
+  return up((lm->vocab + pieces - 1) / pieces, kLmTile);
+}
+
+// Shares of dH's contraction: dH has few tiles when there are few rows, and a share should be a small part of what a
+// CTA does in the launch (which holds dW's tiles too), or the longest one would be waited for.
+int dh_splits(const augtree_lm *lm, int64_t rows_pad, int64_t cols) {
+  const int64_t kb = (cols + 63) / 64, tiles = (rows_pad / 128) * ((lm->hidden + kLmTile - 1) / kLmTile);
+  const int64_t lane_kb = std::max<int64_t>(2 * tiles * kb / lm->n_lanes, 1);  // dW costs as much as dH
+  return (int)std::min<int64_t>(std::min<int64_t>((4 * kb + lane_kb - 1) / lane_kb, 64), kb);
+}
+
+size_t loss_layout(const augtree_lm *lm, int64_t tokens, bool bwd, uint8_t *base, LossWs *w) {
+  const int64_t rp = up(std::max<int64_t>(tokens, 1), 256);
+  Cursor c{base};
+  w->rows.n_rows = c.take<int>(1);
+  w->rows.idx = c.take<int>(rp);
+  w->rows.pos = c.take<int>(rp);
+  w->rows.target = c.take<int>(rp);
+  w->h = c.take<__nv_bfloat16>(rp * lm->hidden);
+  if (!bwd) {
+    w->rows.lse2 = w->rows.gscale = nullptr;
+    w->tlogit = c.take<float>(rp);
+    w->part = c.take<float2>((int64_t)n_part(lm) * rp);
+  } else {
+    const int64_t cols = piece_cols(lm, rp);
+    w->rows.lse2 = c.take<float>(rp);
+    w->rows.gscale = c.take<float>(rp);
+    w->grad = c.take<__nv_bfloat16>(rp * cols);
+    w->dh_part = c.take<float>((int64_t)dh_splits(lm, rp, cols) * rp * lm->hidden);
+  }
+  return c.off;
+}
+
+struct EmbedWs {
+  uint32_t *key[2];
+  int *val[2];
+  int *hist, *total, *start;
+};
+
+size_t embed_layout(const augtree_lm *lm, int64_t tokens, uint8_t *base, EmbedWs *w) {
+  const int64_t n = std::max<int64_t>(tokens, 1), blocks = (n + kSortBlock - 1) / kSortBlock;
+  Cursor c{base};
+  for (int i = 0; i < 2; ++i) { w->key[i] = c.take<uint32_t>(n); w->val[i] = c.take<int>(n); }
+  w->hist = c.take<int>(blocks * kSortBins);
+  w->total = c.take<int>(kSortBins);
+  w->start = c.take<int>((int64_t)lm->vocab + 1);
+  return c.off;
+}
+
+// 2-D map over a row-major bf16 matrix: a box is 64 columns (128 bytes, swizzled) x `box_rows` rows; what lies outside
+// reads as zero.  Box origins are multiples of 64 columns, so every copy starts on a 16-byte boundary.
+int map_2d(CUtensorMap *m, const void *ptr, int64_t rows, int64_t cols, int box_rows) {
+  EncodeTiledFn enc = get_encode();
+  if (!enc) return AUGTREE_ERR_CUDA;
+  const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+  const cuuint64_t strides[1] = {(cuuint64_t)cols * 2};
+  const cuuint32_t box[2] = {64, (cuuint32_t)box_rows};
+  const cuuint32_t estr[2] = {1, 1};
+  const CUresult r = enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(ptr), dims, strides, box, estr,
+                         CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? AUGTREE_OK : AUGTREE_ERR_CUDA;
+}
+
+int check_lm(const augtree_lm *lm) {
+  if (!lm || lm->device < 0) return AUGTREE_ERR_INVALID_ARG;
+  int cur = -1;
+  if (cudaGetDevice(&cur) != cudaSuccess) return AUGTREE_ERR_CUDA;
+  return cur == lm->device ? AUGTREE_OK : AUGTREE_ERR_INVALID_ARG;
+}
+
+int launched() {
+  ++g_launches;
+  return cudaGetLastError() == cudaSuccess ? AUGTREE_OK : AUGTREE_ERR_CUDA;
+}
+
+int compact(const augtree_lm *lm, const void *targets, int id_bytes, int64_t tokens, const void *hidden, const LossWs &w,
+            const float *lse, const float *d_loss, float *loss_out, float *lse_out, cudaStream_t st) {
+  if (id_bytes == 8)
+    lm_compact_kernel<<<1, 1024, 0, st>>>(static_cast<const long long *>(targets), (int)tokens, lm->vocab, w.rows, lse, d_loss,
+                                          lm->logit_scale, loss_out, lse_out, lm->d_status);
+  else
+    lm_compact_kernel<<<1, 1024, 0, st>>>(static_cast<const int *>(targets), (int)tokens, lm->vocab, w.rows, lse, d_loss,
+                                          lm->logit_scale, loss_out, lse_out, lm->d_status);
+  int r = launched();
+  if (r) return r;
+  const unsigned grid = (unsigned)std::min<int64_t>(up(tokens, 256), 8 * lm->n_lanes);
+  lm_gather_kernel<<<grid, 256, 0, st>>>(static_cast<const uint4 *>(hidden), w.rows.idx, w.rows.n_rows,
+                                         reinterpret_cast<uint4 *>(w.h), lm->hidden / 8);
+  return launched();
+}
+
+LmParams base_params(const augtree_lm *lm, const LossWs &w, int64_t rows_pad) {
+  LmParams p = {};
+  p.n_rows = w.rows.n_rows;
+  p.vocab = lm->vocab; p.hidden = lm->hidden;
+  p.rows_pad = rows_pad;
+  p.scale_log2 = lm->logit_scale * 1.4426950408889634f;
+  p.target = w.rows.target; p.lse2 = w.rows.lse2; p.gscale = w.rows.gscale;
+  p.status = lm->d_status;
+  p.wait_budget = (lm->flags & AUGTREE_FLAG_TEST_SHORT_WAIT) ? kWaitBudgetClocksTest : kWaitBudgetClocks;
+  p.test_flags = (lm->flags & AUGTREE_FLAG_TEST_SKIP_FWD_LOAD) ? TEST_SKIP_FWD_LOAD : 0;
+  return p;
+}
+
+struct Maps { CUtensorMap h, w, g, h_mn, w_mn, g_mn; };
+
+int launch_tiles(const augtree_lm *lm, const Maps &m, const LmParams &p, cudaStream_t st) {
+  lm_tile_kernel<<<lm->n_lanes, kLmThreads, LmSmem::kBytes, st>>>(m.h, m.w, m.g, m.h_mn, m.w_mn, m.g_mn, p);
+  return launched();
+}
+
+template <typename Id, typename In>
+int embed_fwd_out(const augtree_lm *lm, const void *table, const void *ids, int tokens, void *out, int out_dtype, cudaStream_t st) {
+  const unsigned grid = (unsigned)std::min<int64_t>(tokens, 32ll * lm->n_lanes);
+  const In *tb = static_cast<const In *>(table);
+  const Id *id = static_cast<const Id *>(ids);
+  if (out_dtype == AUGTREE_BF16)
+    embed_fwd_kernel<<<grid, 128, 0, st>>>(tb, id, tokens, lm->vocab, lm->hidden, lm->embed_scale, static_cast<__nv_bfloat16 *>(out), lm->d_status);
+  else if (out_dtype == AUGTREE_F16)
+    embed_fwd_kernel<<<grid, 128, 0, st>>>(tb, id, tokens, lm->vocab, lm->hidden, lm->embed_scale, static_cast<__half *>(out), lm->d_status);
+  else
+    embed_fwd_kernel<<<grid, 128, 0, st>>>(tb, id, tokens, lm->vocab, lm->hidden, lm->embed_scale, static_cast<float *>(out), lm->d_status);
+  return launched();
+}
+
+template <typename Id>
+int embed_fwd_in(const augtree_lm *lm, const void *table, int table_dtype, const void *ids, int tokens, void *out, int out_dtype, cudaStream_t st) {
+  if (table_dtype == AUGTREE_BF16) return embed_fwd_out<Id, __nv_bfloat16>(lm, table, ids, tokens, out, out_dtype, st);
+  if (table_dtype == AUGTREE_F16) return embed_fwd_out<Id, __half>(lm, table, ids, tokens, out, out_dtype, st);
+  return embed_fwd_out<Id, float>(lm, table, ids, tokens, out, out_dtype, st);
+}
+
+template <typename In>
+int embed_sum(const augtree_lm *lm, const void *d_out, const EmbedWs &w, int src, void *d_table, int dtype, int accumulate, cudaStream_t st) {
+  const unsigned grid = (unsigned)std::min<int64_t>(lm->vocab, 1 << 20);
+  const In *d = static_cast<const In *>(d_out);
+  if (dtype == AUGTREE_BF16)
+    embed_sum_kernel<<<grid, 128, 0, st>>>(d, w.val[src], w.start, lm->vocab, lm->hidden, lm->embed_scale, accumulate, static_cast<__nv_bfloat16 *>(d_table));
+  else if (dtype == AUGTREE_F16)
+    embed_sum_kernel<<<grid, 128, 0, st>>>(d, w.val[src], w.start, lm->vocab, lm->hidden, lm->embed_scale, accumulate, static_cast<__half *>(d_table));
+  else
+    embed_sum_kernel<<<grid, 128, 0, st>>>(d, w.val[src], w.start, lm->vocab, lm->hidden, lm->embed_scale, accumulate, static_cast<float *>(d_table));
+  return launched();
+}
+
+bool dtype_ok(int t) { return t == AUGTREE_BF16 || t == AUGTREE_F16 || t == AUGTREE_F32; }
+
+}  // namespace
+
+extern "C" {
+
+int augtree_lm_create(const augtree_lm_desc_t *desc, int device, augtree_lm_t **out) {
+  if (!out) return AUGTREE_ERR_INVALID_ARG;
+  *out = nullptr;
+  if (!desc || desc->struct_size != sizeof(augtree_lm_desc_t) || desc->version != AUGTREE_VERSION) return AUGTREE_ERR_INVALID_ARG;
+  if (desc->vocab < 1 || desc->hidden < 1 || desc->n_lanes < 0 || desc->piece_bytes < 0) return AUGTREE_ERR_INVALID_ARG;
+  if (!(desc->embed_scale - desc->embed_scale == 0.f) || !(desc->logit_scale - desc->logit_scale == 0.f)) return AUGTREE_ERR_INVALID_ARG;
+  if (desc->hidden % 8 != 0 || desc->hidden > (1 << 20) || desc->vocab > (1 << 27)) return AUGTREE_ERR_UNSUPPORTED;
+  if (device < 0 && desc->n_lanes < 1) return AUGTREE_ERR_INVALID_ARG;
+  augtree_lm *lm = new (std::nothrow) augtree_lm();
+  if (!lm) return AUGTREE_ERR_INTERNAL;
+  lm->vocab = desc->vocab; lm->hidden = desc->hidden; lm->flags = desc->flags; lm->n_lanes = desc->n_lanes;
+  lm->embed_scale = desc->embed_scale == 0.f ? 1.f : desc->embed_scale;
+  lm->logit_scale = desc->logit_scale == 0.f ? 1.f : desc->logit_scale;
+  lm->piece_bytes = desc->piece_bytes;
+  lm->device = device;
+  int r = AUGTREE_OK;
+  if (device >= 0) {
+    int prev = 0;
+    cudaGetDevice(&prev);
+    if (cudaSetDevice(device) != cudaSuccess) r = AUGTREE_ERR_CUDA;
+    if (!r) {
+      int sms = 0;
+      if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess || sms < 1) r = AUGTREE_ERR_CUDA;
+      else if (lm->n_lanes == 0) lm->n_lanes = sms;
+    }
+    if (!r && cudaFuncSetAttribute(lm_tile_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, LmSmem::kBytes) != cudaSuccess) r = AUGTREE_ERR_CUDA;
+    if (!r && (cudaMalloc(&lm->d_status, 2 * sizeof(int)) != cudaSuccess || cudaMemset(lm->d_status, 0, 2 * sizeof(int)) != cudaSuccess)) r = AUGTREE_ERR_CUDA;
+    cudaSetDevice(prev);
+  }
+  if (r) { augtree_lm_destroy(lm); return r; }
+  *out = lm;
+  return AUGTREE_OK;
+}
+
+int augtree_lm_destroy(augtree_lm_t *lm) {
+  if (!lm) return AUGTREE_ERR_INVALID_ARG;
+  if (lm->device >= 0) {
+    int prev = 0;
+    cudaGetDevice(&prev);
+    cudaSetDevice(lm->device);
+    cudaFree(lm->d_status);
+    cudaSetDevice(prev);
+  }
+  delete lm;
+  return AUGTREE_OK;
+}
+
+int augtree_lm_workspace_bytes(const augtree_lm_t *lm, int64_t n_tokens, size_t *loss_fwd, size_t *loss_bwd, size_t *embed_bwd) {
+  if (!lm || n_tokens < 0) return AUGTREE_ERR_INVALID_ARG;
+  if (n_tokens > kMaxTokens) return AUGTREE_ERR_UNSUPPORTED;
+  LossWs l;
+  EmbedWs e;
+  if (loss_fwd) *loss_fwd = loss_layout(lm, n_tokens, false, nullptr, &l);
+  if (loss_bwd) *loss_bwd = loss_layout(lm, n_tokens, true, nullptr, &l);
+  if (embed_bwd) *embed_bwd = embed_layout(lm, n_tokens, nullptr, &e);
+  return AUGTREE_OK;
+}
+
+int augtree_embed_fwd(const augtree_lm_t *lm, const void *table, int table_dtype, const void *ids, int id_bytes, int64_t n_tokens,
+                      void *out, int out_dtype, void *stream) {
+  int r = check_lm(lm);
+  if (r) return r;
+  if (n_tokens < 0 || (id_bytes != 4 && id_bytes != 8) || !dtype_ok(table_dtype) || !dtype_ok(out_dtype)) return AUGTREE_ERR_INVALID_ARG;
+  if (n_tokens > kMaxTokens) return AUGTREE_ERR_UNSUPPORTED;
+  if (n_tokens == 0) return AUGTREE_OK;
+  if (!table || !ids || !out || !aligned16(table) || !aligned16(out)) return AUGTREE_ERR_INVALID_ARG;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  return id_bytes == 8 ? embed_fwd_in<long long>(lm, table, table_dtype, ids, (int)n_tokens, out, out_dtype, st)
+                       : embed_fwd_in<int>(lm, table, table_dtype, ids, (int)n_tokens, out, out_dtype, st);
+}
+
+int augtree_embed_bwd(const augtree_lm_t *lm, const void *d_out, int out_dtype, const void *ids, int id_bytes, int64_t n_tokens,
+                      void *d_table, int table_dtype, int accumulate, void *ws, size_t ws_bytes, void *stream) {
+  int r = check_lm(lm);
+  if (r) return r;
+  if (n_tokens < 0 || (id_bytes != 4 && id_bytes != 8) || !dtype_ok(table_dtype) || !dtype_ok(out_dtype)) return AUGTREE_ERR_INVALID_ARG;
+  if (n_tokens > kMaxTokens || (accumulate && table_dtype != AUGTREE_F32)) return AUGTREE_ERR_UNSUPPORTED;
+  if (!d_table || !aligned16(d_table) || (n_tokens > 0 && (!d_out || !ids || !aligned16(d_out)))) return AUGTREE_ERR_INVALID_ARG;
+  EmbedWs w;
+  if (!ws || !aligned16(ws) || ws_bytes < embed_layout(lm, n_tokens, static_cast<uint8_t *>(ws), &w)) return AUGTREE_ERR_WORKSPACE;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const int n = (int)n_tokens, n_blocks = (n + kSortBlock - 1) / kSortBlock;
+  int src = 0;
+  if (n > 0) {
+    const unsigned g = (unsigned)((n + 255) / 256);
+    if (id_bytes == 8) embed_keys_kernel<<<g, 256, 0, st>>>(static_cast<const long long *>(ids), n, lm->vocab, w.key[0], w.val[0], lm->d_status);
+    else embed_keys_kernel<<<g, 256, 0, st>>>(static_cast<const int *>(ids), n, lm->vocab, w.key[0], w.val[0], lm->d_status);
+    if ((r = launched())) return r;
+    int key_bits = 1;
+    while ((lm->vocab >> key_bits) != 0) ++key_bits;
+    const int passes = (key_bits + 8) / 9, bits = (key_bits + passes - 1) / passes;
+    for (int i = 0; i < passes; ++i, src ^= 1) {
+      embed_hist_kernel<<<n_blocks, 512, 0, st>>>(w.key[src], n, i * bits, bits, w.hist, n_blocks);
+      if ((r = launched())) return r;
+      embed_scan_kernel<<<((1 << bits) + 7) / 8, 256, 0, st>>>(w.hist, n_blocks, 1 << bits, w.total);
+      if ((r = launched())) return r;
+      embed_scatter_kernel<<<n_blocks, 512, 0, st>>>(w.key[src], w.val[src], n, i * bits, bits, w.hist, n_blocks, w.total, w.key[src ^ 1], w.val[src ^ 1]);
+      if ((r = launched())) return r;
+    }
+  }
+  embed_starts_kernel<<<(unsigned)(lm->vocab / 256 + 1), 256, 0, st>>>(w.key[src], n, lm->vocab, w.start);
+  if ((r = launched())) return r;
+  if (out_dtype == AUGTREE_BF16) return embed_sum<__nv_bfloat16>(lm, d_out, w, src, d_table, table_dtype, accumulate, st);
+  if (out_dtype == AUGTREE_F16) return embed_sum<__half>(lm, d_out, w, src, d_table, table_dtype, accumulate, st);
+  return embed_sum<float>(lm, d_out, w, src, d_table, table_dtype, accumulate, st);
+}
+
+int augtree_lm_loss_fwd(const augtree_lm_t *lm, const void *hidden, const void *weight, const void *targets, int id_bytes,
+                        int64_t n_tokens, float *loss, float *lse, void *ws, size_t ws_bytes, void *stream) {
+  int r = check_lm(lm);
+  if (r) return r;
+  if (n_tokens < 0 || (id_bytes != 4 && id_bytes != 8)) return AUGTREE_ERR_INVALID_ARG;
+  if (n_tokens > kMaxTokens) return AUGTREE_ERR_UNSUPPORTED;
+  if (n_tokens == 0) return AUGTREE_OK;
+  if (!hidden || !weight || !targets || !loss || !lse || !aligned16(hidden) || !aligned16(weight)) return AUGTREE_ERR_INVALID_ARG;
+  LossWs w;
+  if (!ws || !aligned16(ws) || ws_bytes < loss_layout(lm, n_tokens, false, static_cast<uint8_t *>(ws), &w)) return AUGTREE_ERR_WORKSPACE;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const int64_t rp = up(n_tokens, 256);
+  if ((r = compact(lm, targets, id_bytes, n_tokens, hidden, w, nullptr, nullptr, loss, lse, st))) return r;
+  Maps m = {};
+  if ((r = map_2d(&m.h, w.h, rp, lm->hidden, 128)) || (r = map_2d(&m.w, weight, lm->vocab, lm->hidden, 128))) return r;
+  LmParams p = base_params(lm, w, rp);
+  p.n_jobs = 1;
+  p.job[0] = {LM_STATS, 0, lm->vocab, lm->hidden, 1};
+  p.part = w.part; p.tlogit = w.tlogit;
+  if ((r = launch_tiles(lm, m, p, st))) return r;
+  const unsigned grid = (unsigned)std::min<int64_t>((n_tokens + 31) / 32, 8 * lm->n_lanes);
+  lm_finish_kernel<<<grid, 256, 0, st>>>(w.part, n_part(lm), rp, w.rows.n_rows, w.rows.idx, w.tlogit, lm->logit_scale, loss, lse);
+  return launched();
+}
+
+int augtree_lm_loss_bwd(const augtree_lm_t *lm, const void *hidden, const void *weight, const void *targets, int id_bytes,
+                        const float *lse, const float *d_loss, int64_t n_tokens, void *d_hidden, void *d_weight,
+                        int weight_dtype, int accumulate, void *ws, size_t ws_bytes, void *stream) {
+  int r = check_lm(lm);
+  if (r) return r;
+  if (n_tokens < 0 || (id_bytes != 4 && id_bytes != 8)) return AUGTREE_ERR_INVALID_ARG;
+  if (d_weight && weight_dtype != AUGTREE_BF16 && weight_dtype != AUGTREE_F32) return AUGTREE_ERR_INVALID_ARG;
+  if (n_tokens > kMaxTokens || (d_weight && accumulate && weight_dtype != AUGTREE_F32)) return AUGTREE_ERR_UNSUPPORTED;
+  if (!aligned16(d_hidden) || !aligned16(d_weight)) return AUGTREE_ERR_INVALID_ARG;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (n_tokens == 0) {
+    if (d_weight && !accumulate &&
+        cudaMemsetAsync(d_weight, 0, (size_t)lm->vocab * lm->hidden * (weight_dtype == AUGTREE_F32 ? 4 : 2), st) != cudaSuccess)
+      return AUGTREE_ERR_CUDA;
+    return AUGTREE_OK;
+  }
+  if (!hidden || !weight || !targets || !lse || !d_loss || !aligned16(hidden) || !aligned16(weight)) return AUGTREE_ERR_INVALID_ARG;
+  LossWs w;
+  if (!ws || !aligned16(ws) || ws_bytes < loss_layout(lm, n_tokens, true, static_cast<uint8_t *>(ws), &w)) return AUGTREE_ERR_WORKSPACE;
+  if (!d_hidden && !d_weight) return AUGTREE_OK;
+  const int64_t rp = up(n_tokens, 256), cols = piece_cols(lm, rp);
+  const int splits = dh_splits(lm, rp, cols);
+  if ((r = compact(lm, targets, id_bytes, n_tokens, hidden, w, lse, d_loss, nullptr, nullptr, st))) return r;
+  Maps m = {};
+  if ((r = map_2d(&m.h, w.h, rp, lm->hidden, 128)) || (r = map_2d(&m.w, weight, lm->vocab, lm->hidden, 128)) ||
+      (r = map_2d(&m.h_mn, w.h, rp, lm->hidden, 64)) || (r = map_2d(&m.w_mn, weight, lm->vocab, lm->hidden, 64)) ||
+      (r = map_2d(&m.g, w.grad, rp, cols, 128)) || (r = map_2d(&m.g_mn, w.grad, rp, cols, 64)))
+    return r;
+  LmParams p = base_params(lm, w, rp);
+  p.grad = w.grad; p.ld_grad = cols; p.dh_part = w.dh_part;
+  p.dw = d_weight; p.dw_f32 = weight_dtype == AUGTREE_F32; p.dw_add = accumulate;
+  for (int64_t v0 = 0; v0 < lm->vocab; v0 += cols) {
+    const int n = (int)std::min<int64_t>(cols, lm->vocab - v0);
+    p.v0 = (int)v0;
+    p.n_jobs = 1;
+    p.job[0] = {LM_GRAD, 0, n, lm->hidden, 1};
+    if ((r = launch_tiles(lm, m, p, st))) return r;
+    p.n_jobs = 0;
+    p.dh_add = v0 > 0;
+    if (d_hidden) p.job[p.n_jobs++] = {LM_DH, 0, lm->hidden, n, splits};
+    if (d_weight) p.job[p.n_jobs++] = {LM_DW, n, lm->hidden, 0, 1};
+    if ((r = launch_tiles(lm, m, p, st))) return r;
+  }
+  if (d_hidden) {
+    const unsigned grid = (unsigned)std::min<int64_t>(n_tokens, 16 * lm->n_lanes);
+    lm_dh_kernel<<<grid, 256, 0, st>>>(w.dh_part, splits, rp, lm->hidden, w.rows.pos, (int)n_tokens, static_cast<__nv_bfloat16 *>(d_hidden));
+    return launched();
+  }
+  return AUGTREE_OK;
+}
+
+int augtree_lm_last_device_status(const augtree_lm_t *lm, int *status, int *detail) {
+  if (!lm || lm->device < 0 || !status) return AUGTREE_ERR_INVALID_ARG;
+  int prev = 0;
+  cudaGetDevice(&prev);
+  cudaSetDevice(lm->device);
+  int h[2] = {0, 0};
+  cudaError_t e = cudaDeviceSynchronize();
+  if (e == cudaSuccess) e = cudaMemcpy(h, lm->d_status, sizeof(h), cudaMemcpyDeviceToHost);
+  if (e == cudaSuccess && (h[0] || h[1])) e = cudaMemset(lm->d_status, 0, sizeof(h));
+  cudaSetDevice(prev);
+  if (e != cudaSuccess) return AUGTREE_ERR_CUDA;
+  *status = h[0];
+  if (detail) *detail = h[1];
+  return AUGTREE_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,345 @@
+// Element-wise kernels around the vocabulary loss, and the embedding lookup with its gradient.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "ptx.cuh"
+
+namespace augtree {
+
+// ---------------------------------------------------------------- compaction of the scored rows
+// Rows with a negative target are not scored.  They are left out of every product: their hidden states may hold
+// anything, NaN included, and 0 x NaN in the contraction of dW would spoil it; and their work is saved.
+// One block walks the targets in order, so the compacted order is that of the tokens.
+struct LmRows {
+  int *n_rows;      // [1]
+  int *idx;         // [rows_pad] compacted row -> token
+  int *pos;         // [tokens] token -> compacted row or -1
+  int *target;      // [rows_pad]
+  float *lse2;      // [rows_pad] backward only
+  float *gscale;    // [rows_pad] backward only
+};
+
+template <typename Id>
+__global__ void __launch_bounds__(1024)
+lm_compact_kernel(const Id *targets, int tokens, int vocab, LmRows o, const float *lse, const float *d_loss, float logit_scale,
+                  float *loss_out, float *lse_out, int *status) {
+  __shared__ int warp_sum[32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int n = 0;
+  for (int t0 = 0; t0 < tokens; t0 += 1024) {
+    const int t = t0 + (int)threadIdx.x;
+    const long long id = t < tokens ? (long long)targets[t] : -1;
+    const bool live = id >= 0 && id < vocab;
+    if (id >= vocab && atomicCAS(status, 0, -1) == 0) status[1] = t;
+    const unsigned m = __ballot_sync(0xffffffffu, live);
+    if (lane == 0) warp_sum[warp] = __popc(m);
+    __syncthreads();
+    if (warp == 0) {
+      int s = warp_sum[lane];
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const int u = __shfl_up_sync(0xffffffffu, s, d);
+        if (lane >= d) s += u;
+      }
+      warp_sum[lane] = s;
+    }
+    __syncthreads();
+    const int r = n + (warp ? warp_sum[warp - 1] : 0) + __popc(m & ((1u << lane) - 1));
+    const int total = warp_sum[31];
+    if (t < tokens) o.pos[t] = live ? r : -1;
+    if (live) {
+      o.idx[r] = t;
+      o.target[r] = (int)id;
+      if (lse) {
+        o.lse2[r] = lse[t] * 1.4426950408889634f;
+        o.gscale[r] = d_loss[t] * logit_scale;
+      }
+    } else if (t < tokens && loss_out) {
+      loss_out[t] = 0.f;
+      lse_out[t] = 0.f;
+    }
+    n += total;
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) *o.n_rows = n;
+}
+
+// Hidden states of the scored rows, packed; zeros up to the next multiple of 256 rows (they enter contractions).
+__global__ void __launch_bounds__(256)
+lm_gather_kernel(const uint4 *hidden, const int *idx, const int *n_rows, uint4 *out, int row_vecs) {
+  const int n = *n_rows, n_pad = (n + 255) / 256 * 256;
+  for (int r = blockIdx.x; r < n_pad; r += gridDim.x) {
+    const uint4 *src = r < n ? hidden + (long long)idx[r] * row_vecs : nullptr;
+    uint4 *dst = out + (long long)r * row_vecs;
+    for (int i = threadIdx.x; i < row_vecs; i += 256) dst[i] = src ? __ldg(src + i) : make_uint4(0, 0, 0, 0);
+  }
+}
+
+// ---------------------------------------------------------------- row statistics
+// lse of a row from its partial (m, l) pairs, merged in a fixed order.  32 rows x 8 shares of the pairs a block.
+__global__ void __launch_bounds__(256)
+lm_finish_kernel(const float2 *part, int n_part, long long rows_pad, const int *n_rows, const int *idx, const float *tlogit,
+                 float logit_scale, float *loss, float *lse) {
+  __shared__ float2 sh[8][32];
+  const int lane = threadIdx.x & 31, seg = threadIdx.x >> 5;
+  const int n = *n_rows;
+  for (int r0 = blockIdx.x * 32; r0 < n; r0 += gridDim.x * 32) {
+    const int r = r0 + lane;
+    float m = -INFINITY, l = 0.f;
+    if (r < n)
+      for (int i = seg; i < n_part; i += 8) {
+        const float2 v = part[(long long)i * rows_pad + r];
+        const float mn = fmaxf(m, v.x), ref = mn == -INFINITY ? 0.f : mn;
+        l = l * ex2(m - ref) + v.y * ex2(v.x - ref);
+        m = mn;
+      }
+    sh[seg][lane] = make_float2(m, l);
+    __syncthreads();
+    if (seg == 0 && r < n) {
+      for (int s = 1; s < 8; ++s) {
+        const float2 v = sh[s][lane];
+        const float mn = fmaxf(m, v.x), ref = mn == -INFINITY ? 0.f : mn;
+        l = l * ex2(m - ref) + v.y * ex2(v.x - ref);
+        m = mn;
+      }
+      const float z = m * 0.6931471805599453f + logf(l);
+      const int t = idx[r];
+      lse[t] = z;
+      loss[t] = z - tlogit[r] * logit_scale;
+    }
+    __syncthreads();
+  }
+}
+
+// dH of every token in bf16: the shares' partial sums added in order; zeros for rows that are not scored.
+__global__ void __launch_bounds__(256)
+lm_dh_kernel(const float *part, int splits, long long rows_pad, int hidden, const int *pos, int tokens, __nv_bfloat16 *d_hidden) {
+  const int vecs = hidden / 8;
+  for (int t = blockIdx.x; t < tokens; t += gridDim.x) {
+    const int r = pos[t];
+    for (int i = threadIdx.x; i < vecs; i += 256) {
+      float x[8] = {};
+      if (r >= 0)
+        for (int s = 0; s < splits; ++s) {
+          const float4 *q = reinterpret_cast<const float4 *>(part + ((long long)s * rows_pad + r) * hidden + i * 8);
+          const float4 a = q[0], b = q[1];
+          x[0] += a.x; x[1] += a.y; x[2] += a.z; x[3] += a.w; x[4] += b.x; x[5] += b.y; x[6] += b.z; x[7] += b.w;
+        }
+      *reinterpret_cast<uint4 *>(d_hidden + (long long)t * hidden + i * 8) =
+          make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+    }
+  }
+}
+
+// ---------------------------------------------------------------- embedding
+template <typename T> struct Vec;  // eight elements
+template <> struct Vec<float> {
+  static __device__ __forceinline__ void load(const float *p, float (&x)[8]) {
+    const float4 a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4);
+    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+  }
+  static __device__ __forceinline__ void store(float *p, const float (&x)[8]) {
+    *reinterpret_cast<float4 *>(p) = make_float4(x[0], x[1], x[2], x[3]);
+    *reinterpret_cast<float4 *>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
+  }
+};
+template <> struct Vec<__nv_bfloat16> {
+  static __device__ __forceinline__ void load(const __nv_bfloat16 *p, float (&x)[8]) {
+    const uint4 v = *reinterpret_cast<const uint4 *>(p);
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(&w[i]));
+      x[2 * i] = f.x; x[2 * i + 1] = f.y;
+    }
+  }
+  static __device__ __forceinline__ void store(__nv_bfloat16 *p, const float (&x)[8]) {
+    *reinterpret_cast<uint4 *>(p) = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+  }
+};
+template <> struct Vec<__half> {
+  static __device__ __forceinline__ void load(const __half *p, float (&x)[8]) {
+    const uint4 v = *reinterpret_cast<const uint4 *>(p);
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&w[i]));
+      x[2 * i] = f.x; x[2 * i + 1] = f.y;
+    }
+  }
+  static __device__ __forceinline__ void store(__half *p, const float (&x)[8]) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const __half2 h = __floats2half2_rn(x[2 * i], x[2 * i + 1]);
+      w[i] = *reinterpret_cast<const uint32_t *>(&h);
+    }
+    *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+};
+
+// out[t] = scale table[id_t]; zeros for a negative id.  The product is rounded once.  HBM-bound: a row read, a row written.
+template <typename Id, typename In, typename Out>
+__global__ void __launch_bounds__(128)
+embed_fwd_kernel(const In *table, const Id *ids, int tokens, int vocab, int hidden, float scale, Out *out, int *status) {
+  for (int t = blockIdx.x; t < tokens; t += gridDim.x) {
+    const long long id = ids[t];
+    const bool live = id >= 0 && id < vocab;
+    if (id >= vocab && threadIdx.x == 0 && atomicCAS(status, 0, -1) == 0) status[1] = t;
+    for (int i = threadIdx.x * 8; i < hidden; i += 1024) {
+      float x[8] = {};
+      if (live) {
+        Vec<In>::load(table + id * hidden + i, x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] *= scale;
+      }
+      Vec<Out>::store(out + (long long)t * hidden + i, x);
+    }
+  }
+}
+
+// ---- tokens sorted by id, stably: least-significant-digit radix passes of at most 9 bits.  Key `vocab` = not embedded.
+constexpr int kSortBlock = 4096;   // keys of one block: 16 warps x 256
+constexpr int kSortBins = 512;
+
+template <typename Id>
+__global__ void embed_keys_kernel(const Id *ids, int tokens, int vocab, uint32_t *key, int *val, int *status) {
+  const int t = blockIdx.x * blockDim.x + threadIdx.x;
+  if (t >= tokens) return;
+  const long long id = ids[t];
+  if (id >= vocab && atomicCAS(status, 0, -1) == 0) status[1] = t;
+  key[t] = id >= 0 && id < vocab ? (uint32_t)id : (uint32_t)vocab;
+  val[t] = t;
+}
+
+__global__ void __launch_bounds__(512)
+embed_hist_kernel(const uint32_t *key, int n, int shift, int bits, int *hist, int n_blocks) {
+  __shared__ int cnt[kSortBins];
+  cnt[threadIdx.x] = 0;
+  __syncthreads();
+  const int b0 = blockIdx.x * kSortBlock;
+  for (int i = threadIdx.x; i < kSortBlock; i += 512)
+    if (b0 + i < n) atomicAdd(&cnt[(key[b0 + i] >> shift) & ((1u << bits) - 1)], 1);  // a count: the order does not matter
+  __syncthreads();
+  if ((int)threadIdx.x < (1 << bits)) hist[(long long)threadIdx.x * n_blocks + blockIdx.x] = cnt[threadIdx.x];
+}
+
+// one warp per bin: exclusive prefix sum over the blocks, total of the bin behind it
+__global__ void __launch_bounds__(256)
+embed_scan_kernel(int *hist, int n_blocks, int bins, int *total) {
+  const int bin = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  if (bin >= bins) return;
+  int run = 0;
+  for (int b = 0; b < n_blocks; b += 32) {
+    const int v = b + lane < n_blocks ? hist[(long long)bin * n_blocks + b + lane] : 0;
+    int s = v;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int u = __shfl_up_sync(0xffffffffu, s, d);
+      if (lane >= d) s += u;
+    }
+    if (b + lane < n_blocks) hist[(long long)bin * n_blocks + b + lane] = run + s - v;
+    run += __shfl_sync(0xffffffffu, s, 31);
+  }
+  if (lane == 0) total[bin] = run;
+}
+
+__global__ void __launch_bounds__(512)
+embed_scatter_kernel(const uint32_t *key, const int *val, int n, int shift, int bits, const int *hist, int n_blocks, const int *total,
+                     uint32_t *key_out, int *val_out) {
+  __shared__ int cnt[16][kSortBins];
+  __shared__ int start[kSortBins];
+  __shared__ int wsum[16];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, bins = 1 << bits;
+  for (int i = threadIdx.x; i < 16 * kSortBins; i += 512) (&cnt[0][0])[i] = 0;
+  // exclusive prefix sum of the bins' totals
+  const int tv = (int)threadIdx.x < bins ? total[threadIdx.x] : 0;
+  int s = tv;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const int u = __shfl_up_sync(0xffffffffu, s, d);
+    if (lane >= d) s += u;
+  }
+  if (lane == 31) wsum[warp] = s;
+  __syncthreads();
+  int before = 0;
+  for (int w = 0; w < warp; ++w) before += wsum[w];
+  if ((int)threadIdx.x < bins) start[threadIdx.x] = before + s - tv + hist[(long long)threadIdx.x * n_blocks + blockIdx.x];
+  __syncthreads();
+  // rank of every key among the warp's earlier keys of the same digit, in order
+  const int w0 = blockIdx.x * kSortBlock + warp * 256;
+  uint32_t k[8];
+  int rank[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const int i = w0 + j * 32 + lane;
+    const bool in = i < n;
+    k[j] = in ? key[i] : 0;
+    const int d = in ? (int)((k[j] >> shift) & (bins - 1)) : -1;
+    const unsigned same = __match_any_sync(0xffffffffu, d);
+    const int first = __ffs(same) - 1;
+    int c = 0;
+    if (in && lane == first) { c = cnt[warp][d]; cnt[warp][d] = c + __popc(same); }
+    __syncwarp();
+    rank[j] = __shfl_sync(0xffffffffu, c, first) + __popc(same & ((1u << lane) - 1));
+  }
+  __syncthreads();
+  if ((int)threadIdx.x < bins) {
+    int run = start[threadIdx.x];
+    for (int w = 0; w < 16; ++w) { const int v = cnt[w][threadIdx.x]; cnt[w][threadIdx.x] = run; run += v; }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const int i = w0 + j * 32 + lane;
+    if (i < n) {
+      const int to = cnt[warp][(k[j] >> shift) & (bins - 1)] + rank[j];
+      key_out[to] = k[j];
+      val_out[to] = val[i];
+    }
+  }
+}
+
+// first sorted place of every id (ids 0 .. vocab; the last is the end of the embedded tokens)
+__global__ void embed_starts_kernel(const uint32_t *key, int n, int vocab, int *start) {
+  const int v = blockIdx.x * blockDim.x + threadIdx.x;
+  if (v > vocab) return;
+  int lo = 0, hi = n;
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (key[mid] < (uint32_t)v) lo = mid + 1; else hi = mid;
+  }
+  start[v] = lo;
+}
+
+// d_table[v] (+)= scale sum of d_out over the tokens of v, in the order of the tokens, in fp32, rounded once
+template <typename In, typename Out>
+__global__ void __launch_bounds__(128)
+embed_sum_kernel(const In *d_out, const int *val, const int *start, int vocab, int hidden, float scale, int accumulate, Out *d_table) {
+  for (int v = blockIdx.x; v < vocab; v += gridDim.x) {
+    const int a = start[v], b = start[v + 1];
+    if (a == b && accumulate) continue;
+    for (int i = threadIdx.x * 8; i < hidden; i += 1024) {
+      float x[8] = {};
+      for (int j = a; j < b; ++j) {
+        float y[8];
+        Vec<In>::load(d_out + (long long)val[j] * hidden + i, y);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] += y[e];
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] *= scale;
+      Out *dst = d_table + (long long)v * hidden + i;
+      if (accumulate) {
+        float y[8];
+        Vec<Out>::load(dst, y);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] += y[e];
+      }
+      Vec<Out>::store(dst, x);
+    }
+  }
+}
+
+}  // namespace augtree

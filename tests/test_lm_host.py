@@ -1,0 +1,61 @@
+"""Host side of the vocabulary operators: descriptor checks and workspace sizes, no GPU."""
+import ctypes as C
+
+import pytest
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_2609_33133_b200 import build
+    build.build()
+    from paper_2609_33133_b200 import binding
+    return binding
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(vocab=0, hidden=64), -1), (dict(vocab=10, hidden=0), -1), (dict(vocab=10, hidden=-8), -1), (dict(vocab=10, hidden=60), -2),
+    (dict(vocab=10, hidden=64, n_lanes=0), -1), (dict(vocab=10, hidden=64, n_lanes=-1), -1), (dict(vocab=10, hidden=64, piece_bytes=-1), -1),
+    (dict(vocab=10, hidden=64, embed_scale=float("nan")), -1), (dict(vocab=10, hidden=64, logit_scale=float("inf")), -1),
+    (dict(vocab=(1 << 27) + 1, hidden=64), -2), (dict(vocab=10, hidden=(1 << 20) + 8), -2)])
+def test_descriptor_checks(B, kw, code):
+    with pytest.raises(B.AugtreeError) as e:
+        B.LM(**{"device": None, "n_lanes": 148, **kw})
+    assert e.value.code == code
+
+
+def test_bad_pointers_and_struct(B):
+    h = C.c_void_p()
+    assert B.lib.augtree_lm_create(None, -1, C.byref(h)) == -1 and not h.value
+    d = B.LmDescC(4, 1, 10, 64, 0.0, 0.0, 0, 148, 0)
+    assert B.lib.augtree_lm_create(C.byref(d), -1, C.byref(h)) == -1 and not h.value
+    d = B.LmDescC(C.sizeof(B.LmDescC), 99, 10, 64, 0.0, 0.0, 0, 148, 0)
+    assert B.lib.augtree_lm_create(C.byref(d), -1, C.byref(h)) == -1 and not h.value
+    assert B.lib.augtree_lm_destroy(None) == -1
+    lm = B.LM(10, 64, device=None, n_lanes=148)
+    n = C.c_size_t()
+    assert B.lib.augtree_lm_workspace_bytes(lm._h, -1, C.byref(n), None, None) == -1
+    assert B.lib.augtree_lm_workspace_bytes(lm._h, 1 << 31, C.byref(n), None, None) == -2
+    # launches on a host-only handle are refused before anything is touched
+    assert B.lib.augtree_embed_fwd(lm._h, None, 0, None, 8, 1, None, 0, None) == -1
+    assert B.lib.augtree_embed_bwd(lm._h, None, 0, None, 8, 1, None, 0, 0, None, 0, None) == -1
+    assert B.lib.augtree_lm_loss_fwd(lm._h, None, None, None, 8, 1, None, None, None, 0, None) == -1
+    assert B.lib.augtree_lm_loss_bwd(lm._h, None, None, None, 8, None, None, 1, None, None, 0, 0, None, 0, None) == -1
+    s = C.c_int()
+    assert B.lib.augtree_lm_last_device_status(lm._h, C.byref(s), None) == -1
+
+
+def test_workspace_stays_far_below_the_logits(B):
+    """The point of the operator: at 16384 rows x 152064 words the logits alone would be 10 GB in fp32."""
+    lm = B.LM(152064, 3584, device=None, n_lanes=148)
+    fwd, bwd, emb = lm.workspace_parts(16384)
+    assert fwd < 0.05 * 16384 * 152064 * 4 and bwd < 0.2 * 16384 * 152064 * 4
+    assert lm.workspace_bytes(16384) == max(fwd, bwd, emb)
+    assert lm.workspace_bytes(0) > 0
+
+
+def test_workspace_grows_with_the_piece_bound(B):
+    small = B.LM(50000, 512, device=None, n_lanes=148, piece_bytes=1).workspace_parts(4096)[1]
+    large = B.LM(50000, 512, device=None, n_lanes=148, piece_bytes=256 << 20).workspace_parts(4096)[1]
+    assert small < large <= small + (256 << 20) + (64 << 20) * 64
+    # sizes beyond 32 bits do not wrap
+    assert B.LM(152064, 8192, device=None, n_lanes=148).workspace_parts(2_000_000)[1] > 2_000_000 * 8192 * 2
