@@ -95,8 +95,18 @@ size_t loss_layout(const augtree_lm *lm, int64_t tokens, bool bwd, uint8_t *base
 struct EmbedWs {
   uint32_t *key[2];
   int *val[2];
-  int *hist, *total, *start;
+  int *hist, *total;
+  float *part;   // [2 x chunks][hidden] sums of the rows that cross from chunk to chunk
+  int chunk, n_chunks;
 };
+
+// Sorted tokens of a chunk: short ones, so that a few thousand tokens fill the GPU, longer ones when there are enough
+// blocks anyway (the crossing rows' sums cost a write and a read of their own).
+int embed_chunk(const augtree_lm *lm, int64_t n) {
+  int chunk = 16;
+  while (chunk < kEmbedMaxChunk && n / chunk > 32ll * lm->n_lanes) chunk *= 2;
+  return chunk;
+}
 
 size_t embed_layout(const augtree_lm *lm, int64_t tokens, uint8_t *base, EmbedWs *w) {
   const int64_t n = std::max<int64_t>(tokens, 1), blocks = (n + kSortBlock - 1) / kSortBlock;
@@ -104,7 +114,9 @@ size_t embed_layout(const augtree_lm *lm, int64_t tokens, uint8_t *base, EmbedWs
   for (int i = 0; i < 2; ++i) { w->key[i] = c.take<uint32_t>(n); w->val[i] = c.take<int>(n); }
   w->hist = c.take<int>(blocks * kSortBins);
   w->total = c.take<int>(kSortBins);
-  w->start = c.take<int>((int64_t)lm->vocab + 1);
+  w->chunk = embed_chunk(lm, n);
+  w->n_chunks = (int)((tokens + w->chunk - 1) / w->chunk);
+  w->part = c.take<float>(2ll * w->n_chunks * lm->hidden);
   return c.off;
 }
 
@@ -192,17 +204,25 @@ int embed_fwd_in(const augtree_lm *lm, const void *table, int table_dtype, const
   return embed_fwd_out<Id, float>(lm, table, ids, tokens, out, out_dtype, st);
 }
 
-template <typename In>
-int embed_sum(const augtree_lm *lm, const void *d_out, const EmbedWs &w, int src, void *d_table, int dtype, int accumulate, cudaStream_t st) {
-  const unsigned grid = (unsigned)std::min<int64_t>(lm->vocab, 1 << 20);
-  const In *d = static_cast<const In *>(d_out);
-  if (dtype == AUGTREE_BF16)
-    embed_sum_kernel<<<grid, 128, 0, st>>>(d, w.val[src], w.start, lm->vocab, lm->hidden, lm->embed_scale, accumulate, static_cast<__nv_bfloat16 *>(d_table));
-  else if (dtype == AUGTREE_F16)
-    embed_sum_kernel<<<grid, 128, 0, st>>>(d, w.val[src], w.start, lm->vocab, lm->hidden, lm->embed_scale, accumulate, static_cast<__half *>(d_table));
-  else
-    embed_sum_kernel<<<grid, 128, 0, st>>>(d, w.val[src], w.start, lm->vocab, lm->hidden, lm->embed_scale, accumulate, static_cast<float *>(d_table));
+template <typename In, typename Out>
+int embed_sum_out(const augtree_lm *lm, const void *d_out, const EmbedWs &w, int src, int n, void *d_table, int accumulate, cudaStream_t st) {
+  const unsigned zero_blocks = accumulate ? 0u : (unsigned)((lm->vocab + kEmbedZeroRows - 1) / kEmbedZeroRows);
+  Out *dt = static_cast<Out *>(d_table);
+  if (w.n_chunks + zero_blocks == 0) return AUGTREE_OK;
+  embed_sum_kernel<<<dim3(w.n_chunks + zero_blocks, (lm->hidden + kEmbedCols - 1) / kEmbedCols), kEmbedThreads, 0, st>>>(
+      static_cast<const In *>(d_out), w.key[src], w.val[src], n, w.chunk, w.n_chunks, lm->vocab, lm->hidden, lm->embed_scale, accumulate, dt, w.part);
+  int r = launched();
+  if (r || w.n_chunks < 2) return r;
+  embed_join_kernel<<<dim3(w.n_chunks - 1, (lm->hidden + 255) / 256), 256, 0, st>>>(w.key[src], n, w.chunk, w.n_chunks, lm->vocab,
+                                                                                  lm->hidden, lm->embed_scale, accumulate, dt, w.part);
   return launched();
+}
+
+template <typename In>
+int embed_sum(const augtree_lm *lm, const void *d_out, const EmbedWs &w, int src, int n, void *d_table, int dtype, int accumulate, cudaStream_t st) {
+  if (dtype == AUGTREE_BF16) return embed_sum_out<In, __nv_bfloat16>(lm, d_out, w, src, n, d_table, accumulate, st);
+  if (dtype == AUGTREE_F16) return embed_sum_out<In, __half>(lm, d_out, w, src, n, d_table, accumulate, st);
+  return embed_sum_out<In, float>(lm, d_out, w, src, n, d_table, accumulate, st);
 }
 
 bool dtype_ok(int t) { return t == AUGTREE_BF16 || t == AUGTREE_F16 || t == AUGTREE_F32; }
@@ -237,6 +257,9 @@ int augtree_lm_create(const augtree_lm_desc_t *desc, int device, augtree_lm_t **
       else if (lm->n_lanes == 0) lm->n_lanes = sms;
     }
     if (!r && cudaFuncSetAttribute(lm_tile_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, LmSmem::kBytes) != cudaSuccess) r = AUGTREE_ERR_CUDA;
+    if (!r && (cudaFuncSetAttribute(embed_sort_small_kernel<int>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSortSmallBytes) != cudaSuccess ||
+               cudaFuncSetAttribute(embed_sort_small_kernel<long long>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSortSmallBytes) != cudaSuccess))
+      r = AUGTREE_ERR_CUDA;
     if (!r && (cudaMalloc(&lm->d_status, 2 * sizeof(int)) != cudaSuccess || cudaMemset(lm->d_status, 0, 2 * sizeof(int)) != cudaSuccess)) r = AUGTREE_ERR_CUDA;
     cudaSetDevice(prev);
   }
@@ -293,15 +316,19 @@ int augtree_embed_bwd(const augtree_lm_t *lm, const void *d_out, int out_dtype, 
   if (!ws || !aligned16(ws) || ws_bytes < embed_layout(lm, n_tokens, static_cast<uint8_t *>(ws), &w)) return AUGTREE_ERR_WORKSPACE;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const int n = (int)n_tokens, n_blocks = (n + kSortBlock - 1) / kSortBlock;
+  int key_bits = 1;
+  while ((lm->vocab >> key_bits) != 0) ++key_bits;
+  const int passes = (key_bits + 8) / 9, bits = (key_bits + passes - 1) / passes;
   int src = 0;
-  if (n > 0) {
+  if (n > 0 && n <= kSortBlock) {
+    if (id_bytes == 8) embed_sort_small_kernel<<<1, 512, kSortSmallBytes, st>>>(static_cast<const long long *>(ids), n, lm->vocab, passes, bits, w.key[0], w.val[0], lm->d_status);
+    else embed_sort_small_kernel<<<1, 512, kSortSmallBytes, st>>>(static_cast<const int *>(ids), n, lm->vocab, passes, bits, w.key[0], w.val[0], lm->d_status);
+    if ((r = launched())) return r;
+  } else if (n > 0) {
     const unsigned g = (unsigned)((n + 255) / 256);
     if (id_bytes == 8) embed_keys_kernel<<<g, 256, 0, st>>>(static_cast<const long long *>(ids), n, lm->vocab, w.key[0], w.val[0], lm->d_status);
     else embed_keys_kernel<<<g, 256, 0, st>>>(static_cast<const int *>(ids), n, lm->vocab, w.key[0], w.val[0], lm->d_status);
     if ((r = launched())) return r;
-    int key_bits = 1;
-    while ((lm->vocab >> key_bits) != 0) ++key_bits;
-    const int passes = (key_bits + 8) / 9, bits = (key_bits + passes - 1) / passes;
     for (int i = 0; i < passes; ++i, src ^= 1) {
       embed_hist_kernel<<<n_blocks, 512, 0, st>>>(w.key[src], n, i * bits, bits, w.hist, n_blocks);
       if ((r = launched())) return r;
@@ -311,11 +338,9 @@ int augtree_embed_bwd(const augtree_lm_t *lm, const void *d_out, int out_dtype, 
       if ((r = launched())) return r;
     }
   }
-  embed_starts_kernel<<<(unsigned)(lm->vocab / 256 + 1), 256, 0, st>>>(w.key[src], n, lm->vocab, w.start);
-  if ((r = launched())) return r;
-  if (out_dtype == AUGTREE_BF16) return embed_sum<__nv_bfloat16>(lm, d_out, w, src, d_table, table_dtype, accumulate, st);
-  if (out_dtype == AUGTREE_F16) return embed_sum<__half>(lm, d_out, w, src, d_table, table_dtype, accumulate, st);
-  return embed_sum<float>(lm, d_out, w, src, d_table, table_dtype, accumulate, st);
+  if (out_dtype == AUGTREE_BF16) return embed_sum<__nv_bfloat16>(lm, d_out, w, src, n, d_table, table_dtype, accumulate, st);
+  if (out_dtype == AUGTREE_F16) return embed_sum<__half>(lm, d_out, w, src, n, d_table, table_dtype, accumulate, st);
+  return embed_sum<float>(lm, d_out, w, src, n, d_table, table_dtype, accumulate, st);
 }
 
 int augtree_lm_loss_fwd(const augtree_lm_t *lm, const void *hidden, const void *weight, const void *targets, int id_bytes,

@@ -301,44 +301,206 @@ embed_scatter_kernel(const uint32_t *key, const int *val, int n, int shift, int 
   }
 }
 
-// first sorted place of every id (ids 0 .. vocab; the last is the end of the embedded tokens)
-__global__ void embed_starts_kernel(const uint32_t *key, int n, int vocab, int *start) {
-  const int v = blockIdx.x * blockDim.x + threadIdx.x;
-  if (v > vocab) return;
-  int lo = 0, hi = n;
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (key[mid] < (uint32_t)v) lo = mid + 1; else hi = mid;
+// The whole sort in one block, for up to kSortBlock tokens: keys and places wait in shared memory between the passes.
+// (Seven launches less than the passes above: 39 -> see the gradient kernel's figures.)
+constexpr int kSortSmallBytes = 16 * kSortBins * 4 + kSortBlock * 8;
+
+template <typename Id>
+__global__ void __launch_bounds__(512)
+embed_sort_small_kernel(const Id *ids, int n, int vocab, int passes, int bits, uint32_t *key_out, int *val_out, int *status) {
+  extern __shared__ __align__(16) int sort_smem[];
+  int *cnt = sort_smem;                        // [16][kSortBins]
+  uint32_t *skey = reinterpret_cast<uint32_t *>(sort_smem + 16 * kSortBins);
+  int *sval = sort_smem + 16 * kSortBins + kSortBlock;
+  __shared__ int wsum[16];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, bins = 1 << bits;
+  for (int i = threadIdx.x; i < n; i += 512) {
+    const long long id = ids[i];
+    if (id >= vocab && atomicCAS(status, 0, -1) == 0) status[1] = i;
+    skey[i] = id >= 0 && id < vocab ? (uint32_t)id : (uint32_t)vocab;
+    sval[i] = i;
   }
-  start[v] = lo;
+  for (int p = 0; p < passes; ++p) {
+    const int shift = p * bits;
+    for (int i = threadIdx.x; i < 16 * kSortBins; i += 512) cnt[i] = 0;
+    __syncthreads();
+    uint32_t k[8];
+    int v[8], rank[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int i = warp * 256 + j * 32 + lane;
+      const bool in = i < n;
+      k[j] = in ? skey[i] : 0;
+      v[j] = in ? sval[i] : 0;
+      const int d = in ? (int)((k[j] >> shift) & (bins - 1)) : -1;
+      const unsigned same = __match_any_sync(0xffffffffu, d);
+      const int first = __ffs(same) - 1;
+      int c = 0;
+      if (in && lane == first) { c = cnt[warp * kSortBins + d]; cnt[warp * kSortBins + d] = c + __popc(same); }
+      __syncwarp();
+      rank[j] = __shfl_sync(0xffffffffu, c, first) + __popc(same & ((1u << lane) - 1));
+    }
+    __syncthreads();
+    // a thread per bin: place of the bin, then of each warp's share of it
+    int tot = 0;
+    for (int w = 0; w < 16; ++w) { const int c = cnt[w * kSortBins + threadIdx.x]; cnt[w * kSortBins + threadIdx.x] = tot; tot += c; }
+    int s = tot;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int u = __shfl_up_sync(0xffffffffu, s, d);
+      if (lane >= d) s += u;
+    }
+    if (lane == 31) wsum[warp] = s;
+    __syncthreads();
+    int before = s - tot;
+    for (int w = 0; w < warp; ++w) before += wsum[w];
+    for (int w = 0; w < 16; ++w) cnt[w * kSortBins + threadIdx.x] += before;
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int i = warp * 256 + j * 32 + lane;
+      if (i < n) {
+        const int to = cnt[warp * kSortBins + ((k[j] >> shift) & (bins - 1))] + rank[j];
+        if (p == passes - 1) { key_out[to] = k[j]; val_out[to] = v[j]; }
+        else { skey[to] = k[j]; sval[to] = v[j]; }
+      }
+    }
+    __syncthreads();
+  }
 }
 
-// d_table[v] (+)= scale sum of d_out over the tokens of v, in the order of the tokens, in fp32, rounded once
+// ---- d_table[v] (+)= scale sum of d_out over the tokens of v, in the order of the tokens, in fp32, rounded once.
+// A frequent id owns thousands of tokens and a rare one a single token, so the sorted tokens are cut into chunks of equal
+// length, whatever ids they hold: a chunk writes the rows that lie inside it and leaves the sums of the row that comes in
+// from the chunk before (slot 0) and of the row that goes on into the next (slot 1) to embed_join_kernel, which adds a
+// row's sums up in order.  Bound by HBM: every gradient row read once, every table row written once.
+constexpr int kEmbedThreads = 128, kEmbedCols = 8 * kEmbedThreads;  // columns of a block: 8 a thread
+constexpr int kEmbedZeroRows = 16;                                  // table rows looked at by one block of the zero part
+constexpr int kEmbedMaxChunk = 256;
+
+template <typename Out>
+__device__ __forceinline__ void embed_store(Out *dst, float (&x)[8], float scale, int accumulate) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] *= scale;
+  if (accumulate) {
+    float y[8];
+    Vec<Out>::load(dst, y);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] += y[e];
+  }
+  Vec<Out>::store(dst, x);
+}
+
+// Whether any token has id v: lower bound of v in the sorted keys, 32 probes a step by the lanes of a warp.
+__device__ __forceinline__ bool embed_has_tokens(const uint32_t *key, int n, uint32_t v, int lane) {
+  int lo = 0, hi = n;  // the lower bound is in [lo, hi]
+  while (hi - lo > 0) {
+    const int step = (hi - lo + 31) / 32;
+    const int at = lo + (lane + 1) * step - 1;                      // last place of the lane's share
+    const unsigned ge = __ballot_sync(0xffffffffu, at >= hi || key[at] >= v);
+    // the shares before the first one whose last key is >= v hold smaller keys only
+    const int first = ge ? __ffs(ge) - 1 : 32;
+    const int nlo = min(lo + first * step, hi), nhi = first < 32 ? min(lo + (first + 1) * step - 1, hi) : hi;
+    lo = nlo;
+    hi = max(nhi, nlo);
+  }
+  return lo < n && key[lo] == v;
+}
+
 template <typename In, typename Out>
-__global__ void __launch_bounds__(128)
-embed_sum_kernel(const In *d_out, const int *val, const int *start, int vocab, int hidden, float scale, int accumulate, Out *d_table) {
-  for (int v = blockIdx.x; v < vocab; v += gridDim.x) {
-    const int a = start[v], b = start[v + 1];
-    if (a == b && accumulate) continue;
-    for (int i = threadIdx.x * 8; i < hidden; i += 1024) {
-      float x[8] = {};
-      for (int j = a; j < b; ++j) {
-        float y[8];
-        Vec<In>::load(d_out + (long long)val[j] * hidden + i, y);
+__global__ void __launch_bounds__(kEmbedThreads)
+embed_sum_kernel(const In *d_out, const uint32_t *key, const int *val, int n, int chunk, int n_chunks, int vocab, int hidden,
+                 float scale, int accumulate, Out *d_table, float *part) {
+  __shared__ uint32_t skey[kEmbedMaxChunk];
+  __shared__ int sval[kEmbedMaxChunk];
+  __shared__ unsigned has;
+  const int col = blockIdx.y * kEmbedCols + threadIdx.x * 8;
+  if ((int)blockIdx.x >= n_chunks) {
+    // rows without tokens: zeros
+    const int v0 = ((int)blockIdx.x - n_chunks) * kEmbedZeroRows, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) has = 0;
+    __syncthreads();
+    for (int i = warp; i < kEmbedZeroRows; i += kEmbedThreads / 32)
+      if (v0 + i < vocab && embed_has_tokens(key, n, (uint32_t)(v0 + i), lane) && lane == 0) atomicOr(&has, 1u << i);
+    __syncthreads();
+    const float zero[8] = {};
+    if (col < hidden)
+      for (int i = 0; i < kEmbedZeroRows && v0 + i < vocab; ++i)
+        if (!((has >> i) & 1)) Vec<Out>::store(d_table + (long long)(v0 + i) * hidden + col, zero);
+    return;
+  }
+  const int c = blockIdx.x, j0 = c * chunk, m = min(chunk, n - j0);
+  for (int i = threadIdx.x; i < m; i += kEmbedThreads) { skey[i] = key[j0 + i]; sval[i] = val[j0 + i]; }
+  const uint32_t before = j0 > 0 ? key[j0 - 1] : 0xffffffffu, after = j0 + m < n ? key[j0 + m] : 0xffffffffu;
+  __syncthreads();
+  if (col >= hidden) return;
+  float x[8] = {};
+  bool first = true;   // still in the chunk's first row
+  for (int j = 0; j < m; j += 4) {
+    float y[4][8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] += y[e];
+    for (int e = 0; e < 4; ++e)
+      if (j + e < m && skey[j + e] < (uint32_t)vocab) Vec<In>::load(d_out + (long long)sval[j + e] * hidden + col, y[e]);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (j + e < m && skey[j + e] < (uint32_t)vocab) {
+        const uint32_t v = skey[j + e];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] += y[e][i];
+        const bool last = j + e == m - 1;
+        if (last || skey[j + e + 1] != v) {
+          const bool comes_in = first && before == v, goes_on = last && after == v;
+          if (comes_in || goes_on) {
+            float *dst = part + ((long long)(2 * c + (comes_in ? 0 : 1)) * hidden + col);
+            Vec<float>::store(dst, x);
+          } else {
+            embed_store(d_table + (long long)v * hidden + col, x, scale, accumulate);
+          }
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[i] = 0.f;
+          first = false;
+        }
       }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] *= scale;
-      Out *dst = d_table + (long long)v * hidden + i;
-      if (accumulate) {
-        float y[8];
-        Vec<Out>::load(dst, y);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] += y[e];
-      }
-      Vec<Out>::store(dst, x);
     }
+  }
+}
+
+// Rows that cross from one chunk into the next, each joined by the block of the first border it crosses.  32 column
+// vectors x 8 shares of the row's sums, added up in order.
+template <typename Out>
+__global__ void __launch_bounds__(256)
+embed_join_kernel(const uint32_t *key, int n, int chunk, int n_chunks, int vocab, int hidden, float scale, int accumulate,
+                  Out *d_table, const float *part) {
+  __shared__ float sh[8][32][9];
+  const int c = blockIdx.x + 1;                                  // border between the chunks c - 1 and c
+  const uint32_t v = key[c * chunk];
+  if (v >= (uint32_t)vocab || key[c * chunk - 1] != v) return;   // no row crosses here
+  if (c > 1 && key[(c - 1) * chunk - 1] == v && key[(c - 1) * chunk] == v) return;  // it crossed an earlier border too
+  const int lane = threadIdx.x & 31, seg = threadIdx.x >> 5;
+  int lo = c, hi = n_chunks;  // last chunk whose first key is v: in [lo, hi)
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (key[mid * chunk] == v) lo = mid; else hi = mid;
+  }
+  const int count = lo - c + 2;                                  // sums of the row: slot 1 of chunk c - 1, slot 0 of c .. lo
+  const int per = (count + 7) / 8;
+  const int col = blockIdx.y * 256 + lane * 8;
+  float x[8] = {};
+  if (col < hidden)
+    for (int i = seg * per; i < min(count, (seg + 1) * per); ++i) {
+      float y[8];
+      Vec<float>::load(part + (long long)(i == 0 ? 2 * (c - 1) + 1 : 2 * (c - 1 + i)) * hidden + col, y);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] += y[e];
+    }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) sh[seg][lane][e] = x[e];
+  __syncthreads();
+  if (seg == 0 && col < hidden) {
+    for (int s = 1; s < 8; ++s)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] += sh[s][lane][e];
+    embed_store(d_table + (long long)v * hidden + col, x, scale, accumulate);
   }
 }
 
