@@ -95,7 +95,7 @@ size_t loss_layout(const augtree_lm *lm, int64_t tokens, bool bwd, uint8_t *base
 struct EmbedWs {
   uint32_t *key[2];
   int *val[2];
-  int *hist, *total;
+  int *hist, *total, *joins;
   float *part;   // [2 x chunks][hidden] sums of the rows that cross from chunk to chunk
   int chunk, n_chunks;
 };
@@ -109,13 +109,14 @@ int embed_chunk(const augtree_lm *lm, int64_t n) {
 }
 
 size_t embed_layout(const augtree_lm *lm, int64_t tokens, uint8_t *base, EmbedWs *w) {
-  const int64_t n = std::max<int64_t>(tokens, 1), blocks = (n + kSortBlock - 1) / kSortBlock;
+  const int64_t n = std::max<int64_t>(tokens, 1), blocks = (n + kRadixBlock - 1) / kRadixBlock;
   Cursor c{base};
   for (int i = 0; i < 2; ++i) { w->key[i] = c.take<uint32_t>(n); w->val[i] = c.take<int>(n); }
   w->hist = c.take<int>(blocks * kSortBins);
   w->total = c.take<int>(kSortBins);
   w->chunk = embed_chunk(lm, n);
   w->n_chunks = (int)((tokens + w->chunk - 1) / w->chunk);
+  w->joins = c.take<int>(w->n_chunks + 1);
   w->part = c.take<float>(2ll * w->n_chunks * lm->hidden);
   return c.off;
 }
@@ -204,17 +205,49 @@ int embed_fwd_in(const augtree_lm *lm, const void *table, int table_dtype, const
   return embed_fwd_out<Id, float>(lm, table, ids, tokens, out, out_dtype, st);
 }
 
+// Tokens sorted by id into w.key[*src], w.val[*src].
+template <typename Id>
+int embed_sort(const augtree_lm *lm, const Id *ids, int n, int passes, int bits, const EmbedWs &w, int *src, cudaStream_t st) {
+  int r;
+  embed_clear_kernel<<<(unsigned)((n + 255) / 256), 256, 0, st>>>(ids, n, lm->vocab, w.joins, lm->d_status);
+  if ((r = launched())) return r;
+  *src = 0;
+  if (n <= kSortSmall) {
+    embed_sort_small_kernel<<<1, 512, kSortSmallBytes, st>>>(ids, n, lm->vocab, passes, bits, w.key[0], w.val[0]);
+    return launched();
+  }
+  const int blocks = (n + kRadixBlock - 1) / kRadixBlock;
+  const KeysFromIds<Id> from_ids{ids, lm->vocab};
+  for (int i = 0; i < passes; ++i) {
+    const KeysSorted sorted{w.key[*src], w.val[*src]};
+    const int to = i == 0 ? 0 : *src ^ 1;
+    if (i == 0) embed_hist_kernel<<<blocks, kRadixThreads, 0, st>>>(from_ids, n, 0, bits, w.hist, blocks);
+    else embed_hist_kernel<<<blocks, kRadixThreads, 0, st>>>(sorted, n, i * bits, bits, w.hist, blocks);
+    if ((r = launched())) return r;
+    embed_scan_kernel<<<((1 << bits) + 7) / 8, 256, 0, st>>>(w.hist, blocks, 1 << bits, w.total);
+    if ((r = launched())) return r;
+    if (i == 0) embed_scatter_kernel<<<blocks, kRadixThreads, 0, st>>>(from_ids, n, 0, bits, w.hist, blocks, w.total, w.key[to], w.val[to]);
+    else embed_scatter_kernel<<<blocks, kRadixThreads, 0, st>>>(sorted, n, i * bits, bits, w.hist, blocks, w.total, w.key[to], w.val[to]);
+    if ((r = launched())) return r;
+    *src = to;
+  }
+  return AUGTREE_OK;
+}
+
 template <typename In, typename Out>
 int embed_sum_out(const augtree_lm *lm, const void *d_out, const EmbedWs &w, int src, int n, void *d_table, int accumulate, cudaStream_t st) {
   const unsigned zero_blocks = accumulate ? 0u : (unsigned)((lm->vocab + kEmbedZeroRows - 1) / kEmbedZeroRows);
   Out *dt = static_cast<Out *>(d_table);
   if (w.n_chunks + zero_blocks == 0) return AUGTREE_OK;
-  embed_sum_kernel<<<dim3(w.n_chunks + zero_blocks, (lm->hidden + kEmbedCols - 1) / kEmbedCols), kEmbedThreads, 0, st>>>(
-      static_cast<const In *>(d_out), w.key[src], w.val[src], n, w.chunk, w.n_chunks, lm->vocab, lm->hidden, lm->embed_scale, accumulate, dt, w.part);
+  const int vecs = lm->hidden / 8, slabs = (vecs + kEmbedMaxThreads - 1) / kEmbedMaxThreads;
+  const int threads = (int)up((vecs + slabs - 1) / slabs, 32);
+  embed_sum_kernel<<<dim3(w.n_chunks + zero_blocks, slabs), threads, 0, st>>>(static_cast<const In *>(d_out), w.key[src], w.val[src], n, w.chunk,
+                                                                           w.n_chunks, lm->vocab, lm->hidden, lm->embed_scale, accumulate,
+                                                                           dt, w.part, w.joins);
   int r = launched();
   if (r || w.n_chunks < 2) return r;
-  embed_join_kernel<<<dim3(w.n_chunks - 1, (lm->hidden + 255) / 256), 256, 0, st>>>(w.key[src], n, w.chunk, w.n_chunks, lm->vocab,
-                                                                                  lm->hidden, lm->embed_scale, accumulate, dt, w.part);
+  const unsigned grid = (unsigned)std::min<int64_t>((int64_t)(w.n_chunks - 1) * ((lm->hidden + 255) / 256), 4 * lm->n_lanes);
+  embed_join_kernel<<<grid, 256, 0, st>>>(w.key[src], w.chunk, w.n_chunks, lm->hidden, lm->embed_scale, accumulate, dt, w.part, w.joins);
   return launched();
 }
 
@@ -315,28 +348,15 @@ int augtree_embed_bwd(const augtree_lm_t *lm, const void *d_out, int out_dtype, 
   EmbedWs w;
   if (!ws || !aligned16(ws) || ws_bytes < embed_layout(lm, n_tokens, static_cast<uint8_t *>(ws), &w)) return AUGTREE_ERR_WORKSPACE;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const int n = (int)n_tokens, n_blocks = (n + kSortBlock - 1) / kSortBlock;
+  const int n = (int)n_tokens, n_blocks = (n + kRadixBlock - 1) / kRadixBlock;
   int key_bits = 1;
   while ((lm->vocab >> key_bits) != 0) ++key_bits;
   const int passes = (key_bits + 8) / 9, bits = (key_bits + passes - 1) / passes;
   int src = 0;
-  if (n > 0 && n <= kSortBlock) {
-    if (id_bytes == 8) embed_sort_small_kernel<<<1, 512, kSortSmallBytes, st>>>(static_cast<const long long *>(ids), n, lm->vocab, passes, bits, w.key[0], w.val[0], lm->d_status);
-    else embed_sort_small_kernel<<<1, 512, kSortSmallBytes, st>>>(static_cast<const int *>(ids), n, lm->vocab, passes, bits, w.key[0], w.val[0], lm->d_status);
-    if ((r = launched())) return r;
-  } else if (n > 0) {
-    const unsigned g = (unsigned)((n + 255) / 256);
-    if (id_bytes == 8) embed_keys_kernel<<<g, 256, 0, st>>>(static_cast<const long long *>(ids), n, lm->vocab, w.key[0], w.val[0], lm->d_status);
-    else embed_keys_kernel<<<g, 256, 0, st>>>(static_cast<const int *>(ids), n, lm->vocab, w.key[0], w.val[0], lm->d_status);
-    if ((r = launched())) return r;
-    for (int i = 0; i < passes; ++i, src ^= 1) {
-      embed_hist_kernel<<<n_blocks, 512, 0, st>>>(w.key[src], n, i * bits, bits, w.hist, n_blocks);
-      if ((r = launched())) return r;
-      embed_scan_kernel<<<((1 << bits) + 7) / 8, 256, 0, st>>>(w.hist, n_blocks, 1 << bits, w.total);
-      if ((r = launched())) return r;
-      embed_scatter_kernel<<<n_blocks, 512, 0, st>>>(w.key[src], w.val[src], n, i * bits, bits, w.hist, n_blocks, w.total, w.key[src ^ 1], w.val[src ^ 1]);
-      if ((r = launched())) return r;
-    }
+  if (n > 0) {
+    r = id_bytes == 8 ? embed_sort(lm, static_cast<const long long *>(ids), n, passes, bits, w, &src, st)
+                      : embed_sort(lm, static_cast<const int *>(ids), n, passes, bits, w, &src, st);
+    if (r) return r;
   }
   if (out_dtype == AUGTREE_BF16) return embed_sum<__nv_bfloat16>(lm, d_out, w, src, n, d_table, table_dtype, accumulate, st);
   if (out_dtype == AUGTREE_F16) return embed_sum<__half>(lm, d_out, w, src, n, d_table, table_dtype, accumulate, st);

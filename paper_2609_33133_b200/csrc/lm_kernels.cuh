@@ -7,6 +7,12 @@
 
 namespace augtree {
 
+// an id beyond the vocabulary is left out like padding, and reported
+template <typename Id>
+__device__ __forceinline__ void check_id(Id id, int t, int vocab, int *status) {
+  if ((long long)id >= vocab && atomicCAS(status, 0, -1) == 0) status[1] = t;
+}
+
 // ---------------------------------------------------------------- compaction of the scored rows
 // Rows with a negative target are not scored.  They are left out of every product: their hidden states may hold
 // anything, NaN included, and 0 x NaN in the contraction of dW would spoil it; and their work is saved.
@@ -31,7 +37,7 @@ lm_compact_kernel(const Id *targets, int tokens, int vocab, LmRows o, const floa
     const int t = t0 + (int)threadIdx.x;
     const long long id = t < tokens ? (long long)targets[t] : -1;
     const bool live = id >= 0 && id < vocab;
-    if (id >= vocab && atomicCAS(status, 0, -1) == 0) status[1] = t;
+    check_id(id, t, vocab, status);
     const unsigned m = __ballot_sync(0xffffffffu, live);
     if (lane == 0) warp_sum[warp] = __popc(m);
     __syncthreads();
@@ -186,7 +192,7 @@ embed_fwd_kernel(const In *table, const Id *ids, int tokens, int vocab, int hidd
   for (int t = blockIdx.x; t < tokens; t += gridDim.x) {
     const long long id = ids[t];
     const bool live = id >= 0 && id < vocab;
-    if (id >= vocab && threadIdx.x == 0 && atomicCAS(status, 0, -1) == 0) status[1] = t;
+    if (threadIdx.x == 0) check_id(id, t, vocab, status);
     for (int i = threadIdx.x * 8; i < hidden; i += 1024) {
       float x[8] = {};
       if (live) {
@@ -200,29 +206,39 @@ embed_fwd_kernel(const In *table, const Id *ids, int tokens, int vocab, int hidd
 }
 
 // ---- tokens sorted by id, stably: least-significant-digit radix passes of at most 9 bits.  Key `vocab` = not embedded.
-constexpr int kSortBlock = 4096;   // keys of one block: 16 warps x 256
+// The first pass reads the ids themselves.  Blocks of 1024 keys: a pass is bound by the latency of its few dependent steps,
+// so many small blocks beat few large ones (24576 tokens, scatter pass: 16 us with 4096 keys a block).
 constexpr int kSortBins = 512;
+constexpr int kRadixBlock = 1024, kRadixThreads = 256, kRadixWarps = 8;  // 128 keys a warp, 4 a lane
 
+struct KeysSorted {   // keys and places of the pass before
+  const uint32_t *key;
+  const int *val;
+  __device__ __forceinline__ uint32_t get(int i) const { return key[i]; }
+  __device__ __forceinline__ int place(int i) const { return val[i]; }
+};
 template <typename Id>
-__global__ void embed_keys_kernel(const Id *ids, int tokens, int vocab, uint32_t *key, int *val, int *status) {
-  const int t = blockIdx.x * blockDim.x + threadIdx.x;
-  if (t >= tokens) return;
-  const long long id = ids[t];
-  if (id >= vocab && atomicCAS(status, 0, -1) == 0) status[1] = t;
-  key[t] = id >= 0 && id < vocab ? (uint32_t)id : (uint32_t)vocab;
-  val[t] = t;
-}
+struct KeysFromIds {
+  const Id *ids;
+  int vocab;
+  __device__ __forceinline__ uint32_t get(int i) const {
+    const long long id = ids[i];
+    return id >= 0 && id < vocab ? (uint32_t)id : (uint32_t)vocab;
+  }
+  __device__ __forceinline__ int place(int i) const { return i; }
+};
 
-__global__ void __launch_bounds__(512)
-embed_hist_kernel(const uint32_t *key, int n, int shift, int bits, int *hist, int n_blocks) {
+template <typename Keys>
+__global__ void __launch_bounds__(kRadixThreads)
+embed_hist_kernel(const Keys in, int n, int shift, int bits, int *hist, int n_blocks) {
   __shared__ int cnt[kSortBins];
-  cnt[threadIdx.x] = 0;
+  for (int i = threadIdx.x; i < kSortBins; i += kRadixThreads) cnt[i] = 0;
   __syncthreads();
-  const int b0 = blockIdx.x * kSortBlock;
-  for (int i = threadIdx.x; i < kSortBlock; i += 512)
-    if (b0 + i < n) atomicAdd(&cnt[(key[b0 + i] >> shift) & ((1u << bits) - 1)], 1);  // a count: the order does not matter
+  const int b0 = blockIdx.x * kRadixBlock;
+  for (int i = threadIdx.x; i < kRadixBlock && b0 + i < n; i += kRadixThreads)
+    atomicAdd(&cnt[(in.get(b0 + i) >> shift) & ((1u << bits) - 1)], 1);  // a count: the order does not matter
   __syncthreads();
-  if ((int)threadIdx.x < (1 << bits)) hist[(long long)threadIdx.x * n_blocks + blockIdx.x] = cnt[threadIdx.x];
+  for (int i = threadIdx.x; i < (1 << bits); i += kRadixThreads) hist[(long long)i * n_blocks + blockIdx.x] = cnt[i];
 }
 
 // one warp per bin: exclusive prefix sum over the blocks, total of the bin behind it
@@ -245,17 +261,28 @@ embed_scan_kernel(int *hist, int n_blocks, int bins, int *total) {
   if (lane == 0) total[bin] = run;
 }
 
-__global__ void __launch_bounds__(512)
-embed_scatter_kernel(const uint32_t *key, const int *val, int n, int shift, int bits, const int *hist, int n_blocks, const int *total,
-                     uint32_t *key_out, int *val_out) {
-  __shared__ int cnt[16][kSortBins];
-  __shared__ int start[kSortBins];
-  __shared__ int wsum[16];
+template <typename Keys>
+__global__ void __launch_bounds__(kRadixThreads)
+embed_scatter_kernel(const Keys in, int n, int shift, int bits, const int *hist, int n_blocks, const int *total, uint32_t *key_out, int *val_out) {
+  __shared__ int cnt[kRadixWarps][kSortBins];
+  __shared__ int wsum[kRadixWarps];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, bins = 1 << bits;
-  for (int i = threadIdx.x; i < 16 * kSortBins; i += 512) (&cnt[0][0])[i] = 0;
-  // exclusive prefix sum of the bins' totals
-  const int tv = (int)threadIdx.x < bins ? total[threadIdx.x] : 0;
-  int s = tv;
+  const int w0 = blockIdx.x * kRadixBlock + warp * 128;
+  uint32_t k[4];
+  int v[4], rank[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int i = w0 + j * 32 + lane;
+    k[j] = i < n ? in.get(i) : 0;
+    v[j] = i < n ? in.place(i) : 0;
+  }
+  for (int i = threadIdx.x; i < kRadixWarps * kSortBins; i += kRadixThreads) (&cnt[0][0])[i] = 0;
+  // places of this thread's two bins: exclusive prefix sum of the totals, plus the share of the earlier blocks
+  const int b0 = threadIdx.x * 2;
+  const int t0 = b0 < bins ? total[b0] : 0, t1 = b0 + 1 < bins ? total[b0 + 1] : 0;
+  const int h0 = b0 < bins ? hist[(long long)b0 * n_blocks + blockIdx.x] : 0;
+  const int h1 = b0 + 1 < bins ? hist[(long long)(b0 + 1) * n_blocks + blockIdx.x] : 0;
+  int s = t0 + t1;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
     const int u = __shfl_up_sync(0xffffffffu, s, d);
@@ -263,61 +290,54 @@ embed_scatter_kernel(const uint32_t *key, const int *val, int n, int shift, int 
   }
   if (lane == 31) wsum[warp] = s;
   __syncthreads();
-  int before = 0;
+  int before = s - t0 - t1;
   for (int w = 0; w < warp; ++w) before += wsum[w];
-  if ((int)threadIdx.x < bins) start[threadIdx.x] = before + s - tv + hist[(long long)threadIdx.x * n_blocks + blockIdx.x];
-  __syncthreads();
   // rank of every key among the warp's earlier keys of the same digit, in order
-  const int w0 = blockIdx.x * kSortBlock + warp * 256;
-  uint32_t k[8];
-  int rank[8];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const int i = w0 + j * 32 + lane;
-    const bool in = i < n;
-    k[j] = in ? key[i] : 0;
-    const int d = in ? (int)((k[j] >> shift) & (bins - 1)) : -1;
+  for (int j = 0; j < 4; ++j) {
+    const bool live = w0 + j * 32 + lane < n;
+    const int d = live ? (int)((k[j] >> shift) & (bins - 1)) : -1;
     const unsigned same = __match_any_sync(0xffffffffu, d);
     const int first = __ffs(same) - 1;
     int c = 0;
-    if (in && lane == first) { c = cnt[warp][d]; cnt[warp][d] = c + __popc(same); }
+    if (live && lane == first) { c = cnt[warp][d]; cnt[warp][d] = c + __popc(same); }
     __syncwarp();
     rank[j] = __shfl_sync(0xffffffffu, c, first) + __popc(same & ((1u << lane) - 1));
   }
   __syncthreads();
-  if ((int)threadIdx.x < bins) {
-    int run = start[threadIdx.x];
-    for (int w = 0; w < 16; ++w) { const int v = cnt[w][threadIdx.x]; cnt[w][threadIdx.x] = run; run += v; }
+  int r0 = before + h0, r1 = before + t0 + h1;
+#pragma unroll
+  for (int w = 0; w < kRadixWarps; ++w) {
+    const int c0 = cnt[w][b0], c1 = cnt[w][b0 + 1];
+    cnt[w][b0] = r0; cnt[w][b0 + 1] = r1;
+    r0 += c0; r1 += c1;
   }
   __syncthreads();
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const int i = w0 + j * 32 + lane;
-    if (i < n) {
+  for (int j = 0; j < 4; ++j)
+    if (w0 + j * 32 + lane < n) {
       const int to = cnt[warp][(k[j] >> shift) & (bins - 1)] + rank[j];
       key_out[to] = k[j];
-      val_out[to] = val[i];
+      val_out[to] = v[j];
     }
-  }
 }
 
-// The whole sort in one block, for up to kSortBlock tokens: keys and places wait in shared memory between the passes.
-// (Seven launches less than the passes above: 39 -> see the gradient kernel's figures.)
-constexpr int kSortSmallBytes = 16 * kSortBins * 4 + kSortBlock * 8;
+// The whole sort in one block, for up to kSortSmall tokens: keys and places wait in shared memory between the passes, and
+// five launches are saved.
+constexpr int kSortSmall = 4096;   // 16 warps x 256 keys
+constexpr int kSortSmallBytes = 16 * kSortBins * 4 + kSortSmall * 8;
 
 template <typename Id>
 __global__ void __launch_bounds__(512)
-embed_sort_small_kernel(const Id *ids, int n, int vocab, int passes, int bits, uint32_t *key_out, int *val_out, int *status) {
+embed_sort_small_kernel(const Id *ids, int n, int vocab, int passes, int bits, uint32_t *key_out, int *val_out) {
   extern __shared__ __align__(16) int sort_smem[];
   int *cnt = sort_smem;                        // [16][kSortBins]
   uint32_t *skey = reinterpret_cast<uint32_t *>(sort_smem + 16 * kSortBins);
-  int *sval = sort_smem + 16 * kSortBins + kSortBlock;
+  int *sval = sort_smem + 16 * kSortBins + kSortSmall;
   __shared__ int wsum[16];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, bins = 1 << bits;
   for (int i = threadIdx.x; i < n; i += 512) {
-    const long long id = ids[i];
-    if (id >= vocab && atomicCAS(status, 0, -1) == 0) status[1] = i;
-    skey[i] = id >= 0 && id < vocab ? (uint32_t)id : (uint32_t)vocab;
+    skey[i] = KeysFromIds<Id>{ids, vocab}.get(i);
     sval[i] = i;
   }
   for (int p = 0; p < passes; ++p) {
@@ -373,9 +393,10 @@ embed_sort_small_kernel(const Id *ids, int n, int vocab, int passes, int bits, u
 // A frequent id owns thousands of tokens and a rare one a single token, so the sorted tokens are cut into chunks of equal
 // length, whatever ids they hold: a chunk writes the rows that lie inside it and leaves the sums of the row that comes in
 // from the chunk before (slot 0) and of the row that goes on into the next (slot 1) to embed_join_kernel, which adds a
-// row's sums up in order.  Bound by HBM: every gradient row read once, every table row written once.
-constexpr int kEmbedThreads = 128, kEmbedCols = 8 * kEmbedThreads;  // columns of a block: 8 a thread
-constexpr int kEmbedZeroRows = 16;                                  // table rows looked at by one block of the zero part
+// row's sums up in order.  Bound by HBM: every gradient row read once, every table row written once.  A thread has eight
+// columns and a block whole rows (up to 4096 columns), so reads and writes are runs of several KB.
+constexpr int kEmbedMaxThreads = 512;
+constexpr int kEmbedZeroRows = 16;      // table rows looked at by one block of the zero part
 constexpr int kEmbedMaxChunk = 256;
 
 template <typename Out>
@@ -407,22 +428,31 @@ __device__ __forceinline__ bool embed_has_tokens(const uint32_t *key, int n, uin
   return lo < n && key[lo] == v;
 }
 
+// joins[0] counts the rows that cross chunks, joins[1 ..] are the chunks they start in (in any order: each row is joined alone).
+// It is cleared, and ids beyond the vocabulary are reported, by embed_clear_kernel, the first launch of the call.
+template <typename Id>
+__global__ void embed_clear_kernel(const Id *ids, int n, int vocab, int *joins, int *status) {
+  const int t = blockIdx.x * blockDim.x + threadIdx.x;
+  if (t == 0) joins[0] = 0;
+  if (t < n) check_id(ids[t], t, vocab, status);
+}
+
 template <typename In, typename Out>
-__global__ void __launch_bounds__(kEmbedThreads)
+__global__ void __launch_bounds__(kEmbedMaxThreads)
 embed_sum_kernel(const In *d_out, const uint32_t *key, const int *val, int n, int chunk, int n_chunks, int vocab, int hidden,
-                 float scale, int accumulate, Out *d_table, float *part) {
+                 float scale, int accumulate, Out *d_table, float *part, int *joins) {
   __shared__ uint32_t skey[kEmbedMaxChunk];
   __shared__ int sval[kEmbedMaxChunk];
-  __shared__ unsigned has;
-  const int col = blockIdx.y * kEmbedCols + threadIdx.x * 8;
+  const int col = (blockIdx.y * blockDim.x + threadIdx.x) * 8;
   if ((int)blockIdx.x >= n_chunks) {
     // rows without tokens: zeros
     const int v0 = ((int)blockIdx.x - n_chunks) * kEmbedZeroRows, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    if (threadIdx.x == 0) has = 0;
+    if (threadIdx.x == 0) skey[0] = 0;
     __syncthreads();
-    for (int i = warp; i < kEmbedZeroRows; i += kEmbedThreads / 32)
-      if (v0 + i < vocab && embed_has_tokens(key, n, (uint32_t)(v0 + i), lane) && lane == 0) atomicOr(&has, 1u << i);
+    for (int i = warp; i < kEmbedZeroRows; i += blockDim.x / 32)
+      if (v0 + i < vocab && embed_has_tokens(key, n, (uint32_t)(v0 + i), lane) && lane == 0) atomicOr(&skey[0], 1u << i);
     __syncthreads();
+    const uint32_t has = skey[0];
     const float zero[8] = {};
     if (col < hidden)
       for (int i = 0; i < kEmbedZeroRows && v0 + i < vocab; ++i)
@@ -430,9 +460,14 @@ embed_sum_kernel(const In *d_out, const uint32_t *key, const int *val, int n, in
     return;
   }
   const int c = blockIdx.x, j0 = c * chunk, m = min(chunk, n - j0);
-  for (int i = threadIdx.x; i < m; i += kEmbedThreads) { skey[i] = key[j0 + i]; sval[i] = val[j0 + i]; }
+  for (int i = threadIdx.x; i < m; i += blockDim.x) { skey[i] = key[j0 + i]; sval[i] = val[j0 + i]; }
   const uint32_t before = j0 > 0 ? key[j0 - 1] : 0xffffffffu, after = j0 + m < n ? key[j0 + m] : 0xffffffffu;
   __syncthreads();
+  if (threadIdx.x == 0 && blockIdx.y == 0) {
+    // the chunk's last row goes on, and does not come in (a chunk full of one row that comes in is in the middle of it)
+    const uint32_t v = skey[m - 1];
+    if (v < (uint32_t)vocab && after == v && !(skey[0] == v && before == v)) joins[1 + atomicAdd(joins, 1)] = c;
+  }
   if (col >= hidden) return;
   float x[8] = {};
   bool first = true;   // still in the chunk's first row
@@ -465,42 +500,44 @@ embed_sum_kernel(const In *d_out, const uint32_t *key, const int *val, int n, in
   }
 }
 
-// Rows that cross from one chunk into the next, each joined by the block of the first border it crosses.  32 column
-// vectors x 8 shares of the row's sums, added up in order.
+// Rows that cross from one chunk into the next.  A block takes 256 columns of a row: 32 column vectors x 8 shares of the
+// row's sums, added up in order.
 template <typename Out>
 __global__ void __launch_bounds__(256)
-embed_join_kernel(const uint32_t *key, int n, int chunk, int n_chunks, int vocab, int hidden, float scale, int accumulate,
-                  Out *d_table, const float *part) {
+embed_join_kernel(const uint32_t *key, int chunk, int n_chunks, int hidden, float scale, int accumulate, Out *d_table, const float *part,
+                  const int *joins) {
   __shared__ float sh[8][32][9];
-  const int c = blockIdx.x + 1;                                  // border between the chunks c - 1 and c
-  const uint32_t v = key[c * chunk];
-  if (v >= (uint32_t)vocab || key[c * chunk - 1] != v) return;   // no row crosses here
-  if (c > 1 && key[(c - 1) * chunk - 1] == v && key[(c - 1) * chunk] == v) return;  // it crossed an earlier border too
   const int lane = threadIdx.x & 31, seg = threadIdx.x >> 5;
-  int lo = c, hi = n_chunks;  // last chunk whose first key is v: in [lo, hi)
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (key[mid * chunk] == v) lo = mid; else hi = mid;
-  }
-  const int count = lo - c + 2;                                  // sums of the row: slot 1 of chunk c - 1, slot 0 of c .. lo
-  const int per = (count + 7) / 8;
-  const int col = blockIdx.y * 256 + lane * 8;
-  float x[8] = {};
-  if (col < hidden)
-    for (int i = seg * per; i < min(count, (seg + 1) * per); ++i) {
-      float y[8];
-      Vec<float>::load(part + (long long)(i == 0 ? 2 * (c - 1) + 1 : 2 * (c - 1 + i)) * hidden + col, y);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] += y[e];
+  const int rows = joins[0], slabs = (hidden + 255) / 256;
+  for (int it = blockIdx.x; it < rows * slabs; it += gridDim.x) {
+    const int c = joins[1 + it / slabs];
+    const uint32_t v = key[(c + 1) * chunk];
+    int lo = c + 1, hi = n_chunks;  // last chunk whose first key is v: in [lo, hi)
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (key[mid * chunk] == v) lo = mid; else hi = mid;
     }
+    const int count = lo - c + 1;   // sums of the row: slot 1 of chunk c, slot 0 of c + 1 .. lo
+    const int per = (count + 7) / 8;
+    const int col = it % slabs * 256 + lane * 8;
+    float x[8] = {};
+    if (col < hidden)
+      for (int i = seg * per; i < min(count, (seg + 1) * per); ++i) {
+        float y[8];
+        Vec<float>::load(part + (long long)(i == 0 ? 2 * c + 1 : 2 * (c + i)) * hidden + col, y);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) sh[seg][lane][e] = x[e];
-  __syncthreads();
-  if (seg == 0 && col < hidden) {
-    for (int s = 1; s < 8; ++s)
+        for (int e = 0; e < 8; ++e) x[e] += y[e];
+      }
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] += sh[s][lane][e];
-    embed_store(d_table + (long long)v * hidden + col, x, scale, accumulate);
+    for (int e = 0; e < 8; ++e) sh[seg][lane][e] = x[e];
+    __syncthreads();
+    if (seg == 0 && col < hidden) {
+      for (int s = 1; s < 8; ++s)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] += sh[s][lane][e];
+      embed_store(d_table + (long long)v * hidden + col, x, scale, accumulate);
+    }
+    __syncthreads();
   }
 }
 
