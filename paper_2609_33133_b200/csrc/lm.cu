@@ -96,6 +96,7 @@ struct EmbedWs {
   uint32_t *key[2];
   int *val[2];
   int *hist, *total, *joins;
+  uint32_t *seen;
   float *part;   // [2 x chunks][hidden] sums of the rows that cross from chunk to chunk
   int chunk, n_chunks;
 };
@@ -116,7 +117,8 @@ size_t embed_layout(const augtree_lm *lm, int64_t tokens, uint8_t *base, EmbedWs
   w->total = c.take<int>(kSortBins);
   w->chunk = embed_chunk(lm, n);
   w->n_chunks = (int)((tokens + w->chunk - 1) / w->chunk);
-  w->joins = c.take<int>(w->n_chunks + 1);
+  w->joins = c.take<int>(w->n_chunks + 2);
+  w->seen = c.take<uint32_t>((lm->vocab + 31) / 32);
   w->part = c.take<float>(2ll * w->n_chunks * lm->hidden);
   return c.off;
 }
@@ -209,15 +211,13 @@ int embed_fwd_in(const augtree_lm *lm, const void *table, int table_dtype, const
 template <typename Id>
 int embed_sort(const augtree_lm *lm, const Id *ids, int n, int passes, int bits, const EmbedWs &w, int *src, cudaStream_t st) {
   int r;
-  embed_clear_kernel<<<(unsigned)((n + 255) / 256), 256, 0, st>>>(ids, n, lm->vocab, w.joins, lm->d_status);
-  if ((r = launched())) return r;
   *src = 0;
-  if (n <= kSortSmall) {
-    embed_sort_small_kernel<<<1, 512, kSortSmallBytes, st>>>(ids, n, lm->vocab, passes, bits, w.key[0], w.val[0]);
+  if (n <= kSortSmall && lm->vocab <= (1 << 20)) {  // (a larger vocabulary's bits are cleared by more than one block)
+    embed_sort_small_kernel<<<1, 512, kSortSmallBytes, st>>>(ids, n, lm->vocab, passes, bits, w.key[0], w.val[0], w.joins, w.seen, lm->d_status);
     return launched();
   }
   const int blocks = (n + kRadixBlock - 1) / kRadixBlock;
-  const KeysFromIds<Id> from_ids{ids, lm->vocab};
+  const KeysFromIds<Id> from_ids{ids, lm->vocab, lm->d_status};
   for (int i = 0; i < passes; ++i) {
     const KeysSorted sorted{w.key[*src], w.val[*src]};
     const int to = i == 0 ? 0 : *src ^ 1;
@@ -231,7 +231,9 @@ int embed_sort(const augtree_lm *lm, const Id *ids, int n, int passes, int bits,
     if ((r = launched())) return r;
     *src = to;
   }
-  return AUGTREE_OK;
+  if (cudaMemsetAsync(w.seen, 0, (size_t)((lm->vocab + 31) / 32) * 4, st) != cudaSuccess) return AUGTREE_ERR_CUDA;
+  embed_mark_kernel<<<(unsigned)((n + 255) / 256), 256, 0, st>>>(w.key[*src], n, lm->vocab, w.seen, w.joins);
+  return launched();
 }
 
 template <typename In, typename Out>
@@ -243,10 +245,10 @@ int embed_sum_out(const augtree_lm *lm, const void *d_out, const EmbedWs &w, int
   const int threads = (int)up((vecs + slabs - 1) / slabs, 32);
   embed_sum_kernel<<<dim3(w.n_chunks + zero_blocks, slabs), threads, 0, st>>>(static_cast<const In *>(d_out), w.key[src], w.val[src], n, w.chunk,
                                                                            w.n_chunks, lm->vocab, lm->hidden, lm->embed_scale, accumulate,
-                                                                           dt, w.part, w.joins);
+                                                                           dt, w.part, w.joins, w.seen);
   int r = launched();
   if (r || w.n_chunks < 2) return r;
-  const unsigned grid = (unsigned)std::min<int64_t>((int64_t)(w.n_chunks - 1) * ((lm->hidden + 255) / 256), 4 * lm->n_lanes);
+  const unsigned grid = (unsigned)std::min<int64_t>((int64_t)(w.n_chunks - 1) * ((lm->hidden + 255) / 256), 8 * lm->n_lanes);
   embed_join_kernel<<<grid, 256, 0, st>>>(w.key[src], w.chunk, w.n_chunks, lm->hidden, lm->embed_scale, accumulate, dt, w.part, w.joins);
   return launched();
 }

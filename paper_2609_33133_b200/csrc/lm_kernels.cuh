@@ -216,11 +216,14 @@ struct KeysSorted {   // keys and places of the pass before
   const int *val;
   __device__ __forceinline__ uint32_t get(int i) const { return key[i]; }
   __device__ __forceinline__ int place(int i) const { return val[i]; }
+  __device__ __forceinline__ void check(int) const {}
 };
 template <typename Id>
 struct KeysFromIds {
   const Id *ids;
   int vocab;
+  int *status;
+  __device__ __forceinline__ void check(int i) const { check_id(ids[i], i, vocab, status); }
   __device__ __forceinline__ uint32_t get(int i) const {
     const long long id = ids[i];
     return id >= 0 && id < vocab ? (uint32_t)id : (uint32_t)vocab;
@@ -235,8 +238,10 @@ embed_hist_kernel(const Keys in, int n, int shift, int bits, int *hist, int n_bl
   for (int i = threadIdx.x; i < kSortBins; i += kRadixThreads) cnt[i] = 0;
   __syncthreads();
   const int b0 = blockIdx.x * kRadixBlock;
-  for (int i = threadIdx.x; i < kRadixBlock && b0 + i < n; i += kRadixThreads)
+  for (int i = threadIdx.x; i < kRadixBlock && b0 + i < n; i += kRadixThreads) {
+    in.check(b0 + i);
     atomicAdd(&cnt[(in.get(b0 + i) >> shift) & ((1u << bits) - 1)], 1);  // a count: the order does not matter
+  }
   __syncthreads();
   for (int i = threadIdx.x; i < (1 << bits); i += kRadixThreads) hist[(long long)i * n_blocks + blockIdx.x] = cnt[i];
 }
@@ -322,6 +327,25 @@ embed_scatter_kernel(const Keys in, int n, int shift, int bits, const int *hist,
     }
 }
 
+// What the sum and join kernels need besides the sorted tokens:
+//   joins[0], joins[1]  numbers of rows that cross chunks: short ones (up to kJoinShort sums) and long ones; behind them the
+//                       chunks the rows start in, short ones from the front, long ones from the back, in any order (each
+//                       row is joined alone)
+//   seen                one bit per table row: whether any token has this id
+// The bits are set from the sorted keys, once for each id: setting them from the tokens took 39 us for 131071 of them, all
+// at the few words of the frequent ids.
+constexpr int kJoinShort = 8;
+
+__device__ __forceinline__ void embed_mark(const uint32_t *key, int i, int vocab, uint32_t *seen) {
+  const uint32_t k = key[i];
+  if (k < (uint32_t)vocab && (i == 0 || key[i - 1] != k)) atomicOr(seen + (k >> 5), 1u << (k & 31));
+}
+__global__ void embed_mark_kernel(const uint32_t *key, int n, int vocab, uint32_t *seen, int *joins) {
+  const int i = blockIdx.x * blockDim.x + threadIdx.x;
+  if (i < 2) joins[i] = 0;
+  if (i < n) embed_mark(key, i, vocab, seen);
+}
+
 // The whole sort in one block, for up to kSortSmall tokens: keys and places wait in shared memory between the passes, and
 // five launches are saved.
 constexpr int kSortSmall = 4096;   // 16 warps x 256 keys
@@ -329,15 +353,19 @@ constexpr int kSortSmallBytes = 16 * kSortBins * 4 + kSortSmall * 8;
 
 template <typename Id>
 __global__ void __launch_bounds__(512)
-embed_sort_small_kernel(const Id *ids, int n, int vocab, int passes, int bits, uint32_t *key_out, int *val_out) {
+embed_sort_small_kernel(const Id *ids, int n, int vocab, int passes, int bits, uint32_t *key_out, int *val_out,
+                        int *joins, uint32_t *seen, int *status) {
   extern __shared__ __align__(16) int sort_smem[];
   int *cnt = sort_smem;                        // [16][kSortBins]
   uint32_t *skey = reinterpret_cast<uint32_t *>(sort_smem + 16 * kSortBins);
   int *sval = sort_smem + 16 * kSortBins + kSortSmall;
   __shared__ int wsum[16];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, bins = 1 << bits;
+  if (threadIdx.x < 2) joins[threadIdx.x] = 0;
+  for (int i = threadIdx.x; i < (vocab + 31) / 32; i += 512) seen[i] = 0;
   for (int i = threadIdx.x; i < n; i += 512) {
-    skey[i] = KeysFromIds<Id>{ids, vocab}.get(i);
+    check_id(ids[i], i, vocab, status);
+    skey[i] = KeysFromIds<Id>{ids, vocab, status}.get(i);
     sval[i] = i;
   }
   for (int p = 0; p < passes; ++p) {
@@ -381,11 +409,16 @@ embed_sort_small_kernel(const Id *ids, int n, int vocab, int passes, int bits, u
       const int i = warp * 256 + j * 32 + lane;
       if (i < n) {
         const int to = cnt[warp * kSortBins + ((k[j] >> shift) & (bins - 1))] + rank[j];
-        if (p == passes - 1) { key_out[to] = k[j]; val_out[to] = v[j]; }
-        else { skey[to] = k[j]; sval[to] = v[j]; }
+        skey[to] = k[j];
+        sval[to] = v[j];
       }
     }
     __syncthreads();
+  }
+  for (int i = threadIdx.x; i < n; i += 512) {
+    key_out[i] = skey[i];
+    val_out[i] = sval[i];
+    embed_mark(skey, i, vocab, seen);
   }
 }
 
@@ -396,7 +429,7 @@ embed_sort_small_kernel(const Id *ids, int n, int vocab, int passes, int bits, u
 // row's sums up in order.  Bound by HBM: every gradient row read once, every table row written once.  A thread has eight
 // columns and a block whole rows (up to 4096 columns), so reads and writes are runs of several KB.
 constexpr int kEmbedMaxThreads = 512;
-constexpr int kEmbedZeroRows = 16;      // table rows looked at by one block of the zero part
+constexpr int kEmbedZeroRows = 16;      // table rows looked at by one block of the zero part (half a word of `seen`)
 constexpr int kEmbedMaxChunk = 256;
 
 template <typename Out>
@@ -412,47 +445,17 @@ __device__ __forceinline__ void embed_store(Out *dst, float (&x)[8], float scale
   Vec<Out>::store(dst, x);
 }
 
-// Whether any token has id v: lower bound of v in the sorted keys, 32 probes a step by the lanes of a warp.
-__device__ __forceinline__ bool embed_has_tokens(const uint32_t *key, int n, uint32_t v, int lane) {
-  int lo = 0, hi = n;  // the lower bound is in [lo, hi]
-  while (hi - lo > 0) {
-    const int step = (hi - lo + 31) / 32;
-    const int at = lo + (lane + 1) * step - 1;                      // last place of the lane's share
-    const unsigned ge = __ballot_sync(0xffffffffu, at >= hi || key[at] >= v);
-    // the shares before the first one whose last key is >= v hold smaller keys only
-    const int first = ge ? __ffs(ge) - 1 : 32;
-    const int nlo = min(lo + first * step, hi), nhi = first < 32 ? min(lo + (first + 1) * step - 1, hi) : hi;
-    lo = nlo;
-    hi = max(nhi, nlo);
-  }
-  return lo < n && key[lo] == v;
-}
-
-// joins[0] counts the rows that cross chunks, joins[1 ..] are the chunks they start in (in any order: each row is joined alone).
-// It is cleared, and ids beyond the vocabulary are reported, by embed_clear_kernel, the first launch of the call.
-template <typename Id>
-__global__ void embed_clear_kernel(const Id *ids, int n, int vocab, int *joins, int *status) {
-  const int t = blockIdx.x * blockDim.x + threadIdx.x;
-  if (t == 0) joins[0] = 0;
-  if (t < n) check_id(ids[t], t, vocab, status);
-}
-
 template <typename In, typename Out>
 __global__ void __launch_bounds__(kEmbedMaxThreads)
 embed_sum_kernel(const In *d_out, const uint32_t *key, const int *val, int n, int chunk, int n_chunks, int vocab, int hidden,
-                 float scale, int accumulate, Out *d_table, float *part, int *joins) {
+                 float scale, int accumulate, Out *d_table, float *part, int *joins, const uint32_t *seen) {
   __shared__ uint32_t skey[kEmbedMaxChunk];
   __shared__ int sval[kEmbedMaxChunk];
   const int col = (blockIdx.y * blockDim.x + threadIdx.x) * 8;
   if ((int)blockIdx.x >= n_chunks) {
     // rows without tokens: zeros
-    const int v0 = ((int)blockIdx.x - n_chunks) * kEmbedZeroRows, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    if (threadIdx.x == 0) skey[0] = 0;
-    __syncthreads();
-    for (int i = warp; i < kEmbedZeroRows; i += blockDim.x / 32)
-      if (v0 + i < vocab && embed_has_tokens(key, n, (uint32_t)(v0 + i), lane) && lane == 0) atomicOr(&skey[0], 1u << i);
-    __syncthreads();
-    const uint32_t has = skey[0];
+    const int v0 = ((int)blockIdx.x - n_chunks) * kEmbedZeroRows;
+    const uint32_t has = n ? seen[v0 >> 5] >> (v0 & 31) : 0;
     const float zero[8] = {};
     if (col < hidden)
       for (int i = 0; i < kEmbedZeroRows && v0 + i < vocab; ++i)
@@ -466,7 +469,10 @@ embed_sum_kernel(const In *d_out, const uint32_t *key, const int *val, int n, in
   if (threadIdx.x == 0 && blockIdx.y == 0) {
     // the chunk's last row goes on, and does not come in (a chunk full of one row that comes in is in the middle of it)
     const uint32_t v = skey[m - 1];
-    if (v < (uint32_t)vocab && after == v && !(skey[0] == v && before == v)) joins[1 + atomicAdd(joins, 1)] = c;
+    if (v < (uint32_t)vocab && after == v && !(skey[0] == v && before == v)) {
+      if (c + kJoinShort < n_chunks && key[(c + kJoinShort) * chunk] == v) joins[1 + n_chunks - atomicAdd(joins + 1, 1)] = c;
+      else joins[2 + atomicAdd(joins, 1)] = c;
+    }
   }
   if (col >= hidden) return;
   float x[8] = {};
@@ -500,41 +506,74 @@ embed_sum_kernel(const In *d_out, const uint32_t *key, const int *val, int n, in
   }
 }
 
-// Rows that cross from one chunk into the next.  A block takes 256 columns of a row: 32 column vectors x 8 shares of the
-// row's sums, added up in order.
+// Rows that cross from one chunk into the next: slot 1 of the chunk c they start in, then slot 0 of the chunks behind it
+// whose first key is theirs, added up in order.  Most cross one border: a block takes 2048 columns of such a row, a thread
+// eight.  A long row is shared out over 32 column vectors x 8 shares of its sums.
 template <typename Out>
 __global__ void __launch_bounds__(256)
 embed_join_kernel(const uint32_t *key, int chunk, int n_chunks, int hidden, float scale, int accumulate, Out *d_table, const float *part,
                   const int *joins) {
-  __shared__ float sh[8][32][9];
+  __shared__ float sh[8][264];
   const int lane = threadIdx.x & 31, seg = threadIdx.x >> 5;
-  const int rows = joins[0], slabs = (hidden + 255) / 256;
-  for (int it = blockIdx.x; it < rows * slabs; it += gridDim.x) {
-    const int c = joins[1 + it / slabs];
-    const uint32_t v = key[(c + 1) * chunk];
-    int lo = c + 1, hi = n_chunks;  // last chunk whose first key is v: in [lo, hi)
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (key[mid * chunk] == v) lo = mid; else hi = mid;
-    }
-    const int count = lo - c + 1;   // sums of the row: slot 1 of chunk c, slot 0 of c + 1 .. lo
-    const int per = (count + 7) / 8;
-    const int col = it % slabs * 256 + lane * 8;
+  const int n_long = joins[1], s_long = (hidden + 255) / 256, items_long = n_long * s_long;
+  const int s_short = (hidden + 2047) / 2048, items = items_long + joins[0] * s_short;
+  for (int it = blockIdx.x; it < items; it += gridDim.x) {
     float x[8] = {};
-    if (col < hidden)
-      for (int i = seg * per; i < min(count, (seg + 1) * per); ++i) {
+    if (it >= items_long) {
+      const int c = joins[2 + (it - items_long) / s_short], col = (it - items_long) % s_short * 2048 + threadIdx.x * 8;
+      const uint32_t v = key[(c + 1) * chunk];
+      uint32_t next[kJoinShort];
+#pragma unroll
+      for (int i = 2; i < kJoinShort; ++i) next[i] = c + i < n_chunks ? key[(c + i) * chunk] : 0xffffffffu;
+      if (col >= hidden) continue;
+      const float *src = part + (long long)2 * c * hidden + col;
+      float y[kJoinShort][8];
+      Vec<float>::load(src + hidden, y[0]);
+      Vec<float>::load(src + (long long)2 * hidden, y[1]);
+#pragma unroll
+      for (int i = 2; i < kJoinShort; ++i)
+        if (next[i] == v) Vec<float>::load(src + (long long)2 * i * hidden, y[i]);
+#pragma unroll
+      for (int i = 0; i < kJoinShort; ++i)
+        if (i < 2 || next[i] == v)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] += y[i][e];
+      embed_store(d_table + (long long)v * hidden + col, x, scale, accumulate);
+      continue;
+    }
+    const int c = joins[1 + n_chunks - it / s_long], col = it % s_long * 256 + lane * 8;
+    const uint32_t v = key[(c + 1) * chunk];
+    int count = 1;
+    for (int b = c + 1;; b += 256) {
+      const int at = b + (int)threadIdx.x;
+      const int more = __syncthreads_count(at < n_chunks && key[at * chunk] == v);
+      count += more;
+      if (more < 256) break;
+    }
+    const int per = (count + 7) / 8, last = min(count, (seg + 1) * per);
+    if (col < hidden) {
+      const float *src = part + (long long)2 * c * hidden + col;
+      for (int i = seg * per; i < last; i += 8) {
+        float y[8][8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (i + e < last) Vec<float>::load(src + (long long)(i + e == 0 ? 1 : 2 * (i + e)) * hidden, y[e]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (i + e < last)
+#pragma unroll
+            for (int q = 0; q < 8; ++q) x[q] += y[e][q];
+      }
+    }
+    Vec<float>::store(&sh[seg][lane * 8], x);
+    __syncthreads();
+    if (seg == 0 && col < hidden) {
+      for (int s = 1; s < 8; ++s) {
         float y[8];
-        Vec<float>::load(part + (long long)(i == 0 ? 2 * c + 1 : 2 * (c + i)) * hidden + col, y);
+        Vec<float>::load(&sh[s][lane * 8], y);
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] += y[e];
       }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) sh[seg][lane][e] = x[e];
-    __syncthreads();
-    if (seg == 0 && col < hidden) {
-      for (int s = 1; s < 8; ++s)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] += sh[s][lane][e];
       embed_store(d_table + (long long)v * hidden + col, x, scale, accumulate);
     }
     __syncthreads();
