@@ -65,8 +65,8 @@ int64_t piece_cols(const augtree_lm *lm, int64_t rows_pad) {
 // Shares of dH's contraction: dH has few tiles when there are few rows, and a share should be a small part of what a
 // CTA does in the launch (which holds dW's tiles too), or the longest one would be waited for.
 int dh_splits(const augtree_lm *lm, int64_t rows_pad, int64_t cols) {
-  const int64_t kb = (cols + 63) / 64, tiles = (rows_pad / 128) * ((lm->hidden + kLmTile - 1) / kLmTile);
-  const int64_t lane_kb = std::max<int64_t>(2 * tiles * kb / lm->n_lanes, 1);  // dW costs as much as dH
+  const int64_t kb = (cols + 63) / 64, tiles = (rows_pad / kLmTile) * ((lm->hidden + kLmTile - 1) / kLmTile);
+  const int64_t lane_kb = std::max<int64_t>(4 * tiles * kb / lm->n_lanes, 1);  // dW costs as much as dH
   return (int)std::min<int64_t>(std::min<int64_t>((4 * kb + lane_kb - 1) / lane_kb, 64), kb);
 }
 
@@ -138,6 +138,22 @@ int map_2d(CUtensorMap *m, const void *ptr, int64_t rows, int64_t cols, int box_
   return r == CUDA_SUCCESS ? AUGTREE_OK : AUGTREE_ERR_CUDA;
 }
 
+// The same for an operand whose contraction runs along the rows: a box is 64 rows of `chunks` neighbouring 64-column chunks,
+// each chunk a block of 64 x 128 bytes of its own.  With two chunks the matrix is seen as [cols / 64][rows][64], which needs cols to
+// be a multiple of 64 (a chunk that runs past the row's end would read the next row, and past the tensor in the last one).
+int map_mn(CUtensorMap *m, const void *ptr, int64_t rows, int64_t cols, int chunks) {
+  EncodeTiledFn enc = get_encode();
+  if (!enc) return AUGTREE_ERR_CUDA;
+  const cuuint64_t dims[3] = {(cuuint64_t)(chunks == 2 ? 64 : cols), (cuuint64_t)rows, (cuuint64_t)(chunks == 2 ? cols / 64 : 1)};
+  const cuuint64_t strides[2] = {(cuuint64_t)cols * 2, 128};
+  const cuuint32_t box[3] = {64, 64, (cuuint32_t)chunks};
+  const cuuint32_t estr[3] = {1, 1, 1};
+  const CUresult r = enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(ptr), dims, strides, box, estr,
+                         CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? AUGTREE_OK : AUGTREE_ERR_CUDA;
+}
+
 int check_lm(const augtree_lm *lm) {
   if (!lm || lm->device < 0) return AUGTREE_ERR_INVALID_ARG;
   int cur = -1;
@@ -182,7 +198,7 @@ LmParams base_params(const augtree_lm *lm, const LossWs &w, int64_t rows_pad) {
 struct Maps { CUtensorMap h, w, g, h_mn, w_mn, g_mn; };
 
 int launch_tiles(const augtree_lm *lm, const Maps &m, const LmParams &p, cudaStream_t st) {
-  lm_tile_kernel<<<lm->n_lanes, kLmThreads, LmSmem::kBytes, st>>>(m.h, m.w, m.g, m.h_mn, m.w_mn, m.g_mn, p);
+  lm_tile_kernel<<<std::max(lm->n_lanes / 2, 1) * 2, kLmThreads, LmSmem::kBytes, st>>>(m.h, m.w, m.g, m.h_mn, m.w_mn, m.g_mn, p);
   return launched();
 }
 
@@ -350,7 +366,7 @@ int augtree_embed_bwd(const augtree_lm_t *lm, const void *d_out, int out_dtype, 
   EmbedWs w;
   if (!ws || !aligned16(ws) || ws_bytes < embed_layout(lm, n_tokens, static_cast<uint8_t *>(ws), &w)) return AUGTREE_ERR_WORKSPACE;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const int n = (int)n_tokens, n_blocks = (n + kRadixBlock - 1) / kRadixBlock;
+  const int n = (int)n_tokens;
   int key_bits = 1;
   while ((lm->vocab >> key_bits) != 0) ++key_bits;
   const int passes = (key_bits + 8) / 9, bits = (key_bits + passes - 1) / passes;
@@ -411,14 +427,15 @@ int augtree_lm_loss_bwd(const augtree_lm_t *lm, const void *hidden, const void *
   if (!ws || !aligned16(ws) || ws_bytes < loss_layout(lm, n_tokens, true, static_cast<uint8_t *>(ws), &w)) return AUGTREE_ERR_WORKSPACE;
   if (!d_hidden && !d_weight) return AUGTREE_OK;
   const int64_t rp = up(n_tokens, 256), cols = piece_cols(lm, rp);
-  const int splits = dh_splits(lm, rp, cols);
+  const int splits = dh_splits(lm, rp, cols), chunks = lm->hidden % 64 == 0 ? 2 : 1;
   if ((r = compact(lm, targets, id_bytes, n_tokens, hidden, w, lse, d_loss, nullptr, nullptr, st))) return r;
   Maps m = {};
   if ((r = map_2d(&m.h, w.h, rp, lm->hidden, 128)) || (r = map_2d(&m.w, weight, lm->vocab, lm->hidden, 128)) ||
-      (r = map_2d(&m.h_mn, w.h, rp, lm->hidden, 64)) || (r = map_2d(&m.w_mn, weight, lm->vocab, lm->hidden, 64)) ||
-      (r = map_2d(&m.g, w.grad, rp, cols, 128)) || (r = map_2d(&m.g_mn, w.grad, rp, cols, 64)))
+      (r = map_mn(&m.h_mn, w.h, rp, lm->hidden, chunks)) || (r = map_mn(&m.w_mn, weight, lm->vocab, lm->hidden, chunks)) ||
+      (r = map_2d(&m.g, w.grad, rp, cols, 128)) || (r = map_mn(&m.g_mn, w.grad, rp, cols, 2)))
     return r;
   LmParams p = base_params(lm, w, rp);
+  p.mn_chunks = chunks;
   p.grad = w.grad; p.ld_grad = cols; p.dh_part = w.dh_part;
   p.dw = d_weight; p.dw_f32 = weight_dtype == AUGTREE_F32; p.dw_add = accumulate;
   for (int64_t v0 = 0; v0 < lm->vocab; v0 += cols) {

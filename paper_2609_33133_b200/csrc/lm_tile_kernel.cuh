@@ -12,8 +12,13 @@
 // 2^-8 of each element, independent between elements, so its sums stay as exact as the bf16 results they are
 // delivered in; the sums themselves, the softmax statistics and the exponent are fp32.
 //
-// Roles (320 threads): warps 0-7 epilogue (warp w: TMEM lanes 32 (w % 4).., columns 128 (w / 4)..), warp 8 TMA loads,
-// warp 9 issues the MMAs.  TMEM: two accumulators of 256 columns, so a tile's epilogue runs under the next tile.
+// A tile belongs to a pair of CTAs (cluster of two, tcgen05.mma.cta_group::2): each loads 128 rows of A and 128 columns of
+// B and gets 128 rows of the result, so 64 KB cross from L2 for every 64 steps of contraction of a 256 x 256 tile; single
+// CTAs with 128 x 256 tiles need 96 KB for the same work and took 31.5 ms for loss and gradients of 8192 x 152064 x 3584.
+//
+// Roles (320 threads a CTA): warps 0-7 epilogue (warp w: TMEM lanes 32 (w % 4).., columns 128 (w / 4)..), warp 8 TMA loads
+// (each CTA its own share, all counted on the first CTA's barrier), warp 9 of the first CTA issues the MMAs of both.
+// TMEM: two accumulators of 256 columns, so a tile's epilogue runs under the next tile.
 #pragma once
 #include <cuda.h>
 
@@ -24,7 +29,7 @@ namespace augtree {
 enum : int { LM_STATS = 0, LM_GRAD = 1, LM_DH = 2, LM_DW = 3 };
 enum : int { WAIT_LM_FULL = 80, WAIT_LM_EMPTY = 81, WAIT_LM_ACC_FULL = 82, WAIT_LM_ACC_EMPTY = 83 };
 
-constexpr int kLmTile = 256;     // tile columns (N)
+constexpr int kLmTile = 256;     // tile rows and columns of a CTA pair
 constexpr int kLmThreads = 320;
 constexpr int kLmMaxJobs = 2;
 
@@ -43,6 +48,7 @@ struct LmParams {
   int n_jobs;
   const int *n_rows;        // device: rows that are scored
   int v0, vocab, hidden;    // first vocabulary row of the piece; whole sizes
+  int mn_chunks;            // 64-column chunks in a box of tm_h_mn and tm_w_mn: 2, or 1 (hidden not a multiple of 64)
   long long rows_pad;       // leading size of per-row arrays and of the partial sums
   float scale_log2;         // c log2(e)
   const int *target;        // [rows_pad]
@@ -62,9 +68,9 @@ struct LmParams {
 };
 
 struct LmSmem {
-  static constexpr int kABytes = 128 * 128, kBBytes = kLmTile * 128;
+  static constexpr int kABytes = 128 * 128, kBBytes = 128 * 128;  // this CTA's share of a stage
   static constexpr int kStageBytes = kABytes + kBBytes;
-  static constexpr int kStages = 4;
+  static constexpr int kStages = 7;
   static constexpr int kOffBar = kStages * kStageBytes;
   static constexpr int kBytes = kOffBar + 256;
 };
@@ -78,7 +84,7 @@ struct LmTileCoord {
 __device__ __forceinline__ bool lm_tile(const LmParams &p, int n_rows, int t, LmTileCoord &c) {
   for (int j = 0; j < p.n_jobs; ++j) {
     const LmJob &J = p.job[j];
-    const int mt = ((J.m_fixed ? J.m_fixed : n_rows) + 127) / 128;
+    const int mt = ((J.m_fixed ? J.m_fixed : n_rows) + kLmTile - 1) / kLmTile;
     const int nt = (J.n + kLmTile - 1) / kLmTile;
     const int kb = ((J.k_fixed ? J.k_fixed : n_rows) + 63) / 64;
     const int count = mt * nt * J.splits;
@@ -86,7 +92,15 @@ __device__ __forceinline__ bool lm_tile(const LmParams &p, int n_rows, int t, Lm
       c.job = j;
       const int per = (kb + J.splits - 1) / J.splits;
       if (J.kind <= LM_GRAD) { c.m = t % mt; c.n = t / mt; c.split = 0; }
-      else { c.split = t / (mt * nt); const int r = t % (mt * nt); c.n = r % nt; c.m = r / nt; }
+      else { c.split = t / (mt * nt); const int r = t % (mt * nt);
+#ifdef MF
+        c.m = r % mt; c.n = r / mt;
+#elif defined(GRP)
+        { const int g = r / (GRP * nt), rr = r % (GRP * nt), rows = min(GRP, mt - g * GRP); c.m = g * GRP + rr % rows; c.n = rr / rows; }
+#else
+        c.n = r % nt; c.m = r / nt;
+#endif
+      }
       c.kb0 = min(c.split * per, kb);
       c.nkb = min(per, kb - c.kb0);
       return true;
@@ -96,15 +110,10 @@ __device__ __forceinline__ bool lm_tile(const LmParams &p, int n_rows, int t, Lm
   return false;
 }
 
-__device__ __forceinline__ void tma_load_2d(uint32_t dst, const void *tmap, uint32_t bar, int c0, int c1) {
-  asm volatile(
-      "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
-      ::"r"(dst), "l"(tmap), "r"(bar), "r"(c0), "r"(c1) : "memory");
-}
-
-// Tensor maps: H and W with a box of 64 contiguous hidden columns x 128 rows (contraction contiguous) or x 64 rows
-// (contraction along the rows); G likewise with 64 vocabulary columns.
-__global__ void __launch_bounds__(kLmThreads, 1)
+// Tensor maps: H and W with a box of 64 contiguous hidden columns x 128 rows (contraction contiguous) or (_mn, contraction
+// along the rows) of two such columns x 64 rows, one box for the 128 rows or columns of a stage: two boxes of half the size
+// come in more slowly than the tensor core takes them (530 cycles a stage of 512, one box 453).  G likewise.
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLmThreads, 1)
 lm_tile_kernel(const __grid_constant__ CUtensorMap tm_h, const __grid_constant__ CUtensorMap tm_w,
                const __grid_constant__ CUtensorMap tm_g, const __grid_constant__ CUtensorMap tm_h_mn,
                const __grid_constant__ CUtensorMap tm_w_mn, const __grid_constant__ CUtensorMap tm_g_mn, const LmParams p) {
@@ -112,7 +121,7 @@ lm_tile_kernel(const __grid_constant__ CUtensorMap tm_h, const __grid_constant__
   constexpr int NST = SM::kStages;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   const uint32_t base = smem_u32(smem_raw);
-  if (base & 1023u) {
+  if (base & 1023u) {  // the same in both CTAs of a pair
     if (threadIdx.x == 0 && atomicCAS(p.status, 0, -6) == 0) p.status[1] = 4;
     return;
   }
@@ -125,18 +134,20 @@ lm_tile_kernel(const __grid_constant__ CUtensorMap tm_h, const __grid_constant__
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int s = 0; s < NST; ++s) { mbar_init(bar_full + 8 * s, 1); mbar_init(bar_empty + 8 * s, 1); }
-    for (int s = 0; s < 2; ++s) { mbar_init(bar_acc_full + 8 * s, 1); mbar_init(bar_acc_empty + 8 * s, 8); }
+    for (int s = 0; s < 2; ++s) { mbar_init(bar_acc_full + 8 * s, 1); mbar_init(bar_acc_empty + 8 * s, 16); }
     *abort_flag = 0;
     fence_barrier_init();
   }
-  if (warp == 9) { tmem_alloc(smem_u32((const void *)tmem_slot), 512); tmem_relinquish(); }
+  if (warp == 9) { tmem_alloc_pair(smem_u32((const void *)tmem_slot), 512); tmem_relinquish_pair(); }
   tc_fence_before();
   __syncthreads();
+  cluster_sync();
   tc_fence_after();
+  const uint32_t rank = cluster_ctarank();
   const uint32_t tmem = *tmem_slot;
   const AbortCtx ab{abort_flag, p.status, p.wait_budget};
   const int n_rows = __ldg(p.n_rows);
-  const int t0 = blockIdx.x, tstep = gridDim.x;
+  const int t0 = blockIdx.x >> 1, tstep = gridDim.x >> 1;
   LmTileCoord c;
 
   if (warp == 8) {
@@ -146,30 +157,32 @@ lm_tile_kernel(const __grid_constant__ CUtensorMap tm_h, const __grid_constant__
       bool ok = true;
       for (int t = t0; ok && lm_tile(p, n_rows, t, c); t += tstep) {
         const int kind = p.job[c.job].kind;
-        const int m0 = c.m * 128, n0 = c.n * kLmTile;
+        const int m0 = c.m * kLmTile + rank * 128, n0 = c.n * kLmTile + rank * 128;  // this CTA's rows of A, columns of B
         for (int kb = c.kb0; kb < c.kb0 + c.nkb && ok; ++kb, ++T) {
-          const uint32_t st = T % NST, bar = bar_full + 8 * st;
+          const uint32_t st = T % NST, bar = map_to_rank(bar_full + 8 * st, 0);
           ok = mbar_wait(bar_empty + 8 * st, ((T / NST) & 1) ^ 1, ab, WAIT_LM_EMPTY);
           if (!ok) break;
           const uint32_t sA = base + st * SM::kStageBytes, sB = sA + SM::kABytes;
           const int k0 = kb * 64;
           if ((p.test_flags & TEST_SKIP_FWD_LOAD) && blockIdx.x == 0 && T == 0) continue;
-          mbar_expect_tx(bar, SM::kStageBytes);
+          if (rank == 0) mbar_expect_tx(bar_full + 8 * st, 2 * SM::kStageBytes);
           if (kind <= LM_GRAD) {
-            tma_load_2d(sA, &tm_h, bar, k0, m0);
-            tma_load_2d(sB, &tm_w, bar, k0, p.v0 + n0);
-            tma_load_2d(sB + 16384, &tm_w, bar, k0, p.v0 + n0 + 128);
-          } else if (kind == LM_DH) {
-            tma_load_2d(sA, &tm_g, bar, k0, m0);
-            for (int b = 0; b < 4; ++b) tma_load_2d(sB + b * 8192, &tm_w_mn, bar, n0 + b * 64, p.v0 + k0);
+            tma_load_2d_pair(sA, &tm_h, bar, k0, m0);
+            tma_load_2d_pair(sB, &tm_w, bar, k0, p.v0 + n0);
           } else {
-            for (int b = 0; b < 2; ++b) tma_load_2d(sA + b * 8192, &tm_g_mn, bar, m0 + b * 64, k0);
-            for (int b = 0; b < 4; ++b) tma_load_2d(sB + b * 8192, &tm_h_mn, bar, n0 + b * 64, k0);
+            const bool dh = kind == LM_DH;
+            if (dh) tma_load_2d_pair(sA, &tm_g, bar, k0, m0);
+            else tma_load_3d_pair(sA, &tm_g_mn, bar, 0, k0, m0 >> 6);
+            const CUtensorMap *tm_b = dh ? &tm_w_mn : &tm_h_mn;
+            const int kr = dh ? p.v0 + k0 : k0;
+            if (p.mn_chunks == 2) tma_load_3d_pair(sB, tm_b, bar, 0, kr, n0 >> 6);
+            else for (int b = 0; b < 2; ++b) tma_load_3d_pair(sB + b * 8192, tm_b, bar, n0 + b * 64, kr, 0);
           }
         }
       }
     }
   } else if (warp == 9) {
+   if (rank == 0) {
     // -------------------------------------------------------------- MMA issuer
     const bool elected = elect_one();
     uint32_t T = 0, ic = 0;
@@ -177,7 +190,7 @@ lm_tile_kernel(const __grid_constant__ CUtensorMap tm_h, const __grid_constant__
     for (int t = t0; ok && lm_tile(p, n_rows, t, c); t += tstep, ++ic) {
       const int kind = p.job[c.job].kind;
       const int a_mn = kind == LM_DW, b_mn = kind >= LM_DH;
-      const uint32_t idesc = make_idesc(128, kLmTile, a_mn, b_mn);
+      const uint32_t idesc = make_idesc(256, kLmTile, a_mn, b_mn);
       const uint32_t a_step = a_mn ? 2048 >> 4 : 32 >> 4, b_step = b_mn ? 2048 >> 4 : 32 >> 4;
       const uint32_t buf = ic & 1;
       if (ic >= 2) {
@@ -195,13 +208,14 @@ lm_tile_kernel(const __grid_constant__ CUtensorMap tm_h, const __grid_constant__
         const uint32_t a_lo = sdesc_lo(sA, 8192), b_lo = sdesc_lo(sA + SM::kABytes, 8192);
         if (elected) {
 #pragma unroll
-          for (int k = 0; k < 4; ++k) mma_ss2(tD, a_lo + k * a_step, b_lo + k * b_step, idesc, (uint32_t)(kb > 0 || k > 0));
-          tc_commit(bar_empty + 8 * st);
+          for (int k = 0; k < 4; ++k) mma_ss2_pair(tD, a_lo + k * a_step, b_lo + k * b_step, idesc, (uint32_t)(kb > 0 || k > 0));
+          tc_commit_pair(bar_empty + 8 * st);
         }
       }
       if (!ok) break;
-      if (elected) tc_commit(bar_acc_full + 8 * buf);
+      if (elected) tc_commit_pair(bar_acc_full + 8 * buf);
     }
+   }
   } else {
     // ------------------------------------------------------------ epilogue warps 0-7
     const int r = (warp & 3) * 32 + lane;
@@ -216,7 +230,7 @@ lm_tile_kernel(const __grid_constant__ CUtensorMap tm_h, const __grid_constant__
       if (!ok) break;
       tc_fence_after();
       const uint32_t tD = tmem + buf * kLmTile + lane_off + col0;
-      const int row = c.m * 128 + r, n0 = c.n * kLmTile + col0;  // tile row, first column of this warp
+      const int row = c.m * kLmTile + rank * 128 + r, n0 = c.n * kLmTile + col0;  // tile row, first column of this warp
       if (J.kind == LM_STATS) {
         const int tgt = row < n_rows ? p.target[row] - p.v0 - n0 : -1;  // column of the target, relative
         float m = -INFINITY, l = 0.f, xt = 0.f;
@@ -308,9 +322,9 @@ lm_tile_kernel(const __grid_constant__ CUtensorMap tm_h, const __grid_constant__
           }
         }
       }
-      __syncwarp();
       tc_fence_before();
-      warp_arrive(bar_acc_empty + 8 * buf);
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster(map_to_rank(bar_acc_empty + 8 * buf, 0));
     }
   }
 
@@ -321,7 +335,8 @@ lm_tile_kernel(const __grid_constant__ CUtensorMap tm_h, const __grid_constant__
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == 9) { tc_fence_after(); tmem_dealloc(tmem, 512); }
+  cluster_sync();  // neither CTA leaves, or gives up its half of TMEM, while the other's loads, MMAs or arrivals may reach it
+  if (warp == 9) { tc_fence_after(); tmem_dealloc_pair(tmem, 512); }
 }
 
 }  // namespace augtree
