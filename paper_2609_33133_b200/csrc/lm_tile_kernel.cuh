@@ -92,14 +92,7 @@ __device__ __forceinline__ bool lm_tile(const LmParams &p, int n_rows, int t, Lm
       c.job = j;
       const int per = (kb + J.splits - 1) / J.splits;
       if (J.kind <= LM_GRAD) { c.m = t % mt; c.n = t / mt; c.split = 0; }
-      else { c.split = t / (mt * nt); const int r = t % (mt * nt);
-#ifdef MF
-        c.m = r % mt; c.n = r / mt;
-#elif defined(GRP)
-        { const int g = r / (GRP * nt), rr = r % (GRP * nt), rows = min(GRP, mt - g * GRP); c.m = g * GRP + rr % rows; c.n = rr / rows; }
-#else
-        c.n = r % nt; c.m = r / nt;
-#endif
+      else { c.split = t / (mt * nt); const int r = t % (mt * nt); c.n = r % nt; c.m = r / nt;
       }
       c.kb0 = min(c.split * per, kb);
       c.nkb = min(per, kb - c.kb0);
