@@ -6,6 +6,7 @@
 #include <new>
 
 #include "launch.h"
+#include "lm_few_kernel.cuh"
 #include "lm_kernels.cuh"
 #include "lm_tile_kernel.cuh"
 #include "../../include/augtree.h"
@@ -52,6 +53,11 @@ struct LossWs {
 
 int n_part(const augtree_lm *lm) { return 2 * (int)((lm->vocab + kLmTile - 1) / kLmTile); }
 
+// Few rows take kernels of their own (lm_few_kernel.cuh): the MMAs' N, 0 for many rows.
+int few_rows(int64_t tokens) { return tokens <= 16 ? 16 : tokens <= 32 ? 32 : tokens <= 64 ? 64 : tokens <= kLmFew ? 128 : 0; }
+// rows of the packed hidden states and of G in the scratch
+int64_t pad_rows(int64_t tokens) { return few_rows(tokens) ? 2 * few_rows(tokens) : up(tokens, 256); }
+
 // Columns of a piece of the vocabulary in the backward pass: as many as fit the scratch bound for G, in equal pieces.
 // With the default bound a piece has 4096 columns at least, so that the additions into dH's partial sums, one per
 // piece, stay a small part of the piece's products however many rows there are.
@@ -70,8 +76,14 @@ int dh_splits(const augtree_lm *lm, int64_t rows_pad, int64_t cols) {
   return (int)std::min<int64_t>(std::min<int64_t>((4 * kb + lane_kb - 1) / lane_kb, 64), kb);
 }
 
+// Few rows: shares of the vocabulary that fill the CTAs in one go.
+int few_splits(const augtree_lm *lm, int64_t cols) {
+  const int64_t tiles = (lm->hidden + 127) / 128;
+  return (int)std::min<int64_t>(std::max<int64_t>(lm->n_lanes / tiles, 1), (cols + 63) / 64);
+}
+
 size_t loss_layout(const augtree_lm *lm, int64_t tokens, bool bwd, uint8_t *base, LossWs *w) {
-  const int64_t rp = up(std::max<int64_t>(tokens, 1), 256);
+  const int64_t few = few_rows(tokens), rp = pad_rows(tokens);
   Cursor c{base};
   w->rows.n_rows = c.take<int>(1);
   w->rows.idx = c.take<int>(rp);
@@ -81,13 +93,13 @@ size_t loss_layout(const augtree_lm *lm, int64_t tokens, bool bwd, uint8_t *base
   if (!bwd) {
     w->rows.lse2 = w->rows.gscale = nullptr;
     w->tlogit = c.take<float>(rp);
-    w->part = c.take<float2>((int64_t)n_part(lm) * rp);
+    w->part = c.take<float2>(few ? 4ll * lm->n_lanes * few : (int64_t)n_part(lm) * rp);
   } else {
     const int64_t cols = piece_cols(lm, rp);
     w->rows.lse2 = c.take<float>(rp);
     w->rows.gscale = c.take<float>(rp);
     w->grad = c.take<__nv_bfloat16>(rp * cols);
-    w->dh_part = c.take<float>((int64_t)dh_splits(lm, rp, cols) * rp * lm->hidden);
+    w->dh_part = c.take<float>((few ? few_splits(lm, cols) * few : dh_splits(lm, rp, cols) * rp) * lm->hidden);
   }
   return c.off;
 }
@@ -154,6 +166,20 @@ int map_mn(CUtensorMap *m, const void *ptr, int64_t rows, int64_t cols, int chun
   return r == CUDA_SUCCESS ? AUGTREE_OK : AUGTREE_ERR_CUDA;
 }
 
+// Map for results that leave through shared memory: a box is 128 bytes (swizzled) x 32 rows.
+int map_out(CUtensorMap *m, const void *ptr, int64_t rows, int64_t cols, bool f32) {
+  EncodeTiledFn enc = get_encode();
+  if (!enc) return AUGTREE_ERR_CUDA;
+  const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+  const cuuint64_t strides[1] = {(cuuint64_t)cols * (f32 ? 4 : 2)};
+  const cuuint32_t box[2] = {f32 ? 32u : 64u, 32};
+  const cuuint32_t estr[2] = {1, 1};
+  const CUresult r = enc(m, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(ptr), dims, strides, box,
+                         estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? AUGTREE_OK : AUGTREE_ERR_CUDA;
+}
+
 int check_lm(const augtree_lm *lm) {
   if (!lm || lm->device < 0) return AUGTREE_ERR_INVALID_ARG;
   int cur = -1;
@@ -168,6 +194,17 @@ int launched() {
 
 int compact(const augtree_lm *lm, const void *targets, int id_bytes, int64_t tokens, const void *hidden, const LossWs &w,
             const float *lse, const float *d_loss, float *loss_out, float *lse_out, cudaStream_t st) {
+  if (const int few = few_rows(tokens)) {
+    const uint4 *src = static_cast<const uint4 *>(hidden);
+    uint4 *dst = reinterpret_cast<uint4 *>(w.h);
+    if (id_bytes == 8)
+      lm_few_rows_kernel<<<few, 128, 0, st>>>(static_cast<const long long *>(targets), (int)tokens, lm->vocab, w.rows, lse, d_loss, lm->logit_scale,
+                                              loss_out, lse_out, lm->d_status, src, dst, lm->hidden / 8, lse != nullptr);
+    else
+      lm_few_rows_kernel<<<few, 128, 0, st>>>(static_cast<const int *>(targets), (int)tokens, lm->vocab, w.rows, lse, d_loss, lm->logit_scale,
+                                              loss_out, lse_out, lm->d_status, src, dst, lm->hidden / 8, lse != nullptr);
+    return launched();
+  }
   if (id_bytes == 8)
     lm_compact_kernel<<<1, 1024, 0, st>>>(static_cast<const long long *>(targets), (int)tokens, lm->vocab, w.rows, lse, d_loss,
                                           lm->logit_scale, loss_out, lse_out, lm->d_status);
@@ -195,11 +232,44 @@ LmParams base_params(const augtree_lm *lm, const LossWs &w, int64_t rows_pad) {
   return p;
 }
 
-struct Maps { CUtensorMap h, w, g, h_mn, w_mn, g_mn; };
+struct Maps { CUtensorMap h, w, g, h_mn, w_mn, g_mn, out, dh; };
 
 int launch_tiles(const augtree_lm *lm, const Maps &m, const LmParams &p, cudaStream_t st) {
-  lm_tile_kernel<<<std::max(lm->n_lanes / 2, 1) * 2, kLmThreads, LmSmem::kBytes, st>>>(m.h, m.w, m.g, m.h_mn, m.w_mn, m.g_mn, p);
+  lm_tile_kernel<<<std::max(lm->n_lanes / 2, 1) * 2, kLmThreads, LmSmem::kBytes, st>>>(m.h, m.w, m.g, m.h_mn, m.w_mn, m.g_mn, m.out, m.dh, p);
   return launched();
+}
+
+template <int KIND, int N>
+int launch_few_n(const augtree_lm *lm, const CUtensorMap &mw, const CUtensorMap &mb, const FewParams &p, cudaStream_t st) {
+  lm_few_kernel<KIND, N><<<lm->n_lanes, kFewThreads, FewSmem<KIND, N>::kBytes, st>>>(mw, mb, p);
+  return launched();
+}
+template <int KIND>
+int launch_few(const augtree_lm *lm, int few, const CUtensorMap &mw, const CUtensorMap &mb, const FewParams &p, cudaStream_t st) {
+  switch (few) {
+    case 16: return launch_few_n<KIND, 16>(lm, mw, mb, p, st);
+    case 32: return launch_few_n<KIND, 32>(lm, mw, mb, p, st);
+    case 64: return launch_few_n<KIND, 64>(lm, mw, mb, p, st);
+    default: return launch_few_n<KIND, 128>(lm, mw, mb, p, st);
+  }
+}
+template <int KIND>
+int few_attributes() {
+  const cudaFuncAttribute a = cudaFuncAttributeMaxDynamicSharedMemorySize;
+  return cudaFuncSetAttribute(lm_few_kernel<KIND, 16>, a, FewSmem<KIND, 16>::kBytes) == cudaSuccess &&
+                 cudaFuncSetAttribute(lm_few_kernel<KIND, 32>, a, FewSmem<KIND, 32>::kBytes) == cudaSuccess &&
+                 cudaFuncSetAttribute(lm_few_kernel<KIND, 64>, a, FewSmem<KIND, 64>::kBytes) == cudaSuccess &&
+                 cudaFuncSetAttribute(lm_few_kernel<KIND, 128>, a, FewSmem<KIND, 128>::kBytes) == cudaSuccess
+             ? AUGTREE_OK : AUGTREE_ERR_CUDA;
+}
+
+FewParams few_params(const augtree_lm *lm, const LossWs &w, const LmParams &b) {
+  FewParams p = {};
+  p.n_rows = b.n_rows; p.vocab = b.vocab; p.hidden = b.hidden; p.scale_log2 = b.scale_log2;
+  p.target = b.target; p.lse2 = b.lse2; p.gscale = b.gscale;
+  p.part = w.part; p.tlogit = w.tlogit; p.grad = w.grad; p.dh_part = w.dh_part;
+  p.status = b.status; p.wait_budget = b.wait_budget; p.test_flags = b.test_flags;
+  return p;
 }
 
 template <typename Id, typename In>
@@ -308,6 +378,7 @@ int augtree_lm_create(const augtree_lm_desc_t *desc, int device, augtree_lm_t **
       else if (lm->n_lanes == 0) lm->n_lanes = sms;
     }
     if (!r && cudaFuncSetAttribute(lm_tile_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, LmSmem::kBytes) != cudaSuccess) r = AUGTREE_ERR_CUDA;
+    if (!r && !(r = few_attributes<LM_STATS>()) && !(r = few_attributes<LM_GRAD>())) r = few_attributes<LM_DH>();
     if (!r && (cudaFuncSetAttribute(embed_sort_small_kernel<int>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSortSmallBytes) != cudaSuccess ||
                cudaFuncSetAttribute(embed_sort_small_kernel<long long>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSortSmallBytes) != cudaSuccess))
       r = AUGTREE_ERR_CUDA;
@@ -392,9 +463,18 @@ int augtree_lm_loss_fwd(const augtree_lm_t *lm, const void *hidden, const void *
   LossWs w;
   if (!ws || !aligned16(ws) || ws_bytes < loss_layout(lm, n_tokens, false, static_cast<uint8_t *>(ws), &w)) return AUGTREE_ERR_WORKSPACE;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const int64_t rp = up(n_tokens, 256);
+  const int64_t rp = pad_rows(n_tokens);
+  const int few = few_rows(n_tokens);
   if ((r = compact(lm, targets, id_bytes, n_tokens, hidden, w, nullptr, nullptr, loss, lse, st))) return r;
   Maps m = {};
+  if (few) {
+    FewParams p = few_params(lm, w, base_params(lm, w, few));
+    p.n = lm->vocab;
+    if ((r = map_2d(&m.h, w.h, few, lm->hidden, few)) || (r = map_2d(&m.w, weight, lm->vocab, lm->hidden, 128))) return r;
+    if ((r = launch_few<LM_STATS>(lm, few, m.w, m.h, p, st))) return r;
+    lm_few_finish_kernel<<<few, 256, 0, st>>>(w.part, 4 * lm->n_lanes, w.rows.n_rows, w.rows.idx, w.tlogit, lm->logit_scale, loss, lse);
+    return launched();
+  }
   if ((r = map_2d(&m.h, w.h, rp, lm->hidden, 128)) || (r = map_2d(&m.w, weight, lm->vocab, lm->hidden, 128))) return r;
   LmParams p = base_params(lm, w, rp);
   p.n_jobs = 1;
@@ -426,33 +506,49 @@ int augtree_lm_loss_bwd(const augtree_lm_t *lm, const void *hidden, const void *
   LossWs w;
   if (!ws || !aligned16(ws) || ws_bytes < loss_layout(lm, n_tokens, true, static_cast<uint8_t *>(ws), &w)) return AUGTREE_ERR_WORKSPACE;
   if (!d_hidden && !d_weight) return AUGTREE_OK;
-  const int64_t rp = up(n_tokens, 256), cols = piece_cols(lm, rp);
-  const int splits = dh_splits(lm, rp, cols), chunks = lm->hidden % 64 == 0 ? 2 : 1;
+  const int few = few_rows(n_tokens);
+  const int64_t rp = pad_rows(n_tokens), cols = piece_cols(lm, rp);
+  const int splits = few ? few_splits(lm, cols) : dh_splits(lm, rp, cols), chunks = lm->hidden % 64 == 0 ? 2 : 1;
   if ((r = compact(lm, targets, id_bytes, n_tokens, hidden, w, lse, d_loss, nullptr, nullptr, st))) return r;
   Maps m = {};
-  if ((r = map_2d(&m.h, w.h, rp, lm->hidden, 128)) || (r = map_2d(&m.w, weight, lm->vocab, lm->hidden, 128)) ||
+  if ((r = map_2d(&m.h, w.h, rp, lm->hidden, few ? few : 128)) || (r = map_2d(&m.w, weight, lm->vocab, lm->hidden, 128)) ||
       (r = map_mn(&m.h_mn, w.h, rp, lm->hidden, chunks)) || (r = map_mn(&m.w_mn, weight, lm->vocab, lm->hidden, chunks)) ||
-      (r = map_2d(&m.g, w.grad, rp, cols, 128)) || (r = map_mn(&m.g_mn, w.grad, rp, cols, 2)))
+      (r = map_2d(&m.g, w.grad, rp, cols, few ? 2 * few : 128)) || (r = map_mn(&m.g_mn, w.grad, rp, cols, 2)))
     return r;
   LmParams p = base_params(lm, w, rp);
   p.mn_chunks = chunks;
-  p.grad = w.grad; p.ld_grad = cols; p.dh_part = w.dh_part;
-  p.dw = d_weight; p.dw_f32 = weight_dtype == AUGTREE_F32; p.dw_add = accumulate;
+  p.dw_f32 = weight_dtype == AUGTREE_F32; p.dw_add = accumulate;
+  CUtensorMap out_g, out_dw;
+  if (!few && ((r = map_out(&out_g, w.grad, rp, cols, false)) || (r = map_out(&m.dh, w.dh_part, splits * rp, lm->hidden, true)))) return r;
+  if (d_weight && (r = map_out(&out_dw, d_weight, lm->vocab, lm->hidden, p.dw_f32))) return r;
+  FewParams f = few_params(lm, w, p);
+  f.ld_grad = cols; f.splits = splits; f.mn_chunks = chunks;
   for (int64_t v0 = 0; v0 < lm->vocab; v0 += cols) {
     const int n = (int)std::min<int64_t>(cols, lm->vocab - v0);
-    p.v0 = (int)v0;
-    p.n_jobs = 1;
-    p.job[0] = {LM_GRAD, 0, n, lm->hidden, 1};
-    if ((r = launch_tiles(lm, m, p, st))) return r;
+    p.v0 = f.v0 = (int)v0;
+    p.dh_add = f.dh_add = v0 > 0;
+    f.n = n;
     p.n_jobs = 0;
-    p.dh_add = v0 > 0;
-    if (d_hidden) p.job[p.n_jobs++] = {LM_DH, 0, lm->hidden, n, splits};
-    if (d_weight) p.job[p.n_jobs++] = {LM_DW, n, lm->hidden, 0, 1};
-    if ((r = launch_tiles(lm, m, p, st))) return r;
+    if (few) {
+      if ((r = launch_few<LM_GRAD>(lm, few, m.w, m.h, f, st))) return r;
+      if (d_hidden && (r = launch_few<LM_DH>(lm, few, m.w_mn, m.g, f, st))) return r;
+      // both halves of G: the rows of the packed hidden states are there twice
+      if (d_weight) p.job[p.n_jobs++] = {LM_DW, n, lm->hidden, (int)rp, 1};
+    } else {
+      p.n_jobs = 1;
+      p.job[0] = {LM_GRAD, 0, n, lm->hidden, 1};
+      m.out = out_g;
+      if ((r = launch_tiles(lm, m, p, st))) return r;
+      p.n_jobs = 0;
+      if (d_hidden) p.job[p.n_jobs++] = {LM_DH, 0, lm->hidden, n, splits};
+      if (d_weight) p.job[p.n_jobs++] = {LM_DW, n, lm->hidden, 0, 1};
+    }
+    if (d_weight) m.out = out_dw;
+    if (p.n_jobs && (r = launch_tiles(lm, m, p, st))) return r;
   }
   if (d_hidden) {
     const unsigned grid = (unsigned)std::min<int64_t>(n_tokens, 16 * lm->n_lanes);
-    lm_dh_kernel<<<grid, 256, 0, st>>>(w.dh_part, splits, rp, lm->hidden, w.rows.pos, (int)n_tokens, static_cast<__nv_bfloat16 *>(d_hidden));
+    lm_dh_kernel<<<grid, 256, 0, st>>>(w.dh_part, splits, few ? few : rp, lm->hidden, w.rows.pos, (int)n_tokens, static_cast<__nv_bfloat16 *>(d_hidden));
     return launched();
   }
   return AUGTREE_OK;

@@ -82,7 +82,81 @@ lm_gather_kernel(const uint4 *hidden, const int *idx, const int *n_rows, uint4 *
   }
 }
 
+// Both for up to 128 tokens in one launch: a block per packed row, each finds its token for itself.  With `twice` the rows are
+// written a second time behind the first N (they multiply the two halves of G, see lm_few_kernel.cuh).
+template <typename Id>
+__global__ void __launch_bounds__(128)
+lm_few_rows_kernel(const Id *targets, int tokens, int vocab, LmRows o, const float *lse, const float *d_loss, float logit_scale,
+                   float *loss_out, float *lse_out, int *status, const uint4 *hidden, uint4 *out, int row_vecs, int twice) {
+  __shared__ int warp_sum[4];
+  __shared__ int from;
+  const int t = threadIdx.x, lane = t & 31, warp = t >> 5, row = blockIdx.x;
+  const long long id = t < tokens ? (long long)targets[t] : -1;
+  const bool live = id >= 0 && id < vocab;
+  const unsigned m = __ballot_sync(0xffffffffu, live);
+  if (lane == 0) warp_sum[warp] = __popc(m);
+  if (t == 0) from = -1;
+  __syncthreads();
+  int r = __popc(m & ((1u << lane) - 1)), n = 0;
+  for (int w = 0; w < 4; ++w) {
+    if (w < warp) r += warp_sum[w];
+    n += warp_sum[w];
+  }
+  if (live && r == row) from = t;
+  if (row == 0) {
+    check_id(id, t, vocab, status);
+    if (t < tokens) o.pos[t] = live ? r : -1;
+    if (live) {
+      o.idx[r] = t;
+      o.target[r] = (int)id;
+      if (lse) {
+        o.lse2[r] = lse[t] * 1.4426950408889634f;
+        o.gscale[r] = d_loss[t] * logit_scale;
+      }
+    } else if (t < tokens && loss_out) {
+      loss_out[t] = 0.f;
+      lse_out[t] = 0.f;
+    }
+    if (t == 0) *o.n_rows = n;
+  }
+  __syncthreads();
+  const uint4 *src = from >= 0 ? hidden + (long long)from * row_vecs : nullptr;
+  for (int i = t; i < row_vecs; i += 128) {
+    const uint4 v = src ? __ldg(src + i) : make_uint4(0, 0, 0, 0);
+    out[(long long)row * row_vecs + i] = v;
+    if (twice) out[(long long)(gridDim.x + row) * row_vecs + i] = v;
+  }
+}
+
 // ---------------------------------------------------------------- row statistics
+__device__ __forceinline__ float2 merge_stats(float2 a, float2 b) {
+  const float m = fmaxf(a.x, b.x), ref = m == -INFINITY ? 0.f : m;
+  return make_float2(m, a.y * ex2(a.x - ref) + b.y * ex2(b.x - ref));
+}
+
+// Few rows: a block per row, its pairs one after the other in memory.
+__global__ void __launch_bounds__(256)
+lm_few_finish_kernel(const float2 *part, int n_part, const int *n_rows, const int *idx, const float *tlogit, float logit_scale,
+                     float *loss, float *lse) {
+  __shared__ float2 sh[8];
+  const int r = blockIdx.x;
+  if (r >= *n_rows) return;
+  float2 s = make_float2(-INFINITY, 0.f);
+  for (int i = threadIdx.x; i < n_part; i += 256) s = merge_stats(s, part[(long long)r * n_part + i]);
+#pragma unroll
+  for (int d = 16; d >= 1; d >>= 1)
+    s = merge_stats(s, make_float2(__shfl_down_sync(0xffffffffu, s.x, d), __shfl_down_sync(0xffffffffu, s.y, d)));
+  if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int w = 1; w < 8; ++w) s = merge_stats(s, sh[w]);
+    const float z = s.x * 0.6931471805599453f + logf(s.y);
+    const int t = idx[r];
+    lse[t] = z;
+    loss[t] = z - tlogit[r] * logit_scale;
+  }
+}
+
 // lse of a row from its partial (m, l) pairs, merged in a fixed order.  32 rows x 8 shares of the pairs a block.
 __global__ void __launch_bounds__(256)
 lm_finish_kernel(const float2 *part, int n_part, long long rows_pad, const int *n_rows, const int *idx, const float *tlogit,
@@ -92,24 +166,20 @@ lm_finish_kernel(const float2 *part, int n_part, long long rows_pad, const int *
   const int n = *n_rows;
   for (int r0 = blockIdx.x * 32; r0 < n; r0 += gridDim.x * 32) {
     const int r = r0 + lane;
-    float m = -INFINITY, l = 0.f;
+    float2 v = make_float2(-INFINITY, 0.f);
     if (r < n)
-      for (int i = seg; i < n_part; i += 8) {
-        const float2 v = part[(long long)i * rows_pad + r];
-        const float mn = fmaxf(m, v.x), ref = mn == -INFINITY ? 0.f : mn;
-        l = l * ex2(m - ref) + v.y * ex2(v.x - ref);
-        m = mn;
+      for (int i = seg; i < n_part; i += 32) {
+        float2 q[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) q[e] = i + 8 * e < n_part ? part[(long long)(i + 8 * e) * rows_pad + r] : make_float2(-INFINITY, 0.f);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v = merge_stats(v, q[e]);
       }
-    sh[seg][lane] = make_float2(m, l);
+    sh[seg][lane] = v;
     __syncthreads();
     if (seg == 0 && r < n) {
-      for (int s = 1; s < 8; ++s) {
-        const float2 v = sh[s][lane];
-        const float mn = fmaxf(m, v.x), ref = mn == -INFINITY ? 0.f : mn;
-        l = l * ex2(m - ref) + v.y * ex2(v.x - ref);
-        m = mn;
-      }
-      const float z = m * 0.6931471805599453f + logf(l);
+      for (int s = 1; s < 8; ++s) v = merge_stats(v, sh[s][lane]);
+      const float z = v.x * 0.6931471805599453f + logf(v.y);
       const int t = idx[r];
       lse[t] = z;
       loss[t] = z - tlogit[r] * logit_scale;

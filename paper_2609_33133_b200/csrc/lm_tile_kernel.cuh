@@ -18,7 +18,9 @@
 //
 // Roles (320 threads a CTA): warps 0-7 epilogue (warp w: TMEM lanes 32 (w % 4).., columns 128 (w / 4)..), warp 8 TMA loads
 // (each CTA its own share, all counted on the first CTA's barrier), warp 9 of the first CTA issues the MMAs of both.
-// TMEM: two accumulators of 256 columns, so a tile's epilogue runs under the next tile.
+// TMEM: two accumulators of 256 columns, so a tile's epilogue runs under the next tile.  Results leave through shared memory
+// and the copy engine, 32 rows x 128 bytes a warp at a time, whole lines: with 16-byte stores, a row per thread, dW of 77
+// rows under 152064 x 3584 was bound by the store unit (680 us for 1.1 GB).
 #pragma once
 #include <cuda.h>
 
@@ -56,12 +58,8 @@ struct LmParams {
   const float *gscale;      // [rows_pad] a_t c; 0 behind the last row
   float2 *part;             // STATS: [2 x vocabulary tiles][rows_pad] (m, l)
   float *tlogit;            // STATS: [rows_pad] x at the target
-  __nv_bfloat16 *grad;      // GRAD out: [rows_pad][ld_grad]
-  long long ld_grad;
-  float *dh_part;           // DH out: [splits][rows_pad][hidden]
-  int dh_add;               // DH: add to what an earlier piece left
-  void *dw;                 // DW out: rows v0.. of [vocab, hidden]
-  int dw_f32, dw_add;
+  int dh_add;               // DH: add to what an earlier piece left in the partial sums
+  int dw_f32, dw_add;       // DW: type of dW, add to what is there
   int *status;
   long long wait_budget;
   int test_flags;
@@ -70,8 +68,9 @@ struct LmParams {
 struct LmSmem {
   static constexpr int kABytes = 128 * 128, kBBytes = 128 * 128;  // this CTA's share of a stage
   static constexpr int kStageBytes = kABytes + kBBytes;
-  static constexpr int kStages = 7;
-  static constexpr int kOffBar = kStages * kStageBytes;
+  static constexpr int kStages = 6;
+  static constexpr int kOffOut = kStages * kStageBytes;   // 4 KB a warp on their way out
+  static constexpr int kOffBar = kOffOut + 8 * 4096;
   static constexpr int kBytes = kOffBar + 256;
 };
 
@@ -103,13 +102,30 @@ __device__ __forceinline__ bool lm_tile(const LmParams &p, int n_rows, int t, Lm
   return false;
 }
 
+// A row's columns into the warp's 4 KB block, in the 128-byte swizzle (16-byte chunk j of row r sits at j ^ (r % 8)): 32 columns
+// of 16 bits as the chunks from `chunk`, or 32 columns of 32 bits.
+__device__ __forceinline__ void stage_bf16(uint32_t s_out, int row, int chunk, const float (&x)[32]) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    st_shared_v4(s_out + row * 128 + (((chunk + e) ^ (row & 7)) << 4), pack_bf16(x[8 * e], x[8 * e + 1]), pack_bf16(x[8 * e + 2], x[8 * e + 3]),
+                 pack_bf16(x[8 * e + 4], x[8 * e + 5]), pack_bf16(x[8 * e + 6], x[8 * e + 7]));
+}
+__device__ __forceinline__ void stage_f32(uint32_t s_out, int row, const float (&x)[32]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    st_shared_v4(s_out + row * 128 + ((e ^ (row & 7)) << 4), __float_as_uint(x[4 * e]), __float_as_uint(x[4 * e + 1]),
+                 __float_as_uint(x[4 * e + 2]), __float_as_uint(x[4 * e + 3]));
+}
+
 // Tensor maps: H and W with a box of 64 contiguous hidden columns x 128 rows (contraction contiguous) or (_mn, contraction
 // along the rows) of two such columns x 64 rows, one box for the 128 rows or columns of a stage: two boxes of half the size
-// come in more slowly than the tensor core takes them (530 cycles a stage of 512, one box 453).  G likewise.
+// come in more slowly than the tensor core takes them (530 cycles a stage of 512, one box 453).  G likewise.  tm_out: G (GRAD)
+// or dW (DW), tm_dh: the partial sums [splits x rows_pad][hidden]; boxes of 128 bytes x 32 rows.
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLmThreads, 1)
 lm_tile_kernel(const __grid_constant__ CUtensorMap tm_h, const __grid_constant__ CUtensorMap tm_w,
                const __grid_constant__ CUtensorMap tm_g, const __grid_constant__ CUtensorMap tm_h_mn,
-               const __grid_constant__ CUtensorMap tm_w_mn, const __grid_constant__ CUtensorMap tm_g_mn, const LmParams p) {
+               const __grid_constant__ CUtensorMap tm_w_mn, const __grid_constant__ CUtensorMap tm_g_mn,
+               const __grid_constant__ CUtensorMap tm_out, const __grid_constant__ CUtensorMap tm_dh, const LmParams p) {
   using SM = LmSmem;
   constexpr int NST = SM::kStages;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
@@ -211,7 +227,7 @@ lm_tile_kernel(const __grid_constant__ CUtensorMap tm_h, const __grid_constant__
    }
   } else {
     // ------------------------------------------------------------ epilogue warps 0-7
-    const int r = (warp & 3) * 32 + lane;
+    const uint32_t s_out = base + SM::kOffOut + warp * 4096;
     const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
     const int half = warp >> 2, col0 = half * 128;
     uint32_t ic = 0;
@@ -223,7 +239,7 @@ lm_tile_kernel(const __grid_constant__ CUtensorMap tm_h, const __grid_constant__
       if (!ok) break;
       tc_fence_after();
       const uint32_t tD = tmem + buf * kLmTile + lane_off + col0;
-      const int row = c.m * kLmTile + rank * 128 + r, n0 = c.n * kLmTile + col0;  // tile row, first column of this warp
+      const int row0 = c.m * kLmTile + rank * 128 + (warp & 3) * 32, row = row0 + lane, n0 = c.n * kLmTile + col0;  // tile row, first column of this warp
       if (J.kind == LM_STATS) {
         const int tgt = row < n_rows ? p.target[row] - p.v0 - n0 : -1;  // column of the target, relative
         float m = -INFINITY, l = 0.f, xt = 0.f;
@@ -259,7 +275,6 @@ lm_tile_kernel(const __grid_constant__ CUtensorMap tm_h, const __grid_constant__
         const bool live = row < n_rows;
         const int tgt = live ? p.target[row] - p.v0 - n0 : -1;
         const float lse2 = live ? p.lse2[row] : 0.f, gs = live ? p.gscale[row] : 0.f;
-        __nv_bfloat16 *dst = p.grad + (long long)row * p.ld_grad + n0;
         for (int q = 0; q < 4; ++q) {
           uint32_t v[32];
           tmem_ld32(tD + q * 32, v);
@@ -271,46 +286,46 @@ lm_tile_kernel(const __grid_constant__ CUtensorMap tm_h, const __grid_constant__
             const float pr = ex2(fmaf(__uint_as_float(v[e]), p.scale_log2, -lse2)) - (tgt - q * 32 == e ? 1.f : 0.f);
             g[e] = live && e < left ? pr * gs : 0.f;
           }
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            uint32_t w[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) w[i] = pack_bf16(g[16 * e + 2 * i], g[16 * e + 2 * i + 1]);
-            st_global_v8(dst + q * 32 + 16 * e, w);
+          if (!(q & 1)) { if (lane == 0) bulk_wait_read(); __syncwarp(); }
+          stage_bf16(s_out, lane, (q & 1) * 4, g);
+          if (q & 1) {
+            fence_async_shared();
+            __syncwarp();
+            if (lane == 0) { tma_store_2d(&tm_out, s_out, n0 + (q - 1) * 32, row0); bulk_commit(); }
           }
         }
       } else {
-        const bool dh = J.kind == LM_DH;
-        const bool live = dh ? row < n_rows : row < J.m_fixed;
-        const bool f32 = dh || p.dw_f32, add = dh ? p.dh_add : p.dw_add;
+        const bool dh = J.kind == LM_DH, f32 = dh || p.dw_f32, add = dh ? p.dh_add : p.dw_add;
         const bool zero = c.nkb == 0;   // an empty contraction: nothing was accumulated
-        const long long off = dh ? ((long long)c.split * p.rows_pad + row) * p.hidden + n0
-                                 : ((long long)p.v0 + row) * p.hidden + n0;
+        const CUtensorMap *map = dh ? &tm_dh : &tm_out;
+        // (a box that begins outside is left out; one that only ends outside is cut off by the map)
+        const bool inside = row0 < (dh ? n_rows : J.m_fixed);
+        const long long out_row = dh ? c.split * p.rows_pad + row0 : p.v0 + row0;
         for (int q = 0; q < 4; ++q) {
           uint32_t v[32];
           tmem_ld32(tD + q * 32, v);
           tc_wait_ld();
-          if (live) {
+          float x[32];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int col = q * 32 + e * 8;
-              if (n0 + col < p.hidden) {   // hidden is a multiple of 8
-                float x[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = zero ? 0.f : __uint_as_float(v[e * 8 + i]);
-                if (f32) {
-                  float4 *d = reinterpret_cast<float4 *>((dh ? p.dh_part : static_cast<float *>(p.dw)) + off + col);
-                  if (add) {
-                    const float4 a = d[0], b = d[1];
-                    x[0] += a.x; x[1] += a.y; x[2] += a.z; x[3] += a.w; x[4] += b.x; x[5] += b.y; x[6] += b.z; x[7] += b.w;
-                  }
-                  d[0] = make_float4(x[0], x[1], x[2], x[3]);
-                  d[1] = make_float4(x[4], x[5], x[6], x[7]);
-                } else {
-                  *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.dw) + off + col) =
-                      make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
-                }
-              }
+          for (int e = 0; e < 32; ++e) x[e] = zero ? 0.f : __uint_as_float(v[e]);
+          const int col = n0 + q * 32;
+          if (f32) {
+            if (lane == 0) bulk_wait_read();
+            __syncwarp();
+            stage_f32(s_out, lane, x);
+            fence_async_shared();
+            __syncwarp();
+            if (lane == 0 && inside && col < p.hidden) {
+              if (add) tma_add_2d(map, s_out, col, (int)out_row); else tma_store_2d(map, s_out, col, (int)out_row);
+              bulk_commit();
+            }
+          } else {
+            if (!(q & 1)) { if (lane == 0) bulk_wait_read(); __syncwarp(); }
+            stage_bf16(s_out, lane, (q & 1) * 4, x);
+            if (q & 1) {
+              fence_async_shared();
+              __syncwarp();
+              if (lane == 0 && inside && col - 32 < p.hidden) { tma_store_2d(map, s_out, col - 32, (int)out_row); bulk_commit(); }
             }
           }
         }
@@ -319,6 +334,7 @@ lm_tile_kernel(const __grid_constant__ CUtensorMap tm_h, const __grid_constant__
       __syncwarp();
       if (lane == 0) mbar_arrive_cluster(map_to_rank(bar_acc_empty + 8 * buf, 0));
     }
+    if (lane == 0) bulk_wait();
   }
 
   __syncwarp();
