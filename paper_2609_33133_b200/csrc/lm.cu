@@ -68,12 +68,26 @@ int64_t piece_cols(const augtree_lm *lm, int64_t rows_pad) {
   return up((lm->vocab + pieces - 1) / pieces, kLmTile);
 }
 
-// Shares of dH's contraction: dH has few tiles when there are few rows, and a share should be a small part of what a
-// CTA does in the launch (which holds dW's tiles too), or the longest one would be waited for.
+// Shares of dH's contraction.  A launch holds dH's tiles (each a contraction over the piece, `kb` steps) and dW's (over the rows,
+// `kr` steps), dealt out to the CTA pairs in turn; the longest pair is waited for.  More shares even the pairs out (and let
+// few rows fill the GPU) but each costs a pass over the partial sums: the fewest within 2 % of the best.
 int dh_splits(const augtree_lm *lm, int64_t rows_pad, int64_t cols) {
-  const int64_t kb = (cols + 63) / 64, tiles = (rows_pad / kLmTile) * ((lm->hidden + kLmTile - 1) / kLmTile);
-  const int64_t lane_kb = std::max<int64_t>(4 * tiles * kb / lm->n_lanes, 1);  // dW costs as much as dH
-  return (int)std::min<int64_t>(std::min<int64_t>((4 * kb + lane_kb - 1) / lane_kb, 64), kb);
+  const int64_t pairs = std::max(lm->n_lanes / 2, 1), nt = (lm->hidden + kLmTile - 1) / kLmTile;
+  const int64_t kb = (cols + 63) / 64, kr = (rows_pad + 63) / 64;
+  const int64_t dh_tiles = rows_pad / kLmTile * nt, dw_tiles = (cols + kLmTile - 1) / kLmTile * nt;
+  auto longest = [&](int64_t s) {
+    int64_t worst = 0;
+    for (int64_t i = 0; i < pairs; ++i) {
+      const int64_t all = (dh_tiles * s + dw_tiles - i + pairs - 1) / pairs, dh = std::max<int64_t>((dh_tiles * s - i + pairs - 1) / pairs, 0);
+      worst = std::max(worst, dh * ((kb + s - 1) / s) + (all - dh) * kr);
+    }
+    return worst;
+  };
+  const int64_t most = std::min<int64_t>(kb, 32);
+  int64_t best = longest(1), pick = 1;
+  for (int64_t s = 2; s <= most; ++s) best = std::min(best, longest(s));
+  while (pick < most && longest(pick) * 100 > best * 102) ++pick;
+  return (int)pick;
 }
 
 // Few rows: shares of the vocabulary that fill the CTAs in one go.
