@@ -276,6 +276,7 @@ class Plan:
 
 _DTYPE_CODE = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
 _ID_BYTES = {torch.int64: 8, torch.int32: 4}
+_BF16, _F32 = (torch.bfloat16,), (torch.float32,)
 
 
 class LM:
@@ -306,7 +307,7 @@ class LM:
         return max(self.workspace_parts(n_tokens))
 
     def _arg(self, t, name, dtypes, shape):
-        if t.dtype not in dtypes or tuple(t.shape) != shape or not t.is_cuda or t.device.index != self.device or not t.is_contiguous():
+        if t.dtype not in dtypes or t.shape != shape or t.get_device() != self.device or not t.is_contiguous():
             raise ValueError(f"{name}: expected a contiguous tensor on cuda:{self.device} of shape {shape} and one of {list(dtypes)}, "
                              f"got {tuple(t.shape)} {t.dtype} on {t.device}")
         return t.data_ptr()
@@ -314,18 +315,23 @@ class LM:
     def _ids(self, t):
         if t.dim() != 1:
             raise ValueError("token ids: expected one dimension")
-        return self._arg(t, "token ids", _ID_BYTES, (t.shape[0],)), _ID_BYTES[t.dtype], t.shape[0]
+        n = t.shape[0]
+        return self._arg(t, "token ids", _ID_BYTES, (n,)), _ID_BYTES[t.dtype], n
 
     def _ws(self, ws):
-        if not ws.is_cuda or ws.device.index != self.device or not ws.is_contiguous():
+        if ws.get_device() != self.device or not ws.is_contiguous():
             raise ValueError(f"ws: expected a contiguous tensor on cuda:{self.device}")
-        return ws.data_ptr(), ws.numel() * ws.element_size()
+        return ws.data_ptr(), ws.nbytes
+
+    def _stream(self):
+        # (the stream handle alone: torch.cuda.current_stream() builds an object, a third of a single-token call)
+        return torch._C._cuda_getCurrentRawStream(self.device)
 
     def embed_fwd(self, table, ids, out):
         """out[t] = embed_scale * table[ids[t]]; zeros for a negative id."""
         i, ib, n = self._ids(ids)
         _check(lib.augtree_embed_fwd(self._h, self._arg(table, "table", _DTYPE_CODE, (self.vocab, self.hidden)), _DTYPE_CODE[table.dtype], i, ib,
-                                     n, self._arg(out, "out", _DTYPE_CODE, (n, self.hidden)), _DTYPE_CODE[out.dtype], Plan._stream()), "embed_fwd")
+                                     n, self._arg(out, "out", _DTYPE_CODE, (n, self.hidden)), _DTYPE_CODE[out.dtype], self._stream()), "embed_fwd")
 
     def embed_bwd(self, d_out, ids, d_table, ws, accumulate=False):
         """d_table[v] = embed_scale * sum of d_out over the tokens of id v (added to an fp32 d_table with accumulate)."""
@@ -333,28 +339,28 @@ class LM:
         w, wb = self._ws(ws)
         _check(lib.augtree_embed_bwd(self._h, self._arg(d_out, "d_out", _DTYPE_CODE, (n, self.hidden)), _DTYPE_CODE[d_out.dtype], i, ib, n,
                                      self._arg(d_table, "d_table", _DTYPE_CODE, (self.vocab, self.hidden)), _DTYPE_CODE[d_table.dtype],
-                                     int(bool(accumulate)), w, wb, Plan._stream()), "embed_bwd")
+                                     int(bool(accumulate)), w, wb, self._stream()), "embed_bwd")
 
     def loss_fwd(self, hidden, weight, targets, loss, lse, ws):
         """Cross entropy and log-sum-exp of every token; zeros where the target is negative."""
         i, ib, n = self._ids(targets)
         w, wb = self._ws(ws)
-        bf, f32 = (torch.bfloat16,), (torch.float32,)
+        bf, f32 = _BF16, _F32
         _check(lib.augtree_lm_loss_fwd(self._h, self._arg(hidden, "hidden", bf, (n, self.hidden)),
                                        self._arg(weight, "weight", bf, (self.vocab, self.hidden)), i, ib, n,
-                                       self._arg(loss, "loss", f32, (n,)), self._arg(lse, "lse", f32, (n,)), w, wb, Plan._stream()), "lm_loss_fwd")
+                                       self._arg(loss, "loss", f32, (n,)), self._arg(lse, "lse", f32, (n,)), w, wb, self._stream()), "lm_loss_fwd")
 
     def loss_bwd(self, hidden, weight, targets, lse, d_loss, d_hidden, d_weight, ws, accumulate=False):
         """Gradients of sum(d_loss * loss); d_hidden or d_weight may be None, and is then not computed."""
         i, ib, n = self._ids(targets)
         w, wb = self._ws(ws)
-        bf, f32 = (torch.bfloat16,), (torch.float32,)
+        bf, f32 = _BF16, _F32
         dh = None if d_hidden is None else self._arg(d_hidden, "d_hidden", bf, (n, self.hidden))
         dw = None if d_weight is None else self._arg(d_weight, "d_weight", bf + f32, (self.vocab, self.hidden))
         _check(lib.augtree_lm_loss_bwd(self._h, self._arg(hidden, "hidden", bf, (n, self.hidden)),
                                        self._arg(weight, "weight", bf, (self.vocab, self.hidden)), i, ib, self._arg(lse, "lse", f32, (n,)),
                                        self._arg(d_loss, "d_loss", f32, (n,)), n, dh, dw, 0 if dw is None else _DTYPE_CODE[d_weight.dtype],
-                                       int(bool(accumulate)), w, wb, Plan._stream()), "lm_loss_bwd")
+                                       int(bool(accumulate)), w, wb, self._stream()), "lm_loss_bwd")
 
     def device_status(self):
         s, d = C.c_int(), C.c_int()

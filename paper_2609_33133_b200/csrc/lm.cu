@@ -106,10 +106,12 @@ size_t loss_layout(const augtree_lm *lm, int64_t tokens, bool bwd, uint8_t *base
   w->h = c.take<__nv_bfloat16>(rp * lm->hidden);
   if (!bwd) {
     w->rows.lse2 = w->rows.gscale = nullptr;
+    w->rows.x_target = c.take<float>(rp);
     w->tlogit = c.take<float>(rp);
     w->part = c.take<float2>(few ? 4ll * lm->n_lanes * few : (int64_t)n_part(lm) * rp);
   } else {
     const int64_t cols = piece_cols(lm, rp);
+    w->rows.x_target = nullptr;
     w->rows.lse2 = c.take<float>(rp);
     w->rows.gscale = c.take<float>(rp);
     w->grad = c.take<__nv_bfloat16>(rp * cols);
@@ -206,17 +208,18 @@ int launched() {
   return cudaGetLastError() == cudaSuccess ? AUGTREE_OK : AUGTREE_ERR_CUDA;
 }
 
-int compact(const augtree_lm *lm, const void *targets, int id_bytes, int64_t tokens, const void *hidden, const LossWs &w,
+// Scored rows packed into the scratch; with `weight` (forward) also their targets' logits.
+int compact(const augtree_lm *lm, const void *targets, int id_bytes, int64_t tokens, const void *hidden, const void *weight, const LossWs &w,
             const float *lse, const float *d_loss, float *loss_out, float *lse_out, cudaStream_t st) {
   if (const int few = few_rows(tokens)) {
     const uint4 *src = static_cast<const uint4 *>(hidden);
     uint4 *dst = reinterpret_cast<uint4 *>(w.h);
     if (id_bytes == 8)
       lm_few_rows_kernel<<<few, 128, 0, st>>>(static_cast<const long long *>(targets), (int)tokens, lm->vocab, w.rows, lse, d_loss, lm->logit_scale,
-                                              loss_out, lse_out, lm->d_status, src, dst, lm->hidden / 8, lse != nullptr);
+                                              loss_out, lse_out, lm->d_status, src, dst, lm->hidden / 8, lse != nullptr, static_cast<const uint4 *>(weight));
     else
       lm_few_rows_kernel<<<few, 128, 0, st>>>(static_cast<const int *>(targets), (int)tokens, lm->vocab, w.rows, lse, d_loss, lm->logit_scale,
-                                              loss_out, lse_out, lm->d_status, src, dst, lm->hidden / 8, lse != nullptr);
+                                              loss_out, lse_out, lm->d_status, src, dst, lm->hidden / 8, lse != nullptr, static_cast<const uint4 *>(weight));
     return launched();
   }
   if (id_bytes == 8)
@@ -228,8 +231,8 @@ int compact(const augtree_lm *lm, const void *targets, int id_bytes, int64_t tok
   int r = launched();
   if (r) return r;
   const unsigned grid = (unsigned)std::min<int64_t>(up(tokens, 256), 8 * lm->n_lanes);
-  lm_gather_kernel<<<grid, 256, 0, st>>>(static_cast<const uint4 *>(hidden), w.rows.idx, w.rows.n_rows,
-                                         reinterpret_cast<uint4 *>(w.h), lm->hidden / 8);
+  lm_gather_kernel<<<grid, 256, 0, st>>>(static_cast<const uint4 *>(hidden), w.rows, reinterpret_cast<uint4 *>(w.h), lm->hidden / 8,
+                                         static_cast<const uint4 *>(weight));
   return launched();
 }
 
@@ -479,14 +482,14 @@ int augtree_lm_loss_fwd(const augtree_lm_t *lm, const void *hidden, const void *
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const int64_t rp = pad_rows(n_tokens);
   const int few = few_rows(n_tokens);
-  if ((r = compact(lm, targets, id_bytes, n_tokens, hidden, w, nullptr, nullptr, loss, lse, st))) return r;
+  if ((r = compact(lm, targets, id_bytes, n_tokens, hidden, weight, w, nullptr, nullptr, loss, lse, st))) return r;
   Maps m = {};
   if (few) {
     FewParams p = few_params(lm, w, base_params(lm, w, few));
     p.n = lm->vocab;
     if ((r = map_2d(&m.h, w.h, few, lm->hidden, few)) || (r = map_2d(&m.w, weight, lm->vocab, lm->hidden, 128))) return r;
     if ((r = launch_few<LM_STATS>(lm, few, m.w, m.h, p, st))) return r;
-    lm_few_finish_kernel<<<few, 256, 0, st>>>(w.part, 4 * lm->n_lanes, w.rows.n_rows, w.rows.idx, w.tlogit, lm->logit_scale, loss, lse);
+    lm_few_finish_kernel<<<few, 256, 0, st>>>(w.part, 4 * lm->n_lanes, w.rows, w.tlogit, lm->logit_scale, loss, lse);
     return launched();
   }
   if ((r = map_2d(&m.h, w.h, rp, lm->hidden, 128)) || (r = map_2d(&m.w, weight, lm->vocab, lm->hidden, 128))) return r;
@@ -495,8 +498,8 @@ int augtree_lm_loss_fwd(const augtree_lm_t *lm, const void *hidden, const void *
   p.job[0] = {LM_STATS, 0, lm->vocab, lm->hidden, 1};
   p.part = w.part; p.tlogit = w.tlogit;
   if ((r = launch_tiles(lm, m, p, st))) return r;
-  const unsigned grid = (unsigned)std::min<int64_t>((n_tokens + 31) / 32, 8 * lm->n_lanes);
-  lm_finish_kernel<<<grid, 256, 0, st>>>(w.part, n_part(lm), rp, w.rows.n_rows, w.rows.idx, w.tlogit, lm->logit_scale, loss, lse);
+  const unsigned grid = (unsigned)std::min<int64_t>((n_tokens + 31) / 32, 2 * lm->n_lanes);
+  lm_finish_kernel<<<grid, 1024, 0, st>>>(w.part, n_part(lm), rp, w.rows, w.tlogit, lm->logit_scale, loss, lse);
   return launched();
 }
 
@@ -523,7 +526,7 @@ int augtree_lm_loss_bwd(const augtree_lm_t *lm, const void *hidden, const void *
   const int few = few_rows(n_tokens);
   const int64_t rp = pad_rows(n_tokens), cols = piece_cols(lm, rp);
   const int splits = few ? few_splits(lm, cols) : dh_splits(lm, rp, cols), chunks = lm->hidden % 64 == 0 ? 2 : 1;
-  if ((r = compact(lm, targets, id_bytes, n_tokens, hidden, w, lse, d_loss, nullptr, nullptr, st))) return r;
+  if ((r = compact(lm, targets, id_bytes, n_tokens, hidden, nullptr, w, lse, d_loss, nullptr, nullptr, st))) return r;
   Maps m = {};
   if ((r = map_2d(&m.h, w.h, rp, lm->hidden, few ? few : 128)) || (r = map_2d(&m.w, weight, lm->vocab, lm->hidden, 128)) ||
       (r = map_mn(&m.h_mn, w.h, rp, lm->hidden, chunks)) || (r = map_mn(&m.w_mn, weight, lm->vocab, lm->hidden, chunks)) ||

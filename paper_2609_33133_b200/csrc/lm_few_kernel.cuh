@@ -4,7 +4,9 @@
 //
 //   STATS  x^T = W H^T, a tile of 128 vocabulary rows; a TMEM lane is a vocabulary row, a column a token.  Maxima and sums over
 //          the vocabulary run across the lanes (halving exchanges: 31 shuffles leave lane j with column j's) and stay in
-//          registers over all tiles of the CTA; one (m, l) pair a warp and token is left at the end.
+//          registers over all tiles of the CTA; one (m, l) pair a warp and token is left at the end.  The contraction is cut into
+//          up to four accumulators, added up with rounding: the tensor core's own additions drop what does not fit, always
+//          towards zero, in proportion to the length of the chain.
 //   GRAD   G, rounded to bf16 twice: G = hi + lo, lo = bf16(G - hi), so that the few rows' gradients, in which single elements of
 //          G dominate, carry no rounding of G (2^-17 is left).  hi is row t of the scratch, lo row N + t.
 //   DH     dH^T = W^T G^T, 128 hidden columns x [hi | lo] of the tokens, a share of the vocabulary each
@@ -99,12 +101,16 @@ __device__ __forceinline__ void few_unit(const FewParams &p, int u, int &tile, i
   nkb = (int)((long long)kb * (split + 1) / p.splits) - kb0;
 }
 
+// The accumulator that step kb of a contraction goes to.  With fewer steps than accumulators each step has its own, from 0 up.
+__device__ __forceinline__ int few_part(int kb, int nkb, int n_acc) { return nkb <= n_acc ? kb : kb * n_acc / nkb; }
+
 template <int KIND, int N>
 __global__ void __launch_bounds__(kFewThreads, 1)
 lm_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_b, const FewParams p) {
   using SM = FewSmem<KIND, N>;
   constexpr int NST = SM::kStages;
   constexpr int W = N < 32 ? 16 : 32, NG = N / W;   // columns of a group, groups
+  constexpr int NACC = KIND == LM_STATS ? (N <= 64 ? 4 : 2) : 1;  // accumulators of a tile, each N (DH: 2 N) columns
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   const uint32_t base = smem_u32(smem_raw);
   if (base & 1023u) {
@@ -193,9 +199,12 @@ lm_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ 
         tc_fence_after();
         const uint32_t sA = base + st * SM::kStageBytes;
         const uint32_t a_lo = sdesc_lo(sA, 8192), b_lo = sdesc_lo(sA + SM::kABytes, 8192);
+        const int part = few_part(kb, nkb, NACC);
+        const bool fresh = kb == 0 || few_part(kb - 1, nkb, NACC) != part;
+        const uint32_t tD = tmem + buf * 256 + part * N;
         if (elected) {
 #pragma unroll
-          for (int k = 0; k < 4; ++k) mma_ss2(tmem + buf * 256, a_lo + k * kAStep, b_lo + k * 2, kIdesc, (uint32_t)(kb > 0 || k > 0));
+          for (int k = 0; k < 4; ++k) mma_ss2(tD, a_lo + k * kAStep, b_lo + k * 2, kIdesc, (uint32_t)(!fresh || k > 0));
           tc_commit(bar_empty + 8 * st);
         }
       }
@@ -222,14 +231,22 @@ lm_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ 
         const bool exists = r < p.n;
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
-          uint32_t raw[W];
-          tmem_ld_cols(tD + g * W, raw);
-          tc_wait_ld();
           float x[W], a[W];
 #pragma unroll
+          for (int j = 0; j < W; ++j) x[j] = 0.f;
+#pragma unroll
+          for (int q = 0; q < NACC; ++q) {
+            if (q >= nkb) break;   // (a short contraction fills fewer accumulators)
+            uint32_t raw[W];
+            tmem_ld_cols(tD + q * N + g * W, raw);
+            tc_wait_ld();
+#pragma unroll
+            for (int j = 0; j < W; ++j) x[j] += __uint_as_float(raw[j]);
+          }
+#pragma unroll
           for (int j = 0; j < W; ++j) {
-            if (exists && s_target[g * W + j] == v) p.tlogit[g * W + j] = __uint_as_float(raw[j]);
-            x[j] = a[j] = exists ? __uint_as_float(raw[j]) * p.scale_log2 : -INFINITY;
+            if (exists && s_target[g * W + j] == v) p.tlogit[g * W + j] = x[j];
+            x[j] = a[j] = exists ? x[j] * p.scale_log2 : -INFINITY;
           }
           const float top = reduce_columns(a, lane, [](float s, float t) { return fmaxf(s, t); });
           const float mn = fmaxf(m[g], top), ref = mn == -INFINITY ? 0.f : mn;

@@ -24,6 +24,7 @@ struct LmRows {
   int *target;      // [rows_pad]
   float *lse2;      // [rows_pad] backward only
   float *gscale;    // [rows_pad] backward only
+  float *x_target;  // [rows_pad] forward only: h . W_target
 };
 
 template <typename Id>
@@ -71,14 +72,53 @@ lm_compact_kernel(const Id *targets, int tokens, int vocab, LmRows o, const floa
   if (threadIdx.x == 0) *o.n_rows = n;
 }
 
-// Hidden states of the scored rows, packed; zeros up to the next multiple of 256 rows (they enter contractions).
+// h . W_target of a row in fp32 by a whole block, from 16-byte vectors of eight bf16 numbers.  The tensor core's adder drops
+// what does not fit its accumulator, 224 times for 3584 columns, always towards zero: 3e-6 of a large logit, and the
+// target's is the large one in a confident row.  This sum rounds to nearest, in short chains.  Valid in thread 0.
+__device__ __forceinline__ float dot8(const uint4 a, const uint4 b) {
+  const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 u = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(&x[i]));
+    const float2 v = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(&y[i]));
+    s = fmaf(u.x, v.x, s);
+    s = fmaf(u.y, v.y, s);
+  }
+  return s;
+}
+template <int THREADS>
+__device__ __forceinline__ float block_sum(float s, float *sh) {
+#pragma unroll
+  for (int d = 16; d >= 1; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+  __syncthreads();
+  if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = s;
+  __syncthreads();
+  if (threadIdx.x == 0)
+    for (int w = 1; w < THREADS / 32; ++w) s += sh[w];
+  return s;
+}
+
+// Hidden states of the scored rows, packed; zeros up to the next multiple of 256 rows (they enter contractions).  With `weight`
+// also their targets' logits.
 __global__ void __launch_bounds__(256)
-lm_gather_kernel(const uint4 *hidden, const int *idx, const int *n_rows, uint4 *out, int row_vecs) {
-  const int n = *n_rows, n_pad = (n + 255) / 256 * 256;
+lm_gather_kernel(const uint4 *hidden, const LmRows rows, uint4 *out, int row_vecs, const uint4 *weight) {
+  __shared__ float sh[8];
+  const int n = *rows.n_rows, n_pad = (n + 255) / 256 * 256;
   for (int r = blockIdx.x; r < n_pad; r += gridDim.x) {
-    const uint4 *src = r < n ? hidden + (long long)idx[r] * row_vecs : nullptr;
+    const uint4 *src = r < n ? hidden + (long long)rows.idx[r] * row_vecs : nullptr;
+    const uint4 *wt = src && weight ? weight + (long long)rows.target[r] * row_vecs : nullptr;
     uint4 *dst = out + (long long)r * row_vecs;
-    for (int i = threadIdx.x; i < row_vecs; i += 256) dst[i] = src ? __ldg(src + i) : make_uint4(0, 0, 0, 0);
+    float s = 0.f;
+    for (int i = threadIdx.x; i < row_vecs; i += 256) {
+      const uint4 v = src ? __ldg(src + i) : make_uint4(0, 0, 0, 0);
+      if (wt) s += dot8(v, __ldg(wt + i));
+      dst[i] = v;
+    }
+    if (wt) {
+      s = block_sum<256>(s, sh);
+      if (threadIdx.x == 0) rows.x_target[r] = s;
+    }
   }
 }
 
@@ -87,8 +127,10 @@ lm_gather_kernel(const uint4 *hidden, const int *idx, const int *n_rows, uint4 *
 template <typename Id>
 __global__ void __launch_bounds__(128)
 lm_few_rows_kernel(const Id *targets, int tokens, int vocab, LmRows o, const float *lse, const float *d_loss, float logit_scale,
-                   float *loss_out, float *lse_out, int *status, const uint4 *hidden, uint4 *out, int row_vecs, int twice) {
+                   float *loss_out, float *lse_out, int *status, const uint4 *hidden, uint4 *out, int row_vecs, int twice,
+                   const uint4 *weight) {
   __shared__ int warp_sum[4];
+  __shared__ float sh[4];
   __shared__ int from;
   const int t = threadIdx.x, lane = t & 31, warp = t >> 5, row = blockIdx.x;
   const long long id = t < tokens ? (long long)targets[t] : -1;
@@ -121,10 +163,17 @@ lm_few_rows_kernel(const Id *targets, int tokens, int vocab, LmRows o, const flo
   }
   __syncthreads();
   const uint4 *src = from >= 0 ? hidden + (long long)from * row_vecs : nullptr;
+  const uint4 *wt = src && weight ? weight + (long long)targets[from] * row_vecs : nullptr;
+  float s = 0.f;
   for (int i = t; i < row_vecs; i += 128) {
     const uint4 v = src ? __ldg(src + i) : make_uint4(0, 0, 0, 0);
+    if (wt) s += dot8(v, __ldg(wt + i));
     out[(long long)row * row_vecs + i] = v;
     if (twice) out[(long long)(gridDim.x + row) * row_vecs + i] = v;
+  }
+  if (wt) {
+    s = block_sum<128>(s, sh);
+    if (t == 0) o.x_target[row] = s;
   }
 }
 
@@ -134,13 +183,26 @@ __device__ __forceinline__ float2 merge_stats(float2 a, float2 b) {
   return make_float2(m, a.y * ex2(a.x - ref) + b.y * ex2(b.x - ref));
 }
 
+// Loss and lse of a row from its merged (m, l).  The target's term of the sum is 2^(t2 - m) with t2 = c log2(e) tlogit as the
+// tile kernels rounded it; d is what t2 lacks of the exact x_target, and puts the term right.  The loss is taken as
+// log of the sum relative to the target's term, so that a small loss is not the difference of two large numbers.
+__device__ __forceinline__ void write_loss(float2 s, float tlogit, float x_target, float logit_scale, float *loss, float *lse) {
+  constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+  const float c = logit_scale * kLog2e, t2 = tlogit * c;
+  const float d = fmaf(tlogit, c, -t2) + (x_target - tlogit) * c;
+  const float l = s.y + ex2(t2 - s.x) * expm1f(d * kLn2);
+  const float v = (s.x - t2 - d) * kLn2 + logf(l);
+  *loss = v;
+  *lse = v + x_target * logit_scale;
+}
+
 // Few rows: a block per row, its pairs one after the other in memory.
 __global__ void __launch_bounds__(256)
-lm_few_finish_kernel(const float2 *part, int n_part, const int *n_rows, const int *idx, const float *tlogit, float logit_scale,
+lm_few_finish_kernel(const float2 *part, int n_part, const LmRows rows, const float *tlogit, float logit_scale,
                      float *loss, float *lse) {
   __shared__ float2 sh[8];
   const int r = blockIdx.x;
-  if (r >= *n_rows) return;
+  if (r >= *rows.n_rows) return;
   float2 s = make_float2(-INFINITY, 0.f);
   for (int i = threadIdx.x; i < n_part; i += 256) s = merge_stats(s, part[(long long)r * n_part + i]);
 #pragma unroll
@@ -150,39 +212,38 @@ lm_few_finish_kernel(const float2 *part, int n_part, const int *n_rows, const in
   __syncthreads();
   if (threadIdx.x == 0) {
     for (int w = 1; w < 8; ++w) s = merge_stats(s, sh[w]);
-    const float z = s.x * 0.6931471805599453f + logf(s.y);
-    const int t = idx[r];
-    lse[t] = z;
-    loss[t] = z - tlogit[r] * logit_scale;
+    const int t = rows.idx[r];
+    write_loss(s, tlogit[r], rows.x_target[r], logit_scale, loss + t, lse + t);
   }
 }
 
-// lse of a row from its partial (m, l) pairs, merged in a fixed order.  32 rows x 8 shares of the pairs a block.
-__global__ void __launch_bounds__(256)
-lm_finish_kernel(const float2 *part, int n_part, long long rows_pad, const int *n_rows, const int *idx, const float *tlogit,
-                 float logit_scale, float *loss, float *lse) {
-  __shared__ float2 sh[8][32];
+// Many rows: 32 rows x 32 shares of their pairs a block, merged in a fixed order.
+__global__ void __launch_bounds__(1024)
+lm_finish_kernel(const float2 *part, int n_part, long long rows_pad, const LmRows rows, const float *tlogit, float logit_scale,
+                 float *loss, float *lse) {
+  __shared__ float2 sh[32][33];
   const int lane = threadIdx.x & 31, seg = threadIdx.x >> 5;
-  const int n = *n_rows;
+  const int n = *rows.n_rows;
   for (int r0 = blockIdx.x * 32; r0 < n; r0 += gridDim.x * 32) {
     const int r = r0 + lane;
     float2 v = make_float2(-INFINITY, 0.f);
     if (r < n)
-      for (int i = seg; i < n_part; i += 32) {
+      for (int i = seg; i < n_part; i += 128) {
         float2 q[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) q[e] = i + 8 * e < n_part ? part[(long long)(i + 8 * e) * rows_pad + r] : make_float2(-INFINITY, 0.f);
+        for (int e = 0; e < 4; ++e) q[e] = i + 32 * e < n_part ? part[(long long)(i + 32 * e) * rows_pad + r] : make_float2(-INFINITY, 0.f);
 #pragma unroll
         for (int e = 0; e < 4; ++e) v = merge_stats(v, q[e]);
       }
-    sh[seg][lane] = v;
+    sh[lane][seg] = v;
     __syncthreads();
-    if (seg == 0 && r < n) {
-      for (int s = 1; s < 8; ++s) v = merge_stats(v, sh[s][lane]);
-      const float z = v.x * 0.6931471805599453f + logf(v.y);
-      const int t = idx[r];
-      lse[t] = z;
-      loss[t] = z - tlogit[r] * logit_scale;
+    v = sh[seg][lane];   // warp: row, lane: share
+#pragma unroll
+    for (int d = 16; d >= 1; d >>= 1)
+      v = merge_stats(v, make_float2(__shfl_down_sync(0xffffffffu, v.x, d), __shfl_down_sync(0xffffffffu, v.y, d)));
+    if (lane == 0 && r0 + seg < n) {
+      const int t = rows.idx[r0 + seg];
+      write_loss(v, tlogit[r0 + seg], rows.x_target[r0 + seg], logit_scale, loss + t, lse + t);
     }
     __syncthreads();
   }
