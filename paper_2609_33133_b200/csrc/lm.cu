@@ -4,6 +4,7 @@
 
 #include <algorithm>
 #include <new>
+#include <type_traits>
 
 #include "launch.h"
 #include "lm_few_kernel.cuh"
@@ -203,37 +204,42 @@ int check_lm(const augtree_lm *lm) {
   return cur == lm->device ? AUGTREE_OK : AUGTREE_ERR_INVALID_ARG;
 }
 
-int launched() {
+// Every kernel of this file is launched as a programmatic dependent of the one before it in the stream: it may be set up while
+// that one still runs, and begins with wait_previous() (ptx.cuh).
+template <typename... P, typename... A>
+int launch(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, A &&...args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid; cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = smem; cfg.stream = st;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr; cfg.numAttrs = 1;
   ++g_launches;
-  return cudaGetLastError() == cudaSuccess ? AUGTREE_OK : AUGTREE_ERR_CUDA;
+  return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...) == cudaSuccess ? AUGTREE_OK : AUGTREE_ERR_CUDA;
 }
 
 // Scored rows packed into the scratch; with `weight` (forward) also their targets' logits.
 int compact(const augtree_lm *lm, const void *targets, int id_bytes, int64_t tokens, const void *hidden, const void *weight, const LossWs &w,
             const float *lse, const float *d_loss, float *loss_out, float *lse_out, cudaStream_t st) {
+  const auto *ids64 = static_cast<const long long *>(targets);
+  const auto *ids32 = static_cast<const int *>(targets);
+  const auto *src = static_cast<const uint4 *>(hidden), *wt = static_cast<const uint4 *>(weight);
+  auto *dst = reinterpret_cast<uint4 *>(w.h);
+  const int n = (int)tokens, row_vecs = lm->hidden / 8;
   if (const int few = few_rows(tokens)) {
-    const uint4 *src = static_cast<const uint4 *>(hidden);
-    uint4 *dst = reinterpret_cast<uint4 *>(w.h);
     if (id_bytes == 8)
-      lm_few_rows_kernel<<<few, 128, 0, st>>>(static_cast<const long long *>(targets), (int)tokens, lm->vocab, w.rows, lse, d_loss, lm->logit_scale,
-                                              loss_out, lse_out, lm->d_status, src, dst, lm->hidden / 8, lse != nullptr, static_cast<const uint4 *>(weight));
-    else
-      lm_few_rows_kernel<<<few, 128, 0, st>>>(static_cast<const int *>(targets), (int)tokens, lm->vocab, w.rows, lse, d_loss, lm->logit_scale,
-                                              loss_out, lse_out, lm->d_status, src, dst, lm->hidden / 8, lse != nullptr, static_cast<const uint4 *>(weight));
-    return launched();
+      return launch(lm_few_rows_kernel<long long>, few, 128, 0, st, ids64, n, lm->vocab, w.rows, lse, d_loss, lm->logit_scale, loss_out, lse_out,
+                    lm->d_status, src, dst, row_vecs, lse != nullptr, wt);
+    return launch(lm_few_rows_kernel<int>, few, 128, 0, st, ids32, n, lm->vocab, w.rows, lse, d_loss, lm->logit_scale, loss_out, lse_out,
+                  lm->d_status, src, dst, row_vecs, lse != nullptr, wt);
   }
-  if (id_bytes == 8)
-    lm_compact_kernel<<<1, 1024, 0, st>>>(static_cast<const long long *>(targets), (int)tokens, lm->vocab, w.rows, lse, d_loss,
-                                          lm->logit_scale, loss_out, lse_out, lm->d_status);
-  else
-    lm_compact_kernel<<<1, 1024, 0, st>>>(static_cast<const int *>(targets), (int)tokens, lm->vocab, w.rows, lse, d_loss,
-                                          lm->logit_scale, loss_out, lse_out, lm->d_status);
-  int r = launched();
+  const int r = id_bytes == 8 ? launch(lm_compact_kernel<long long>, 1, 1024, 0, st, ids64, n, lm->vocab, w.rows, lse, d_loss, lm->logit_scale,
+                                       loss_out, lse_out, lm->d_status)
+                              : launch(lm_compact_kernel<int>, 1, 1024, 0, st, ids32, n, lm->vocab, w.rows, lse, d_loss, lm->logit_scale,
+                                       loss_out, lse_out, lm->d_status);
   if (r) return r;
   const unsigned grid = (unsigned)std::min<int64_t>(up(tokens, 256), 8 * lm->n_lanes);
-  lm_gather_kernel<<<grid, 256, 0, st>>>(static_cast<const uint4 *>(hidden), w.rows, reinterpret_cast<uint4 *>(w.h), lm->hidden / 8,
-                                         static_cast<const uint4 *>(weight));
-  return launched();
+  return launch(lm_gather_kernel, grid, 256, 0, st, src, w.rows, dst, row_vecs, wt);
 }
 
 LmParams base_params(const augtree_lm *lm, const LossWs &w, int64_t rows_pad) {
@@ -252,14 +258,13 @@ LmParams base_params(const augtree_lm *lm, const LossWs &w, int64_t rows_pad) {
 struct Maps { CUtensorMap h, w, g, h_mn, w_mn, g_mn, out, dh; };
 
 int launch_tiles(const augtree_lm *lm, const Maps &m, const LmParams &p, cudaStream_t st) {
-  lm_tile_kernel<<<std::max(lm->n_lanes / 2, 1) * 2, kLmThreads, LmSmem::kBytes, st>>>(m.h, m.w, m.g, m.h_mn, m.w_mn, m.g_mn, m.out, m.dh, p);
-  return launched();
+  return launch(lm_tile_kernel, std::max(lm->n_lanes / 2, 1) * 2, kLmThreads, LmSmem::kBytes, st, m.h, m.w, m.g, m.h_mn, m.w_mn, m.g_mn, m.out,
+                m.dh, p);
 }
 
 template <int KIND, int N>
 int launch_few_n(const augtree_lm *lm, const CUtensorMap &mw, const CUtensorMap &mb, const FewParams &p, cudaStream_t st) {
-  lm_few_kernel<KIND, N><<<lm->n_lanes, kFewThreads, FewSmem<KIND, N>::kBytes, st>>>(mw, mb, p);
-  return launched();
+  return launch(lm_few_kernel<KIND, N>, lm->n_lanes, kFewThreads, FewSmem<KIND, N>::kBytes, st, mw, mb, p);
 }
 template <int KIND>
 int launch_few(const augtree_lm *lm, int few, const CUtensorMap &mw, const CUtensorMap &mb, const FewParams &p, cudaStream_t st) {
@@ -294,13 +299,13 @@ int embed_fwd_out(const augtree_lm *lm, const void *table, const void *ids, int 
   const unsigned grid = (unsigned)std::min<int64_t>(tokens, 32ll * lm->n_lanes);
   const In *tb = static_cast<const In *>(table);
   const Id *id = static_cast<const Id *>(ids);
-  if (out_dtype == AUGTREE_BF16)
-    embed_fwd_kernel<<<grid, 128, 0, st>>>(tb, id, tokens, lm->vocab, lm->hidden, lm->embed_scale, static_cast<__nv_bfloat16 *>(out), lm->d_status);
-  else if (out_dtype == AUGTREE_F16)
-    embed_fwd_kernel<<<grid, 128, 0, st>>>(tb, id, tokens, lm->vocab, lm->hidden, lm->embed_scale, static_cast<__half *>(out), lm->d_status);
-  else
-    embed_fwd_kernel<<<grid, 128, 0, st>>>(tb, id, tokens, lm->vocab, lm->hidden, lm->embed_scale, static_cast<float *>(out), lm->d_status);
-  return launched();
+  auto run = [&](auto *o) {
+    return launch(embed_fwd_kernel<Id, In, std::remove_pointer_t<decltype(o)>>, grid, 128, 0, st, tb, id, tokens, lm->vocab, lm->hidden,
+                  lm->embed_scale, o, lm->d_status);
+  };
+  if (out_dtype == AUGTREE_BF16) return run(static_cast<__nv_bfloat16 *>(out));
+  if (out_dtype == AUGTREE_F16) return run(static_cast<__half *>(out));
+  return run(static_cast<float *>(out));
 }
 
 template <typename Id>
@@ -316,27 +321,27 @@ int embed_sort(const augtree_lm *lm, const Id *ids, int n, int passes, int bits,
   int r;
   *src = 0;
   if (n <= kSortSmall && lm->vocab <= (1 << 20)) {  // (a larger vocabulary's bits are cleared by more than one block)
-    embed_sort_small_kernel<<<1, 512, kSortSmallBytes, st>>>(ids, n, lm->vocab, passes, bits, w.key[0], w.val[0], w.joins, w.seen, lm->d_status);
-    return launched();
+    return launch(embed_sort_small_kernel<Id>, 1, 512, kSortSmallBytes, st, ids, n, lm->vocab, passes, bits, w.key[0], w.val[0], w.joins,
+                  w.seen, lm->d_status);
   }
   const int blocks = (n + kRadixBlock - 1) / kRadixBlock;
   const KeysFromIds<Id> from_ids{ids, lm->vocab, lm->d_status};
   for (int i = 0; i < passes; ++i) {
     const KeysSorted sorted{w.key[*src], w.val[*src]};
     const int to = i == 0 ? 0 : *src ^ 1;
-    if (i == 0) embed_hist_kernel<<<blocks, kRadixThreads, 0, st>>>(from_ids, n, 0, bits, w.hist, blocks);
-    else embed_hist_kernel<<<blocks, kRadixThreads, 0, st>>>(sorted, n, i * bits, bits, w.hist, blocks);
-    if ((r = launched())) return r;
-    embed_scan_kernel<<<((1 << bits) + 7) / 8, 256, 0, st>>>(w.hist, blocks, 1 << bits, w.total);
-    if ((r = launched())) return r;
-    if (i == 0) embed_scatter_kernel<<<blocks, kRadixThreads, 0, st>>>(from_ids, n, 0, bits, w.hist, blocks, w.total, w.key[to], w.val[to]);
-    else embed_scatter_kernel<<<blocks, kRadixThreads, 0, st>>>(sorted, n, i * bits, bits, w.hist, blocks, w.total, w.key[to], w.val[to]);
-    if ((r = launched())) return r;
+    if (i == 0) r = launch(embed_hist_kernel<KeysFromIds<Id>>, blocks, kRadixThreads, 0, st, from_ids, n, 0, bits, w.hist, blocks, w.seen,
+                           (lm->vocab + 31) / 32);
+    else r = launch(embed_hist_kernel<KeysSorted>, blocks, kRadixThreads, 0, st, sorted, n, i * bits, bits, w.hist, blocks, nullptr, 0);
+    if (r) return r;
+    if ((r = launch(embed_scan_kernel, ((1 << bits) + 7) / 8, 256, 0, st, w.hist, blocks, 1 << bits, w.total))) return r;
+    if (i == 0) r = launch(embed_scatter_kernel<KeysFromIds<Id>>, blocks, kRadixThreads, 0, st, from_ids, n, 0, bits, w.hist, blocks, w.total,
+                           w.key[to], w.val[to]);
+    else r = launch(embed_scatter_kernel<KeysSorted>, blocks, kRadixThreads, 0, st, sorted, n, i * bits, bits, w.hist, blocks, w.total,
+                    w.key[to], w.val[to]);
+    if (r) return r;
     *src = to;
   }
-  if (cudaMemsetAsync(w.seen, 0, (size_t)((lm->vocab + 31) / 32) * 4, st) != cudaSuccess) return AUGTREE_ERR_CUDA;
-  embed_mark_kernel<<<(unsigned)((n + 255) / 256), 256, 0, st>>>(w.key[*src], n, lm->vocab, w.seen, w.joins);
-  return launched();
+  return launch(embed_mark_kernel, (unsigned)((n + 255) / 256), 256, 0, st, w.key[*src], n, lm->vocab, w.seen, w.joins);
 }
 
 template <typename In, typename Out>
@@ -346,14 +351,12 @@ int embed_sum_out(const augtree_lm *lm, const void *d_out, const EmbedWs &w, int
   if (w.n_chunks + zero_blocks == 0) return AUGTREE_OK;
   const int vecs = lm->hidden / 8, slabs = (vecs + kEmbedMaxThreads - 1) / kEmbedMaxThreads;
   const int threads = (int)up((vecs + slabs - 1) / slabs, 32);
-  embed_sum_kernel<<<dim3(w.n_chunks + zero_blocks, slabs), threads, 0, st>>>(static_cast<const In *>(d_out), w.key[src], w.val[src], n, w.chunk,
-                                                                           w.n_chunks, lm->vocab, lm->hidden, lm->embed_scale, accumulate,
-                                                                           dt, w.part, w.joins, w.seen);
-  int r = launched();
+  int r = launch(embed_sum_kernel<In, Out>, dim3(w.n_chunks + zero_blocks, slabs), threads, 0, st, static_cast<const In *>(d_out), w.key[src],
+                 w.val[src], n, w.chunk, w.n_chunks, lm->vocab, lm->hidden, lm->embed_scale, accumulate, dt, w.part, w.joins, w.seen);
   if (r || w.n_chunks < 2) return r;
   const unsigned grid = (unsigned)std::min<int64_t>((int64_t)(w.n_chunks - 1) * ((lm->hidden + 255) / 256), 8 * lm->n_lanes);
-  embed_join_kernel<<<grid, 256, 0, st>>>(w.key[src], w.chunk, w.n_chunks, lm->hidden, lm->embed_scale, accumulate, dt, w.part, w.joins);
-  return launched();
+  return launch(embed_join_kernel<Out>, grid, 256, 0, st, w.key[src], w.chunk, w.n_chunks, lm->hidden, lm->embed_scale, accumulate, dt, w.part,
+                w.joins);
 }
 
 template <typename In>
@@ -489,8 +492,7 @@ int augtree_lm_loss_fwd(const augtree_lm_t *lm, const void *hidden, const void *
     p.n = lm->vocab;
     if ((r = map_2d(&m.h, w.h, few, lm->hidden, few)) || (r = map_2d(&m.w, weight, lm->vocab, lm->hidden, 128))) return r;
     if ((r = launch_few<LM_STATS>(lm, few, m.w, m.h, p, st))) return r;
-    lm_few_finish_kernel<<<few, 256, 0, st>>>(w.part, 4 * lm->n_lanes, w.rows, w.tlogit, lm->logit_scale, loss, lse);
-    return launched();
+    return launch(lm_few_finish_kernel, few, 256, 0, st, w.part, 4 * lm->n_lanes, w.rows, w.tlogit, lm->logit_scale, loss, lse);
   }
   if ((r = map_2d(&m.h, w.h, rp, lm->hidden, 128)) || (r = map_2d(&m.w, weight, lm->vocab, lm->hidden, 128))) return r;
   LmParams p = base_params(lm, w, rp);
@@ -499,8 +501,7 @@ int augtree_lm_loss_fwd(const augtree_lm_t *lm, const void *hidden, const void *
   p.part = w.part; p.tlogit = w.tlogit;
   if ((r = launch_tiles(lm, m, p, st))) return r;
   const unsigned grid = (unsigned)std::min<int64_t>((n_tokens + 31) / 32, 2 * lm->n_lanes);
-  lm_finish_kernel<<<grid, 1024, 0, st>>>(w.part, n_part(lm), rp, w.rows, w.tlogit, lm->logit_scale, loss, lse);
-  return launched();
+  return launch(lm_finish_kernel, grid, 1024, 0, st, w.part, n_part(lm), rp, w.rows, w.tlogit, lm->logit_scale, loss, lse);
 }
 
 int augtree_lm_loss_bwd(const augtree_lm_t *lm, const void *hidden, const void *weight, const void *targets, int id_bytes,
@@ -565,8 +566,8 @@ int augtree_lm_loss_bwd(const augtree_lm_t *lm, const void *hidden, const void *
   }
   if (d_hidden) {
     const unsigned grid = (unsigned)std::min<int64_t>(n_tokens, 16 * lm->n_lanes);
-    lm_dh_kernel<<<grid, 256, 0, st>>>(w.dh_part, splits, few ? few : rp, lm->hidden, w.rows.pos, (int)n_tokens, static_cast<__nv_bfloat16 *>(d_hidden));
-    return launched();
+    return launch(lm_dh_kernel, grid, 256, 0, st, w.dh_part, splits, few ? few : rp, lm->hidden, w.rows.pos, (int)n_tokens,
+                  static_cast<__nv_bfloat16 *>(d_hidden));
   }
   return AUGTREE_OK;
 }

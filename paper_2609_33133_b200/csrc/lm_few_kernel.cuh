@@ -113,6 +113,7 @@ lm_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ 
   constexpr int NACC = KIND == LM_STATS ? (N <= 64 ? 4 : 2) : 1;  // accumulators of a tile, each N (DH: 2 N) columns
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   const uint32_t base = smem_u32(smem_raw);
+  launch_next();
   if (base & 1023u) {
     if (threadIdx.x == 0 && atomicCAS(p.status, 0, -6) == 0) p.status[1] = 5;
     return;
@@ -126,13 +127,15 @@ lm_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ 
   float *s_lse2 = reinterpret_cast<float *>(s_target + kLmFew), *s_gscale = s_lse2 + kLmFew;
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int n_rows = __ldg(p.n_rows);
   if (threadIdx.x == 0) {
     for (int s = 0; s < NST; ++s) { mbar_init(bar_full + 8 * s, 1); mbar_init(bar_empty + 8 * s, 1); }
     for (int s = 0; s < 2; ++s) { mbar_init(bar_acc_full + 8 * s, 1); mbar_init(bar_acc_empty + 8 * s, 4); }
     *abort_flag = 0;
     fence_barrier_init();
   }
+  if (warp == 5) { tmem_alloc(smem_u32((const void *)tmem_slot), 512); tmem_relinquish(); }
+  wait_previous();
+  const int n_rows = *reinterpret_cast<const volatile int *>(p.n_rows);
   if (KIND != LM_DH && threadIdx.x < N) {
     const bool live = threadIdx.x < n_rows;
     s_target[threadIdx.x] = live ? p.target[threadIdx.x] : -1;
@@ -141,7 +144,6 @@ lm_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ 
       s_gscale[threadIdx.x] = live ? p.gscale[threadIdx.x] : 0.f;
     }
   }
-  if (warp == 5) { tmem_alloc(smem_u32((const void *)tmem_slot), 512); tmem_relinquish(); }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();

@@ -31,6 +31,8 @@ template <typename Id>
 __global__ void __launch_bounds__(1024)
 lm_compact_kernel(const Id *targets, int tokens, int vocab, LmRows o, const float *lse, const float *d_loss, float logit_scale,
                   float *loss_out, float *lse_out, int *status) {
+  launch_next();
+  wait_previous();
   __shared__ int warp_sum[32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   int n = 0;
@@ -103,6 +105,8 @@ __device__ __forceinline__ float block_sum(float s, float *sh) {
 // also their targets' logits.
 __global__ void __launch_bounds__(256)
 lm_gather_kernel(const uint4 *hidden, const LmRows rows, uint4 *out, int row_vecs, const uint4 *weight) {
+  launch_next();
+  wait_previous();
   __shared__ float sh[8];
   const int n = *rows.n_rows, n_pad = (n + 255) / 256 * 256;
   for (int r = blockIdx.x; r < n_pad; r += gridDim.x) {
@@ -111,8 +115,8 @@ lm_gather_kernel(const uint4 *hidden, const LmRows rows, uint4 *out, int row_vec
     uint4 *dst = out + (long long)r * row_vecs;
     float s = 0.f;
     for (int i = threadIdx.x; i < row_vecs; i += 256) {
-      const uint4 v = src ? __ldg(src + i) : make_uint4(0, 0, 0, 0);
-      if (wt) s += dot8(v, __ldg(wt + i));
+      const uint4 v = src ? src[i] : make_uint4(0, 0, 0, 0);
+      if (wt) s += dot8(v, wt[i]);
       dst[i] = v;
     }
     if (wt) {
@@ -129,6 +133,8 @@ __global__ void __launch_bounds__(128)
 lm_few_rows_kernel(const Id *targets, int tokens, int vocab, LmRows o, const float *lse, const float *d_loss, float logit_scale,
                    float *loss_out, float *lse_out, int *status, const uint4 *hidden, uint4 *out, int row_vecs, int twice,
                    const uint4 *weight) {
+  launch_next();
+  wait_previous();
   __shared__ int warp_sum[4];
   __shared__ float sh[4];
   __shared__ int from;
@@ -166,8 +172,8 @@ lm_few_rows_kernel(const Id *targets, int tokens, int vocab, LmRows o, const flo
   const uint4 *wt = src && weight ? weight + (long long)targets[from] * row_vecs : nullptr;
   float s = 0.f;
   for (int i = t; i < row_vecs; i += 128) {
-    const uint4 v = src ? __ldg(src + i) : make_uint4(0, 0, 0, 0);
-    if (wt) s += dot8(v, __ldg(wt + i));
+    const uint4 v = src ? src[i] : make_uint4(0, 0, 0, 0);
+    if (wt) s += dot8(v, wt[i]);
     out[(long long)row * row_vecs + i] = v;
     if (twice) out[(long long)(gridDim.x + row) * row_vecs + i] = v;
   }
@@ -200,6 +206,8 @@ __device__ __forceinline__ void write_loss(float2 s, float tlogit, float x_targe
 __global__ void __launch_bounds__(256)
 lm_few_finish_kernel(const float2 *part, int n_part, const LmRows rows, const float *tlogit, float logit_scale,
                      float *loss, float *lse) {
+  launch_next();
+  wait_previous();
   __shared__ float2 sh[8];
   const int r = blockIdx.x;
   if (r >= *rows.n_rows) return;
@@ -221,6 +229,8 @@ lm_few_finish_kernel(const float2 *part, int n_part, const LmRows rows, const fl
 __global__ void __launch_bounds__(1024)
 lm_finish_kernel(const float2 *part, int n_part, long long rows_pad, const LmRows rows, const float *tlogit, float logit_scale,
                  float *loss, float *lse) {
+  launch_next();
+  wait_previous();
   __shared__ float2 sh[32][33];
   const int lane = threadIdx.x & 31, seg = threadIdx.x >> 5;
   const int n = *rows.n_rows;
@@ -252,6 +262,8 @@ lm_finish_kernel(const float2 *part, int n_part, long long rows_pad, const LmRow
 // dH of every token in bf16: the shares' partial sums added in order; zeros for rows that are not scored.
 __global__ void __launch_bounds__(256)
 lm_dh_kernel(const float *part, int splits, long long rows_pad, int hidden, const int *pos, int tokens, __nv_bfloat16 *d_hidden) {
+  launch_next();
+  wait_previous();
   const int vecs = hidden / 8;
   for (int t = blockIdx.x; t < tokens; t += gridDim.x) {
     const int r = pos[t];
@@ -320,6 +332,8 @@ template <> struct Vec<__half> {
 template <typename Id, typename In, typename Out>
 __global__ void __launch_bounds__(128)
 embed_fwd_kernel(const In *table, const Id *ids, int tokens, int vocab, int hidden, float scale, Out *out, int *status) {
+  launch_next();
+  wait_previous();
   for (int t = blockIdx.x; t < tokens; t += gridDim.x) {
     const long long id = ids[t];
     const bool live = id >= 0 && id < vocab;
@@ -364,9 +378,12 @@ struct KeysFromIds {
 
 template <typename Keys>
 __global__ void __launch_bounds__(kRadixThreads)
-embed_hist_kernel(const Keys in, int n, int shift, int bits, int *hist, int n_blocks) {
+embed_hist_kernel(const Keys in, int n, int shift, int bits, int *hist, int n_blocks, uint32_t *seen, int seen_words) {
+  launch_next();
+  wait_previous();
   __shared__ int cnt[kSortBins];
   for (int i = threadIdx.x; i < kSortBins; i += kRadixThreads) cnt[i] = 0;
+  for (int i = blockIdx.x * kRadixThreads + threadIdx.x; i < seen_words; i += gridDim.x * kRadixThreads) seen[i] = 0;  // (first pass)
   __syncthreads();
   const int b0 = blockIdx.x * kRadixBlock;
   for (int i = threadIdx.x; i < kRadixBlock && b0 + i < n; i += kRadixThreads) {
@@ -380,6 +397,8 @@ embed_hist_kernel(const Keys in, int n, int shift, int bits, int *hist, int n_bl
 // one warp per bin: exclusive prefix sum over the blocks, total of the bin behind it
 __global__ void __launch_bounds__(256)
 embed_scan_kernel(int *hist, int n_blocks, int bins, int *total) {
+  launch_next();
+  wait_previous();
   const int bin = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
   if (bin >= bins) return;
   int run = 0;
@@ -400,6 +419,8 @@ embed_scan_kernel(int *hist, int n_blocks, int bins, int *total) {
 template <typename Keys>
 __global__ void __launch_bounds__(kRadixThreads)
 embed_scatter_kernel(const Keys in, int n, int shift, int bits, const int *hist, int n_blocks, const int *total, uint32_t *key_out, int *val_out) {
+  launch_next();
+  wait_previous();
   __shared__ int cnt[kRadixWarps][kSortBins];
   __shared__ int wsum[kRadixWarps];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, bins = 1 << bits;
@@ -472,6 +493,8 @@ __device__ __forceinline__ void embed_mark(const uint32_t *key, int i, int vocab
   if (k < (uint32_t)vocab && (i == 0 || key[i - 1] != k)) atomicOr(seen + (k >> 5), 1u << (k & 31));
 }
 __global__ void embed_mark_kernel(const uint32_t *key, int n, int vocab, uint32_t *seen, int *joins) {
+  launch_next();
+  wait_previous();
   const int i = blockIdx.x * blockDim.x + threadIdx.x;
   if (i < 2) joins[i] = 0;
   if (i < n) embed_mark(key, i, vocab, seen);
@@ -486,6 +509,8 @@ template <typename Id>
 __global__ void __launch_bounds__(512)
 embed_sort_small_kernel(const Id *ids, int n, int vocab, int passes, int bits, uint32_t *key_out, int *val_out,
                         int *joins, uint32_t *seen, int *status) {
+  launch_next();
+  wait_previous();
   extern __shared__ __align__(16) int sort_smem[];
   int *cnt = sort_smem;                        // [16][kSortBins]
   uint32_t *skey = reinterpret_cast<uint32_t *>(sort_smem + 16 * kSortBins);
@@ -580,6 +605,8 @@ template <typename In, typename Out>
 __global__ void __launch_bounds__(kEmbedMaxThreads)
 embed_sum_kernel(const In *d_out, const uint32_t *key, const int *val, int n, int chunk, int n_chunks, int vocab, int hidden,
                  float scale, int accumulate, Out *d_table, float *part, int *joins, const uint32_t *seen) {
+  launch_next();
+  wait_previous();
   __shared__ uint32_t skey[kEmbedMaxChunk];
   __shared__ int sval[kEmbedMaxChunk];
   const int col = (blockIdx.y * blockDim.x + threadIdx.x) * 8;
@@ -644,6 +671,8 @@ template <typename Out>
 __global__ void __launch_bounds__(256)
 embed_join_kernel(const uint32_t *key, int chunk, int n_chunks, int hidden, float scale, int accumulate, Out *d_table, const float *part,
                   const int *joins) {
+  launch_next();
+  wait_previous();
   __shared__ float sh[8][264];
   const int lane = threadIdx.x & 31, seg = threadIdx.x >> 5;
   const int n_long = joins[1], s_long = (hidden + 255) / 256, items_long = n_long * s_long;

@@ -130,6 +130,7 @@ lm_tile_kernel(const __grid_constant__ CUtensorMap tm_h, const __grid_constant__
   constexpr int NST = SM::kStages;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   const uint32_t base = smem_u32(smem_raw);
+  launch_next();
   if (base & 1023u) {  // the same in both CTAs of a pair
     if (threadIdx.x == 0 && atomicCAS(p.status, 0, -6) == 0) p.status[1] = 4;
     return;
@@ -153,9 +154,10 @@ lm_tile_kernel(const __grid_constant__ CUtensorMap tm_h, const __grid_constant__
   cluster_sync();
   tc_fence_after();
   const uint32_t rank = cluster_ctarank();
+  wait_previous();
   const uint32_t tmem = *tmem_slot;
   const AbortCtx ab{abort_flag, p.status, p.wait_budget};
-  const int n_rows = __ldg(p.n_rows);
+  const int n_rows = *reinterpret_cast<const volatile int *>(p.n_rows);
   const int t0 = blockIdx.x >> 1, tstep = gridDim.x >> 1;
   LmTileCoord c;
 
