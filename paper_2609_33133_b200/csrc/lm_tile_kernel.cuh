@@ -24,6 +24,8 @@
 #pragma once
 #include <cuda.h>
 
+#include <type_traits>
+
 #include "ptx.cuh"
 
 namespace augtree {
@@ -159,37 +161,49 @@ lm_tile_kernel(const __grid_constant__ CUtensorMap tm_h, const __grid_constant__
   const AbortCtx ab{abort_flag, p.status, p.wait_budget};
   const int n_rows = *reinterpret_cast<const volatile int *>(p.n_rows);
   const int t0 = blockIdx.x >> 1, tstep = gridDim.x >> 1;
-  LmTileCoord c;
+  LmTileCoord c = {};
 
   if (warp == 8) {
     // ------------------------------------------------------------ TMA producer
+    // One thread issues every load, so its own instructions are on the path of a stage: the loop is compiled for each kind,
+    // with the maps as constants and nothing left to compute but coordinates.
     if (lane == 0) {
-      uint32_t T = 0;
-      bool ok = true;
+      const uint32_t full_leader = map_to_rank(bar_full, 0);
+      uint32_t st = 0, phase = 1;
+      bool ok = true, skip = (p.test_flags & TEST_SKIP_FWD_LOAD) && blockIdx.x == 0;
+      auto produce = [&](auto kind_tag) {
+        constexpr int kKind = decltype(kind_tag)::value;
+        const int m0 = c.m * kLmTile + rank * 128, n0 = c.n * kLmTile + rank * 128;  // this CTA's rows of A, columns of B
+        const int mc = m0 >> 6, nc = n0 >> 6, w0 = p.v0 + n0;
+        const bool one_box = p.mn_chunks == 2;
+        int k0 = c.kb0 * 64;
+        for (int left = c.nkb; left > 0; --left, k0 += 64) {
+          if (!mbar_wait(bar_empty + 8 * st, phase, ab, WAIT_LM_EMPTY)) { ok = false; break; }
+          const uint32_t sA = base + st * SM::kStageBytes, sB = sA + SM::kABytes, bar = full_leader + 8 * st;
+          if (!skip) {
+            if (rank == 0) mbar_expect_tx(bar_full + 8 * st, 2 * SM::kStageBytes);
+            if constexpr (kKind <= LM_GRAD) {
+              tma_load_2d_pair(sA, &tm_h, bar, k0, m0);
+              tma_load_2d_pair(sB, &tm_w, bar, k0, w0);
+            } else if constexpr (kKind == LM_DH) {
+              tma_load_2d_pair(sA, &tm_g, bar, k0, m0);
+              if (one_box) tma_load_3d_pair(sB, &tm_w_mn, bar, 0, p.v0 + k0, nc);
+              else for (int b = 0; b < 2; ++b) tma_load_3d_pair(sB + b * 8192, &tm_w_mn, bar, n0 + b * 64, p.v0 + k0, 0);
+            } else {
+              tma_load_3d_pair(sA, &tm_g_mn, bar, 0, k0, mc);
+              if (one_box) tma_load_3d_pair(sB, &tm_h_mn, bar, 0, k0, nc);
+              else for (int b = 0; b < 2; ++b) tma_load_3d_pair(sB + b * 8192, &tm_h_mn, bar, n0 + b * 64, k0, 0);
+            }
+          }
+          skip = false;
+          if (++st == NST) { st = 0; phase ^= 1; }
+        }
+      };
       for (int t = t0; ok && lm_tile(p, n_rows, t, c); t += tstep) {
         const int kind = p.job[c.job].kind;
-        const int m0 = c.m * kLmTile + rank * 128, n0 = c.n * kLmTile + rank * 128;  // this CTA's rows of A, columns of B
-        for (int kb = c.kb0; kb < c.kb0 + c.nkb && ok; ++kb, ++T) {
-          const uint32_t st = T % NST, bar = map_to_rank(bar_full + 8 * st, 0);
-          ok = mbar_wait(bar_empty + 8 * st, ((T / NST) & 1) ^ 1, ab, WAIT_LM_EMPTY);
-          if (!ok) break;
-          const uint32_t sA = base + st * SM::kStageBytes, sB = sA + SM::kABytes;
-          const int k0 = kb * 64;
-          if ((p.test_flags & TEST_SKIP_FWD_LOAD) && blockIdx.x == 0 && T == 0) continue;
-          if (rank == 0) mbar_expect_tx(bar_full + 8 * st, 2 * SM::kStageBytes);
-          if (kind <= LM_GRAD) {
-            tma_load_2d_pair(sA, &tm_h, bar, k0, m0);
-            tma_load_2d_pair(sB, &tm_w, bar, k0, p.v0 + n0);
-          } else {
-            const bool dh = kind == LM_DH;
-            if (dh) tma_load_2d_pair(sA, &tm_g, bar, k0, m0);
-            else tma_load_3d_pair(sA, &tm_g_mn, bar, 0, k0, m0 >> 6);
-            const CUtensorMap *tm_b = dh ? &tm_w_mn : &tm_h_mn;
-            const int kr = dh ? p.v0 + k0 : k0;
-            if (p.mn_chunks == 2) tma_load_3d_pair(sB, tm_b, bar, 0, kr, n0 >> 6);
-            else for (int b = 0; b < 2; ++b) tma_load_3d_pair(sB + b * 8192, tm_b, bar, n0 + b * 64, kr, 0);
-          }
-        }
+        if (kind <= LM_GRAD) produce(std::integral_constant<int, LM_GRAD>{});
+        else if (kind == LM_DH) produce(std::integral_constant<int, LM_DH>{});
+        else produce(std::integral_constant<int, LM_DW>{});
       }
     }
   } else if (warp == 9) {
