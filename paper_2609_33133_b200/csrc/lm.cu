@@ -45,7 +45,7 @@ struct Cursor {
 
 struct LossWs {
   LmRows rows;
-  __nv_bfloat16 *h;       // [rows_pad][hidden] scored rows
+  __nv_bfloat16 *h;       // [rows_pad][pad_cols] scored rows
   float *tlogit;          // forward
   float2 *part;           // forward: [n_part][rows_pad]
   __nv_bfloat16 *grad;    // backward: [rows_pad][piece]
@@ -58,6 +58,8 @@ int n_part(const augtree_lm *lm) { return 2 * (int)((lm->vocab + kLmTile - 1) / 
 int few_rows(int64_t tokens) { return tokens <= 16 ? 16 : tokens <= 32 ? 32 : tokens <= 64 ? 64 : tokens <= kLmFew ? 128 : 0; }
 // rows of the packed hidden states and of G in the scratch
 int64_t pad_rows(int64_t tokens) { return few_rows(tokens) ? 2 * few_rows(tokens) : up(tokens, 256); }
+
+int64_t pad_cols(const augtree_lm *lm) { return up(lm->hidden, 64); }
 
 // Columns of a piece of the vocabulary in the backward pass: as many as fit the scratch bound for G, in equal pieces.
 // With the default bound a piece has 4096 columns at least, so that the additions into dH's partial sums, one per
@@ -104,7 +106,7 @@ size_t loss_layout(const augtree_lm *lm, int64_t tokens, bool bwd, uint8_t *base
   w->rows.idx = c.take<int>(rp);
   w->rows.pos = c.take<int>(rp);
   w->rows.target = c.take<int>(rp);
-  w->h = c.take<__nv_bfloat16>(rp * lm->hidden);
+  w->h = c.take<__nv_bfloat16>(rp * pad_cols(lm));
   if (!bwd) {
     w->rows.lse2 = w->rows.gscale = nullptr;
     w->rows.x_target = c.take<float>(rp);
@@ -225,13 +227,13 @@ int compact(const augtree_lm *lm, const void *targets, int id_bytes, int64_t tok
   const auto *ids32 = static_cast<const int *>(targets);
   const auto *src = static_cast<const uint4 *>(hidden), *wt = static_cast<const uint4 *>(weight);
   auto *dst = reinterpret_cast<uint4 *>(w.h);
-  const int n = (int)tokens, row_vecs = lm->hidden / 8;
+  const int n = (int)tokens, row_vecs = lm->hidden / 8, out_vecs = (int)pad_cols(lm) / 8;
   if (const int few = few_rows(tokens)) {
     if (id_bytes == 8)
       return launch(lm_few_rows_kernel<long long>, few, 128, 0, st, ids64, n, lm->vocab, w.rows, lse, d_loss, lm->logit_scale, loss_out, lse_out,
-                    lm->d_status, src, dst, row_vecs, lse != nullptr, wt);
+                    lm->d_status, src, dst, row_vecs, out_vecs, lse != nullptr, wt);
     return launch(lm_few_rows_kernel<int>, few, 128, 0, st, ids32, n, lm->vocab, w.rows, lse, d_loss, lm->logit_scale, loss_out, lse_out,
-                  lm->d_status, src, dst, row_vecs, lse != nullptr, wt);
+                  lm->d_status, src, dst, row_vecs, out_vecs, lse != nullptr, wt);
   }
   const int r = id_bytes == 8 ? launch(lm_compact_kernel<long long>, 1, 1024, 0, st, ids64, n, lm->vocab, w.rows, lse, d_loss, lm->logit_scale,
                                        loss_out, lse_out, lm->d_status)
@@ -239,7 +241,7 @@ int compact(const augtree_lm *lm, const void *targets, int id_bytes, int64_t tok
                                        loss_out, lse_out, lm->d_status);
   if (r) return r;
   const unsigned grid = (unsigned)std::min<int64_t>(up(tokens, 256), 8 * lm->n_lanes);
-  return launch(lm_gather_kernel, grid, 256, 0, st, src, w.rows, dst, row_vecs, wt);
+  return launch(lm_gather_kernel, grid, 256, 0, st, src, w.rows, dst, row_vecs, out_vecs, wt);
 }
 
 LmParams base_params(const augtree_lm *lm, const LossWs &w, int64_t rows_pad) {
@@ -490,11 +492,11 @@ int augtree_lm_loss_fwd(const augtree_lm_t *lm, const void *hidden, const void *
   if (few) {
     FewParams p = few_params(lm, w, base_params(lm, w, few));
     p.n = lm->vocab;
-    if ((r = map_2d(&m.h, w.h, few, lm->hidden, few)) || (r = map_2d(&m.w, weight, lm->vocab, lm->hidden, 128))) return r;
+    if ((r = map_2d(&m.h, w.h, few, pad_cols(lm), few)) || (r = map_2d(&m.w, weight, lm->vocab, lm->hidden, 128))) return r;
     if ((r = launch_few<LM_STATS>(lm, few, m.w, m.h, p, st))) return r;
     return launch(lm_few_finish_kernel, few, 256, 0, st, w.part, 4 * lm->n_lanes, w.rows, w.tlogit, lm->logit_scale, loss, lse);
   }
-  if ((r = map_2d(&m.h, w.h, rp, lm->hidden, 128)) || (r = map_2d(&m.w, weight, lm->vocab, lm->hidden, 128))) return r;
+  if ((r = map_2d(&m.h, w.h, rp, pad_cols(lm), 128)) || (r = map_2d(&m.w, weight, lm->vocab, lm->hidden, 128))) return r;
   LmParams p = base_params(lm, w, rp);
   p.n_jobs = 1;
   p.job[0] = {LM_STATS, 0, lm->vocab, lm->hidden, 1};
@@ -529,8 +531,8 @@ int augtree_lm_loss_bwd(const augtree_lm_t *lm, const void *hidden, const void *
   const int splits = few ? few_splits(lm, cols) : dh_splits(lm, rp, cols), chunks = lm->hidden % 64 == 0 ? 2 : 1;
   if ((r = compact(lm, targets, id_bytes, n_tokens, hidden, nullptr, w, lse, d_loss, nullptr, nullptr, st))) return r;
   Maps m = {};
-  if ((r = map_2d(&m.h, w.h, rp, lm->hidden, few ? few : 128)) || (r = map_2d(&m.w, weight, lm->vocab, lm->hidden, 128)) ||
-      (r = map_mn(&m.h_mn, w.h, rp, lm->hidden, chunks)) || (r = map_mn(&m.w_mn, weight, lm->vocab, lm->hidden, chunks)) ||
+  if ((r = map_2d(&m.h, w.h, rp, pad_cols(lm), few ? few : 128)) || (r = map_2d(&m.w, weight, lm->vocab, lm->hidden, 128)) ||
+      (r = map_mn(&m.h_mn, w.h, rp, pad_cols(lm), 2)) || (r = map_mn(&m.w_mn, weight, lm->vocab, lm->hidden, chunks)) ||
       (r = map_2d(&m.g, w.grad, rp, cols, few ? 2 * few : 128)) || (r = map_mn(&m.g_mn, w.grad, rp, cols, 2)))
     return r;
   LmParams p = base_params(lm, w, rp);

@@ -101,10 +101,10 @@ __device__ __forceinline__ float block_sum(float s, float *sh) {
   return s;
 }
 
-// Hidden states of the scored rows, packed; zeros up to the next multiple of 256 rows (they enter contractions).  With `weight`
-// also their targets' logits.
+// Hidden states of the scored rows, packed; zeros up to the next multiple of 256 rows (they enter contractions), and up to the next
+// multiple of 64 columns, so that every box of the copy engine is whole lines.  With `weight` also their targets' logits.
 __global__ void __launch_bounds__(256)
-lm_gather_kernel(const uint4 *hidden, const LmRows rows, uint4 *out, int row_vecs, const uint4 *weight) {
+lm_gather_kernel(const uint4 *hidden, const LmRows rows, uint4 *out, int row_vecs, int out_vecs, const uint4 *weight) {
   launch_next();
   wait_previous();
   __shared__ float sh[8];
@@ -112,11 +112,11 @@ lm_gather_kernel(const uint4 *hidden, const LmRows rows, uint4 *out, int row_vec
   for (int r = blockIdx.x; r < n_pad; r += gridDim.x) {
     const uint4 *src = r < n ? hidden + (long long)rows.idx[r] * row_vecs : nullptr;
     const uint4 *wt = src && weight ? weight + (long long)rows.target[r] * row_vecs : nullptr;
-    uint4 *dst = out + (long long)r * row_vecs;
+    uint4 *dst = out + (long long)r * out_vecs;
     float s = 0.f;
-    for (int i = threadIdx.x; i < row_vecs; i += 256) {
-      const uint4 v = src ? src[i] : make_uint4(0, 0, 0, 0);
-      if (wt) s += dot8(v, wt[i]);
+    for (int i = threadIdx.x; i < out_vecs; i += 256) {
+      const uint4 v = src && i < row_vecs ? src[i] : make_uint4(0, 0, 0, 0);
+      if (wt && i < row_vecs) s += dot8(v, wt[i]);
       dst[i] = v;
     }
     if (wt) {
@@ -131,8 +131,8 @@ lm_gather_kernel(const uint4 *hidden, const LmRows rows, uint4 *out, int row_vec
 template <typename Id>
 __global__ void __launch_bounds__(128)
 lm_few_rows_kernel(const Id *targets, int tokens, int vocab, LmRows o, const float *lse, const float *d_loss, float logit_scale,
-                   float *loss_out, float *lse_out, int *status, const uint4 *hidden, uint4 *out, int row_vecs, int twice,
-                   const uint4 *weight) {
+                   float *loss_out, float *lse_out, int *status, const uint4 *hidden, uint4 *out, int row_vecs,
+                   int out_vecs, int twice, const uint4 *weight) {
   launch_next();
   wait_previous();
   __shared__ int warp_sum[4];
@@ -171,11 +171,11 @@ lm_few_rows_kernel(const Id *targets, int tokens, int vocab, LmRows o, const flo
   const uint4 *src = from >= 0 ? hidden + (long long)from * row_vecs : nullptr;
   const uint4 *wt = src && weight ? weight + (long long)targets[from] * row_vecs : nullptr;
   float s = 0.f;
-  for (int i = t; i < row_vecs; i += 128) {
-    const uint4 v = src ? src[i] : make_uint4(0, 0, 0, 0);
-    if (wt) s += dot8(v, wt[i]);
-    out[(long long)row * row_vecs + i] = v;
-    if (twice) out[(long long)(gridDim.x + row) * row_vecs + i] = v;
+  for (int i = t; i < out_vecs; i += 128) {
+    const uint4 v = src && i < row_vecs ? src[i] : make_uint4(0, 0, 0, 0);
+    if (wt && i < row_vecs) s += dot8(v, wt[i]);
+    out[(long long)row * out_vecs + i] = v;
+    if (twice) out[(long long)(gridDim.x + row) * out_vecs + i] = v;
   }
   if (wt) {
     s = block_sum<128>(s, sh);

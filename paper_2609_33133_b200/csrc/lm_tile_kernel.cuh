@@ -52,7 +52,7 @@ struct LmParams {
   int n_jobs;
   const int *n_rows;        // device: rows that are scored
   int v0, vocab, hidden;    // first vocabulary row of the piece; whole sizes
-  int mn_chunks;            // 64-column chunks in a box of tm_h_mn and tm_w_mn: 2, or 1 (hidden not a multiple of 64)
+  int mn_chunks;            // 64-column chunks in a box of tm_w_mn: 2, or 1 (hidden not a multiple of 64)
   long long rows_pad;       // leading size of per-row arrays and of the partial sums
   float scale_log2;         // c log2(e)
   const int *target;        // [rows_pad]
@@ -191,8 +191,7 @@ lm_tile_kernel(const __grid_constant__ CUtensorMap tm_h, const __grid_constant__
               else for (int b = 0; b < 2; ++b) tma_load_3d_pair(sB + b * 8192, &tm_w_mn, bar, n0 + b * 64, p.v0 + k0, 0);
             } else {
               tma_load_3d_pair(sA, &tm_g_mn, bar, 0, k0, mc);
-              if (one_box) tma_load_3d_pair(sB, &tm_h_mn, bar, 0, k0, nc);
-              else for (int b = 0; b < 2; ++b) tma_load_3d_pair(sB + b * 8192, &tm_h_mn, bar, n0 + b * 64, k0, 0);
+              tma_load_3d_pair(sB, &tm_h_mn, bar, 0, k0, nc);
             }
           }
           skip = false;
