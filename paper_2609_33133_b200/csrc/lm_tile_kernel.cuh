@@ -76,33 +76,59 @@ struct LmSmem {
   static constexpr int kBytes = kOffBar + 256;
 };
 
-struct LmTileCoord {
-  int job, m, n, split, kb0, nkb;
-};
+// Walks the tiles of one CTA pair: tile t0, t0 + step, .. of all jobs in a row.  The index that runs fastest is the one whose
+// operand is the smaller: the tiles in flight then share the large operand's rows while the small one stays in L2.  From tile to
+// tile the coordinates move on by additions alone; divisions are left to the start of a job (with them in every step each
+// role spent 2400 cycles a tile on finding it, more than a tile of 64 rows takes).
+struct LmTile {
+  int kind, m, n, split, kb0, nkb;   // product, tile coordinates, share of the contraction: first step, steps
+  int cols, m_fixed;                 // of the job
+  int t, job, first, count, step, mt, nt, kb, per, d_fast, d_slow;
 
-// Tile number -> job, tile coordinates and contraction range.  The index that runs fastest is the one whose operand
-// is the smaller: the tiles in flight then share the large operand's rows while the small one stays in L2.
-__device__ __forceinline__ bool lm_tile(const LmParams &p, int n_rows, int t, LmTileCoord &c) {
-  for (int j = 0; j < p.n_jobs; ++j) {
-    const LmJob &J = p.job[j];
-    const int mt = ((J.m_fixed ? J.m_fixed : n_rows) + kLmTile - 1) / kLmTile;
-    const int nt = (J.n + kLmTile - 1) / kLmTile;
-    const int kb = ((J.k_fixed ? J.k_fixed : n_rows) + 63) / 64;
-    const int count = mt * nt * J.splits;
-    if (t < count) {
-      c.job = j;
-      const int per = (kb + J.splits - 1) / J.splits;
-      if (J.kind <= LM_GRAD) { c.m = t % mt; c.n = t / mt; c.split = 0; }
-      else { c.split = t / (mt * nt); const int r = t % (mt * nt); c.n = r % nt; c.m = r / nt;
-      }
-      c.kb0 = min(c.split * per, kb);
-      c.nkb = min(per, kb - c.kb0);
-      return true;
-    }
-    t -= count;
+  __device__ __forceinline__ bool start(const LmParams &p, int n_rows, int t0, int tile_step) {
+    t = t0; step = tile_step; job = 0; first = 0;
+    return enter(p, n_rows);
   }
-  return false;
-}
+  // the job that holds tile t, from `job` on
+  __device__ __forceinline__ bool enter(const LmParams &p, int n_rows) {
+    for (; job < p.n_jobs; ++job, first += count) {
+      const LmJob J = job == 0 ? p.job[0] : p.job[1];
+      kind = J.kind; cols = J.n; m_fixed = J.m_fixed;
+      mt = ((J.m_fixed ? J.m_fixed : n_rows) + kLmTile - 1) / kLmTile;
+      nt = (J.n + kLmTile - 1) / kLmTile;
+      kb = ((J.k_fixed ? J.k_fixed : n_rows) + 63) / 64;
+      count = mt * nt * J.splits;
+      if (t < first + count) {
+        const int r = t - first, fast = kind <= LM_GRAD ? mt : nt;
+        per = (kb + J.splits - 1) / J.splits;
+        d_fast = step % fast; d_slow = step / fast;
+        if (kind <= LM_GRAD) { m = r % mt; n = r / mt; split = 0; }
+        else { n = r % nt; m = r / nt; split = m / mt; m -= split * mt; }
+        range();
+        return true;
+      }
+    }
+    return false;
+  }
+  __device__ __forceinline__ void range() {
+    kb0 = min(split * per, kb);
+    nkb = min(per, kb - kb0);
+  }
+  __device__ __forceinline__ bool next(const LmParams &p, int n_rows) {
+    t += step;
+    if (t >= first + count) { first += count; ++job; return enter(p, n_rows); }
+    if (kind <= LM_GRAD) {
+      m += d_fast; n += d_slow;
+      if (m >= mt) { m -= mt; ++n; }
+    } else {
+      n += d_fast; m += d_slow;
+      if (n >= nt) { n -= nt; ++m; }
+      while (m >= mt) { m -= mt; ++split; }
+      range();
+    }
+    return true;
+  }
+};
 
 // A row's columns into the warp's 4 KB block, in the 128-byte swizzle (16-byte chunk j of row r sits at j ^ (r % 8)): 32 columns
 // of 16 bits as the chunks from `chunk`, or 32 columns of 32 bits.
@@ -161,7 +187,8 @@ lm_tile_kernel(const __grid_constant__ CUtensorMap tm_h, const __grid_constant__
   const AbortCtx ab{abort_flag, p.status, p.wait_budget};
   const int n_rows = *reinterpret_cast<const volatile int *>(p.n_rows);
   const int t0 = blockIdx.x >> 1, tstep = gridDim.x >> 1;
-  LmTileCoord c = {};
+  LmTile c = {};
+  bool more = c.start(p, n_rows, t0, tstep);
 
   if (warp == 8) {
     // ------------------------------------------------------------ TMA producer
@@ -198,10 +225,9 @@ lm_tile_kernel(const __grid_constant__ CUtensorMap tm_h, const __grid_constant__
           if (++st == NST) { st = 0; phase ^= 1; }
         }
       };
-      for (int t = t0; ok && lm_tile(p, n_rows, t, c); t += tstep) {
-        const int kind = p.job[c.job].kind;
-        if (kind <= LM_GRAD) produce(std::integral_constant<int, LM_GRAD>{});
-        else if (kind == LM_DH) produce(std::integral_constant<int, LM_DH>{});
+      for (; ok && more; more = c.next(p, n_rows)) {
+        if (c.kind <= LM_GRAD) produce(std::integral_constant<int, LM_GRAD>{});
+        else if (c.kind == LM_DH) produce(std::integral_constant<int, LM_DH>{});
         else produce(std::integral_constant<int, LM_DW>{});
       }
     }
@@ -211,9 +237,8 @@ lm_tile_kernel(const __grid_constant__ CUtensorMap tm_h, const __grid_constant__
     const bool elected = elect_one();
     uint32_t T = 0, ic = 0;
     bool ok = true;
-    for (int t = t0; ok && lm_tile(p, n_rows, t, c); t += tstep, ++ic) {
-      const int kind = p.job[c.job].kind;
-      const int a_mn = kind == LM_DW, b_mn = kind >= LM_DH;
+    for (; ok && more; more = c.next(p, n_rows), ++ic) {
+      const int a_mn = c.kind == LM_DW, b_mn = c.kind >= LM_DH;
       const uint32_t idesc = make_idesc(256, kLmTile, a_mn, b_mn);
       const uint32_t a_step = a_mn ? 2048 >> 4 : 32 >> 4, b_step = b_mn ? 2048 >> 4 : 32 >> 4;
       const uint32_t buf = ic & 1;
@@ -247,15 +272,14 @@ lm_tile_kernel(const __grid_constant__ CUtensorMap tm_h, const __grid_constant__
     const int half = warp >> 2, col0 = half * 128;
     uint32_t ic = 0;
     bool ok = true;
-    for (int t = t0; ok && lm_tile(p, n_rows, t, c); t += tstep, ++ic) {
-      const LmJob &J = p.job[c.job];
+    for (; ok && more; more = c.next(p, n_rows), ++ic) {
       const uint32_t buf = ic & 1;
       ok = mbar_wait(bar_acc_full + 8 * buf, (ic >> 1) & 1, ab, WAIT_LM_ACC_FULL);
       if (!ok) break;
       tc_fence_after();
       const uint32_t tD = tmem + buf * kLmTile + lane_off + col0;
       const int row0 = c.m * kLmTile + rank * 128 + (warp & 3) * 32, row = row0 + lane, n0 = c.n * kLmTile + col0;  // tile row, first column of this warp
-      if (J.kind == LM_STATS) {
+      if (c.kind == LM_STATS) {
         const int tgt = row < n_rows ? p.target[row] - p.v0 - n0 : -1;  // column of the target, relative
         float m = -INFINITY, l = 0.f, xt = 0.f;
         bool hit = false;
@@ -263,7 +287,7 @@ lm_tile_kernel(const __grid_constant__ CUtensorMap tm_h, const __grid_constant__
           uint32_t v[32];
           tmem_ld32(tD + q * 32, v);
           tc_wait_ld();
-          const int left = J.n - (n0 + q * 32);  // columns that exist
+          const int left = c.cols - (n0 + q * 32);  // columns that exist
           if ((unsigned)(tgt - q * 32) < 32u) {
             hit = true;
 #pragma unroll
@@ -286,7 +310,7 @@ lm_tile_kernel(const __grid_constant__ CUtensorMap tm_h, const __grid_constant__
           p.part[(long long)(2 * ((p.v0 / kLmTile) + c.n) + half) * p.rows_pad + row] = make_float2(m, l);
           if (hit) p.tlogit[row] = xt;
         }
-      } else if (J.kind == LM_GRAD) {
+      } else if (c.kind == LM_GRAD) {
         const bool live = row < n_rows;
         const int tgt = live ? p.target[row] - p.v0 - n0 : -1;
         const float lse2 = live ? p.lse2[row] : 0.f, gs = live ? p.gscale[row] : 0.f;
@@ -294,7 +318,7 @@ lm_tile_kernel(const __grid_constant__ CUtensorMap tm_h, const __grid_constant__
           uint32_t v[32];
           tmem_ld32(tD + q * 32, v);
           tc_wait_ld();
-          const int left = J.n - (n0 + q * 32);
+          const int left = c.cols - (n0 + q * 32);
           float g[32];
 #pragma unroll
           for (int e = 0; e < 32; ++e) {
@@ -310,11 +334,11 @@ lm_tile_kernel(const __grid_constant__ CUtensorMap tm_h, const __grid_constant__
           }
         }
       } else {
-        const bool dh = J.kind == LM_DH, f32 = dh || p.dw_f32, add = dh ? p.dh_add : p.dw_add;
+        const bool dh = c.kind == LM_DH, f32 = dh || p.dw_f32, add = dh ? p.dh_add : p.dw_add;
         const bool zero = c.nkb == 0;   // an empty contraction: nothing was accumulated
         const CUtensorMap *map = dh ? &tm_dh : &tm_out;
         // (a box that begins outside is left out; one that only ends outside is cut off by the map)
-        const bool inside = row0 < (dh ? n_rows : J.m_fixed);
+        const bool inside = row0 < (dh ? n_rows : c.m_fixed);
         const long long out_row = dh ? c.split * p.rows_pad + row0 : p.v0 + row0;
         for (int q = 0; q < 4; ++q) {
           uint32_t v[32];
