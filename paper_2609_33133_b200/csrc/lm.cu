@@ -132,11 +132,11 @@ struct EmbedWs {
   int chunk, n_chunks;
 };
 
-// Sorted tokens of a chunk: short ones, so that a few thousand tokens fill the GPU, longer ones when there are enough
-// blocks anyway (the crossing rows' sums cost a write and a read of their own).
+// Sorted tokens of a chunk: 32 (24576 tokens x 3584 bf16: 237 us against 243 with 16; 131071 x 1032 fp32: 151 us against 155 with 64), half
+// of that when there are too few to give every SM blocks, more when the sums of the rows that cross chunks would grow large.
 int embed_chunk(const augtree_lm *lm, int64_t n) {
-  int chunk = 16;
-  while (chunk < kEmbedMaxChunk && n / chunk > 32ll * lm->n_lanes) chunk *= 2;
+  int chunk = n <= 8192 ? 16 : 32;
+  while (chunk < kEmbedMaxChunk && n / chunk > 64ll * lm->n_lanes) chunk *= 2;
   return chunk;
 }
 

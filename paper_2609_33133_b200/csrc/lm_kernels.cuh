@@ -580,9 +580,10 @@ embed_sort_small_kernel(const Id *ids, int n, int vocab, int passes, int bits, u
 
 // ---- d_table[v] (+)= scale sum of d_out over the tokens of v, in the order of the tokens, in fp32, rounded once.
 // A frequent id owns thousands of tokens and a rare one a single token, so the sorted tokens are cut into chunks of equal
-// length, whatever ids they hold: a chunk writes the rows that lie inside it and leaves the sums of the row that comes in
-// from the chunk before (slot 0) and of the row that goes on into the next (slot 1) to embed_join_kernel, which adds a
-// row's sums up in order.  Bound by HBM: every gradient row read once, every table row written once.  A thread has eight
+// length, whatever ids they hold: a chunk writes the rows that lie inside it.  A row that starts in a chunk and ends in the next
+// belongs to the first of the two, which goes on to the row's end.  Of a row over three chunks or more each leaves its sum
+// (slot 0 for the row that comes in, slot 1 for the one that goes on) to embed_join_kernel, which adds them up in order.
+// Bound by HBM: every gradient row read once, every table row written once.  A thread has eight
 // columns and a block whole rows (up to 4096 columns), so reads and writes are runs of several KB.
 constexpr int kEmbedMaxThreads = 512;
 constexpr int kEmbedZeroRows = 16;      // table rows looked at by one block of the zero part (half a word of `seen`)
@@ -601,14 +602,23 @@ __device__ __forceinline__ void embed_store(Out *dst, float (&x)[8], float scale
   Vec<Out>::store(dst, x);
 }
 
+// end of the run of v that starts at lo, in sorted keys
+__device__ __forceinline__ int run_end(const uint32_t *key, int lo, int hi, uint32_t v) {
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (key[mid] == v) lo = mid + 1; else hi = mid;
+  }
+  return lo;
+}
+
 template <typename In, typename Out>
 __global__ void __launch_bounds__(kEmbedMaxThreads)
 embed_sum_kernel(const In *d_out, const uint32_t *key, const int *val, int n, int chunk, int n_chunks, int vocab, int hidden,
                  float scale, int accumulate, Out *d_table, float *part, int *joins, const uint32_t *seen) {
   launch_next();
   wait_previous();
-  __shared__ uint32_t skey[kEmbedMaxChunk];
-  __shared__ int sval[kEmbedMaxChunk];
+  __shared__ uint32_t skey[2 * kEmbedMaxChunk];
+  __shared__ int sval[2 * kEmbedMaxChunk];
   const int col = (blockIdx.y * blockDim.x + threadIdx.x) * 8;
   if ((int)blockIdx.x >= n_chunks) {
     // rows without tokens: zeros
@@ -620,22 +630,32 @@ embed_sum_kernel(const In *d_out, const uint32_t *key, const int *val, int n, in
         if (!((has >> i) & 1)) Vec<Out>::store(d_table + (long long)(v0 + i) * hidden + col, zero);
     return;
   }
-  const int c = blockIdx.x, j0 = c * chunk, m = min(chunk, n - j0);
-  for (int i = threadIdx.x; i < m; i += blockDim.x) { skey[i] = key[j0 + i]; sval[i] = val[j0 + i]; }
-  const uint32_t before = j0 > 0 ? key[j0 - 1] : 0xffffffffu, after = j0 + m < n ? key[j0 + m] : 0xffffffffu;
+  const int c = blockIdx.x, j0 = c * chunk, m0 = min(chunk, n - j0), m1 = min(2 * chunk, n - j0);
+  for (int i = threadIdx.x; i < m1; i += blockDim.x) { skey[i] = key[j0 + i]; sval[i] = val[j0 + i]; }
+  const uint32_t none = 0xffffffffu, before = j0 > 0 ? key[j0 - 1] : none;
+  const uint32_t before2 = j0 > chunk ? key[j0 - chunk - 1] : none, after2 = j0 + m1 < n ? key[j0 + m1] : none;
   __syncthreads();
-  if (threadIdx.x == 0 && blockIdx.y == 0) {
-    // the chunk's last row goes on, and does not come in (a chunk full of one row that comes in is in the middle of it)
-    const uint32_t v = skey[m - 1];
-    if (v < (uint32_t)vocab && after == v && !(skey[0] == v && before == v)) {
-      if (c + kJoinShort < n_chunks && key[(c + kJoinShort) * chunk] == v) joins[1 + n_chunks - atomicAdd(joins + 1, 1)] = c;
-      else joins[2 + atomicAdd(joins, 1)] = c;
-    }
+  // the row that comes in: this chunk's, unless it started in the chunk before and ends in this one
+  const uint32_t v_in = skey[0], after = m0 < m1 ? skey[m0] : none;
+  int begin = 0, m = m0;
+  if (before == v_in && before2 != v_in && after != v_in)
+    begin = run_end(skey, 0, m0, v_in);
+  // the row that goes on: followed to its end, if it starts here and ends in the next chunk
+  const uint32_t v_out = skey[m0 - 1];
+  const bool starts_here = !(v_out == v_in && before == v_in);
+  bool goes_on = after == v_out;
+  if (goes_on && starts_here && after2 != v_out) {
+    m = run_end(skey, m0, m1, v_out);
+    goes_on = false;
+  }
+  if (threadIdx.x == 0 && blockIdx.y == 0 && goes_on && starts_here && v_out < (uint32_t)vocab) {
+    if (c + kJoinShort < n_chunks && key[(c + kJoinShort) * chunk] == v_out) joins[1 + n_chunks - atomicAdd(joins + 1, 1)] = c;
+    else joins[2 + atomicAdd(joins, 1)] = c;
   }
   if (col >= hidden) return;
   float x[8] = {};
-  bool first = true;   // still in the chunk's first row
-  for (int j = 0; j < m; j += 4) {
+  bool first = begin == 0;   // still in the row that comes in
+  for (int j = begin; j < m; j += 4) {
     float y[4][8];
 #pragma unroll
     for (int e = 0; e < 4; ++e)
@@ -648,8 +668,8 @@ embed_sum_kernel(const In *d_out, const uint32_t *key, const int *val, int n, in
         for (int i = 0; i < 8; ++i) x[i] += y[e][i];
         const bool last = j + e == m - 1;
         if (last || skey[j + e + 1] != v) {
-          const bool comes_in = first && before == v, goes_on = last && after == v;
-          if (comes_in || goes_on) {
+          const bool comes_in = first && before == v;
+          if (comes_in || (last && goes_on)) {
             float *dst = part + ((long long)(2 * c + (comes_in ? 0 : 1)) * hidden + col);
             Vec<float>::store(dst, x);
           } else {
@@ -665,8 +685,7 @@ embed_sum_kernel(const In *d_out, const uint32_t *key, const int *val, int n, in
 }
 
 // Rows that cross from one chunk into the next: slot 1 of the chunk c they start in, then slot 0 of the chunks behind it
-// whose first key is theirs, added up in order.  Most cross one border: a block takes 2048 columns of such a row, a thread
-// eight.  A long row is shared out over 32 column vectors x 8 shares of its sums.
+// whose first key is theirs, three or more, added up in order.  Of a short one a block takes 2048 columns, a thread eight.  A long row is shared out over 32 column vectors x 8 shares of its sums.
 template <typename Out>
 __global__ void __launch_bounds__(256)
 embed_join_kernel(const uint32_t *key, int chunk, int n_chunks, int hidden, float scale, int accumulate, Out *d_table, const float *part,

@@ -12,7 +12,9 @@ standard pre-norm decoder layer:
   element-wise ops);
 * loss: token-level cross-entropy on the response tokens.  The first token of every response is scored from the
   LAST PROMPT hidden state of its group, and that loss flows back through the prompt's own graph (Sec. 3.2, response
-  replay): that state therefore carries one target per branch.
+  replay): that state therefore carries one target per branch;
+* the vocabulary ends: given a `binding.LM` handle, `tree_embed` looks up prompts and responses in one call and
+  `tree_lm_loss` never holds the logits (16384 response tokens over 152064 words would be 15 GB of them in bf16 and fp32).
 
 Nothing here is on the measured hot path; tests compare loss and weight gradients with the flattened execution.
 """
@@ -22,7 +24,7 @@ import torch
 import torch.nn.functional as F
 
 from . import binding as B
-from .autograd import tree_attention
+from .autograd import embed, lm_loss, tree_attention
 
 BF16 = torch.bfloat16
 
@@ -105,10 +107,21 @@ class TreeDecoderLayer(torch.nn.Module):
         return self.after_attention(x_p, o_p), self.after_attention(x_r, o_r)
 
 
-def tree_lm_loss(plan: B.Plan, h_p, h_r, lm_head, resp_tokens, seam=None):
+def tree_embed(lm: B.LM, table, prompt_tokens, resp_tokens):
+    """Embeddings of the packed prompt tokens (each group's prompt once) and of the packed response tokens, fp32, for the residual
+    stream.  One lookup for both, so that the table gets one gradient pass."""
+    x = embed(lm, table, torch.cat([prompt_tokens, resp_tokens]), torch.float32)
+    return x[: prompt_tokens.shape[0]], x[prompt_tokens.shape[0]:]
+
+
+def tree_lm_loss(plan: B.Plan, h_p, h_r, lm_head, resp_tokens, seam=None, lm=None):
     """Sum of the token-level cross-entropies of all response tokens.  h_p, h_r: final hidden states of the packed prompt
-    and response tokens; lm_head [vocab, hidden]; resp_tokens [sumR] the packed response token ids."""
+    and response tokens; lm_head [vocab, hidden]; resp_tokens [sumR] the packed response token ids.  With an LM handle `lm` the
+    logits stay inside the kernels (fp32, times lm.logit_scale) and a negative id is padding; without one they are made by a
+    library GEMM and rounded to bf16."""
     from_prompt, index = seam if seam is not None else seam_index(plan, h_p.device)
     src = torch.where(from_prompt[:, None], h_p[index.clamp(max=max(h_p.shape[0] - 1, 0))], h_r[index.clamp(max=max(h_r.shape[0] - 1, 0))])
+    if lm is not None:
+        return lm_loss(lm, src.to(BF16), lm_head.to(BF16), resp_tokens).sum()
     logits = F.linear(src.to(BF16), lm_head.to(BF16)).float()
     return F.cross_entropy(logits, resp_tokens, reduction="sum")
