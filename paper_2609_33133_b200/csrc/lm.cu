@@ -56,8 +56,10 @@ int n_part(const augtree_lm *lm) { return 2 * (int)((lm->vocab + kLmTile - 1) / 
 
 // Few rows take kernels of their own (lm_few_kernel.cuh): the MMAs' N, 0 for many rows.
 int few_rows(int64_t tokens) { return tokens <= 16 ? 16 : tokens <= 32 ? 32 : tokens <= 64 ? 64 : tokens <= kLmFew ? 128 : 0; }
-// rows of the packed hidden states and of G in the scratch
-int64_t pad_rows(int64_t tokens) { return few_rows(tokens) ? 2 * few_rows(tokens) : up(tokens, 256); }
+// Rows of the call as the kernels see them, and whether G is kept in two halves (lm_tile_kernel.cuh).
+int64_t tile_rows(int64_t tokens) { return few_rows(tokens) ? few_rows(tokens) : up(tokens, kLmTile); }
+int halves(int64_t tokens) { return tokens <= kLmTile ? 2 : 1; }
+constexpr int kRowsOneLaunch = 256;  // up to here the scored rows are found and packed in one launch
 
 int64_t pad_cols(const augtree_lm *lm) { return up(lm->hidden, 64); }
 
@@ -74,9 +76,9 @@ int64_t piece_cols(const augtree_lm *lm, int64_t rows_pad) {
 // Shares of dH's contraction.  A launch holds dH's tiles (each a contraction over the piece, `kb` steps) and dW's (over the rows,
 // `kr` steps), dealt out to the CTA pairs in turn; the longest pair is waited for.  More shares even the pairs out (and let
 // few rows fill the GPU) but each costs a pass over the partial sums: the fewest within 2 % of the best.
-int dh_splits(const augtree_lm *lm, int64_t rows_pad, int64_t cols) {
+int dh_splits(const augtree_lm *lm, int64_t rows_pad, int halves, int64_t cols) {
   const int64_t pairs = std::max(lm->n_lanes / 2, 1), nt = (lm->hidden + kLmTile - 1) / kLmTile;
-  const int64_t kb = (cols + 63) / 64, kr = (rows_pad + 63) / 64;
+  const int64_t kb = halves * ((cols + 63) / 64), kr = halves * ((rows_pad + 63) / 64);
   const int64_t dh_tiles = rows_pad / kLmTile * nt, dw_tiles = (cols + kLmTile - 1) / kLmTile * nt;
   auto longest = [&](int64_t s) {
     int64_t worst = 0;
@@ -100,25 +102,25 @@ int few_splits(const augtree_lm *lm, int64_t cols) {
 }
 
 size_t loss_layout(const augtree_lm *lm, int64_t tokens, bool bwd, uint8_t *base, LossWs *w) {
-  const int64_t few = few_rows(tokens), rp = pad_rows(tokens);
+  const int64_t few = few_rows(tokens), rp = tile_rows(tokens), gr = rp * halves(tokens);
   Cursor c{base};
   w->rows.n_rows = c.take<int>(1);
   w->rows.idx = c.take<int>(rp);
-  w->rows.pos = c.take<int>(rp);
+  w->rows.pos = c.take<int>(std::max(rp, tokens));
   w->rows.target = c.take<int>(rp);
-  w->h = c.take<__nv_bfloat16>(rp * pad_cols(lm));
+  w->h = c.take<__nv_bfloat16>((bwd ? gr : rp) * pad_cols(lm));
   if (!bwd) {
     w->rows.lse2 = w->rows.gscale = nullptr;
     w->rows.x_target = c.take<float>(rp);
     w->tlogit = c.take<float>(rp);
     w->part = c.take<float2>(few ? 4ll * lm->n_lanes * few : (int64_t)n_part(lm) * rp);
   } else {
-    const int64_t cols = piece_cols(lm, rp);
+    const int64_t cols = piece_cols(lm, gr);
     w->rows.x_target = nullptr;
     w->rows.lse2 = c.take<float>(rp);
     w->rows.gscale = c.take<float>(rp);
-    w->grad = c.take<__nv_bfloat16>(rp * cols);
-    w->dh_part = c.take<float>((few ? few_splits(lm, cols) * few : dh_splits(lm, rp, cols) * rp) * lm->hidden);
+    w->grad = c.take<__nv_bfloat16>(gr * cols);
+    w->dh_part = c.take<float>((few ? few_splits(lm, cols) : dh_splits(lm, rp, halves(tokens), cols)) * rp * lm->hidden);
   }
   return c.off;
 }
@@ -228,12 +230,17 @@ int compact(const augtree_lm *lm, const void *targets, int id_bytes, int64_t tok
   const auto *src = static_cast<const uint4 *>(hidden), *wt = static_cast<const uint4 *>(weight);
   auto *dst = reinterpret_cast<uint4 *>(w.h);
   const int n = (int)tokens, row_vecs = lm->hidden / 8, out_vecs = (int)pad_cols(lm) / 8;
-  if (const int few = few_rows(tokens)) {
-    if (id_bytes == 8)
-      return launch(lm_few_rows_kernel<long long>, few, 128, 0, st, ids64, n, lm->vocab, w.rows, lse, d_loss, lm->logit_scale, loss_out, lse_out,
-                    lm->d_status, src, dst, row_vecs, out_vecs, lse != nullptr, wt);
-    return launch(lm_few_rows_kernel<int>, few, 128, 0, st, ids32, n, lm->vocab, w.rows, lse, d_loss, lm->logit_scale, loss_out, lse_out,
-                  lm->d_status, src, dst, row_vecs, out_vecs, lse != nullptr, wt);
+  if (tokens <= kRowsOneLaunch) {
+    const int twice = lse && halves(tokens) == 2;
+    const unsigned rows = (unsigned)tile_rows(tokens);
+    auto run = [&](auto kernel, int threads, auto *ids) {
+      return launch(kernel, rows, threads, 0, st, ids, n, lm->vocab, w.rows, lse, d_loss, lm->logit_scale, loss_out, lse_out, lm->d_status, src,
+                    dst, row_vecs, out_vecs, twice, wt);
+    };
+    if (few_rows(tokens))
+      return id_bytes == 8 ? run(lm_rows_kernel<long long, kLmFew>, kLmFew, ids64) : run(lm_rows_kernel<int, kLmFew>, kLmFew, ids32);
+    return id_bytes == 8 ? run(lm_rows_kernel<long long, kRowsOneLaunch>, kRowsOneLaunch, ids64)
+                         : run(lm_rows_kernel<int, kRowsOneLaunch>, kRowsOneLaunch, ids32);
   }
   const int r = id_bytes == 8 ? launch(lm_compact_kernel<long long>, 1, 1024, 0, st, ids64, n, lm->vocab, w.rows, lse, d_loss, lm->logit_scale,
                                        loss_out, lse_out, lm->d_status)
@@ -249,6 +256,7 @@ LmParams base_params(const augtree_lm *lm, const LossWs &w, int64_t rows_pad) {
   p.n_rows = w.rows.n_rows;
   p.vocab = lm->vocab; p.hidden = lm->hidden;
   p.rows_pad = rows_pad;
+  p.halves = 1;
   p.scale_log2 = lm->logit_scale * 1.4426950408889634f;
   p.target = w.rows.target; p.lse2 = w.rows.lse2; p.gscale = w.rows.gscale;
   p.status = lm->d_status;
@@ -485,7 +493,7 @@ int augtree_lm_loss_fwd(const augtree_lm_t *lm, const void *hidden, const void *
   LossWs w;
   if (!ws || !aligned16(ws) || ws_bytes < loss_layout(lm, n_tokens, false, static_cast<uint8_t *>(ws), &w)) return AUGTREE_ERR_WORKSPACE;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const int64_t rp = pad_rows(n_tokens);
+  const int64_t rp = tile_rows(n_tokens);
   const int few = few_rows(n_tokens);
   if ((r = compact(lm, targets, id_bytes, n_tokens, hidden, weight, w, nullptr, nullptr, loss, lse, st))) return r;
   Maps m = {};
@@ -526,20 +534,21 @@ int augtree_lm_loss_bwd(const augtree_lm_t *lm, const void *hidden, const void *
   LossWs w;
   if (!ws || !aligned16(ws) || ws_bytes < loss_layout(lm, n_tokens, true, static_cast<uint8_t *>(ws), &w)) return AUGTREE_ERR_WORKSPACE;
   if (!d_hidden && !d_weight) return AUGTREE_OK;
-  const int few = few_rows(n_tokens);
-  const int64_t rp = pad_rows(n_tokens), cols = piece_cols(lm, rp);
-  const int splits = few ? few_splits(lm, cols) : dh_splits(lm, rp, cols), chunks = lm->hidden % 64 == 0 ? 2 : 1;
+  const int few = few_rows(n_tokens), half = halves(n_tokens);
+  const int64_t rp = tile_rows(n_tokens), gr = rp * half, cols = piece_cols(lm, gr);
+  const int splits = few ? few_splits(lm, cols) : dh_splits(lm, rp, half, cols), chunks = lm->hidden % 64 == 0 ? 2 : 1;
   if ((r = compact(lm, targets, id_bytes, n_tokens, hidden, nullptr, w, lse, d_loss, nullptr, nullptr, st))) return r;
   Maps m = {};
-  if ((r = map_2d(&m.h, w.h, rp, pad_cols(lm), few ? few : 128)) || (r = map_2d(&m.w, weight, lm->vocab, lm->hidden, 128)) ||
-      (r = map_mn(&m.h_mn, w.h, rp, pad_cols(lm), 2)) || (r = map_mn(&m.w_mn, weight, lm->vocab, lm->hidden, chunks)) ||
-      (r = map_2d(&m.g, w.grad, rp, cols, few ? 2 * few : 128)) || (r = map_mn(&m.g_mn, w.grad, rp, cols, 2)))
+  if ((r = map_2d(&m.h, w.h, gr, pad_cols(lm), few ? few : 128)) || (r = map_2d(&m.w, weight, lm->vocab, lm->hidden, 128)) ||
+      (r = map_mn(&m.h_mn, w.h, gr, pad_cols(lm), 2)) || (r = map_mn(&m.w_mn, weight, lm->vocab, lm->hidden, chunks)) ||
+      (r = map_2d(&m.g, w.grad, gr, cols, few ? 2 * few : 128)) || (r = map_mn(&m.g_mn, w.grad, gr, cols, 2)))
     return r;
   LmParams p = base_params(lm, w, rp);
   p.mn_chunks = chunks;
+  p.halves = half;
   p.dw_f32 = weight_dtype == AUGTREE_F32; p.dw_add = accumulate;
   CUtensorMap out_g, out_dw;
-  if (!few && ((r = map_out(&out_g, w.grad, rp, cols, false)) || (r = map_out(&m.dh, w.dh_part, splits * rp, lm->hidden, true)))) return r;
+  if (!few && ((r = map_out(&out_g, w.grad, gr, cols, false)) || (r = map_out(&m.dh, w.dh_part, splits * rp, lm->hidden, true)))) return r;
   if (d_weight && (r = map_out(&out_dw, d_weight, lm->vocab, lm->hidden, p.dw_f32))) return r;
   FewParams f = few_params(lm, w, p);
   f.ld_grad = cols; f.splits = splits; f.mn_chunks = chunks;
@@ -549,26 +558,26 @@ int augtree_lm_loss_bwd(const augtree_lm_t *lm, const void *hidden, const void *
     p.dh_add = f.dh_add = v0 > 0;
     f.n = n;
     p.n_jobs = 0;
+    p.half_k = (int)up(n, 64);
     if (few) {
       if ((r = launch_few<LM_GRAD>(lm, few, m.w, m.h, f, st))) return r;
       if (d_hidden && (r = launch_few<LM_DH>(lm, few, m.w_mn, m.g, f, st))) return r;
-      // both halves of G: the rows of the packed hidden states are there twice
-      if (d_weight) p.job[p.n_jobs++] = {LM_DW, n, lm->hidden, (int)rp, 1};
     } else {
       p.n_jobs = 1;
       p.job[0] = {LM_GRAD, 0, n, lm->hidden, 1};
       m.out = out_g;
       if ((r = launch_tiles(lm, m, p, st))) return r;
       p.n_jobs = 0;
-      if (d_hidden) p.job[p.n_jobs++] = {LM_DH, 0, lm->hidden, n, splits};
-      if (d_weight) p.job[p.n_jobs++] = {LM_DW, n, lm->hidden, 0, 1};
+      if (d_hidden) p.job[p.n_jobs++] = {LM_DH, 0, lm->hidden, half * p.half_k, splits};
     }
+    // (with two halves of G the rows of the packed hidden states are there twice)
+    if (d_weight) p.job[p.n_jobs++] = {LM_DW, n, lm->hidden, half == 2 ? (int)gr : 0, 1};
     if (d_weight) m.out = out_dw;
     if (p.n_jobs && (r = launch_tiles(lm, m, p, st))) return r;
   }
   if (d_hidden) {
     const unsigned grid = (unsigned)std::min<int64_t>(n_tokens, 16 * lm->n_lanes);
-    return launch(lm_dh_kernel, grid, 256, 0, st, w.dh_part, splits, few ? few : rp, lm->hidden, w.rows.pos, (int)n_tokens,
+    return launch(lm_dh_kernel, grid, 256, 0, st, w.dh_part, splits, rp, lm->hidden, w.rows.pos, (int)n_tokens,
                   static_cast<__nv_bfloat16 *>(d_hidden));
   }
   return AUGTREE_OK;

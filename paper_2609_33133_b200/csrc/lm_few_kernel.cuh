@@ -134,6 +134,7 @@ lm_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ 
     fence_barrier_init();
   }
   if (warp == 5) { tmem_alloc(smem_u32((const void *)tmem_slot), 512); tmem_relinquish(); }
+  if (warp == 4 && lane == 0) { tma_prefetch_desc(&tm_w); tma_prefetch_desc(&tm_b); }
   wait_previous();
   const int n_rows = *reinterpret_cast<const volatile int *>(p.n_rows);
   if (KIND != LM_DH && threadIdx.x < N) {
@@ -155,7 +156,6 @@ lm_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ 
   if (warp == 4) {
     // ------------------------------------------------------------ TMA producer
     if (lane == 0) {
-      tma_prefetch_desc(&tm_w); tma_prefetch_desc(&tm_b);
       uint32_t T = 0;
       bool ok = true;
       for (int u = blockIdx.x; ok && u < units; u += gridDim.x) {

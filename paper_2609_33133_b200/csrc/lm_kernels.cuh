@@ -126,17 +126,17 @@ lm_gather_kernel(const uint4 *hidden, const LmRows rows, uint4 *out, int row_vec
   }
 }
 
-// Both for up to 128 tokens in one launch: a block per packed row, each finds its token for itself.  With `twice` the rows are
-// written a second time behind the first N (they multiply the two halves of G, see lm_few_kernel.cuh).
-template <typename Id>
-__global__ void __launch_bounds__(128)
-lm_few_rows_kernel(const Id *targets, int tokens, int vocab, LmRows o, const float *lse, const float *d_loss, float logit_scale,
+// Both in one launch for as many tokens as a block has threads: a block per packed row, each finds its token for itself.  With
+// `twice` the rows are written a second time behind the first ones (they multiply the two halves of G).
+template <typename Id, int THREADS>
+__global__ void __launch_bounds__(THREADS)
+lm_rows_kernel(const Id *targets, int tokens, int vocab, LmRows o, const float *lse, const float *d_loss, float logit_scale,
                    float *loss_out, float *lse_out, int *status, const uint4 *hidden, uint4 *out, int row_vecs,
                    int out_vecs, int twice, const uint4 *weight) {
   launch_next();
   wait_previous();
-  __shared__ int warp_sum[4];
-  __shared__ float sh[4];
+  __shared__ int warp_sum[THREADS / 32];
+  __shared__ float sh[THREADS / 32];
   __shared__ int from;
   const int t = threadIdx.x, lane = t & 31, warp = t >> 5, row = blockIdx.x;
   const long long id = t < tokens ? (long long)targets[t] : -1;
@@ -146,7 +146,7 @@ lm_few_rows_kernel(const Id *targets, int tokens, int vocab, LmRows o, const flo
   if (t == 0) from = -1;
   __syncthreads();
   int r = __popc(m & ((1u << lane) - 1)), n = 0;
-  for (int w = 0; w < 4; ++w) {
+  for (int w = 0; w < THREADS / 32; ++w) {
     if (w < warp) r += warp_sum[w];
     n += warp_sum[w];
   }
@@ -171,14 +171,14 @@ lm_few_rows_kernel(const Id *targets, int tokens, int vocab, LmRows o, const flo
   const uint4 *src = from >= 0 ? hidden + (long long)from * row_vecs : nullptr;
   const uint4 *wt = src && weight ? weight + (long long)targets[from] * row_vecs : nullptr;
   float s = 0.f;
-  for (int i = t; i < out_vecs; i += 128) {
+  for (int i = t; i < out_vecs; i += THREADS) {
     const uint4 v = src && i < row_vecs ? src[i] : make_uint4(0, 0, 0, 0);
     if (wt && i < row_vecs) s += dot8(v, wt[i]);
     out[(long long)row * out_vecs + i] = v;
     if (twice) out[(long long)(gridDim.x + row) * out_vecs + i] = v;
   }
   if (wt) {
-    s = block_sum<128>(s, sh);
+    s = block_sum<THREADS>(s, sh);
     if (t == 0) o.x_target[row] = s;
   }
 }

@@ -10,7 +10,9 @@
 // which operand has its contraction index contiguous in memory (the tensor core takes either order) and in the epilogue.
 // G is rounded to bf16 because the two products that use it take bf16 operands: an error of at most half a step,
 // 2^-8 of each element, independent between elements, so its sums stay as exact as the bf16 results they are
-// delivered in; the sums themselves, the softmax statistics and the exponent are fp32.
+// delivered in; the sums themselves, the softmax statistics and the exponent are fp32.  With up to 256 rows single elements (the
+// targets') dominate a result and their roundings with it; then G is kept in two halves, hi = bf16(G) and lo = bf16(G - hi),
+// and the contractions of dH and dW run over both, which few rows can afford: W and dW pass through memory just the same.
 //
 // A tile belongs to a pair of CTAs (cluster of two, tcgen05.mma.cta_group::2): each loads 128 rows of A and 128 columns of
 // B and gets 128 rows of the result, so 64 KB cross from L2 for every 64 steps of contraction of a 256 x 256 tile; single
@@ -60,6 +62,8 @@ struct LmParams {
   const float *gscale;      // [rows_pad] a_t c; 0 behind the last row
   float2 *part;             // STATS: [2 x vocabulary tiles][rows_pad] (m, l)
   float *tlogit;            // STATS: [rows_pad] x at the target
+  int halves;               // 2: G is hi in rows 0 .. rows_pad, lo in the rows behind them; 1: hi alone
+  int half_k;               // DH: contraction steps x 64 of one half
   int dh_add;               // DH: add to what an earlier piece left in the partial sums
   int dw_f32, dw_add;       // DW: type of dW, add to what is there
   int *status;
@@ -177,6 +181,15 @@ lm_tile_kernel(const __grid_constant__ CUtensorMap tm_h, const __grid_constant__
     fence_barrier_init();
   }
   if (warp == 9) { tmem_alloc_pair(smem_u32((const void *)tmem_slot), 512); tmem_relinquish_pair(); }
+  if (warp == 8 && lane == 0) {
+    for (int j = 0; j < p.n_jobs; ++j) {
+      const int kind = p.job[j].kind;
+      if (kind <= LM_GRAD) { tma_prefetch_desc(&tm_h); tma_prefetch_desc(&tm_w); }
+      if (kind == LM_DH) { tma_prefetch_desc(&tm_g); tma_prefetch_desc(&tm_w_mn); tma_prefetch_desc(&tm_dh); }
+      if (kind == LM_DW) { tma_prefetch_desc(&tm_g_mn); tma_prefetch_desc(&tm_h_mn); }
+      if (kind == LM_GRAD || kind == LM_DW) tma_prefetch_desc(&tm_out);
+    }
+  }
   tc_fence_before();
   __syncthreads();
   cluster_sync();
@@ -213,9 +226,11 @@ lm_tile_kernel(const __grid_constant__ CUtensorMap tm_h, const __grid_constant__
               tma_load_2d_pair(sA, &tm_h, bar, k0, m0);
               tma_load_2d_pair(sB, &tm_w, bar, k0, w0);
             } else if constexpr (kKind == LM_DH) {
-              tma_load_2d_pair(sA, &tm_g, bar, k0, m0);
-              if (one_box) tma_load_3d_pair(sB, &tm_w_mn, bar, 0, p.v0 + k0, nc);
-              else for (int b = 0; b < 2; ++b) tma_load_3d_pair(sB + b * 8192, &tm_w_mn, bar, n0 + b * 64, p.v0 + k0, 0);
+              const bool lo = k0 >= p.half_k;
+              const int kc = lo ? k0 - p.half_k : k0, vr = p.v0 + kc;
+              tma_load_2d_pair(sA, &tm_g, bar, kc, lo ? m0 + (int)p.rows_pad : m0);
+              if (one_box) tma_load_3d_pair(sB, &tm_w_mn, bar, 0, vr, nc);
+              else for (int b = 0; b < 2; ++b) tma_load_3d_pair(sB + b * 8192, &tm_w_mn, bar, n0 + b * 64, vr, 0);
             } else {
               tma_load_3d_pair(sA, &tm_g_mn, bar, 0, k0, mc);
               tma_load_3d_pair(sB, &tm_h_mn, bar, 0, k0, nc);
@@ -314,7 +329,8 @@ lm_tile_kernel(const __grid_constant__ CUtensorMap tm_h, const __grid_constant__
         const bool live = row < n_rows;
         const int tgt = live ? p.target[row] - p.v0 - n0 : -1;
         const float lse2 = live ? p.lse2[row] : 0.f, gs = live ? p.gscale[row] : 0.f;
-        for (int q = 0; q < 4; ++q) {
+        for (int i = 0; i < 4 * p.halves; ++i) {
+          const int q = i & 3;
           uint32_t v[32];
           tmem_ld32(tD + q * 32, v);
           tc_wait_ld();
@@ -324,13 +340,14 @@ lm_tile_kernel(const __grid_constant__ CUtensorMap tm_h, const __grid_constant__
           for (int e = 0; e < 32; ++e) {
             const float pr = ex2(fmaf(__uint_as_float(v[e]), p.scale_log2, -lse2)) - (tgt - q * 32 == e ? 1.f : 0.f);
             g[e] = live && e < left ? pr * gs : 0.f;
+            if (i >= 4) g[e] -= __bfloat162float(__float2bfloat16_rn(g[e]));
           }
           if (!(q & 1)) { if (lane == 0) bulk_wait_read(); __syncwarp(); }
           stage_bf16(s_out, lane, (q & 1) * 4, g);
           if (q & 1) {
             fence_async_shared();
             __syncwarp();
-            if (lane == 0) { tma_store_2d(&tm_out, s_out, n0 + (q - 1) * 32, row0); bulk_commit(); }
+            if (lane == 0) { tma_store_2d(&tm_out, s_out, n0 + (q - 1) * 32, i < 4 ? row0 : row0 + (int)p.rows_pad); bulk_commit(); }
           }
         }
       } else {
