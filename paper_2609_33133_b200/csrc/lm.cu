@@ -95,6 +95,13 @@ int dh_splits(const augtree_lm *lm, int64_t rows_pad, int halves, int64_t cols) 
   return (int)pick;
 }
 
+// Row tiles of a group (LmTile): hidden states of at most 32 MB, a quarter of L2, in equal groups.
+int row_group(const augtree_lm *lm, int64_t rows) {
+  const int64_t tiles = rows / kLmTile, most = std::max<int64_t>(((int64_t)32 << 20) / (kLmTile * pad_cols(lm) * 2), 1);
+  const int64_t groups = (tiles + most - 1) / most;
+  return (int)((tiles + groups - 1) / groups);
+}
+
 // Few rows: shares of the vocabulary that fill the CTAs in one go.
 int few_splits(const augtree_lm *lm, int64_t cols) {
   const int64_t tiles = (lm->hidden + 127) / 128;
@@ -507,7 +514,7 @@ int augtree_lm_loss_fwd(const augtree_lm_t *lm, const void *hidden, const void *
   if ((r = map_2d(&m.h, w.h, rp, pad_cols(lm), 128)) || (r = map_2d(&m.w, weight, lm->vocab, lm->hidden, 128))) return r;
   LmParams p = base_params(lm, w, rp);
   p.n_jobs = 1;
-  p.job[0] = {LM_STATS, 0, lm->vocab, lm->hidden, 1};
+  p.job[0] = {LM_STATS, 0, lm->vocab, lm->hidden, 1, row_group(lm, rp)};
   p.part = w.part; p.tlogit = w.tlogit;
   if ((r = launch_tiles(lm, m, p, st))) return r;
   const unsigned grid = (unsigned)std::min<int64_t>((n_tokens + 31) / 32, 2 * lm->n_lanes);
@@ -564,14 +571,14 @@ int augtree_lm_loss_bwd(const augtree_lm_t *lm, const void *hidden, const void *
       if (d_hidden && (r = launch_few<LM_DH>(lm, few, m.w_mn, m.g, f, st))) return r;
     } else {
       p.n_jobs = 1;
-      p.job[0] = {LM_GRAD, 0, n, lm->hidden, 1};
+      p.job[0] = {LM_GRAD, 0, n, lm->hidden, 1, row_group(lm, rp)};
       m.out = out_g;
       if ((r = launch_tiles(lm, m, p, st))) return r;
       p.n_jobs = 0;
-      if (d_hidden) p.job[p.n_jobs++] = {LM_DH, 0, lm->hidden, half * p.half_k, splits};
+      if (d_hidden) p.job[p.n_jobs++] = {LM_DH, 0, lm->hidden, half * p.half_k, splits, 0};
     }
     // (with two halves of G the rows of the packed hidden states are there twice)
-    if (d_weight) p.job[p.n_jobs++] = {LM_DW, n, lm->hidden, half == 2 ? (int)gr : 0, 1};
+    if (d_weight) p.job[p.n_jobs++] = {LM_DW, n, lm->hidden, half == 2 ? (int)gr : 0, 1, 0};
     if (d_weight) m.out = out_dw;
     if (p.n_jobs && (r = launch_tiles(lm, m, p, st))) return r;
   }

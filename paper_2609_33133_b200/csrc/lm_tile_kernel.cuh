@@ -47,6 +47,7 @@ struct LmJob {
   int n;           // columns: vocabulary columns of the piece (STATS, GRAD) or hidden (DH, DW)
   int k_fixed;     // contraction length; 0 = the token rows (DW)
   int splits;      // shares of the contraction (DH), 1 otherwise
+  int group;       // STATS, GRAD: row tiles that are taken over all columns before the next ones
 };
 
 struct LmParams {
@@ -80,37 +81,51 @@ struct LmSmem {
   static constexpr int kBytes = kOffBar + 256;
 };
 
-// Walks the tiles of one CTA pair: tile t0, t0 + step, .. of all jobs in a row.  The index that runs fastest is the one whose
-// operand is the smaller: the tiles in flight then share the large operand's rows while the small one stays in L2.  From tile to
-// tile the coordinates move on by additions alone; divisions are left to the start of a job (with them in every step each
-// role spent 2400 cycles a tile on finding it, more than a tile of 64 rows takes).
+// Walks the tiles of one CTA pair: tile t0, t0 + step, .. of all jobs in a row.
+//   STATS, GRAD  row tiles run fastest, within a group whose hidden states stay in L2 while W streams past, once a group.  (With
+//                all rows of 16384 x 3584 in one group, 117 MB, they come from HBM again for every column of tiles.)
+//   DH, DW       hidden columns run fastest: a row of tiles shares its G, which then passes once
+// From tile to tile the coordinates move on by additions; divisions are left to the start of a job or group (with them in every
+// step each role spent 2400 cycles a tile on finding it, more than a tile of 64 rows takes).
 struct LmTile {
   int kind, m, n, split, kb0, nkb;   // product, tile coordinates, share of the contraction: first step, steps
   int cols, m_fixed;                 // of the job
-  int t, job, first, count, step, mt, nt, kb, per, d_fast, d_slow;
+  int t, job, first, end, step;      // tile number, its job, the numbers of the job's or group's tiles
+  int m0, rows, mt, nt, kb, per, d_fast, d_slow;
 
   __device__ __forceinline__ bool start(const LmParams &p, int n_rows, int t0, int tile_step) {
     t = t0; step = tile_step; job = 0; first = 0;
     return enter(p, n_rows);
   }
-  // the job that holds tile t, from `job` on
+  // the job and group that hold tile t; `first` is the first tile of `job`
   __device__ __forceinline__ bool enter(const LmParams &p, int n_rows) {
-    for (; job < p.n_jobs; ++job, first += count) {
+    for (; job < p.n_jobs; ++job) {
       const LmJob J = job == 0 ? p.job[0] : p.job[1];
       kind = J.kind; cols = J.n; m_fixed = J.m_fixed;
       mt = ((J.m_fixed ? J.m_fixed : n_rows) + kLmTile - 1) / kLmTile;
       nt = (J.n + kLmTile - 1) / kLmTile;
       kb = ((J.k_fixed ? J.k_fixed : n_rows) + 63) / 64;
-      count = mt * nt * J.splits;
+      const int count = mt * nt * J.splits;
       if (t < first + count) {
-        const int r = t - first, fast = kind <= LM_GRAD ? mt : nt;
+        int r = t - first;
         per = (kb + J.splits - 1) / J.splits;
-        d_fast = step % fast; d_slow = step / fast;
-        if (kind <= LM_GRAD) { m = r % mt; n = r / mt; split = 0; }
-        else { n = r % nt; m = r / nt; split = m / mt; m -= split * mt; }
+        if (kind <= LM_GRAD) {
+          const int g = r / (J.group * nt);
+          m0 = g * J.group;
+          rows = min(J.group, mt - m0);
+          r -= m0 * nt;
+          m = m0 + r % rows; n = r / rows; split = 0;
+          end = first + (m0 + rows) * nt;
+        } else {
+          m0 = 0; rows = nt;
+          n = r % nt; m = r / nt; split = m / mt; m -= split * mt;
+          end = first + count;
+        }
+        d_fast = step % rows; d_slow = step / rows;
         range();
         return true;
       }
+      first += count;
     }
     return false;
   }
@@ -120,10 +135,10 @@ struct LmTile {
   }
   __device__ __forceinline__ bool next(const LmParams &p, int n_rows) {
     t += step;
-    if (t >= first + count) { first += count; ++job; return enter(p, n_rows); }
+    if (t >= end) return enter(p, n_rows);
     if (kind <= LM_GRAD) {
       m += d_fast; n += d_slow;
-      if (m >= mt) { m -= mt; ++n; }
+      if (m >= m0 + rows) { m -= rows; ++n; }
     } else {
       n += d_fast; m += d_slow;
       if (n >= nt) { n -= nt; ++m; }
