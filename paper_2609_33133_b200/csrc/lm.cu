@@ -55,7 +55,7 @@ struct LossWs {
 int n_part(const augtree_lm *lm) { return 2 * (int)((lm->vocab + kLmTile - 1) / kLmTile); }
 
 // Few rows take kernels of their own (lm_few_kernel.cuh): the MMAs' N, 0 for many rows.
-int few_rows(int64_t tokens) { return tokens <= 16 ? 16 : tokens <= 32 ? 32 : tokens <= 64 ? 64 : tokens <= kLmFew ? 128 : 0; }
+int few_rows(int64_t tokens) { return tokens <= kLmFew ? (int)up(std::max<int64_t>(tokens, 1), 16) : 0; }
 // Rows of the call as the kernels see them, and whether G is kept in two halves (lm_tile_kernel.cuh).
 int64_t tile_rows(int64_t tokens) { return few_rows(tokens) ? few_rows(tokens) : up(tokens, kLmTile); }
 int halves(int64_t tokens) { return tokens <= kLmTile ? 2 : 1; }
@@ -104,7 +104,7 @@ int row_group(const augtree_lm *lm, int64_t rows) {
 
 // Few rows: shares of the vocabulary that fill the CTAs in one go.
 int few_splits(const augtree_lm *lm, int64_t cols) {
-  const int64_t tiles = (lm->hidden + 127) / 128;
+  const int64_t tiles = (lm->hidden + 255) / 256;
   return (int)std::min<int64_t>(std::max<int64_t>(lm->n_lanes / tiles, 1), (cols + 63) / 64);
 }
 
@@ -283,23 +283,35 @@ template <int KIND, int N>
 int launch_few_n(const augtree_lm *lm, const CUtensorMap &mw, const CUtensorMap &mb, const FewParams &p, cudaStream_t st) {
   return launch(lm_few_kernel<KIND, N>, lm->n_lanes, kFewThreads, FewSmem<KIND, N>::kBytes, st, mw, mb, p);
 }
-template <int KIND>
-int launch_few(const augtree_lm *lm, int few, const CUtensorMap &mw, const CUtensorMap &mb, const FewParams &p, cudaStream_t st) {
+// calls f with the row count as a compile-time constant
+template <class F>
+int with_few(int few, F f) {
   switch (few) {
-    case 16: return launch_few_n<KIND, 16>(lm, mw, mb, p, st);
-    case 32: return launch_few_n<KIND, 32>(lm, mw, mb, p, st);
-    case 64: return launch_few_n<KIND, 64>(lm, mw, mb, p, st);
-    default: return launch_few_n<KIND, 128>(lm, mw, mb, p, st);
+    case 16: return f(std::integral_constant<int, 16>{});
+    case 32: return f(std::integral_constant<int, 32>{});
+    case 48: return f(std::integral_constant<int, 48>{});
+    case 64: return f(std::integral_constant<int, 64>{});
+    case 80: return f(std::integral_constant<int, 80>{});
+    case 96: return f(std::integral_constant<int, 96>{});
+    case 112: return f(std::integral_constant<int, 112>{});
+    default: return f(std::integral_constant<int, 128>{});
   }
 }
 template <int KIND>
+int launch_few(const augtree_lm *lm, int few, const CUtensorMap &mw, const CUtensorMap &mb, const FewParams &p, cudaStream_t st) {
+  return with_few(few, [&](auto n) { return launch_few_n<KIND, decltype(n)::value>(lm, mw, mb, p, st); });
+}
+template <int KIND>
 int few_attributes() {
-  const cudaFuncAttribute a = cudaFuncAttributeMaxDynamicSharedMemorySize;
-  return cudaFuncSetAttribute(lm_few_kernel<KIND, 16>, a, FewSmem<KIND, 16>::kBytes) == cudaSuccess &&
-                 cudaFuncSetAttribute(lm_few_kernel<KIND, 32>, a, FewSmem<KIND, 32>::kBytes) == cudaSuccess &&
-                 cudaFuncSetAttribute(lm_few_kernel<KIND, 64>, a, FewSmem<KIND, 64>::kBytes) == cudaSuccess &&
-                 cudaFuncSetAttribute(lm_few_kernel<KIND, 128>, a, FewSmem<KIND, 128>::kBytes) == cudaSuccess
-             ? AUGTREE_OK : AUGTREE_ERR_CUDA;
+  for (int few = 16; few <= kLmFew; few += 16) {
+    const int r = with_few(few, [](auto n) {
+      constexpr int N = decltype(n)::value;
+      return cudaFuncSetAttribute(lm_few_kernel<KIND, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewSmem<KIND, N>::kBytes) == cudaSuccess
+                 ? AUGTREE_OK : AUGTREE_ERR_CUDA;
+    });
+    if (r) return r;
+  }
+  return AUGTREE_OK;
 }
 
 FewParams few_params(const augtree_lm *lm, const LossWs &w, const LmParams &b) {

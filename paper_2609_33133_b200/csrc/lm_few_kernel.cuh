@@ -1,6 +1,8 @@
 // The products of the vocabulary loss for few rows (up to 128): the work is reading W once, so the roles of the operands
-// are turned round.  W's rows (or, for dH, its columns) fill the tensor core's M = 128 and the tokens its N = 16 .. 128, so the
-// MMAs cost what the tokens need and a persistent CTA per SM streams its share of W through a deep ring of stages.
+// are turned round.  W's rows (or, for dH, its columns) fill the tensor core's M = 128 and the tokens its N, the next multiple of 16:
+// the MMAs and the loads of H or G cost what the tokens need, and a persistent CTA per SM streams its share of W through a ring of
+// as many stages as fit.  (N = 128 for 77 rows left 6 stages, 96 KB of W in flight an SM, and 220 us where 180 is the
+// memory's; HBM's latency at its full rate wants more.)
 //
 //   STATS  x^T = W H^T, a tile of 128 vocabulary rows; a TMEM lane is a vocabulary row, a column a token.  Maxima and sums over
 //          the vocabulary run across the lanes (halving exchanges: 31 shuffles leave lane j with column j's) and stay in
@@ -9,7 +11,7 @@
 //          towards zero, in proportion to the length of the chain.
 //   GRAD   G, rounded to bf16 twice: G = hi + lo, lo = bf16(G - hi), so that the few rows' gradients, in which single elements of
 //          G dominate, carry no rounding of G (2^-17 is left).  hi is row t of the scratch, lo row N + t.
-//   DH     dH^T = W^T G^T, 128 hidden columns x [hi | lo] of the tokens, a share of the vocabulary each
+//   DH     dH^T = W^T G^T, 256 hidden columns (two MMAs that share G's load) x [hi | lo] of the tokens, a share of the vocabulary each
 // Bound by HBM: W is read once by each of the three.  (Tokens on M, with 256-row tiles of CTA pairs, took 189 / 204 us for STATS
 // and GRAD of one row under 152064 x 3584, but 38 us more for the 1188 partial sums a row that they leave, and 1000 us for dH and dW of 77.)
 //
@@ -47,14 +49,15 @@ struct FewParams {
 
 template <int KIND, int N>
 struct FewSmem {
+  static constexpr int kSub = KIND == LM_DH ? 2 : 1;          // tiles of 128 rows of A that share a load of B
   static constexpr int kBRows = KIND == LM_DH ? 2 * N : N;
-  static constexpr int kABytes = 128 * 128, kBBytes = kBRows * 128;
+  static constexpr int kABytes = kSub * 128 * 128, kBBytes = kBRows * 128;
   static constexpr int kStageBytes = kABytes + kBBytes;
-  static constexpr int kStages = (208 * 1024) / kStageBytes;  // 6 (DH, N = 128) .. 11
+  static constexpr int kStages = (220 * 1024) / kStageBytes;  // 3 (DH, N = 128) .. 12
   static constexpr int kOffRows = kStages * kStageBytes;      // target, lse2, gscale
   static constexpr int kOffBar = kOffRows + 3 * kLmFew * 4;
   static constexpr int kBytes = kOffBar + 256;
-  static_assert(kStages <= 12 && kBytes <= 227 * 1024, "stage ring");
+  static_assert(kStages >= 3 && kStages <= 12 && kBytes <= 227 * 1024, "stage ring");
 };
 
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const void *tmap, uint32_t bar, int c0, int c1) {
@@ -89,12 +92,12 @@ __device__ __forceinline__ void tmem_ld_cols(uint32_t taddr, uint32_t (&r)[W]) {
 // Units of the kernel: vocabulary tiles (STATS, GRAD), or (share, hidden tile) pairs (DH).
 template <int KIND>
 __device__ __forceinline__ int few_units(const FewParams &p) {
-  return KIND == LM_DH ? (p.hidden + 127) / 128 * p.splits : (p.n + 127) / 128;
+  return KIND == LM_DH ? (p.hidden + 255) / 256 * p.splits : (p.n + 127) / 128;
 }
 template <int KIND>
 __device__ __forceinline__ void few_unit(const FewParams &p, int u, int &tile, int &split, int &kb0, int &nkb) {
   if (KIND != LM_DH) { tile = u; split = 0; kb0 = 0; nkb = (p.hidden + 63) / 64; return; }
-  const int tiles = (p.hidden + 127) / 128, kb = (p.n + 63) / 64;
+  const int tiles = (p.hidden + 255) / 256, kb = (p.n + 63) / 64;
   split = u / tiles;
   tile = u % tiles;
   kb0 = (int)((long long)kb * split / p.splits);
@@ -109,8 +112,9 @@ __global__ void __launch_bounds__(kFewThreads, 1)
 lm_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_b, const FewParams p) {
   using SM = FewSmem<KIND, N>;
   constexpr int NST = SM::kStages;
-  constexpr int W = N < 32 ? 16 : 32, NG = N / W;   // columns of a group, groups
-  constexpr int NACC = KIND == LM_STATS ? (N <= 64 ? 4 : 2) : 1;  // accumulators of a tile, each N (DH: 2 N) columns
+  constexpr int W = N % 32 ? 16 : 32, NG = N / W;   // columns of a group, groups
+  constexpr int NACC = KIND == LM_STATS ? (N <= 64 ? 4 : 256 / N) : 1;  // accumulators of a tile, N columns each
+  constexpr int NSUB = SM::kSub, NBUF = KIND == LM_DH ? 1 : 2;  // DH: two tiles of 2 N columns, a unit or two a CTA
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   const uint32_t base = smem_u32(smem_raw);
   launch_next();
@@ -168,9 +172,9 @@ lm_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ 
           if ((p.test_flags & TEST_SKIP_FWD_LOAD) && blockIdx.x == 0 && T == 0) continue;
           mbar_expect_tx(bar, SM::kStageBytes);
           if (KIND == LM_DH) {
-            const int k0 = tile * 128, vr = p.v0 + kb * 64;
-            if (p.mn_chunks == 2) tma_load_3d(sA, &tm_w, bar, 0, vr, k0 >> 6);
-            else for (int b = 0; b < 2; ++b) tma_load_3d(sA + b * 8192, &tm_w, bar, k0 + b * 64, vr, 0);
+            const int k0 = tile * 256, vr = p.v0 + kb * 64;
+            if (p.mn_chunks == 2) for (int b = 0; b < 2; ++b) tma_load_3d(sA + b * 16384, &tm_w, bar, 0, vr, (k0 >> 6) + 2 * b);
+            else for (int b = 0; b < 4; ++b) tma_load_3d(sA + b * 8192, &tm_w, bar, k0 + b * 64, vr, 0);
           } else {
             tma_load_2d(sA, &tm_w, bar, kb * 64, p.v0 + tile * 128);
           }
@@ -188,9 +192,9 @@ lm_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ 
     bool ok = true;
     for (int u = blockIdx.x; ok && u < units; u += gridDim.x, ++ic) {
       few_unit<KIND>(p, u, tile, split, kb0, nkb);
-      const uint32_t buf = ic & 1;
-      if (ic >= 2) {
-        ok = mbar_wait(bar_acc_empty + 8 * buf, ((ic >> 1) - 1) & 1, ab, WAIT_FEW_ACC_EMPTY);
+      const uint32_t buf = ic % NBUF;
+      if (ic >= NBUF) {
+        ok = mbar_wait(bar_acc_empty + 8 * buf, (ic / NBUF - 1) & 1, ab, WAIT_FEW_ACC_EMPTY);
         if (!ok) break;
         tc_fence_after();
       }
@@ -206,7 +210,10 @@ lm_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ 
         const uint32_t tD = tmem + buf * 256 + part * N;
         if (elected) {
 #pragma unroll
-          for (int k = 0; k < 4; ++k) mma_ss2(tD, a_lo + k * kAStep, b_lo + k * 2, kIdesc, (uint32_t)(!fresh || k > 0));
+          for (int s = 0; s < NSUB; ++s)
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              mma_ss2(tD + s * 256, a_lo + s * (16384 >> 4) + k * kAStep, b_lo + k * 2, kIdesc, (uint32_t)(!fresh || k > 0));
           tc_commit(bar_empty + 8 * st);
         }
       }
@@ -223,11 +230,11 @@ lm_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ 
     for (int g = 0; g < NG; ++g) { m[g] = -INFINITY; l[g] = 0.f; }
     for (int u = blockIdx.x; ok && u < units; u += gridDim.x, ++ic) {
       few_unit<KIND>(p, u, tile, split, kb0, nkb);
-      const uint32_t buf = ic & 1, tD = tmem + buf * 256 + lane_off;
-      ok = mbar_wait(bar_acc_full + 8 * buf, (ic >> 1) & 1, ab, WAIT_FEW_ACC_FULL);
+      const uint32_t buf = ic % NBUF, tD = tmem + buf * 256 + lane_off;
+      ok = mbar_wait(bar_acc_full + 8 * buf, (ic / NBUF) & 1, ab, WAIT_FEW_ACC_FULL);
       if (!ok) break;
       tc_fence_after();
-      const int r = tile * 128 + warp * 32 + lane;   // vocabulary row of the piece, or hidden column
+      const int r = tile * (128 * NSUB) + warp * 32 + lane;   // vocabulary row of the piece, or (first) hidden column
       if (KIND == LM_STATS) {
         const int v = p.v0 + r;
         const bool exists = r < p.n;
@@ -278,20 +285,24 @@ lm_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ 
           }
         }
       } else {
-        float *dst = p.dh_part + (long long)split * N * p.hidden + r;
 #pragma unroll
-        for (int g = 0; g < N / 16; ++g) {
-          uint32_t hi[16], lo[16];
-          tmem_ld16(tD + g * 16, hi);
-          tmem_ld16(tD + N + g * 16, lo);
-          tc_wait_ld();
+        for (int s = 0; s < NSUB; ++s) {
+          const int col = r + s * 128;
+          float *dst = p.dh_part + (long long)split * N * p.hidden + col;
 #pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            const int t = g * 16 + j;
-            if (t < n_rows && r < p.hidden) {
-              float x = nkb ? __uint_as_float(hi[j]) + __uint_as_float(lo[j]) : 0.f;
-              if (p.dh_add) x += dst[(long long)t * p.hidden];
-              dst[(long long)t * p.hidden] = x;
+          for (int g = 0; g < N / 16; ++g) {
+            uint32_t hi[16], lo[16];
+            tmem_ld16(tD + s * 256 + g * 16, hi);
+            tmem_ld16(tD + s * 256 + N + g * 16, lo);
+            tc_wait_ld();
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+              const int t = g * 16 + j;
+              if (t < n_rows && col < p.hidden) {
+                float x = nkb ? __uint_as_float(hi[j]) + __uint_as_float(lo[j]) : 0.f;
+                if (p.dh_add) x += dst[(long long)t * p.hidden];
+                dst[(long long)t * p.hidden] = x;
+              }
             }
           }
         }

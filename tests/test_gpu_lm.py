@@ -63,14 +63,23 @@ LOSS_CASES = [
     (1, 503, 256, 0.0, 1.0, 0),
     (2, 129, 72, 0.0, 0.7, 0),
     (17, 257, 64, 0.2, 1.0, 0),
+    (33, 700, 320, 0.0, 1.0, 0),
     (64, 1000, 128, 0.0, 1.0, 0),
+    (77, 3001, 1000, 0.1, 1.0, 0),
+    (90, 300, 4104, 0.0, 1.0, 1),           # two pieces of 256 columns, seventeen tiles of hidden columns
+    (100, 40000, 64, 0.0, 1.0, 0),          # more tiles than SMs
+    (128, 2000, 192, 0.3, 1.0, 0),
     (65, 255, 120, 0.0, 1.0, 0),
     (127, 513, 264, 0.1, 1.3, 0),
     (129, 503, 256, 0.1, 1.0, 0),
     (200, 2049, 520, 0.5, 1.0, 1),          # nine pieces of 256 columns
     (257, 3001, 1032, 0.25, 1.0, 0),
     (300, 1500, 200, 0.0, 1.0, 700 * 1024),  # two pieces
+    (256, 5000, 136, 0.0, 1.0, 1 << 20),
     (700, 777, 328, 0.0, 1.0, 0),
+    (1500, 300, 24, 0.6, 1.0, 0),
+    (40, 513, 65536, 0.0, 1.0, 0),          # a row of 128 KB
+    (600, 700, 33024, 0.0, 1.0, 0),         # hidden states of more than a row group: groups of one tile of rows
 ]
 
 
