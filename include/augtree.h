@@ -444,7 +444,7 @@ int augtree_plan_tree(const augtree_tree_t *tree, const augtree_profile_t *profi
  *                included) enters no result, and its work is saved
  *   id >= vocab  is treated like padding, and AUGTREE_ERR_INVALID_ARG with the position of the token as detail is
  *                recorded in the status word
- * No atomics on floating-point values: results are bitwise repeatable.
+ * No atomics on floating-point values: results are bitwise repeatable.  Outputs and scratch must not overlap inputs.
  */
 enum { AUGTREE_BF16 = 0, AUGTREE_F16 = 1, AUGTREE_F32 = 2 };
 typedef struct {
@@ -466,7 +466,7 @@ typedef struct augtree_lm augtree_lm_t;
 int augtree_lm_create(const augtree_lm_desc_t *desc, int device, augtree_lm_t **out);
 int augtree_lm_destroy(augtree_lm_t *lm);
 
-/* Scratch (16-byte aligned) that the calls need for n_tokens tokens; any of the pointers may be NULL. */
+/* Scratch (16-byte aligned) that is enough for the calls on up to n_tokens tokens; any of the pointers may be NULL. */
 int augtree_lm_workspace_bytes(const augtree_lm_t *lm, int64_t n_tokens, size_t *loss_fwd, size_t *loss_bwd, size_t *embed_bwd);
 
 /* out[t] = embed_scale * table[id_t], rounded once.  table and out: any of the three types each, 16-byte aligned. */

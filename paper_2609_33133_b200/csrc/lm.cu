@@ -66,9 +66,10 @@ int64_t pad_cols(const augtree_lm *lm) { return up(lm->hidden, 64); }
 // Columns of a piece of the vocabulary in the backward pass: as many as fit the scratch bound for G, in equal pieces.
 // With the default bound a piece has 4096 columns at least, so that the additions into dH's partial sums, one per
 // piece, stay a small part of the piece's products however many rows there are.
+int64_t piece_bound(const augtree_lm *lm) { return lm->piece_bytes > 0 ? lm->piece_bytes : (int64_t)512 << 20; }
+int64_t piece_least(const augtree_lm *lm) { return lm->piece_bytes > 0 ? kLmTile : 4096; }
 int64_t piece_cols(const augtree_lm *lm, int64_t rows_pad) {
-  const int64_t bound = lm->piece_bytes > 0 ? lm->piece_bytes : (int64_t)512 << 20, least = lm->piece_bytes > 0 ? kLmTile : 4096;
-  const int64_t cols = std::max<int64_t>(bound / (rows_pad * 2) / kLmTile * kLmTile, least);
+  const int64_t cols = std::max<int64_t>(piece_bound(lm) / (rows_pad * 2) / kLmTile * kLmTile, piece_least(lm));
   const int64_t pieces = (lm->vocab + cols - 1) / cols;
   return up((lm->vocab + pieces - 1) / pieces, kLmTile);
 }
@@ -76,19 +77,20 @@ int64_t piece_cols(const augtree_lm *lm, int64_t rows_pad) {
 // Shares of dH's contraction.  A launch holds dH's tiles (each a contraction over the piece, `kb` steps) and dW's (over the rows,
 // `kr` steps), dealt out to the CTA pairs in turn; the longest pair is waited for.  More shares even the pairs out (and let
 // few rows fill the GPU) but each costs a pass over the partial sums: the fewest within 2 % of the best.
+int64_t most_splits(int64_t rows) { return std::min<int64_t>(std::max<int64_t>(16384 / rows, 2), 32); }
 int dh_splits(const augtree_lm *lm, int64_t rows_pad, int halves, int64_t cols) {
   const int64_t pairs = std::max(lm->n_lanes / 2, 1), nt = (lm->hidden + kLmTile - 1) / kLmTile;
   const int64_t kb = halves * ((cols + 63) / 64), kr = halves * ((rows_pad + 63) / 64);
   const int64_t dh_tiles = rows_pad / kLmTile * nt, dw_tiles = (cols + kLmTile - 1) / kLmTile * nt;
   auto longest = [&](int64_t s) {
-    int64_t worst = 0;
-    for (int64_t i = 0; i < pairs; ++i) {
-      const int64_t all = (dh_tiles * s + dw_tiles - i + pairs - 1) / pairs, dh = std::max<int64_t>((dh_tiles * s - i + pairs - 1) / pairs, 0);
-      worst = std::max(worst, dh * ((kb + s - 1) / s) + (all - dh) * kr);
-    }
-    return worst;
+    // pair i has every pairs-th tile from i on: the longest is pair 0 or the first one with a dH tile less
+    auto load = [&](int64_t i) {
+      const int64_t dh = (dh_tiles * s - i + pairs - 1) / pairs, all = (dh_tiles * s + dw_tiles - i + pairs - 1) / pairs;
+      return dh * ((kb + s - 1) / s) + (all - dh) * kr;
+    };
+    return std::max(load(0), load(dh_tiles * s % pairs));
   };
-  const int64_t most = std::min<int64_t>(kb, 32);
+  const int64_t most = std::min<int64_t>(kb, most_splits(rows_pad));
   int64_t best = longest(1), pick = 1;
   for (int64_t s = 2; s <= most; ++s) best = std::min(best, longest(s));
   while (pick < most && longest(pick) * 100 > best * 102) ++pick;
@@ -108,8 +110,10 @@ int few_splits(const augtree_lm *lm, int64_t cols) {
   return (int)std::min<int64_t>(std::max<int64_t>(lm->n_lanes / tiles, 1), (cols + 63) / 64);
 }
 
-size_t loss_layout(const augtree_lm *lm, int64_t tokens, bool bwd, uint8_t *base, LossWs *w) {
-  const int64_t few = few_rows(tokens), rp = tile_rows(tokens), gr = rp * halves(tokens);
+// Cuts the scratch of a call on `tokens` tokens.  What a call needs does not always grow with its tokens (pieces, shares and the
+// few-row kernels change with them), so the size that a caller is told (`told`) takes the most of each part up to there.
+size_t loss_layout(const augtree_lm *lm, int64_t tokens, bool bwd, uint8_t *base, LossWs *w, bool told = false) {
+  const int64_t few = few_rows(tokens), rp = tile_rows(tokens), gr = rp * halves(tokens), few_most = std::min<int64_t>(rp, kLmFew);
   Cursor c{base};
   w->rows.n_rows = c.take<int>(1);
   w->rows.idx = c.take<int>(rp);
@@ -117,17 +121,24 @@ size_t loss_layout(const augtree_lm *lm, int64_t tokens, bool bwd, uint8_t *base
   w->rows.target = c.take<int>(rp);
   w->h = c.take<__nv_bfloat16>((bwd ? gr : rp) * pad_cols(lm));
   if (!bwd) {
+    const int64_t part_few = 4ll * lm->n_lanes * few_most, part_many = few ? 0 : (int64_t)n_part(lm) * rp;
     w->rows.lse2 = w->rows.gscale = nullptr;
     w->rows.x_target = c.take<float>(rp);
     w->tlogit = c.take<float>(rp);
-    w->part = c.take<float2>(few ? 4ll * lm->n_lanes * few : (int64_t)n_part(lm) * rp);
+    w->part = c.take<float2>(told ? std::max(part_few, part_many) : few ? part_few : part_many);
   } else {
     const int64_t cols = piece_cols(lm, gr);
+    int64_t grad = gr * cols, dh = (few ? few_splits(lm, cols) : dh_splits(lm, rp, halves(tokens), cols)) * rp;
+    if (told) {
+      const int64_t whole = up(lm->vocab, kLmTile), bound = std::max(piece_bound(lm) / 2, gr * piece_least(lm));
+      grad = std::min(gr * whole, bound + gr * kLmTile);   // (equal pieces are rounded up to whole tiles)
+      dh = std::max(few_splits(lm, whole) * few_most, few ? 0 : std::min<int64_t>(32 * rp, std::max<int64_t>(16384, 2 * rp)));
+    }
     w->rows.x_target = nullptr;
     w->rows.lse2 = c.take<float>(rp);
     w->rows.gscale = c.take<float>(rp);
-    w->grad = c.take<__nv_bfloat16>(gr * cols);
-    w->dh_part = c.take<float>((few ? few_splits(lm, cols) : dh_splits(lm, rp, halves(tokens), cols)) * rp * lm->hidden);
+    w->grad = c.take<__nv_bfloat16>(grad);
+    w->dh_part = c.take<float>(dh * lm->hidden);
   }
   return c.off;
 }
@@ -149,7 +160,7 @@ int embed_chunk(const augtree_lm *lm, int64_t n) {
   return chunk;
 }
 
-size_t embed_layout(const augtree_lm *lm, int64_t tokens, uint8_t *base, EmbedWs *w) {
+size_t embed_layout(const augtree_lm *lm, int64_t tokens, uint8_t *base, EmbedWs *w, bool told = false) {
   const int64_t n = std::max<int64_t>(tokens, 1), blocks = (n + kRadixBlock - 1) / kRadixBlock;
   Cursor c{base};
   for (int i = 0; i < 2; ++i) { w->key[i] = c.take<uint32_t>(n); w->val[i] = c.take<int>(n); }
@@ -157,9 +168,11 @@ size_t embed_layout(const augtree_lm *lm, int64_t tokens, uint8_t *base, EmbedWs
   w->total = c.take<int>(kSortBins);
   w->chunk = embed_chunk(lm, n);
   w->n_chunks = (int)((tokens + w->chunk - 1) / w->chunk);
-  w->joins = c.take<int>(w->n_chunks + 2);
+  const int64_t few_chunks = (std::min<int64_t>(n, 8192) + 15) / 16;  // (up to 8192 tokens the chunks are half as long)
+  const int64_t chunks = told ? std::max<int64_t>({few_chunks, w->n_chunks, std::min<int64_t>((n + 31) / 32, 64ll * lm->n_lanes + 1)}) : w->n_chunks;
+  w->joins = c.take<int>(chunks + 2);
   w->seen = c.take<uint32_t>((lm->vocab + 31) / 32);
-  w->part = c.take<float>(2ll * w->n_chunks * lm->hidden);
+  w->part = c.take<float>(2 * chunks * lm->hidden);
   return c.off;
 }
 
@@ -226,7 +239,9 @@ int launch(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream
   attr.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &attr; cfg.numAttrs = 1;
   ++g_launches;
-  return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...) == cudaSuccess ? AUGTREE_OK : AUGTREE_ERR_CUDA;
+  if (cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...) == cudaSuccess) return AUGTREE_OK;
+  cudaGetLastError();  // reported by the return value; not left for the caller's next check
+  return AUGTREE_ERR_CUDA;
 }
 
 // Scored rows packed into the scratch; with `weight` (forward) also their targets' logits.
@@ -457,9 +472,9 @@ int augtree_lm_workspace_bytes(const augtree_lm_t *lm, int64_t n_tokens, size_t 
   if (n_tokens > kMaxTokens) return AUGTREE_ERR_UNSUPPORTED;
   LossWs l;
   EmbedWs e;
-  if (loss_fwd) *loss_fwd = loss_layout(lm, n_tokens, false, nullptr, &l);
-  if (loss_bwd) *loss_bwd = loss_layout(lm, n_tokens, true, nullptr, &l);
-  if (embed_bwd) *embed_bwd = embed_layout(lm, n_tokens, nullptr, &e);
+  if (loss_fwd) *loss_fwd = loss_layout(lm, n_tokens, false, nullptr, &l, true);
+  if (loss_bwd) *loss_bwd = loss_layout(lm, n_tokens, true, nullptr, &l, true);
+  if (embed_bwd) *embed_bwd = embed_layout(lm, n_tokens, nullptr, &e, true);
   return AUGTREE_OK;
 }
 

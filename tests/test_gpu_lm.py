@@ -362,6 +362,73 @@ def test_two_streams_with_workspaces_of_their_own(B):
             assert torch.equal(x, q["want"][n]), n
 
 
+def test_one_workspace_for_every_smaller_call(B):
+    """A program keeps the scratch for its largest batch: every smaller call runs in it, whatever ran before."""
+    v, k, most = 2100, 72, 5400
+    lm = B.LM(v, k, device=0)
+    ws, check = guarded((lm.workspace_bytes(most),), torch.uint8, fill=0xFF)
+    h, w, y, a = lu.make_loss(most, v, k, seed=51, masked=0.1)
+    hc, wc, yc, ac = h.cuda(), w.cuda(), y.cuda(), a.cuda()
+    tab = torch.empty(v, k, device="cuda")
+    for t in (5400, 1, 4096, 128, 129, 256, 257, 511, 2000, 64, 5000, 4097):
+        loss, lse = torch.empty(t, device="cuda"), torch.empty(t, device="cuda")
+        dh, dw = torch.empty(t, k, device="cuda", dtype=BF16), torch.empty(v, k, device="cuda", dtype=BF16)
+        lm.loss_fwd(hc[:t], wc, yc[:t], loss, lse, ws)
+        lm.loss_bwd(hc[:t], wc, yc[:t], lse, ac[:t], dh, dw, ws)
+        lm.embed_bwd(hc[:t], yc[:t], tab, ws)
+        ref = lu.loss_reference(h[:t], w, y[:t], a[:t])
+        b = lu.loss_bounds(ref, v, k, t)
+        for n, x in (("loss", loss), ("d_hidden", dh), ("d_weight", dw)):
+            lu.assert_within(x, ref[n], b[n], (t, n))
+        check()
+    assert lm.device_status() == (0, 0)
+
+
+@pytest.mark.parametrize("lanes", [1, 3, 7, 1000])
+@pytest.mark.parametrize("t", [20, 140, 900])
+def test_any_number_of_lanes(B, lanes, t):
+    """Few CTAs walk many tiles each, through every turn of the rings and accumulators; more CTAs than the GPU holds queue."""
+    v, k = 3333, 328
+    h, w, y, a = lu.make_loss(t, v, k, seed=61, masked=0.1)
+    lm = B.LM(v, k, device=0, n_lanes=lanes, piece_bytes=1 << 21)
+    out = run_loss(B, h, w, y, a, lm=lm)
+    ref = lu.loss_reference(h, w, y, a)
+    b = lu.loss_bounds(ref, v, k, t)
+    for n in ("lse", "loss", "d_hidden", "d_weight"):
+        lu.assert_within(out[n], ref[n], b[n], n)
+    d = torch.randn(t, k, generator=torch.Generator().manual_seed(1))
+    tab = torch.empty(v, k, device="cuda")
+    lm.embed_bwd(d.cuda(), y.cuda(), tab, workspace(lm, t))
+    want, bound = lu.embed_grad_reference(d, y, v, 1.0)
+    lu.assert_within(tab, want, bound, "d_table")
+
+
+@pytest.mark.parametrize("t,v,k", [(5000, 300, 16), (6000, 300000, 8), (70000, 5, 8), (40000, 1 << 20, 8), (3000, 1500000, 8)])
+def test_embedding_gradient_sort_passes(B, t, v, k):
+    """One, two and three radix passes, a table of five rows under 70000 tokens, vocabularies beyond the one-block sort's."""
+    g = torch.Generator().manual_seed(t)
+    ids = ids_of("frequent", t, v, g)
+    ids[::9] = -1
+    d = torch.randn(t, k, generator=g)
+    lm = B.LM(v, k, device=0)
+    out = torch.full((v, k), float("nan"), device="cuda")
+    lm.embed_bwd(d.cuda(), ids.cuda(), out, workspace(lm, t))
+    want, bound = lu.embed_grad_reference(d, ids, v, 1.0)
+    lu.assert_within(out, want, bound, "d_table")
+
+
+def test_negative_and_tiny_scales(B):
+    t, v, k = 60, 500, 64
+    h, w, y, a = lu.make_loss(t, v, k, seed=71)
+    for scale in (-1.5, 1e-3, 7.0):
+        out = run_loss(B, h, w, y, a, scale)
+        ref = lu.loss_reference(h, w, y, a, scale)
+        ref["reach"] = abs(ref["reach"])
+        b = lu.loss_bounds(ref, v, k, t)
+        for n in ("lse", "loss", "d_hidden", "d_weight"):
+            lu.assert_within(out[n], ref[n], b[n], (scale, n))
+
+
 def test_refusals(B):
     t, v, k = 10, 100, 64
     lm = B.LM(v, k, device=0)

@@ -59,3 +59,14 @@ def test_workspace_grows_with_the_piece_bound(B):
     assert small < large <= small + (256 << 20) + (64 << 20) * 64
     # sizes beyond 32 bits do not wrap
     assert B.LM(152064, 8192, device=None, n_lanes=148).workspace_parts(2_000_000)[1] > 2_000_000 * 8192 * 2
+
+
+@pytest.mark.parametrize("vocab,hidden,lanes,piece", [(152064, 3584, 148, 0), (503, 256, 148, 0), (50257, 1032, 148, 1 << 24), (700, 64, 3, 1), (40000, 8, 1000, 0)])
+def test_workspace_for_more_tokens_is_enough_for_fewer(B, vocab, hidden, lanes, piece):
+    """Pieces, shares and the few-row kernels change with the number of tokens; the size that is told never shrinks with it."""
+    lm = B.LM(vocab, hidden, device=None, n_lanes=lanes, piece_bytes=piece)
+    last = (0, 0, 0)
+    for n in sorted({*range(0, 700, 3), *range(700, 20000, 397), 127, 128, 129, 256, 257, 4096, 4097, 8192, 8193, 303104, 303105, 1000000}):
+        now = lm.workspace_parts(n)
+        assert all(a >= b for a, b in zip(now, last)), (n, now, last)
+        last = now
