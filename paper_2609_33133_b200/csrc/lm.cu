@@ -529,15 +529,21 @@ int augtree_lm_loss_fwd(const augtree_lm_t *lm, const void *hidden, const void *
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const int64_t rp = tile_rows(n_tokens);
   const int few = few_rows(n_tokens);
-  if ((r = compact(lm, targets, id_bytes, n_tokens, hidden, weight, w, nullptr, nullptr, loss, lse, st))) return r;
   Maps m = {};
   if (few) {
     FewParams p = few_params(lm, w, base_params(lm, w, few));
     p.n = lm->vocab;
-    if ((r = map_2d(&m.h, w.h, few, pad_cols(lm), few)) || (r = map_2d(&m.w, weight, lm->vocab, lm->hidden, 128))) return r;
+    p.ids = targets; p.id_bytes = id_bytes; p.tokens = (int)n_tokens;
+    if ((r = map_2d(&m.h, hidden, n_tokens, lm->hidden, few)) || (r = map_2d(&m.w, weight, lm->vocab, lm->hidden, 128))) return r;
     if ((r = launch_few<LM_STATS>(lm, few, m.w, m.h, p, st))) return r;
-    return launch(lm_few_finish_kernel, few, 256, 0, st, w.part, 4 * lm->n_lanes, w.rows, w.tlogit, lm->logit_scale, loss, lse);
+    auto finish = [&](auto kernel, auto *ids) {
+      return launch(kernel, (unsigned)n_tokens, 256, 0, st, w.part, 4 * lm->n_lanes, ids, lm->vocab, static_cast<const uint4 *>(hidden),
+                    static_cast<const uint4 *>(weight), lm->hidden / 8, w.tlogit, lm->logit_scale, loss, lse, lm->d_status);
+    };
+    return id_bytes == 8 ? finish(lm_few_finish_kernel<long long>, static_cast<const long long *>(targets))
+                         : finish(lm_few_finish_kernel<int>, static_cast<const int *>(targets));
   }
+  if ((r = compact(lm, targets, id_bytes, n_tokens, hidden, weight, w, nullptr, nullptr, loss, lse, st))) return r;
   if ((r = map_2d(&m.h, w.h, rp, pad_cols(lm), 128)) || (r = map_2d(&m.w, weight, lm->vocab, lm->hidden, 128))) return r;
   LmParams p = base_params(lm, w, rp);
   p.n_jobs = 1;

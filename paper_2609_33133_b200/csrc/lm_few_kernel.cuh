@@ -29,12 +29,14 @@ constexpr int kLmFew = 128;       // most rows
 constexpr int kFewThreads = 192;
 
 struct FewParams {
-  const int *n_rows;
+  const int *n_rows;              // GRAD, DH: packed rows (device)
+  const void *ids;                // STATS: the targets themselves, [tokens]; the rows are not packed, a row is only its column
+  int id_bytes, tokens;
   int v0, n, vocab, hidden;       // first vocabulary row of the piece, its rows; whole sizes
   int splits;                     // DH: shares of the piece
   float scale_log2;
-  const int *target;              // [N]
-  const float *lse2, *gscale;     // [N]
+  const int *target;              // GRAD: [N]
+  const float *lse2, *gscale;     // GRAD: [N]
   float2 *part;                   // STATS: [N][4 gridDim.x]
   float *tlogit;                  // STATS: [N]
   __nv_bfloat16 *grad;            // GRAD: [2 N][ld_grad]
@@ -140,13 +142,17 @@ lm_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ 
   if (warp == 5) { tmem_alloc(smem_u32((const void *)tmem_slot), 512); tmem_relinquish(); }
   if (warp == 4 && lane == 0) { tma_prefetch_desc(&tm_w); tma_prefetch_desc(&tm_b); }
   wait_previous();
-  const int n_rows = *reinterpret_cast<const volatile int *>(p.n_rows);
+  const int n_rows = KIND == LM_STATS ? p.tokens : *reinterpret_cast<const volatile int *>(p.n_rows);
   if (KIND != LM_DH && threadIdx.x < N) {
-    const bool live = threadIdx.x < n_rows;
-    s_target[threadIdx.x] = live ? p.target[threadIdx.x] : -1;
-    if (KIND == LM_GRAD) {
-      s_lse2[threadIdx.x] = live ? p.lse2[threadIdx.x] : 0.f;
-      s_gscale[threadIdx.x] = live ? p.gscale[threadIdx.x] : 0.f;
+    const int t = threadIdx.x;
+    const bool live = t < n_rows;
+    if (KIND == LM_STATS) {
+      const long long id = !live ? -1 : p.id_bytes == 8 ? static_cast<const long long *>(p.ids)[t] : static_cast<const int *>(p.ids)[t];
+      s_target[t] = id >= 0 && id < p.vocab ? (int)id : -1;
+    } else {
+      s_target[t] = live ? p.target[t] : -1;
+      s_lse2[t] = live ? p.lse2[t] : 0.f;
+      s_gscale[t] = live ? p.gscale[t] : 0.f;
     }
   }
   tc_fence_before();

@@ -202,26 +202,34 @@ __device__ __forceinline__ void write_loss(float2 s, float tlogit, float x_targe
   *lse = v + x_target * logit_scale;
 }
 
-// Few rows: a block per row, its pairs one after the other in memory.
+// Few rows: a block per token, its pairs one after the other in memory, and its target's logit beside them.
+template <typename Id>
 __global__ void __launch_bounds__(256)
-lm_few_finish_kernel(const float2 *part, int n_part, const LmRows rows, const float *tlogit, float logit_scale,
-                     float *loss, float *lse) {
+lm_few_finish_kernel(const float2 *part, int n_part, const Id *targets, int vocab, const uint4 *hidden, const uint4 *weight, int row_vecs,
+                     const float *tlogit, float logit_scale, float *loss, float *lse, int *status) {
   launch_next();
   wait_previous();
   __shared__ float2 sh[8];
-  const int r = blockIdx.x;
-  if (r >= *rows.n_rows) return;
+  __shared__ float dot[8];
+  const int t = blockIdx.x;
+  const long long id = targets[t];
+  if (threadIdx.x == 0) check_id(targets[t], t, vocab, status);
+  if (id < 0 || id >= vocab) {
+    if (threadIdx.x == 0) { loss[t] = 0.f; lse[t] = 0.f; }
+    return;
+  }
+  float x = 0.f;
+  for (int i = threadIdx.x; i < row_vecs; i += 256) x += dot8(hidden[(long long)t * row_vecs + i], weight[id * row_vecs + i]);
   float2 s = make_float2(-INFINITY, 0.f);
-  for (int i = threadIdx.x; i < n_part; i += 256) s = merge_stats(s, part[(long long)r * n_part + i]);
+  for (int i = threadIdx.x; i < n_part; i += 256) s = merge_stats(s, part[(long long)t * n_part + i]);
 #pragma unroll
   for (int d = 16; d >= 1; d >>= 1)
     s = merge_stats(s, make_float2(__shfl_down_sync(0xffffffffu, s.x, d), __shfl_down_sync(0xffffffffu, s.y, d)));
   if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = s;
-  __syncthreads();
+  x = block_sum<256>(x, dot);
   if (threadIdx.x == 0) {
     for (int w = 1; w < 8; ++w) s = merge_stats(s, sh[w]);
-    const int t = rows.idx[r];
-    write_loss(s, tlogit[r], rows.x_target[r], logit_scale, loss + t, lse + t);
+    write_loss(s, tlogit[t], x, logit_scale, loss + t, lse + t);
   }
 }
 

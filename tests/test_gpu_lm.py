@@ -77,6 +77,11 @@ LOSS_CASES = [
     (300, 1500, 200, 0.0, 1.0, 700 * 1024),  # two pieces
     (256, 5000, 136, 0.0, 1.0, 1 << 20),
     (700, 777, 328, 0.0, 1.0, 0),
+    (300, 600, 288, 0.0, 1.0, 0),           # hidden sizes whose last tile has 32, 64, 128, 40 and 192 columns
+    (300, 600, 320, 0.0, 1.0, 0),
+    (260, 600, 384, 0.1, 1.0, 0),
+    (260, 600, 296, 0.0, 1.0, 0),
+    (150, 600, 448, 0.0, 1.0, 0),
     (1500, 300, 24, 0.6, 1.0, 0),
     (40, 513, 65536, 0.0, 1.0, 0),          # a row of 128 KB
     (600, 700, 33024, 0.0, 1.0, 0),         # hidden states of more than a row group: groups of one tile of rows
