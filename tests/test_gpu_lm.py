@@ -472,9 +472,10 @@ def test_refusals(B):
     assert lm.device_status() == (0, 0)
 
 
-def test_a_wait_that_runs_out_is_reported(B):
+@pytest.mark.parametrize("t", [20, 130])
+def test_a_wait_that_runs_out_is_reported(B, t):
     """A tile that is never loaded: the call returns, the status word names the wait, the next call is right."""
-    t, v, k = 130, 700, 136
+    v, k = 700, 136
     h, w, y, a = lu.make_loss(t, v, k, seed=41)
     bad = B.LM(v, k, device=0, flags=B.FLAG_TEST_SHORT_WAIT | B.FLAG_TEST_SKIP_FWD_LOAD)
     ws = workspace(bad, t)
