@@ -586,6 +586,7 @@ int augtree_lm_loss_bwd(const augtree_lm_t *lm, const void *hidden, const void *
   LmParams p = base_params(lm, w, rp);
   p.mn_chunks = chunks;
   p.halves = half;
+  p.grad_lo = w.grad + rp * cols; p.ld_grad = cols;
   p.dw_f32 = weight_dtype == AUGTREE_F32; p.dw_add = accumulate;
   CUtensorMap out_g, out_dw;
   if (!few && ((r = map_out(&out_g, w.grad, gr, cols, false)) || (r = map_out(&m.dh, w.dh_part, splits * rp, lm->hidden, true)))) return r;

@@ -67,6 +67,8 @@ struct LmParams {
   float2 *part;             // STATS: [2 x vocabulary tiles][rows_pad] (m, l)
   float *tlogit;            // STATS: [rows_pad] x at the target
   int halves;               // 2: G is hi in rows 0 .. rows_pad, lo in the rows behind them; 1: hi alone
+  __nv_bfloat16 *grad_lo;   // GRAD with two halves: [rows_pad][ld_grad], where lo goes
+  long long ld_grad;
   int half_k;               // DH: contraction steps x 64 of one half
   int dh_add;               // DH: add to what an earlier piece left in the partial sums
   int dw_f32, dw_add;       // DW: type of dW, add to what is there
@@ -347,8 +349,7 @@ lm_tile_kernel(const __grid_constant__ CUtensorMap tm_h, const __grid_constant__
         const bool live = row < n_rows;
         const int tgt = live ? p.target[row] - p.v0 - n0 : -1;
         const float lse2 = live ? p.lse2[row] : 0.f, gs = live ? p.gscale[row] : 0.f;
-        for (int i = 0; i < 4 * p.halves; ++i) {
-          const int q = i & 3;
+        for (int q = 0; q < 4; ++q) {
           uint32_t v[32];
           tmem_ld32(tD + q * 32, v);
           tc_wait_ld();
@@ -358,14 +359,26 @@ lm_tile_kernel(const __grid_constant__ CUtensorMap tm_h, const __grid_constant__
           for (int e = 0; e < 32; ++e) {
             const float pr = ex2(fmaf(__uint_as_float(v[e]), p.scale_log2, -lse2)) - (tgt - q * 32 == e ? 1.f : 0.f);
             g[e] = live && e < left ? pr * gs : 0.f;
-            if (i >= 4) g[e] -= __bfloat162float(__float2bfloat16_rn(g[e]));
           }
           if (!(q & 1)) { if (lane == 0) bulk_wait_read(); __syncwarp(); }
           stage_bf16(s_out, lane, (q & 1) * 4, g);
+          if (p.halves == 2) {  // few rows: lo by plain stores, there is no second block to stage it in
+            __nv_bfloat16 *lo = p.grad_lo + (long long)row * p.ld_grad + n0 + q * 32;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              uint32_t w[4];
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                const float a = g[8 * e + 2 * j], b = g[8 * e + 2 * j + 1];
+                w[j] = pack_bf16(a - __bfloat162float(__float2bfloat16_rn(a)), b - __bfloat162float(__float2bfloat16_rn(b)));
+              }
+              *reinterpret_cast<uint4 *>(lo + 8 * e) = make_uint4(w[0], w[1], w[2], w[3]);  // (the scratch is aligned to 16 bytes)
+            }
+          }
           if (q & 1) {
             fence_async_shared();
             __syncwarp();
-            if (lane == 0) { tma_store_2d(&tm_out, s_out, n0 + (q - 1) * 32, i < 4 ? row0 : row0 + (int)p.rows_pad); bulk_commit(); }
+            if (lane == 0) { tma_store_2d(&tm_out, s_out, n0 + (q - 1) * 32, row0); bulk_commit(); }
           }
         }
       } else {

@@ -389,6 +389,35 @@ def test_one_workspace_for_every_smaller_call(B):
     assert lm.device_status() == (0, 0)
 
 
+@pytest.mark.parametrize("t", [20, 140, 300, 5000])
+def test_tensors_and_scratch_on_odd_16_byte_boundaries(B, t):
+    """Everything 16 bytes off the allocator's boundaries, which is all that the interface asks for."""
+    v, k = 777, 72
+
+    def off(x):
+        raw = torch.empty(x.nbytes + 16, device="cuda", dtype=torch.uint8)
+        y = raw[16:].view(x.dtype).view(x.shape)
+        y.copy_(x)
+        assert y.data_ptr() % 32 == 16
+        return y
+    h, w, y, a = lu.make_loss(t, v, k, seed=81, masked=0.1)
+    lm = B.LM(v, k, device=0)
+    hc, wc, ws = off(h.cuda()), off(w.cuda()), off(workspace(lm, t))
+    dh, dw, tab = off(torch.zeros(t, k, device="cuda", dtype=BF16)), off(torch.zeros(v, k, device="cuda", dtype=BF16)), off(torch.zeros(v, k, device="cuda"))
+    loss, lse = torch.zeros(t, device="cuda"), torch.zeros(t, device="cuda")
+    lm.loss_fwd(hc, wc, y.cuda(), loss, lse, ws)
+    lm.loss_bwd(hc, wc, y.cuda(), lse, a.cuda(), dh, dw, ws)
+    lm.embed_bwd(hc, y.cuda(), tab, ws)
+    ref = lu.loss_reference(h, w, y, a)
+    b = lu.loss_bounds(ref, v, k, t)
+    for n, x in (("loss", loss), ("d_hidden", dh), ("d_weight", dw)):
+        lu.assert_within(x, ref[n], b[n], n)
+    want, bound = lu.embed_grad_reference(h, y, v, 1.0)
+    lu.assert_within(tab, want, bound, "d_table")
+    lm.embed_fwd(wc, y.cuda(), dh)
+    assert torch.equal(dh, torch.where(y.cuda()[:, None] >= 0, wc[y.cuda().clamp(min=0)].float(), 0.0).to(BF16))
+
+
 @pytest.mark.parametrize("lanes", [1, 3, 7, 1000])
 @pytest.mark.parametrize("t", [20, 140, 900])
 def test_any_number_of_lanes(B, lanes, t):
