@@ -152,10 +152,14 @@ struct EmbedWs {
   int chunk, n_chunks;
 };
 
-// Sorted tokens of a chunk: 32 (24576 tokens x 3584 bf16: 237 us against 243 with 16; 131071 x 1032 fp32: 151 us against 155 with 64), half
-// of that when there are too few to give every SM blocks, more when the sums of the rows that cross chunks would grow large.
+// Sorted tokens of a chunk.  A few tokens wait for memory, a chunk's one after the other, so they are spread over four blocks an
+// SM as far as chunks of 8 allow (2000 tokens into 5000 x 256: 16 us with 8 a chunk, 22 with 16; 100 tokens into 5000 x 1024: 16 us
+// with 8, 22 with 4, which leave more rows to join); many take chunks of 32 (24576
+// tokens x 3584 bf16: 237 us against 243 with 16; 131071 x 1032 fp32: 151 against 155 with 64), and more when the sums of the rows
+// that cross chunks would grow large.
 int embed_chunk(const augtree_lm *lm, int64_t n) {
-  int chunk = n <= 8192 ? 16 : 32;
+  int chunk = 8;
+  while (chunk < 32 && n / chunk > 4ll * lm->n_lanes) chunk *= 2;
   while (chunk < kEmbedMaxChunk && n / chunk > 64ll * lm->n_lanes) chunk *= 2;
   return chunk;
 }
@@ -168,8 +172,8 @@ size_t embed_layout(const augtree_lm *lm, int64_t tokens, uint8_t *base, EmbedWs
   w->total = c.take<int>(kSortBins);
   w->chunk = embed_chunk(lm, n);
   w->n_chunks = (int)((tokens + w->chunk - 1) / w->chunk);
-  const int64_t few_chunks = (std::min<int64_t>(n, 8192) + 15) / 16;  // (up to 8192 tokens the chunks are half as long)
-  const int64_t chunks = told ? std::max<int64_t>({few_chunks, w->n_chunks, std::min<int64_t>((n + 31) / 32, 64ll * lm->n_lanes + 1)}) : w->n_chunks;
+  const int64_t most = std::max(std::min<int64_t>((n + 7) / 8, 4ll * lm->n_lanes + 1), std::min<int64_t>((n + 31) / 32, 64ll * lm->n_lanes + 1));
+  const int64_t chunks = told ? std::max<int64_t>(most, w->n_chunks) : w->n_chunks;
   w->joins = c.take<int>(chunks + 2);
   w->seen = c.take<uint32_t>((lm->vocab + 31) / 32);
   w->part = c.take<float>(2 * chunks * lm->hidden);
