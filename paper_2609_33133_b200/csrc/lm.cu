@@ -134,7 +134,7 @@ size_t loss_layout(const augtree_lm *lm, int64_t tokens, bool bwd, uint8_t *base
       grad = std::min(gr * whole, bound + gr * kLmTile);   // (equal pieces are rounded up to whole tiles)
       dh = std::max(few_splits(lm, whole) * few_most, few ? 0 : std::min<int64_t>(32 * rp, std::max<int64_t>(16384, 2 * rp)));
     }
-    w->rows.x_target = nullptr;
+    w->rows.x_target = c.take<float>(rp);
     w->rows.lse2 = c.take<float>(rp);
     w->rows.gscale = c.take<float>(rp);
     w->grad = c.take<__nv_bfloat16>(grad);
@@ -248,7 +248,7 @@ int launch(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream
   return AUGTREE_ERR_CUDA;
 }
 
-// Scored rows packed into the scratch; with `weight` (forward) also their targets' logits.
+// Scored rows packed into the scratch, and their targets' logits (forward: lse null) or gradients.
 int compact(const augtree_lm *lm, const void *targets, int id_bytes, int64_t tokens, const void *hidden, const void *weight, const LossWs &w,
             const float *lse, const float *d_loss, float *loss_out, float *lse_out, cudaStream_t st) {
   const auto *ids64 = static_cast<const long long *>(targets);
@@ -274,7 +274,7 @@ int compact(const augtree_lm *lm, const void *targets, int id_bytes, int64_t tok
                                        loss_out, lse_out, lm->d_status);
   if (r) return r;
   const unsigned grid = (unsigned)std::min<int64_t>(up(tokens, 256), 8 * lm->n_lanes);
-  return launch(lm_gather_kernel, grid, 256, 0, st, src, w.rows, dst, row_vecs, out_vecs, wt);
+  return launch(lm_gather_kernel, grid, 256, 0, st, src, w.rows, dst, row_vecs, out_vecs, wt, lse, lm->logit_scale);
 }
 
 LmParams base_params(const augtree_lm *lm, const LossWs &w, int64_t rows_pad) {
@@ -284,7 +284,7 @@ LmParams base_params(const augtree_lm *lm, const LossWs &w, int64_t rows_pad) {
   p.rows_pad = rows_pad;
   p.halves = 1;
   p.scale_log2 = lm->logit_scale * 1.4426950408889634f;
-  p.target = w.rows.target; p.lse2 = w.rows.lse2; p.gscale = w.rows.gscale;
+  p.target = w.rows.target; p.lse2 = w.rows.lse2; p.gscale = w.rows.gscale; p.gtarget = w.rows.x_target;
   p.status = lm->d_status;
   p.wait_budget = (lm->flags & AUGTREE_FLAG_TEST_SHORT_WAIT) ? kWaitBudgetClocksTest : kWaitBudgetClocks;
   p.test_flags = (lm->flags & AUGTREE_FLAG_TEST_SKIP_FWD_LOAD) ? TEST_SKIP_FWD_LOAD : 0;
@@ -336,7 +336,7 @@ int few_attributes() {
 FewParams few_params(const augtree_lm *lm, const LossWs &w, const LmParams &b) {
   FewParams p = {};
   p.n_rows = b.n_rows; p.vocab = b.vocab; p.hidden = b.hidden; p.scale_log2 = b.scale_log2;
-  p.target = b.target; p.lse2 = b.lse2; p.gscale = b.gscale;
+  p.target = b.target; p.lse2 = b.lse2; p.gscale = b.gscale; p.gtarget = b.gtarget;
   p.part = w.part; p.tlogit = w.tlogit; p.grad = w.grad; p.dh_part = w.dh_part;
   p.status = b.status; p.wait_budget = b.wait_budget; p.test_flags = b.test_flags;
   return p;
@@ -581,7 +581,7 @@ int augtree_lm_loss_bwd(const augtree_lm_t *lm, const void *hidden, const void *
   const int few = few_rows(n_tokens), half = halves(n_tokens);
   const int64_t rp = tile_rows(n_tokens), gr = rp * half, cols = piece_cols(lm, gr);
   const int splits = few ? few_splits(lm, cols) : dh_splits(lm, rp, half, cols), chunks = lm->hidden % 64 == 0 ? 2 : 1;
-  if ((r = compact(lm, targets, id_bytes, n_tokens, hidden, nullptr, w, lse, d_loss, nullptr, nullptr, st))) return r;
+  if ((r = compact(lm, targets, id_bytes, n_tokens, hidden, weight, w, lse, d_loss, nullptr, nullptr, st))) return r;
   Maps m = {};
   if ((r = map_2d(&m.h, w.h, gr, pad_cols(lm), few ? few : 128)) || (r = map_2d(&m.w, weight, lm->vocab, lm->hidden, 128)) ||
       (r = map_mn(&m.h_mn, w.h, gr, pad_cols(lm), 2)) || (r = map_mn(&m.w_mn, weight, lm->vocab, lm->hidden, chunks)) ||

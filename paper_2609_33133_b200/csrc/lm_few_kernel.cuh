@@ -37,7 +37,7 @@ struct FewParams {
   int splits;                     // DH: shares of the piece
   float scale_log2;
   const int *target;              // GRAD: [N]
-  const float *lse2, *gscale;     // GRAD: [N]
+  const float *lse2, *gscale, *gtarget;  // GRAD: [N]
   float2 *part;                   // STATS: [N][4 gridDim.x]
   float *tlogit;                  // STATS: [N]
   __nv_bfloat16 *grad;            // GRAD: [2 N][ld_grad]
@@ -57,8 +57,8 @@ struct FewSmem {
   static constexpr int kABytes = kSub * 128 * 128, kBBytes = kBRows * 128;
   static constexpr int kStageBytes = kABytes + kBBytes;
   static constexpr int kStages = (220 * 1024) / kStageBytes;  // 3 (DH, N = 128) .. 12
-  static constexpr int kOffRows = kStages * kStageBytes;      // target, lse2, gscale
-  static constexpr int kOffBar = kOffRows + 3 * kLmFew * 4;
+  static constexpr int kOffRows = kStages * kStageBytes;      // target, lse2, gscale, gtarget
+  static constexpr int kOffBar = kOffRows + 4 * kLmFew * 4;
   static constexpr int kBytes = kOffBar + 256;
   static_assert(kStages >= 3 && kStages <= 12 && kBytes <= 227 * 1024, "stage ring");
 };
@@ -131,7 +131,7 @@ lm_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ 
   volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(smem_raw + SM::kOffBar + 224);
   volatile int *abort_flag = reinterpret_cast<volatile int *>(smem_raw + SM::kOffBar + 232);
   int *s_target = reinterpret_cast<int *>(smem_raw + SM::kOffRows);
-  float *s_lse2 = reinterpret_cast<float *>(s_target + kLmFew), *s_gscale = s_lse2 + kLmFew;
+  float *s_lse2 = reinterpret_cast<float *>(s_target + kLmFew), *s_gscale = s_lse2 + kLmFew, *s_gtarget = s_gscale + kLmFew;
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
@@ -154,6 +154,7 @@ lm_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ 
       s_target[t] = live ? p.target[t] : -1;
       s_lse2[t] = live ? p.lse2[t] : 0.f;
       s_gscale[t] = live ? p.gscale[t] : 0.f;
+      s_gtarget[t] = live ? p.gtarget[t] : 0.f;
     }
   }
   tc_fence_before();
@@ -284,8 +285,8 @@ lm_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ 
 #pragma unroll
           for (int j = 0; j < W; ++j) {
             const int t = g * W + j;
-            const float pr = ex2(fmaf(__uint_as_float(raw[j]), p.scale_log2, -s_lse2[t])) - (s_target[t] == v ? 1.f : 0.f);
-            const float d = exists && t < n_rows ? pr * s_gscale[t] : 0.f;
+            const float pr = ex2(fmaf(__uint_as_float(raw[j]), p.scale_log2, -s_lse2[t]));
+            const float d = !(exists && t < n_rows) ? 0.f : s_target[t] == v ? s_gtarget[t] : pr * s_gscale[t];
             const __nv_bfloat16 hi = __float2bfloat16_rn(d);
             dst[t * p.ld_grad] = hi;
             dst[(N + t) * p.ld_grad] = __float2bfloat16_rn(d - __bfloat162float(hi));

@@ -24,7 +24,7 @@ struct LmRows {
   int *target;      // [rows_pad]
   float *lse2;      // [rows_pad] backward only
   float *gscale;    // [rows_pad] backward only
-  float *x_target;  // [rows_pad] forward only: h . W_target
+  float *x_target;  // [rows_pad] forward: h . W_target; backward: the target's gradient a c (p - 1)
 };
 
 template <typename Id>
@@ -76,7 +76,8 @@ lm_compact_kernel(const Id *targets, int tokens, int vocab, LmRows o, const floa
 
 // h . W_target of a row in fp32 by a whole block, from 16-byte vectors of eight bf16 numbers.  The tensor core's adder drops
 // what does not fit its accumulator, 224 times for 3584 columns, always towards zero: 3e-6 of a large logit, and the
-// target's is the large one in a confident row.  This sum rounds to nearest, in short chains.  Valid in thread 0.
+// target's is the large one in a confident row.  This sum rounds to nearest, in short chains.  Valid in thread 0.  (The backward
+// pass needs it too: p - 1 of a confident target is small, and 4e-5 of logit is 4 % of it where p is 0.999.)
 __device__ __forceinline__ float dot8(const uint4 a, const uint4 b) {
   const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
   float s = 0.f;
@@ -101,17 +102,23 @@ __device__ __forceinline__ float block_sum(float s, float *sh) {
   return s;
 }
 
+// p - 1 of the target from its logit, without the cancellation
+__device__ __forceinline__ float target_gradient(float gscale, float x_target, float logit_scale, float lse) {
+  return gscale * expm1f(fmaf(x_target, logit_scale, -lse));
+}
+
 // Hidden states of the scored rows, packed; zeros up to the next multiple of 256 rows (they enter contractions), and up to the next
-// multiple of 64 columns, so that every box of the copy engine is whole lines.  With `weight` also their targets' logits.
+// multiple of 64 columns, so that every box of the copy engine is whole lines.  Also their targets' logits (lse null) or gradients.
 __global__ void __launch_bounds__(256)
-lm_gather_kernel(const uint4 *hidden, const LmRows rows, uint4 *out, int row_vecs, int out_vecs, const uint4 *weight) {
+lm_gather_kernel(const uint4 *hidden, const LmRows rows, uint4 *out, int row_vecs, int out_vecs, const uint4 *weight, const float *lse,
+                 float logit_scale) {
   launch_next();
   wait_previous();
   __shared__ float sh[8];
   const int n = *rows.n_rows, n_pad = (n + 255) / 256 * 256;
   for (int r = blockIdx.x; r < n_pad; r += gridDim.x) {
     const uint4 *src = r < n ? hidden + (long long)rows.idx[r] * row_vecs : nullptr;
-    const uint4 *wt = src && weight ? weight + (long long)rows.target[r] * row_vecs : nullptr;
+    const uint4 *wt = src ? weight + (long long)rows.target[r] * row_vecs : nullptr;
     uint4 *dst = out + (long long)r * out_vecs;
     float s = 0.f;
     for (int i = threadIdx.x; i < out_vecs; i += 256) {
@@ -121,7 +128,7 @@ lm_gather_kernel(const uint4 *hidden, const LmRows rows, uint4 *out, int row_vec
     }
     if (wt) {
       s = block_sum<256>(s, sh);
-      if (threadIdx.x == 0) rows.x_target[r] = s;
+      if (threadIdx.x == 0) rows.x_target[r] = lse ? target_gradient(rows.gscale[r], s, logit_scale, lse[rows.idx[r]]) : s;
     }
   }
 }
@@ -169,7 +176,7 @@ lm_rows_kernel(const Id *targets, int tokens, int vocab, LmRows o, const float *
   }
   __syncthreads();
   const uint4 *src = from >= 0 ? hidden + (long long)from * row_vecs : nullptr;
-  const uint4 *wt = src && weight ? weight + (long long)targets[from] * row_vecs : nullptr;
+  const uint4 *wt = src ? weight + (long long)targets[from] * row_vecs : nullptr;
   float s = 0.f;
   for (int i = t; i < out_vecs; i += THREADS) {
     const uint4 v = src && i < row_vecs ? src[i] : make_uint4(0, 0, 0, 0);
@@ -179,7 +186,7 @@ lm_rows_kernel(const Id *targets, int tokens, int vocab, LmRows o, const float *
   }
   if (wt) {
     s = block_sum<THREADS>(s, sh);
-    if (t == 0) o.x_target[row] = s;
+    if (t == 0) o.x_target[row] = lse ? target_gradient(d_loss[from] * logit_scale, s, logit_scale, lse[from]) : s;
   }
 }
 

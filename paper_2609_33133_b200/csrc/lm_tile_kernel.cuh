@@ -64,6 +64,7 @@ struct LmParams {
   const int *target;        // [rows_pad]
   const float *lse2;        // [rows_pad] lse log2(e)
   const float *gscale;      // [rows_pad] a_t c; 0 behind the last row
+  const float *gtarget;     // [rows_pad] G at the target, from an fp32 logit
   float2 *part;             // STATS: [2 x vocabulary tiles][rows_pad] (m, l)
   float *tlogit;            // STATS: [rows_pad] x at the target
   int halves;               // 2: G is hi in rows 0 .. rows_pad, lo in the rows behind them; 1: hi alone
@@ -348,7 +349,7 @@ lm_tile_kernel(const __grid_constant__ CUtensorMap tm_h, const __grid_constant__
       } else if (c.kind == LM_GRAD) {
         const bool live = row < n_rows;
         const int tgt = live ? p.target[row] - p.v0 - n0 : -1;
-        const float lse2 = live ? p.lse2[row] : 0.f, gs = live ? p.gscale[row] : 0.f;
+        const float lse2 = live ? p.lse2[row] : 0.f, gs = live ? p.gscale[row] : 0.f, gt = live ? p.gtarget[row] : 0.f;
         for (int q = 0; q < 4; ++q) {
           uint32_t v[32];
           tmem_ld32(tD + q * 32, v);
@@ -357,8 +358,8 @@ lm_tile_kernel(const __grid_constant__ CUtensorMap tm_h, const __grid_constant__
           float g[32];
 #pragma unroll
           for (int e = 0; e < 32; ++e) {
-            const float pr = ex2(fmaf(__uint_as_float(v[e]), p.scale_log2, -lse2)) - (tgt - q * 32 == e ? 1.f : 0.f);
-            g[e] = live && e < left ? pr * gs : 0.f;
+            const float pr = ex2(fmaf(__uint_as_float(v[e]), p.scale_log2, -lse2));
+            g[e] = tgt - q * 32 == e ? gt : live && e < left ? pr * gs : 0.f;
           }
           if (!(q & 1)) { if (lane == 0) bulk_wait_read(); __syncwarp(); }
           stage_bf16(s_out, lane, (q & 1) * 4, g);

@@ -181,6 +181,29 @@ def test_confident_and_large_logits(B, t):
         lu.assert_within(out[n], ref[n], bound[n], n)
 
 
+@pytest.mark.parametrize("t", [7, 150, 400])
+def test_confident_rows_keep_their_gradient(B, t):
+    """Targets with 1 - p from 1e-3 to 1/2 at a long contraction.  dH of a row is (1 - p) a times a mean difference of rows of W, so an error
+    dz of the target's logit less lse is dz / (1 - p) of it.  dz: lse and its roundings, 4 half steps of numbers below 32, 4 x 2^-20;
+    the dot product, chains of at most 16 + 9 additions of partial sums below 32, 25 x 2^-20.  The other elements of G are as exact as
+    their logits, hidden x 2^-23 |h| |w| relative.  Two roundings to bf16."""
+    v, k = 300, 3584
+    g = torch.Generator().manual_seed(t)
+    w = (torch.randn(v, k, generator=g) * k ** -0.5).to(BF16)
+    y = torch.randint(0, v, (t,), generator=g)
+    h = (0.3 * torch.randn(t, k, generator=g) + (6.0 + 6.5 * torch.rand(t, 1, generator=g)) * w[y].float()).to(BF16)
+    a = torch.ones(t)
+    out = run_loss(B, h, w, y, a)
+    ref = lu.loss_reference(h, w, y, a)
+    left = 1 - torch.exp(-ref["loss"])
+    assert left.min() > 5e-4 and (left < 5e-3).any()
+    err = (out["d_hidden"].cpu().double() - ref["d_hidden"]).norm(dim=1) / ref["d_hidden"].norm(dim=1)
+    size = h.double().norm(dim=1) * w.double().norm(dim=1).max()
+    assert (err <= 2 * 2.0 ** -8 + 29 * 2.0 ** -20 / left + k * 2.0 ** -23 * size).all(), err.max()
+    if t <= 256:   # (G in two halves: its rounding to bf16 is gone)
+        assert (err <= 2.0 ** -8 + 29 * 2.0 ** -20 / left + k * 2.0 ** -23 * size).all(), err.max()
+
+
 def test_nan_in_one_scored_row_stays_in_it(B):
     t, v, k = 140, 400, 64
     h, w, y, a = lu.make_loss(t, v, k, seed=10)
