@@ -48,7 +48,7 @@ struct LmJob {
   int kind;
   int m_fixed;     // DW: rows of the piece; other kinds: 0 (M = the token rows)
   int n;           // columns: vocabulary columns of the piece (STATS, GRAD) or hidden (DH, DW)
-  int k_fixed;     // contraction length; 0 = the token rows (DW)
+  int k_fixed;     // contraction length; 0 = the token rows (DW).  Empty in any case when no row is scored
   int splits;      // shares of the contraction (DH), 1 otherwise
   int group;       // STATS, GRAD: row tiles that are taken over all columns before the next ones
 };
@@ -110,7 +110,8 @@ struct LmTile {
       kind = J.kind; cols = J.n; m_fixed = J.m_fixed;
       mt = ((J.m_fixed ? J.m_fixed : n_rows) + kLmTile - 1) / kLmTile;
       nt = (J.n + kLmTile - 1) / kLmTile;
-      kb = ((J.k_fixed ? J.k_fixed : n_rows) + 63) / 64;
+      // Without scored rows GRAD has no tiles and G is not written: nothing of it may be read, whatever length the host knows.
+      kb = n_rows == 0 ? 0 : ((J.k_fixed ? J.k_fixed : n_rows) + 63) / 64;
       const int count = mt * nt * J.splits;
       if (t < first + count) {
         int r = t - first;

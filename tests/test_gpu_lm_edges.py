@@ -1,0 +1,58 @@
+"""Vocabulary operators where they can go wrong at their edges: batches of which nothing is scored, forbidden words, very large
+logits, the border between G in one and in two halves, long contractions, matrices of more than 2^31 elements, refusals."""
+import numpy as np
+import pytest
+import torch
+
+from tests import lm_util as lu
+from tests.test_gpu_lm import B, guarded, run_loss, workspace  # noqa: F401  (B is a fixture)
+
+pytestmark = pytest.mark.gpu
+BF16, F32, F64 = torch.bfloat16, torch.float32, torch.float64
+
+
+@pytest.mark.parametrize("dw_dtype", [BF16, F32])
+@pytest.mark.parametrize("piece", [0, 1])                    # one piece of the vocabulary, three of them
+@pytest.mark.parametrize("t", [128, 129, 200, 256, 257])
+def test_no_row_scored_either_side_of_every_limit(B, t, piece, dw_dtype):
+    """Every row masked and full of NaN, scratch full of NaN: zeros everywhere, an accumulator that stays as it was."""
+    v, k = 700, 72
+    h = torch.full((t, k), float("nan"), dtype=BF16)
+    _, w, _, _ = lu.make_loss(1, v, k, seed=8)
+    y, a = torch.full((t,), -1), torch.full((t,), float("nan"))
+    out = run_loss(B, h, w, y, a, piece_bytes=piece, dw_dtype=dw_dtype)
+    for n, x in out.items():
+        assert (x == 0).all(), n
+    if dw_dtype == F32:
+        lm = B.LM(v, k, device=0, piece_bytes=piece)
+        acc = torch.full((v, k), 3.0, device="cuda")
+        lm.loss_bwd(h.cuda(), w.cuda(), y.cuda(), out["lse"], a.cuda(), None, acc, workspace(lm, t), accumulate=True)
+        assert (acc == 3).all()
+
+
+def test_no_row_scored_because_every_id_is_out_of_range(B):
+    t, v, k = 200, 300, 64
+    h, w, y, a = lu.make_loss(t, v, k, seed=14)
+    lm = B.LM(v, k, device=0)
+    ws, y = workspace(lm, t), (y + v).cuda()
+    loss, lse, dh, dw = (torch.full(s, float("nan"), device="cuda", dtype=d) for s, d in (((t,), F32), ((t,), F32), ((t, k), BF16), ((v, k), BF16)))
+    lm.loss_fwd(h.cuda(), w.cuda(), y, loss, lse, ws)
+    ws.fill_(0xFF)
+    lm.loss_bwd(h.cuda(), w.cuda(), y, lse, a.cuda(), dh, dw, ws)
+    assert lm.device_status()[0] == -1
+    for x in (loss, lse, dh, dw):
+        assert (x == 0).all()
+
+
+def test_no_row_scored_through_autograd(B):
+    """A wholly masked micro-batch of a training loop, its scratch where the allocator last held NaN."""
+    from paper_2609_33133_b200 import autograd as A
+    t, v, k = 200, 300, 64
+    h, w, _, _ = lu.make_loss(t, v, k, seed=15)
+    lm = B.LM(v, k, device=0)
+    hc, wc = h.cuda().requires_grad_(True), w.cuda().requires_grad_(True)
+    loss = A.lm_loss(lm, hc, wc, torch.full((t,), -100, device="cuda"))
+    stale = torch.full((lm.workspace_parts(t)[1],), 0xFF, device="cuda", dtype=torch.uint8)
+    del stale
+    loss.sum().backward()
+    assert (loss == 0).all() and (hc.grad == 0).all() and (wc.grad == 0).all()
