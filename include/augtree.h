@@ -481,7 +481,8 @@ int augtree_embed_bwd(const augtree_lm_t *lm, const void *d_out, int out_dtype, 
 
 /* Cross entropy of every token without its logits in memory:
  *   lse[t] = ln sum_v exp(logit_scale h_t . W_v),   loss[t] = lse[t] - logit_scale h_t . W_target     (fp32; zeros for padding)
- * hidden [n_tokens, hidden], weight [vocab, hidden]: bf16, 16-byte aligned.  -loss[t] is the token's log-probability. */
+ * hidden [n_tokens, hidden], weight [vocab, hidden]: bf16, 16-byte aligned.  -loss[t] is the token's log-probability.
+ * A logit of minus infinity has probability 0; as the target's it makes the loss infinite and leaves lse that of the others. */
 int augtree_lm_loss_fwd(const augtree_lm_t *lm, const void *hidden, const void *weight, const void *targets, int id_bytes,
                         int64_t n_tokens, float *loss, float *lse, void *ws, size_t ws_bytes, void *stream);
 

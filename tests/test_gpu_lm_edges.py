@@ -56,3 +56,39 @@ def test_no_row_scored_through_autograd(B):
     del stale
     loss.sum().backward()
     assert (loss == 0).all() and (hc.grad == 0).all() and (wc.grad == 0).all()
+
+
+@pytest.mark.parametrize("t", [6, 140, 300])
+@pytest.mark.parametrize("value", [float("-inf"), torch.finfo(BF16).min])
+def test_forbidden_words(B, t, value):
+    """Words that a column of the weight rules out, with minus infinity or with the type's lowest value (under a hidden state of one there):
+    nothing changes for the others, and a row whose target is one of them has the lse of the others and an infinite loss (or one of
+    3.4e38).  The gradient of the target's logit is then -a, as p is zero."""
+    v, k, out_of = 300, 64, 20
+    h, w, y, a = lu.make_loss(t, v - out_of, k, seed=16, push=4.0)
+    h[:, 0] = 1
+    w = torch.cat([w[:out_of], w])
+    w[:out_of, 0] = value
+    ref = lu.loss_reference(h, w[out_of:], y, a)
+    bound = lu.loss_bounds(ref, v, k, t)
+    y = y + out_of
+    y[1], y[4] = 7, 13
+    lost = torch.tensor([1, 4])
+    kept = torch.ones(t, dtype=torch.bool).index_fill_(0, lost, False)
+    out = run_loss(B, h, w, y, a)
+    lu.assert_within(out["lse"], ref["lse"], bound["lse"], "lse")
+    lu.assert_within(out["loss"].cpu()[kept], ref["loss"][kept], bound["loss"][kept], "loss")
+    loss = out["loss"].cpu()[lost]
+    if value == float("-inf"):
+        assert (loss == float("inf")).all(), loss
+    else:     # (lse - value, one product and a rounding or two)
+        assert (loss.double() / -value - 1).abs().max() <= 2.0 ** -22, loss
+    # dW: relative to the magnitudes the bound of the unrestricted words has, at these rows' own p
+    x = h.double() @ w[out_of:].double().T
+    p = torch.exp(x - torch.logsumexp(x, 1, keepdim=True))
+    hot = torch.nn.functional.one_hot(y, v).double()
+    p = torch.cat([torch.zeros(t, out_of, dtype=F64), p], 1)
+    want = (a.double()[:, None] * (p - hot)).T @ h.double()
+    mag = (a.double().abs()[:, None] * (p + hot)).T @ h.double().abs()
+    p_err = 2 * (k + 2) * 2.0 ** -23 * ref["reach"] + 2.0 ** -15      # logit and lse; exp2, sums and their roundings
+    lu.assert_within(out["d_weight"], want, (2.0 ** -7 + p_err) * mag + 2.0 ** -100, "d_weight")
