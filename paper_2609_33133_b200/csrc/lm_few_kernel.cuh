@@ -264,7 +264,7 @@ lm_few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ 
 #pragma unroll
           for (int j = 0; j < W; ++j) {
             if (exists && s_target[g * W + j] == v) p.tlogit[g * W + j] = x[j];
-            x[j] = a[j] = exists ? x[j] * p.scale_log2 : -INFINITY;
+            x[j] = a[j] = exists ? __fmul_rn(x[j], p.scale_log2) : -INFINITY;  // (write_loss counts on this rounding)
           }
           const float top = reduce_columns(a, lane, [](float s, float t) { return fmaxf(s, t); });
           const float mn = fmaxf(m[g], top), ref = mn == -INFINITY ? 0.f : mn;

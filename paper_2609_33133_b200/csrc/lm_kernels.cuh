@@ -197,13 +197,14 @@ __device__ __forceinline__ float2 merge_stats(float2 a, float2 b) {
 }
 
 // Loss and lse of a row from its merged (m, l).  The target's term of the sum is 2^(t2 - m) with t2 = c log2(e) tlogit as the
-// tile kernels rounded it; d is what t2 lacks of the exact x_target, and puts the term right.  The loss is taken as
+// tile kernels rounded it (__fmul_rn there and here: a product left to be fused into the subtraction of m would not be that number);
+// d is what t2 lacks of the exact x_target, and puts the term right.  The loss is taken as
 // log of the sum relative to the target's term, so that a small loss is not the difference of two large numbers.
 // A target that is ruled out (a logit of minus infinity, or one so low that base 2 makes it that) has no term in the sum and nothing
 // to put right: the lse is that of the others.  (A logit of plus infinity leaves NaN in the sum, and so in both.)
 __device__ __forceinline__ void write_loss(float2 s, float tlogit, float x_target, float logit_scale, float *loss, float *lse) {
   constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-  const float c = logit_scale * kLog2e, t2 = tlogit * c;
+  const float c = logit_scale * kLog2e, t2 = __fmul_rn(tlogit, c);
   const float d = fmaf(tlogit, c, -t2) + (x_target - tlogit) * c;
   if (!isfinite(d)) {
     const float v = s.x * kLn2 + logf(s.y);

@@ -333,7 +333,7 @@ lm_tile_kernel(const __grid_constant__ CUtensorMap tm_h, const __grid_constant__
           float cm = -INFINITY;
 #pragma unroll
           for (int e = 0; e < 32; ++e) {
-            const float x = e < left ? __uint_as_float(v[e]) * p.scale_log2 : -INFINITY;
+            const float x = e < left ? __fmul_rn(__uint_as_float(v[e]), p.scale_log2) : -INFINITY;  // (write_loss counts on this rounding)
             v[e] = __float_as_uint(x);
             cm = fmaxf(cm, x);
           }

@@ -92,3 +92,21 @@ def test_forbidden_words(B, t, value):
     mag = (a.double().abs()[:, None] * (p + hot)).T @ h.double().abs()
     p_err = 2 * (k + 2) * 2.0 ** -23 * ref["reach"] + 2.0 ** -15      # logit and lse; exp2, sums and their roundings
     lu.assert_within(out["d_weight"], want, (2.0 ** -7 + p_err) * mag + 2.0 ** -100, "d_weight")
+
+
+@pytest.mark.parametrize("t", [5, 140, 300])
+@pytest.mark.parametrize("scale", [1.0, 0.7])
+def test_loss_of_certain_targets_with_large_logits(B, t, scale):
+    """Targets ahead of every other word by more than 200: the loss is zero, exp(-200) aside.  The target is the row's maximum, so the sum
+    is 1, and with d the difference of the exact and the tensor core's logit the loss is log(1 + expm1(d)) - d, whatever d is: one
+    rounding of the sum, 2^-24 (1 + |d|), and eight of numbers as large as d, which is at most (hidden + 2) 2^-23 |h| |w| < 0.1.  Together
+    under 4 x 2^-24.  (A logit near 2000 has a half step of 6e-5: nothing of that may be left in the result.)"""
+    v, k = 300, 256
+    g = torch.Generator().manual_seed(t)
+    w = (torch.randn(v, k, generator=g) * k ** -0.5).to(BF16)
+    y = torch.randint(0, v, (t,), generator=g)
+    h = ((1000 + 1000 * torch.rand(t, 1, generator=g)) * w[y].float()).to(BF16)
+    ref = lu.loss_reference(h, w, y, torch.ones(t), scale)
+    assert ref["loss"].max() < 1e-80 and (k + 2) * 2.0 ** -23 * ref["reach"] < 0.1
+    out = run_loss(B, h, w, y, torch.ones(t), scale)
+    assert out["loss"].abs().max().item() <= 2.0 ** -22, out["loss"].abs().max().item()
