@@ -454,7 +454,7 @@ typedef struct {
   float embed_scale;           /* out = embed_scale * table[id]; 0 => 1                              */
   float logit_scale;           /* logits = logit_scale * (h . W): an inverse temperature; 0 => 1     */
   uint32_t flags;              /* AUGTREE_FLAG_TEST_SHORT_WAIT, AUGTREE_FLAG_TEST_SKIP_FWD_LOAD      */
-  int32_t n_lanes;             /* persistent CTAs; 0 => SM count of device                           */
+  int32_t n_lanes;             /* persistent CTAs; 0 => SM count of device; at most 2^20             */
   int64_t piece_bytes;         /* bound on the scratch that holds a piece of the logit gradient in the backward
                                   pass (bf16, rows x piece of the vocabulary); 0 => 512 MiB, more if that were
                                   under 4096 columns                                                 */

@@ -28,6 +28,7 @@ namespace {
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 constexpr int64_t kMaxTokens = (1ll << 31) - 4096;
+constexpr int kMaxLanes = 1 << 20;   // as a plan's: grids are at most 32 times that
 
 int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
@@ -426,7 +427,7 @@ int augtree_lm_create(const augtree_lm_desc_t *desc, int device, augtree_lm_t **
   if (!desc || desc->struct_size != sizeof(augtree_lm_desc_t) || desc->version != AUGTREE_VERSION) return AUGTREE_ERR_INVALID_ARG;
   if (desc->vocab < 1 || desc->hidden < 1 || desc->n_lanes < 0 || desc->piece_bytes < 0) return AUGTREE_ERR_INVALID_ARG;
   if (!(desc->embed_scale - desc->embed_scale == 0.f) || !(desc->logit_scale - desc->logit_scale == 0.f)) return AUGTREE_ERR_INVALID_ARG;
-  if (desc->hidden % 8 != 0 || desc->hidden > (1 << 20) || desc->vocab > (1 << 27)) return AUGTREE_ERR_UNSUPPORTED;
+  if (desc->hidden % 8 != 0 || desc->hidden > (1 << 20) || desc->vocab > (1 << 27) || desc->n_lanes > kMaxLanes) return AUGTREE_ERR_UNSUPPORTED;
   if (device < 0 && desc->n_lanes < 1) return AUGTREE_ERR_INVALID_ARG;
   augtree_lm *lm = new (std::nothrow) augtree_lm();
   if (!lm) return AUGTREE_ERR_INTERNAL;

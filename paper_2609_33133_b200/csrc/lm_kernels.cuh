@@ -116,10 +116,10 @@ lm_gather_kernel(const uint4 *hidden, const LmRows rows, uint4 *out, int row_vec
   wait_previous();
   __shared__ float sh[8];
   const int n = *rows.n_rows, n_pad = (n + 255) / 256 * 256;
-  for (int r = blockIdx.x; r < n_pad; r += gridDim.x) {
+  for (long long r = blockIdx.x; r < n_pad; r += gridDim.x) {   // (64 bits, here and below: a step past the last row passes 2^31)
     const uint4 *src = r < n ? hidden + (long long)rows.idx[r] * row_vecs : nullptr;
     const uint4 *wt = src ? weight + (long long)rows.target[r] * row_vecs : nullptr;
-    uint4 *dst = out + (long long)r * out_vecs;
+    uint4 *dst = out + r * out_vecs;
     float s = 0.f;
     for (int i = threadIdx.x; i < out_vecs; i += 256) {
       const uint4 v = src && i < row_vecs ? src[i] : make_uint4(0, 0, 0, 0);
@@ -258,8 +258,8 @@ lm_finish_kernel(const float2 *part, int n_part, long long rows_pad, const LmRow
   __shared__ float2 sh[32][33];
   const int lane = threadIdx.x & 31, seg = threadIdx.x >> 5;
   const int n = *rows.n_rows;
-  for (int r0 = blockIdx.x * 32; r0 < n; r0 += gridDim.x * 32) {
-    const int r = r0 + lane;
+  for (long long r0 = blockIdx.x * 32ll; r0 < n; r0 += gridDim.x * 32ll) {
+    const long long r = r0 + lane;
     float2 v = make_float2(-INFINITY, 0.f);
     if (r < n)
       for (int i = seg; i < n_part; i += 128) {
@@ -289,7 +289,7 @@ lm_dh_kernel(const float *part, int splits, long long rows_pad, int hidden, cons
   launch_next();
   wait_previous();
   const int vecs = hidden / 8;
-  for (int t = blockIdx.x; t < tokens; t += gridDim.x) {
+  for (long long t = blockIdx.x; t < tokens; t += gridDim.x) {
     const int r = pos[t];
     for (int i = threadIdx.x; i < vecs; i += 256) {
       float x[8] = {};
@@ -299,7 +299,7 @@ lm_dh_kernel(const float *part, int splits, long long rows_pad, int hidden, cons
           const float4 a = q[0], b = q[1];
           x[0] += a.x; x[1] += a.y; x[2] += a.z; x[3] += a.w; x[4] += b.x; x[5] += b.y; x[6] += b.z; x[7] += b.w;
         }
-      *reinterpret_cast<uint4 *>(d_hidden + (long long)t * hidden + i * 8) =
+      *reinterpret_cast<uint4 *>(d_hidden + t * hidden + i * 8) =
           make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
     }
   }
@@ -359,10 +359,10 @@ __global__ void __launch_bounds__(128)
 embed_fwd_kernel(const In *table, const Id *ids, int tokens, int vocab, int hidden, float scale, Out *out, int *status) {
   launch_next();
   wait_previous();
-  for (int t = blockIdx.x; t < tokens; t += gridDim.x) {
+  for (long long t = blockIdx.x; t < tokens; t += gridDim.x) {
     const long long id = ids[t];
     const bool live = id >= 0 && id < vocab;
-    if (threadIdx.x == 0) check_id(id, t, vocab, status);
+    if (threadIdx.x == 0) check_id(id, (int)t, vocab, status);
     for (int i = threadIdx.x * 8; i < hidden; i += 1024) {
       float x[8] = {};
       if (live) {
@@ -370,7 +370,7 @@ embed_fwd_kernel(const In *table, const Id *ids, int tokens, int vocab, int hidd
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] *= scale;
       }
-      Vec<Out>::store(out + (long long)t * hidden + i, x);
+      Vec<Out>::store(out + t * hidden + i, x);
     }
   }
 }

@@ -110,3 +110,26 @@ def test_loss_of_certain_targets_with_large_logits(B, t, scale):
     assert ref["loss"].max() < 1e-80 and (k + 2) * 2.0 ** -23 * ref["reach"] < 0.1
     out = run_loss(B, h, w, y, torch.ones(t), scale)
     assert out["loss"].abs().max().item() <= 2.0 ** -22, out["loss"].abs().max().item()
+
+
+def test_lookup_of_as_many_tokens_as_there_can_be(B):
+    """2^31 - 4096 tokens of eight columns: the last step of a block's walk over them ends beyond 2^31."""
+    t, v, k = (1 << 31) - 4096, 4, 8
+    if torch.cuda.mem_get_info()[0] < 60 << 30:
+        pytest.skip("needs 43 GB of device memory")
+    lm = B.LM(v, k, device=0)
+    table = (torch.arange(v * k, device="cuda").view(v, k) + 1).to(BF16)
+    ids = torch.empty(t, device="cuda", dtype=torch.int32)
+    step = 1 << 27
+    for b in range(0, t, step):                                  # -1, 0, 1, 2, 3, -1, ..
+        n = min(step, t - b)
+        ids[b:b + n] = torch.arange(b, b + n, device="cuda").remainder_(5).sub_(1)
+    out = torch.full((t, k), float("nan"), device="cuda", dtype=BF16)
+    lm.embed_fwd(table, ids, out)
+    padded = torch.cat([torch.zeros(1, k, device="cuda", dtype=BF16), table])
+    for b in range(0, t, step):
+        n = min(step, t - b)
+        assert torch.equal(out[b:b + n], padded[ids[b:b + n].long() + 1]), b
+    assert lm.device_status() == (0, 0)
+    del ids, out
+    torch.cuda.empty_cache()

@@ -70,3 +70,12 @@ def test_workspace_for_more_tokens_is_enough_for_fewer(B, vocab, hidden, lanes, 
         now = lm.workspace_parts(n)
         assert all(a >= b for a, b in zip(now, last)), (n, now, last)
         last = now
+
+
+def test_no_more_lanes_than_index_arithmetic_holds(B):
+    """Grids are multiples of the lanes (32 of them for the lookup), and a partial sum is kept for each: a plan's limit holds here too."""
+    assert B.LM(500, 64, device=None, n_lanes=1 << 20).workspace_bytes(100) > 0
+    for lanes in ((1 << 20) + 1, (1 << 31) - 1):
+        with pytest.raises(B.AugtreeError) as e:
+            B.LM(500, 64, device=None, n_lanes=lanes)
+        assert e.value.code == -2
