@@ -32,6 +32,13 @@ constexpr int kMaxLanes = 1 << 20;   // as a plan's: grids are at most 32 times 
 
 int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
+// A failed runtime call is reported by the return value and not left in the runtime's last error as well, where the attention's
+// entry points, which look at it behind their launches, would find it and report a failure of their own.
+int cuda_failed() {
+  cudaGetLastError();
+  return AUGTREE_ERR_CUDA;
+}
+
 // Scratch of one call, cut from the caller's block: every part starts on 256 bytes.
 struct Cursor {
   uint8_t *base;
@@ -229,7 +236,7 @@ int map_out(CUtensorMap *m, const void *ptr, int64_t rows, int64_t cols, bool f3
 int check_lm(const augtree_lm *lm) {
   if (!lm || lm->device < 0) return AUGTREE_ERR_INVALID_ARG;
   int cur = -1;
-  if (cudaGetDevice(&cur) != cudaSuccess) return AUGTREE_ERR_CUDA;
+  if (cudaGetDevice(&cur) != cudaSuccess) return cuda_failed();
   return cur == lm->device ? AUGTREE_OK : AUGTREE_ERR_INVALID_ARG;
 }
 
@@ -244,9 +251,7 @@ int launch(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream
   attr.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &attr; cfg.numAttrs = 1;
   ++g_launches;
-  if (cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...) == cudaSuccess) return AUGTREE_OK;
-  cudaGetLastError();  // reported by the return value; not left for the caller's next check
-  return AUGTREE_ERR_CUDA;
+  return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...) == cudaSuccess ? AUGTREE_OK : cuda_failed();
 }
 
 // Scored rows packed into the scratch, and their targets' logits (forward: lse null) or gradients.
@@ -454,7 +459,11 @@ int augtree_lm_create(const augtree_lm_desc_t *desc, int device, augtree_lm_t **
     if (!r && (cudaMalloc(&lm->d_status, 2 * sizeof(int)) != cudaSuccess || cudaMemset(lm->d_status, 0, 2 * sizeof(int)) != cudaSuccess)) r = AUGTREE_ERR_CUDA;
     cudaSetDevice(prev);
   }
-  if (r) { augtree_lm_destroy(lm); return r; }
+  if (r) {
+    augtree_lm_destroy(lm);
+    if (r == AUGTREE_ERR_CUDA) cuda_failed();
+    return r;
+  }
   *out = lm;
   return AUGTREE_OK;
 }
@@ -572,7 +581,7 @@ int augtree_lm_loss_bwd(const augtree_lm_t *lm, const void *hidden, const void *
   if (n_tokens == 0) {
     if (d_weight && !accumulate &&
         cudaMemsetAsync(d_weight, 0, (size_t)lm->vocab * lm->hidden * (weight_dtype == AUGTREE_F32 ? 4 : 2), st) != cudaSuccess)
-      return AUGTREE_ERR_CUDA;
+      return cuda_failed();
     return AUGTREE_OK;
   }
   if (!hidden || !weight || !targets || !lse || !d_loss || !aligned16(hidden) || !aligned16(weight)) return AUGTREE_ERR_INVALID_ARG;
@@ -639,7 +648,7 @@ int augtree_lm_last_device_status(const augtree_lm_t *lm, int *status, int *deta
   if (e == cudaSuccess) e = cudaMemcpy(h, lm->d_status, sizeof(h), cudaMemcpyDeviceToHost);
   if (e == cudaSuccess && (h[0] || h[1])) e = cudaMemset(lm->d_status, 0, sizeof(h));
   cudaSetDevice(prev);
-  if (e != cudaSuccess) return AUGTREE_ERR_CUDA;
+  if (e != cudaSuccess) return cuda_failed();
   *status = h[0];
   if (detail) *detail = h[1];
   return AUGTREE_OK;

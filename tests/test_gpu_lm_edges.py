@@ -133,3 +133,20 @@ def test_lookup_of_as_many_tokens_as_there_can_be(B):
     assert lm.device_status() == (0, 0)
     del ids, out
     torch.cuda.empty_cache()
+
+
+def test_a_handle_that_cannot_be_made_leaves_no_error_behind(B):
+    """The failure is the return value's: a call on another handle or plan that follows does not report it again."""
+    from paper_2609_33133_b200 import autograd as A
+    plan, lm = B.Plan([130], [[64, 33]], 4, 2, 64, device=0), B.LM(100, 64, device=0)
+    g = torch.Generator().manual_seed(17)
+    x = [torch.randn(n, h, 64, generator=g).to(BF16).cuda() for n, h in ((130, 4), (130, 2), (130, 2), (97, 4), (97, 2), (97, 2))]
+    want = A.tree_attention(plan, *x)
+    with pytest.raises(B.AugtreeError) as e:
+        B.LM(100, 64, device=torch.cuda.device_count() + 7)
+    assert e.value.code == -4
+    got = A.tree_attention(plan, *x)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    table, out = torch.ones(100, 64, device="cuda"), torch.zeros(3, 64, device="cuda")
+    lm.embed_fwd(table, torch.arange(3, device="cuda"), out)
+    assert (out == 1).all() and lm.device_status() == (0, 0) and plan.device_status() == (0, 0)
