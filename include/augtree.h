@@ -439,7 +439,8 @@ int augtree_plan_tree(const augtree_tree_t *tree, const augtree_profile_t *profi
  * A handle holds the sizes, the scales and a status word; it does not depend on the number of tokens, so one handle
  * serves a whole run, from single tokens to whole micro-batches.  It is immutable after creation and belongs to a
  * device exactly as a plan does (same rule for the current device, streams and concurrent calls: each call that may
- * overlap another needs a workspace of its own).  Token ids are int64 or int32 (id_bytes 8 or 4) device arrays.
+ * overlap another needs a workspace of its own).  Token ids are int64 or int32 (id_bytes 8 or 4) device arrays; they and the
+ * fp32 arrays of a number per token start on a multiple of their element's size (AUGTREE_ERR_INVALID_ARG otherwise).
  *   id < 0       padding: a zero row of the embedding, a row that is not scored; whatever its hidden state holds (NaN
  *                included) enters no result, and its work is saved
  *   id >= vocab  is treated like padding, and AUGTREE_ERR_INVALID_ARG with the position of the token as detail is

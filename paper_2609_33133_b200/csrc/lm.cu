@@ -26,7 +26,8 @@ struct augtree_lm {
 
 namespace {
 
-bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+bool aligned(const void *p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) == 0; }
+bool aligned16(const void *p) { return aligned(p, 16); }
 constexpr int64_t kMaxTokens = (1ll << 31) - 4096;
 constexpr int kMaxLanes = 1 << 20;   // as a plan's: grids are at most 32 times that
 
@@ -499,7 +500,7 @@ int augtree_embed_fwd(const augtree_lm_t *lm, const void *table, int table_dtype
   if (n_tokens < 0 || (id_bytes != 4 && id_bytes != 8) || !dtype_ok(table_dtype) || !dtype_ok(out_dtype)) return AUGTREE_ERR_INVALID_ARG;
   if (n_tokens > kMaxTokens) return AUGTREE_ERR_UNSUPPORTED;
   if (n_tokens == 0) return AUGTREE_OK;
-  if (!table || !ids || !out || !aligned16(table) || !aligned16(out)) return AUGTREE_ERR_INVALID_ARG;
+  if (!table || !ids || !out || !aligned16(table) || !aligned16(out) || !aligned(ids, id_bytes)) return AUGTREE_ERR_INVALID_ARG;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   return id_bytes == 8 ? embed_fwd_in<long long>(lm, table, table_dtype, ids, (int)n_tokens, out, out_dtype, st)
                        : embed_fwd_in<int>(lm, table, table_dtype, ids, (int)n_tokens, out, out_dtype, st);
@@ -511,7 +512,7 @@ int augtree_embed_bwd(const augtree_lm_t *lm, const void *d_out, int out_dtype, 
   if (r) return r;
   if (n_tokens < 0 || (id_bytes != 4 && id_bytes != 8) || !dtype_ok(table_dtype) || !dtype_ok(out_dtype)) return AUGTREE_ERR_INVALID_ARG;
   if (n_tokens > kMaxTokens || (accumulate && table_dtype != AUGTREE_F32)) return AUGTREE_ERR_UNSUPPORTED;
-  if (!d_table || !aligned16(d_table) || (n_tokens > 0 && (!d_out || !ids || !aligned16(d_out)))) return AUGTREE_ERR_INVALID_ARG;
+  if (!d_table || !aligned16(d_table) || (n_tokens > 0 && (!d_out || !ids || !aligned16(d_out) || !aligned(ids, id_bytes)))) return AUGTREE_ERR_INVALID_ARG;
   EmbedWs w;
   if (!ws || !aligned16(ws) || ws_bytes < embed_layout(lm, n_tokens, static_cast<uint8_t *>(ws), &w)) return AUGTREE_ERR_WORKSPACE;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -538,6 +539,7 @@ int augtree_lm_loss_fwd(const augtree_lm_t *lm, const void *hidden, const void *
   if (n_tokens > kMaxTokens) return AUGTREE_ERR_UNSUPPORTED;
   if (n_tokens == 0) return AUGTREE_OK;
   if (!hidden || !weight || !targets || !loss || !lse || !aligned16(hidden) || !aligned16(weight)) return AUGTREE_ERR_INVALID_ARG;
+  if (!aligned(targets, id_bytes) || !aligned(loss, 4) || !aligned(lse, 4)) return AUGTREE_ERR_INVALID_ARG;
   LossWs w;
   if (!ws || !aligned16(ws) || ws_bytes < loss_layout(lm, n_tokens, false, static_cast<uint8_t *>(ws), &w)) return AUGTREE_ERR_WORKSPACE;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -585,6 +587,7 @@ int augtree_lm_loss_bwd(const augtree_lm_t *lm, const void *hidden, const void *
     return AUGTREE_OK;
   }
   if (!hidden || !weight || !targets || !lse || !d_loss || !aligned16(hidden) || !aligned16(weight)) return AUGTREE_ERR_INVALID_ARG;
+  if (!aligned(targets, id_bytes) || !aligned(lse, 4) || !aligned(d_loss, 4)) return AUGTREE_ERR_INVALID_ARG;
   LossWs w;
   if (!ws || !aligned16(ws) || ws_bytes < loss_layout(lm, n_tokens, true, static_cast<uint8_t *>(ws), &w)) return AUGTREE_ERR_WORKSPACE;
   if (!d_hidden && !d_weight) return AUGTREE_OK;

@@ -150,3 +150,31 @@ def test_a_handle_that_cannot_be_made_leaves_no_error_behind(B):
     table, out = torch.ones(100, 64, device="cuda"), torch.zeros(3, 64, device="cuda")
     lm.embed_fwd(table, torch.arange(3, device="cuda"), out)
     assert (out == 1).all() and lm.device_status() == (0, 0) and plan.device_status() == (0, 0)
+
+
+def test_arrays_of_a_number_per_token_off_their_elements_boundaries_are_refused(B):
+    """Through the C interface (torch makes no such tensor): refused before anything is launched or written."""
+    t, v, k = 10, 100, 64
+    lm = B.LM(v, k, device=0)
+    h, w, y, a = (x.cuda() for x in lu.make_loss(t, v, k, seed=18))
+    f, dh, dw, ws = torch.full((t + 1,), 7.0, device="cuda"), torch.full_like(h, 7), torch.full_like(w, 7), workspace(lm, t)
+    p = lambda x: x.data_ptr()
+    st = torch.cuda.current_stream().cuda_stream
+    fwd = dict(targets=p(y), id_bytes=8, loss=p(f), lse=p(f))
+    bwd = dict(targets=p(y), id_bytes=8, lse=p(f), d_loss=p(a))
+    for name, off in (("targets", 4), ("targets", 1), ("loss", 2), ("lse", 1)):
+        q = {**fwd, name: fwd[name] + off}
+        assert B.lib.augtree_lm_loss_fwd(lm._h, p(h), p(w), q["targets"], q["id_bytes"], t - 1, q["loss"], q["lse"], p(ws), ws.nbytes, st) == -1
+    for name, off in (("targets", 4), ("lse", 2), ("d_loss", 1)):
+        q = {**bwd, name: bwd[name] + off}
+        assert B.lib.augtree_lm_loss_bwd(lm._h, p(h), p(w), q["targets"], q["id_bytes"], q["lse"], q["d_loss"], t - 1, p(dh), p(dw), 0, 0,
+                                         p(ws), ws.nbytes, st) == -1
+    for off, id_bytes in ((4, 8), (2, 4), (1, 8)):
+        assert B.lib.augtree_embed_fwd(lm._h, p(w), 0, p(y) + off, id_bytes, t - 1, p(dh), 0, st) == -1
+        assert B.lib.augtree_embed_bwd(lm._h, p(h), 0, p(y) + off, id_bytes, t - 1, p(dw), 0, 0, p(ws), ws.nbytes, st) == -1
+    torch.cuda.synchronize()
+    assert (f == 7).all() and (dh == 7).all() and (dw == 7).all() and lm.device_status() == (0, 0)
+    # int32 ids on a boundary of four bytes are in order
+    y4 = torch.cat([torch.zeros(1, device="cuda", dtype=torch.int32), y.int()])[1:]
+    lm.embed_fwd(w, y4, dh)
+    assert torch.equal(dh, w[y])
