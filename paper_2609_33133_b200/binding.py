@@ -8,6 +8,7 @@ run `python -m paper_2609_33133_b200.build`.
 from __future__ import annotations
 
 import ctypes as C
+import operator
 import os
 
 import numpy as np
@@ -279,6 +280,14 @@ _ID_BYTES = {torch.int64: 8, torch.int32: 4}
 _BF16, _F32 = (torch.bfloat16,), (torch.float32,)
 
 
+def _fits(name, x, bits, signed=True):
+    """ctypes cuts a number off at its field's width without a word."""
+    x = operator.index(x)
+    if not (-(1 << bits - 1) <= x < 1 << bits - 1 if signed else 0 <= x < 1 << bits):
+        raise ValueError(f"{name}: {x} does not fit {bits} bits")
+    return x
+
+
 class LM:
     """Owns an augtree_lm_t: the embedding lookup and the vocabulary cross entropy of a [vocab, hidden] matrix, with their
     gradients.  device=None builds a host-only handle (workspace queries only).  Every method checks its tensors, launches on
@@ -286,7 +295,10 @@ class LM:
 
     def __init__(self, vocab, hidden, *, device=0, embed_scale=0.0, logit_scale=0.0, flags=0, n_lanes=0, piece_bytes=0):
         self.vocab, self.hidden, self.device = int(vocab), int(hidden), device
-        d = LmDescC(C.sizeof(LmDescC), 1, vocab, hidden, embed_scale, logit_scale, flags, n_lanes, piece_bytes)
+        if any(x and not C.c_float(x).value for x in (embed_scale, logit_scale)):   # (zero stands for one there)
+            raise ValueError(f"embed_scale {embed_scale}, logit_scale {logit_scale}: too small for fp32")
+        d = LmDescC(C.sizeof(LmDescC), 1, _fits("vocab", vocab, 32), _fits("hidden", hidden, 32), embed_scale, logit_scale,
+                    _fits("flags", flags, 32, signed=False), _fits("n_lanes", n_lanes, 32), _fits("piece_bytes", piece_bytes, 64))
         self._h = C.c_void_p()
         _check(lib.augtree_lm_create(C.byref(d), -1 if device is None else int(device), C.byref(self._h)), "lm_create")
 
@@ -299,7 +311,7 @@ class LM:
     def workspace_parts(self, n_tokens):
         """Scratch bytes of (loss_fwd, loss_bwd, embed_bwd) for n_tokens tokens."""
         f, b, e = _sz(), _sz(), _sz()
-        _check(lib.augtree_lm_workspace_bytes(self._h, int(n_tokens), C.byref(f), C.byref(b), C.byref(e)), "lm_workspace_bytes")
+        _check(lib.augtree_lm_workspace_bytes(self._h, _fits("n_tokens", int(n_tokens), 64), C.byref(f), C.byref(b), C.byref(e)), "lm_workspace_bytes")
         return f.value, b.value, e.value
 
     def workspace_bytes(self, n_tokens) -> int:

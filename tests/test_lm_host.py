@@ -79,3 +79,19 @@ def test_no_more_lanes_than_index_arithmetic_holds(B):
         with pytest.raises(B.AugtreeError) as e:
             B.LM(500, 64, device=None, n_lanes=lanes)
         assert e.value.code == -2
+
+
+@pytest.mark.parametrize("kw", [dict(vocab=(1 << 32) + 503), dict(hidden=(1 << 32) + 64), dict(n_lanes=(1 << 32) + 1), dict(vocab=-(1 << 32) + 503),
+                                dict(piece_bytes=(1 << 64) + 1), dict(flags=1 << 32), dict(flags=-1),
+                                dict(embed_scale=1e-50), dict(logit_scale=-1e-50)])
+def test_numbers_beyond_the_descriptors_fields_are_refused(B, kw):
+    """A field of 32 or 64 bits takes what fits of a number: a handle of other sizes than those that were asked for."""
+    with pytest.raises(ValueError):
+        B.LM(**{"vocab": 503, "hidden": 64, "device": None, "n_lanes": 148, **kw})
+
+
+def test_token_counts_beyond_the_interface_are_refused(B):
+    lm = B.LM(503, 64, device=None, n_lanes=148)
+    for n in ((1 << 64) + 5, -(1 << 64) + 5):
+        with pytest.raises(ValueError):
+            lm.workspace_parts(n)
