@@ -79,3 +79,24 @@ def assert_within(got, ref, bound, name=""):
     assert torch.isfinite(got).all(), (name, "not finite")
     over = (got - ref).abs() - bound
     assert not got.numel() or over.max().item() <= 0, (name, over.max().item(), (got - ref).abs().max().item())
+
+
+def gradient_bounds_two_halves(ref, vocab, hidden, tokens):
+    """Bounds of dH and dW before they are delivered, for up to 256 rows: as in loss_bounds, but G is hi + lo with hi = bf16(G) and
+    lo = bf16(G - hi), which leaves 2^-8 of 2^-8 of an element, and the contractions run over both halves, twice as many additions."""
+    u, low = 2.0 ** -23, 2.0 ** -126
+    x = (hidden + 2) * u * ref["reach"]
+    lse = x + (4 + 128 + vocab / 512) * u + 3 * u * (ref["lse"].abs().max().item() + ref["reach"])
+    p = x + lse + 4 * u + 3 * u * ref["reach"]
+    return {"d_hidden": 2 ** -16 * ref["g_dh"] + (p + 2 * vocab * u) * 1.01 * ref["m_dh"] + low * (ref["low_dh"] + 2 * vocab + 2),
+            "d_weight": 2 ** -16 * ref["g_dw"] + (p + 2 * tokens * u) * 1.01 * ref["m_dw"] + low * (ref["low_dw"] + 2 * tokens + 2)}
+
+
+def half_step_bf16(x):
+    """Half the distance of neighbouring bf16 numbers at x: 2^(e - 9) for |x| = m 2^e with m in [1/2, 1)."""
+    return torch.exp2((torch.frexp(x.to(F64).abs())[1] - 9).to(F64))
+
+
+def delivered_bf16(ref, bound):
+    """Bound of a result that is within `bound` of ref before it is rounded to bf16."""
+    return bound + half_step_bf16(ref.abs() + bound)

@@ -178,3 +178,19 @@ def test_arrays_of_a_number_per_token_off_their_elements_boundaries_are_refused(
     y4 = torch.cat([torch.zeros(1, device="cuda", dtype=torch.int32), y.int()])[1:]
     lm.embed_fwd(w, y4, dh)
     assert torch.equal(dh, w[y])
+
+
+@pytest.mark.parametrize("t", [3, 128, 129, 256])
+def test_gradients_of_few_rows_carry_no_rounding_of_the_logit_gradient(B, t):
+    """Up to 256 rows G has two halves; both gradients to within their sums' errors and their own delivery.  (With hi alone they are out of
+    these bounds: tests/test_lm_host.py.)"""
+    v, k = 257, 64
+    h, w, y, a = lu.make_loss(t, v, k, seed=t, push=4.0)
+    ref = lu.loss_reference(h, w, y, a)
+    bound = lu.gradient_bounds_two_halves(ref, v, k, t)
+    for piece in (0, 1):
+        out = run_loss(B, h, w, y, a, dw_dtype=F32, piece_bytes=piece)
+        lu.assert_within(out["d_weight"], ref["d_weight"], bound["d_weight"] + 2.0 ** -24 * ref["d_weight"].abs(), "d_weight fp32")
+        lu.assert_within(out["d_hidden"], ref["d_hidden"], lu.delivered_bf16(ref["d_hidden"], bound["d_hidden"]), "d_hidden")
+        out = run_loss(B, h, w, y, a, piece_bytes=piece)
+        lu.assert_within(out["d_weight"], ref["d_weight"], lu.delivered_bf16(ref["d_weight"], bound["d_weight"]), "d_weight bf16")

@@ -2,6 +2,9 @@
 import ctypes as C
 
 import pytest
+import torch
+
+from tests import lm_util as lu
 
 
 @pytest.fixture(scope="module")
@@ -95,3 +98,24 @@ def test_token_counts_beyond_the_interface_are_refused(B):
     for n in ((1 << 64) + 5, -(1 << 64) + 5):
         with pytest.raises(ValueError):
             lm.workspace_parts(n)
+
+
+@pytest.mark.parametrize("t", [3, 128, 129, 256])
+def test_bounds_of_two_halves_see_a_missing_half(t):
+    """G rounded to bf16 once, in the plain form: outside the bounds that the kernels' two halves are held to; hi + lo is inside."""
+    v, k = 257, 64
+    h, w, y, a = lu.make_loss(t, v, k, seed=t, push=4.0)
+    ref = lu.loss_reference(h, w, y, a)
+    bound = lu.gradient_bounds_two_halves(ref, v, k, t)
+    hd, wd = h.double(), w.double()
+    x = hd @ wd.T
+    g = a.double()[:, None] * (torch.softmax(x, 1) - torch.nn.functional.one_hot(y, v))
+    hi = g.to(torch.bfloat16).double()
+    lo = (g - hi).to(torch.bfloat16).double()
+    bf = lambda z: z.to(torch.bfloat16).double()
+    for name, one, two in (("d_hidden", hi @ wd, (hi + lo) @ wd), ("d_weight", hi.T @ hd, (hi + lo).T @ hd)):
+        allowed = lu.delivered_bf16(ref[name], bound[name])
+        assert ((bf(two) - ref[name]).abs() <= allowed).all(), name
+        assert ((bf(one) - ref[name]).abs() > allowed).double().mean() > 0.02, name
+    assert ((hi.T @ hd - ref["d_weight"]).abs() > bound["d_weight"] + 2.0 ** -24 * ref["d_weight"].abs()).double().mean() > 0.2
+    assert ((hi + lo).T @ hd - ref["d_weight"]).abs().le(bound["d_weight"]).all()
