@@ -100,3 +100,16 @@ def half_step_bf16(x):
 def delivered_bf16(ref, bound):
     """Bound of a result that is within `bound` of ref before it is rounded to bf16."""
     return bound + half_step_bf16(ref.abs() + bound)
+
+
+LONG_CASES = [(40, 513, 65536), (600, 700, 33024)]   # a row of 128 KB; hidden states of more than a row group
+
+
+def make_long(tokens, vocab, hidden, seed):
+    """Long contractions whose bounds still see a wrong result: |h| |w| near one, so that hidden 2^-23 |h| |w| is under 1e-2, and losses
+    that differ by up to one from row to row."""
+    g = torch.Generator().manual_seed(seed)
+    w = (torch.randn(vocab, hidden, generator=g) * hidden ** -0.5).to(BF16)
+    y = torch.randint(0, vocab, (tokens,), generator=g)
+    h = (torch.randn(tokens, hidden, generator=g) * 0.3 * hidden ** -0.5 + torch.rand(tokens, 1, generator=g) * w[y].float()).to(BF16)
+    return h, w, y, torch.randn(tokens, generator=g)

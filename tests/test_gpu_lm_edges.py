@@ -194,3 +194,14 @@ def test_gradients_of_few_rows_carry_no_rounding_of_the_logit_gradient(B, t):
         lu.assert_within(out["d_hidden"], ref["d_hidden"], lu.delivered_bf16(ref["d_hidden"], bound["d_hidden"]), "d_hidden")
         out = run_loss(B, h, w, y, a, piece_bytes=piece)
         lu.assert_within(out["d_weight"], ref["d_weight"], lu.delivered_bf16(ref["d_weight"], bound["d_weight"]), "d_weight bf16")
+
+
+@pytest.mark.parametrize("t,v,k", lu.LONG_CASES)
+def test_long_contractions(B, t, v, k):
+    """(That these bounds see zeros, swapped rows and swapped tiles: tests/test_lm_host.py.)"""
+    h, w, y, a = lu.make_long(t, v, k, seed=t)
+    ref = lu.loss_reference(h, w, y, a)
+    bound = lu.loss_bounds(ref, v, k, t)
+    out = run_loss(B, h, w, y, a)
+    for n in ("lse", "loss", "d_hidden", "d_weight"):
+        lu.assert_within(out[n], ref[n], bound[n], n)

@@ -119,3 +119,23 @@ def test_bounds_of_two_halves_see_a_missing_half(t):
         assert ((bf(one) - ref[name]).abs() > allowed).double().mean() > 0.02, name
     assert ((hi.T @ hd - ref["d_weight"]).abs() > bound["d_weight"] + 2.0 ** -24 * ref["d_weight"].abs()).double().mean() > 0.2
     assert ((hi + lo).T @ hd - ref["d_weight"]).abs().le(bound["d_weight"]).all()
+
+
+@pytest.mark.parametrize("t,v,k", lu.LONG_CASES)
+def test_bounds_of_long_contractions_see_wrong_results(t, v, k):
+    h, w, y, a = lu.make_long(t, v, k, seed=t)
+    ref = lu.loss_reference(h, w, y, a)
+    bound = lu.loss_bounds(ref, v, k, t)
+    # (rows of dW without a target are all sum_t a_t h_t / vocab but for the spread of p: only the targets' rows tell where they stand)
+    rows = {"d_hidden": torch.arange(t), "d_weight": torch.unique(y), "loss": torch.arange(t), "lse": torch.arange(t)}
+    out = lambda name, x: ((x - ref[name]).abs() > bound[name])[rows[name]].double().mean()
+    for name in ("d_hidden", "d_weight"):
+        assert out(name, torch.zeros_like(ref[name])) > 0.9                                   # nothing written
+        assert out(name, ref[name].roll(1, 0)) > 0.9                                          # rows one off
+        assert out(name, torch.cat([ref[name][:, 256:], ref[name][:, :256]], 1)) > 0.9        # column tiles one off
+    assert out("d_weight", ref["d_weight"].roll(256, 0)) > 0.9                                # row tiles one off
+    if t > 256:
+        assert out("d_hidden", ref["d_hidden"].roll(256, 0)) > 0.9
+    for name in ("loss", "lse"):
+        assert out(name, torch.zeros_like(ref[name])) == 1
+    assert out("loss", ref["loss"].roll(1)) > 0.8
