@@ -139,3 +139,14 @@ def test_bounds_of_long_contractions_see_wrong_results(t, v, k):
     for name in ("loss", "lse"):
         assert out(name, torch.zeros_like(ref[name])) == 1
     assert out("loss", ref["loss"].roll(1)) > 0.8
+
+
+def test_workspace_follows_the_piece_bound_and_no_more(B):
+    """From a piece of one tile of columns (256, and 256 that equal pieces may be rounded up by) to one of 256 MiB: G grows by the bound less
+    a tile, 16 a row of everything else is as before."""
+    rows, mib = 4096, 1 << 20
+    small = B.LM(50000, 512, device=None, n_lanes=148, piece_bytes=1).workspace_parts(rows)[1]
+    large = B.LM(50000, 512, device=None, n_lanes=148, piece_bytes=256 * mib).workspace_parts(rows)[1]
+    assert 250 * mib < large - small <= 256 * mib
+    # the rest: packed hidden states, partial sums of dH (at most 16384 rows of them, or twice the rows), a few numbers a row
+    assert small <= rows * 512 * 2 + max(16384, 2 * rows) * 512 * 4 + rows * 512 * 2 + 64 * rows + (1 << 14)
