@@ -205,3 +205,69 @@ def test_long_contractions(B, t, v, k):
     out = run_loss(B, h, w, y, a)
     for n in ("lse", "loss", "d_hidden", "d_weight"):
         lu.assert_within(out[n], ref[n], bound[n], n)
+
+
+@pytest.mark.parametrize("t", [3, 130, 300])
+def test_matrices_of_more_than_2_31_elements(B, t):
+    """600064 x 3584, 2.15e9 elements: ids, targets and rows of the gradients on both sides of element 2^31."""
+    v, k = 600064, 3584
+    assert v * k > 1 << 31
+    if torch.cuda.mem_get_info()[0] < 50 << 30:
+        pytest.skip("needs 40 GB of device memory")
+    g = torch.Generator(device="cuda").manual_seed(t)
+    rn = lambda *s: torch.randn(*s, generator=g, device="cuda", dtype=BF16)
+    w = rn(v, k).mul_(k ** -0.5)
+    y = torch.randint(0, v, (t,), generator=g, device="cuda")
+    y[0], y[1], y[2] = v - 1, 599187, 5                            # row 599186 holds element 2^31
+    h = (rn(t, k).float() + 8 * w[y].float()).to(BF16)
+    a = torch.randn(t, generator=g, device="cuda")
+    lm = B.LM(v, k, device=0)
+    ws = torch.full((lm.workspace_bytes(t),), 0xFF, device="cuda", dtype=torch.uint8)
+    loss, lse, dh = torch.empty(t, device="cuda"), torch.empty(t, device="cuda"), torch.empty_like(h)
+    dw = torch.full_like(w, float("nan"))
+    lm.loss_fwd(h, w, y, loss, lse, ws)
+    lm.loss_bwd(h, w, y, lse, a, dh, dw, ws)
+    assert lm.device_status() == (0, 0)
+    # the plain form in 64 bits, a block of words at a time; bounds as everywhere (loss_bounds), sums of magnitudes likewise
+    hd, ad = h.double(), a.double()
+    blocks = [slice(b, min(b + 40000, v)) for b in range(0, v, 40000)]
+    want_lse = torch.logsumexp(torch.stack([torch.logsumexp(hd @ w[s].double().T, 1) for s in blocks]), 0)
+    want_loss = want_lse - (hd * w[y].double()).sum(1)
+    u = 2.0 ** -23
+    reach = float(hd.norm(dim=1).max() * max(w[s].double().norm(dim=1).max() for s in blocks))
+    x = (k + 2) * u * reach
+    b_lse = x + (4 + 128 + v / 512) * u + 3 * u * (want_lse.abs() + reach)
+    assert ((lse.double() - want_lse).abs() <= b_lse).all() and ((loss.double() - want_loss).abs() <= b_lse + x).all()
+    p_err = x + b_lse.max().item() + 4 * u + 3 * u * reach
+    want_dh, mag_dh, abs_dh = (torch.zeros(t, k, device="cuda", dtype=F64) for _ in range(3))
+    step = lambda z: 2.0 ** -8 * z.abs()
+    for s in blocks:
+        wd = w[s].double()
+        p = torch.exp(hd @ wd.T - want_lse[:, None])
+        hot = (y[:, None] == torch.arange(s.start, s.stop, device="cuda")).double()
+        gr, mag = ad[:, None] * (p - hot), ad.abs()[:, None] * (p + hot)
+        want_dh += gr @ wd
+        mag_dh += mag @ wd.abs()
+        abs_dh += gr.abs() @ wd.abs()
+        ref = gr.T @ hd
+        off = 2 ** -8 * (gr.abs().T @ hd.abs()) + (p_err + t * u) * 1.01 * (mag.T @ hd.abs()) + 2.0 ** -100
+        assert ((dw[s].double() - ref).abs() <= off * (1 + 2 ** -8) + step(ref)).all(), s
+    off = 2 ** -8 * abs_dh + (p_err + v * u) * 1.01 * mag_dh + 2.0 ** -100
+    assert ((dh.double() - want_dh).abs() <= off * (1 + 2 ** -8) + step(want_dh)).all()
+    # the embedding of the same words, and its gradient
+    ids = torch.cat([y, torch.tensor([599185, 599186, v - 1, -1], device="cuda")])
+    out = torch.empty(len(ids), k, device="cuda", dtype=BF16)
+    lm.embed_fwd(w, ids, out)
+    assert torch.equal(out[:-1], w[ids[:-1]]) and (out[-1] == 0).all()
+    dw.fill_(float("nan"))
+    lm.embed_bwd(out, ids, dw, ws)
+    want = torch.zeros(len(ids), k, device="cuda", dtype=F64)
+    rows, back = torch.unique(ids[:-1], return_inverse=True)
+    want.index_add_(0, back, out[:-1].double())
+    assert (dw[rows].double() - want[: len(rows)]).abs().le(step(want[: len(rows)]) * (1 + 2.0 ** -14)).all()
+    dw[rows] = 0
+    for s in blocks:
+        assert (dw[s] == 0).all(), s
+    assert lm.device_status() == (0, 0)
+    del w, dw, ws
+    torch.cuda.empty_cache()
