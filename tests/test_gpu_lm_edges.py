@@ -271,3 +271,103 @@ def test_matrices_of_more_than_2_31_elements(B, t):
     assert lm.device_status() == (0, 0)
     del w, dw, ws
     torch.cuda.empty_cache()
+
+
+def test_calls_behind_an_event_of_another_stream(B):
+    """Launches are programmatic dependents of the kernel before them in their stream; what another stream's event stands for is waited
+    for all the same, right behind such a kernel."""
+    t, v, k = 64, 300, 64
+    lm = B.LM(v, k, device=0)
+    h, w, y, a = (x.cuda() for x in lu.make_loss(t, v, k, seed=31, masked=0.1))
+    want = run_loss(B, h, w, y, a)
+    one, two = torch.cuda.Stream(), torch.cuda.Stream()
+    ws, other = workspace(lm, t), workspace(lm, t)
+    e = lambda s, d: torch.zeros(s, device="cuda", dtype=d)
+    loss, lse, junk, tab = e((t,), F32), e((t,), F32), e((t,), F32), e((t, k), BF16)
+    for _ in range(5):
+        src = torch.zeros_like(h)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(two):
+            torch.cuda._sleep(3_000_000)
+            src.copy_(h)
+            ready = two.record_event()
+        with torch.cuda.stream(one):
+            lm.loss_fwd(h, w, y, junk, junk.clone(), other)
+            lm.embed_fwd(w, y, tab)
+            one.wait_event(ready)
+            lm.loss_fwd(src, w, y, loss, lse, ws)
+        torch.cuda.synchronize()
+        assert torch.equal(loss, want["loss"]) and torch.equal(lse, want["lse"])
+
+
+def test_a_graph_with_branches(B):
+    """Two branches of a captured graph, each with a workspace of its own, that part behind one kernel and join before another."""
+    t, v, k = 140, 500, 64
+    lm = B.LM(v, k, device=0)
+    h, w, y, a = (x.cuda() for x in lu.make_loss(t, v, k, seed=32, masked=0.1))
+    e = lambda s, d: torch.full(s, float("nan"), device="cuda", dtype=d)
+    x, loss, lse, dh, dw, tab, back = e((t, k), BF16), e((t,), F32), e((t,), F32), e((t, k), BF16), e((v, k), BF16), e((v, k), F32), e((t, k), F32)
+    ws, ws2 = workspace(lm, t), workspace(lm, t)
+    main, side = torch.cuda.Stream(), torch.cuda.Stream()
+
+    def step():
+        lm.embed_fwd(w, y, x)                           # both branches read it
+        side.wait_stream(main)
+        lm.loss_fwd(h, w, y, loss, lse, ws)
+        lm.loss_bwd(h, w, y, lse, a, dh, dw, ws)
+        with torch.cuda.stream(side):
+            lm.embed_bwd(x, y, tab, ws2)
+        main.wait_stream(side)
+        lm.embed_fwd(tab, y, back)                      # reads the side branch's result
+    main.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(main):
+        step()
+        main.synchronize()
+        want = [z.clone() for z in (x, loss, lse, dh, dw, tab, back)]
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=main):
+            step()
+    for _ in range(20):
+        for z in (x, loss, lse, dh, dw, tab, back):
+            z.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(z, r) for z, r in zip((x, loss, lse, dh, dw, tab, back), want))
+    assert lm.device_status() == (0, 0)
+
+
+def test_no_tokens_through_autograd(B):
+    from paper_2609_33133_b200 import autograd as A
+    v, k = 300, 64
+    lm = B.LM(v, k, device=0)
+    table = torch.ones(v, k, device="cuda", requires_grad=True)
+    none = torch.zeros(0, device="cuda", dtype=torch.int64)
+    A.embed(lm, table, none).sum().backward()
+    h = torch.zeros(0, k, device="cuda", dtype=BF16, requires_grad=True)
+    w = torch.ones(v, k, device="cuda", dtype=BF16, requires_grad=True)
+    loss = A.lm_loss(lm, h, w, none).sum()
+    loss.backward()
+    assert loss == 0 and (table.grad == 0).all() and (w.grad == 0).all() and h.grad.shape == h.shape
+
+
+def test_a_graph_of_a_backward_pass_beside_an_eager_one(B):
+    """The gradients of leaves whose eager backward pass has run, and whose eager graph still lives, captured and replayed."""
+    from paper_2609_33133_b200 import autograd as A
+    t, v, k = 140, 500, 64
+    lm = B.LM(v, k, device=0)
+    h, w, y, a = (x.cuda() for x in lu.make_loss(t, v, k, seed=33, masked=0.1))
+    h.requires_grad_(True), w.requires_grad_(True)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        eager = A.lm_loss(lm, h, w, y)
+        want = torch.autograd.grad((eager * a).sum(), (h, w), retain_graph=True)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            got = torch.autograd.grad((A.lm_loss(lm, h, w, y) * a).sum(), (h, w))
+    again = torch.autograd.grad((eager * a).sum(), (h, w))
+    for z in got:
+        z.fill_(float("nan"))
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(p, q) and torch.equal(p, r) for p, q, r in zip(got, want, again))
