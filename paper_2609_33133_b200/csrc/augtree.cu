@@ -320,6 +320,7 @@ int augtree_plan_create(const augtree_desc_t *desc, int device, augtree_plan_t *
     int sms = 0;
     if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess || sms < 1) {
       delete pl;
+      cudaGetLastError();  // reported by the return value; not left for the next launch's check
       return AUGTREE_ERR_CUDA;
     }
     d.n_lanes = sms;
@@ -359,7 +360,11 @@ int augtree_plan_create(const augtree_desc_t *desc, int device, augtree_plan_t *
         r = AUGTREE_ERR_CUDA;
     }
     cudaSetDevice(prev);
-    if (r) { augtree_plan_destroy(pl); return r; }
+    if (r) {
+      augtree_plan_destroy(pl);
+      cudaGetLastError();
+      return r;
+    }
   }
   *out = pl;
   return AUGTREE_OK;

@@ -162,3 +162,18 @@ def test_guard_bands_around_outputs_stay_untouched(B, case):
         assert bool((raw[GUARD + n:] == 0xA5).all()), f"{k}: bytes past the end of the tensor were written"
     got = {k: v.float().cpu().numpy().astype(np.float64) for k, v in out.items() if k != "ws"}
     pu.assert_parity_elementwise(got, pu.run_oracle(w, t_cpu), pu.rounding_error_sigma(w, t_cpu))
+
+
+@pytest.mark.parametrize("lanes", [0, LANES])    # the device is asked for its SM count, or made current first
+def test_a_plan_that_cannot_be_made_leaves_no_error_behind(B, lanes):
+    """A device that is not there: the failure is the return value's, and the next call on a good plan does not report it again."""
+    from paper_2609_33133_b200 import autograd as A
+    plan = B.Plan([130], [[64, 33]], 4, 2, 64, device=0)
+    g = torch.Generator().manual_seed(17)
+    x = [torch.randn(n, h, 64, generator=g).bfloat16().cuda() for n, h in ((130, 4), (130, 2), (130, 2), (97, 4), (97, 2), (97, 2))]
+    want = A.tree_attention(plan, *x)
+    with pytest.raises(B.AugtreeError) as e:
+        B.Plan([130], [[64, 33]], 4, 2, 64, device=torch.cuda.device_count() + 7, n_lanes=lanes)
+    assert e.value.code == -4
+    got = A.tree_attention(plan, *x)
+    assert all(torch.equal(a, b) for a, b in zip(got, want)) and plan.device_status() == (0, 0)
