@@ -30,7 +30,9 @@
  *    return AUGTREE_ERR_INVALID_ARG and launch nothing.  One process may hold
  *    plans for several devices and use them from several threads; a plan is
  *    immutable after creation, and concurrent calls on one plan are safe as
- *    long as each has its own workspace.  Plan creation, destruction and the
+ *    long as each has its own workspace.  It has to outlive the CUDA graphs
+ *    that its calls were captured into; it may be destroyed while another
+ *    capture is under way.  Plan creation, destruction and the
  *    status and timing queries switch to the plan's device themselves and
  *    restore the caller's.
  *  - Every function returns AUGTREE_OK (0) or a negative augtree_status code;

@@ -373,6 +373,7 @@ int augtree_plan_create(const augtree_desc_t *desc, int device, augtree_plan_t *
 int augtree_plan_destroy(augtree_plan_t *pl) {
   if (!pl) return AUGTREE_ERR_INVALID_ARG;
   if (pl->device >= 0) {
+    const RelaxedCapture relaxed;
     int prev = 0;
     cudaGetDevice(&prev);
     cudaSetDevice(pl->device);

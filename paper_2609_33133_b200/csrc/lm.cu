@@ -472,6 +472,7 @@ int augtree_lm_create(const augtree_lm_desc_t *desc, int device, augtree_lm_t **
 int augtree_lm_destroy(augtree_lm_t *lm) {
   if (!lm) return AUGTREE_ERR_INVALID_ARG;
   if (lm->device >= 0) {
+    const RelaxedCapture relaxed;
     int prev = 0;
     cudaGetDevice(&prev);
     cudaSetDevice(lm->device);

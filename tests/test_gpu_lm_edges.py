@@ -371,3 +371,26 @@ def test_a_graph_of_a_backward_pass_beside_an_eager_one(B):
     graph.replay()
     torch.cuda.synchronize()
     assert all(torch.equal(p, q) and torch.equal(p, r) for p, q, r in zip(got, want, again))
+
+
+@pytest.mark.parametrize("what", ["handle", "plan"])
+def test_a_handle_or_plan_that_dies_during_a_capture(B, what):
+    """Python's collector may end an old handle anywhere, in the middle of a capture too: freeing its memory does not spoil that."""
+    t, v, k = 40, 300, 64
+    lm = B.LM(v, k, device=0)
+    _, w, y, _ = (x.cuda() for x in lu.make_loss(t, v, k, seed=34))
+    out = torch.zeros(t, k, device="cuda", dtype=BF16)
+    lm.embed_fwd(w, y, out)
+    old = B.LM(77, 64, device=0) if what == "handle" else B.Plan([130], [[64, 33]], 4, 2, 64, device=0)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            lm.embed_fwd(w, y, out)
+            del old
+            lm.embed_fwd(w, y, out)
+    out.fill_(0)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, w[y])
