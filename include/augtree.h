@@ -472,7 +472,7 @@ int augtree_lm_destroy(augtree_lm_t *lm);
 /* Scratch (16-byte aligned) that is enough for the calls on up to n_tokens tokens; any of the pointers may be NULL. */
 int augtree_lm_workspace_bytes(const augtree_lm_t *lm, int64_t n_tokens, size_t *loss_fwd, size_t *loss_bwd, size_t *embed_bwd);
 
-/* out[t] = embed_scale * table[id_t], rounded once.  table and out: any of the three types each, 16-byte aligned. */
+/* out[t] = embed_scale * table[id_t] in fp32, rounded to out's type.  table and out: any of the three types each, 16-byte aligned. */
 int augtree_embed_fwd(const augtree_lm_t *lm, const void *table, int table_dtype, const void *ids, int id_bytes,
                       int64_t n_tokens, void *out, int out_dtype, void *stream);
 

@@ -86,7 +86,7 @@ class _Embed(torch.autograd.Function):
 
 
 def embed(lm: B.LM, table, ids, out_dtype=None):
-    """lm.embed_scale * table[ids], rounded once to out_dtype (default: the table's); zeros for negative ids.  Differentiable in
+    """lm.embed_scale * table[ids] in fp32, rounded to out_dtype (default: the table's); zeros for negative ids.  Differentiable in
     table (fp32, bf16 or fp16), whose gradient is dense and in its type."""
     return _Embed.apply(lm, table, ids, out_dtype)
 

@@ -352,7 +352,7 @@ template <> struct Vec<__half> {
   }
 };
 
-// out[t] = scale table[id_t]; zeros for a negative id.  The product is rounded once.  HBM-bound: a row read, a row written (24576 tokens
+// out[t] = scale table[id_t]; zeros for a negative id.  The product is taken in fp32 and rounded to the output's type.  HBM-bound: a row read, a row written (24576 tokens
 // of 3584 bf16 columns: 47 us, frequent rows from L2).
 template <typename Id, typename In, typename Out>
 __global__ void __launch_bounds__(128)
