@@ -212,7 +212,8 @@ def _in_8_bits(x):
     v = torch.nn.functional.pad(x.float(), (0, -c % 32)).view(t, -1, 32)
     m, e = torch.frexp(v.abs().amax(dim=2, keepdim=True))          # max = m 2^e, 1/2 <= m < 1
     e = (e - 7 + (m >= 127.5 / 128).int()).clamp_(min=-126)
-    return torch.ldexp(torch.ldexp(v, -e).round_(), e).view(t, -1)[:, :c]
+    unit, per = ((127 + e) << 23).view(F32), ((127 - e) << 23).view(F32)   # 2^e, 2^-e
+    return (v * per).round_().mul_(unit).view(t, -1)[:, :c]
 
 
 def _rsqrt_mean(v):
