@@ -450,6 +450,7 @@ int augtree_plan_tree(const augtree_tree_t *tree, const augtree_profile_t *profi
  * No atomics on floating-point values: results are bitwise repeatable.  Outputs and scratch must not overlap inputs.
  */
 enum { AUGTREE_BF16 = 0, AUGTREE_F16 = 1, AUGTREE_F32 = 2 };
+#define AUGTREE_CKPT 3   /* an 8-bit checkpoint, where a saved tensor may be one (augtree_ckpt_pack) */
 typedef struct {
   uint32_t struct_size;        /* sizeof(augtree_lm_desc_t)                                          */
   uint32_t version;            /* AUGTREE_VERSION                                                    */
@@ -500,6 +501,97 @@ int augtree_lm_loss_bwd(const augtree_lm_t *lm, const void *hidden, const void *
 
 /* As augtree_last_device_status, for a handle. */
 int augtree_lm_last_device_status(const augtree_lm_t *lm, int *status, int *detail);
+
+/*
+ * The ends of a decoder block, activation checkpoints in 8 bits, and what reads them in the backward pass.  (The paper has no
+ * counterpart: what lies around the attention is the base trainer's, Sec. 4.)
+ *
+ * A handle holds the width of the residual stream, the scales, the form of the gate and a status word; it does not depend on the
+ * number of tokens.  It is immutable after creation and belongs to a device exactly as a plan does (same rule for the current device,
+ * streams and concurrent calls: calls that may overlap need workspaces of their own).  Tensors are row-major [n_tokens, columns]
+ * without padding unless a leading size `ld` (elements, a multiple of 8; 0 => the columns) is given; base pointers are 16-byte
+ * aligned; r_in, r_out, a gate of one number a token and `row` on their element's size.  Columns: a multiple of 8.  Types: any of the three.
+ * Sums and statistics are fp32; every output is rounded once.  No atomics: results are bitwise repeatable.
+ */
+enum { AUGTREE_GATE_NONE = 0, AUGTREE_GATE_TOKEN = 1, AUGTREE_GATE_CHANNEL = 2, AUGTREE_GATE_FULL = 3 };  /* none, [n], [hidden], [n, hidden] */
+typedef struct {
+  uint32_t struct_size;        /* sizeof(augtree_block_desc_t)                                       */
+  uint32_t version;            /* AUGTREE_VERSION                                                    */
+  int32_t hidden;              /* a multiple of 8, at most 8192                                      */
+  float eps;                   /* of the norms; 0 => 1e-6                                            */
+  float residual_scale;        /* s; 0 => 1                                                          */
+  int32_t gate;                /* AUGTREE_GATE_*                                                     */
+  int32_t gate_sigmoid;        /* a(g): 0 = g itself, otherwise 1 / (1 + exp(-g))                    */
+  uint32_t flags;              /* AUGTREE_FLAG_TEST_SHORT_WAIT, AUGTREE_FLAG_TEST_SKIP_FWD_LOAD      */
+  int32_t n_lanes;             /* persistent CTAs; 0 => SM count of device; at most 2^20             */
+} augtree_block_desc_t;
+typedef struct augtree_block augtree_block_t;
+
+/* As augtree_lm_create and augtree_lm_destroy. */
+int augtree_block_create(const augtree_block_desc_t *desc, int device, augtree_block_t **out);
+int augtree_block_destroy(augtree_block_t *block);
+
+/*
+ * End of a block and norm before the next one:
+ *   z = w_out o r_out,  r_out = 1 / sqrt(mean o^2 + eps)   (w_out NULL: z = o);     y = x + s a(gate) z
+ *   h = w_in y r_in,    r_in  = 1 / sqrt(mean y^2 + eps)   (from y before it is rounded to its type)
+ * x, y: x_dtype; y may be x itself.  o: NULL for the norm before a block alone (then y, w_out, gate and ckpt_o are NULL and h is made of
+ * x).  h and w_in: both or neither.  gate: as the handle says, wherever there is an o.  r_out, r_in [n_tokens] fp32: what the backward pass
+ * needs, NULL if there is none.  ckpt_y, ckpt_o (or NULL): the 8-bit forms of y (of x without an o), as delivered, and of o.
+ * AUGTREE_ERR_UNSUPPORTED when a row of all inputs does not fit a CTA's shared memory (hidden near 8192 with everything in fp32).
+ */
+int augtree_block_fwd(const augtree_block_t *block, const void *x, int x_dtype, const void *o, int o_dtype, const void *gate, int gate_dtype,
+                      const void *w_out, const void *w_in, int w_dtype, int64_t n_tokens, void *y, void *h, int h_dtype, float *r_out,
+                      float *r_in, void *ckpt_y, void *ckpt_o, void *stream);
+
+/* Scratch (16-byte aligned) of the backward call; the same for any number of tokens. */
+int augtree_block_workspace_bytes(const augtree_block_t *block, int64_t n_tokens, size_t *bytes);
+
+/*
+ * Its gradients under dy (x_dtype, of the residual stream) and dh (of h); either may be NULL and then counts as zero.  y and o: as the forward
+ * call left them, or their 8-bit forms (dtype AUGTREE_CKPT); without an o the forward's x stands for y.
+ *   dx (x_dtype; may be dy itself), d_o, d_gate (type and shape of the gate), dw_out, dw_in [hidden] (w_dtype): each may be NULL and is
+ *   then not written.  With accumulate != 0 the sums over tokens (dw_out, dw_in, d_gate of one number a channel) are ADDED to what is
+ *   there (fp32 only, else AUGTREE_ERR_UNSUPPORTED).  With dh NULL, w_in, y and r_in are NULL too or not read.
+ */
+int augtree_block_bwd(const augtree_block_t *block, const void *dy, int x_dtype, const void *dh, int h_dtype, const void *y, int y_dtype,
+                      const void *o, int o_dtype, const void *gate, int gate_dtype, const void *w_out, const void *w_in, int w_dtype,
+                      const float *r_out, const float *r_in, int64_t n_tokens, void *dx, void *d_o, int do_dtype, void *d_gate, void *dw_out,
+                      void *dw_in, int accumulate, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * Checkpoints: [n_tokens] rows of *pitch bytes: ceil16(cols) integers -127 .. 127, then ceil16(ceil(cols / 32)) bytes e + 127.  32 neighbouring
+ * columns share 2^e, the smallest power of two with max |x| < 127.5 2^e and e >= -126; a value stands for its integer times 2^e (the nearest,
+ * ties to even).  A group with a NaN or an infinity (byte 255) stands for NaN.  Bytes behind the last column and group are not defined.
+ * unpack: out = 2^e q, times row[t] (fp32) and then col[c] where they are not NULL, in fp32, rounded to out's type.
+ */
+int augtree_ckpt_pitch(int64_t cols, int64_t *pitch);
+int augtree_ckpt_pack(const augtree_block_t *block, const void *x, int dtype, int64_t ld, int64_t n_tokens, int64_t cols, void *ckpt, void *stream);
+int augtree_ckpt_unpack(const augtree_block_t *block, const void *ckpt, int64_t n_tokens, int64_t cols, const float *row, const void *col,
+                        int col_dtype, void *out, int dtype, int64_t ld, void *stream);
+
+/*
+ * Gated MLP: a = g / (1 + exp(-g)) u, all of one type; g and u with a leading size (the halves of one product), a without.  ckpt_g and
+ * ckpt_u: both or neither.  Backward from g and u (saved_dtype = dtype) or from their checkpoints (AUGTREE_CKPT; ld is not used): dg, du with a leading
+ * size of their own, and a once more where it is not NULL.
+ */
+int augtree_glu_fwd(const augtree_block_t *block, const void *g, const void *u, int64_t ld, int dtype, int64_t n_tokens, int64_t cols, void *a,
+                    void *ckpt_g, void *ckpt_u, void *stream);
+int augtree_glu_bwd(const augtree_block_t *block, const void *da, int dtype, const void *g, const void *u, int64_t ld, int saved_dtype,
+                    int64_t n_tokens, int64_t cols, void *dg, void *du, int64_t ld_grad, void *a, void *stream);
+
+/*
+ * Weight gradient of a product whose input was kept in 8 bits: d_weight [out_features, cols] = dy^T X with dy [n_tokens, out_features] bf16 and
+ * X = 2^e q, times row[t] (then rounded to bf16, as an operand of the tensor core) and col[c] where they are not NULL: with r_in and w_in X
+ * is the norm's output h.  d_weight: bf16 or fp32, the latter also added to (accumulate != 0, else AUGTREE_ERR_UNSUPPORTED).
+ */
+int augtree_ckpt_wgrad_bytes(const augtree_block_t *block, int64_t n_tokens, int64_t out_features, int64_t cols, size_t *bytes);
+int augtree_ckpt_wgrad(const augtree_block_t *block, const void *dy, int64_t n_tokens, int64_t out_features, const void *ckpt, int64_t cols,
+                       const float *row, const void *col, int col_dtype, void *d_weight, int weight_dtype, int accumulate, void *ws,
+                       size_t ws_bytes, void *stream);
+
+/* As augtree_last_device_status, for a handle. */
+int augtree_block_last_device_status(const augtree_block_t *block, int *status, int *detail);
 
 const char *augtree_status_string(int status);
 

@@ -8,8 +8,9 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libaugtree.so")
-SOURCES = ["augtree.cu", "lm.cu", "plan.cpp", "planner.cpp"]
-HEADERS = ["ptx.cuh", "fwd_kernel.cuh", "bwd_kernel.cuh", "dq_kernel.cuh", "dql_kernel.cuh", "lm_tile_kernel.cuh", "lm_few_kernel.cuh", "lm_kernels.cuh", "launch.h", "plan.h", os.path.join("..", "..", "include", "augtree.h")]
+SOURCES = ["augtree.cu", "lm.cu", "block.cu", "plan.cpp", "planner.cpp"]
+HEADERS = ["ptx.cuh", "fwd_kernel.cuh", "bwd_kernel.cuh", "dq_kernel.cuh", "dql_kernel.cuh", "pair_tile.cuh", "lm_tile_kernel.cuh", "lm_few_kernel.cuh", "lm_kernels.cuh", "ckpt.cuh", "act_kernels.cuh",
+           "block_kernels.cuh", "wgrad_kernel.cuh", "handle.h", "launch.h", "plan.h", os.path.join("..", "..", "include", "augtree.h")]
 
 
 def _stale() -> bool:

@@ -1,0 +1,560 @@
+// The ends of a decoder block: norm after the block, gate, residual scale, residual, norm before the next block, and their gradients.
+//
+//   forward    z = w_o o r_o,  r_o = rsqrt(mean o^2 + eps)        (z = o without a norm after the block)
+//              y = x + s a(g) z,  h = w_i y r_i,  r_i = rsqrt(mean y^2 + eps)
+//   backward   v = y r_i,  d = dy + r_i (w_i dh - v mean(w_i dh v)) = dx,      dw_i = sum over tokens of dh v
+//              u = o r_o,  do = r_o (w_o s a d - u mean(w_o s a d u)),           dw_o = sum over tokens of s a d u
+//              dg = s a'(g) d w_o u, summed over the channels for a gate of one number a token and over the tokens for one a channel
+//
+// Bound by memory: a row passes once, all arithmetic is in registers.  The rows' bytes are fetched ahead by the copy engine (one bulk
+// copy per tensor and block of rows, which are contiguous) into a ring of stages in shared memory, so what is in flight does not depend on
+// how many threads wait: 44 GB/s and SM at 6.5 TB/s need 35 KB in flight against 0.8 us of latency, and a row of 3584 channels is
+// 21 KB forward and 43 KB backward.  One CTA an SM; its warps form `groups` of as many warps as a row of 512 columns a warp needs (256 up
+// to 256 columns), and each group takes a row of a stage at a time, so one group's reductions run under another's arithmetic.
+// A group's sum over a row: shuffles, then the warps' sums through shared memory behind one named barrier.
+// The sums over tokens stay in registers (every thread owns its columns for all rows of its CTA), go over the groups through shared memory
+// and from CTA to CTA through scratch and a second kernel, in an order that depends on the sizes alone: no atomics, bitwise repeatable.
+// Every sum, statistic and product is fp32; values are rounded once, on delivery.  The 8-bit form of y is made from y as it is
+// delivered, so that it is the form that ckpt_pack makes of the tensor.
+#pragma once
+#include "act_kernels.cuh"
+
+namespace augtree {
+
+enum : int { GATE_NONE = 0, GATE_TOKEN = 1, GATE_CHANNEL = 2, GATE_FULL = 3 };
+enum : int { WAIT_BLOCK_FULL = 90, WAIT_BLOCK_EMPTY = 91 };
+
+constexpr int kBlockMaxHidden = 8192;
+// Warps that compute; one more loads.  With it the count divides by the four schedulers of an SM, whose registers a thread's share is
+// cut from: 96 forward, 128 backward.  Rows of more than 7680 columns take 16 warps backward, with 96 and some spills.
+constexpr int kBlockFwdWarps = 19, kBlockBwdWarps = 15, kBlockBwdWarpsWide = 16;
+constexpr int kBlockSmem = 227 * 1024;
+constexpr int kBlockFixed = 256 + kBlockFwdWarps * 256;   // barriers, the groups' sums
+constexpr int kBlockMaxStages = 8;
+constexpr int kBlockMaxInputs = 5;
+
+// The shape of a launch, chosen on the host.
+struct BlockShape {
+  int rows, hidden, vecs;         // vecs: pieces of 8 columns of a row
+  int warps_row, groups;          // warps of a group; groups of a CTA
+  int block_rows, blocks;         // rows of a stage; blocks of rows of the call
+  int per_group;                  // rows of a stage that a group takes
+  int stages, stage_bytes;
+  int n_inputs;
+  const uint8_t *input[kBlockMaxInputs];
+  int row_bytes[kBlockMaxInputs], offset[kBlockMaxInputs];   // bytes of a row; where its block lies in a stage
+  int weights;                    // fp32 copies of per-channel vectors behind the stages: how many
+};
+
+struct BlockParams {
+  BlockShape s;
+  float inv_hidden, eps, scale;
+  int gate, sigmoid, gate_type;
+  const void *gate_ptr;
+  const void *w_out, *w_in;       // null: no such norm
+  int w_type;
+  float *r_out, *r_in;            // forward: written where not null; backward: read
+  int x_type, o_type, h_type, y_type;    // x: stream (x, y, dy, dx); o: branch or its 8-bit form; backward: y_type of what v is read from
+  int do_type;
+  int has_branch, has_dy, has_dh;
+  void *y, *h;                    // forward
+  CkptRows ckpt_y, ckpt_o;        // forward: base null = not kept
+  void *dx, *d_o, *dg;            // backward
+  float *part;                    // backward: [CTAs][2][hidden]
+  int *status;
+  long long wait_budget;
+  int test_flags;
+};
+
+// 8 columns of a row in shared memory
+__device__ __forceinline__ void block_load8(const uint8_t *row, int vec, int type, int hidden, float (&x)[8]) {
+  if (type == T_BF16) Row8<__nv_bfloat16>::load(reinterpret_cast<const __nv_bfloat16 *>(row) + vec * 8, x);
+  else if (type == T_F32) Row8<float>::load(reinterpret_cast<const float *>(row) + vec * 8, x);
+  else if (type == T_CKPT)
+    ckpt_decode(*reinterpret_cast<const uint2 *>(row + vec * 8), ckpt_unit(row[ckpt_scale_offset(hidden) + (vec >> 2)]), x);
+  else Row8<__half>::load(reinterpret_cast<const __half *>(row) + vec * 8, x);
+}
+__device__ __forceinline__ void block_store8(void *base, long long at, int type, const float (&x)[8]) {
+  if (type == T_BF16) Row8<__nv_bfloat16>::store(static_cast<__nv_bfloat16 *>(base) + at, x);
+  else if (type == T_F32) Row8<float>::store(static_cast<float *>(base) + at, x);
+  else Row8<__half>::store(static_cast<__half *>(base) + at, x);
+}
+__device__ __forceinline__ float block_scalar(const void *p, long long i, int type) {
+  if (type == T_BF16) return __bfloat162float(static_cast<const __nv_bfloat16 *>(p)[i]);
+  if (type == T_F32) return static_cast<const float *>(p)[i];
+  return __half2float(static_cast<const __half *>(p)[i]);
+}
+__device__ __forceinline__ void block_scalar_store(void *p, long long i, int type, float v) {
+  if (type == T_BF16) static_cast<__nv_bfloat16 *>(p)[i] = __float2bfloat16_rn(v);
+  else if (type == T_F32) static_cast<float *>(p)[i] = v;
+  else static_cast<__half *>(p)[i] = __float2half_rn(v);
+}
+__device__ __forceinline__ float block_round(float x, int type) {
+  if (type == T_BF16) return Row8<__nv_bfloat16>::round(x);
+  if (type == T_F16) return Row8<__half>::round(x);
+  return x;
+}
+
+// What the roles of a CTA share.
+struct BlockCta {
+  uint8_t *smem;
+  uint32_t base, bar_full, bar_empty;
+  float *sums;        // [groups][2][32]
+  volatile int *abort_flag;
+  float *weights;     // [s.weights][hidden]
+};
+
+__device__ __forceinline__ BlockCta block_setup(uint8_t *smem, const BlockParams &p) {
+  BlockCta c;
+  c.smem = smem;
+  c.base = smem_u32(smem);
+  c.bar_full = c.base;
+  c.bar_empty = c.base + 8 * kBlockMaxStages;
+  c.abort_flag = reinterpret_cast<volatile int *>(smem + 16 * kBlockMaxStages);
+  c.sums = reinterpret_cast<float *>(smem + 256);
+  c.weights = reinterpret_cast<float *>(smem + kBlockFixed);
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < p.s.stages; ++i) { mbar_init(c.bar_full + 8 * i, 1); mbar_init(c.bar_empty + 8 * i, p.s.groups * p.s.warps_row); }
+    *c.abort_flag = 0;
+    fence_barrier_init();
+  }
+  // (the entries behind a group's warps stay zero, so that the sums are read four at a time)
+  for (int i = threadIdx.x; i < p.s.groups * 64; i += blockDim.x) c.sums[i] = 0.f;
+  return c;
+}
+__device__ __forceinline__ uint8_t *block_stage(const BlockCta &c, const BlockParams &p, int stage) {
+  return c.smem + kBlockFixed + p.s.weights * p.s.hidden * 4 + stage * p.s.stage_bytes;
+}
+// a vector of one number a channel into shared memory as fp32
+__device__ __forceinline__ void block_weights(const BlockCta &c, const BlockParams &p, int slot, const void *w, int type) {
+  float *dst = c.weights + slot * p.s.hidden;
+  for (int i = threadIdx.x; i < p.s.vecs; i += blockDim.x) {
+    float x[8];
+    if (type == T_BF16) Row8<__nv_bfloat16>::load(static_cast<const __nv_bfloat16 *>(w) + i * 8, x);
+    else if (type == T_F32) Row8<float>::load(static_cast<const float *>(w) + i * 8, x);
+    else Row8<__half>::load(static_cast<const __half *>(w) + i * 8, x);
+    reinterpret_cast<float4 *>(dst)[2 * i] = make_float4(x[0], x[1], x[2], x[3]);
+    reinterpret_cast<float4 *>(dst)[2 * i + 1] = make_float4(x[4], x[5], x[6], x[7]);
+  }
+}
+
+// The loading warp: one thread, a ring of stages.  After a wait that gave up it loads nothing more; the copies that are under way
+// are waited for by those who read them, and the CTA stays for a while before it leaves (block_leave).
+__device__ __forceinline__ void block_produce(const BlockCta &c, const BlockParams &p, const AbortCtx &ab) {
+  const BlockShape &s = p.s;
+  int st = 0;
+  uint32_t phase = 1;
+  bool skip = (p.test_flags & TEST_SKIP_FWD_LOAD) && blockIdx.x == 0;
+  for (long long b = blockIdx.x; b < s.blocks; b += gridDim.x) {
+    if (!mbar_wait(c.bar_empty + 8 * st, phase, ab, WAIT_BLOCK_EMPTY)) return;
+    const long long row0 = b * s.block_rows;
+    const int rows = (int)min((long long)s.block_rows, s.rows - row0);
+    const uint32_t full = c.bar_full + 8 * st, dst = smem_u32(block_stage(c, p, st));
+    if (!skip) {
+      int bytes = 0;
+#pragma unroll
+      for (int i = 0; i < kBlockMaxInputs; ++i) if (i < s.n_inputs) bytes += rows * s.row_bytes[i];
+      mbar_expect_tx(full, bytes);
+#pragma unroll
+      for (int i = 0; i < kBlockMaxInputs; ++i)
+        if (i < s.n_inputs) bulk_load_1d(dst + s.offset[i], s.input[i] + row0 * s.row_bytes[i], rows * s.row_bytes[i], full);
+    }
+    skip = false;
+    if (++st == s.stages) { st = 0; phase ^= 1; }
+  }
+}
+__device__ __forceinline__ void block_leave(const BlockCta &c) {
+  __syncwarp();
+  if (*c.abort_flag) {
+    const long long t0 = clock64();
+    while (clock64() - t0 < 400000) {}
+  }
+}
+
+// Sum over a row, the same in every thread of the group.  `flip` alternates between two places, so that one barrier is enough: whoever
+// writes a place again has passed the barrier of the sum between, behind which everybody has read it.
+struct BlockGroup {
+  float *sums;
+  int warps, warp, bar, flip;
+  __device__ __forceinline__ float sum(float v) {
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+    if (warps == 1) return v;
+    float *place = sums + flip * 32;
+    if ((threadIdx.x & 31) == 0) place[warp] = v;
+    asm volatile("bar.sync %0, %1;" ::"r"(bar), "r"(warps * 32) : "memory");
+    v = 0.f;
+    for (int i = 0; i < warps; i += 4) {
+      const float4 q = *reinterpret_cast<const float4 *>(place + i);
+      v += (q.x + q.y) + (q.z + q.w);
+    }
+    flip ^= 1;
+    return v;
+  }
+};
+
+template <int VPT>
+__global__ void __launch_bounds__((kBlockFwdWarps + 1) * 32, 1)
+block_fwd_kernel(const __grid_constant__ BlockParams p) {
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  const BlockShape &s = p.s;
+  launch_next();
+  const BlockCta c = block_setup(smem_raw, p);
+  __syncthreads();
+  wait_previous();
+  // slots of the vectors: w_in, w_out, gate of a channel (with the residual scale)
+  const int slot_out = p.w_in ? 1 : 0, slot_gate = slot_out + (p.w_out ? 1 : 0);
+  if (p.w_in) block_weights(c, p, 0, p.w_in, p.w_type);
+  if (p.w_out) block_weights(c, p, slot_out, p.w_out, p.w_type);
+  if (p.gate == GATE_CHANNEL) block_weights(c, p, slot_gate, p.gate_ptr, p.gate_type);
+  __syncthreads();
+  const AbortCtx ab{c.abort_flag, p.status, p.wait_budget};
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (warp == s.groups * s.warps_row) {
+    if (lane == 0) block_produce(c, p, ab);
+  } else {
+    const int group = warp / s.warps_row;
+    BlockGroup g{c.sums + group * 64, s.warps_row, warp - group * s.warps_row, group + 1, 0};
+    const int v0 = g.warp * 32 + lane, step = s.warps_row * 32;     // pieces v0, v0 + step
+    int st = 0;
+    uint32_t phase = 0;
+    for (long long b = blockIdx.x; b < s.blocks; b += gridDim.x) {
+      const long long row0 = b * s.block_rows;
+      const int rows = (int)min((long long)s.block_rows, s.rows - row0);
+      // A wait that gave up: the group goes on with whatever is there, so that nobody is left alone at a barrier; its results are
+      // void, which the status word says, and every later wait gives up at once.
+      mbar_wait(c.bar_full + 8 * st, phase, ab, WAIT_BLOCK_FULL);
+      const uint8_t *stage = block_stage(c, p, st);
+      for (int r = group; r < rows; r += s.groups) {
+        const long long t = row0 + r;
+        const uint8_t *rx = stage + s.offset[0] + (long long)r * s.row_bytes[0], *ro = stage + s.offset[1] + (long long)r * s.row_bytes[1];
+        const uint8_t *rg = stage + s.offset[2] + (long long)r * s.row_bytes[2];
+        float y[VPT][8], r_o = 1.f;
+#pragma unroll
+        for (int k = 0; k < VPT; ++k) {
+          const int v = v0 + k * step;
+          if (v < s.vecs) block_load8(rx, v, p.x_type, s.hidden, y[k]);
+          else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[k][i] = 0.f;
+          }
+        }
+        if (p.has_branch) {
+          float o[VPT][8], ga = p.scale;
+          if (p.gate == GATE_TOKEN) {
+            const float gt = block_scalar(p.gate_ptr, t, p.gate_type);
+            ga *= p.sigmoid ? logistic(gt) : gt;
+          }
+          float ss = 0.f;
+#pragma unroll
+          for (int k = 0; k < VPT; ++k) {
+            const int v = v0 + k * step;
+            if (v < s.vecs) block_load8(ro, v, p.o_type, s.hidden, o[k]);
+            else {
+#pragma unroll
+              for (int i = 0; i < 8; ++i) o[k][i] = 0.f;
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) ss = fmaf(o[k][i], o[k][i], ss);
+          }
+          if (p.w_out) {
+            r_o = rsqrtf(fmaf(g.sum(ss), p.inv_hidden, p.eps));
+            if (p.r_out && g.warp == 0 && lane == 0) p.r_out[t] = r_o;
+          }
+          if (p.ckpt_o.base) {
+#pragma unroll
+            for (int k = 0; k < VPT; ++k) {
+              const int v = v0 + k * step;
+              uint2 q;
+              uint32_t byte;
+              ckpt_encode(o[k], q, byte);
+              if (v < s.vecs) p.ckpt_o.store(t, v, q, byte);
+            }
+          }
+#pragma unroll
+          for (int k = 0; k < VPT; ++k) {
+            const int v = v0 + k * step;
+            if (v >= s.vecs) continue;
+            if (p.w_out) {
+              float w[8];
+              Row8<float>::load(c.weights + slot_out * s.hidden + v * 8, w);
+#pragma unroll
+              for (int i = 0; i < 8; ++i) o[k][i] = w[i] * (o[k][i] * r_o);
+            }
+            if (p.gate >= GATE_CHANNEL) {
+              float a[8];
+              if (p.gate == GATE_FULL) block_load8(rg, v, p.gate_type, s.hidden, a);
+              else Row8<float>::load(c.weights + slot_gate * s.hidden + v * 8, a);
+#pragma unroll
+              for (int i = 0; i < 8; ++i) o[k][i] *= p.sigmoid ? logistic(a[i]) : a[i];
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[k][i] = fmaf(ga, o[k][i], y[k][i]);
+            if (p.y) block_store8(p.y, t * s.hidden + v * 8, p.x_type, y[k]);
+          }
+        }
+        float r_i = 1.f;
+        if (p.w_in) {
+          float ss = 0.f;
+#pragma unroll
+          for (int k = 0; k < VPT; ++k)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) ss = fmaf(y[k][i], y[k][i], ss);
+          r_i = rsqrtf(fmaf(g.sum(ss), p.inv_hidden, p.eps));
+          if (p.r_in && g.warp == 0 && lane == 0) p.r_in[t] = r_i;
+        }
+#pragma unroll
+        for (int k = 0; k < VPT; ++k) {
+          const int v = v0 + k * step;
+          if (p.w_in && v < s.vecs) {
+            float w[8], h[8];
+            Row8<float>::load(c.weights + v * 8, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) h[i] = w[i] * (y[k][i] * r_i);
+            block_store8(p.h, t * s.hidden + v * 8, p.h_type, h);
+          }
+          if (p.ckpt_y.base) {
+            uint2 q;
+            uint32_t byte;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[k][i] = block_round(y[k][i], p.x_type);
+            ckpt_encode(y[k], q, byte);
+            if (v < s.vecs) p.ckpt_y.store(t, v, q, byte);
+          }
+        }
+      }
+      warp_arrive(c.bar_empty + 8 * st);
+      if (++st == s.stages) { st = 0; phase ^= 1; }
+    }
+  }
+  block_leave(c);
+}
+
+template <int VPT, int kWarps>
+__global__ void __launch_bounds__((kWarps + 1) * 32, 1)
+block_bwd_kernel(const __grid_constant__ BlockParams p) {
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  const BlockShape &s = p.s;
+  launch_next();
+  const BlockCta c = block_setup(smem_raw, p);
+  __syncthreads();
+  wait_previous();
+  const int slot_out = p.w_in ? 1 : 0, slot_gate = slot_out + (p.w_out ? 1 : 0);
+  if (p.w_in) block_weights(c, p, 0, p.w_in, p.w_type);
+  if (p.w_out) block_weights(c, p, slot_out, p.w_out, p.w_type);
+  if (p.gate == GATE_CHANNEL) block_weights(c, p, slot_gate, p.gate_ptr, p.gate_type);
+  __syncthreads();
+  const AbortCtx ab{c.abort_flag, p.status, p.wait_budget};
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  float acc_in[VPT][8], acc_out[VPT][8];
+#pragma unroll
+  for (int k = 0; k < VPT; ++k)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) acc_in[k][i] = acc_out[k][i] = 0.f;
+  const int group = warp / s.warps_row;
+  BlockGroup g{c.sums + group * 64, s.warps_row, warp - group * s.warps_row, group + 1, 0};
+  const int v0 = g.warp * 32 + lane, step = s.warps_row * 32;
+  const bool computes = group < s.groups;
+  if (!computes) {
+    if (lane == 0) block_produce(c, p, ab);
+    __syncwarp();
+  } else {
+    int st = 0;
+    uint32_t phase = 0;
+    // inputs in the order that the host lists them: dy, dh, y, o, gate, each only where there is one
+    const int at_dh = p.has_dy, at_y = at_dh + p.has_dh, at_o = at_y + p.has_dh, at_g = at_o + p.has_branch;
+    for (long long b = blockIdx.x; b < s.blocks; b += gridDim.x) {
+      const long long row0 = b * s.block_rows;
+      const int rows = (int)min((long long)s.block_rows, s.rows - row0);
+      mbar_wait(c.bar_full + 8 * st, phase, ab, WAIT_BLOCK_FULL);
+      const uint8_t *stage = block_stage(c, p, st);
+      for (int r = group; r < rows; r += s.groups) {
+        const long long t = row0 + r;
+        auto row = [&](int i) { return stage + s.offset[i] + (long long)r * s.row_bytes[i]; };
+        const float r_i = p.has_dh ? p.r_in[t] : 0.f, r_o = p.w_out ? p.r_out[t] : 1.f;
+        float gt = 1.f;
+        if (p.gate == GATE_TOKEN) gt = block_scalar(p.gate_ptr, t, p.gate_type);
+        const float at = p.gate == GATE_TOKEN ? (p.sigmoid ? logistic(gt) : gt) : 1.f;
+        float d[VPT][8];
+#pragma unroll
+        for (int k = 0; k < VPT; ++k) {
+          const int v = v0 + k * step;
+          if (p.has_dy && v < s.vecs) block_load8(row(0), v, p.x_type, s.hidden, d[k]);
+          else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) d[k][i] = 0.f;
+          }
+        }
+        if (p.has_dh) {
+          // the sum with y itself; its norm comes in behind the reduction
+          float dot = 0.f;
+#pragma unroll
+          for (int k = 0; k < VPT; ++k) {
+            const int v = v0 + k * step;
+            if (v >= s.vecs) continue;
+            float dh[8], y[8], w[8];
+            block_load8(row(at_dh), v, p.h_type, s.hidden, dh);
+            block_load8(row(at_y), v, p.y_type, s.hidden, y);
+            Row8<float>::load(c.weights + v * 8, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              y[i] *= r_i;
+              acc_in[k][i] = fmaf(dh[i], y[i], acc_in[k][i]);
+              dot = fmaf(w[i] * dh[i], y[i], dot);
+            }
+          }
+          const float mean = g.sum(dot) * p.inv_hidden;
+#pragma unroll
+          for (int k = 0; k < VPT; ++k) {
+            const int v = v0 + k * step;
+            if (v >= s.vecs) continue;
+            float dh[8], y[8], w[8];
+            block_load8(row(at_dh), v, p.h_type, s.hidden, dh);
+            block_load8(row(at_y), v, p.y_type, s.hidden, y);
+            Row8<float>::load(c.weights + v * 8, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) d[k][i] = fmaf(r_i, fmaf(-mean, y[i] * r_i, w[i] * dh[i]), d[k][i]);
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < VPT; ++k) {
+          const int v = v0 + k * step;
+          if (v < s.vecs && p.dx) block_store8(p.dx, t * s.hidden + v * 8, p.x_type, d[k]);
+        }
+        if (p.has_branch) {
+          float dot = 0.f;    // sum of w_o q u (a): what the norm and a gate of one number a token need
+#pragma unroll
+          for (int k = 0; k < VPT; ++k) {
+            const int v = v0 + k * step;
+            if (v >= s.vecs) continue;
+            float u[8], w[8], a[8], da[8];
+            block_load8(row(at_o), v, p.o_type, s.hidden, u);
+            if (p.w_out) Row8<float>::load(c.weights + slot_out * s.hidden + v * 8, w);
+            if (p.gate >= GATE_CHANNEL) {
+              if (p.gate == GATE_FULL) block_load8(row(at_g), v, p.gate_type, s.hidden, a);
+              else Row8<float>::load(c.weights + slot_gate * s.hidden + v * 8, a);
+              if (p.sigmoid) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) { a[i] = logistic(a[i]); da[i] = a[i] * (1.f - a[i]); }
+              } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) da[i] = 1.f;
+              }
+            } else {
+#pragma unroll
+              for (int i = 0; i < 8; ++i) a[i] = at;
+            }
+            float dg[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const float q = p.scale * d[k][i];
+              u[i] *= r_o;
+              const float wu = p.w_out ? w[i] * u[i] : u[i];
+              dg[i] = q * wu;                                        // d a(g)
+              dot = fmaf(dg[i], p.gate >= GATE_CHANNEL ? a[i] : 1.f, dot);
+              acc_out[k][i] = fmaf(p.gate == GATE_CHANNEL ? q : q * a[i], u[i], acc_out[k][i]);
+              d[k][i] = (p.w_out ? w[i] : 1.f) * (q * a[i]);         // d u
+            }
+            if (p.gate == GATE_FULL && p.dg) {
+#pragma unroll
+              for (int i = 0; i < 8; ++i) dg[i] *= da[i];
+              block_store8(p.dg, t * s.hidden + v * 8, p.gate_type, dg);
+            }
+          }
+          float mean = 0.f;
+          if (p.w_out || p.gate == GATE_TOKEN) {
+            const float total = g.sum(dot);
+            mean = total * at * p.inv_hidden;
+            if (p.gate == GATE_TOKEN && p.dg && g.warp == 0 && lane == 0)
+              block_scalar_store(p.dg, t, p.gate_type, total * (p.sigmoid ? at * (1.f - at) : 1.f));
+          }
+          if (p.d_o) {
+#pragma unroll
+            for (int k = 0; k < VPT; ++k) {
+              const int v = v0 + k * step;
+              if (v >= s.vecs) continue;
+              if (p.w_out) {
+                float u[8];
+                block_load8(row(at_o), v, p.o_type, s.hidden, u);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) d[k][i] = r_o * fmaf(-mean, u[i] * r_o, d[k][i]);
+              }
+              block_store8(p.d_o, t * s.hidden + v * 8, p.do_type, d[k]);
+            }
+          }
+        }
+      }
+      warp_arrive(c.bar_empty + 8 * st);
+      if (++st == s.stages) { st = 0; phase ^= 1; }
+    }
+  }
+  block_leave(c);
+  // the groups' sums, one after the other, where the stages were (every copy into them has been read)
+  __syncthreads();
+  float *sum = reinterpret_cast<float *>(block_stage(c, p, 0));      // [groups][2][hidden]
+  if (computes) {
+#pragma unroll
+    for (int k = 0; k < VPT; ++k) {
+      const int v = v0 + k * step;
+      if (v >= s.vecs) continue;
+      float4 *q = reinterpret_cast<float4 *>(sum + (long long)group * 2 * s.hidden + v * 8);
+      q[0] = make_float4(acc_in[k][0], acc_in[k][1], acc_in[k][2], acc_in[k][3]);
+      q[1] = make_float4(acc_in[k][4], acc_in[k][5], acc_in[k][6], acc_in[k][7]);
+      q = reinterpret_cast<float4 *>(sum + (long long)group * 2 * s.hidden + s.hidden + v * 8);
+      q[0] = make_float4(acc_out[k][0], acc_out[k][1], acc_out[k][2], acc_out[k][3]);
+      q[1] = make_float4(acc_out[k][4], acc_out[k][5], acc_out[k][6], acc_out[k][7]);
+    }
+  }
+  __syncthreads();
+  const bool any_in = p.has_dh, any_out = p.w_out || p.gate == GATE_CHANNEL;
+  for (int i = threadIdx.x; i < 2 * s.hidden; i += blockDim.x) {
+    if (!(i < s.hidden ? any_in : any_out)) continue;
+    float v = sum[i];
+    for (int j = 1; j < s.groups; ++j) v += sum[(long long)j * 2 * s.hidden + i];
+    p.part[(long long)blockIdx.x * 2 * s.hidden + i] = v;
+  }
+}
+
+// The CTAs' sums over tokens into dw_in, dw_out and the gradient of a gate of one number a channel: 32 columns a block, eight
+// runs of CTAs side by side.  With such a gate the second sum is S = sum s d u, and dw_out = a(g) S, dg = a'(g) w_out S.
+struct BlockSums {
+  const float *part;
+  int parts, hidden;
+  const void *w_out, *gate;
+  int w_type, gate_type, sigmoid, accumulate;
+  void *dw_in, *dw_out, *dg;       // null: not wanted
+};
+__global__ void __launch_bounds__(256) block_sums_kernel(const BlockSums p) {
+  launch_next();
+  wait_previous();
+  __shared__ float run[8][33];
+  const int lane = threadIdx.x & 31, slice = threadIdx.x >> 5, second = blockIdx.y;
+  const int c = blockIdx.x * 32 + lane;
+  float v = 0.f;
+  if (c < p.hidden) {
+    const float *q = p.part + (long long)second * p.hidden + c;
+#pragma unroll 4
+    for (int i = slice; i < p.parts; i += 8) v += q[(long long)i * 2 * p.hidden];
+  }
+  run[slice][lane] = v;
+  __syncthreads();
+  if (slice || c >= p.hidden) return;
+  for (int i = 1; i < 8; ++i) v += run[i][lane];
+  auto put = [&](void *dst, int type, float x) {
+    if (p.accumulate) x += static_cast<const float *>(dst)[c];    // (fp32 only)
+    block_scalar_store(dst, c, type, x);
+  };
+  if (!second) {
+    if (p.dw_in) put(p.dw_in, p.w_type, v);
+    return;
+  }
+  float a = 1.f, slope = 1.f;
+  if (p.gate) {
+    a = block_scalar(p.gate, c, p.gate_type);
+    if (p.sigmoid) { a = logistic(a); slope = a * (1.f - a); }
+    if (p.dg) put(p.dg, p.gate_type, v * slope * (p.w_out ? block_scalar(p.w_out, c, p.w_type) : 1.f));
+  }
+  if (p.dw_out) put(p.dw_out, p.w_type, v * a);
+}
+
+}  // namespace augtree

@@ -32,15 +32,13 @@
 
 #include <type_traits>
 
-#include "ptx.cuh"
+#include "pair_tile.cuh"
 
 namespace augtree {
 
 enum : int { LM_STATS = 0, LM_GRAD = 1, LM_DH = 2, LM_DW = 3 };
 enum : int { WAIT_LM_FULL = 80, WAIT_LM_EMPTY = 81, WAIT_LM_ACC_FULL = 82, WAIT_LM_ACC_EMPTY = 83 };
 
-constexpr int kLmTile = 256;     // tile rows and columns of a CTA pair
-constexpr int kLmThreads = 320;
 constexpr int kLmMaxJobs = 2;
 
 // One product.  Rows of the compacted token block (their number is known on the device only) take part in every
@@ -77,15 +75,6 @@ struct LmParams {
   int *status;
   long long wait_budget;
   int test_flags;
-};
-
-struct LmSmem {
-  static constexpr int kABytes = 128 * 128, kBBytes = 128 * 128;  // this CTA's share of a stage
-  static constexpr int kStageBytes = kABytes + kBBytes;
-  static constexpr int kStages = 6;
-  static constexpr int kOffOut = kStages * kStageBytes;   // 4 KB a warp on their way out
-  static constexpr int kOffBar = kOffOut + 8 * 4096;
-  static constexpr int kBytes = kOffBar + 256;
 };
 
 // Walks the tiles of one CTA pair: tile t0, t0 + step, .. of all jobs in a row.
@@ -156,21 +145,6 @@ struct LmTile {
     return true;
   }
 };
-
-// A row's columns into the warp's 4 KB block, in the 128-byte swizzle (16-byte chunk j of row r sits at j ^ (r % 8)): 32 columns
-// of 16 bits as the chunks from `chunk`, or 32 columns of 32 bits.
-__device__ __forceinline__ void stage_bf16(uint32_t s_out, int row, int chunk, const float (&x)[32]) {
-#pragma unroll
-  for (int e = 0; e < 4; ++e)
-    st_shared_v4(s_out + row * 128 + (((chunk + e) ^ (row & 7)) << 4), pack_bf16(x[8 * e], x[8 * e + 1]), pack_bf16(x[8 * e + 2], x[8 * e + 3]),
-                 pack_bf16(x[8 * e + 4], x[8 * e + 5]), pack_bf16(x[8 * e + 6], x[8 * e + 7]));
-}
-__device__ __forceinline__ void stage_f32(uint32_t s_out, int row, const float (&x)[32]) {
-#pragma unroll
-  for (int e = 0; e < 8; ++e)
-    st_shared_v4(s_out + row * 128 + ((e ^ (row & 7)) << 4), __float_as_uint(x[4 * e]), __float_as_uint(x[4 * e + 1]),
-                 __float_as_uint(x[4 * e + 2]), __float_as_uint(x[4 * e + 3]));
-}
 
 // Tensor maps: H and W with a box of 64 contiguous hidden columns x 128 rows (contraction contiguous) or (_mn, contraction
 // along the rows) of two such columns x 64 rows, one box for the 128 rows or columns of a stage: two boxes of half the size
