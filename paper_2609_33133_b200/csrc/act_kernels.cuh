@@ -29,6 +29,13 @@ struct Pieces {
 // error below 1e-6 for |g| < 8 and absolute below 1e-6 everywhere, far under the rounding of 16-bit results.
 __device__ __forceinline__ float logistic(float g) { return __fdividef(1.f, 1.f + __expf(-g)); }
 
+__device__ __forceinline__ V8 logistic(const V8 &g) {
+  V8 s;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) s[i] = logistic(g[i]);
+  return s;
+}
+
 struct CkptRows {        // where a checkpoint is read or written
   uint8_t *base;
   long long pitch, scales;
@@ -48,18 +55,14 @@ ckpt_pack_kernel(const In *x, long long ld, const Pieces p, const CkptRows out) 
   launch_next();
   wait_previous();
   const long long first = (long long)blockIdx.x * (kActThreads * kPieces) + threadIdx.x;
-  float v[kPieces][8];
+  V8 v[kPieces];
   long long row[kPieces];
   int piece[kPieces];
   bool ok[kPieces];
 #pragma unroll
   for (int k = 0; k < kPieces; ++k) {
     ok[k] = p.at(first + k * kActThreads, row[k], piece[k]);
-    if (ok[k]) Row8<In>::load(x + row[k] * ld + piece[k] * 8, v[k]);
-    else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[k][i] = 0.f;
-    }
+    v[k] = ok[k] ? Row8<In>::load(x + row[k] * ld + piece[k] * 8) : v8(0.f);
   }
 #pragma unroll
   for (int k = 0; k < kPieces; ++k) {
@@ -92,21 +95,13 @@ ckpt_unpack_kernel(const CkptRows in, const Pieces p, int have, const float *row
 #pragma unroll
   for (int k = 0; k < kPieces; ++k) {
     if (!ok[k]) continue;
-    float v[8];
-    ckpt_decode(q[k], ckpt_unit(byte[k]), v);
-    if (row_factor) {
-      const float r = row_factor[row[k]];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] *= r;
-    }
+    V8 v = ckpt_decode(q[k], ckpt_unit(byte[k]));
+    if (row_factor) v = v * row_factor[row[k]];
     if (col_factor) {
-      float w[8];
       const long long c = piece[k] * 8;
-      if (col_type == T_BF16) Row8<__nv_bfloat16>::load(static_cast<const __nv_bfloat16 *>(col_factor) + c, w);
-      else if (col_type == T_F16) Row8<__half>::load(static_cast<const __half *>(col_factor) + c, w);
-      else Row8<float>::load(static_cast<const float *>(col_factor) + c, w);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] *= w[i];
+      if (col_type == T_BF16) v = v * Row8<__nv_bfloat16>::load(static_cast<const __nv_bfloat16 *>(col_factor) + c);
+      else if (col_type == T_F16) v = v * Row8<__half>::load(static_cast<const __half *>(col_factor) + c);
+      else v = v * Row8<float>::load(static_cast<const float *>(col_factor) + c);
     }
     Row8<Out>::store(out + row[k] * ld + piece[k] * 8, v);
   }
@@ -119,20 +114,15 @@ glu_fwd_kernel(const T *g, const T *u, long long ld, const Pieces p, T *a, long 
   launch_next();
   wait_previous();
   const long long first = (long long)blockIdx.x * (kActThreads * kPieces) + threadIdx.x;
-  float x[kPieces][8], y[kPieces][8];
+  V8 x[kPieces], y[kPieces];
   long long row[kPieces];
   int piece[kPieces];
   bool ok[kPieces];
 #pragma unroll
   for (int k = 0; k < kPieces; ++k) {
     ok[k] = p.at(first + k * kActThreads, row[k], piece[k]);
-    if (ok[k]) {
-      Row8<T>::load(g + row[k] * ld + piece[k] * 8, x[k]);
-      Row8<T>::load(u + row[k] * ld + piece[k] * 8, y[k]);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[k][i] = y[k][i] = 0.f;
-    }
+    x[k] = ok[k] ? Row8<T>::load(g + row[k] * ld + piece[k] * 8) : v8(0.f);
+    y[k] = ok[k] ? Row8<T>::load(u + row[k] * ld + piece[k] * 8) : v8(0.f);
   }
 #pragma unroll
   for (int k = 0; k < kPieces; ++k) {
@@ -145,10 +135,7 @@ glu_fwd_kernel(const T *g, const T *u, long long ld, const Pieces p, T *a, long 
       if (ok[k]) ckpt_u.store(row[k], piece[k], q, byte);
     }
     if (!ok[k]) continue;
-    float v[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = x[k][i] * logistic(x[k][i]) * y[k][i];
-    Row8<T>::store(a + row[k] * cols + piece[k] * 8, v);
+    Row8<T>::store(a + row[k] * cols + piece[k] * 8, x[k] * logistic(x[k]) * y[k]);
   }
 }
 
@@ -160,7 +147,7 @@ glu_bwd_kernel(const T *da, const T *g, const T *u, long long ld, const CkptRows
   launch_next();
   wait_previous();
   const long long first = (long long)blockIdx.x * (kActThreads * kPieces) + threadIdx.x;
-  float d[kPieces][8], x[kPieces][8], y[kPieces][8];
+  V8 d[kPieces], x[kPieces], y[kPieces];
   uint2 qg[kPieces], qu[kPieces];
   uint32_t bg[kPieces], bu[kPieces];
   long long row[kPieces];
@@ -170,37 +157,26 @@ glu_bwd_kernel(const T *da, const T *g, const T *u, long long ld, const CkptRows
   for (int k = 0; k < kPieces; ++k) {
     ok[k] = p.at(first + k * kActThreads, row[k], piece[k]);
     if (!ok[k]) continue;
-    Row8<T>::load(da + row[k] * cols + piece[k] * 8, d[k]);
+    d[k] = Row8<T>::load(da + row[k] * cols + piece[k] * 8);
     if constexpr (kKept) {
       qg[k] = ckpt_g.bytes(row[k], piece[k]); bg[k] = ckpt_g.scale(row[k], piece[k]);
       qu[k] = ckpt_u.bytes(row[k], piece[k]); bu[k] = ckpt_u.scale(row[k], piece[k]);
     } else {
-      Row8<T>::load(g + row[k] * ld + piece[k] * 8, x[k]);
-      Row8<T>::load(u + row[k] * ld + piece[k] * 8, y[k]);
+      x[k] = Row8<T>::load(g + row[k] * ld + piece[k] * 8);
+      y[k] = Row8<T>::load(u + row[k] * ld + piece[k] * 8);
     }
   }
 #pragma unroll
   for (int k = 0; k < kPieces; ++k) {
     if (!ok[k]) continue;
     if constexpr (kKept) {
-      ckpt_decode(qg[k], ckpt_unit(bg[k]), x[k]);
-      ckpt_decode(qu[k], ckpt_unit(bu[k]), y[k]);
+      x[k] = ckpt_decode(qg[k], ckpt_unit(bg[k]));
+      y[k] = ckpt_decode(qu[k], ckpt_unit(bu[k]));
     }
-    float o[8], s[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      s[i] = logistic(x[k][i]);
-      o[i] = d[k][i] * y[k][i] * s[i] * fmaf(x[k][i], 1.f - s[i], 1.f);
-    }
-    Row8<T>::store(dg + row[k] * ld_grad + piece[k] * 8, o);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) { s[i] *= x[k][i]; o[i] = d[k][i] * s[i]; }
-    Row8<T>::store(du + row[k] * ld_grad + piece[k] * 8, o);
-    if (a) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) o[i] = s[i] * y[k][i];
-      Row8<T>::store(a + row[k] * cols + piece[k] * 8, o);
-    }
+    const V8 s = logistic(x[k]), silu = x[k] * s;
+    Row8<T>::store(dg + row[k] * ld_grad + piece[k] * 8, d[k] * y[k] * s * fma(x[k], fma(s, -1.f, v8(1.f)), v8(1.f)));
+    Row8<T>::store(du + row[k] * ld_grad + piece[k] * 8, d[k] * silu);
+    if (a) Row8<T>::store(a + row[k] * cols + piece[k] * 8, silu * y[k]);
   }
 }
 

@@ -75,6 +75,29 @@ int with_type(int type, F f) {
 // ---------------------------------------------------------------- block ends
 int vecs_per_thread(int hidden) { return hidden <= 256 ? 1 : 2; }
 
+bool wide_bwd(int hidden) { return hidden > kBlockBwdWarps * 512; }
+
+// calls f with the kernel for a width and a stream type (kAny: types looked up)
+template <class F>
+int with_fwd(int hidden, int x, F f) {
+  if (vecs_per_thread(hidden) == 1)
+    return x == T_F32 ? f(block_fwd_kernel<1, T_F32, T_BF16>) : x == T_BF16 ? f(block_fwd_kernel<1, T_BF16, T_BF16>) : f(block_fwd_kernel<1, kAny, kAny>);
+  return x == T_F32 ? f(block_fwd_kernel<2, T_F32, T_BF16>) : x == T_BF16 ? f(block_fwd_kernel<2, T_BF16, T_BF16>) : f(block_fwd_kernel<2, kAny, kAny>);
+}
+template <int VPT, int W, class F>
+int with_bwd_types(int x, bool kept, F f) {
+  if (x == T_F32) return kept ? f(block_bwd_kernel<VPT, W, T_F32, T_BF16, true>) : f(block_bwd_kernel<VPT, W, T_F32, T_BF16, false>);
+  if (x == T_BF16) return kept ? f(block_bwd_kernel<VPT, W, T_BF16, T_BF16, true>) : f(block_bwd_kernel<VPT, W, T_BF16, T_BF16, false>);
+  return f(block_bwd_kernel<VPT, W, kAny, kAny, false>);
+}
+template <class F>
+int with_bwd(int hidden, int x, bool kept, F f) {
+  if (vecs_per_thread(hidden) == 1) return with_bwd_types<1, kBlockBwdWarps>(x, kept, f);
+  return wide_bwd(hidden) ? with_bwd_types<2, kBlockBwdWarpsWide>(x, kept, f) : with_bwd_types<2, kBlockBwdWarps>(x, kept, f);
+}
+// what is there has the branch's usual type
+bool bf16_or_none(bool there, int type) { return !there || type == AUGTREE_BF16; }
+
 struct Input { const void *p; int64_t row_bytes; };
 
 // Groups, stages and grid of a call; false if one row of all inputs does not fit shared memory.
@@ -190,9 +213,11 @@ int augtree_block_create(const augtree_block_desc_t *desc, int device, augtree_b
     auto room = [&](auto kernel, int bytes) {
       if (!r && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) r = AUGTREE_ERR_CUDA;
     };
-    room(block_fwd_kernel<1>, kBlockSmem); room(block_fwd_kernel<2>, kBlockSmem);
-    room(block_bwd_kernel<1, kBlockBwdWarps>, kBlockSmem); room(block_bwd_kernel<2, kBlockBwdWarps>, kBlockSmem);
-    room(block_bwd_kernel<2, kBlockBwdWarpsWide>, kBlockSmem);
+    for (int x : {(int)T_F32, (int)T_BF16, kAny})
+      for (int kept = 0; kept < 2; ++kept) {
+        if (!kept) with_fwd(b->hidden, x, [&](auto kernel) { room(kernel, kBlockSmem); return 0; });
+        with_bwd(b->hidden, x, kept, [&](auto kernel) { room(kernel, kBlockSmem); return 0; });
+      }
     room(wgrad_kernel, LmSmem::kBytes);
     if (!r && (cudaMalloc(&b->d_status, 2 * sizeof(int)) != cudaSuccess || cudaMemset(b->d_status, 0, 2 * sizeof(int)) != cudaSuccess)) r = AUGTREE_ERR_CUDA;
     cudaSetDevice(prev);
@@ -266,7 +291,9 @@ int augtree_block_fwd(const augtree_block_t *b, const void *x, int x_dtype, cons
   p.ckpt_y = ckpt_rows(ckpt_y, c); p.ckpt_o = ckpt_rows(ckpt_o, c);
   const int threads = (p.s.groups * p.s.warps_row + 1) * 32;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  return vecs_per_thread(b->hidden) == 1 ? launch(block_fwd_kernel<1>, grid, threads, smem, st, p) : launch(block_fwd_kernel<2>, grid, threads, smem, st, p);
+  // (compiled types: everything of the branch in bf16)
+  const bool usual = bf16_or_none(h, h_dtype) && bf16_or_none(o, o_dtype) && bf16_or_none(p.gate == GATE_FULL, gate_dtype) && x_dtype != AUGTREE_F16;
+  return with_fwd(b->hidden, usual ? x_dtype : kAny, [&](auto kernel) { return launch(kernel, grid, threads, smem, st, p); });
 }
 
 int augtree_block_bwd(const augtree_block_t *b, const void *dy, int x_dtype, const void *dh, int h_dtype, const void *y, int y_dtype,
@@ -313,10 +340,9 @@ int augtree_block_bwd(const augtree_block_t *b, const void *dy, int x_dtype, con
   if (dh) { in[n_in++] = {dh, row_of(h_dtype)}; in[n_in++] = {y, row_of(y_dtype)}; }
   if (o) in[n_in++] = {o, row_of(o_dtype)};
   if (p.gate == GATE_FULL) in[n_in++] = {gate, row_of(gate_dtype)};
-  const bool wide = c > kBlockBwdWarps * 512;
   int grid;
   size_t smem;
-  if (!block_shape(b, n_tokens, in, n_in, !!w_in + !!w_out + channel, wide ? kBlockBwdWarpsWide : kBlockBwdWarps, &p.s, &grid, &smem)) return AUGTREE_ERR_UNSUPPORTED;
+  if (!block_shape(b, n_tokens, in, n_in, !!w_in + !!w_out + channel, wide_bwd(b->hidden) ? kBlockBwdWarpsWide : kBlockBwdWarps, &p.s, &grid, &smem)) return AUGTREE_ERR_UNSUPPORTED;
   p.gate_type = gate_dtype; p.gate_ptr = gate;
   p.w_out = w_out; p.w_in = w_in; p.w_type = w_dtype;
   p.r_out = const_cast<float *>(r_out); p.r_in = const_cast<float *>(r_in);
@@ -325,9 +351,10 @@ int augtree_block_bwd(const augtree_block_t *b, const void *dy, int x_dtype, con
   p.dx = dx; p.d_o = d_o; p.dg = d_gate;
   p.part = static_cast<float *>(ws);
   const int threads = (p.s.groups * p.s.warps_row + 1) * 32;
-  r = vecs_per_thread(b->hidden) == 1 ? launch(block_bwd_kernel<1, kBlockBwdWarps>, grid, threads, smem, st, p)
-      : !wide                         ? launch(block_bwd_kernel<2, kBlockBwdWarps>, grid, threads, smem, st, p)
-                                      : launch(block_bwd_kernel<2, kBlockBwdWarpsWide>, grid, threads, smem, st, p);
+  const bool kept = y_dtype == AUGTREE_CKPT || (!dh && o_dtype == AUGTREE_CKPT);
+  const bool usual = bf16_or_none(dh, h_dtype) && bf16_or_none(d_o, do_dtype) && bf16_or_none(p.gate == GATE_FULL, gate_dtype) && x_dtype != AUGTREE_F16 &&
+                     (!dh || (kept ? y_dtype == AUGTREE_CKPT : y_dtype == x_dtype)) && (!o || o_dtype == (kept ? AUGTREE_CKPT : (int)AUGTREE_BF16));
+  r = with_bwd(b->hidden, usual ? x_dtype : kAny, kept, [&](auto kernel) { return launch(kernel, grid, threads, smem, st, p); });
   const bool second = dw_out || (channel && d_gate);
   if (r || (!dw_in && !second)) return r;
   const BlockSums q = {p.part, grid, b->hidden, w_out, channel ? gate : nullptr, w_dtype, gate_dtype, b->sigmoid, accumulate, dw_in, dw_out, channel ? d_gate : nullptr};

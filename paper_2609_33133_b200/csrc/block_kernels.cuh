@@ -66,17 +66,24 @@ struct BlockParams {
   int test_flags;
 };
 
+// Types are compiled in for the usual pairs of stream and branch (fp32 or bf16 with bf16) and looked up for the others: kAny.  With the
+// look-ups a value cost 60 instructions forward and 90 backward (bf16, checkpoints), and the issue rate was the bound.
+constexpr int kAny = -1;
+
 // 8 columns of a row in shared memory
-__device__ __forceinline__ void block_load8(const uint8_t *row, int vec, int type, int hidden, float (&x)[8]) {
-  if (type == T_BF16) Row8<__nv_bfloat16>::load(reinterpret_cast<const __nv_bfloat16 *>(row) + vec * 8, x);
-  else if (type == T_F32) Row8<float>::load(reinterpret_cast<const float *>(row) + vec * 8, x);
-  else if (type == T_CKPT)
-    ckpt_decode(*reinterpret_cast<const uint2 *>(row + vec * 8), ckpt_unit(row[ckpt_scale_offset(hidden) + (vec >> 2)]), x);
-  else Row8<__half>::load(reinterpret_cast<const __half *>(row) + vec * 8, x);
+template <int T>
+__device__ __forceinline__ V8 block_load8(const uint8_t *row, int vec, int type, int hidden) {
+  const int k = T == kAny ? type : T;
+  if (k == T_BF16) return Row8<__nv_bfloat16>::load(reinterpret_cast<const __nv_bfloat16 *>(row) + vec * 8);
+  if (k == T_F32) return Row8<float>::load(reinterpret_cast<const float *>(row) + vec * 8);
+  if (k == T_CKPT) return ckpt_decode(*reinterpret_cast<const uint2 *>(row + vec * 8), ckpt_unit(row[ckpt_scale_offset(hidden) + (vec >> 2)]));
+  return Row8<__half>::load(reinterpret_cast<const __half *>(row) + vec * 8);
 }
-__device__ __forceinline__ void block_store8(void *base, long long at, int type, const float (&x)[8]) {
-  if (type == T_BF16) Row8<__nv_bfloat16>::store(static_cast<__nv_bfloat16 *>(base) + at, x);
-  else if (type == T_F32) Row8<float>::store(static_cast<float *>(base) + at, x);
+template <int T>
+__device__ __forceinline__ void block_store8(void *base, long long at, int type, const V8 &x) {
+  const int k = T == kAny ? type : T;
+  if (k == T_BF16) Row8<__nv_bfloat16>::store(static_cast<__nv_bfloat16 *>(base) + at, x);
+  else if (k == T_F32) Row8<float>::store(static_cast<float *>(base) + at, x);
   else Row8<__half>::store(static_cast<__half *>(base) + at, x);
 }
 __device__ __forceinline__ float block_scalar(const void *p, long long i, int type) {
@@ -89,10 +96,16 @@ __device__ __forceinline__ void block_scalar_store(void *p, long long i, int typ
   else if (type == T_F32) static_cast<float *>(p)[i] = v;
   else static_cast<__half *>(p)[i] = __float2half_rn(v);
 }
-__device__ __forceinline__ float block_round(float x, int type) {
-  if (type == T_BF16) return Row8<__nv_bfloat16>::round(x);
-  if (type == T_F16) return Row8<__half>::round(x);
-  return x;
+template <int T>
+__device__ __forceinline__ V8 block_round(const V8 &x, int type) {
+  const int k = T == kAny ? type : T;
+  V8 y = x;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (k == T_BF16) y.p[i] = Row8<__nv_bfloat16>::round(x.p[i]);
+    else if (k == T_F16) y.p[i] = Row8<__half>::round(x.p[i]);
+  }
+  return y;
 }
 
 // What the roles of a CTA share.
@@ -129,10 +142,10 @@ __device__ __forceinline__ uint8_t *block_stage(const BlockCta &c, const BlockPa
 __device__ __forceinline__ void block_weights(const BlockCta &c, const BlockParams &p, int slot, const void *w, int type) {
   float *dst = c.weights + slot * p.s.hidden;
   for (int i = threadIdx.x; i < p.s.vecs; i += blockDim.x) {
-    float x[8];
-    if (type == T_BF16) Row8<__nv_bfloat16>::load(static_cast<const __nv_bfloat16 *>(w) + i * 8, x);
-    else if (type == T_F32) Row8<float>::load(static_cast<const float *>(w) + i * 8, x);
-    else Row8<__half>::load(static_cast<const __half *>(w) + i * 8, x);
+    V8 x;
+    if (type == T_BF16) x = Row8<__nv_bfloat16>::load(static_cast<const __nv_bfloat16 *>(w) + i * 8);
+    else if (type == T_F32) x = Row8<float>::load(static_cast<const float *>(w) + i * 8);
+    else x = Row8<__half>::load(static_cast<const __half *>(w) + i * 8);
     reinterpret_cast<float4 *>(dst)[2 * i] = make_float4(x[0], x[1], x[2], x[3]);
     reinterpret_cast<float4 *>(dst)[2 * i + 1] = make_float4(x[4], x[5], x[6], x[7]);
   }
@@ -193,7 +206,14 @@ struct BlockGroup {
   }
 };
 
-template <int VPT>
+// Where a group's row behind row r of block b lies; -1 if there is none.
+__device__ __forceinline__ long long block_next_row(const BlockShape &s, int group, long long b, int r, int rows) {
+  if (r + s.groups < rows) return b * s.block_rows + r + s.groups;
+  const long long row0 = (b + gridDim.x) * s.block_rows;
+  return group < s.block_rows && row0 + group < s.rows ? row0 + group : -1;
+}
+
+template <int VPT, int XT, int OT>
 __global__ void __launch_bounds__((kBlockFwdWarps + 1) * 32, 1)
 block_fwd_kernel(const __grid_constant__ BlockParams p) {
   extern __shared__ __align__(1024) uint8_t smem_raw[];
@@ -202,7 +222,7 @@ block_fwd_kernel(const __grid_constant__ BlockParams p) {
   const BlockCta c = block_setup(smem_raw, p);
   __syncthreads();
   wait_previous();
-  // slots of the vectors: w_in, w_out, gate of a channel (with the residual scale)
+  // slots of the vectors: w_in, w_out, gate of a channel
   const int slot_out = p.w_in ? 1 : 0, slot_gate = slot_out + (p.w_out ? 1 : 0);
   if (p.w_in) block_weights(c, p, 0, p.w_in, p.w_type);
   if (p.w_out) block_weights(c, p, slot_out, p.w_out, p.w_type);
@@ -216,8 +236,11 @@ block_fwd_kernel(const __grid_constant__ BlockParams p) {
     const int group = warp / s.warps_row;
     BlockGroup g{c.sums + group * 64, s.warps_row, warp - group * s.warps_row, group + 1, 0};
     const int v0 = g.warp * 32 + lane, step = s.warps_row * 32;     // pieces v0, v0 + step
+    const bool writer = g.warp == 0 && lane == 0, token = p.gate == GATE_TOKEN;
     int st = 0;
     uint32_t phase = 0;
+    long long t = (long long)blockIdx.x * s.block_rows + group;
+    float gt_next = token && group < s.block_rows && t < s.rows ? block_scalar(p.gate_ptr, t, p.gate_type) : 0.f;
     for (long long b = blockIdx.x; b < s.blocks; b += gridDim.x) {
       const long long row0 = b * s.block_rows;
       const int rows = (int)min((long long)s.block_rows, s.rows - row0);
@@ -226,40 +249,29 @@ block_fwd_kernel(const __grid_constant__ BlockParams p) {
       mbar_wait(c.bar_full + 8 * st, phase, ab, WAIT_BLOCK_FULL);
       const uint8_t *stage = block_stage(c, p, st);
       for (int r = group; r < rows; r += s.groups) {
-        const long long t = row0 + r;
-        const uint8_t *rx = stage + s.offset[0] + (long long)r * s.row_bytes[0], *ro = stage + s.offset[1] + (long long)r * s.row_bytes[1];
-        const uint8_t *rg = stage + s.offset[2] + (long long)r * s.row_bytes[2];
-        float y[VPT][8], r_o = 1.f;
-#pragma unroll
-        for (int k = 0; k < VPT; ++k) {
-          const int v = v0 + k * step;
-          if (v < s.vecs) block_load8(rx, v, p.x_type, s.hidden, y[k]);
-          else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) y[k][i] = 0.f;
-          }
+        t = row0 + r;
+        const uint8_t *rx = stage + s.offset[0] + r * s.row_bytes[0], *ro = stage + s.offset[1] + r * s.row_bytes[1];
+        const uint8_t *rg = stage + s.offset[2] + r * s.row_bytes[2];
+        float ga = p.scale;
+        if (token) {     // (the next row's gate is on its way while this row is worked on)
+          ga *= p.sigmoid ? logistic(gt_next) : gt_next;
+          const long long next = block_next_row(s, group, b, r, rows);
+          if (next >= 0) gt_next = block_scalar(p.gate_ptr, next, p.gate_type);
         }
+        V8 y[VPT];
         if (p.has_branch) {
-          float o[VPT][8], ga = p.scale;
-          if (p.gate == GATE_TOKEN) {
-            const float gt = block_scalar(p.gate_ptr, t, p.gate_type);
-            ga *= p.sigmoid ? logistic(gt) : gt;
-          }
-          float ss = 0.f;
+          V8 o[VPT];
+          float2 ss = both(0.f);
+          float r_o = 1.f;
 #pragma unroll
           for (int k = 0; k < VPT; ++k) {
             const int v = v0 + k * step;
-            if (v < s.vecs) block_load8(ro, v, p.o_type, s.hidden, o[k]);
-            else {
-#pragma unroll
-              for (int i = 0; i < 8; ++i) o[k][i] = 0.f;
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) ss = fmaf(o[k][i], o[k][i], ss);
+            o[k] = v < s.vecs ? block_load8<OT>(ro, v, p.o_type, s.hidden) : v8(0.f);
+            ss = dot2(o[k], o[k], ss);
           }
           if (p.w_out) {
-            r_o = rsqrtf(fmaf(g.sum(ss), p.inv_hidden, p.eps));
-            if (p.r_out && g.warp == 0 && lane == 0) p.r_out[t] = r_o;
+            r_o = rsqrtf(fmaf(g.sum(ss.x + ss.y), p.inv_hidden, p.eps));
+            if (p.r_out && writer) p.r_out[t] = r_o;
           }
           if (p.ckpt_o.base) {
 #pragma unroll
@@ -274,51 +286,44 @@ block_fwd_kernel(const __grid_constant__ BlockParams p) {
 #pragma unroll
           for (int k = 0; k < VPT; ++k) {
             const int v = v0 + k * step;
-            if (v >= s.vecs) continue;
-            if (p.w_out) {
-              float w[8];
-              Row8<float>::load(c.weights + slot_out * s.hidden + v * 8, w);
-#pragma unroll
-              for (int i = 0; i < 8; ++i) o[k][i] = w[i] * (o[k][i] * r_o);
+            if (v < s.vecs) {
+              if (p.w_out) o[k] = Row8<float>::load(c.weights + slot_out * s.hidden + v * 8) * (o[k] * r_o);
+              if (p.gate >= GATE_CHANNEL) {
+                const V8 a = p.gate == GATE_FULL ? block_load8<OT>(rg, v, p.gate_type, s.hidden) : Row8<float>::load(c.weights + slot_gate * s.hidden + v * 8);
+                o[k] = o[k] * (p.sigmoid ? logistic(a) : a);
+              }
+              y[k] = fma(o[k], ga, block_load8<XT>(rx, v, p.x_type, s.hidden));
+              block_store8<XT>(p.y, t * s.hidden + v * 8, p.x_type, y[k]);
+            } else {
+              y[k] = v8(0.f);
             }
-            if (p.gate >= GATE_CHANNEL) {
-              float a[8];
-              if (p.gate == GATE_FULL) block_load8(rg, v, p.gate_type, s.hidden, a);
-              else Row8<float>::load(c.weights + slot_gate * s.hidden + v * 8, a);
+          }
+        } else {
 #pragma unroll
-              for (int i = 0; i < 8; ++i) o[k][i] *= p.sigmoid ? logistic(a[i]) : a[i];
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) y[k][i] = fmaf(ga, o[k][i], y[k][i]);
-            if (p.y) block_store8(p.y, t * s.hidden + v * 8, p.x_type, y[k]);
+          for (int k = 0; k < VPT; ++k) {
+            const int v = v0 + k * step;
+            y[k] = v < s.vecs ? block_load8<XT>(rx, v, p.x_type, s.hidden) : v8(0.f);
           }
         }
-        float r_i = 1.f;
         if (p.w_in) {
-          float ss = 0.f;
+          float2 ss = both(0.f);
 #pragma unroll
-          for (int k = 0; k < VPT; ++k)
+          for (int k = 0; k < VPT; ++k) ss = dot2(y[k], y[k], ss);
+          const float r_i = rsqrtf(fmaf(g.sum(ss.x + ss.y), p.inv_hidden, p.eps));
+          if (p.r_in && writer) p.r_in[t] = r_i;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) ss = fmaf(y[k][i], y[k][i], ss);
-          r_i = rsqrtf(fmaf(g.sum(ss), p.inv_hidden, p.eps));
-          if (p.r_in && g.warp == 0 && lane == 0) p.r_in[t] = r_i;
-        }
-#pragma unroll
-        for (int k = 0; k < VPT; ++k) {
-          const int v = v0 + k * step;
-          if (p.w_in && v < s.vecs) {
-            float w[8], h[8];
-            Row8<float>::load(c.weights + v * 8, w);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) h[i] = w[i] * (y[k][i] * r_i);
-            block_store8(p.h, t * s.hidden + v * 8, p.h_type, h);
+          for (int k = 0; k < VPT; ++k) {
+            const int v = v0 + k * step;
+            if (v < s.vecs) block_store8<OT>(p.h, t * s.hidden + v * 8, p.h_type, Row8<float>::load(c.weights + v * 8) * (y[k] * r_i));
           }
-          if (p.ckpt_y.base) {
+        }
+        if (p.ckpt_y.base) {
+#pragma unroll
+          for (int k = 0; k < VPT; ++k) {
+            const int v = v0 + k * step;
             uint2 q;
             uint32_t byte;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) y[k][i] = block_round(y[k][i], p.x_type);
-            ckpt_encode(y[k], q, byte);
+            ckpt_encode(block_round<XT>(y[k], p.x_type), q, byte);
             if (v < s.vecs) p.ckpt_y.store(t, v, q, byte);
           }
         }
@@ -330,10 +335,12 @@ block_fwd_kernel(const __grid_constant__ BlockParams p) {
   block_leave(c);
 }
 
-template <int VPT, int kWarps>
+// kKept: v and u are read from checkpoints, both (with kAny each from what its type says).
+template <int VPT, int kWarps, int XT, int OT, bool kKept>
 __global__ void __launch_bounds__((kWarps + 1) * 32, 1)
 block_bwd_kernel(const __grid_constant__ BlockParams p) {
   extern __shared__ __align__(1024) uint8_t smem_raw[];
+  constexpr int YT = XT == kAny ? kAny : kKept ? (int)T_CKPT : XT, ST = OT == kAny ? kAny : kKept ? (int)T_CKPT : OT;   // of the saved y and o
   const BlockShape &s = p.s;
   launch_next();
   const BlockCta c = block_setup(smem_raw, p);
@@ -346,15 +353,13 @@ block_bwd_kernel(const __grid_constant__ BlockParams p) {
   __syncthreads();
   const AbortCtx ab{c.abort_flag, p.status, p.wait_budget};
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  float acc_in[VPT][8], acc_out[VPT][8];
+  V8 acc_in[VPT], acc_out[VPT];
 #pragma unroll
-  for (int k = 0; k < VPT; ++k)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) acc_in[k][i] = acc_out[k][i] = 0.f;
+  for (int k = 0; k < VPT; ++k) acc_in[k] = acc_out[k] = v8(0.f);
   const int group = warp / s.warps_row;
   BlockGroup g{c.sums + group * 64, s.warps_row, warp - group * s.warps_row, group + 1, 0};
   const int v0 = g.warp * 32 + lane, step = s.warps_row * 32;
-  const bool computes = group < s.groups;
+  const bool computes = group < s.groups, writer = g.warp == 0 && lane == 0, token = p.gate == GATE_TOKEN;
   if (!computes) {
     if (lane == 0) block_produce(c, p, ab);
     __syncwarp();
@@ -363,6 +368,16 @@ block_bwd_kernel(const __grid_constant__ BlockParams p) {
     uint32_t phase = 0;
     // inputs in the order that the host lists them: dy, dh, y, o, gate, each only where there is one
     const int at_dh = p.has_dy, at_y = at_dh + p.has_dh, at_o = at_y + p.has_dh, at_g = at_o + p.has_branch;
+    // a row's numbers, fetched while the row before it is worked on
+    float ri_next = 0.f, ro_next = 1.f, gt_next = 1.f;
+    auto fetch = [&](long long t) {
+      if (t < 0) return;
+      if (p.has_dh) ri_next = p.r_in[t];
+      if (p.w_out) ro_next = p.r_out[t];
+      if (token) gt_next = block_scalar(p.gate_ptr, t, p.gate_type);
+    };
+    const long long first = (long long)blockIdx.x * s.block_rows + group;
+    fetch(group < s.block_rows && first < s.rows ? first : -1);
     for (long long b = blockIdx.x; b < s.blocks; b += gridDim.x) {
       const long long row0 = b * s.block_rows;
       const int rows = (int)min((long long)s.block_rows, s.rows - row0);
@@ -370,116 +385,79 @@ block_bwd_kernel(const __grid_constant__ BlockParams p) {
       const uint8_t *stage = block_stage(c, p, st);
       for (int r = group; r < rows; r += s.groups) {
         const long long t = row0 + r;
-        auto row = [&](int i) { return stage + s.offset[i] + (long long)r * s.row_bytes[i]; };
-        const float r_i = p.has_dh ? p.r_in[t] : 0.f, r_o = p.w_out ? p.r_out[t] : 1.f;
-        float gt = 1.f;
-        if (p.gate == GATE_TOKEN) gt = block_scalar(p.gate_ptr, t, p.gate_type);
-        const float at = p.gate == GATE_TOKEN ? (p.sigmoid ? logistic(gt) : gt) : 1.f;
-        float d[VPT][8];
-#pragma unroll
-        for (int k = 0; k < VPT; ++k) {
-          const int v = v0 + k * step;
-          if (p.has_dy && v < s.vecs) block_load8(row(0), v, p.x_type, s.hidden, d[k]);
-          else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) d[k][i] = 0.f;
-          }
-        }
+        auto row = [&](int i) { return stage + s.offset[i] + r * s.row_bytes[i]; };
+        const float r_i = ri_next, r_o = ro_next, at = token && p.sigmoid ? logistic(gt_next) : gt_next;
+        fetch(block_next_row(s, group, b, r, rows));
+        V8 d[VPT];
         if (p.has_dh) {
-          // the sum with y itself; its norm comes in behind the reduction
-          float dot = 0.f;
+          V8 v[VPT];
+          float2 dot = both(0.f);
 #pragma unroll
           for (int k = 0; k < VPT; ++k) {
-            const int v = v0 + k * step;
-            if (v >= s.vecs) continue;
-            float dh[8], y[8], w[8];
-            block_load8(row(at_dh), v, p.h_type, s.hidden, dh);
-            block_load8(row(at_y), v, p.y_type, s.hidden, y);
-            Row8<float>::load(c.weights + v * 8, w);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              y[i] *= r_i;
-              acc_in[k][i] = fmaf(dh[i], y[i], acc_in[k][i]);
-              dot = fmaf(w[i] * dh[i], y[i], dot);
+            const int at8 = v0 + k * step;
+            if (at8 < s.vecs) {
+              const V8 dh = block_load8<OT>(row(at_dh), at8, p.h_type, s.hidden);
+              v[k] = block_load8<YT>(row(at_y), at8, p.y_type, s.hidden) * r_i;
+              acc_in[k] = fma(dh, v[k], acc_in[k]);
+              d[k] = Row8<float>::load(c.weights + at8 * 8) * dh;
+            } else {
+              v[k] = d[k] = v8(0.f);
             }
+            dot = dot2(d[k], v[k], dot);
           }
-          const float mean = g.sum(dot) * p.inv_hidden;
+          const float mean = g.sum(dot.x + dot.y) * p.inv_hidden;
 #pragma unroll
-          for (int k = 0; k < VPT; ++k) {
-            const int v = v0 + k * step;
-            if (v >= s.vecs) continue;
-            float dh[8], y[8], w[8];
-            block_load8(row(at_dh), v, p.h_type, s.hidden, dh);
-            block_load8(row(at_y), v, p.y_type, s.hidden, y);
-            Row8<float>::load(c.weights + v * 8, w);
+          for (int k = 0; k < VPT; ++k) d[k] = fma(v[k], -mean, d[k]) * r_i;
+        } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) d[k][i] = fmaf(r_i, fmaf(-mean, y[i] * r_i, w[i] * dh[i]), d[k][i]);
-          }
+          for (int k = 0; k < VPT; ++k) d[k] = v8(0.f);
         }
 #pragma unroll
         for (int k = 0; k < VPT; ++k) {
-          const int v = v0 + k * step;
-          if (v < s.vecs && p.dx) block_store8(p.dx, t * s.hidden + v * 8, p.x_type, d[k]);
+          const int at8 = v0 + k * step;
+          if (at8 >= s.vecs) continue;
+          if (p.has_dy) d[k] = d[k] + block_load8<XT>(row(0), at8, p.x_type, s.hidden);
+          if (p.dx) block_store8<XT>(p.dx, t * s.hidden + at8 * 8, p.x_type, d[k]);
         }
         if (p.has_branch) {
-          float dot = 0.f;    // sum of w_o q u (a): what the norm and a gate of one number a token need
+          V8 u[VPT];
+          float2 dot = both(0.f);    // sum of w_o q u a(g), without the a(g) of a token
 #pragma unroll
           for (int k = 0; k < VPT; ++k) {
-            const int v = v0 + k * step;
-            if (v >= s.vecs) continue;
-            float u[8], w[8], a[8], da[8];
-            block_load8(row(at_o), v, p.o_type, s.hidden, u);
-            if (p.w_out) Row8<float>::load(c.weights + slot_out * s.hidden + v * 8, w);
+            const int at8 = v0 + k * step;
+            if (at8 >= s.vecs) { u[k] = v8(0.f); continue; }
+            const V8 q = d[k] * p.scale;
+            u[k] = block_load8<ST>(row(at_o), at8, p.o_type, s.hidden) * r_o;
             if (p.gate >= GATE_CHANNEL) {
-              if (p.gate == GATE_FULL) block_load8(row(at_g), v, p.gate_type, s.hidden, a);
-              else Row8<float>::load(c.weights + slot_gate * s.hidden + v * 8, a);
-              if (p.sigmoid) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) { a[i] = logistic(a[i]); da[i] = a[i] * (1.f - a[i]); }
-              } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) da[i] = 1.f;
+              V8 a = p.gate == GATE_FULL ? block_load8<OT>(row(at_g), at8, p.gate_type, s.hidden) : Row8<float>::load(c.weights + slot_gate * s.hidden + at8 * 8);
+              if (p.sigmoid) a = logistic(a);
+              const V8 qa = q * a, w = p.w_out ? Row8<float>::load(c.weights + slot_out * s.hidden + at8 * 8) : v8(1.f);
+              acc_out[k] = fma(p.gate == GATE_CHANNEL ? q : qa, u[k], acc_out[k]);
+              d[k] = w * qa;
+              if (p.gate == GATE_FULL && p.dg) {
+                V8 dg = q * (w * u[k]);
+                if (p.sigmoid) dg = dg * (a * fma(a, -1.f, v8(1.f)));
+                block_store8<OT>(p.dg, t * s.hidden + at8 * 8, p.gate_type, dg);
               }
             } else {
-#pragma unroll
-              for (int i = 0; i < 8; ++i) a[i] = at;
+              acc_out[k] = fma(q * at, u[k], acc_out[k]);
+              d[k] = p.w_out ? Row8<float>::load(c.weights + slot_out * s.hidden + at8 * 8) * q : q;
             }
-            float dg[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const float q = p.scale * d[k][i];
-              u[i] *= r_o;
-              const float wu = p.w_out ? w[i] * u[i] : u[i];
-              dg[i] = q * wu;                                        // d a(g)
-              dot = fmaf(dg[i], p.gate >= GATE_CHANNEL ? a[i] : 1.f, dot);
-              acc_out[k][i] = fmaf(p.gate == GATE_CHANNEL ? q : q * a[i], u[i], acc_out[k][i]);
-              d[k][i] = (p.w_out ? w[i] : 1.f) * (q * a[i]);         // d u
-            }
-            if (p.gate == GATE_FULL && p.dg) {
-#pragma unroll
-              for (int i = 0; i < 8; ++i) dg[i] *= da[i];
-              block_store8(p.dg, t * s.hidden + v * 8, p.gate_type, dg);
-            }
+            dot = dot2(d[k], u[k], dot);
           }
           float mean = 0.f;
-          if (p.w_out || p.gate == GATE_TOKEN) {
-            const float total = g.sum(dot);
-            mean = total * at * p.inv_hidden;
-            if (p.gate == GATE_TOKEN && p.dg && g.warp == 0 && lane == 0)
-              block_scalar_store(p.dg, t, p.gate_type, total * (p.sigmoid ? at * (1.f - at) : 1.f));
+          if (p.w_out || token) {
+            const float total = g.sum(dot.x + dot.y);
+            mean = total * p.inv_hidden;
+            if (token && p.dg && writer) block_scalar_store(p.dg, t, p.gate_type, total * (p.sigmoid ? at * (1.f - at) : 1.f));
           }
           if (p.d_o) {
+            const float f = r_o * at;      // (1 without a norm, 1 without a gate of one number a token)
 #pragma unroll
             for (int k = 0; k < VPT; ++k) {
-              const int v = v0 + k * step;
-              if (v >= s.vecs) continue;
-              if (p.w_out) {
-                float u[8];
-                block_load8(row(at_o), v, p.o_type, s.hidden, u);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) d[k][i] = r_o * fmaf(-mean, u[i] * r_o, d[k][i]);
-              }
-              block_store8(p.d_o, t * s.hidden + v * 8, p.do_type, d[k]);
+              const int at8 = v0 + k * step;
+              if (at8 >= s.vecs) continue;
+              block_store8<OT>(p.d_o, t * s.hidden + at8 * 8, p.do_type, (p.w_out ? fma(u[k], -mean, d[k]) : d[k]) * f);
             }
           }
         }

@@ -21,46 +21,77 @@ enum : int { T_BF16 = 0, T_F16 = 1, T_F32 = 2, T_CKPT = 3 };   // as AUGTREE_BF1
 __host__ __device__ inline long long ckpt_scale_offset(long long cols) { return (cols + 15) / 16 * 16; }
 __host__ __device__ inline long long ckpt_pitch(long long cols) { return ckpt_scale_offset(cols) + ((cols + 31) / 32 + 15) / 16 * 16; }
 
-// ---------------------------------------------------------------- 8 values to and from memory
+// ---------------------------------------------------------------- 8 values in registers
+// In pairs, for the packed fp32 instructions of sm_100 (one issue slot for two values: these kernels are as near to the issue rate as
+// to the memory's).
+struct V8 {
+  float2 p[4];
+  __device__ __forceinline__ float &operator[](int i) { return (i & 1) ? p[i >> 1].y : p[i >> 1].x; }
+  __device__ __forceinline__ float operator[](int i) const { return (i & 1) ? p[i >> 1].y : p[i >> 1].x; }
+};
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+__device__ __forceinline__ V8 v8(float x) { return {{both(x), both(x), both(x), both(x)}}; }
+__device__ __forceinline__ V8 operator*(const V8 &a, const V8 &b) {
+  return {{__fmul2_rn(a.p[0], b.p[0]), __fmul2_rn(a.p[1], b.p[1]), __fmul2_rn(a.p[2], b.p[2]), __fmul2_rn(a.p[3], b.p[3])}};
+}
+__device__ __forceinline__ V8 operator*(const V8 &a, float s) { return a * v8(s); }
+__device__ __forceinline__ V8 operator+(const V8 &a, const V8 &b) {
+  return {{__fadd2_rn(a.p[0], b.p[0]), __fadd2_rn(a.p[1], b.p[1]), __fadd2_rn(a.p[2], b.p[2]), __fadd2_rn(a.p[3], b.p[3])}};
+}
+__device__ __forceinline__ V8 fma(const V8 &a, const V8 &b, const V8 &c) {
+  return {{__ffma2_rn(a.p[0], b.p[0], c.p[0]), __ffma2_rn(a.p[1], b.p[1], c.p[1]), __ffma2_rn(a.p[2], b.p[2], c.p[2]), __ffma2_rn(a.p[3], b.p[3], c.p[3])}};
+}
+__device__ __forceinline__ V8 fma(const V8 &a, float s, const V8 &c) { return fma(a, v8(s), c); }
+__device__ __forceinline__ float2 dot2(const V8 &a, const V8 &b, float2 s) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) s = __ffma2_rn(a.p[i], b.p[i], s);
+  return s;
+}
+
+// ---------------------------------------------------------------- to and from memory
 template <typename T> struct Row8;
 template <> struct Row8<__nv_bfloat16> {
-  static __device__ __forceinline__ void unpack(uint4 w, float (&x)[8]) {
-    const uint32_t v[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(v[i] << 16); x[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u); }
-  }
-  static __device__ __forceinline__ uint4 pack(const float (&x)[8]) {
-    return make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
-  }
-  static __device__ __forceinline__ void load(const __nv_bfloat16 *p, float (&x)[8]) { unpack(*reinterpret_cast<const uint4 *>(p), x); }
-  static __device__ __forceinline__ void store(__nv_bfloat16 *p, const float (&x)[8]) { *reinterpret_cast<uint4 *>(p) = pack(x); }
-  static __device__ __forceinline__ float round(float x) { return __bfloat162float(__float2bfloat16_rn(x)); }
-};
-template <> struct Row8<__half> {
-  static __device__ __forceinline__ void load(const __half *p, float (&x)[8]) {
+  static __device__ __forceinline__ V8 load(const __nv_bfloat16 *p) {
     const uint4 w = *reinterpret_cast<const uint4 *>(p);
     const uint32_t v[4] = {w.x, w.y, w.z, w.w};
+    V8 x;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&v[i]));
-      x[2 * i] = f.x; x[2 * i + 1] = f.y;
-    }
+    for (int i = 0; i < 4; ++i) x.p[i] = make_float2(__uint_as_float(v[i] << 16), __uint_as_float(v[i] & 0xffff0000u));
+    return x;
   }
-  static __device__ __forceinline__ void store(__half *p, const float (&x)[8]) {
+  static __device__ __forceinline__ void store(__nv_bfloat16 *p, const V8 &x) {
+    *reinterpret_cast<uint4 *>(p) = make_uint4(pack_bf16(x.p[0].x, x.p[0].y), pack_bf16(x.p[1].x, x.p[1].y), pack_bf16(x.p[2].x, x.p[2].y),
+                                               pack_bf16(x.p[3].x, x.p[3].y));
+  }
+  static __device__ __forceinline__ float2 round(float2 x) {
+    const uint32_t w = pack_bf16(x.x, x.y);
+    return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+  }
+};
+template <> struct Row8<__half> {
+  static __device__ __forceinline__ V8 load(const __half *p) {
+    const uint4 w = *reinterpret_cast<const uint4 *>(p);
+    const uint32_t v[4] = {w.x, w.y, w.z, w.w};
+    V8 x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x.p[i] = __half22float2(*reinterpret_cast<const __half2 *>(&v[i]));
+    return x;
+  }
+  static __device__ __forceinline__ void store(__half *p, const V8 &x) {
     uint32_t v[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) { const __half2 h = __floats2half2_rn(x[2 * i], x[2 * i + 1]); v[i] = *reinterpret_cast<const uint32_t *>(&h); }
+    for (int i = 0; i < 4; ++i) { const __half2 h = __floats2half2_rn(x.p[i].x, x.p[i].y); v[i] = *reinterpret_cast<const uint32_t *>(&h); }
     *reinterpret_cast<uint4 *>(p) = make_uint4(v[0], v[1], v[2], v[3]);
   }
-  static __device__ __forceinline__ float round(float x) { return __half2float(__float2half_rn(x)); }
+  static __device__ __forceinline__ float2 round(float2 x) { return __half22float2(__floats2half2_rn(x.x, x.y)); }
 };
 template <> struct Row8<float> {
-  static __device__ __forceinline__ void load(const float *p, float (&x)[8]) {
+  static __device__ __forceinline__ V8 load(const float *p) {
     const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
-    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+    return {{make_float2(a.x, a.y), make_float2(a.z, a.w), make_float2(b.x, b.y), make_float2(b.z, b.w)}};
   }
   // (base pointers are aligned to 16 bytes, not to the 32 of one wide store)
-  static __device__ __forceinline__ void store(float *p, const float (&x)[8]) {
+  static __device__ __forceinline__ void store(float *p, const V8 &x) {
     if ((reinterpret_cast<uintptr_t>(p) & 31) == 0) {
       uint32_t w[8];
 #pragma unroll
@@ -71,41 +102,48 @@ template <> struct Row8<float> {
       reinterpret_cast<float4 *>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
     }
   }
-  static __device__ __forceinline__ float round(float x) { return x; }
+  static __device__ __forceinline__ float2 round(float2 x) { return x; }
 };
 
 // ---------------------------------------------------------------- the 8-bit form
+// max(a, |b|, |c|), NaN if one of them is
+__device__ __forceinline__ float max_magnitude(float a, float b, float c) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(fabsf(b)), "f"(fabsf(c)));
+  return d;
+}
 // 8 columns of a thread; the four threads of a lane quad hold a group of 32.  Every lane of the warp takes part; columns behind the
 // row's end are zero.
-__device__ __forceinline__ void ckpt_encode(const float (&x)[8], uint2 &q, uint32_t &byte) {
-  uint32_t m = 0;
+__device__ __forceinline__ void ckpt_encode(const V8 &x, uint2 &q, uint32_t &byte) {
+  float top = 0.f;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(x[i]) & 0x7fffffffu);   // magnitudes order like their bits, NaN on top
+  for (int i = 0; i < 4; ++i) top = max_magnitude(top, x.p[i].x, x.p[i].y);
+  uint32_t m = __float_as_uint(top);           // magnitudes order like their bits, infinity and NaN on top
   m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
   m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
   const bool finite = m < 0x7f800000u;
   // m = f 2^k, 1 <= f < 2: e = k - 6, one more from f = 127.5 / 64 on, where the added bits carry into the exponent
-  const int biased = (int)((m + 0x10000u) >> 23);
-  byte = finite ? (uint32_t)max(biased - 6, 1) : 255u;
+  byte = finite ? (uint32_t)max((int)((m + 0x10000u) >> 23) - 6, 1) : 255u;
   const float per = finite ? __uint_as_float((254u - byte) << 23) : 0.f;          // 2^-e
-  uint32_t b[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) b[i] = __float_as_uint(fmaf(x[i], per, 12582912.f));  // + 1.5 2^23: the integer in the low bits
+  const V8 b = fma(x, per, v8(12582912.f));    // + 1.5 2^23: the integer in the low bits
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    const uint32_t lo = __byte_perm(b[4 * h], b[4 * h + 1], 0x0040), hi = __byte_perm(b[4 * h + 2], b[4 * h + 3], 0x0040);
+    const uint32_t lo = __byte_perm(__float_as_uint(b.p[2 * h].x), __float_as_uint(b.p[2 * h].y), 0x0040);
+    const uint32_t hi = __byte_perm(__float_as_uint(b.p[2 * h + 1].x), __float_as_uint(b.p[2 * h + 1].y), 0x0040);
     (h ? q.y : q.x) = __byte_perm(lo, hi, 0x5410);
   }
 }
 __device__ __forceinline__ float ckpt_unit(uint32_t byte) {   // 2^e
-  return byte == 255u ? __uint_as_float(0x7fffffffu) : __uint_as_float(byte << 23);
+  return __uint_as_float(byte == 255u ? 0x7fffffffu : byte << 23);
 }
-__device__ __forceinline__ void ckpt_decode(uint2 q, float unit, float (&x)[8]) {
+// The values times a number: (2^e q) factor with one rounding, as 2^e factor is exact.
+__device__ __forceinline__ V8 ckpt_decode(uint2 q, float unit) {
   // the byte q + 128 in the low bits of 2^23 is 2^23 + 128 + q; both steps are exact
   const uint32_t w[2] = {q.x ^ 0x80808080u, q.y ^ 0x80808080u};
+  V8 x;
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
-    x[i] = (__uint_as_float(__byte_perm(w[i >> 2], 0x4b000000u, 0x7650 | (i & 3))) - 8388736.f) * unit;
+  for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(__byte_perm(w[i >> 2], 0x4b000000u, 0x7650 | (i & 3)));
+  return (x + v8(-8388736.f)) * unit;
 }
 
 }  // namespace augtree

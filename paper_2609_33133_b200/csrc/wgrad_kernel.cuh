@@ -232,26 +232,15 @@ wgrad_join_kernel(const float *part, int splits, long long part_rows, int out, i
   wait_previous();
   const long long vecs = cols / 8, total = out * vecs, stride = part_rows * cols;
   for (long long i = blockIdx.x * 256ll + threadIdx.x; i < total; i += gridDim.x * 256ll) {
-    float x[8];
-    Row8<float>::load(part + i * 8, x);
-    for (int s = 1; s < splits; ++s) {
-      float y[8];
-      Row8<float>::load(part + s * stride + i * 8, y);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] += y[e];
-    }
+    V8 x = Row8<float>::load(part + i * 8);
+    for (int s = 1; s < splits; ++s) x = x + Row8<float>::load(part + s * stride + i * 8);
     if (col) {
       const long long c0 = i % vecs * 8;
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[e] *= block_scalar(col, c0 + e, col_type);
     }
-    if (add) {
-      float y[8];
-      Row8<float>::load(static_cast<const float *>(dw) + i * 8, y);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] += y[e];
-    }
-    block_store8(dw, i * 8, type, x);
+    if (add) x = x + Row8<float>::load(static_cast<const float *>(dw) + i * 8);
+    block_store8<kAny>(dw, i * 8, type, x);
   }
 }
 
