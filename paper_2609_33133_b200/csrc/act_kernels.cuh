@@ -48,6 +48,16 @@ struct CkptRows {        // where a checkpoint is read or written
   __device__ __forceinline__ uint32_t scale(long long row, int piece) const { return base[row * pitch + scales + (piece >> 2)]; }
 };
 
+// 8 columns of a row's checkpoint; every lane of the warp takes part, pieces from `valid` on are not written
+__device__ __forceinline__ void ckpt_store(uint8_t *row, int piece, int valid, long long scales, const V8 &x) {
+  uint2 q;
+  uint32_t byte;
+  ckpt_encode(x, q, byte);
+  if (piece >= valid) return;
+  *reinterpret_cast<uint2 *>(row + piece * 8) = q;
+  if ((piece & 3) == 0) row[scales + (piece >> 2)] = (uint8_t)byte;
+}
+
 template <typename In>
 __global__ void __launch_bounds__(kActThreads)
 ckpt_pack_kernel(const In *x, long long ld, const Pieces p, const CkptRows out) {

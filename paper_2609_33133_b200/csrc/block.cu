@@ -77,23 +77,45 @@ int vecs_per_thread(int hidden) { return hidden <= 256 ? 1 : 2; }
 
 bool wide_bwd(int hidden) { return hidden > kBlockBwdWarps * 512; }
 
-// calls f with the kernel for a width and a stream type (kAny: types looked up)
-template <class F>
-int with_fwd(int hidden, int x, F f) {
-  if (vecs_per_thread(hidden) == 1)
-    return x == T_F32 ? f(block_fwd_kernel<1, T_F32, T_BF16>) : x == T_BF16 ? f(block_fwd_kernel<1, T_BF16, T_BF16>) : f(block_fwd_kernel<1, kAny, kAny>);
-  return x == T_F32 ? f(block_fwd_kernel<2, T_F32, T_BF16>) : x == T_BF16 ? f(block_fwd_kernel<2, T_BF16, T_BF16>) : f(block_fwd_kernel<2, kAny, kAny>);
+// calls f with the kernel for a width, a stream type (kAny: types looked up), a form of the call and a gate
+template <int VPT, int X, class F>
+int with_fwd_form(int form, int gate, F f) {
+  if (form == kBefore) return f(block_fwd_kernel<VPT, X, T_BF16, kBefore, GATE_NONE>);
+  if (gate == GATE_NONE) return f(block_fwd_kernel<VPT, X, T_BF16, kBoth, GATE_NONE>);
+  if (gate == GATE_TOKEN) return f(block_fwd_kernel<VPT, X, T_BF16, kBoth, GATE_TOKEN>);
+  if (gate == GATE_CHANNEL) return f(block_fwd_kernel<VPT, X, T_BF16, kBoth, GATE_CHANNEL>);
+  return f(block_fwd_kernel<VPT, X, T_BF16, kBoth, GATE_FULL>);
 }
-template <int VPT, int W, class F>
-int with_bwd_types(int x, bool kept, F f) {
-  if (x == T_F32) return kept ? f(block_bwd_kernel<VPT, W, T_F32, T_BF16, true>) : f(block_bwd_kernel<VPT, W, T_F32, T_BF16, false>);
-  if (x == T_BF16) return kept ? f(block_bwd_kernel<VPT, W, T_BF16, T_BF16, true>) : f(block_bwd_kernel<VPT, W, T_BF16, T_BF16, false>);
-  return f(block_bwd_kernel<VPT, W, kAny, kAny, false>);
+template <int VPT, class F>
+int with_fwd_types(int x, int form, int gate, F f) {
+  if (x == T_F32) return with_fwd_form<VPT, T_F32>(form, gate, f);
+  if (x == T_BF16) return with_fwd_form<VPT, T_BF16>(form, gate, f);
+  return f(block_fwd_kernel<VPT, kAny, kAny, kAny, kAny>);
 }
 template <class F>
-int with_bwd(int hidden, int x, bool kept, F f) {
-  if (vecs_per_thread(hidden) == 1) return with_bwd_types<1, kBlockBwdWarps>(x, kept, f);
-  return wide_bwd(hidden) ? with_bwd_types<2, kBlockBwdWarpsWide>(x, kept, f) : with_bwd_types<2, kBlockBwdWarps>(x, kept, f);
+int with_fwd(int hidden, int x, int form, int gate, F f) {
+  return vecs_per_thread(hidden) == 1 ? with_fwd_types<1>(x, form, gate, f) : with_fwd_types<2>(x, form, gate, f);
+}
+template <int VPT, int X, bool kKept, class F>
+int with_bwd_form(int form, int gate, F f) {
+  constexpr int W = kBlockBwdWarps;
+  if (form == kBefore) return f(block_bwd_kernel<VPT, W, X, T_BF16, kBefore, GATE_NONE, kKept>);
+  if (gate == GATE_NONE) return f(block_bwd_kernel<VPT, W, X, T_BF16, kBoth, GATE_NONE, kKept>);
+  if (gate == GATE_TOKEN) return f(block_bwd_kernel<VPT, W, X, T_BF16, kBoth, GATE_TOKEN, kKept>);
+  if (gate == GATE_CHANNEL) return f(block_bwd_kernel<VPT, W, X, T_BF16, kBoth, GATE_CHANNEL, kKept>);
+  return f(block_bwd_kernel<VPT, W, X, T_BF16, kBoth, GATE_FULL, kKept>);
+}
+template <int VPT, class F>
+int with_bwd_types(int x, int form, int gate, bool kept, F f) {
+  if (x == T_F32) return kept ? with_bwd_form<VPT, T_F32, true>(form, gate, f) : with_bwd_form<VPT, T_F32, false>(form, gate, f);
+  if (x == T_BF16) return kept ? with_bwd_form<VPT, T_BF16, true>(form, gate, f) : with_bwd_form<VPT, T_BF16, false>(form, gate, f);
+  return f(block_bwd_kernel<VPT, kBlockBwdWarps, kAny, kAny, kAny, kAny, false>);
+}
+// (rows of more than 7680 columns are always looked up)
+template <class F>
+int with_bwd(int hidden, int x, int form, int gate, bool kept, F f) {
+  if (wide_bwd(hidden)) return f(block_bwd_kernel<2, kBlockBwdWarpsWide, kAny, kAny, kAny, kAny, false>);
+  return vecs_per_thread(hidden) == 1 ? with_bwd_types<1>(x, form, gate, kept, f) : with_bwd_types<2>(x, form, gate, kept, f);
 }
 // what is there has the branch's usual type
 bool bf16_or_none(bool there, int type) { return !there || type == AUGTREE_BF16; }
@@ -213,10 +235,12 @@ int augtree_block_create(const augtree_block_desc_t *desc, int device, augtree_b
     auto room = [&](auto kernel, int bytes) {
       if (!r && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) r = AUGTREE_ERR_CUDA;
     };
+    // (the kernels that calls with this handle can reach)
+    auto kernel_room = [&](auto kernel) { room(kernel, kBlockSmem); return 0; };
     for (int x : {(int)T_F32, (int)T_BF16, kAny})
-      for (int kept = 0; kept < 2; ++kept) {
-        if (!kept) with_fwd(b->hidden, x, [&](auto kernel) { room(kernel, kBlockSmem); return 0; });
-        with_bwd(b->hidden, x, kept, [&](auto kernel) { room(kernel, kBlockSmem); return 0; });
+      for (int form : {(int)kBoth, (int)kBefore}) {
+        with_fwd(b->hidden, x, form, b->gate, kernel_room);
+        for (bool kept : {false, true}) with_bwd(b->hidden, x, form, b->gate, kept, kernel_room);
       }
     room(wgrad_kernel, LmSmem::kBytes);
     if (!r && (cudaMalloc(&b->d_status, 2 * sizeof(int)) != cudaSuccess || cudaMemset(b->d_status, 0, 2 * sizeof(int)) != cudaSuccess)) r = AUGTREE_ERR_CUDA;
@@ -291,9 +315,9 @@ int augtree_block_fwd(const augtree_block_t *b, const void *x, int x_dtype, cons
   p.ckpt_y = ckpt_rows(ckpt_y, c); p.ckpt_o = ckpt_rows(ckpt_o, c);
   const int threads = (p.s.groups * p.s.warps_row + 1) * 32;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  // (compiled types: everything of the branch in bf16)
-  const bool usual = bf16_or_none(h, h_dtype) && bf16_or_none(o, o_dtype) && bf16_or_none(p.gate == GATE_FULL, gate_dtype) && x_dtype != AUGTREE_F16;
-  return with_fwd(b->hidden, usual ? x_dtype : kAny, [&](auto kernel) { return launch(kernel, grid, threads, smem, st, p); });
+  // what is compiled in (block_kernels.cuh): everything of the branch in bf16, a norm before the next block
+  const bool usual = h && bf16_or_none(h, h_dtype) && bf16_or_none(o, o_dtype) && bf16_or_none(p.gate == GATE_FULL, gate_dtype) && x_dtype != AUGTREE_F16;
+  return with_fwd(b->hidden, usual ? x_dtype : kAny, o ? kBoth : kBefore, p.gate, [&](auto kernel) { return launch(kernel, grid, threads, smem, st, p); });
 }
 
 int augtree_block_bwd(const augtree_block_t *b, const void *dy, int x_dtype, const void *dh, int h_dtype, const void *y, int y_dtype,
@@ -351,10 +375,10 @@ int augtree_block_bwd(const augtree_block_t *b, const void *dy, int x_dtype, con
   p.dx = dx; p.d_o = d_o; p.dg = d_gate;
   p.part = static_cast<float *>(ws);
   const int threads = (p.s.groups * p.s.warps_row + 1) * 32;
-  const bool kept = y_dtype == AUGTREE_CKPT || (!dh && o_dtype == AUGTREE_CKPT);
-  const bool usual = bf16_or_none(dh, h_dtype) && bf16_or_none(d_o, do_dtype) && bf16_or_none(p.gate == GATE_FULL, gate_dtype) && x_dtype != AUGTREE_F16 &&
-                     (!dh || (kept ? y_dtype == AUGTREE_CKPT : y_dtype == x_dtype)) && (!o || o_dtype == (kept ? AUGTREE_CKPT : (int)AUGTREE_BF16));
-  r = with_bwd(b->hidden, usual ? x_dtype : kAny, kept, [&](auto kernel) { return launch(kernel, grid, threads, smem, st, p); });
+  const bool kept = y_dtype == AUGTREE_CKPT;
+  const bool usual = dy && dh && dx && !o == !d_o && bf16_or_none(dh, h_dtype) && bf16_or_none(d_o, do_dtype) && bf16_or_none(p.gate == GATE_FULL, gate_dtype) && x_dtype != AUGTREE_F16 &&
+                     (kept || y_dtype == x_dtype) && (!o || o_dtype == (kept ? AUGTREE_CKPT : (int)AUGTREE_BF16));
+  r = with_bwd(b->hidden, usual ? x_dtype : kAny, o ? kBoth : kBefore, p.gate, kept, [&](auto kernel) { return launch(kernel, grid, threads, smem, st, p); });
   const bool second = dw_out || (channel && d_gate);
   if (r || (!dw_in && !second)) return r;
   const BlockSums q = {p.part, grid, b->hidden, w_out, channel ? gate : nullptr, w_dtype, gate_dtype, b->sigmoid, accumulate, dw_in, dw_out, channel ? d_gate : nullptr};

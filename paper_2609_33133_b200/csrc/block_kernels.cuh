@@ -66,25 +66,41 @@ struct BlockParams {
   int test_flags;
 };
 
-// Types are compiled in for the usual pairs of stream and branch (fp32 or bf16 with bf16) and looked up for the others: kAny.  With the
-// look-ups a value cost 60 instructions forward and 90 backward (bf16, checkpoints), and the issue rate was the bound.
+// What is compiled in.  Types for the usual pairs of stream and branch (fp32 or bf16 with bf16); kAny: looked up.  Form of the call:
+// kBoth (a branch, a norm before the next block, every gradient wanted; the norm after the block is looked up) with its gate, kBefore
+// (the norm before a block alone), kAny.  With everything looked up a value cost 60 instructions forward and 90 backward (bf16, checkpoints) where
+// its arithmetic is about 20, and the issue rate was the bound.
 constexpr int kAny = -1;
+enum : int { kBoth = 0, kBefore = 1 };
 
-// 8 columns of a row in shared memory
+__device__ __forceinline__ int type_bytes(int type) { return type == T_F32 ? 4 : 2; }
+
+// 8 columns of a row in shared memory, from the row's first byte
 template <int T>
-__device__ __forceinline__ V8 block_load8(const uint8_t *row, int vec, int type, int hidden) {
+__device__ __forceinline__ V8 block_load8(const uint8_t *row, int vec, int type, int scales) {
   const int k = T == kAny ? type : T;
-  if (k == T_BF16) return Row8<__nv_bfloat16>::load(reinterpret_cast<const __nv_bfloat16 *>(row) + vec * 8);
-  if (k == T_F32) return Row8<float>::load(reinterpret_cast<const float *>(row) + vec * 8);
-  if (k == T_CKPT) return ckpt_decode(*reinterpret_cast<const uint2 *>(row + vec * 8), ckpt_unit(row[ckpt_scale_offset(hidden) + (vec >> 2)]));
-  return Row8<__half>::load(reinterpret_cast<const __half *>(row) + vec * 8);
+  if (k == T_BF16) return Row8<__nv_bfloat16>::load(reinterpret_cast<const __nv_bfloat16 *>(row + vec * 16));
+  if (k == T_F32) return Row8<float>::load(reinterpret_cast<const float *>(row + vec * 32));
+  if (k == T_CKPT) return ckpt_decode(*reinterpret_cast<const uint2 *>(row + vec * 8), ckpt_unit(row[scales + (vec >> 2)]));
+  return Row8<__half>::load(reinterpret_cast<const __half *>(row + vec * 16));
+}
+// the same times a number; one rounding either way
+template <int T>
+__device__ __forceinline__ V8 block_load8_times(const uint8_t *row, int vec, int type, int scales, float f) {
+  if (T == T_CKPT) return ckpt_decode(*reinterpret_cast<const uint2 *>(row + vec * 8), ckpt_unit(row[scales + (vec >> 2)]) * f);
+  return block_load8<T>(row, vec, type, scales) * f;
 }
 template <int T>
-__device__ __forceinline__ void block_store8(void *base, long long at, int type, const V8 &x) {
+__device__ __forceinline__ void block_store8(uint8_t *row, int vec, int type, const V8 &x) {
   const int k = T == kAny ? type : T;
-  if (k == T_BF16) Row8<__nv_bfloat16>::store(static_cast<__nv_bfloat16 *>(base) + at, x);
-  else if (k == T_F32) Row8<float>::store(static_cast<float *>(base) + at, x);
-  else Row8<__half>::store(static_cast<__half *>(base) + at, x);
+  if (k == T_BF16) Row8<__nv_bfloat16>::store(reinterpret_cast<__nv_bfloat16 *>(row + vec * 16), x);
+  else if (k == T_F32) Row8<float>::store(reinterpret_cast<float *>(row + vec * 32), x);
+  else Row8<__half>::store(reinterpret_cast<__half *>(row + vec * 16), x);
+}
+// row t of a matrix in global memory
+template <int T>
+__device__ __forceinline__ uint8_t *block_row(void *base, long long t, int hidden, int type) {
+  return static_cast<uint8_t *>(base) + t * (hidden * type_bytes(T == kAny ? type : T));
 }
 __device__ __forceinline__ float block_scalar(const void *p, long long i, int type) {
   if (type == T_BF16) return __bfloat162float(static_cast<const __nv_bfloat16 *>(p)[i]);
@@ -206,27 +222,41 @@ struct BlockGroup {
   }
 };
 
-// Where a group's row behind row r of block b lies; -1 if there is none.
-__device__ __forceinline__ long long block_next_row(const BlockShape &s, int group, long long b, int r, int rows) {
-  if (r + s.groups < rows) return b * s.block_rows + r + s.groups;
-  const long long row0 = (b + gridDim.x) * s.block_rows;
-  return group < s.block_rows && row0 + group < s.rows ? row0 + group : -1;
-}
+// A group's walk over its rows: block after block of the CTA, in each the rows group, group + groups, ..  `next` is the row behind
+// the present one, -1 if there is none: its numbers are fetched while this one is worked on.
+struct BlockWalk {
+  int group, groups, block_rows, rows;
+  long long t, next;             // row; the one behind it
+  __device__ __forceinline__ BlockWalk(const BlockShape &s, int group_)
+      : group(group_), groups(s.groups), block_rows(s.block_rows), rows(s.rows) {
+    const long long first = (long long)blockIdx.x * block_rows + group;
+    next = group < block_rows && first < rows ? first : -1;
+  }
+  __device__ __forceinline__ void at(long long row0, int r, int block) {      // `block`: rows of this block
+    t = row0 + r;
+    if (r + groups < block) { next = t + groups; return; }
+    const long long first = row0 + (long long)gridDim.x * block_rows + group;
+    next = first < rows ? first : -1;     // (a group without a row in a block has none behind it either)
+  }
+};
 
-template <int VPT, int XT, int OT>
+template <int VPT, int XT, int OT, int FORM, int GATE>
 __global__ void __launch_bounds__((kBlockFwdWarps + 1) * 32, 1)
 block_fwd_kernel(const __grid_constant__ BlockParams p) {
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   const BlockShape &s = p.s;
+  const bool branch = FORM == kAny ? p.has_branch : FORM == kBoth, norm_in = FORM == kAny ? p.w_in != nullptr : true, norm_out = branch && p.w_out;
+  const int gate = GATE == kAny ? p.gate : GATE;
   launch_next();
   const BlockCta c = block_setup(smem_raw, p);
   __syncthreads();
   wait_previous();
-  // slots of the vectors: w_in, w_out, gate of a channel
-  const int slot_out = p.w_in ? 1 : 0, slot_gate = slot_out + (p.w_out ? 1 : 0);
-  if (p.w_in) block_weights(c, p, 0, p.w_in, p.w_type);
-  if (p.w_out) block_weights(c, p, slot_out, p.w_out, p.w_type);
-  if (p.gate == GATE_CHANNEL) block_weights(c, p, slot_gate, p.gate_ptr, p.gate_type);
+  const int hidden = s.hidden;
+  // per-channel vectors: w_in, w_out, gate of a channel
+  const float *w_in = c.weights, *w_out = w_in + (norm_in ? hidden : 0), *g_ch = w_out + (norm_out ? hidden : 0);
+  if (norm_in) block_weights(c, p, 0, p.w_in, p.w_type);
+  if (norm_out) block_weights(c, p, (int)(w_out - w_in) / hidden, p.w_out, p.w_type);
+  if (gate == GATE_CHANNEL) block_weights(c, p, (int)(g_ch - w_in) / hidden, p.gate_ptr, p.gate_type);
   __syncthreads();
   const AbortCtx ab{c.abort_flag, p.status, p.wait_budget};
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -235,12 +265,12 @@ block_fwd_kernel(const __grid_constant__ BlockParams p) {
   } else {
     const int group = warp / s.warps_row;
     BlockGroup g{c.sums + group * 64, s.warps_row, warp - group * s.warps_row, group + 1, 0};
-    const int v0 = g.warp * 32 + lane, step = s.warps_row * 32;     // pieces v0, v0 + step
-    const bool writer = g.warp == 0 && lane == 0, token = p.gate == GATE_TOKEN;
+    const int v0 = g.warp * 32 + lane, step = s.warps_row * 32, vecs = s.vecs;     // pieces v0, v0 + step
+    const bool writer = g.warp == 0 && lane == 0;
     int st = 0;
     uint32_t phase = 0;
-    long long t = (long long)blockIdx.x * s.block_rows + group;
-    float gt_next = token && group < s.block_rows && t < s.rows ? block_scalar(p.gate_ptr, t, p.gate_type) : 0.f;
+    BlockWalk walk(s, group);
+    float gt_next = gate == GATE_TOKEN && walk.next >= 0 ? block_scalar(p.gate_ptr, walk.next, p.gate_type) : 0.f;
     for (long long b = blockIdx.x; b < s.blocks; b += gridDim.x) {
       const long long row0 = b * s.block_rows;
       const int rows = (int)min((long long)s.block_rows, s.rows - row0);
@@ -249,83 +279,73 @@ block_fwd_kernel(const __grid_constant__ BlockParams p) {
       mbar_wait(c.bar_full + 8 * st, phase, ab, WAIT_BLOCK_FULL);
       const uint8_t *stage = block_stage(c, p, st);
       for (int r = group; r < rows; r += s.groups) {
-        t = row0 + r;
+        walk.at(row0, r, rows);
+        const long long t = walk.t;
         const uint8_t *rx = stage + s.offset[0] + r * s.row_bytes[0], *ro = stage + s.offset[1] + r * s.row_bytes[1];
-        const uint8_t *rg = stage + s.offset[2] + r * s.row_bytes[2];
         float ga = p.scale;
-        if (token) {     // (the next row's gate is on its way while this row is worked on)
+        if (gate == GATE_TOKEN) {
           ga *= p.sigmoid ? logistic(gt_next) : gt_next;
-          const long long next = block_next_row(s, group, b, r, rows);
-          if (next >= 0) gt_next = block_scalar(p.gate_ptr, next, p.gate_type);
+          if (walk.next >= 0) gt_next = block_scalar(p.gate_ptr, walk.next, p.gate_type);
         }
         V8 y[VPT];
-        if (p.has_branch) {
+        if (branch) {
           V8 o[VPT];
           float2 ss = both(0.f);
           float r_o = 1.f;
 #pragma unroll
           for (int k = 0; k < VPT; ++k) {
             const int v = v0 + k * step;
-            o[k] = v < s.vecs ? block_load8<OT>(ro, v, p.o_type, s.hidden) : v8(0.f);
+            o[k] = v < vecs ? block_load8<OT>(ro, v, p.o_type, 0) : v8(0.f);
             ss = dot2(o[k], o[k], ss);
           }
-          if (p.w_out) {
+          if (norm_out) {
             r_o = rsqrtf(fmaf(g.sum(ss.x + ss.y), p.inv_hidden, p.eps));
             if (p.r_out && writer) p.r_out[t] = r_o;
           }
           if (p.ckpt_o.base) {
+            uint8_t *row = p.ckpt_o.base + t * p.ckpt_o.pitch;
 #pragma unroll
-            for (int k = 0; k < VPT; ++k) {
-              const int v = v0 + k * step;
-              uint2 q;
-              uint32_t byte;
-              ckpt_encode(o[k], q, byte);
-              if (v < s.vecs) p.ckpt_o.store(t, v, q, byte);
-            }
+            for (int k = 0; k < VPT; ++k) ckpt_store(row, v0 + k * step, vecs, p.ckpt_o.scales, o[k]);
           }
+          uint8_t *ry = block_row<XT>(p.y, t, hidden, p.x_type);
 #pragma unroll
           for (int k = 0; k < VPT; ++k) {
             const int v = v0 + k * step;
-            if (v < s.vecs) {
-              if (p.w_out) o[k] = Row8<float>::load(c.weights + slot_out * s.hidden + v * 8) * (o[k] * r_o);
-              if (p.gate >= GATE_CHANNEL) {
-                const V8 a = p.gate == GATE_FULL ? block_load8<OT>(rg, v, p.gate_type, s.hidden) : Row8<float>::load(c.weights + slot_gate * s.hidden + v * 8);
+            y[k] = v8(0.f);
+            if (v < vecs) {
+              if (norm_out) o[k] = Row8<float>::load(w_out + v * 8) * (o[k] * r_o);
+              if (gate >= GATE_CHANNEL) {
+                const V8 a = gate == GATE_FULL ? block_load8<OT>(stage + s.offset[2] + r * s.row_bytes[2], v, p.gate_type, 0) : Row8<float>::load(g_ch + v * 8);
                 o[k] = o[k] * (p.sigmoid ? logistic(a) : a);
               }
-              y[k] = fma(o[k], ga, block_load8<XT>(rx, v, p.x_type, s.hidden));
-              block_store8<XT>(p.y, t * s.hidden + v * 8, p.x_type, y[k]);
-            } else {
-              y[k] = v8(0.f);
+              y[k] = fma(o[k], ga, block_load8<XT>(rx, v, p.x_type, 0));
+              block_store8<XT>(ry, v, p.x_type, y[k]);
             }
           }
         } else {
 #pragma unroll
           for (int k = 0; k < VPT; ++k) {
             const int v = v0 + k * step;
-            y[k] = v < s.vecs ? block_load8<XT>(rx, v, p.x_type, s.hidden) : v8(0.f);
+            y[k] = v < vecs ? block_load8<XT>(rx, v, p.x_type, 0) : v8(0.f);
           }
         }
-        if (p.w_in) {
+        if (norm_in) {
           float2 ss = both(0.f);
 #pragma unroll
           for (int k = 0; k < VPT; ++k) ss = dot2(y[k], y[k], ss);
           const float r_i = rsqrtf(fmaf(g.sum(ss.x + ss.y), p.inv_hidden, p.eps));
           if (p.r_in && writer) p.r_in[t] = r_i;
+          uint8_t *rh = block_row<OT>(p.h, t, hidden, p.h_type);
 #pragma unroll
           for (int k = 0; k < VPT; ++k) {
             const int v = v0 + k * step;
-            if (v < s.vecs) block_store8<OT>(p.h, t * s.hidden + v * 8, p.h_type, Row8<float>::load(c.weights + v * 8) * (y[k] * r_i));
+            if (v < vecs) block_store8<OT>(rh, v, p.h_type, Row8<float>::load(w_in + v * 8) * (y[k] * r_i));
           }
         }
         if (p.ckpt_y.base) {
+          uint8_t *row = p.ckpt_y.base + t * p.ckpt_y.pitch;
 #pragma unroll
-          for (int k = 0; k < VPT; ++k) {
-            const int v = v0 + k * step;
-            uint2 q;
-            uint32_t byte;
-            ckpt_encode(block_round<XT>(y[k], p.x_type), q, byte);
-            if (v < s.vecs) p.ckpt_y.store(t, v, q, byte);
-          }
+          for (int k = 0; k < VPT; ++k) ckpt_store(row, v0 + k * step, vecs, p.ckpt_y.scales, block_round<XT>(y[k], p.x_type));
         }
       }
       warp_arrive(c.bar_empty + 8 * st);
@@ -336,20 +356,24 @@ block_fwd_kernel(const __grid_constant__ BlockParams p) {
 }
 
 // kKept: v and u are read from checkpoints, both (with kAny each from what its type says).
-template <int VPT, int kWarps, int XT, int OT, bool kKept>
+template <int VPT, int kWarps, int XT, int OT, int FORM, int GATE, bool kKept>
 __global__ void __launch_bounds__((kWarps + 1) * 32, 1)
 block_bwd_kernel(const __grid_constant__ BlockParams p) {
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   constexpr int YT = XT == kAny ? kAny : kKept ? (int)T_CKPT : XT, ST = OT == kAny ? kAny : kKept ? (int)T_CKPT : OT;   // of the saved y and o
   const BlockShape &s = p.s;
+  const bool branch = FORM == kAny ? p.has_branch : FORM == kBoth, has_dy = FORM == kAny ? p.has_dy : true, has_dh = FORM == kAny ? p.has_dh : true;
+  const bool norm_out = branch && p.w_out, put_dx = FORM == kAny ? p.dx != nullptr : true, put_do = FORM == kAny ? p.d_o != nullptr : true;
+  const int gate = GATE == kAny ? p.gate : GATE;
   launch_next();
   const BlockCta c = block_setup(smem_raw, p);
   __syncthreads();
   wait_previous();
-  const int slot_out = p.w_in ? 1 : 0, slot_gate = slot_out + (p.w_out ? 1 : 0);
+  const int hidden = s.hidden;
+  const float *w_in = c.weights, *w_out = w_in + (p.w_in ? hidden : 0), *g_ch = w_out + (norm_out ? hidden : 0);
   if (p.w_in) block_weights(c, p, 0, p.w_in, p.w_type);
-  if (p.w_out) block_weights(c, p, slot_out, p.w_out, p.w_type);
-  if (p.gate == GATE_CHANNEL) block_weights(c, p, slot_gate, p.gate_ptr, p.gate_type);
+  if (norm_out) block_weights(c, p, (int)(w_out - w_in) / hidden, p.w_out, p.w_type);
+  if (gate == GATE_CHANNEL) block_weights(c, p, (int)(g_ch - w_in) / hidden, p.gate_ptr, p.gate_type);
   __syncthreads();
   const AbortCtx ab{c.abort_flag, p.status, p.wait_budget};
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -358,8 +382,8 @@ block_bwd_kernel(const __grid_constant__ BlockParams p) {
   for (int k = 0; k < VPT; ++k) acc_in[k] = acc_out[k] = v8(0.f);
   const int group = warp / s.warps_row;
   BlockGroup g{c.sums + group * 64, s.warps_row, warp - group * s.warps_row, group + 1, 0};
-  const int v0 = g.warp * 32 + lane, step = s.warps_row * 32;
-  const bool computes = group < s.groups, writer = g.warp == 0 && lane == 0, token = p.gate == GATE_TOKEN;
+  const int v0 = g.warp * 32 + lane, step = s.warps_row * 32, vecs = s.vecs;
+  const bool computes = group < s.groups, writer = g.warp == 0 && lane == 0;
   if (!computes) {
     if (lane == 0) block_produce(c, p, ab);
     __syncwarp();
@@ -367,41 +391,42 @@ block_bwd_kernel(const __grid_constant__ BlockParams p) {
     int st = 0;
     uint32_t phase = 0;
     // inputs in the order that the host lists them: dy, dh, y, o, gate, each only where there is one
-    const int at_dh = p.has_dy, at_y = at_dh + p.has_dh, at_o = at_y + p.has_dh, at_g = at_o + p.has_branch;
-    // a row's numbers, fetched while the row before it is worked on
+    const int at_dh = has_dy, at_y = at_dh + has_dh, at_o = at_y + has_dh, at_g = at_o + branch;
+    const int scales = (int)ckpt_scale_offset(hidden);
+    BlockWalk walk(s, group);
     float ri_next = 0.f, ro_next = 1.f, gt_next = 1.f;
-    auto fetch = [&](long long t) {
-      if (t < 0) return;
-      if (p.has_dh) ri_next = p.r_in[t];
-      if (p.w_out) ro_next = p.r_out[t];
-      if (token) gt_next = block_scalar(p.gate_ptr, t, p.gate_type);
+    auto fetch = [&]() {
+      if (walk.next < 0) return;
+      if (has_dh) ri_next = p.r_in[walk.next];
+      if (norm_out) ro_next = p.r_out[walk.next];
+      if (gate == GATE_TOKEN) gt_next = block_scalar(p.gate_ptr, walk.next, p.gate_type);
     };
-    const long long first = (long long)blockIdx.x * s.block_rows + group;
-    fetch(group < s.block_rows && first < s.rows ? first : -1);
+    fetch();
     for (long long b = blockIdx.x; b < s.blocks; b += gridDim.x) {
       const long long row0 = b * s.block_rows;
       const int rows = (int)min((long long)s.block_rows, s.rows - row0);
       mbar_wait(c.bar_full + 8 * st, phase, ab, WAIT_BLOCK_FULL);
       const uint8_t *stage = block_stage(c, p, st);
       for (int r = group; r < rows; r += s.groups) {
-        const long long t = row0 + r;
+        walk.at(row0, r, rows);
+        const long long t = walk.t;
         auto row = [&](int i) { return stage + s.offset[i] + r * s.row_bytes[i]; };
-        const float r_i = ri_next, r_o = ro_next, at = token && p.sigmoid ? logistic(gt_next) : gt_next;
-        fetch(block_next_row(s, group, b, r, rows));
+        const float r_i = ri_next, r_o = ro_next, at = gate == GATE_TOKEN && p.sigmoid ? logistic(gt_next) : gt_next;
+        fetch();
         V8 d[VPT];
-        if (p.has_dh) {
+        if (has_dh) {
           V8 v[VPT];
           float2 dot = both(0.f);
+          const uint8_t *rh = row(at_dh), *ry = row(at_y);
 #pragma unroll
           for (int k = 0; k < VPT; ++k) {
             const int at8 = v0 + k * step;
-            if (at8 < s.vecs) {
-              const V8 dh = block_load8<OT>(row(at_dh), at8, p.h_type, s.hidden);
-              v[k] = block_load8<YT>(row(at_y), at8, p.y_type, s.hidden) * r_i;
+            v[k] = d[k] = v8(0.f);
+            if (at8 < vecs) {
+              const V8 dh = block_load8<OT>(rh, at8, p.h_type, 0);
+              v[k] = block_load8_times<YT>(ry, at8, p.y_type, scales, r_i);
               acc_in[k] = fma(dh, v[k], acc_in[k]);
-              d[k] = Row8<float>::load(c.weights + at8 * 8) * dh;
-            } else {
-              v[k] = d[k] = v8(0.f);
+              d[k] = Row8<float>::load(w_in + at8 * 8) * dh;
             }
             dot = dot2(d[k], v[k], dot);
           }
@@ -412,52 +437,58 @@ block_bwd_kernel(const __grid_constant__ BlockParams p) {
 #pragma unroll
           for (int k = 0; k < VPT; ++k) d[k] = v8(0.f);
         }
-#pragma unroll
-        for (int k = 0; k < VPT; ++k) {
-          const int at8 = v0 + k * step;
-          if (at8 >= s.vecs) continue;
-          if (p.has_dy) d[k] = d[k] + block_load8<XT>(row(0), at8, p.x_type, s.hidden);
-          if (p.dx) block_store8<XT>(p.dx, t * s.hidden + at8 * 8, p.x_type, d[k]);
-        }
-        if (p.has_branch) {
-          V8 u[VPT];
-          float2 dot = both(0.f);    // sum of w_o q u a(g), without the a(g) of a token
+        {
+          const uint8_t *ry = row(0);
+          uint8_t *rx = block_row<XT>(p.dx, t, hidden, p.x_type);
 #pragma unroll
           for (int k = 0; k < VPT; ++k) {
             const int at8 = v0 + k * step;
-            if (at8 >= s.vecs) { u[k] = v8(0.f); continue; }
+            if (at8 >= vecs) continue;
+            if (has_dy) d[k] = d[k] + block_load8<XT>(ry, at8, p.x_type, 0);
+            if (put_dx) block_store8<XT>(rx, at8, p.x_type, d[k]);
+          }
+        }
+        if (branch) {
+          V8 u[VPT];
+          float2 dot = both(0.f);    // sum of w_o q u a(g), without the a(g) of a token
+          const uint8_t *ro = row(at_o);
+#pragma unroll
+          for (int k = 0; k < VPT; ++k) {
+            const int at8 = v0 + k * step;
+            u[k] = v8(0.f);
+            if (at8 >= vecs) continue;
             const V8 q = d[k] * p.scale;
-            u[k] = block_load8<ST>(row(at_o), at8, p.o_type, s.hidden) * r_o;
-            if (p.gate >= GATE_CHANNEL) {
-              V8 a = p.gate == GATE_FULL ? block_load8<OT>(row(at_g), at8, p.gate_type, s.hidden) : Row8<float>::load(c.weights + slot_gate * s.hidden + at8 * 8);
+            u[k] = block_load8_times<ST>(ro, at8, p.o_type, scales, r_o);
+            if (gate >= GATE_CHANNEL) {
+              V8 a = gate == GATE_FULL ? block_load8<OT>(row(at_g), at8, p.gate_type, 0) : Row8<float>::load(g_ch + at8 * 8);
               if (p.sigmoid) a = logistic(a);
-              const V8 qa = q * a, w = p.w_out ? Row8<float>::load(c.weights + slot_out * s.hidden + at8 * 8) : v8(1.f);
-              acc_out[k] = fma(p.gate == GATE_CHANNEL ? q : qa, u[k], acc_out[k]);
+              const V8 qa = q * a, w = norm_out ? Row8<float>::load(w_out + at8 * 8) : v8(1.f);
+              acc_out[k] = fma(gate == GATE_CHANNEL ? q : qa, u[k], acc_out[k]);
               d[k] = w * qa;
-              if (p.gate == GATE_FULL && p.dg) {
+              if (gate == GATE_FULL && p.dg) {
                 V8 dg = q * (w * u[k]);
                 if (p.sigmoid) dg = dg * (a * fma(a, -1.f, v8(1.f)));
-                block_store8<OT>(p.dg, t * s.hidden + at8 * 8, p.gate_type, dg);
+                block_store8<OT>(block_row<OT>(p.dg, t, hidden, p.gate_type), at8, p.gate_type, dg);
               }
             } else {
-              acc_out[k] = fma(q * at, u[k], acc_out[k]);
-              d[k] = p.w_out ? Row8<float>::load(c.weights + slot_out * s.hidden + at8 * 8) * q : q;
+              acc_out[k] = fma(gate == GATE_TOKEN ? q * at : q, u[k], acc_out[k]);
+              d[k] = norm_out ? Row8<float>::load(w_out + at8 * 8) * q : q;
             }
             dot = dot2(d[k], u[k], dot);
           }
           float mean = 0.f;
-          if (p.w_out || token) {
+          if (norm_out || gate == GATE_TOKEN) {
             const float total = g.sum(dot.x + dot.y);
-            mean = total * p.inv_hidden;
-            if (token && p.dg && writer) block_scalar_store(p.dg, t, p.gate_type, total * (p.sigmoid ? at * (1.f - at) : 1.f));
+            mean = norm_out ? total * p.inv_hidden : 0.f;
+            if (gate == GATE_TOKEN && p.dg && writer) block_scalar_store(p.dg, t, p.gate_type, total * (p.sigmoid ? at * (1.f - at) : 1.f));
           }
-          if (p.d_o) {
+          if (put_do) {
             const float f = r_o * at;      // (1 without a norm, 1 without a gate of one number a token)
+            uint8_t *rd = block_row<OT>(p.d_o, t, hidden, p.do_type);
 #pragma unroll
             for (int k = 0; k < VPT; ++k) {
               const int at8 = v0 + k * step;
-              if (at8 >= s.vecs) continue;
-              block_store8<OT>(p.d_o, t * s.hidden + at8 * 8, p.do_type, (p.w_out ? fma(u[k], -mean, d[k]) : d[k]) * f);
+              if (at8 < vecs) block_store8<OT>(rd, at8, p.do_type, fma(u[k], -mean, d[k]) * f);
             }
           }
         }

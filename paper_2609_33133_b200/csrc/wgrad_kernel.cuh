@@ -240,7 +240,7 @@ wgrad_join_kernel(const float *part, int splits, long long part_rows, int out, i
       for (int e = 0; e < 8; ++e) x[e] *= block_scalar(col, c0 + e, col_type);
     }
     if (add) x = x + Row8<float>::load(static_cast<const float *>(dw) + i * 8);
-    block_store8<kAny>(dw, i * 8, type, x);
+    block_store8<kAny>(static_cast<uint8_t *>(dw) + i * 8 * type_bytes(type), 0, type, x);
   }
 }
 
