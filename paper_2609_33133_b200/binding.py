@@ -1,4 +1,4 @@
-"""ctypes binding of libaugtree.so: argument marshalling only.
+"""Binding of libaugtree.so (ctypes; Block's calls through csrc/marshal.cpp): argument marshalling only.
 
 Every step of the path runs inside the library's kernels.  PyTorch appears only
 as the owner of device memory and of the current stream.  Importing this module
@@ -19,6 +19,7 @@ LIB_PATH = os.environ.get("AUGTREE_LIB") or os.path.join(_HERE, "libaugtree.so")
 if not os.path.exists(LIB_PATH):
     raise ImportError(f"{LIB_PATH} is missing: build it with `python -m paper_2609_33133_b200.build`")
 lib = C.CDLL(LIB_PATH)
+from . import _marshal  # noqa: E402  (Block's argument checks and calls, csrc/marshal.cpp)
 
 FLAG_ZERO_PROMPT_GRAD = 1
 FLAG_TEST_SHORT_WAIT, FLAG_TEST_SKIP_FWD_LOAD, FLAG_TEST_SKIP_BWD_LOAD, FLAG_TEST_DROP_ITEM = 0x100, 0x200, 0x400, 0x800
@@ -123,15 +124,10 @@ _i, _l = C.c_int, C.c_int64
 lib.augtree_block_create.argtypes = [C.POINTER(BlockDescC), _i, C.POINTER(_vp)]
 lib.augtree_block_destroy.argtypes = [_vp]
 lib.augtree_block_workspace_bytes.argtypes = [_vp, _l, C.POINTER(_sz)]
-lib.augtree_block_fwd.argtypes = [_vp, _vp, _i, _vp, _i, _vp, _i, _vp, _vp, _i, _l, _vp, _vp, _i, _vp, _vp, _vp, _vp, _vp]
-lib.augtree_block_bwd.argtypes = ([_vp] + [_vp, _i] * 5 + [_vp, _vp, _i, _vp, _vp, _l, _vp, _vp, _i, _vp, _vp, _vp, _i, _vp, _sz, _vp])
 lib.augtree_ckpt_pitch.argtypes = [_l, C.POINTER(_l)]
-lib.augtree_ckpt_pack.argtypes = [_vp, _vp, _i, _l, _l, _l, _vp, _vp]
-lib.augtree_ckpt_unpack.argtypes = [_vp, _vp, _l, _l, _vp, _vp, _i, _vp, _i, _l, _vp]
-lib.augtree_glu_fwd.argtypes = [_vp, _vp, _vp, _l, _i, _l, _l, _vp, _vp, _vp, _vp]
-lib.augtree_glu_bwd.argtypes = [_vp, _vp, _i, _vp, _vp, _l, _i, _l, _l, _vp, _vp, _l, _vp, _vp]
 lib.augtree_ckpt_wgrad_bytes.argtypes = [_vp, _l, _l, _l, C.POINTER(_sz)]
-lib.augtree_ckpt_wgrad.argtypes = [_vp, _vp, _l, _l, _vp, _l, _vp, _vp, _i, _vp, _i, _i, _vp, _sz, _vp]
+_marshal.init(*[C.cast(getattr(lib, "augtree_" + n), _vp).value for n in ("block_fwd", "block_bwd", "ckpt_pitch", "ckpt_pack", "ckpt_unpack", "glu_fwd",
+                                                                          "glu_bwd", "ckpt_wgrad")])
 lib.augtree_block_last_device_status.argtypes = [_vp, C.POINTER(_i), C.POINTER(_i)]
 lib.augtree_plan_tree.argtypes = [C.POINTER(TreeC), C.POINTER(ProfileC), C.POINTER(ChoiceC), _i32p, _i32p]
 
@@ -403,9 +399,7 @@ class LM:
         return s.value, d.value
 
 
-CKPT = 3
 GATES = {"none": 0, "token": 1, "channel": 2, "full": 3}
-_U8_CODE, _F32_CODE, _BF16_CODE, _WGRAD_CODE = {torch.uint8: CKPT}, {torch.float32: 2}, {torch.bfloat16: 0}, {torch.bfloat16: 0, torch.float32: 2}
 
 
 def ckpt_pitch(cols) -> int:
@@ -433,7 +427,7 @@ class Block:
                        _fits("flags", flags, 32, signed=False), _fits("n_lanes", n_lanes, 32))
         self._h = C.c_void_p()
         _check(lib.augtree_block_create(C.byref(d), -1 if device is None else int(device), C.byref(self._h)), "block_create")
-        self._pitch = ckpt_pitch(self.hidden)
+        self._call = (self._h.value, -1 if device is None else int(device), self.hidden, ckpt_pitch(self.hidden), GATES[gate])
 
     def __del__(self):
         h = getattr(self, "_h", None)
@@ -454,159 +448,37 @@ class Block:
                                             _fits("cols", cols, 64), C.byref(n)), "ckpt_wgrad_bytes")
         return n.value
 
-    def _arg(self, t, name, codes, shape):
-        """(address, type code) of a contiguous tensor of the given shape; (None, 0) for None."""
-        if t is None:
-            return None, 0
-        code = codes.get(t.dtype)
-        if code is None or t.shape != shape or t.get_device() != self.device or not t.is_contiguous():
-            raise ValueError(f"{name}: expected a contiguous tensor on cuda:{self.device} of shape {tuple(shape)} and one of {list(codes)}, "
-                             f"got {tuple(t.shape)} {t.dtype} on {t.device}")
-        return t.data_ptr(), code
-
-    def _saved(self, t, name, n, cols, pitch):
-        if t is not None and t.dtype is torch.uint8:
-            return self._arg(t, name, _U8_CODE, (n, pitch))
-        return self._arg(t, name, _DTYPE_CODE, (n, cols))
-
-    def _strided(self, t, name, dtype, shape):
-        """(address, leading size) of a matrix whose rows are contiguous."""
-        if t.dtype is not dtype or t.shape != shape or t.get_device() != self.device or (shape[1] > 1 and t.stride(1) != 1):
-            raise ValueError(f"{name}: expected a tensor on cuda:{self.device} of shape {tuple(shape)} and type {dtype} with contiguous rows, "
-                             f"got {tuple(t.shape)} {t.dtype} on {t.device} with strides {t.stride()}")
-        ld = t.stride(0) if shape[0] > 1 else shape[1]
-        if ld < shape[1]:
-            raise ValueError(f"{name}: rows overlap (strides {t.stride()})")
-        return t.data_ptr(), ld
-
-    def _rows(self, t, name):
-        if t is None or t.dim() != 2:
-            raise ValueError(f"{name}: expected two dimensions")
-        return t.shape
-
-    def _gate_shape(self, n):
-        return {"token": (n,), "channel": (self.hidden,), "full": (n, self.hidden)}.get(self.gate)
-
-    def _weights(self, w_out, w_in):
-        if w_out is not None and w_in is not None and w_out.dtype is not w_in.dtype:
-            raise ValueError(f"w_out, w_in: expected one type, got {w_out.dtype} and {w_in.dtype}")
-        (wo, ct), (wi, ci) = self._arg(w_out, "w_out", _DTYPE_CODE, (self.hidden,)), self._arg(w_in, "w_in", _DTYPE_CODE, (self.hidden,))
-        return wo, wi, ct if wo else ci
-
-    def _stream(self):
-        return torch._C._cuda_getCurrentRawStream(self.device)
-
-    def _same(self, t, like, name):
-        if t is not None and (like is None or t.dtype is not like.dtype):
-            raise ValueError(f"{name}: expected {'none' if like is None else like.dtype}, got {t.dtype}")
-
     def fwd(self, x, o, gate, w_out, w_in, y, h, r_out, r_in, ckpt_y=None, ckpt_o=None):
         """y = x + s a(gate) (w_out o r_out), h = w_in y r_in with the reciprocal root mean squares r_out of o and r_in of y.  o None: the norm
         before a block alone (h from x).  w_out None: no norm after the block.  w_in and h None: no norm before the next.  y may be x."""
-        n, c = self._rows(x, "x")
-        row, vec = (n, self.hidden), (n,)
-        xp, xt = self._arg(x, "x", _DTYPE_CODE, row)
-        op, ot = self._arg(o, "o", _DTYPE_CODE, row)
-        gp, gt = (None, 0) if gate is None else self._arg(gate, "gate", _DTYPE_CODE, self._gate_shape(n) or (0,))
-        wo, wi, wt = self._weights(w_out, w_in)
-        self._same(y, x, "y")
-        hp, ht = self._arg(h, "h", _DTYPE_CODE, row)
-        _check(lib.augtree_block_fwd(self._h, xp, xt, op, ot, gp, gt, wo, wi, wt, n, self._arg(y, "y", _DTYPE_CODE, row)[0], hp, ht,
-                                     self._arg(r_out, "r_out", _F32_CODE, vec)[0], self._arg(r_in, "r_in", _F32_CODE, vec)[0],
-                                     self._arg(ckpt_y, "ckpt_y", _U8_CODE, (n, self._pitch))[0], self._arg(ckpt_o, "ckpt_o", _U8_CODE, (n, self._pitch))[0],
-                                     self._stream()), "block_fwd")
+        _check(_marshal.block_fwd(self._call, x, o, gate, w_out, w_in, y, h, r_out, r_in, ckpt_y, ckpt_o), "block_fwd")
 
     def bwd(self, dy, dh, y, o, gate, w_out, w_in, r_out, r_in, dx, d_o, d_gate, dw_out, dw_in, ws, accumulate=False):
         """Gradients of `fwd` under dy (of y, the residual stream) and dh (of h), either None for zero.  y (x if there was no o) and o: as `fwd` took and
         left them, or their checkpoints.  Outputs that are None are not written; accumulate adds the sums over tokens to fp32 dw_out, dw_in (and
-        d_gate of one number a channel)."""
-        lead = dy if dy is not None else dh
-        n, c = self._rows(lead, "dy or dh")
-        row, vec, code = (n, self.hidden), (n,), _DTYPE_CODE
-        yp, yt = self._arg(dy, "dy", code, row)
-        dxp, dxt = self._arg(dx, "dx", code, row)
-        if dy is not None:
-            self._same(dx, dy, "dx")
-        hp, ht = self._arg(dh, "dh", code, row)
-        vp, vt = self._saved(y, "y", n, self.hidden, self._pitch)
-        op, ot = self._saved(o, "o", n, self.hidden, self._pitch)
-        dop, dot = self._arg(d_o, "d_o", code, row)
-        shape = self._gate_shape(n) or (0,)
-        gp, gt = (None, 0) if gate is None else self._arg(gate, "gate", code, shape)
-        self._same(d_gate, gate, "d_gate")
-        wo, wi, wt = self._weights(w_out, w_in)
-        self._same(dw_out, w_out, "dw_out")
-        self._same(dw_in, w_in, "dw_in")
-        if ws.get_device() != self.device or not ws.is_contiguous():
-            raise ValueError(f"ws: expected a contiguous tensor on cuda:{self.device}")
-        col = (self.hidden,)
-        _check(lib.augtree_block_bwd(self._h, yp, yt if dy is not None else dxt, hp, ht, vp, vt, op, ot, gp, gt, wo, wi, wt,
-                                     self._arg(r_out, "r_out", _F32_CODE, vec)[0], self._arg(r_in, "r_in", _F32_CODE, vec)[0], n, dxp, dop, dot,
-                                     self._arg(d_gate, "d_gate", code, shape)[0], self._arg(dw_out, "dw_out", code, col)[0],
-                                     self._arg(dw_in, "dw_in", code, col)[0], 1 if accumulate else 0, ws.data_ptr(), ws.nbytes, self._stream()), "block_bwd")
+        d_gate of one number a channel).  dx may be dy."""
+        _check(_marshal.block_bwd(self._call, dy, dh, y, o, gate, w_out, w_in, r_out, r_in, dx, d_o, d_gate, dw_out, dw_in, ws, accumulate), "block_bwd")
 
     def pack(self, x, ckpt):
         """The 8-bit form of x [tokens, columns] (rows contiguous, any leading size that is a multiple of 8)."""
-        n, c = self._rows(x, "x")
-        code = _DTYPE_CODE.get(x.dtype)
-        if code is None:
-            raise ValueError(f"x: expected one of {list(_DTYPE_CODE)}, got {x.dtype}")
-        xp, ld = self._strided(x, "x", x.dtype, (n, c))
-        _check(lib.augtree_ckpt_pack(self._h, xp, code, ld, n, c, self._arg(ckpt, "ckpt", _U8_CODE, (n, ckpt_pitch(c)))[0], self._stream()), "ckpt_pack")
+        _check(_marshal.ckpt_pack(self._call, x, ckpt), "ckpt_pack")
 
     def unpack(self, ckpt, out, row=None, col=None):
         """What a checkpoint stands for, times row[t] (fp32) and then col[c] where given, rounded once to out's type."""
-        n, c = self._rows(out, "out")
-        code = _DTYPE_CODE.get(out.dtype)
-        if code is None:
-            raise ValueError(f"out: expected one of {list(_DTYPE_CODE)}, got {out.dtype}")
-        op, ld = self._strided(out, "out", out.dtype, (n, c))
-        cp, ct = self._arg(col, "col", _DTYPE_CODE, (c,))
-        _check(lib.augtree_ckpt_unpack(self._h, self._arg(ckpt, "ckpt", _U8_CODE, (n, ckpt_pitch(c)))[0], n, c, self._arg(row, "row", _F32_CODE, (n,))[0],
-                                       cp, ct, op, code, ld, self._stream()), "ckpt_unpack")
+        _check(_marshal.ckpt_unpack(self._call, ckpt, out, row, col), "ckpt_unpack")
 
     def glu_fwd(self, g, u, a, ckpt_g=None, ckpt_u=None):
         """a = g / (1 + exp(-g)) u.  g and u may be the halves of one tensor (rows contiguous, one leading size); the checkpoints come together."""
-        n, c = self._rows(g, "g")
-        ap, at = self._arg(a, "a", _DTYPE_CODE, (n, c))
-        (gp, ld), (up, lu) = self._strided(g, "g", a.dtype, (n, c)), self._strided(u, "u", a.dtype, (n, c))
-        if ld != lu:
-            raise ValueError(f"g, u: expected one leading size, got {ld} and {lu}")
-        kg = ku = None
-        if ckpt_g is not None or ckpt_u is not None:
-            pitch = ckpt_pitch(c)
-            kg, ku = self._arg(ckpt_g, "ckpt_g", _U8_CODE, (n, pitch))[0], self._arg(ckpt_u, "ckpt_u", _U8_CODE, (n, pitch))[0]
-        _check(lib.augtree_glu_fwd(self._h, gp, up, ld, at, n, c, ap, kg, ku, self._stream()), "glu_fwd")
+        _check(_marshal.glu_fwd(self._call, g, u, a, ckpt_g, ckpt_u), "glu_fwd")
 
     def glu_bwd(self, da, g, u, dg, du, a=None):
         """Gradients of `glu_fwd` from g and u or from their checkpoints; a, if given, gets the activation once more."""
-        n, c = self._rows(da, "da")
-        dp, dt = self._arg(da, "da", _DTYPE_CODE, (n, c))
-        if g.dtype is torch.uint8:
-            pitch = ckpt_pitch(c)
-            gp, up, ld, st = self._arg(g, "g", _U8_CODE, (n, pitch))[0], self._arg(u, "u", _U8_CODE, (n, pitch))[0], 0, CKPT
-        else:
-            (gp, ld), (up, lu), st = self._strided(g, "g", da.dtype, (n, c)), self._strided(u, "u", da.dtype, (n, c)), dt
-            if ld != lu:
-                raise ValueError(f"g, u: expected one leading size, got {ld} and {lu}")
-        (dgp, lg), (dup, lu) = self._strided(dg, "dg", da.dtype, (n, c)), self._strided(du, "du", da.dtype, (n, c))
-        if lg != lu:
-            raise ValueError(f"dg, du: expected one leading size, got {lg} and {lu}")
-        self._same(a, da, "a")
-        _check(lib.augtree_glu_bwd(self._h, dp, dt, gp, up, ld, st, n, c, dgp, dup, lg, self._arg(a, "a", _DTYPE_CODE, (n, c))[0], self._stream()), "glu_bwd")
+        _check(_marshal.glu_bwd(self._call, da, g, u, dg, du, a), "glu_bwd")
 
     def wgrad(self, dy, ckpt, d_weight, ws, row=None, col=None, accumulate=False):
         """d_weight [out, columns] = dy.T @ X (bf16 or fp32, the latter also added to), X what the checkpoint stands for times row[t] and col[c] where
         given; dy [tokens, out] bf16."""
-        n, m = self._rows(dy, "dy")
-        c = self._rows(d_weight, "d_weight")[1]
-        wp, wt = self._arg(d_weight, "d_weight", _WGRAD_CODE, (m, c))
-        cp, ct = self._arg(col, "col", _DTYPE_CODE, (c,))
-        if ws.get_device() != self.device or not ws.is_contiguous():
-            raise ValueError(f"ws: expected a contiguous tensor on cuda:{self.device}")
-        _check(lib.augtree_ckpt_wgrad(self._h, self._arg(dy, "dy", _BF16_CODE, (n, m))[0], n, m, self._arg(ckpt, "ckpt", _U8_CODE, (n, ckpt_pitch(c)))[0],
-                                      c, self._arg(row, "row", _F32_CODE, (n,))[0], cp, ct, wp, wt, 1 if accumulate else 0, ws.data_ptr(), ws.nbytes,
-                                      self._stream()), "ckpt_wgrad")
+        _check(_marshal.ckpt_wgrad(self._call, dy, ckpt, d_weight, ws, row, col, accumulate), "ckpt_wgrad")
 
     def device_status(self):
         s, d = C.c_int(), C.c_int()

@@ -1,41 +1,62 @@
-"""Builds libaugtree.so (sm_100a) in-tree with nvcc.  `python -m paper_2609_33133_b200.build`."""
+"""Builds libaugtree.so (sm_100a, nvcc) and _marshal.so (g++) in-tree.  `python -m paper_2609_33133_b200.build`."""
 from __future__ import annotations
 
 import os
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
-LIB = os.path.join(HERE, "libaugtree.so")
+LIB, MARSHAL = os.path.join(HERE, "libaugtree.so"), os.path.join(HERE, "_marshal.so")
+CUDA = "/usr/local/cuda"
 SOURCES = ["augtree.cu", "lm.cu", "block.cu", "plan.cpp", "planner.cpp"]
 HEADERS = ["ptx.cuh", "fwd_kernel.cuh", "bwd_kernel.cuh", "dq_kernel.cuh", "dql_kernel.cuh", "pair_tile.cuh", "lm_tile_kernel.cuh", "lm_few_kernel.cuh", "lm_kernels.cuh", "ckpt.cuh", "act_kernels.cuh",
            "block_kernels.cuh", "wgrad_kernel.cuh", "handle.h", "launch.h", "plan.h", os.path.join("..", "..", "include", "augtree.h")]
+MARSHAL_SOURCES = ["marshal.cpp", os.path.join("..", "..", "include", "augtree.h")]
 
 
-def _stale() -> bool:
-    if not os.path.exists(LIB):
+def _stale(target, sources) -> bool:
+    if not os.path.exists(target):
         return True
-    t = os.path.getmtime(LIB)
-    return any(os.path.getmtime(os.path.join(CSRC, f)) > t for f in SOURCES + HEADERS)
+    t = os.path.getmtime(target)
+    return any(os.path.getmtime(os.path.join(CSRC, f)) > t for f in sources)
+
+
+def _start_marshal():
+    """g++ on the argument marshalling of binding.Block, against the headers of the torch that runs it."""
+    import torch
+    at = os.path.dirname(torch.__file__)
+    cmd = ["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-I" + os.path.join(at, "include"),
+           "-I" + os.path.join(at, "include", "torch", "csrc", "api", "include"), "-I" + sysconfig.get_paths()["include"], "-I" + CUDA + "/include",
+           "-o", MARSHAL, os.path.join(CSRC, MARSHAL_SOURCES[0]), "-L" + os.path.join(at, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
+    return subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    if not force and not _stale():
-        return LIB
-    nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
-    cmd = [nvcc, "--threads", "0", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-shared",
-           "-Xcompiler", "-fPIC", "-cudart", "static",
-           "-o", LIB] + [os.path.join(CSRC, f) for f in SOURCES]
-    if verbose:
-        cmd.insert(1, "-Xptxas")
-        cmd.insert(2, "-v")
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    if res.returncode != 0:
-        sys.stderr.write(res.stdout + res.stderr)
-        raise RuntimeError("nvcc failed building libaugtree.so")
-    if verbose:
-        sys.stderr.write(res.stderr)
+    marshal = _start_marshal() if force or _stale(MARSHAL, MARSHAL_SOURCES) else None
+    failed = []
+    if force or _stale(LIB, SOURCES + HEADERS):
+        nvcc = os.environ.get("NVCC", CUDA + "/bin/nvcc")
+        cmd = [nvcc, "--threads", "0", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-shared",
+               "-Xcompiler", "-fPIC", "-cudart", "static",
+               "-o", LIB] + [os.path.join(CSRC, f) for f in SOURCES]
+        if verbose:
+            cmd.insert(1, "-Xptxas")
+            cmd.insert(2, "-v")
+        res = subprocess.run(cmd, capture_output=True, text=True)
+        if res.returncode != 0:
+            sys.stderr.write(res.stdout + res.stderr)
+            failed.append("nvcc failed building libaugtree.so")
+        elif verbose:
+            sys.stderr.write(res.stderr)
+    if marshal is not None:
+        out = marshal.communicate()[0]
+        if marshal.returncode != 0:
+            sys.stderr.write(out)
+            failed.append("the C++ compiler failed building _marshal.so")
+    if failed:
+        raise RuntimeError("; ".join(failed))
     return LIB
 
 
