@@ -53,16 +53,20 @@ bool ld_ok(int64_t &ld, int64_t cols) {
   return ld >= cols && ld % 8 == 0;
 }
 
-Pieces pieces(int64_t rows, int64_t cols, int64_t padded) {
+// The walk over a matrix (act_kernels.cuh) and its grid: as many blocks as the SMs hold at a time.
+Pieces pieces(const augtree_block *b, int64_t rows, int64_t cols, int64_t padded, int blocks, unsigned *grid) {
   Pieces p;
   p.per_row = (int)(up(padded / 8, 4));
   p.valid = (int)(cols / 8);
   p.total = rows * p.per_row;
-  p.inv = ~0ull / (unsigned long long)p.per_row + 1;   // ceil(2^64 / per_row): per_row is at least 4, and if it divides 2^64 this is the quotient
+  p.inv = ~0ull / (unsigned long long)p.per_row + 1;   // (per_row is at least 4; where it divides 2^64 this is the quotient)
+  *grid = (unsigned)std::min<int64_t>((p.total + kActThreads - 1) / kActThreads, (int64_t)blocks * b->n_lanes);
+  const int64_t step = (int64_t)*grid * kActThreads;
+  p.step_rows = step / p.per_row;
+  p.step_pieces = (int)(step % p.per_row);
   return p;
 }
 CkptRows ckpt_rows(const void *p, int64_t cols) { return {static_cast<uint8_t *>(const_cast<void *>(p)), ckpt_pitch(cols), ckpt_scale_offset(cols)}; }
-int64_t act_blocks(const Pieces &p, int per_thread) { return (p.total + kActThreads * per_thread - 1) / (kActThreads * per_thread); }
 
 // calls f with a null pointer of the type
 template <class F>
@@ -391,10 +395,11 @@ int augtree_ckpt_pack(const augtree_block_t *b, const void *x, int dtype, int64_
   if (!dtype_ok(dtype) || !ld_ok(ld, cols)) return AUGTREE_ERR_INVALID_ARG;
   if (n_tokens == 0) return AUGTREE_OK;
   if (!x || !ckpt || !aligned16(x) || !aligned16(ckpt)) return AUGTREE_ERR_INVALID_ARG;
-  const Pieces p = pieces(n_tokens, cols, cols);
+  unsigned grid;
+  const Pieces p = pieces(b, n_tokens, cols, cols, kPackBlocks, &grid);
   return with_type(dtype, [&](auto *t) {
     using T = std::remove_pointer_t<decltype(t)>;
-    return launch(ckpt_pack_kernel<T>, (unsigned)act_blocks(p, 4), kActThreads, 0, static_cast<cudaStream_t>(stream), static_cast<const T *>(x), ld, p, ckpt_rows(ckpt, cols));
+    return launch(ckpt_pack_kernel<T>, grid, kActThreads, 0, static_cast<cudaStream_t>(stream), static_cast<const T *>(x), ld, p, ckpt_rows(ckpt, cols));
   });
 }
 
@@ -405,10 +410,11 @@ int augtree_ckpt_unpack(const augtree_block_t *b, const void *ckpt, int64_t n_to
   if (!dtype_ok(dtype) || (col && !dtype_ok(col_dtype)) || !ld_ok(ld, cols)) return AUGTREE_ERR_INVALID_ARG;
   if (n_tokens == 0) return AUGTREE_OK;
   if (!ckpt || !out || !aligned16(ckpt) || !aligned16(out) || !aligned(row, 4) || !aligned16(col)) return AUGTREE_ERR_INVALID_ARG;
-  const Pieces p = pieces(n_tokens, cols, cols);
+  unsigned grid;
+  const Pieces p = pieces(b, n_tokens, cols, cols, kPackBlocks, &grid);
   return with_type(dtype, [&](auto *t) {
     using T = std::remove_pointer_t<decltype(t)>;
-    return launch(ckpt_unpack_kernel<T>, (unsigned)act_blocks(p, 4), kActThreads, 0, static_cast<cudaStream_t>(stream), ckpt_rows(ckpt, cols), p, (int)(cols / 8), row, col,
+    return launch(ckpt_unpack_kernel<T>, grid, kActThreads, 0, static_cast<cudaStream_t>(stream), ckpt_rows(ckpt, cols), p, (int)(cols / 8), row, col,
                   col_dtype, static_cast<T *>(out), ld);
   });
 }
@@ -420,11 +426,12 @@ int augtree_glu_fwd(const augtree_block_t *b, const void *g, const void *u, int6
   if (!dtype_ok(dtype) || !ld_ok(ld, cols) || !ckpt_g != !ckpt_u) return AUGTREE_ERR_INVALID_ARG;
   if (n_tokens == 0) return AUGTREE_OK;
   if (!g || !u || !a || !aligned16(g) || !aligned16(u) || !aligned16(a) || !aligned16(ckpt_g) || !aligned16(ckpt_u)) return AUGTREE_ERR_INVALID_ARG;
-  const Pieces p = pieces(n_tokens, cols, cols);
+  unsigned grid;
+  const Pieces p = pieces(b, n_tokens, cols, cols, kGluFwdBlocks, &grid);
   return with_type(dtype, [&](auto *t) {
     using T = std::remove_pointer_t<decltype(t)>;
     auto run = [&](auto kernel) {
-      return launch(kernel, (unsigned)act_blocks(p, 2), kActThreads, 0, static_cast<cudaStream_t>(stream), static_cast<const T *>(g), static_cast<const T *>(u), ld, p,
+      return launch(kernel, grid, kActThreads, 0, static_cast<cudaStream_t>(stream), static_cast<const T *>(g), static_cast<const T *>(u), ld, p,
                     static_cast<T *>(a), cols, ckpt_rows(ckpt_g, cols), ckpt_rows(ckpt_u, cols));
     };
     return ckpt_g ? run(glu_fwd_kernel<T, true>) : run(glu_fwd_kernel<T, false>);
@@ -441,11 +448,12 @@ int augtree_glu_bwd(const augtree_block_t *b, const void *da, int dtype, const v
   if (!da || !g || !u || !dg || !du) return AUGTREE_ERR_INVALID_ARG;
   for (const void *q : {da, g, u, (const void *)dg, (const void *)du, (const void *)a})
     if (!aligned16(q)) return AUGTREE_ERR_INVALID_ARG;
-  const Pieces p = pieces(n_tokens, cols, cols);
+  unsigned grid;
+  const Pieces p = pieces(b, n_tokens, cols, cols, kGluBwdBlocks, &grid);
   return with_type(dtype, [&](auto *t) {
     using T = std::remove_pointer_t<decltype(t)>;
     auto run = [&](auto kernel) {
-      return launch(kernel, (unsigned)act_blocks(p, 2), kActThreads, 0, static_cast<cudaStream_t>(stream), static_cast<const T *>(da), static_cast<const T *>(g),
+      return launch(kernel, grid, kActThreads, 0, static_cast<cudaStream_t>(stream), static_cast<const T *>(da), static_cast<const T *>(g),
                     static_cast<const T *>(u), ld, ckpt_rows(g, cols), ckpt_rows(u, cols), p, cols, static_cast<T *>(dg), static_cast<T *>(du),
                     ld_grad, static_cast<T *>(a));
     };
@@ -480,9 +488,10 @@ int augtree_ckpt_wgrad(const augtree_block_t *b, const void *dy, int64_t n_token
   WgradWs w;
   if (!ws || !aligned16(ws) || ws_bytes < wgrad_layout(b, n_tokens, out_features, cols, static_cast<uint8_t *>(ws), &w)) return AUGTREE_ERR_WORKSPACE;
   const int64_t padded = up(cols, 64);
-  Pieces pc = pieces(n_tokens, cols, padded);
+  unsigned blocks;
+  Pieces pc = pieces(b, n_tokens, cols, padded, kPackBlocks, &blocks);
   pc.valid = pc.per_row;
-  if ((r = launch(ckpt_unpack_kernel<__nv_bfloat16>, (unsigned)act_blocks(pc, 4), kActThreads, 0, st, ckpt_rows(ckpt, cols), pc, (int)(cols / 8), row, nullptr, 0,
+  if ((r = launch(ckpt_unpack_kernel<__nv_bfloat16>, blocks, kActThreads, 0, st, ckpt_rows(ckpt, cols), pc, (int)(cols / 8), row, nullptr, 0,
                   w.x, padded)))
     return r;
   WgradParams p = {};
