@@ -3,6 +3,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <initializer_list>
 #include <new>
 #include <type_traits>
 
@@ -53,13 +54,16 @@ bool ld_ok(int64_t &ld, int64_t cols) {
   return ld >= cols && ld % 8 == 0;
 }
 
-// The walk over a matrix (act_kernels.cuh) and its grid: as many blocks as the SMs hold at a time.
-Pieces pieces(const augtree_block *b, int64_t rows, int64_t cols, int64_t padded, int blocks, unsigned *grid) {
+// The walk over matrices of `cols` columns (act_kernels.cuh) and its grid: as many blocks as the SMs hold at a time.
+struct Matrix { const void *p; int64_t ld; int bytes; };    // bytes of an element
+Pieces pieces(const augtree_block *b, int64_t rows, int64_t cols, int blocks, std::initializer_list<Matrix> all, unsigned *grid) {
   Pieces p;
-  p.per_row = (int)(up(padded / 8, 4));
+  p.per_row = (int)(up(cols, 32) / 16);
   p.valid = (int)(cols / 8);
   p.total = rows * p.per_row;
-  p.inv = ~0ull / (unsigned long long)p.per_row + 1;   // (per_row is at least 4; where it divides 2^64 this is the quotient)
+  p.inv = ~0ull / (unsigned long long)p.per_row + 1;   // (per_row is at least 2; where it divides 2^64 this is the quotient)
+  p.wide = true;
+  for (const Matrix &m : all) p.wide = p.wide && aligned(m.p, 32) && m.ld * m.bytes % 32 == 0;
   *grid = (unsigned)std::min<int64_t>((p.total + kActThreads - 1) / kActThreads, (int64_t)blocks * b->n_lanes);
   const int64_t step = (int64_t)*grid * kActThreads;
   p.step_rows = step / p.per_row;
@@ -396,7 +400,7 @@ int augtree_ckpt_pack(const augtree_block_t *b, const void *x, int dtype, int64_
   if (n_tokens == 0) return AUGTREE_OK;
   if (!x || !ckpt || !aligned16(x) || !aligned16(ckpt)) return AUGTREE_ERR_INVALID_ARG;
   unsigned grid;
-  const Pieces p = pieces(b, n_tokens, cols, cols, kPackBlocks, &grid);
+  const Pieces p = pieces(b, n_tokens, cols, dtype == AUGTREE_F32 ? kPackBlocks<float> : kPackBlocks<__half>, {{x, ld, size_of(dtype)}}, &grid);
   return with_type(dtype, [&](auto *t) {
     using T = std::remove_pointer_t<decltype(t)>;
     return launch(ckpt_pack_kernel<T>, grid, kActThreads, 0, static_cast<cudaStream_t>(stream), static_cast<const T *>(x), ld, p, ckpt_rows(ckpt, cols));
@@ -411,7 +415,7 @@ int augtree_ckpt_unpack(const augtree_block_t *b, const void *ckpt, int64_t n_to
   if (n_tokens == 0) return AUGTREE_OK;
   if (!ckpt || !out || !aligned16(ckpt) || !aligned16(out) || !aligned(row, 4) || !aligned16(col)) return AUGTREE_ERR_INVALID_ARG;
   unsigned grid;
-  const Pieces p = pieces(b, n_tokens, cols, cols, kPackBlocks, &grid);
+  const Pieces p = pieces(b, n_tokens, cols, kUnpackBlocks, {{out, ld, size_of(dtype)}}, &grid);
   return with_type(dtype, [&](auto *t) {
     using T = std::remove_pointer_t<decltype(t)>;
     return launch(ckpt_unpack_kernel<T>, grid, kActThreads, 0, static_cast<cudaStream_t>(stream), ckpt_rows(ckpt, cols), p, (int)(cols / 8), row, col,
@@ -426,8 +430,9 @@ int augtree_glu_fwd(const augtree_block_t *b, const void *g, const void *u, int6
   if (!dtype_ok(dtype) || !ld_ok(ld, cols) || !ckpt_g != !ckpt_u) return AUGTREE_ERR_INVALID_ARG;
   if (n_tokens == 0) return AUGTREE_OK;
   if (!g || !u || !a || !aligned16(g) || !aligned16(u) || !aligned16(a) || !aligned16(ckpt_g) || !aligned16(ckpt_u)) return AUGTREE_ERR_INVALID_ARG;
+  const int size = size_of(dtype);
   unsigned grid;
-  const Pieces p = pieces(b, n_tokens, cols, cols, kGluFwdBlocks, &grid);
+  const Pieces p = pieces(b, n_tokens, cols, kGluBlocks, {{g, ld, size}, {u, ld, size}, {a, cols, size}}, &grid);
   return with_type(dtype, [&](auto *t) {
     using T = std::remove_pointer_t<decltype(t)>;
     auto run = [&](auto kernel) {
@@ -448,8 +453,11 @@ int augtree_glu_bwd(const augtree_block_t *b, const void *da, int dtype, const v
   if (!da || !g || !u || !dg || !du) return AUGTREE_ERR_INVALID_ARG;
   for (const void *q : {da, g, u, (const void *)dg, (const void *)du, (const void *)a})
     if (!aligned16(q)) return AUGTREE_ERR_INVALID_ARG;
+  const int size = size_of(dtype);
   unsigned grid;
-  const Pieces p = pieces(b, n_tokens, cols, cols, kGluBwdBlocks, &grid);
+  const Pieces p = kept ? pieces(b, n_tokens, cols, kGluBlocks, {{da, cols, size}, {dg, ld_grad, size}, {du, ld_grad, size}, {a, cols, size}}, &grid)
+                        : pieces(b, n_tokens, cols, kGluBlocks, {{da, cols, size}, {g, ld, size}, {u, ld, size}, {dg, ld_grad, size}, {du, ld_grad, size},
+                                                                     {a, cols, size}}, &grid);
   return with_type(dtype, [&](auto *t) {
     using T = std::remove_pointer_t<decltype(t)>;
     auto run = [&](auto kernel) {
@@ -489,10 +497,8 @@ int augtree_ckpt_wgrad(const augtree_block_t *b, const void *dy, int64_t n_token
   if (!ws || !aligned16(ws) || ws_bytes < wgrad_layout(b, n_tokens, out_features, cols, static_cast<uint8_t *>(ws), &w)) return AUGTREE_ERR_WORKSPACE;
   const int64_t padded = up(cols, 64);
   unsigned blocks;
-  Pieces pc = pieces(b, n_tokens, cols, padded, kPackBlocks, &blocks);
-  pc.valid = pc.per_row;
-  if ((r = launch(ckpt_unpack_kernel<__nv_bfloat16>, blocks, kActThreads, 0, st, ckpt_rows(ckpt, cols), pc, (int)(cols / 8), row, nullptr, 0,
-                  w.x, padded)))
+  const Pieces pc = pieces(b, n_tokens, padded, kUnpackBlocks, {{w.x, padded, 2}}, &blocks);
+  if ((r = launch(ckpt_unpack_kernel<__nv_bfloat16>, blocks, kActThreads, 0, st, ckpt_rows(ckpt, cols), pc, (int)(cols / 8), row, nullptr, 0, w.x, padded)))
     return r;
   WgradParams p = {};
   p.out = (int)out_features; p.cols = (int)cols; p.steps = (int)((n_tokens + 63) / 64);
