@@ -141,17 +141,7 @@ __device__ __forceinline__ V8 values(const RawCkpt &r, int run, float f = 1.f) {
   return ckpt_decode(run ? make_uint2(r.q.z, r.q.w) : make_uint2(r.q.x, r.q.y), ckpt_unit(r.byte) * f);
 }
 
-// 8 columns of a row's checkpoint; every lane of the warp takes part, pieces from `valid` on are not written
-__device__ __forceinline__ void ckpt_store(uint8_t *row, int piece, int valid, long long scales, const V8 &x) {
-  uint2 q;
-  uint32_t byte;
-  ckpt_encode(x, q, byte);
-  if (piece >= valid) return;
-  *reinterpret_cast<uint2 *>(row + piece * 8) = q;
-  if ((piece & 3) == 0) row[scales + (piece >> 2)] = (uint8_t)byte;
-}
-
-// 16 columns of a row's checkpoint, likewise
+// 16 columns of a row's checkpoint; every lane of the warp takes part
 __device__ __forceinline__ void ckpt_store16(uint8_t *row, int piece, bool there, long long scales, const V8 &lo, const V8 &hi) {
   uint4 q;
   uint32_t byte;

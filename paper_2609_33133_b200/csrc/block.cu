@@ -81,49 +81,60 @@ int with_type(int type, F f) {
 }
 
 // ---------------------------------------------------------------- block ends
-int vecs_per_thread(int hidden) { return hidden <= 256 ? 1 : 2; }
-
+// Pieces of 8 columns of a thread (kParts): one for rows that a warp covers with them, two otherwise, four forward with a 16-bit stream: the more, the
+// fewer warps share a row and the less its reductions and addresses cost (16384 x 3584 bf16 with checkpoints, forward: 154 us with two, 131 with three, 118
+// with four), but an fp32 stream, whose rows are as near to memory's rate with two, takes the stages that more groups need (162 us; 162 to 191 with four).
+// The backward pass keeps its sums over tokens in registers, which leave no room for more than two.
+int fwd_parts(int hidden, int x) { return hidden <= 256 ? 1 : x == T_BF16 ? 4 : 2; }
+int bwd_parts(int hidden) { return hidden <= 256 ? 1 : 2; }
 bool wide_bwd(int hidden) { return hidden > kBlockBwdWarps * 512; }
 
 // calls f with the kernel for a width, a stream type (kAny: types looked up), a form of the call and a gate
-template <int VPT, int X, class F>
+template <int P, int X, class F>
 int with_fwd_form(int form, int gate, F f) {
-  if (form == kBefore) return f(block_fwd_kernel<VPT, X, T_BF16, kBefore, GATE_NONE>);
-  if (gate == GATE_NONE) return f(block_fwd_kernel<VPT, X, T_BF16, kBoth, GATE_NONE>);
-  if (gate == GATE_TOKEN) return f(block_fwd_kernel<VPT, X, T_BF16, kBoth, GATE_TOKEN>);
-  if (gate == GATE_CHANNEL) return f(block_fwd_kernel<VPT, X, T_BF16, kBoth, GATE_CHANNEL>);
-  return f(block_fwd_kernel<VPT, X, T_BF16, kBoth, GATE_FULL>);
+  if (form == kBefore) return f(block_fwd_kernel<P, X, T_BF16, kBefore, GATE_NONE>);
+  if (gate == GATE_NONE) return f(block_fwd_kernel<P, X, T_BF16, kBoth, GATE_NONE>);
+  if (gate == GATE_TOKEN) return f(block_fwd_kernel<P, X, T_BF16, kBoth, GATE_TOKEN>);
+  if (gate == GATE_CHANNEL) return f(block_fwd_kernel<P, X, T_BF16, kBoth, GATE_CHANNEL>);
+  return f(block_fwd_kernel<P, X, T_BF16, kBoth, GATE_FULL>);
 }
-template <int VPT, class F>
+template <int P, class F>
 int with_fwd_types(int x, int form, int gate, F f) {
-  if (x == T_F32) return with_fwd_form<VPT, T_F32>(form, gate, f);
-  if (x == T_BF16) return with_fwd_form<VPT, T_BF16>(form, gate, f);
-  return f(block_fwd_kernel<VPT, kAny, kAny, kAny, kAny>);
+  if constexpr (P != 4) {
+    if (x == T_F32) return with_fwd_form<P, T_F32>(form, gate, f);
+    if (x == kAny) return f(block_fwd_kernel<P, kAny, kAny, kAny, kAny>);
+  }
+  if constexpr (P != 2) return with_fwd_form<P, T_BF16>(form, gate, f);
+  return AUGTREE_ERR_INTERNAL;
 }
 template <class F>
 int with_fwd(int hidden, int x, int form, int gate, F f) {
-  return vecs_per_thread(hidden) == 1 ? with_fwd_types<1>(x, form, gate, f) : with_fwd_types<2>(x, form, gate, f);
+  switch (fwd_parts(hidden, x)) {
+    case 1: return with_fwd_types<1>(x, form, gate, f);
+    case 2: return with_fwd_types<2>(x, form, gate, f);
+    default: return with_fwd_types<4>(x, form, gate, f);
+  }
 }
-template <int VPT, int X, bool kKept, class F>
+template <int P, int X, bool kKept, class F>
 int with_bwd_form(int form, int gate, F f) {
   constexpr int W = kBlockBwdWarps;
-  if (form == kBefore) return f(block_bwd_kernel<VPT, W, X, T_BF16, kBefore, GATE_NONE, kKept>);
-  if (gate == GATE_NONE) return f(block_bwd_kernel<VPT, W, X, T_BF16, kBoth, GATE_NONE, kKept>);
-  if (gate == GATE_TOKEN) return f(block_bwd_kernel<VPT, W, X, T_BF16, kBoth, GATE_TOKEN, kKept>);
-  if (gate == GATE_CHANNEL) return f(block_bwd_kernel<VPT, W, X, T_BF16, kBoth, GATE_CHANNEL, kKept>);
-  return f(block_bwd_kernel<VPT, W, X, T_BF16, kBoth, GATE_FULL, kKept>);
+  if (form == kBefore) return f(block_bwd_kernel<P, W, X, T_BF16, kBefore, GATE_NONE, kKept>);
+  if (gate == GATE_NONE) return f(block_bwd_kernel<P, W, X, T_BF16, kBoth, GATE_NONE, kKept>);
+  if (gate == GATE_TOKEN) return f(block_bwd_kernel<P, W, X, T_BF16, kBoth, GATE_TOKEN, kKept>);
+  if (gate == GATE_CHANNEL) return f(block_bwd_kernel<P, W, X, T_BF16, kBoth, GATE_CHANNEL, kKept>);
+  return f(block_bwd_kernel<P, W, X, T_BF16, kBoth, GATE_FULL, kKept>);
 }
-template <int VPT, class F>
+template <int P, class F>
 int with_bwd_types(int x, int form, int gate, bool kept, F f) {
-  if (x == T_F32) return kept ? with_bwd_form<VPT, T_F32, true>(form, gate, f) : with_bwd_form<VPT, T_F32, false>(form, gate, f);
-  if (x == T_BF16) return kept ? with_bwd_form<VPT, T_BF16, true>(form, gate, f) : with_bwd_form<VPT, T_BF16, false>(form, gate, f);
-  return f(block_bwd_kernel<VPT, kBlockBwdWarps, kAny, kAny, kAny, kAny, false>);
+  if (x == T_F32) return kept ? with_bwd_form<P, T_F32, true>(form, gate, f) : with_bwd_form<P, T_F32, false>(form, gate, f);
+  if (x == T_BF16) return kept ? with_bwd_form<P, T_BF16, true>(form, gate, f) : with_bwd_form<P, T_BF16, false>(form, gate, f);
+  return f(block_bwd_kernel<P, kBlockBwdWarps, kAny, kAny, kAny, kAny, false>);
 }
 // (rows of more than 7680 columns are always looked up)
 template <class F>
 int with_bwd(int hidden, int x, int form, int gate, bool kept, F f) {
   if (wide_bwd(hidden)) return f(block_bwd_kernel<2, kBlockBwdWarpsWide, kAny, kAny, kAny, kAny, false>);
-  return vecs_per_thread(hidden) == 1 ? with_bwd_types<1>(x, form, gate, kept, f) : with_bwd_types<2>(x, form, gate, kept, f);
+  return bwd_parts(hidden) == 1 ? with_bwd_types<1>(x, form, gate, kept, f) : with_bwd_types<2>(x, form, gate, kept, f);
 }
 // what is there has the branch's usual type
 bool bf16_or_none(bool there, int type) { return !there || type == AUGTREE_BF16; }
@@ -131,24 +142,26 @@ bool bf16_or_none(bool there, int type) { return !there || type == AUGTREE_BF16;
 struct Input { const void *p; int64_t row_bytes; };
 
 // Groups, stages and grid of a call; false if one row of all inputs does not fit shared memory.
-bool block_shape(const augtree_block *b, int64_t rows, const Input *in, int n_in, int weights, int max_warps, BlockShape *s, int *grid, size_t *smem) {
+bool block_shape(const augtree_block *b, int64_t rows, const Input *in, int n_in, int weights, int max_warps, int parts, BlockShape *s, int *grid, size_t *smem) {
   const int hidden = b->hidden;
   *s = {};
   s->rows = (int)rows; s->hidden = hidden; s->vecs = hidden / 8; s->weights = weights;
-  s->warps_row = (int)((s->vecs + 32 * vecs_per_thread(hidden) - 1) / (32 * vecs_per_thread(hidden)));
+  const int warp_vecs = 32 * parts;
+  s->warps_row = (s->vecs + warp_vecs - 1) / warp_vecs;
   int64_t row = 0;
   for (int i = 0; i < n_in; ++i) row += in[i].row_bytes;
   const int64_t fixed = kBlockFixed + (int64_t)weights * hidden * 4, room = kBlockSmem - fixed;
   if (row > room) return false;
-  int64_t groups = max_warps / s->warps_row;
-  while (groups > 1 && 2 * groups * row > room) --groups;        // two stages at least
+  // As many groups as leave three stages, or two where two groups would not.
+  const int64_t most = max_warps / s->warps_row;
+  int64_t groups = std::min<int64_t>(most, std::max<int64_t>(room / (3 * row), std::min<int64_t>(2, room / (2 * row))));
+  groups = std::max<int64_t>(groups, 1);
   s->groups = (int)groups;
   // Rows of a stage: one a group, more for narrow rows (a bulk copy of a few KB costs as much as one of 32 KB) as long as every
   // lane still gets eight blocks; fewer than one a group if the rows would not reach all lanes otherwise.
   int64_t per = 1, block = groups;
   if (rows < groups * b->n_lanes) block = std::max<int64_t>((rows + b->n_lanes - 1) / b->n_lanes, 1);
   else while (per < 8 && groups * (per + 1) * row <= 32 << 10 && rows >= groups * (per + 1) * b->n_lanes * 8) block = groups * ++per;
-  s->per_group = (int)per;
   s->block_rows = (int)block;
   s->blocks = (int)((rows + block - 1) / block);
   int64_t off = 0;
@@ -310,9 +323,13 @@ int augtree_block_fwd(const augtree_block_t *b, const void *x, int x_dtype, cons
   const int64_t c = b->hidden;
   p.gate = o ? b->gate : GATE_NONE;
   const Input in[3] = {{x, c * size_of(x_dtype)}, {o, o ? c * size_of(o_dtype) : 0}, {gate, p.gate == GATE_FULL ? c * size_of(gate_dtype) : 0}};
+  // what is compiled in (block_kernels.cuh): everything of the branch in bf16, a norm before the next block
+  const bool usual = h && bf16_or_none(h, h_dtype) && bf16_or_none(o, o_dtype) && bf16_or_none(p.gate == GATE_FULL, gate_dtype) && x_dtype != AUGTREE_F16;
+  const int types = usual ? x_dtype : kAny;
   int grid;
   size_t smem;
-  if (!block_shape(b, n_tokens, in, o ? p.gate == GATE_FULL ? 3 : 2 : 1, !!w_in + !!w_out + (p.gate == GATE_CHANNEL), kBlockFwdWarps, &p.s, &grid, &smem))
+  if (!block_shape(b, n_tokens, in, o ? p.gate == GATE_FULL ? 3 : 2 : 1, !!w_in + !!w_out + (p.gate == GATE_CHANNEL), kBlockFwdWarps,
+                   fwd_parts(b->hidden, types), &p.s, &grid, &smem))
     return AUGTREE_ERR_UNSUPPORTED;
   p.gate_type = gate_dtype; p.gate_ptr = gate;
   p.w_out = w_out; p.w_in = w_in; p.w_type = w_dtype;
@@ -323,9 +340,7 @@ int augtree_block_fwd(const augtree_block_t *b, const void *x, int x_dtype, cons
   p.ckpt_y = ckpt_rows(ckpt_y, c); p.ckpt_o = ckpt_rows(ckpt_o, c);
   const int threads = (p.s.groups * p.s.warps_row + 1) * 32;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  // what is compiled in (block_kernels.cuh): everything of the branch in bf16, a norm before the next block
-  const bool usual = h && bf16_or_none(h, h_dtype) && bf16_or_none(o, o_dtype) && bf16_or_none(p.gate == GATE_FULL, gate_dtype) && x_dtype != AUGTREE_F16;
-  return with_fwd(b->hidden, usual ? x_dtype : kAny, o ? kBoth : kBefore, p.gate, [&](auto kernel) { return launch(kernel, grid, threads, smem, st, p); });
+  return with_fwd(b->hidden, types, o ? kBoth : kBefore, p.gate, [&](auto kernel) { return launch(kernel, grid, threads, smem, st, p); });
 }
 
 int augtree_block_bwd(const augtree_block_t *b, const void *dy, int x_dtype, const void *dh, int h_dtype, const void *y, int y_dtype,
@@ -374,7 +389,7 @@ int augtree_block_bwd(const augtree_block_t *b, const void *dy, int x_dtype, con
   if (p.gate == GATE_FULL) in[n_in++] = {gate, row_of(gate_dtype)};
   int grid;
   size_t smem;
-  if (!block_shape(b, n_tokens, in, n_in, !!w_in + !!w_out + channel, wide_bwd(b->hidden) ? kBlockBwdWarpsWide : kBlockBwdWarps, &p.s, &grid, &smem)) return AUGTREE_ERR_UNSUPPORTED;
+  if (!block_shape(b, n_tokens, in, n_in, !!w_in + !!w_out + channel, wide_bwd(b->hidden) ? kBlockBwdWarpsWide : kBlockBwdWarps, bwd_parts(b->hidden), &p.s, &grid, &smem)) return AUGTREE_ERR_UNSUPPORTED;
   p.gate_type = gate_dtype; p.gate_ptr = gate;
   p.w_out = w_out; p.w_in = w_in; p.w_type = w_dtype;
   p.r_out = const_cast<float *>(r_out); p.r_in = const_cast<float *>(r_in);

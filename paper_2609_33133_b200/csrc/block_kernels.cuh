@@ -6,13 +6,14 @@
 //              u = o r_o,  do = r_o (w_o s a d - u mean(w_o s a d u)),           dw_o = sum over tokens of s a d u
 //              dg = s a'(g) d w_o u, summed over the channels for a gate of one number a token and over the tokens for one a channel
 //
-// Bound by memory: a row passes once, all arithmetic is in registers.  The rows' bytes are fetched ahead by the copy engine (one bulk
-// copy per tensor and block of rows, which are contiguous) into a ring of stages in shared memory, so what is in flight does not depend on
-// how many threads wait: 44 GB/s and SM at 6.5 TB/s need 35 KB in flight against 0.8 us of latency, and a row of 3584 channels is
-// 21 KB forward and 43 KB backward.  One CTA an SM; its warps form `groups` of as many warps as a row of 512 columns a warp needs (256 up
-// to 256 columns), and each group takes a row of a stage at a time, so one group's reductions run under another's arithmetic.
+// Bound by memory: a row passes once, all arithmetic is in registers.  Rows are fetched ahead by the copy engine (one bulk copy per tensor and
+// block of rows, which are contiguous) into a ring of stages in shared memory, so what is in flight does not depend on how many threads
+// wait: 44 GB/s and SM at 6.5 TB/s need 35 KB in flight against 0.8 us of latency, and a row of 3584 channels is 21 KB forward and 43 KB
+// backward.  One CTA an SM; its warps form `groups`, and each takes a row of a stage at a time, so one group's reductions run under another's
+// arithmetic.  A thread holds kParts pieces of 8 columns of a row.  (Rings of single rows, one for each group: 279 us instead of 240 for the
+// backward pass of 24576 x 3584 fp32, with the same instructions: copies of one row keep the memory less busy than copies of two.)
 // A group's sum over a row: shuffles, then the warps' sums through shared memory behind one named barrier.
-// The sums over tokens stay in registers (every thread owns its columns for all rows of its CTA), go over the groups through shared memory
+// The sums over tokens stay in registers (every thread owns its columns for all rows of its group), go over the groups through shared memory
 // and from CTA to CTA through scratch and a second kernel, in an order that depends on the sizes alone: no atomics, bitwise repeatable.
 // Every sum, statistic and product is fp32; values are rounded once, on delivery.  The 8-bit form of y is made from y as it is
 // delivered, so that it is the form that ckpt_pack makes of the tensor.
@@ -38,7 +39,6 @@ struct BlockShape {
   int rows, hidden, vecs;         // vecs: pieces of 8 columns of a row
   int warps_row, groups;          // warps of a group; groups of a CTA
   int block_rows, blocks;         // rows of a stage; blocks of rows of the call
-  int per_group;                  // rows of a stage that a group takes
   int stages, stage_bytes;
   int n_inputs;
   const uint8_t *input[kBlockMaxInputs];
@@ -84,11 +84,16 @@ __device__ __forceinline__ V8 block_load8(const uint8_t *row, int vec, int type,
   if (k == T_CKPT) return ckpt_decode(*reinterpret_cast<const uint2 *>(row + vec * 8), ckpt_unit(row[scales + (vec >> 2)]));
   return Row8<__half>::load(reinterpret_cast<const __half *>(row + vec * 16));
 }
-// the same times a number; one rounding either way
+// the same times a number (one rounding either way)
 template <int T>
 __device__ __forceinline__ V8 block_load8_times(const uint8_t *row, int vec, int type, int scales, float f) {
-  if (T == T_CKPT) return ckpt_decode(*reinterpret_cast<const uint2 *>(row + vec * 8), ckpt_unit(row[scales + (vec >> 2)]) * f);
-  return block_load8<T>(row, vec, type, scales) * f;
+  if constexpr (T == T_CKPT) return ckpt_decode(*reinterpret_cast<const uint2 *>(row + vec * 8), ckpt_unit(row[scales + (vec >> 2)]) * f);
+  else return block_load8<T>(row, vec, type, scales) * f;
+}
+__device__ __forceinline__ V8 only_if(bool there, V8 x) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = there ? x[i] : 0.f;
+  return x;
 }
 template <int T>
 __device__ __forceinline__ void block_store8(uint8_t *row, int vec, int type, const V8 &x) {
@@ -96,6 +101,34 @@ __device__ __forceinline__ void block_store8(uint8_t *row, int vec, int type, co
   if (k == T_BF16) Row8<__nv_bfloat16>::store(reinterpret_cast<__nv_bfloat16 *>(row + vec * 16), x);
   else if (k == T_F32) Row8<float>::store(reinterpret_cast<float *>(row + vec * 32), x);
   else Row8<__half>::store(reinterpret_cast<__half *>(row + vec * 16), x);
+}
+// A thread's kParts pieces of a row into its checkpoint.  The four lanes of a quad hold a group of 32 columns in each part; two parts' exponents go
+// through one pair of shuffles, and each lane of the quad writes one part's.
+template <int kParts>
+__device__ __forceinline__ void block_keep(uint8_t *row, int v0, int step, int vecs, long long scales, const V8 (&x)[kParts]) {
+  uint32_t byte[kParts];
+#pragma unroll
+  for (int k = 0; k < kParts; ++k) byte[k] = ckpt_byte(max_magnitude(x[k]));
+#pragma unroll
+  for (int k = 0; k < kParts; k += 2) {
+    uint32_t two = byte[k];
+    if (k + 1 < kParts) two |= byte[k + 1] << 16;
+    two = __vmaxu2(two, __shfl_xor_sync(0xffffffffu, two, 1));
+    two = __vmaxu2(two, __shfl_xor_sync(0xffffffffu, two, 2));
+    byte[k] = two & 0xffffu;
+    if (k + 1 < kParts) byte[k + 1] = two >> 16;
+  }
+  const int quad = v0 & 3;
+  uint32_t mine = byte[0];
+#pragma unroll
+  for (int k = 0; k < kParts; ++k) {
+    const int v = v0 + k * step;
+    const uint2 q = ckpt_integers(x[k], ckpt_per(byte[k]));
+    if (v < vecs) *reinterpret_cast<uint2 *>(row + v * 8) = q;
+    if (k == quad) mine = byte[k];
+  }
+  const int v = (v0 - quad) + quad * step;     // the group's first piece in part `quad`
+  if (quad < kParts && v < vecs) row[scales + (v >> 2)] = (uint8_t)mine;
 }
 // row t of a matrix in global memory
 template <int T>
@@ -154,7 +187,12 @@ __device__ __forceinline__ BlockCta block_setup(uint8_t *smem, const BlockParams
 __device__ __forceinline__ uint8_t *block_stage(const BlockCta &c, const BlockParams &p, int stage) {
   return c.smem + kBlockFixed + p.s.weights * p.s.hidden * 4 + stage * p.s.stage_bytes;
 }
-// a vector of one number a channel into shared memory as fp32
+// A vector of one number a channel into shared memory as fp32, the halves of its pieces of 8 in two runs, so that neighbouring lanes read
+// neighbouring 16 bytes.
+__device__ __forceinline__ V8 block_weight(const float *w, int vec, int vecs) {
+  const float4 a = reinterpret_cast<const float4 *>(w)[vec], b = reinterpret_cast<const float4 *>(w)[vecs + vec];
+  return {{make_float2(a.x, a.y), make_float2(a.z, a.w), make_float2(b.x, b.y), make_float2(b.z, b.w)}};
+}
 __device__ __forceinline__ void block_weights(const BlockCta &c, const BlockParams &p, int slot, const void *w, int type) {
   float *dst = c.weights + slot * p.s.hidden;
   for (int i = threadIdx.x; i < p.s.vecs; i += blockDim.x) {
@@ -162,8 +200,8 @@ __device__ __forceinline__ void block_weights(const BlockCta &c, const BlockPara
     if (type == T_BF16) x = Row8<__nv_bfloat16>::load(static_cast<const __nv_bfloat16 *>(w) + i * 8);
     else if (type == T_F32) x = Row8<float>::load(static_cast<const float *>(w) + i * 8);
     else x = Row8<__half>::load(static_cast<const __half *>(w) + i * 8);
-    reinterpret_cast<float4 *>(dst)[2 * i] = make_float4(x[0], x[1], x[2], x[3]);
-    reinterpret_cast<float4 *>(dst)[2 * i + 1] = make_float4(x[4], x[5], x[6], x[7]);
+    reinterpret_cast<float4 *>(dst)[i] = make_float4(x[0], x[1], x[2], x[3]);
+    reinterpret_cast<float4 *>(dst)[p.s.vecs + i] = make_float4(x[4], x[5], x[6], x[7]);
   }
 }
 
@@ -240,7 +278,7 @@ struct BlockWalk {
   }
 };
 
-template <int VPT, int XT, int OT, int FORM, int GATE>
+template <int kParts, int XT, int OT, int FORM, int GATE>
 __global__ void __launch_bounds__((kBlockFwdWarps + 1) * 32, 1)
 block_fwd_kernel(const __grid_constant__ BlockParams p) {
   extern __shared__ __align__(1024) uint8_t smem_raw[];
@@ -265,8 +303,12 @@ block_fwd_kernel(const __grid_constant__ BlockParams p) {
   } else {
     const int group = warp / s.warps_row;
     BlockGroup g{c.sums + group * 64, s.warps_row, warp - group * s.warps_row, group + 1, 0};
-    const int v0 = g.warp * 32 + lane, step = s.warps_row * 32, vecs = s.vecs;     // pieces v0, v0 + step
+    const int v0 = g.warp * 32 + lane, step = s.warps_row * 32, vecs = s.vecs;     // pieces of 8 columns: v0, v0 + step, ..
     const bool writer = g.warp == 0 && lane == 0;
+    int at[kParts];
+    bool there[kParts];
+#pragma unroll
+    for (int k = 0; k < kParts; ++k) { there[k] = v0 + k * step < vecs; at[k] = min(v0 + k * step, vecs - 1); }
     int st = 0;
     uint32_t phase = 0;
     BlockWalk walk(s, group);
@@ -287,65 +329,58 @@ block_fwd_kernel(const __grid_constant__ BlockParams p) {
           ga *= p.sigmoid ? logistic(gt_next) : gt_next;
           if (walk.next >= 0) gt_next = block_scalar(p.gate_ptr, walk.next, p.gate_type);
         }
-        V8 y[VPT];
+        // Straight through, without a branch for the pieces behind the row's end: their threads work on the last piece (at[k]) and count for nothing.
+        V8 y[kParts];
         if (branch) {
-          V8 o[VPT];
-          float2 ss = both(0.f);
+          // (o is read twice rather than kept: registers are warps)
           float r_o = 1.f;
+          if (norm_out || p.ckpt_o.base) {
+            V8 o[kParts];
+            float2 ss = both(0.f);
 #pragma unroll
-          for (int k = 0; k < VPT; ++k) {
-            const int v = v0 + k * step;
-            o[k] = v < vecs ? block_load8<OT>(ro, v, p.o_type, 0) : v8(0.f);
-            ss = dot2(o[k], o[k], ss);
-          }
-          if (norm_out) {
-            r_o = rsqrtf(fmaf(g.sum(ss.x + ss.y), p.inv_hidden, p.eps));
-            if (p.r_out && writer) p.r_out[t] = r_o;
-          }
-          if (p.ckpt_o.base) {
-            uint8_t *row = p.ckpt_o.base + t * p.ckpt_o.pitch;
-#pragma unroll
-            for (int k = 0; k < VPT; ++k) ckpt_store(row, v0 + k * step, vecs, p.ckpt_o.scales, o[k]);
+            for (int k = 0; k < kParts; ++k) {
+              o[k] = only_if(there[k], block_load8<OT>(ro, at[k], p.o_type, 0));
+              ss = dot2(o[k], o[k], ss);
+            }
+            if (p.ckpt_o.base) block_keep(p.ckpt_o.base + t * p.ckpt_o.pitch, v0, step, vecs, p.ckpt_o.scales, o);
+            if (norm_out) {
+              r_o = rsqrtf(fmaf(g.sum(ss.x + ss.y), p.inv_hidden, p.eps));
+              if (p.r_out && writer) p.r_out[t] = r_o;
+            }
           }
           uint8_t *ry = block_row<XT>(p.y, t, hidden, p.x_type);
 #pragma unroll
-          for (int k = 0; k < VPT; ++k) {
-            const int v = v0 + k * step;
-            y[k] = v8(0.f);
-            if (v < vecs) {
-              if (norm_out) o[k] = Row8<float>::load(w_out + v * 8) * (o[k] * r_o);
-              if (gate >= GATE_CHANNEL) {
-                const V8 a = gate == GATE_FULL ? block_load8<OT>(stage + s.offset[2] + r * s.row_bytes[2], v, p.gate_type, 0) : Row8<float>::load(g_ch + v * 8);
-                o[k] = o[k] * (p.sigmoid ? logistic(a) : a);
-              }
-              y[k] = fma(o[k], ga, block_load8<XT>(rx, v, p.x_type, 0));
-              block_store8<XT>(ry, v, p.x_type, y[k]);
+          for (int k = 0; k < kParts; ++k) {
+            V8 z = block_load8<OT>(ro, at[k], p.o_type, 0);
+            if (norm_out) z = block_weight(w_out, at[k], vecs) * (z * r_o);
+            if (gate >= GATE_CHANNEL) {
+              const V8 a = gate == GATE_FULL ? block_load8<OT>(stage + s.offset[2] + r * s.row_bytes[2], at[k], p.gate_type, 0) : block_weight(g_ch, at[k], vecs);
+              z = z * (p.sigmoid ? logistic(a) : a);
             }
+            y[k] = only_if(there[k], fma(z, ga, block_load8<XT>(rx, at[k], p.x_type, 0)));
+            if (there[k]) block_store8<XT>(ry, at[k], p.x_type, y[k]);
           }
         } else {
 #pragma unroll
-          for (int k = 0; k < VPT; ++k) {
-            const int v = v0 + k * step;
-            y[k] = v < vecs ? block_load8<XT>(rx, v, p.x_type, 0) : v8(0.f);
-          }
+          for (int k = 0; k < kParts; ++k) y[k] = only_if(there[k], block_load8<XT>(rx, at[k], p.x_type, 0));
         }
         if (norm_in) {
           float2 ss = both(0.f);
 #pragma unroll
-          for (int k = 0; k < VPT; ++k) ss = dot2(y[k], y[k], ss);
+          for (int k = 0; k < kParts; ++k) ss = dot2(y[k], y[k], ss);
           const float r_i = rsqrtf(fmaf(g.sum(ss.x + ss.y), p.inv_hidden, p.eps));
           if (p.r_in && writer) p.r_in[t] = r_i;
           uint8_t *rh = block_row<OT>(p.h, t, hidden, p.h_type);
 #pragma unroll
-          for (int k = 0; k < VPT; ++k) {
-            const int v = v0 + k * step;
-            if (v < vecs) block_store8<OT>(rh, v, p.h_type, Row8<float>::load(w_in + v * 8) * (y[k] * r_i));
+          for (int k = 0; k < kParts; ++k) {
+            const V8 h = block_weight(w_in, at[k], vecs) * (y[k] * r_i);
+            if (there[k]) block_store8<OT>(rh, at[k], p.h_type, h);
           }
         }
         if (p.ckpt_y.base) {
-          uint8_t *row = p.ckpt_y.base + t * p.ckpt_y.pitch;
 #pragma unroll
-          for (int k = 0; k < VPT; ++k) ckpt_store(row, v0 + k * step, vecs, p.ckpt_y.scales, block_round<XT>(y[k], p.x_type));
+          for (int k = 0; k < kParts; ++k) y[k] = block_round<XT>(y[k], p.x_type);
+          block_keep(p.ckpt_y.base + t * p.ckpt_y.pitch, v0, step, vecs, p.ckpt_y.scales, y);
         }
       }
       warp_arrive(c.bar_empty + 8 * st);
@@ -356,7 +391,7 @@ block_fwd_kernel(const __grid_constant__ BlockParams p) {
 }
 
 // kKept: v and u are read from checkpoints, both (with kAny each from what its type says).
-template <int VPT, int kWarps, int XT, int OT, int FORM, int GATE, bool kKept>
+template <int kParts, int kWarps, int XT, int OT, int FORM, int GATE, bool kKept>
 __global__ void __launch_bounds__((kWarps + 1) * 32, 1)
 block_bwd_kernel(const __grid_constant__ BlockParams p) {
   extern __shared__ __align__(1024) uint8_t smem_raw[];
@@ -377,13 +412,17 @@ block_bwd_kernel(const __grid_constant__ BlockParams p) {
   __syncthreads();
   const AbortCtx ab{c.abort_flag, p.status, p.wait_budget};
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  V8 acc_in[VPT], acc_out[VPT];
+  V8 acc_in[kParts], acc_out[kParts];
 #pragma unroll
-  for (int k = 0; k < VPT; ++k) acc_in[k] = acc_out[k] = v8(0.f);
+  for (int k = 0; k < kParts; ++k) acc_in[k] = acc_out[k] = v8(0.f);
   const int group = warp / s.warps_row;
   BlockGroup g{c.sums + group * 64, s.warps_row, warp - group * s.warps_row, group + 1, 0};
   const int v0 = g.warp * 32 + lane, step = s.warps_row * 32, vecs = s.vecs;
   const bool computes = group < s.groups, writer = g.warp == 0 && lane == 0;
+  int at[kParts];        // the thread's pieces, those behind the row's end replaced by the last one: see the forward kernel
+  bool there[kParts];
+#pragma unroll
+  for (int k = 0; k < kParts; ++k) { there[k] = v0 + k * step < vecs; at[k] = min(v0 + k * step, vecs - 1); }
   if (!computes) {
     if (lane == 0) block_produce(c, p, ab);
     __syncwarp();
@@ -411,84 +450,84 @@ block_bwd_kernel(const __grid_constant__ BlockParams p) {
         walk.at(row0, r, rows);
         const long long t = walk.t;
         auto row = [&](int i) { return stage + s.offset[i] + r * s.row_bytes[i]; };
-        const float r_i = ri_next, r_o = ro_next, at = gate == GATE_TOKEN && p.sigmoid ? logistic(gt_next) : gt_next;
+        const float r_i = ri_next, r_o = ro_next, gate_t = gate == GATE_TOKEN && p.sigmoid ? logistic(gt_next) : gt_next;
         fetch();
-        V8 d[VPT];
+        // v and u from checkpoints are kept between their two uses, others are read again (24576 x 3584 fp32: 240 us against 258 kept; 16384 x 3584
+        // bf16 with checkpoints: 160 us kept against 175).
+        V8 d[kParts];
         if (has_dh) {
-          V8 v[VPT];
+          V8 v[kParts];
           float2 dot = both(0.f);
           const uint8_t *rh = row(at_dh), *ry = row(at_y);
 #pragma unroll
-          for (int k = 0; k < VPT; ++k) {
-            const int at8 = v0 + k * step;
-            v[k] = d[k] = v8(0.f);
-            if (at8 < vecs) {
-              const V8 dh = block_load8<OT>(rh, at8, p.h_type, 0);
-              v[k] = block_load8_times<YT>(ry, at8, p.y_type, scales, r_i);
-              acc_in[k] = fma(dh, v[k], acc_in[k]);
-              d[k] = Row8<float>::load(w_in + at8 * 8) * dh;
-            }
+          for (int k = 0; k < kParts; ++k) {
+            const V8 dh = only_if(there[k], block_load8<OT>(rh, at[k], p.h_type, 0));
+            v[k] = block_load8_times<YT>(ry, at[k], p.y_type, scales, r_i);
+            acc_in[k] = fma(dh, v[k], acc_in[k]);
+            d[k] = block_weight(w_in, at[k], vecs) * dh;
             dot = dot2(d[k], v[k], dot);
           }
-          const float mean = g.sum(dot.x + dot.y) * p.inv_hidden;
+          const float mean = -g.sum(dot.x + dot.y) * p.inv_hidden;
 #pragma unroll
-          for (int k = 0; k < VPT; ++k) d[k] = fma(v[k], -mean, d[k]) * r_i;
+          for (int k = 0; k < kParts; ++k) {
+            if (YT != T_CKPT) v[k] = block_load8_times<YT>(ry, at[k], p.y_type, scales, r_i);
+            d[k] = fma(v[k], mean, d[k]) * r_i;
+          }
         } else {
 #pragma unroll
-          for (int k = 0; k < VPT; ++k) d[k] = v8(0.f);
+          for (int k = 0; k < kParts; ++k) d[k] = v8(0.f);
         }
         {
           const uint8_t *ry = row(0);
           uint8_t *rx = block_row<XT>(p.dx, t, hidden, p.x_type);
 #pragma unroll
-          for (int k = 0; k < VPT; ++k) {
-            const int at8 = v0 + k * step;
-            if (at8 >= vecs) continue;
-            if (has_dy) d[k] = d[k] + block_load8<XT>(ry, at8, p.x_type, 0);
-            if (put_dx) block_store8<XT>(rx, at8, p.x_type, d[k]);
+          for (int k = 0; k < kParts; ++k) {
+            if (has_dy) d[k] = d[k] + block_load8<XT>(ry, at[k], p.x_type, 0);
+            if (put_dx && there[k]) block_store8<XT>(rx, at[k], p.x_type, d[k]);
           }
         }
         if (branch) {
-          V8 u[VPT];
+          V8 u[kParts];
           float2 dot = both(0.f);    // sum of w_o q u a(g), without the a(g) of a token
           const uint8_t *ro = row(at_o);
 #pragma unroll
-          for (int k = 0; k < VPT; ++k) {
-            const int at8 = v0 + k * step;
-            u[k] = v8(0.f);
-            if (at8 >= vecs) continue;
+          for (int k = 0; k < kParts; ++k) {
+            u[k] = only_if(there[k], block_load8_times<ST>(ro, at[k], p.o_type, scales, r_o));
             const V8 q = d[k] * p.scale;
-            u[k] = block_load8_times<ST>(ro, at8, p.o_type, scales, r_o);
             if (gate >= GATE_CHANNEL) {
-              V8 a = gate == GATE_FULL ? block_load8<OT>(row(at_g), at8, p.gate_type, 0) : Row8<float>::load(g_ch + at8 * 8);
+              V8 a = gate == GATE_FULL ? block_load8<OT>(row(at_g), at[k], p.gate_type, 0) : block_weight(g_ch, at[k], vecs);
               if (p.sigmoid) a = logistic(a);
-              const V8 qa = q * a, w = norm_out ? Row8<float>::load(w_out + at8 * 8) : v8(1.f);
+              const V8 qa = q * a, w = norm_out ? block_weight(w_out, at[k], vecs) : v8(1.f);
               acc_out[k] = fma(gate == GATE_CHANNEL ? q : qa, u[k], acc_out[k]);
               d[k] = w * qa;
-              if (gate == GATE_FULL && p.dg) {
+              if (gate == GATE_FULL && p.dg && there[k]) {
                 V8 dg = q * (w * u[k]);
                 if (p.sigmoid) dg = dg * (a * fma(a, -1.f, v8(1.f)));
-                block_store8<OT>(block_row<OT>(p.dg, t, hidden, p.gate_type), at8, p.gate_type, dg);
+                block_store8<OT>(block_row<OT>(p.dg, t, hidden, p.gate_type), at[k], p.gate_type, dg);
               }
             } else {
-              acc_out[k] = fma(gate == GATE_TOKEN ? q * at : q, u[k], acc_out[k]);
-              d[k] = norm_out ? Row8<float>::load(w_out + at8 * 8) * q : q;
+              acc_out[k] = fma(gate == GATE_TOKEN ? q * gate_t : q, u[k], acc_out[k]);
+              d[k] = norm_out ? block_weight(w_out, at[k], vecs) * q : q;
             }
             dot = dot2(d[k], u[k], dot);
           }
           float mean = 0.f;
           if (norm_out || gate == GATE_TOKEN) {
             const float total = g.sum(dot.x + dot.y);
-            mean = norm_out ? total * p.inv_hidden : 0.f;
-            if (gate == GATE_TOKEN && p.dg && writer) block_scalar_store(p.dg, t, p.gate_type, total * (p.sigmoid ? at * (1.f - at) : 1.f));
+            mean = -total * p.inv_hidden;
+            if (gate == GATE_TOKEN && p.dg && writer) block_scalar_store(p.dg, t, p.gate_type, total * (p.sigmoid ? gate_t * (1.f - gate_t) : 1.f));
           }
           if (put_do) {
-            const float f = r_o * at;      // (1 without a norm, 1 without a gate of one number a token)
+            const float f = r_o * gate_t;      // (1 without a norm, 1 without a gate of one number a token)
             uint8_t *rd = block_row<OT>(p.d_o, t, hidden, p.do_type);
 #pragma unroll
-            for (int k = 0; k < VPT; ++k) {
-              const int at8 = v0 + k * step;
-              if (at8 < vecs) block_store8<OT>(rd, at8, p.do_type, fma(u[k], -mean, d[k]) * f);
+            for (int k = 0; k < kParts; ++k) {
+              if (norm_out) {
+                if (ST != T_CKPT) u[k] = block_load8_times<ST>(ro, at[k], p.o_type, scales, r_o);
+                d[k] = fma(u[k], mean, d[k]);
+              }
+              const V8 out = d[k] * f;
+              if (there[k]) block_store8<OT>(rd, at[k], p.do_type, out);
             }
           }
         }
@@ -502,16 +541,17 @@ block_bwd_kernel(const __grid_constant__ BlockParams p) {
   __syncthreads();
   float *sum = reinterpret_cast<float *>(block_stage(c, p, 0));      // [groups][2][hidden]
   if (computes) {
+    auto put = [&](float *dst, const V8 &x) {
+      reinterpret_cast<float4 *>(dst)[0] = make_float4(x[0], x[1], x[2], x[3]);
+      reinterpret_cast<float4 *>(dst)[1] = make_float4(x[4], x[5], x[6], x[7]);
+    };
+    float *mine = sum + (long long)group * 2 * hidden;
 #pragma unroll
-    for (int k = 0; k < VPT; ++k) {
-      const int v = v0 + k * step;
-      if (v >= s.vecs) continue;
-      float4 *q = reinterpret_cast<float4 *>(sum + (long long)group * 2 * s.hidden + v * 8);
-      q[0] = make_float4(acc_in[k][0], acc_in[k][1], acc_in[k][2], acc_in[k][3]);
-      q[1] = make_float4(acc_in[k][4], acc_in[k][5], acc_in[k][6], acc_in[k][7]);
-      q = reinterpret_cast<float4 *>(sum + (long long)group * 2 * s.hidden + s.hidden + v * 8);
-      q[0] = make_float4(acc_out[k][0], acc_out[k][1], acc_out[k][2], acc_out[k][3]);
-      q[1] = make_float4(acc_out[k][4], acc_out[k][5], acc_out[k][6], acc_out[k][7]);
+    for (int k = 0; k < kParts; ++k) {
+      const int at8 = v0 + k * step;
+      if (at8 >= vecs) continue;
+      put(mine + at8 * 8, acc_in[k]);
+      put(mine + hidden + at8 * 8, acc_out[k]);
     }
   }
   __syncthreads();

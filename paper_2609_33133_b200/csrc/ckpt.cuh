@@ -112,13 +112,14 @@ __device__ __forceinline__ float max_magnitude(float a, float b, float c) {
   asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(fabsf(b)), "f"(fabsf(c)));
   return d;
 }
-// The exponent byte of a group whose largest magnitude has the bits m (magnitudes order like their bits, infinity and NaN on top), and 2^-e.
-__device__ __forceinline__ float ckpt_exponent(uint32_t m, uint32_t &byte) {
-  const bool finite = m < 0x7f800000u;
+// The exponent byte of a group whose largest magnitude is `top` (magnitudes order like their bits, infinity and NaN on top).  It grows with
+// `top`, so the byte of a group is also the largest of its parts' bytes.
+__device__ __forceinline__ uint32_t ckpt_byte(float top) {
+  const uint32_t m = __float_as_uint(top);
   // m = f 2^k, 1 <= f < 2: e = k - 6, one more from f = 127.5 / 64 on, where the added bits carry into the exponent
-  byte = finite ? (uint32_t)max((int)((m + 0x10000u) >> 23) - 6, 1) : 255u;
-  return finite ? __uint_as_float((254u - byte) << 23) : 0.f;
+  return m < 0x7f800000u ? (uint32_t)max((int)((m + 0x10000u) >> 23) - 6, 1) : 255u;
 }
+__device__ __forceinline__ float ckpt_per(uint32_t byte) { return byte == 255u ? 0.f : __uint_as_float((254u - byte) << 23); }   // 2^-e
 __device__ __forceinline__ uint2 ckpt_integers(const V8 &x, float per) {
   const V8 b = fma(x, per, v8(12582912.f));    // + 1.5 2^23: the integer in the low bits
   uint32_t q[2];
@@ -130,28 +131,20 @@ __device__ __forceinline__ uint2 ckpt_integers(const V8 &x, float per) {
   }
   return make_uint2(q[0], q[1]);
 }
-// 8 columns of a thread; the four threads of a lane quad hold a group of 32.  Every lane of the warp takes part; columns behind the
-// row's end are zero.
-__device__ __forceinline__ void ckpt_encode(const V8 &x, uint2 &q, uint32_t &byte) {
-  float top = 0.f;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) top = max_magnitude(top, x.p[i].x, x.p[i].y);
-  uint32_t m = __float_as_uint(top);
-  m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
-  m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
-  q = ckpt_integers(x, ckpt_exponent(m, byte));
-}
 __device__ __forceinline__ float ckpt_unit(uint32_t byte) {   // 2^e
   return __uint_as_float(byte == 255u ? 0x7fffffffu : byte << 23);
 }
-// 16 columns of a thread; a lane pair holds a group.
-__device__ __forceinline__ void ckpt_encode(const V8 &lo, const V8 &hi, uint4 &q, uint32_t &byte) {
+__device__ __forceinline__ float max_magnitude(const V8 &x) {
   float top = 0.f;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) top = max_magnitude(max_magnitude(top, lo.p[i].x, lo.p[i].y), hi.p[i].x, hi.p[i].y);
-  uint32_t m = __float_as_uint(top);
-  m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
-  const float per = ckpt_exponent(m, byte);
+  for (int i = 0; i < 4; ++i) top = max_magnitude(top, x.p[i].x, x.p[i].y);
+  return top;
+}
+// 16 columns of a thread; a lane pair holds a group.  Every lane of the warp takes part; columns behind the row's end are zero.
+__device__ __forceinline__ void ckpt_encode(const V8 &lo, const V8 &hi, uint4 &q, uint32_t &byte) {
+  byte = ckpt_byte(max_magnitude(max_magnitude(lo), max_magnitude(hi), 0.f));
+  byte = max(byte, __shfl_xor_sync(0xffffffffu, byte, 1));
+  const float per = ckpt_per(byte);
   const uint2 a = ckpt_integers(lo, per), b = ckpt_integers(hi, per);
   q = make_uint4(a.x, a.y, b.x, b.y);
 }
