@@ -405,7 +405,7 @@ int augtree_block_bwd(const augtree_block_t *b, const void *dy, int x_dtype, con
   const bool second = dw_out || (channel && d_gate);
   if (r || (!dw_in && !second)) return r;
   const BlockSums q = {p.part, grid, b->hidden, w_out, channel ? gate : nullptr, w_dtype, gate_dtype, b->sigmoid, accumulate, dw_in, dw_out, channel ? d_gate : nullptr};
-  return launch(block_sums_kernel, dim3((b->hidden + 31) / 32, second ? 2 : 1), 256, 0, st, q);
+  return launch(block_sums_kernel, dim3((b->hidden + 31) / 32, second ? 2 : 1), 1024, 0, st, q);
 }
 
 int augtree_ckpt_pack(const augtree_block_t *b, const void *x, int dtype, int64_t ld, int64_t n_tokens, int64_t cols, void *ckpt, void *stream) {

@@ -195,7 +195,7 @@ __device__ __forceinline__ V8 block_weight(const float *w, int vec, int vecs) {
 }
 __device__ __forceinline__ void block_weights(const BlockCta &c, const BlockParams &p, int slot, const void *w, int type) {
   float *dst = c.weights + slot * p.s.hidden;
-  for (int i = threadIdx.x; i < p.s.vecs; i += blockDim.x) {
+  for (int i = threadIdx.x; i < p.s.vecs; i += blockDim.x - 32) {      // (all warps but the loading one)
     V8 x;
     if (type == T_BF16) x = Row8<__nv_bfloat16>::load(static_cast<const __nv_bfloat16 *>(w) + i * 8);
     else if (type == T_F32) x = Row8<float>::load(static_cast<const float *>(w) + i * 8);
@@ -230,6 +230,8 @@ __device__ __forceinline__ void block_produce(const BlockCta &c, const BlockPara
     if (++st == s.stages) { st = 0; phase ^= 1; }
   }
 }
+// A barrier of the warps that compute (the groups' own have the numbers from 1 on, ten at most).
+__device__ __forceinline__ void block_sync_compute() { asm volatile("bar.sync 15, %0;" ::"r"(blockDim.x - 32) : "memory"); }
 __device__ __forceinline__ void block_leave(const BlockCta &c) {
   __syncwarp();
   if (*c.abort_flag) {
@@ -292,15 +294,15 @@ block_fwd_kernel(const __grid_constant__ BlockParams p) {
   const int hidden = s.hidden;
   // per-channel vectors: w_in, w_out, gate of a channel
   const float *w_in = c.weights, *w_out = w_in + (norm_in ? hidden : 0), *g_ch = w_out + (norm_out ? hidden : 0);
-  if (norm_in) block_weights(c, p, 0, p.w_in, p.w_type);
-  if (norm_out) block_weights(c, p, (int)(w_out - w_in) / hidden, p.w_out, p.w_type);
-  if (gate == GATE_CHANNEL) block_weights(c, p, (int)(g_ch - w_in) / hidden, p.gate_ptr, p.gate_type);
-  __syncthreads();
   const AbortCtx ab{c.abort_flag, p.status, p.wait_budget};
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (warp == s.groups * s.warps_row) {
     if (lane == 0) block_produce(c, p, ab);
   } else {
+    if (norm_in) block_weights(c, p, 0, p.w_in, p.w_type);
+    if (norm_out) block_weights(c, p, (int)(w_out - w_in) / hidden, p.w_out, p.w_type);
+    if (gate == GATE_CHANNEL) block_weights(c, p, (int)(g_ch - w_in) / hidden, p.gate_ptr, p.gate_type);
+    block_sync_compute();
     const int group = warp / s.warps_row;
     BlockGroup g{c.sums + group * 64, s.warps_row, warp - group * s.warps_row, group + 1, 0};
     const int v0 = g.warp * 32 + lane, step = s.warps_row * 32, vecs = s.vecs;     // pieces of 8 columns: v0, v0 + step, ..
@@ -406,10 +408,6 @@ block_bwd_kernel(const __grid_constant__ BlockParams p) {
   wait_previous();
   const int hidden = s.hidden;
   const float *w_in = c.weights, *w_out = w_in + (p.w_in ? hidden : 0), *g_ch = w_out + (norm_out ? hidden : 0);
-  if (p.w_in) block_weights(c, p, 0, p.w_in, p.w_type);
-  if (norm_out) block_weights(c, p, (int)(w_out - w_in) / hidden, p.w_out, p.w_type);
-  if (gate == GATE_CHANNEL) block_weights(c, p, (int)(g_ch - w_in) / hidden, p.gate_ptr, p.gate_type);
-  __syncthreads();
   const AbortCtx ab{c.abort_flag, p.status, p.wait_budget};
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   V8 acc_in[kParts], acc_out[kParts];
@@ -427,6 +425,10 @@ block_bwd_kernel(const __grid_constant__ BlockParams p) {
     if (lane == 0) block_produce(c, p, ab);
     __syncwarp();
   } else {
+    if (p.w_in) block_weights(c, p, 0, p.w_in, p.w_type);
+    if (norm_out) block_weights(c, p, (int)(w_out - w_in) / hidden, p.w_out, p.w_type);
+    if (gate == GATE_CHANNEL) block_weights(c, p, (int)(g_ch - w_in) / hidden, p.gate_ptr, p.gate_type);
+    block_sync_compute();
     int st = 0;
     uint32_t phase = 0;
     // inputs in the order that the host lists them: dy, dh, y, o, gate, each only where there is one
@@ -564,8 +566,9 @@ block_bwd_kernel(const __grid_constant__ BlockParams p) {
   }
 }
 
-// The CTAs' sums over tokens into dw_in, dw_out and the gradient of a gate of one number a channel: 32 columns a block, eight
-// runs of CTAs side by side.  With such a gate the second sum is S = sum s d u, and dw_out = a(g) S, dg = a'(g) w_out S.
+// The CTAs' sums over tokens into dw_in, dw_out and the gradient of a gate of one number a channel: 32 columns a block, 32 runs of CTAs
+// side by side, a run's loads all at once (with 8 runs this kernel waited for memory five times, 2 us more).
+// With such a gate the second sum is S = sum s d u, and dw_out = a(g) S, dg = a'(g) w_out S.
 struct BlockSums {
   const float *part;
   int parts, hidden;
@@ -573,22 +576,23 @@ struct BlockSums {
   int w_type, gate_type, sigmoid, accumulate;
   void *dw_in, *dw_out, *dg;       // null: not wanted
 };
-__global__ void __launch_bounds__(256) block_sums_kernel(const BlockSums p) {
+__global__ void __launch_bounds__(1024) block_sums_kernel(const BlockSums p) {
   launch_next();
   wait_previous();
-  __shared__ float run[8][33];
+  __shared__ float run[32][33];
   const int lane = threadIdx.x & 31, slice = threadIdx.x >> 5, second = blockIdx.y;
   const int c = blockIdx.x * 32 + lane;
   float v = 0.f;
   if (c < p.hidden) {
     const float *q = p.part + (long long)second * p.hidden + c;
-#pragma unroll 4
-    for (int i = slice; i < p.parts; i += 8) v += q[(long long)i * 2 * p.hidden];
+#pragma unroll 5
+    for (int i = slice; i < p.parts; i += 32) v += q[(long long)i * 2 * p.hidden];
   }
   run[slice][lane] = v;
   __syncthreads();
   if (slice || c >= p.hidden) return;
-  for (int i = 1; i < 8; ++i) v += run[i][lane];
+#pragma unroll
+  for (int i = 1; i < 32; ++i) v += run[i][lane];
   auto put = [&](void *dst, int type, float x) {
     if (p.accumulate) x += static_cast<const float *>(dst)[c];    // (fp32 only)
     block_scalar_store(dst, c, type, x);
