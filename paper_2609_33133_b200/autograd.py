@@ -1,4 +1,4 @@
-"""torch.autograd wrappers around the entry points (argument marshalling only): tree attention, embedding, vocabulary loss.
+"""torch.autograd wrappers around the entry points (argument marshalling only): tree attention, embedding, vocabulary loss, block ends.
 
 `tree_attention(plan, q_p, k_p, v_p, q_r, k_r, v_r)` returns `(o_p, o_r)` for the packed prompt and
 response tokens of a plan's groups; backward fills the gradients of all six inputs.  The order inside
@@ -11,10 +11,16 @@ available as `plan.prompt_grad_fp32 = (dK_P, dV_P)` for callers that want them u
 
 `embed(lm, table, ids)` and `lm_loss(lm, hidden, weight, targets)` are the two vocabulary ends of a model around it: a
 `binding.LM` handle carries the sizes and scales.  Negative ids are padding in both.
+
+`block(blk, x, o, ..)`, `norm(blk, x, w)` and `glu(blk, g, u)` are what lies between a decoder layer's products; a `binding.Block` handle
+carries the width, the scales and the form of the gate.  With `ckpt=True` what their backward passes need is kept in 8 bits, and `linear` and
+`glu_linear` take their weight gradients from the same checkpoints, so that neither the residual stream, nor the norms' outputs, nor the MLP's
+inner activations outlive the forward pass in full.
 """
 from __future__ import annotations
 
 import torch
+import torch.nn.functional as F
 
 from . import binding as B
 
@@ -119,3 +125,125 @@ def lm_loss(lm: B.LM, hidden, weight, targets):
     are never held: hidden [tokens, hidden] and weight [vocab, hidden] bf16.  Differentiable in both; a gradient that nobody
     asks for is not computed.  The negative of it is the log-probability of the target."""
     return _LmLoss.apply(lm, hidden, weight, targets)
+
+
+class Kept:
+    """A tensor in 8 bits, as a norm's output: what `ckpt` [tokens, pitch] stands for times row[t] and col[c]."""
+
+    def __init__(self, ckpt, row, col):
+        self.ckpt, self.row, self.col = ckpt, row, col
+
+
+def _like(t, shape=None, dtype=None):
+    return None if t is None else torch.empty(t.shape if shape is None else shape, device=t.device, dtype=dtype or t.dtype)
+
+
+class _Block(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, blk, x, o, gate, w_out, w_in, h_dtype, ckpt):
+        n, dev = x.shape[0], x.device
+        f32 = lambda: torch.empty(n, device=dev, dtype=torch.float32)
+        box = lambda: torch.empty((n, B.ckpt_pitch(blk.hidden)), device=dev, dtype=torch.uint8)
+        y = None if o is None else torch.empty_like(x)
+        h = None if w_in is None else torch.empty((n, blk.hidden), device=dev, dtype=h_dtype)
+        r_out, r_in = None if w_out is None else f32(), None if w_in is None else f32()
+        kept_y, kept_o = (box() if w_in is not None else None, None if o is None else box()) if ckpt else (None, None)
+        blk.fwd(x, o, gate, w_out, w_in, y, h, r_out, r_in, kept_y, kept_o)
+        ctx.set_materialize_grads(False)
+        ctx.blk, ctx.ckpt, ctx.like = blk, ckpt, (x.dtype, None if o is None else o.dtype)
+        ctx.numbers = (r_out, r_in, kept_y, kept_o)
+        ctx.save_for_backward(gate, w_out, w_in, *((None, None) if ckpt else (x if o is None else y, o)))
+        kept = Kept(kept_y, r_in, w_in.detach()) if kept_y is not None else None
+        return y, h, kept
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy, dh, _):
+        blk, (r_out, r_in, kept_y, kept_o) = ctx.blk, ctx.numbers
+        gate, w_out, w_in, y, o = ctx.saved_tensors
+        x_dtype, o_dtype = ctx.like
+        if dy is None and dh is None:
+            return (None,) * 8
+        lead = dh if dy is None else dy
+        dy, dh = (None if t is None else t.contiguous() for t in (dy, dh))
+        y, o = (kept_y, kept_o) if ctx.ckpt else (y, o)
+        if dh is None:
+            y = r_in = w_in = None
+        need = ctx.needs_input_grad
+        dx = _like(lead, dtype=x_dtype) if need[1] else None
+        d_o = _like(lead, dtype=o_dtype) if need[2] else None
+        d_gate, dw_out, dw_in = (_like(t) if wanted else None for t, wanted in zip((gate, w_out, w_in), need[3:6]))
+        ws = torch.empty(blk.workspace_bytes(lead.shape[0]), device=lead.device, dtype=torch.uint8)
+        blk.bwd(dy, dh, y, o, gate, w_out, w_in, r_out, r_in, dx, d_o, d_gate, dw_out, dw_in, ws)
+        return None, dx, d_o, d_gate, dw_out, dw_in, None, None
+
+
+def block(blk: B.Block, x, o, gate=None, w_out=None, w_in=None, *, h_dtype=torch.bfloat16, ckpt=False):
+    """End of a block: y = x + s a(gate) norm(o, w_out) (o itself without w_out) and, with w_in, h = norm(y, w_in) in h_dtype.  Returns
+    (y, h or None, Kept or None): the last with ckpt=True, where y and o are kept in 8 bits for the backward pass.  Differentiable in all tensors."""
+    return _Block.apply(blk, x, o, gate, w_out, w_in, h_dtype, ckpt)
+
+
+def norm(blk: B.Block, x, w, *, h_dtype=torch.bfloat16, ckpt=False):
+    """h = x / rms(x) * w in h_dtype; returns (h, Kept or None)."""
+    return _Block.apply(blk, x, None, None, None, w, h_dtype, ckpt)[1:]
+
+
+class _Linear(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, blk, h, weight, kept):
+        ctx.blk, ctx.kept = blk, kept
+        ctx.save_for_backward(weight)
+        return F.linear(h, weight)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, d):
+        blk, kept, (weight,) = ctx.blk, ctx.kept, ctx.saved_tensors
+        d = d.contiguous()
+        dw = None
+        if ctx.needs_input_grad[2]:
+            dw = torch.empty_like(weight)
+            ws = torch.empty(blk.wgrad_workspace_bytes(d.shape[0], *weight.shape), device=d.device, dtype=torch.uint8)
+            blk.wgrad(d, kept.ckpt, dw, ws, kept.row, kept.col)
+        return None, d @ weight if ctx.needs_input_grad[1] else None, dw, None
+
+
+def linear(blk: B.Block, h, weight, kept=None):
+    """h @ weight.T in bf16.  With `kept` (of the same h) the weight's gradient comes from the checkpoint and h is not saved."""
+    return F.linear(h, weight) if kept is None else _Linear.apply(blk, h, weight, kept)
+
+
+class _Glu(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, blk, g, u, weight, ckpt):
+        n, cols = g.shape
+        a = torch.empty((n, cols), device=g.device, dtype=g.dtype)
+        box = lambda: torch.empty((n, B.ckpt_pitch(cols)), device=g.device, dtype=torch.uint8) if ckpt else None
+        kept = (box(), box())
+        blk.glu_fwd(g, u, a, *kept)
+        ctx.blk, ctx.kept = blk, kept if ckpt else None
+        ctx.save_for_backward(weight, *((None, None) if ckpt else (g, u)))
+        return a if weight is None else F.linear(a, weight)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, d):
+        weight, g, u = ctx.saved_tensors
+        g, u = ctx.kept or (g, u)
+        da = (d if weight is None else d @ weight).contiguous()
+        dg, du = torch.empty_like(da), torch.empty_like(da)
+        a = torch.empty_like(da) if weight is not None and ctx.needs_input_grad[3] else None
+        ctx.blk.glu_bwd(da, g, u, dg, du, a)
+        return None, dg, du, None if a is None else d.t() @ a, None
+
+
+def glu(blk: B.Block, g, u, *, ckpt=False):
+    """g / (1 + exp(-g)) u (rows contiguous, one type); with ckpt=True g and u are kept in 8 bits for the backward pass."""
+    return _Glu.apply(blk, g, u, None, ckpt)
+
+
+def glu_linear(blk: B.Block, g, u, weight, *, ckpt=False):
+    """glu(g, u) @ weight.T: the product behind a gated MLP, whose weight gradient takes the activation made again in the backward pass, so that it is
+    never saved."""
+    return _Glu.apply(blk, g, u, weight, ckpt)

@@ -124,7 +124,14 @@ _i, _l = C.c_int, C.c_int64
 lib.augtree_block_create.argtypes = [C.POINTER(BlockDescC), _i, C.POINTER(_vp)]
 lib.augtree_block_destroy.argtypes = [_vp]
 lib.augtree_block_workspace_bytes.argtypes = [_vp, _l, C.POINTER(_sz)]
+lib.augtree_block_fwd.argtypes = [_vp, _vp, _i, _vp, _i, _vp, _i, _vp, _vp, _i, _l, _vp, _vp, _i, _vp, _vp, _vp, _vp, _vp]
+lib.augtree_block_bwd.argtypes = [_vp] + [_vp, _i] * 5 + [_vp, _vp, _i, _vp, _vp, _l, _vp, _vp, _i, _vp, _vp, _vp, _i, _vp, _sz, _vp]
 lib.augtree_ckpt_pitch.argtypes = [_l, C.POINTER(_l)]
+lib.augtree_ckpt_pack.argtypes = [_vp, _vp, _i, _l, _l, _l, _vp, _vp]
+lib.augtree_ckpt_unpack.argtypes = [_vp, _vp, _l, _l, _vp, _vp, _i, _vp, _i, _l, _vp]
+lib.augtree_glu_fwd.argtypes = [_vp, _vp, _vp, _l, _i, _l, _l, _vp, _vp, _vp, _vp]
+lib.augtree_glu_bwd.argtypes = [_vp, _vp, _i, _vp, _vp, _l, _i, _l, _l, _vp, _vp, _l, _vp, _vp]
+lib.augtree_ckpt_wgrad.argtypes = [_vp, _vp, _l, _l, _vp, _l, _vp, _vp, _i, _vp, _i, _i, _vp, _sz, _vp]
 lib.augtree_ckpt_wgrad_bytes.argtypes = [_vp, _l, _l, _l, C.POINTER(_sz)]
 _marshal.init(*[C.cast(getattr(lib, "augtree_" + n), _vp).value for n in ("block_fwd", "block_bwd", "ckpt_pitch", "ckpt_pack", "ckpt_unpack", "glu_fwd",
                                                                           "glu_bwd", "ckpt_wgrad")])

@@ -311,9 +311,9 @@ int augtree_block_fwd(const augtree_block_t *b, const void *x, int x_dtype, cons
   if (r) return r;
   if (n_tokens < 0 || !dtype_ok(x_dtype) || (o && !dtype_ok(o_dtype)) || ((w_out || w_in) && !dtype_ok(w_dtype)) || (h && !dtype_ok(h_dtype)))
     return AUGTREE_ERR_INVALID_ARG;
-  if (!h != !w_in || (!o && (y || w_out || ckpt_o)) || (o && !y)) return AUGTREE_ERR_INVALID_ARG;
   if (n_tokens > kMaxTokens) return AUGTREE_ERR_UNSUPPORTED;
-  if (n_tokens == 0) return AUGTREE_OK;
+  if (n_tokens == 0) return AUGTREE_OK;     // (tensors of no tokens have no address)
+  if (!h != !w_in || (!o && (y || w_out || ckpt_o)) || (o && !y)) return AUGTREE_ERR_INVALID_ARG;
   if (!x || (!o && !h && !ckpt_y)) return AUGTREE_ERR_INVALID_ARG;
   if ((r = check_gate(b, o, gate, gate_dtype))) return r;
   for (const void *q : {x, o, w_out, w_in, (const void *)y, (const void *)h, (const void *)ckpt_y, (const void *)ckpt_o})

@@ -35,10 +35,10 @@ int code_of(at::ScalarType t) {
   }
 }
 std::string names(unsigned types) {
-  std::string s;
+  std::string s;   // "[..]"
   for (auto [bit, name] : {std::pair{BF16, "torch.bfloat16"}, {F16, "torch.float16"}, {F32, "torch.float32"}, {U8, "torch.uint8"}})
     if (types & bit) s += (s.empty() ? "[" : ", ") + std::string(name);
-  return s + "]";
+  return (s.empty() ? "[" : s) + "]";
 }
 std::string got(PyObject *o) {
   if (!THPVariable_Check(o)) return Py_TYPE(o)->tp_name;
@@ -55,6 +55,7 @@ struct Arg {
   void *p = nullptr;
   int code = 0;
   int64_t ld = 0;
+  bool given = false;   // (a tensor of no elements has no address)
 };
 
 // The handle of a call: (address, device, hidden, bytes of a checkpoint row of `hidden`, gate)
@@ -100,6 +101,7 @@ struct Call {
       if (a.code >= 0 && (types >> a.code & 1) && (int64_t)s.size() == (s1 < 0 ? 1 : 2) && s[0] == s0 && (s1 < 0 || s[1] == s1) && t.is_cuda() &&
           t.get_device() == device && t.is_contiguous()) {
         a.p = t.data_ptr();
+        a.given = true;
         return a;
       }
     }
@@ -120,6 +122,7 @@ struct Call {
         a.ld = n > 1 ? t.stride(0) : c;
         if (a.ld < c) fail(std::string(name) + ": rows overlap (" + got(o) + ")");
         a.p = t.data_ptr();
+        a.given = true;
         return a;
       }
     }
@@ -127,9 +130,16 @@ struct Call {
          " with contiguous rows, got " + got(o));
     return a;
   }
+  // (nothing is asked of the interpreter once an exception is set)
+  bool is_u8(PyObject *o) const { return ok && o != Py_None && THPVariable_Check(o) && THPVariable_Unpack(o).scalar_type() == at::kByte; }
+  bool truth(PyObject *o) {
+    const int r = ok ? PyObject_IsTrue(o) : 0;
+    ok = ok && r >= 0;
+    return r > 0;
+  }
   // a saved tensor: in full, or a checkpoint
   Arg saved(PyObject *o, const char *name, int64_t n, int64_t c, int64_t row) {
-    const bool u8 = o != Py_None && THPVariable_Check(o) && THPVariable_Unpack(o).scalar_type() == at::kByte;
+    const bool u8 = is_u8(o);
     return u8 ? whole(o, name, U8, n, row) : whole(o, name, FLOATS, n, c);
   }
   Arg gate_like(PyObject *o, const char *name, unsigned types, int64_t n) {
@@ -143,8 +153,8 @@ struct Call {
   int weights(PyObject *w_out, PyObject *w_in, Arg &o, Arg &i) {
     o = whole(w_out, "w_out", FLOATS, hidden);
     i = whole(w_in, "w_in", FLOATS, hidden);
-    if (o.p && i.p && o.code != i.code) fail("w_out, w_in: expected one type, got " + names(1u << o.code) + " and " + names(1u << i.code));
-    return o.p ? o.code : i.code;
+    if (o.given && i.given && o.code != i.code) fail("w_out, w_in: expected one type, got " + names(1u << o.code) + " and " + names(1u << i.code));
+    return o.given ? o.code : i.code;
   }
   Arg scratch(PyObject *o) {
     Arg a;
@@ -153,6 +163,7 @@ struct Call {
       const at::Tensor &t = THPVariable_Unpack(o);
       if (t.is_cuda() && t.get_device() == device && t.is_contiguous()) {
         a.p = t.data_ptr();
+        a.given = true;
         a.ld = (int64_t)t.nbytes();
         return a;
       }
@@ -165,7 +176,7 @@ struct Call {
     if (ok && f_ckpt_pitch(cols, &p)) fail("columns: expected a multiple of 8, at most 2^20, got " + std::to_string(cols));
     return p;
   }
-  static unsigned like(const Arg &a) { return a.p ? 1u << a.code : 0u; }
+  static unsigned like(const Arg &a) { return a.given ? 1u << a.code : 0u; }
   // the call itself, without the interpreter's lock: its return code, or null with an exception set
   template <class F>
   PyObject *run(F f) {
@@ -219,13 +230,13 @@ MARSHAL(block_bwd, 17) {
   Arg wo, wi;
   const int wt = c.weights(a[6], a[7], wo, wi);
   const Arg ro = c.whole(a[8], "r_out", F32, n), ri = c.whole(a[9], "r_in", F32, n);
-  const Arg dx = c.whole(a[10], "dx", dy.p ? Call::like(dy) : FLOATS, n, c.hidden), d_o = c.whole(a[11], "d_o", FLOATS, n, c.hidden);
+  const Arg dx = c.whole(a[10], "dx", dy.given ? Call::like(dy) : FLOATS, n, c.hidden), d_o = c.whole(a[11], "d_o", FLOATS, n, c.hidden);
   const Arg dg = c.gate_like(a[12], "d_gate", Call::like(g), n);
   const Arg dwo = c.whole(a[13], "dw_out", Call::like(wo), c.hidden), dwi = c.whole(a[14], "dw_in", Call::like(wi), c.hidden);
   const Arg ws = c.scratch(a[15]);
-  const int add = PyObject_IsTrue(a[16]);
+  const int add = c.truth(a[16]);
   return c.run([&](void *st) {
-    return f_block_bwd(static_cast<augtree_block_t *>(c.handle), dy.p, dy.p ? dy.code : dx.code, dh.p, dh.code, y.p, y.code, o.p, o.code, g.p, g.code,
+    return f_block_bwd(static_cast<augtree_block_t *>(c.handle), dy.p, dy.given ? dy.code : dx.code, dh.p, dh.code, y.p, y.code, o.p, o.code, g.p, g.code,
                        wo.p, wi.p, wt, static_cast<const float *>(ro.p), static_cast<const float *>(ri.p), n, dx.p, d_o.p, d_o.code, dg.p, dwo.p, dwi.p,
                        add, ws.p, (size_t)ws.ld, st);
   });
@@ -272,7 +283,7 @@ MARSHAL(glu_bwd, 7) {
   int64_t n, cols;
   c.rows(a[1], "da", n, cols);
   const Arg da = c.whole(a[1], "da", FLOATS, n, cols);
-  const bool kept = THPVariable_Check(a[2]) && THPVariable_Unpack(a[2]).scalar_type() == at::kByte;
+  const bool kept = c.is_u8(a[2]);
   Arg g, u;
   if (kept) {
     const int64_t row = c.pitch_of(cols);
@@ -299,7 +310,7 @@ MARSHAL(ckpt_wgrad, 8) {
   c.rows(a[3], "d_weight", out, cols);
   const Arg dy = c.whole(a[1], "dy", BF16, n, m), k = c.whole(a[2], "ckpt", U8, n, c.pitch_of(cols)), dw = c.whole(a[3], "d_weight", BF16 | F32, m, cols);
   const Arg row = c.whole(a[5], "row", F32, n), col = c.whole(a[6], "col", FLOATS, cols), ws = c.scratch(a[4]);
-  const int add = PyObject_IsTrue(a[7]);
+  const int add = c.truth(a[7]);
   return c.run([&](void *st) {
     return f_ckpt_wgrad(static_cast<augtree_block_t *>(c.handle), dy.p, n, m, k.p, cols, static_cast<const float *>(row.p), col.p, col.code, dw.p, dw.code, add,
                         ws.p, (size_t)ws.ld, st);

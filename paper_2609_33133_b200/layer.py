@@ -13,6 +13,8 @@ standard pre-norm decoder layer:
 * loss: token-level cross-entropy on the response tokens.  The first token of every response is scored from the
   LAST PROMPT hidden state of its group, and that loss flows back through the prompt's own graph (Sec. 3.2, response
   replay): that state therefore carries one target per branch;
+* what lies between the products: `tree_stack` runs a stack of layers with the fused block ends and gated MLP of a `binding.Block` handle, the
+  end of one block and the norm before the next in one kernel, and with `ckpt=True` with 8-bit activation checkpoints;
 * the vocabulary ends: given a `binding.LM` handle, `tree_embed` looks up prompts and responses in one call and
   `tree_lm_loss` never holds the logits (16384 response tokens over 152064 words would be 15 GB of them in bf16 and fp32).
 
@@ -24,7 +26,7 @@ import torch
 import torch.nn.functional as F
 
 from . import binding as B
-from .autograd import embed, lm_loss, tree_attention
+from .autograd import block, embed, glu_linear, linear, lm_loss, norm, tree_attention
 
 BF16 = torch.bfloat16
 
@@ -69,9 +71,10 @@ def rms_norm(x, weight, eps=1e-6):
 
 class TreeDecoderLayer(torch.nn.Module):
     """Pre-norm decoder layer: RMSNorm, GQA self-attention with RoPE, SwiGLU MLP.  fp32 parameters and residual
-    stream, bf16 GEMMs and attention."""
+    stream, bf16 GEMMs and attention.  post_norm: a norm behind each of its two blocks as well, before the residual sum; layer_scale (a start
+    value): a learned factor for each channel of what each block adds."""
 
-    def __init__(self, hidden, h_q, h_kv, head_dim, mlp_hidden, rope_theta=10000.0):
+    def __init__(self, hidden, h_q, h_kv, head_dim, mlp_hidden, rope_theta=10000.0, post_norm=False, layer_scale=None):
         super().__init__()
         self.h_q, self.h_kv, self.head_dim, self.rope_theta = h_q, h_kv, head_dim, rope_theta
         mk = lambda o, i: torch.nn.Parameter(torch.randn(o, i) * i ** -0.5)
@@ -79,6 +82,9 @@ class TreeDecoderLayer(torch.nn.Module):
         self.wo = mk(hidden, h_q * head_dim)
         self.w_gate, self.w_up, self.w_down = mk(mlp_hidden, hidden), mk(mlp_hidden, hidden), mk(hidden, mlp_hidden)
         self.norm1, self.norm2 = torch.nn.Parameter(torch.ones(hidden)), torch.nn.Parameter(torch.ones(hidden))
+        per = lambda start: torch.nn.Parameter(torch.full((hidden,), float(start)))
+        self.post1, self.post2 = (per(1.0), per(1.0)) if post_norm else (None, None)
+        self.scale1, self.scale2 = (per(layer_scale), per(layer_scale)) if layer_scale is not None else (None, None)
 
     @staticmethod
     def _lin(x, w):
@@ -93,11 +99,16 @@ class TreeDecoderLayer(torch.nn.Module):
         v = self._lin(h, self.wv).view(t, self.h_kv, self.head_dim)
         return q.contiguous(), k.contiguous(), v.contiguous()
 
+    @staticmethod
+    def _end(x, o, post, scale):
+        o = o.float() if post is None else rms_norm(o, post)
+        return x + (o if scale is None else o * scale)
+
     def after_attention(self, x, o):
         """Output projection, residual, MLP, residual."""
-        x = x + self._lin(o.reshape(o.shape[0], -1), self.wo).float()
+        x = self._end(x, self._lin(o.reshape(o.shape[0], -1), self.wo), self.post1, self.scale1)
         h = rms_norm(x, self.norm2)
-        return x + self._lin(F.silu(self._lin(h, self.w_gate).float()) * self._lin(h, self.w_up).float(), self.w_down).float()
+        return self._end(x, self._lin(F.silu(self._lin(h, self.w_gate).float()) * self._lin(h, self.w_up).float(), self.w_down), self.post2, self.scale2)
 
     def forward(self, plan: B.Plan, x_p, x_r, pos_p, pos_r):
         """x_p [sumP, hidden], x_r [sumR, hidden] fp32 -> the same shapes; the prompt is computed once per group."""
@@ -105,6 +116,33 @@ class TreeDecoderLayer(torch.nn.Module):
         q_r, k_r, v_r = self.qkv(x_r, pos_r)
         o_p, o_r = tree_attention(plan, q_p, k_p, v_p, q_r, k_r, v_r)
         return self.after_attention(x_p, o_p), self.after_attention(x_r, o_r)
+
+
+def tree_stack(blk: B.Block, layers, plan: B.Plan, x_p, x_r, pos_p, pos_r, final_norm, ckpt=False):
+    """The layers one after the other with the block ends of `blk` (gate "channel" for layers with a layer_scale, "none" for others): x_p, x_r
+    fp32 -> the final norm's outputs of prompt and response tokens, bf16.  Every sum into the residual stream is one kernel with the norm before the next
+    block, and the gated MLP's activation is one kernel.  With ckpt=True the backward pass works from 8-bit checkpoints of the residual stream at
+    every norm, of what the blocks add and of the MLP's two inner activations; attention keeps its own tensors as they are, since its
+    probabilities have to fit the saved log-sum-exp."""
+    xs, poss, hs, kept = [x_p, x_r], (pos_p, pos_r), [None, None], [None, None]
+    for j in range(2):
+        hs[j], kept[j] = norm(blk, xs[j], layers[0].norm1 if len(layers) else final_norm, ckpt=ckpt)
+    for i, layer in enumerate(layers):
+        w = lambda p: p.to(BF16)
+        qkv = []
+        for h, k, pos in zip(hs, kept, poss):
+            t = h.shape[0]
+            head = lambda weight, n: linear(blk, h, w(weight), k).view(t, n, layer.head_dim)
+            qkv += [rope(head(layer.wq, layer.h_q), pos, layer.rope_theta).contiguous(), rope(head(layer.wk, layer.h_kv), pos, layer.rope_theta).contiguous(),
+                    head(layer.wv, layer.h_kv).contiguous()]
+        os = tree_attention(plan, *qkv)
+        following = layers[i + 1].norm1 if i + 1 < len(layers) else final_norm
+        for j in range(2):
+            o = F.linear(os[j].flatten(1), w(layer.wo))
+            x, h, k = block(blk, xs[j], o, layer.scale1, layer.post1, layer.norm2, ckpt=ckpt)
+            m = glu_linear(blk, linear(blk, h, w(layer.w_gate), k), linear(blk, h, w(layer.w_up), k), w(layer.w_down), ckpt=ckpt)
+            xs[j], hs[j], kept[j] = block(blk, x, m, layer.scale2, layer.post2, following, ckpt=ckpt)
+    return hs[0], hs[1]
 
 
 def tree_embed(lm: B.LM, table, prompt_tokens, resp_tokens):

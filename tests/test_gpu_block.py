@@ -127,12 +127,9 @@ def test_sizes(B, n, c, ckpt):
     Case(B, n, c, kind="token", sigmoid=True, seed=n + c).check_all(ckpt)
 
 
-@pytest.mark.parametrize("kind", ["none", "token", "channel", "full"])
-@pytest.mark.parametrize("sigmoid", [False, True])
+@pytest.mark.parametrize("kind,sigmoid", [("none", False)] + [(k, s) for k in ("token", "channel", "full") for s in (False, True)])
 @pytest.mark.parametrize("post", [False, True])
 def test_gates(B, kind, sigmoid, post):
-    if kind == "none" and sigmoid:
-        pytest.skip("no gate to take a function of")
     for ckpt in (False, True):
         Case(B, 77, 1032, kind=kind, sigmoid=sigmoid, post=post, seed=7).check_all(ckpt)
 
