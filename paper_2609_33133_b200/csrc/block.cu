@@ -200,28 +200,31 @@ int check_gate(const augtree_block *b, const void *o, const void *gate, int gate
 size_t bwd_bytes(const augtree_block *b) { return (size_t)b->n_lanes * 2 * b->hidden * 4; }
 
 // ---------------------------------------------------------------- weight gradient
-// Shares of the contraction: the time of the longest CTA pair (a stage of 64 tokens 0.28 us, a tile's start and end 2 us) plus that of
-// the partial sums' way through memory (4 us and their bytes, written and read, at 6 TB/s).
-int wgrad_splits(int lanes, int64_t n, int64_t out, int64_t cols) {
+// How a call is done: shares of the contraction, and whether X is turned into bf16 in the kernel (kBits, wgrad_kernel.cuh).  By the time of the longest
+// CTA pair (a stage of 64 tokens 0.28 us from bf16 and 0.4 from bits, a tile's start and end 2 us), of the partial sums' way through memory (4 us and
+// their bytes, written and read, at 6 TB/s) and of a bf16 X's (2 us and its 3 bytes a value).
+struct WgradWay { int splits; bool bits; };
+WgradWay wgrad_way(int lanes, int64_t n, int64_t out, int64_t cols) {
   const int64_t pairs = std::max(lanes / 2, 1), tiles = ((out + kLmTile - 1) / kLmTile) * ((cols + kLmTile - 1) / kLmTile);
   const int64_t steps = std::max<int64_t>((n + 63) / 64, 1);
-  auto cost = [&](int64_t s) {
-    const double longest = (double)((tiles * s + pairs - 1) / pairs) * (0.28 * (double)((steps + s - 1) / s) + 2.0);
-    return longest + (s > 1 ? 4.0 + (double)(s * out * cols) * 8e-6 / 6.0 : 0.0);
+  auto cost = [&](int64_t s, bool bits) {
+    const double longest = (double)((tiles * s + pairs - 1) / pairs) * ((bits ? 0.4 : 0.28) * (double)((steps + s - 1) / s) + 2.0);
+    return longest + (s > 1 ? 4.0 + (double)(s * out * cols) * 8e-6 / 6.0 : 0.0) + (bits ? 0.0 : 2.0 + (double)(n * cols) * 3e-6 / 6.0);
   };
-  int64_t pick = 1;
-  for (int64_t s = 2; s <= std::min<int64_t>(steps, 32); ++s)
-    if (cost(s) < cost(pick)) pick = s;
-  const int64_t share = (steps + pick - 1) / pick;
-  return (int)((steps + share - 1) / share);   // (no empty share)
+  WgradWay pick = {1, true};
+  for (bool bits : {true, false})
+    for (int64_t s = 1; s <= std::min<int64_t>(steps, 32); ++s)
+      if (cost(s, bits) < cost(pick.splits, pick.bits)) pick = {(int)s, bits};
+  const int64_t share = (steps + pick.splits - 1) / pick.splits;
+  pick.splits = (int)((steps + share - 1) / share);   // (no empty share)
+  return pick;
 }
 
 struct WgradWs { __nv_bfloat16 *x; float *part; };
-size_t wgrad_layout(const augtree_block *b, int64_t n, int64_t out, int64_t cols, uint8_t *base, WgradWs *w) {
-  const int splits = wgrad_splits(b->n_lanes, n, out, cols);
+size_t wgrad_layout(const WgradWay &way, int64_t n, int64_t out, int64_t cols, uint8_t *base, WgradWs *w) {
   Cursor c{base};
-  w->x = c.take<__nv_bfloat16>(n * up(cols, 64));
-  w->part = c.take<float>(splits > 1 ? splits * up(out, kLmTile) * cols : 0);
+  w->x = c.take<__nv_bfloat16>(way.bits ? 0 : n * up(cols, 64));
+  w->part = c.take<float>(way.splits > 1 ? way.splits * up(out, kLmTile) * cols : 0);
   return c.off;
 }
 
@@ -263,7 +266,7 @@ int augtree_block_create(const augtree_block_desc_t *desc, int device, augtree_b
         with_fwd(b->hidden, x, form, b->gate, kernel_room);
         for (bool kept : {false, true}) with_bwd(b->hidden, x, form, b->gate, kept, kernel_room);
       }
-    room(wgrad_kernel, LmSmem::kBytes);
+    room(wgrad_kernel<true>, WgSmem<true>::kBytes); room(wgrad_kernel<false>, WgSmem<false>::kBytes);
     if (!r && (cudaMalloc(&b->d_status, 2 * sizeof(int)) != cudaSuccess || cudaMemset(b->d_status, 0, 2 * sizeof(int)) != cudaSuccess)) r = AUGTREE_ERR_CUDA;
     cudaSetDevice(prev);
   }
@@ -489,7 +492,7 @@ int augtree_ckpt_wgrad_bytes(const augtree_block_t *b, int64_t n_tokens, int64_t
   int r = check_size(n_tokens, cols);
   if (r || (r = check_size(n_tokens, out_features))) return r;
   WgradWs w;
-  *bytes = wgrad_layout(b, n_tokens, out_features, cols, nullptr, &w);
+  *bytes = wgrad_layout(wgrad_way(b->n_lanes, n_tokens, out_features, cols), n_tokens, out_features, cols, nullptr, &w);
   return AUGTREE_OK;
 }
 
@@ -508,31 +511,43 @@ int augtree_ckpt_wgrad(const augtree_block_t *b, const void *dy, int64_t n_token
     return AUGTREE_OK;
   }
   if (!dy || !ckpt || !aligned16(dy) || !aligned16(ckpt)) return AUGTREE_ERR_INVALID_ARG;
+  const WgradWay way = wgrad_way(b->n_lanes, n_tokens, out_features, cols);
   WgradWs w;
-  if (!ws || !aligned16(ws) || ws_bytes < wgrad_layout(b, n_tokens, out_features, cols, static_cast<uint8_t *>(ws), &w)) return AUGTREE_ERR_WORKSPACE;
+  if (!ws || !aligned16(ws) || ws_bytes < wgrad_layout(way, n_tokens, out_features, cols, static_cast<uint8_t *>(ws), &w)) return AUGTREE_ERR_WORKSPACE;
   const int64_t padded = up(cols, 64);
-  unsigned blocks;
-  const Pieces pc = pieces(b, n_tokens, padded, kUnpackBlocks, {{w.x, padded, 2}}, &blocks);
-  if ((r = launch(ckpt_unpack_kernel<__nv_bfloat16>, blocks, kActThreads, 0, st, ckpt_rows(ckpt, cols), pc, (int)(cols / 8), row, nullptr, 0, w.x, padded)))
-    return r;
+  if (!way.bits) {
+    unsigned blocks;
+    const Pieces pc = pieces(b, n_tokens, padded, kUnpackBlocks, {{w.x, padded, 2}}, &blocks);
+    if ((r = launch(ckpt_unpack_kernel<__nv_bfloat16>, blocks, kActThreads, 0, st, ckpt_rows(ckpt, cols), pc, (int)(cols / 8), row, nullptr, 0, w.x, padded)))
+      return r;
+  }
   WgradParams p = {};
   p.out = (int)out_features; p.cols = (int)cols; p.steps = (int)((n_tokens + 63) / 64);
   p.mt = (int)((out_features + kLmTile - 1) / kLmTile); p.nt = (int)((cols + kLmTile - 1) / kLmTile);
-  p.splits = wgrad_splits(b->n_lanes, n_tokens, out_features, cols);
+  p.splits = way.splits;
   p.share = (p.steps + p.splits - 1) / p.splits;
   p.a_chunks = out_features % 64 == 0 ? 2 : 1;
   p.part_rows = (int64_t)p.mt * kLmTile;
+  p.scales = (int)ckpt_scale_offset(cols); p.rows = (int)n_tokens; p.row = row;
   const bool joined = p.splits > 1;
   p.f32 = joined || f32; p.add = !joined && accumulate;
   p.col = joined ? nullptr : col; p.col_type = col_dtype;
   p.status = b->d_status;
   p.wait_budget = (b->flags & AUGTREE_FLAG_TEST_SHORT_WAIT) ? kWaitBudgetClocksTest : kWaitBudgetClocks;
   p.test_flags = (b->flags & AUGTREE_FLAG_TEST_SKIP_FWD_LOAD) ? TEST_SKIP_FWD_LOAD : 0;
-  CUtensorMap m_dy, m_x, m_out;
-  if ((r = map_mn(&m_dy, dy, n_tokens, out_features, p.a_chunks)) || (r = map_mn(&m_x, w.x, n_tokens, padded, 2)) ||
+  CUtensorMap m_dy, m_x = {}, m_raw = {}, m_scale = {}, m_out;
+  if ((r = map_mn(&m_dy, dy, n_tokens, out_features, p.a_chunks)) ||
       (r = joined ? map_out(&m_out, w.part, p.splits * p.part_rows, cols, true) : map_out(&m_out, d_weight, out_features, cols, f32)))
     return r;
-  if ((r = launch(wgrad_kernel, std::max(b->n_lanes / 2, 1) * 2, kLmThreads, LmSmem::kBytes, st, m_dy, m_x, m_out, p)) || !joined) return r;
+  if (way.bits) {
+    if ((r = map_bytes(&m_raw, ckpt, n_tokens, ckpt_pitch(cols), 128)) || (r = map_bytes(&m_scale, ckpt, n_tokens, ckpt_pitch(cols), 16))) return r;
+  } else if ((r = map_mn(&m_x, w.x, n_tokens, padded, 2))) {
+    return r;
+  }
+  const int pairs = std::max(b->n_lanes / 2, 1);
+  r = way.bits ? launch(wgrad_kernel<true>, 2 * pairs, kWgThreads<true>, WgSmem<true>::kBytes, st, m_dy, m_x, m_raw, m_scale, m_out, p)
+               : launch(wgrad_kernel<false>, 2 * pairs, kWgThreads<false>, WgSmem<false>::kBytes, st, m_dy, m_x, m_raw, m_scale, m_out, p);
+  if (r || !joined) return r;
   const unsigned grid = (unsigned)std::min<int64_t>((out_features * (cols / 8) + 255) / 256, 8ll * b->n_lanes);
   return launch(wgrad_join_kernel, grid, 256, 0, st, w.part, p.splits, p.part_rows, (int)out_features, (int)cols, col, col_dtype, d_weight, weight_dtype, accumulate);
 }

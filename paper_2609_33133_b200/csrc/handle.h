@@ -65,6 +65,20 @@ inline int map_mn(CUtensorMap *m, const void *ptr, int64_t rows, int64_t cols, i
   return r == CUDA_SUCCESS ? AUGTREE_OK : AUGTREE_ERR_CUDA;
 }
 
+// Map over bytes: a box is `box_bytes` of a row x 64 rows.
+inline int map_bytes(CUtensorMap *m, const void *ptr, int64_t rows, int64_t pitch, int box_bytes) {
+  EncodeTiledFn enc = get_encode();
+  if (!enc) return AUGTREE_ERR_CUDA;
+  const cuuint64_t dims[2] = {(cuuint64_t)pitch, (cuuint64_t)rows};
+  const cuuint64_t strides[1] = {(cuuint64_t)pitch};
+  const cuuint32_t box[2] = {(cuuint32_t)box_bytes, 64};
+  const cuuint32_t estr[2] = {1, 1};
+  const CUresult r = enc(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(ptr), dims, strides, box, estr,
+                         CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? AUGTREE_OK : AUGTREE_ERR_CUDA;
+}
+
 // Map for results that leave through shared memory: a box is 128 bytes (swizzled) x 32 rows.
 inline int map_out(CUtensorMap *m, const void *ptr, int64_t rows, int64_t cols, bool f32) {
   EncodeTiledFn enc = get_encode();

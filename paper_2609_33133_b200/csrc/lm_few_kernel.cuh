@@ -64,12 +64,6 @@ struct FewSmem {
   static_assert(kStages >= 3 && kStages <= 12 && kBytes <= 227 * 1024, "stage ring");
 };
 
-__device__ __forceinline__ void tma_load_2d(uint32_t dst, const void *tmap, uint32_t bar, int c0, int c1) {
-  asm volatile(
-      "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
-      ::"r"(dst), "l"(tmap), "r"(bar), "r"(c0), "r"(c1) : "memory");
-}
-
 // Reduces W columns over the 32 lanes of a warp: lane j ends up with column j % W.  Halving exchanges: each step a lane gives
 // away the half of its columns that belongs to its partner.
 template <int W, class Op>

@@ -262,12 +262,15 @@ def test_glu_halves_of_one_product(B):
 
 
 # ------------------------------------------------------------------------------------------------ weight gradient
-@pytest.mark.parametrize("n,out,c", [(1, 8, 8), (63, 64, 64), (64, 256, 256), (65, 264, 200), (129, 256, 512), (743, 520, 1032), (2183, 512, 136),
-                                     (5000, 72, 328), (4160, 640, 576)])
+@pytest.mark.parametrize("n,out,c,lanes", [(1, 8, 8, 0), (63, 64, 64, 0), (64, 256, 256, 0), (65, 264, 200, 0), (129, 256, 512, 0), (743, 520, 1032, 0), (2183, 512, 136, 0),
+                                           (5000, 72, 328, 0), (4160, 640, 576, 0), (700, 520, 328, 2), (1000, 328, 520, 4), (2200, 72, 264, 2), (2049, 512, 512, 4)])
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("factors", [False, True])
-def test_wgrad(B, n, out, c, dtype, factors):
-    blk = B.Block(64, device=0)
+def test_wgrad(B, n, out, c, lanes, dtype, factors):
+    """Few lanes: many tiles a CTA pair, the operand by way of bf16 scratch; all lanes: from the bits."""
+    blk = B.Block(64, device=0, n_lanes=lanes)
+    if lanes:
+        assert blk.wgrad_workspace_bytes(n, out, c) == -(-n * -(-c // 64) * 128 // 256) * 256 + 256      # a bf16 copy, no shares
     dy, x = rand((n, out), 1, BF16), rand((n, c), 2, BF16, 2.0)
     row, col = (rand((n,), 3).abs() + 0.1, rand((c,), 4, F32)) if factors else (None, None)
     ckpt, dw = e((n, B.ckpt_pitch(c)), U8), e((out, c), dtype)

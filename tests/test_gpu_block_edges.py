@@ -100,6 +100,13 @@ def test_more_than_two_to_the_31_elements(B):
     blk.unpack(ky, y)
     blk.unpack(small[4], small[0])
     assert torch.equal(y[t], small[0])
+    # the weight gradient: nothing but the last tokens count, and n is a multiple of a stage's 64, so they meet in the same order
+    x[: n - tail] = 0
+    k, dw = torch.empty(n, B.ckpt_pitch(64), device="cuda", dtype=U8), [torch.empty(c, 64, device="cuda") for _ in range(2)]
+    blk.pack(o[:, :64], k)
+    for m, out in ((n, dw[0]), (tail, dw[1])):
+        blk.wgrad(x[n - m:].clone(), k[n - m:].clone(), out, torch.empty(blk.wgrad_workspace_bytes(m, c, 64), device="cuda", dtype=U8))
+    assert (dw[1] != 0).any() and torch.equal(*dw)
     assert blk.device_status() == (0, 0)
 
 
@@ -301,6 +308,18 @@ def test_repeatable_on_streams_in_graphs_and_with_a_shared_workspace(B):
     assert s.blk.device_status() == (0, 0)
 
 
+@pytest.mark.parametrize("c", [256, 1032, 8192])
+def test_one_saved_in_full_and_one_in_8_bits(B, c):
+    """y and o are saved independently of each other, in any of the types."""
+    s = Case(B, 40, c, kind="token", seed=21)
+    fw = s.forward(True)
+    q = lambda t: bu.in_8_bits(t.cpu())
+    for y, o, yr, orr in ((fw["ckpt_y"], cu(s.o), q(fw["y"]), s.o), (fw["y"], fw["ckpt_o"], fw["y"], q(s.o)), (fw["y"].to(BF16), cu(s.o).float(), fw["y"].to(BF16), s.o)):
+        bw = s.backward(fw, y, o)
+        for k, want in s.backward_ref(fw, yr, orr).items():
+            bu.check(bw[k], want, k)
+
+
 @pytest.mark.parametrize("kind", ["channel", "none"])
 def test_gradients_added_to_what_is_there(B, kind):
     s = Case(B, 200, 264, kind=kind, seed=15)
@@ -404,9 +423,11 @@ def test_a_wait_that_runs_out_is_reported(B):
     assert status == -5 and site == 90
     dy, k, dw = rand((700, 256), 1, BF16).cuda(), fw["ckpt_o"], e((256, 520), F32)
     s.blk.pack(cu(s.o), k)
-    s.blk.wgrad(dy, k, dw, e((s.blk.wgrad_workspace_bytes(700, 256, 520),), U8))
-    status, site = s.blk.device_status()
-    assert status == -5 and 100 <= site < 104
+    for lanes, end in ((0, 108), (2, 104)):      # from the bits, by way of bf16 scratch (whichever of the waits on one another is the first to give up)
+        blk = B.Block(64, device=0, flags=flags, n_lanes=lanes)
+        blk.wgrad(dy, k, dw, e((blk.wgrad_workspace_bytes(700, 256, 520),), U8))
+        status, site = blk.device_status()
+        assert status == -5 and 100 <= site < end, site
     Case(B, 700, 520, kind="none", seed=19).check_all(True)
 
 
