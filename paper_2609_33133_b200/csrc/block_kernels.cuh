@@ -108,7 +108,7 @@ __device__ __forceinline__ void block_store8(uint8_t *row, int vec, int type, co
 // A thread's kParts pieces of a row into its checkpoint.  The four lanes of a quad hold a group of 32 columns in each part; two parts' exponents go
 // through one pair of shuffles, and each lane of the quad writes one part's.
 template <int kParts>
-__device__ __forceinline__ void block_keep(uint8_t *row, int v0, int step, int vecs, long long scales, const V8 (&x)[kParts]) {
+__device__ __forceinline__ void block_keep(uint8_t *row, int v0, int step, int vecs, int scales, const V8 (&x)[kParts]) {
   uint32_t byte[kParts];
 #pragma unroll
   for (int k = 0; k < kParts; ++k) byte[k] = ckpt_byte(max_magnitude(x[k]));
@@ -135,8 +135,8 @@ __device__ __forceinline__ void block_keep(uint8_t *row, int v0, int step, int v
 }
 // row t of a matrix in global memory
 template <int T>
-__device__ __forceinline__ uint8_t *block_row(void *base, long long t, int hidden, int type) {
-  return static_cast<uint8_t *>(base) + t * (hidden * type_bytes(T == kAny ? type : T));
+__device__ __forceinline__ uint8_t *block_row(void *base, unsigned t, int hidden, int type) {
+  return static_cast<uint8_t *>(base) + (size_t)t * (unsigned)(hidden * type_bytes(T == kAny ? type : T));
 }
 __device__ __forceinline__ float block_scalar(const void *p, long long i, int type) {
   if (type == T_BF16) return __bfloat162float(static_cast<const __nv_bfloat16 *>(p)[i]);
@@ -255,10 +255,13 @@ struct BlockGroup {
     float *place = sums + flip * 32;
     if ((threadIdx.x & 31) == 0) place[warp] = v;
     asm volatile("bar.sync %0, %1;" ::"r"(bar), "r"(warps * 32) : "memory");
-    v = 0.f;
-    for (int i = 0; i < warps; i += 4) {
-      const float4 q = *reinterpret_cast<const float4 *>(place + i);
-      v += (q.x + q.y) + (q.z + q.w);
+    // (16 warps at most, and zeros behind the last one)
+    const float4 *q = reinterpret_cast<const float4 *>(place);
+    const float4 a = q[0], b = q[1];
+    v = ((a.x + a.y) + (a.z + a.w)) + ((b.x + b.y) + (b.z + b.w));
+    if (warps > 8) {
+      const float4 c = q[2], d = q[3];
+      v += ((c.x + c.y) + (c.z + c.w)) + ((d.x + d.y) + (d.z + d.w));
     }
     flip ^= 1;
     return v;
@@ -266,20 +269,22 @@ struct BlockGroup {
 };
 
 // A group's walk over its rows: block after block of the CTA, in each the rows group, group + groups, ..  `next` is the row behind
-// the present one, -1 if there is none: its numbers are fetched while this one is worked on.
+// the present one, kNone if there is none: its numbers are fetched while this one is worked on.  (Rows and blocks in 32 bits: there are less than 2^31 rows, and
+// a turn of the grid is not longer than they are.)
 struct BlockWalk {
   int group, groups, block_rows, rows;
-  long long t, next;             // row; the one behind it
+  unsigned t, next;              // row; the one behind it
+  static constexpr unsigned kNone = ~0u;
   __device__ __forceinline__ BlockWalk(const BlockShape &s, int group_)
       : group(group_), groups(s.groups), block_rows(s.block_rows), rows(s.rows) {
-    const long long first = (long long)blockIdx.x * block_rows + group;
-    next = group < block_rows && first < rows ? first : -1;
+    const unsigned first = blockIdx.x * block_rows + group;
+    next = group < block_rows && first < (unsigned)rows ? first : kNone;
   }
-  __device__ __forceinline__ void at(long long row0, int r, int block) {      // `block`: rows of this block
+  __device__ __forceinline__ void at(unsigned row0, int r, int block) {      // `block`: rows of this block
     t = row0 + r;
     if (r + groups < block) { next = t + groups; return; }
-    const long long first = row0 + (long long)gridDim.x * block_rows + group;
-    next = first < rows ? first : -1;     // (a group without a row in a block has none behind it either)
+    const unsigned first = row0 + gridDim.x * block_rows + group;
+    next = first < (unsigned)rows ? first : kNone;     // (a group without a row in a block has none behind it either)
   }
 };
 
@@ -317,22 +322,22 @@ block_fwd_kernel(const __grid_constant__ BlockParams p) {
     int st = 0;
     uint32_t phase = 0;
     BlockWalk walk(s, group);
-    float gt_next = gate == GATE_TOKEN && walk.next >= 0 ? block_scalar(p.gate_ptr, walk.next, p.gate_type) : 0.f;
-    for (long long b = blockIdx.x; b < s.blocks; b += gridDim.x) {
-      const long long row0 = b * s.block_rows;
-      const int rows = (int)min((long long)s.block_rows, s.rows - row0);
+    float gt_next = gate == GATE_TOKEN && walk.next != BlockWalk::kNone ? block_scalar(p.gate_ptr, walk.next, p.gate_type) : 0.f;
+    for (unsigned b = blockIdx.x; b < (unsigned)s.blocks; b += gridDim.x) {
+      const unsigned row0 = b * s.block_rows;
+      const int rows = min(s.block_rows, (int)(s.rows - row0));
       // A wait that gave up: the group goes on with whatever is there, so that nobody is left alone at a barrier; its results are
       // void, which the status word says, and every later wait gives up at once.
       mbar_wait(c.bar_full + 8 * st, phase, ab, WAIT_BLOCK_FULL);
       const uint8_t *stage = block_stage(c, p, st);
       for (int r = group; r < rows; r += s.groups) {
         walk.at(row0, r, rows);
-        const long long t = walk.t;
+        const unsigned t = walk.t;
         const uint8_t *rx = stage + s.offset[0] + r * s.row_bytes[0], *ro = stage + s.offset[1] + r * s.row_bytes[1];
         float ga = p.scale;
         if (gate == GATE_TOKEN) {
           ga *= p.sigmoid ? logistic(gt_next) : gt_next;
-          if (walk.next >= 0) gt_next = block_scalar(p.gate_ptr, walk.next, p.gate_type);
+          if (walk.next != BlockWalk::kNone) gt_next = block_scalar(p.gate_ptr, walk.next, p.gate_type);
         }
         // Straight through, without a branch for the pieces behind the row's end: their threads work on the last piece (at[k]) and count for nothing.
         V8 y[kParts];
@@ -347,7 +352,7 @@ block_fwd_kernel(const __grid_constant__ BlockParams p) {
               o[k] = only_if(there[k], block_load8<OT>(ro, at[k], p.o_type, 0));
               ss = dot2(o[k], o[k], ss);
             }
-            if (p.ckpt_o.base) block_keep(p.ckpt_o.base + t * p.ckpt_o.pitch, v0, step, vecs, p.ckpt_o.scales, o);
+            if (p.ckpt_o.base) block_keep(p.ckpt_o.base + (size_t)t * (unsigned)p.ckpt_o.pitch, v0, step, vecs, (int)p.ckpt_o.scales, o);
             if (norm_out) {
               r_o = rsqrtf(fmaf(g.sum(ss.x + ss.y), p.inv_hidden, p.eps));
               if (p.r_out && writer) p.r_out[t] = r_o;
@@ -385,7 +390,7 @@ block_fwd_kernel(const __grid_constant__ BlockParams p) {
         if (p.ckpt_y.base) {
 #pragma unroll
           for (int k = 0; k < kParts; ++k) y[k] = block_round<XT>(y[k], p.x_type);
-          block_keep(p.ckpt_y.base + t * p.ckpt_y.pitch, v0, step, vecs, p.ckpt_y.scales, y);
+          block_keep(p.ckpt_y.base + (size_t)t * (unsigned)p.ckpt_y.pitch, v0, step, vecs, (int)p.ckpt_y.scales, y);
         }
       }
       warp_arrive(c.bar_empty + 8 * st);
@@ -440,20 +445,20 @@ block_bwd_kernel(const __grid_constant__ BlockParams p) {
     BlockWalk walk(s, group);
     float ri_next = 0.f, ro_next = 1.f, gt_next = 1.f;
     auto fetch = [&]() {
-      if (walk.next < 0) return;
+      if (walk.next == BlockWalk::kNone) return;
       if (has_dh) ri_next = p.r_in[walk.next];
       if (norm_out) ro_next = p.r_out[walk.next];
       if (gate == GATE_TOKEN) gt_next = block_scalar(p.gate_ptr, walk.next, p.gate_type);
     };
     fetch();
-    for (long long b = blockIdx.x; b < s.blocks; b += gridDim.x) {
-      const long long row0 = b * s.block_rows;
-      const int rows = (int)min((long long)s.block_rows, s.rows - row0);
+    for (unsigned b = blockIdx.x; b < (unsigned)s.blocks; b += gridDim.x) {
+      const unsigned row0 = b * s.block_rows;
+      const int rows = min(s.block_rows, (int)(s.rows - row0));
       mbar_wait(c.bar_full + 8 * st, phase, ab, WAIT_BLOCK_FULL);
       const uint8_t *stage = block_stage(c, p, st);
       for (int r = group; r < rows; r += s.groups) {
         walk.at(row0, r, rows);
-        const long long t = walk.t;
+        const unsigned t = walk.t;
         auto row = [&](int i) { return stage + s.offset[i] + r * s.row_bytes[i]; };
         const float r_i = ri_next, r_o = ro_next, gate_t = gate == GATE_TOKEN && p.sigmoid ? logistic(gt_next) : gt_next;
         fetch();
