@@ -511,7 +511,8 @@ int augtree_lm_last_device_status(const augtree_lm_t *lm, int *status, int *deta
  * streams and concurrent calls: calls that may overlap need workspaces of their own).  Tensors are row-major [n_tokens, columns]
  * without padding unless a leading size `ld` (elements, a multiple of 8; 0 => the columns) is given; base pointers are 16-byte
  * aligned; r_in, r_out, a gate of one number a token and `row` on their element's size.  Columns: a multiple of 8.  Types: any of the three.
- * Sums and statistics are fp32; every output is rounded once.  No atomics: results are bitwise repeatable.
+ * Sums and statistics are fp32; every output is rounded once.  No atomics: results are bitwise repeatable.  Outputs and scratch must not
+ * overlap inputs or one another, but where it is said (y may be x, dx may be dy).
  */
 enum { AUGTREE_GATE_NONE = 0, AUGTREE_GATE_TOKEN = 1, AUGTREE_GATE_CHANNEL = 2, AUGTREE_GATE_FULL = 3 };  /* none, [n], [hidden], [n, hidden] */
 typedef struct {

@@ -193,19 +193,19 @@ class _Linear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, blk, h, weight, kept):
         ctx.blk, ctx.kept = blk, kept
-        ctx.save_for_backward(weight)
+        ctx.save_for_backward(weight, kept.col)     # (a norm's weight that is changed before the backward pass is an error, as everywhere)
         return F.linear(h, weight)
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, d):
-        blk, kept, (weight,) = ctx.blk, ctx.kept, ctx.saved_tensors
+        blk, kept, (weight, col) = ctx.blk, ctx.kept, ctx.saved_tensors
         d = d.contiguous()
         dw = None
         if ctx.needs_input_grad[2]:
-            dw = torch.empty_like(weight)
+            dw = _like(weight)      # (contiguous, whatever the weight's strides)
             ws = torch.empty(blk.wgrad_workspace_bytes(d.shape[0], *weight.shape), device=d.device, dtype=torch.uint8)
-            blk.wgrad(d, kept.ckpt, dw, ws, kept.row, kept.col)
+            blk.wgrad(d, kept.ckpt, dw, ws, kept.row, col)
         return None, d @ weight if ctx.needs_input_grad[1] else None, dw, None
 
 

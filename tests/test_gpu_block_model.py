@@ -100,6 +100,29 @@ def test_linear_takes_its_gradient_from_the_checkpoint(mods):
     bu.check(weight.grad, (val, bound))
 
 
+def test_linear_with_a_transposed_weight(mods):
+    B, A, _ = mods
+    n, c, out = 70, 72, 136
+    blk = B.Block(c, device=0)
+    x, w, d = leaf((n, c), 1), leaf((c,), 2), leaf((n, out), 4).detach().to(BF16)
+    base = leaf((c, out), 3, 0.1, BF16)
+    h, kept = A.norm(blk, x, w, ckpt=True)
+    A.linear(blk, h, base.t(), kept).backward(d)
+    val, bound = bu.wgrad(d.cpu(), bu.in_8_bits(x.detach().cpu()), kept.row.cpu(), w.detach().cpu(), BF16)
+    bu.check(base.grad.t(), (val, bound))
+
+
+def test_a_norm_weight_changed_before_the_backward_pass_is_an_error(mods):
+    B, A, _ = mods
+    blk = B.Block(64, device=0)
+    x, w, weight = leaf((5, 64), 1).detach(), leaf((64,), 2).detach(), leaf((72, 64), 3, dtype=BF16)
+    h, kept = A.norm(blk, x, w, ckpt=True)      # (nothing of the norm wants a gradient: its own backward pass will not run)
+    y = A.linear(blk, h, weight, kept)
+    w.mul_(2.0)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.float().sum().backward()
+
+
 def test_memory_kept_between_forward_and_backward(mods):
     """What a block end and a gated MLP keep: y and o in full (6 bytes a value), or two checkpoints (2.1)."""
     B, A, _ = mods
