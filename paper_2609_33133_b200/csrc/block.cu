@@ -162,6 +162,9 @@ bool block_shape(const augtree_block *b, int64_t rows, const Input *in, int n_in
   int64_t per = 1, block = groups;
   if (rows < groups * b->n_lanes) block = std::max<int64_t>((rows + b->n_lanes - 1) / b->n_lanes, 1);
   else while (per < 8 && groups * (per + 1) * row <= 32 << 10 && rows >= groups * (per + 1) * b->n_lanes * 8) block = groups * ++per;
+  // As many turns of the lanes as that takes, but no lane has more rows than it has to (2183 x 1032 fp32, blocks of 5 rows instead of 6: forward 9.1 to 8.4 us).
+  const int64_t round = (rows + block * b->n_lanes - 1) / (block * b->n_lanes) * b->n_lanes;
+  block = (rows + round - 1) / round;
   s->block_rows = (int)block;
   s->blocks = (int)((rows + block - 1) / block);
   int64_t off = 0;
