@@ -82,8 +82,9 @@ int with_type(int type, F f) {
 
 // ---------------------------------------------------------------- block ends
 // Pieces of 8 columns of a thread (kParts): one for rows that a warp covers with them, two otherwise, four forward with a 16-bit stream: the more, the
-// fewer warps share a row and the less its reductions and addresses cost (16384 x 3584 bf16 with checkpoints, forward: 154 us with two, 131 with three, 118
-// with four), but an fp32 stream, whose rows are as near to memory's rate with two, takes the stages that more groups need (162 us; 162 to 191 with four).
+// fewer warps share a row and the less its reductions and addresses cost (16384 x 3584 bf16 with checkpoints, forward: 130 us with two, 109 with four), but an
+// fp32 stream, whose rows are as near to memory's rate with two, takes the stages that more groups need (a pass of 24576 x 3584 in both directions: 414 us with
+// two, 443 with four).
 // The backward pass keeps its sums over tokens in registers, which leave no room for more than two.
 int fwd_parts(int hidden, int x) { return hidden <= 256 ? 1 : x == T_BF16 ? 4 : 2; }
 int bwd_parts(int hidden) { return hidden <= 256 ? 1 : 2; }

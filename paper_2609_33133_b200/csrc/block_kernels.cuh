@@ -10,14 +10,16 @@
 // block of rows, which are contiguous) into a ring of stages in shared memory, so what is in flight does not depend on how many threads
 // wait: 44 GB/s and SM at 6.5 TB/s need 35 KB in flight against 0.8 us of latency, and a row of 3584 channels is 21 KB forward and 43 KB
 // backward.  One CTA an SM; its warps form `groups`, and each takes a row of a stage at a time, so one group's reductions run under another's
-// arithmetic.  A thread holds kParts pieces of 8 columns of a row.  (Rings of single rows, one for each group: 279 us instead of 240 for the
-// backward pass of 24576 x 3584 fp32, with the same instructions: copies of one row keep the memory less busy than copies of two.)
+// arithmetic.  A thread holds kParts pieces of 8 columns of a row.  (Rings of single rows, one for each group, took a sixth longer for the backward pass of
+// 24576 x 3584 fp32, with the same instructions: copies of one row keep the memory less busy than copies of two.)
 // A group's sum over a row: shuffles, then the warps' sums through shared memory behind one named barrier.
 // The sums over tokens stay in registers (every thread owns its columns for all rows of its group), go over the groups through shared memory
 // and from CTA to CTA through scratch and a second kernel, in an order that depends on the sizes alone: no atomics, bitwise repeatable.
-// Measured (share of the bytes' time at 6.56 TB/s): 24576 x 3584 with an fp32 stream, forward 162 us (99 %), backward 245 us (99 %); 16384 x 3584 with a bf16
-// stream and checkpoints, which has 10 bytes a value for about the same arithmetic, forward 118 us (76 %, issue slots 80 % busy), backward 151 us (60 %): there
-// 14 warps of 128 registers are all that fit, and each waits for its own row's sums and loads half of the time.
+// Measured (share of the bytes' time at 6.56 TB/s): 24576 x 3584 with an fp32 stream, forward and backward 414 to 420 us (97 %; a loop of one direction alone takes
+// 181 and 260); 16384 x 3584 with a bf16 stream and checkpoints, which has 10 bytes a value for about the same arithmetic, forward 109 to 115 us (80 %),
+// backward 134 us (67 %): 36 instructions a value in both, of which half are arithmetic on the values, issue slots 60 % busy.  Forward 16 warps, backward 14 of 128 registers
+// are all that fit, and the rest is waits for fixed latencies, shared memory and the row's sums.  (Both means of the backward pass from three sums behind
+// one barrier, which d's linearity allows: one more product a value, and no faster.)
 // Every sum, statistic and product is fp32; values are rounded once, on delivery.  The 8-bit form of y is made from y as it is
 // delivered, so that it is the form that ckpt_pack makes of the tensor.
 #pragma once
@@ -462,8 +464,8 @@ block_bwd_kernel(const __grid_constant__ BlockParams p) {
         auto row = [&](int i) { return stage + s.offset[i] + r * s.row_bytes[i]; };
         const float r_i = ri_next, r_o = ro_next, gate_t = gate == GATE_TOKEN && p.sigmoid ? logistic(gt_next) : gt_next;
         fetch();
-        // v and u from checkpoints are kept between their two uses, others are read again (24576 x 3584 fp32: 240 us against 258 kept; 16384 x 3584
-        // bf16 with checkpoints: 160 us kept against 175).
+        // v and u from checkpoints are kept between their two uses, others are read again (24576 x 3584 fp32, both directions: 414 us against 420 kept; 16384 x 3584
+        // bf16 with checkpoints, backward: 133 us kept against 143).
         V8 d[kParts];
         if (has_dh) {
           V8 v[kParts];
