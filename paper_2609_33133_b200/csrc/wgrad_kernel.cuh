@@ -22,7 +22,8 @@
 //
 // Roles: warps 0-7 epilogue (warp w: TMEM lanes 32 (w % 4).., columns 128 (w / 4)..), warp 8 loads dY and a bf16 X (each CTA its own
 // share, all counted on the first CTA's barrier), warp 9 of the first CTA issues the MMAs of both; with kBits also warp 10, which loads X in 8 bits,
-// warp 11, which brings the tokens' factors, and warps 12-19, which turn X into bf16 and tell the first CTA.
+// warp 11, which brings the tokens' factors, and warps 12-19, which turn X into bf16 and tell the first CTA: what they have written is handed over at cluster scope, since an
+// MMA that the first CTA issues reads the second one's as well.
 #pragma once
 #include <cuda.h>
 
@@ -250,7 +251,7 @@ wgrad_kernel(const __grid_constant__ CUtensorMap tm_dy, const __grid_constant__ 
         }
         fence_async_shared();      // the tensor core reads what was written here
         __syncwarp();
-        if (lane == 0) mbar_arrive_cluster(map_to_rank(x_full + 8 * sx, 0));
+        if (lane == 0) mbar_arrive_cluster_release(map_to_rank(x_full + 8 * sx, 0));
         sr += kWgTeams;
         if (sr >= SM::kRaw) { sr -= SM::kRaw; pr ^= 1; }
         sx += kWgTeams;
@@ -276,7 +277,7 @@ wgrad_kernel(const __grid_constant__ CUtensorMap tm_dy, const __grid_constant__ 
           }
           const int end = min(kb + chunk, c.steps);
           for (bool first = true; kb < end; ++kb, first = false) {
-            ok = mbar_wait(a_full + 8 * sa, pa, ab, WAIT_WG_FULL) && (!kBits || mbar_wait(x_full + 8 * sx, px, ab, WAIT_WG_X_FULL));
+            ok = mbar_wait(a_full + 8 * sa, pa, ab, WAIT_WG_FULL) && (!kBits || mbar_wait_cluster(x_full + 8 * sx, px, ab, WAIT_WG_X_FULL));
             if (!ok) break;
             tc_fence_after();
             const uint32_t a_lo = sdesc_lo(base + sa * SM::kABytes, 8192), b_lo = sdesc_lo(base + SM::kOffX + sx * SM::kXBytes, 8192);
