@@ -150,23 +150,22 @@ class _Block(torch.autograd.Function):
         kept_y, kept_o = (box() if w_in is not None else None, None if o is None else box()) if ckpt else (None, None)
         blk.fwd(x, o, gate, w_out, w_in, y, h, r_out, r_in, kept_y, kept_o)
         ctx.set_materialize_grads(False)
-        ctx.blk, ctx.ckpt, ctx.like = blk, ckpt, (x.dtype, None if o is None else o.dtype)
-        ctx.numbers = (r_out, r_in, kept_y, kept_o)
-        ctx.save_for_backward(gate, w_out, w_in, *((None, None) if ckpt else (x if o is None else y, o)))
+        ctx.blk, ctx.like = blk, (x.dtype, None if o is None else o.dtype)
+        # (all of it as saved tensors: an attribute would outlive the backward pass as long as somebody holds the loss)
+        ctx.save_for_backward(gate, w_out, w_in, r_out, r_in, *((kept_y, kept_o) if ckpt else (x if o is None else y, o)))
         kept = Kept(kept_y, r_in, w_in.detach()) if kept_y is not None else None
         return y, h, kept
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dy, dh, _):
-        blk, (r_out, r_in, kept_y, kept_o) = ctx.blk, ctx.numbers
-        gate, w_out, w_in, y, o = ctx.saved_tensors
+        blk = ctx.blk
+        gate, w_out, w_in, r_out, r_in, y, o = ctx.saved_tensors
         x_dtype, o_dtype = ctx.like
         if dy is None and dh is None:
             return (None,) * 8
         lead = dh if dy is None else dy
         dy, dh = (None if t is None else t.contiguous() for t in (dy, dh))
-        y, o = (kept_y, kept_o) if ctx.ckpt else (y, o)
         if dh is None:
             y = r_in = w_in = None
         need = ctx.needs_input_grad
@@ -192,20 +191,20 @@ def norm(blk: B.Block, x, w, *, h_dtype=torch.bfloat16, ckpt=False):
 class _Linear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, blk, h, weight, kept):
-        ctx.blk, ctx.kept = blk, kept
-        ctx.save_for_backward(weight, kept.col)     # (a norm's weight that is changed before the backward pass is an error, as everywhere)
+        ctx.blk = blk
+        ctx.save_for_backward(weight, kept.ckpt, kept.row, kept.col)     # (what is changed before the backward pass is an error, as everywhere)
         return F.linear(h, weight)
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, d):
-        blk, kept, (weight, col) = ctx.blk, ctx.kept, ctx.saved_tensors
+        blk, (weight, ckpt, row, col) = ctx.blk, ctx.saved_tensors
         d = d.contiguous()
         dw = None
         if ctx.needs_input_grad[2]:
             dw = _like(weight)      # (contiguous, whatever the weight's strides)
             ws = torch.empty(blk.wgrad_workspace_bytes(d.shape[0], *weight.shape), device=d.device, dtype=torch.uint8)
-            blk.wgrad(d, kept.ckpt, dw, ws, kept.row, col)
+            blk.wgrad(d, ckpt, dw, ws, row, col)
         return None, d @ weight if ctx.needs_input_grad[1] else None, dw, None
 
 
@@ -222,15 +221,14 @@ class _Glu(torch.autograd.Function):
         box = lambda: torch.empty((n, B.ckpt_pitch(cols)), device=g.device, dtype=torch.uint8) if ckpt else None
         kept = (box(), box())
         blk.glu_fwd(g, u, a, *kept)
-        ctx.blk, ctx.kept = blk, kept if ckpt else None
-        ctx.save_for_backward(weight, *((None, None) if ckpt else (g, u)))
+        ctx.blk = blk
+        ctx.save_for_backward(weight, *(kept if ckpt else (g, u)))
         return a if weight is None else F.linear(a, weight)
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, d):
         weight, g, u = ctx.saved_tensors
-        g, u = ctx.kept or (g, u)
         da = (d if weight is None else d @ weight).contiguous()
         dg, du = torch.empty_like(da), torch.empty_like(da)
         a = torch.empty_like(da) if weight is not None and ctx.needs_input_grad[3] else None

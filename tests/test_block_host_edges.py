@@ -1,6 +1,8 @@
 """Host side of the block ends and checkpoints, continued: what can be seen without a GPU."""
+import gc
 import os
 import re
+import weakref
 
 import pytest
 import torch
@@ -36,3 +38,57 @@ def test_shared_memory_for_the_other_cta_is_handed_over_at_cluster_scope():
     assert re.search(r"fence\.release\.sync_restrict::shared::cta\.cluster;.*mbarrier\.arrive\.relaxed\.cluster\.shared::cluster", body("mbar_arrive_cluster_release"))
     assert "mbarrier.try_wait.parity.relaxed.cluster.shared::cta" in body("mbar_try_wait_cluster")
     assert "fence.acquire.sync_restrict::shared::cluster.cluster;" in body("acquire_cluster_shared") and "acquire_cluster_shared();" in body("mbar_wait_cluster")
+
+
+# ------------------------------------------------------------------------------------------------ autograd, with a handle that does no arithmetic
+class Still:
+    """A handle whose calls do nothing: what autograd keeps, releases and refuses does not depend on the numbers."""
+
+    def __init__(self, hidden):
+        self.hidden, self.calls = hidden, []
+
+    def __getattr__(self, name):
+        return lambda *a, **k: self.calls.append((name, a, k))
+
+    def workspace_bytes(self, n):
+        return 16
+
+    def wgrad_workspace_bytes(self, *a):
+        return 16
+
+
+def chain(A, blk, ckpt):
+    """(loss, checkpoints) of a block end, a product of its norm and a gated MLP."""
+    leaf = lambda *s, dtype=torch.float32: torch.ones(s, dtype=dtype, requires_grad=True)
+    x, o, w = leaf(6, 64), leaf(6, 64, dtype=torch.bfloat16), leaf(64)
+    _, h, kept = A.block(blk, x, o, None, w, w, ckpt=ckpt)
+    z = A.linear(blk, h, leaf(72, 64, dtype=torch.bfloat16), kept)
+    return A.glu_linear(blk, z, z * 2, leaf(64, 72, dtype=torch.bfloat16), ckpt=ckpt).float().sum(), kept
+
+
+def test_checkpoints_are_saved_tensors(B):
+    """Released as the backward pass goes by even if the loss is held, seen by hooks, and a change in place is an error."""
+    from paper_2609_33133_b200 import autograd as A
+    blk, live = Still(64), []
+    alive = lambda: sum(r() is not None for r in live)
+
+    def pack(t):
+        if t.dtype is torch.uint8:
+            live.append(weakref.ref(t))
+        return t
+    with torch.autograd.graph.saved_tensors_hooks(pack, lambda t: t):
+        loss, kept = chain(A, blk, True)
+    assert len(live) == 5 and kept.ckpt.shape == (6, B.ckpt_pitch(64))     # y and o of the block end, y again for the product, g and u
+    blk.calls.clear()
+    del kept
+    gc.collect()
+    assert alive() == 5
+    loss.backward()
+    blk.calls.clear()
+    gc.collect()
+    assert loss is not None and alive() == 0
+    for change in ("ckpt", "row"):
+        loss, kept = chain(A, Still(64), True)
+        getattr(kept, change).zero_()
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            loss.backward()

@@ -34,3 +34,26 @@ def test_a_weight_gradient_of_whole_numbers_is_exact(B, n, out, c):
         blk.wgrad(dy.to(BF16), ckpt, dw, ws)
         assert torch.equal(dw.double(), dy.double().t() @ x.double())
     assert blk.device_status() == (0, 0)
+
+
+def test_memory_after_the_backward_pass_while_the_loss_is_held(B):
+    """Checkpoints (2.1 bytes a value of a block end, the same again of a gated MLP) are gone as the uncheckpointed tensors are."""
+    from paper_2609_33133_b200 import autograd as A
+    n, c = 4096, 1024
+    blk = B.Block(c, device=0)
+    x = torch.randn(n, c, device="cuda").requires_grad_(True)
+    o = torch.randn(n, c, device="cuda").to(BF16).requires_grad_(True)
+    w, wt = torch.ones(c, device="cuda", requires_grad=True), torch.randn(c, c, device="cuda").mul_(0.03).to(BF16).requires_grad_(True)
+
+    def loss(ckpt):
+        _, h, kept = A.block(blk, x, o, None, w, w, ckpt=ckpt)
+        return A.glu(blk, A.linear(blk, h, wt, kept), h, ckpt=ckpt).float().sum()
+    for ckpt in (False, True):
+        loss(ckpt).backward()              # (gradients of the leaves and the library's workspaces are there from here on)
+        torch.cuda.synchronize()
+        before = torch.cuda.memory_allocated()
+        s = loss(ckpt)
+        assert torch.cuda.memory_allocated() - before > 4 * n * c
+        s.backward()
+        assert torch.cuda.memory_allocated() - before <= 1 << 16, ckpt
+        del s
