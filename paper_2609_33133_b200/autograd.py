@@ -209,8 +209,19 @@ class _Linear(torch.autograd.Function):
 
 
 def linear(blk: B.Block, h, weight, kept=None):
-    """h @ weight.T in bf16.  With `kept` (of the same h) the weight's gradient comes from the checkpoint and h is not saved."""
-    return F.linear(h, weight) if kept is None else _Linear.apply(blk, h, weight, kept)
+    """h @ weight.T in bf16.  With `kept` (of the same h) the weight's gradient comes from the checkpoint and h is not saved; what that gradient's product does
+    not take (other types, more dimensions, a number of features that is no multiple of 8) is refused here and not in the backward pass."""
+    if kept is None:
+        return F.linear(h, weight)
+    y = _Linear.apply(blk, h, weight, kept)
+    if weight.requires_grad and torch.is_grad_enabled():
+        got = lambda t: f"{tuple(t.shape)} {t.dtype}"
+        if h.dim() != 2 or y.dtype is not torch.bfloat16 or weight.dtype not in (torch.bfloat16, torch.float32) or weight.shape[0] % 8:
+            raise ValueError("linear with a checkpoint: expected a bf16 product of h [tokens, columns] with a bf16 or fp32 weight [a multiple of 8, columns], got "
+                             f"{got(h)} and {got(weight)}, product {y.dtype}")
+        if kept.ckpt.shape != (h.shape[0], B.ckpt_pitch(h.shape[1])):
+            raise ValueError(f"linear: h is {got(h)}, the checkpoint is of another tensor: {got(kept.ckpt)}")
+    return y
 
 
 class _Glu(torch.autograd.Function):
