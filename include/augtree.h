@@ -584,7 +584,8 @@ int augtree_glu_bwd(const augtree_block_t *block, const void *da, int dtype, con
 /*
  * Weight gradient of a product whose input was kept in 8 bits: d_weight [out_features, cols] = dy^T X with dy [n_tokens, out_features] bf16 and
  * X = 2^e q, times row[t] (then rounded to bf16, as an operand of the tensor core) and col[c] where they are not NULL: with r_in and w_in X
- * is the norm's output h.  d_weight: bf16 or fp32, the latter also added to (accumulate != 0, else AUGTREE_ERR_UNSUPPORTED).
+ * is the norm's output h.  d_weight: bf16 or fp32, the latter also added to (accumulate != 0, else AUGTREE_ERR_UNSUPPORTED).  Sums of more than 32768
+ * tokens go through fp32 scratch for a bf16 d_weight, too; the scratch of such sizes has room for it whatever d_weight's type.
  */
 int augtree_ckpt_wgrad_bytes(const augtree_block_t *block, int64_t n_tokens, int64_t out_features, int64_t cols, size_t *bytes);
 int augtree_ckpt_wgrad(const augtree_block_t *block, const void *dy, int64_t n_tokens, int64_t out_features, const void *ckpt, int64_t cols,

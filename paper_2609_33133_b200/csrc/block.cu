@@ -207,7 +207,7 @@ size_t bwd_bytes(const augtree_block *b) { return (size_t)b->n_lanes * 2 * b->hi
 // How a call is done: shares of the contraction, and whether X is turned into bf16 in the kernel (kBits, wgrad_kernel.cuh).  By the time of the longest
 // CTA pair (a stage of 64 tokens 0.28 us from bf16 and 0.4 from bits, a tile's start and end 2 us), of the partial sums' way through memory (4 us and
 // their bytes, written and read, at 6 TB/s) and of a bf16 X's (2 us and its 3 bytes a value).
-struct WgradWay { int splits; bool bits; };
+struct WgradWay { int splits; bool bits; int parts; };    // parts: results of the tensors' size in fp32 that the scratch has room for
 WgradWay wgrad_way(int lanes, int64_t n, int64_t out, int64_t cols) {
   const int64_t pairs = std::max(lanes / 2, 1), tiles = ((out + kLmTile - 1) / kLmTile) * ((cols + kLmTile - 1) / kLmTile);
   const int64_t steps = std::max<int64_t>((n + 63) / 64, 1);
@@ -215,12 +215,13 @@ WgradWay wgrad_way(int lanes, int64_t n, int64_t out, int64_t cols) {
     const double longest = (double)((tiles * s + pairs - 1) / pairs) * ((bits ? 0.4 : 0.28) * (double)((steps + s - 1) / s) + 2.0);
     return longest + (s > 1 ? 4.0 + (double)(s * out * cols) * 8e-6 / 6.0 : 0.0) + (bits ? 0.0 : 2.0 + (double)(n * cols) * 3e-6 / 6.0);
   };
-  WgradWay pick = {1, true};
+  WgradWay pick = {1, true, 0};
   for (bool bits : {true, false})
     for (int64_t s = 1; s <= std::min<int64_t>(steps, 32); ++s)
-      if (cost(s, bits) < cost(pick.splits, pick.bits)) pick = {(int)s, bits};
+      if (cost(s, bits) < cost(pick.splits, pick.bits)) pick = {(int)s, bits, 0};
   const int64_t share = (steps + pick.splits - 1) / pick.splits;
   pick.splits = (int)((steps + share - 1) / share);   // (no empty share)
+  pick.parts = pick.splits > 1 || steps > kWgLong ? pick.splits : 0;    // (a call does not say here what its result's type will be)
   return pick;
 }
 
@@ -228,7 +229,7 @@ struct WgradWs { __nv_bfloat16 *x; float *part; };
 size_t wgrad_layout(const WgradWay &way, int64_t n, int64_t out, int64_t cols, uint8_t *base, WgradWs *w) {
   Cursor c{base};
   w->x = c.take<__nv_bfloat16>(way.bits ? 0 : n * up(cols, 64));
-  w->part = c.take<float>(way.splits > 1 ? way.splits * up(out, kLmTile) * cols : 0);
+  w->part = c.take<float>(way.parts * up(out, kLmTile) * cols);
   return c.off;
 }
 
@@ -533,7 +534,7 @@ int augtree_ckpt_wgrad(const augtree_block_t *b, const void *dy, int64_t n_token
   p.a_chunks = out_features % 64 == 0 ? 2 : 1;
   p.part_rows = (int64_t)p.mt * kLmTile;
   p.scales = (int)ckpt_scale_offset(cols); p.rows = (int)n_tokens; p.row = row;
-  const bool joined = p.splits > 1;
+  const bool joined = p.splits > 1 || (!f32 && p.steps > kWgLong);
   p.f32 = joined || f32; p.add = !joined && accumulate;
   p.col = joined ? nullptr : col; p.col_type = col_dtype;
   p.status = b->d_status;

@@ -14,9 +14,10 @@
 // 1770 us, 1257 TFLOP/s, and the library's product of the same sizes 1610.
 //
 // The tensor core's adder drops what does not fit, always towards zero, 2^-24 to 2^-23 of the accumulator for every 16 tokens: over
-// 16384 tokens 3e-5 of a result, far under a bf16 result's rounding but not under an fp32 one's.  So for fp32 a tile's contraction is cut into
+// 16384 tokens of one sign 1e-4 of a result, far under a bf16 result's rounding but not under an fp32 one's.  So for fp32 a tile's contraction is cut into
 // pieces of kWgChunk stages; the two halves of TMEM take them in turn, and the pieces are added in memory by the copy engine, rounded to
-// nearest, one behind the other (each warp waits for its own addition to be done before it starts the next).
+// nearest, one behind the other (each warp waits for its own addition to be done before it starts the next).  A bf16 result goes that way through fp32
+// scratch, too, from more than kWgLong stages on: in one accumulator a million tokens of one sign lost 6.6e-3 of it, twice its rounding.
 //
 // Few tiles share their contraction out further (`splits`), each share into fp32 scratch, and wgrad_join_kernel adds them in order.
 //
@@ -33,6 +34,7 @@
 namespace augtree {
 
 constexpr int kWgChunk = 32;   // stages (of 64 tokens) between additions of an fp32 result
+constexpr int kWgLong = 512;   // stages that a bf16 result may take in one accumulator: 2048 additions, which lose 2.4e-4 of it at most, an eighth of its rounding's half step or less
 constexpr int kWgTeams = 2, kWgTeam = 4;    // teams of warps that turn X into bf16, stage by stage in turn; warps of a team
 template <bool kBits> constexpr int kWgThreads = kBits ? (12 + kWgTeams * kWgTeam) * 32 : 320;
 enum : int { WAIT_WG_FULL = 100, WAIT_WG_EMPTY = 101, WAIT_WG_ACC_FULL = 102, WAIT_WG_ACC_EMPTY = 103, WAIT_WG_RAW_FULL = 104, WAIT_WG_RAW_EMPTY = 105,
@@ -368,7 +370,7 @@ wgrad_kernel(const __grid_constant__ CUtensorMap tm_dy, const __grid_constant__ 
   if (warp == 9) { tc_fence_after(); tmem_dealloc_pair(tmem, 512); }
 }
 
-// Shares' partial sums into dW, in the order of the shares.
+// Shares' partial sums (or a long bf16 result's only one) into dW, in the order of the shares.
 __global__ void __launch_bounds__(256)
 wgrad_join_kernel(const float *part, int splits, long long part_rows, int out, int cols, const void *col, int col_type, void *dw, int type, int add) {
   launch_next();

@@ -57,3 +57,34 @@ def test_memory_after_the_backward_pass_while_the_loss_is_held(B):
         s.backward()
         assert torch.cuda.memory_allocated() - before <= 1 << 16, ckpt
         del s
+
+
+def between(got, val, off):
+    """A rounding of some value within `off` of `val`: rounding keeps the order, so its bounds are the roundings of the interval's ends."""
+    lo, hi = (val - off).to(got.dtype), (val + off).to(got.dtype)
+    bad = ~((lo <= got) & (got <= hi))
+    assert not bad.any(), (int(bad.sum()), ((got.double() - val) / val)[bad].mean().item())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n,lanes", [(32768, 2), (32769, 2), ((1 << 20) + 37, 2), ((1 << 20) + 37, 0)])
+def test_a_weight_gradient_over_many_tokens_of_one_sign(B, n, lanes, dtype):
+    """Two lanes: one share.  The tensor core's adder loses up to 2^-23 of its sum for every 16 tokens, always downwards: over 32768 tokens in one accumulator 2049 times; in
+    pieces of 2048 tokens 128 times, and one rounding for each piece and share."""
+    out, c = 64, 72
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    rand = lambda *s: torch.rand(s, generator=gen, device="cuda")
+    blk = B.Block(64, device=0, n_lanes=lanes)
+    dy, x, col = ((0.5 + rand(n, out)) * (1 + rand(out))).to(BF16), 0.5 + rand(n, c), 1 + rand(c)     # (products spread over a factor of four: their roundings differ)
+    ckpt, dw = torch.empty((n, B.ckpt_pitch(c)), device="cuda", dtype=U8), torch.full((out, c), float("nan"), device="cuda", dtype=dtype)
+    blk.pack(x, ckpt)
+    blk.wgrad(dy, ckpt, dw, torch.empty(blk.wgrad_workspace_bytes(n, out, c), device="cuda", dtype=U8), None, col)
+    blk.unpack(ckpt, x)
+    val = torch.zeros((out, c), device="cuda", dtype=F64)
+    for i in range(0, n, 1 << 17):
+        val += dy[i:i + (1 << 17)].double().t() @ x[i:i + (1 << 17)].double()
+    val *= col.double()
+    one = dtype is BF16 and n <= 32768 and lanes == 2
+    adds = 2 * 2049 if one else 2 * 128 + n / 2048 + 40
+    between(dw, val, (adds + 4) * bu.U * val)
+    assert blk.device_status() == (0, 0)
