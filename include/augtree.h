@@ -539,7 +539,6 @@ int augtree_block_destroy(augtree_block_t *block);
  * x, y: x_dtype; y may be x itself.  o: NULL for the norm before a block alone (then y, w_out, gate and ckpt_o are NULL and h is made of
  * x).  h and w_in: both or neither.  gate: as the handle says, wherever there is an o.  r_out, r_in [n_tokens] fp32: what the backward pass
  * needs, NULL if there is none.  ckpt_y, ckpt_o (or NULL): the 8-bit forms of y (of x without an o), as delivered, and of o.
- * AUGTREE_ERR_UNSUPPORTED when a row of all inputs does not fit a CTA's shared memory (hidden near 8192 with everything in fp32).
  */
 int augtree_block_fwd(const augtree_block_t *block, const void *x, int x_dtype, const void *o, int o_dtype, const void *gate, int gate_dtype,
                       const void *w_out, const void *w_in, int w_dtype, int64_t n_tokens, void *y, void *h, int h_dtype, float *r_out,
@@ -553,7 +552,9 @@ int augtree_block_workspace_bytes(const augtree_block_t *block, int64_t n_tokens
  * call left them, or their 8-bit forms (dtype AUGTREE_CKPT); without an o the forward's x stands for y.
  *   dx (x_dtype; may be dy itself), d_o, d_gate (type and shape of the gate), dw_out, dw_in [hidden] (w_dtype): each may be NULL and is
  *   then not written.  With accumulate != 0 the sums over tokens (dw_out, dw_in, d_gate of one number a channel) are ADDED to what is
- *   there (fp32 only, else AUGTREE_ERR_UNSUPPORTED).  With dh NULL, w_in, y and r_in are NULL too or not read.
+ *   there (fp32 only, else AUGTREE_ERR_UNSUPPORTED).  With dh NULL, w_in and dw_in have to be NULL too, and y and r_in are not read.
+ * AUGTREE_ERR_UNSUPPORTED as well when a row of all inputs does not fit a CTA's shared memory: hidden from 8120 on with dy, dh, y, o and a gate of one
+ * number a channel or of each, all in fp32, and both norms.  Two calls do that: one with o NULL, and one with its dx as dy and dh NULL.
  */
 int augtree_block_bwd(const augtree_block_t *block, const void *dy, int x_dtype, const void *dh, int h_dtype, const void *y, int y_dtype,
                       const void *o, int o_dtype, const void *gate, int gate_dtype, const void *w_out, const void *w_in, int w_dtype,

@@ -173,7 +173,17 @@ class _Block(torch.autograd.Function):
         d_o = _like(lead, dtype=o_dtype) if need[2] else None
         d_gate, dw_out, dw_in = (_like(t) if wanted else None for t, wanted in zip((gate, w_out, w_in), need[3:6]))
         ws = torch.empty(blk.workspace_bytes(lead.shape[0]), device=lead.device, dtype=torch.uint8)
-        blk.bwd(dy, dh, y, o, gate, w_out, w_in, r_out, r_in, dx, d_o, d_gate, dw_out, dw_in, ws)
+        try:
+            blk.bwd(dy, dh, y, o, gate, w_out, w_in, r_out, r_in, dx, d_o, d_gate, dw_out, dw_in, ws)
+        except B.AugtreeError as err:
+            if err.code != B.ERR_UNSUPPORTED or o is None or dh is None:
+                raise
+            # A row of all inputs does not fit a CTA: about 8192 channels, everything in fp32 and a gate.  In two calls then, the norm before the next block
+            # and what lies before it.  What passes between them is the gradient of y in fp32, which one call would have held as well.
+            dx = _like(lead, dtype=x_dtype) if dx is None else dx
+            blk.bwd(dy, dh, y, None, None, None, w_in, None, r_in, dx, None, None, None, dw_in, ws)
+            blk.bwd(dx, None, None, o, gate, w_out, None, r_out, None, None, d_o, d_gate, dw_out, None, ws)
+            dx = dx if need[1] else None
         return None, dx, d_o, d_gate, dw_out, dw_in, None, None
 
 

@@ -154,6 +154,9 @@ def plan_tree(prompt_len, branch_len, h_q, h_kv, degrees, profile: dict, b_max=0
             "solved_exactly": bool(ch.solved_exactly), "n_candidates": ch.n_candidates, "X": (list(rounds[:G]), list(lanes[:G]))}
 
 
+ERR_UNSUPPORTED = -2
+
+
 class AugtreeError(RuntimeError):
     def __init__(self, code, where):
         self.code = code

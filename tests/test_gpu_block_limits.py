@@ -88,3 +88,31 @@ def test_a_weight_gradient_over_many_tokens_of_one_sign(B, n, lanes, dtype):
     adds = 2 * 2049 if one else 2 * 128 + n / 2048 + 40
     between(dw, val, (adds + 4) * bu.U * val)
     assert blk.device_status() == (0, 0)
+
+
+@pytest.mark.parametrize("kind", ["full", "channel"])
+@pytest.mark.parametrize("c", [8112, 8120, 8192])
+@pytest.mark.parametrize("x_grad", [False, True])
+def test_the_widest_rows_through_autograd(B, kind, c, x_grad):
+    """Everything in fp32: from 8120 channels on the rows of all of the backward pass' inputs do not fit a CTA together.  r of the reference is a rounding of the 64-bit one, the
+    kernel's is within 30 half steps of it, and every term of a gradient has at most three factors r: 100 half steps of the terms' sizes, which the largest gradient of a
+    tensor bounds within a factor of ten."""
+    from paper_2609_33133_b200 import autograd as A
+    n, eps = 5, 1e-5
+    gen = torch.Generator().manual_seed(c)
+    leaf = lambda *s: torch.randn(s, generator=gen).cuda().requires_grad_(True)
+    x, o, w_out, w_in, g = leaf(n, c), leaf(n, c), leaf(c), leaf(c), leaf(n, c) if kind == "full" else leaf(c)
+    dy, dh = torch.randn(n, c, generator=gen).cuda(), torch.randn(n, c, generator=gen).cuda()
+    blk = B.Block(c, device=0, eps=eps, residual_scale=0.7, gate=kind)
+    y, h, _ = A.block(blk, x if x_grad else x.detach(), o, g, w_out, w_in, h_dtype=F32)
+    torch.autograd.backward((y, h), (dy, dh))
+    d = lambda t: t.detach().cpu()
+    r = lambda t: torch.rsqrt(t.double().pow(2).mean(1) + eps).float()
+    ref = bu.block_bwd(d(dy), d(dh), d(y), d(o), d(g), d(w_out), d(w_in), r(d(o)), r(d(y)), kind=kind, sigmoid=False, scale=0.7,
+                       types={"x": F32, "o": F32, "w": F32, "gate": F32})
+    assert (x.grad is not None) == x_grad
+    for name, t in (("dx", x), ("d_o", o), ("d_gate", g), ("dw_out", w_out), ("dw_in", w_in)):
+        val, bound = ref[name]
+        if t.grad is not None:
+            bu.check(t.grad, (val, bound + 1000 * bu.U * val.abs().max()), name)
+    assert blk.device_status() == (0, 0)
