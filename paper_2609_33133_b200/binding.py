@@ -8,18 +8,38 @@ run `python -m paper_2609_33133_b200.build`.
 from __future__ import annotations
 
 import ctypes as C
+import importlib.machinery
+import importlib.util
 import operator
 import os
 
 import numpy as np
 import torch
 
+from . import build as _build
+
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("AUGTREE_LIB") or os.path.join(_HERE, "libaugtree.so")   # AUGTREE_LIB: another build of the library
 if not os.path.exists(LIB_PATH):
     raise ImportError(f"{LIB_PATH} is missing: build it with `python -m paper_2609_33133_b200.build`")
 lib = C.CDLL(LIB_PATH)
-from . import _marshal  # noqa: E402  (Block's argument checks and calls, csrc/marshal.cpp)
+
+
+def _load_marshal():
+    """Block's argument checks and calls (csrc/marshal.cpp), or why there are none: nothing but Block needs them."""
+    path = _build.marshal_path()
+    if not os.path.exists(path):
+        return None, f"{path} is missing"
+    try:
+        loader = importlib.machinery.ExtensionFileLoader(__package__ + "._marshal", path)
+        module = importlib.util.module_from_spec(importlib.util.spec_from_loader(loader.name, loader))
+        loader.exec_module(module)
+        return module, None
+    except ImportError as err:
+        return None, f"{path} does not load: {err}"
+
+
+_marshal, _no_marshal = _load_marshal()
 
 FLAG_ZERO_PROMPT_GRAD = 1
 FLAG_TEST_SHORT_WAIT, FLAG_TEST_SKIP_FWD_LOAD, FLAG_TEST_SKIP_BWD_LOAD, FLAG_TEST_DROP_ITEM = 0x100, 0x200, 0x400, 0x800
@@ -133,7 +153,8 @@ lib.augtree_glu_fwd.argtypes = [_vp, _vp, _vp, _l, _i, _l, _l, _vp, _vp, _vp, _v
 lib.augtree_glu_bwd.argtypes = [_vp, _vp, _i, _vp, _vp, _l, _i, _l, _l, _vp, _vp, _l, _vp, _vp]
 lib.augtree_ckpt_wgrad.argtypes = [_vp, _vp, _l, _l, _vp, _l, _vp, _vp, _i, _vp, _i, _i, _vp, _sz, _vp]
 lib.augtree_ckpt_wgrad_bytes.argtypes = [_vp, _l, _l, _l, C.POINTER(_sz)]
-_marshal.init(*[C.cast(getattr(lib, "augtree_" + n), _vp).value for n in ("block_fwd", "block_bwd", "ckpt_pitch", "ckpt_pack", "ckpt_unpack", "glu_fwd",
+if _marshal:
+    _marshal.init(*[C.cast(getattr(lib, "augtree_" + n), _vp).value for n in ("block_fwd", "block_bwd", "ckpt_pitch", "ckpt_pack", "ckpt_unpack", "glu_fwd",
                                                                           "glu_bwd", "ckpt_wgrad")])
 lib.augtree_block_last_device_status.argtypes = [_vp, C.POINTER(_i), C.POINTER(_i)]
 lib.augtree_plan_tree.argtypes = [C.POINTER(TreeC), C.POINTER(ProfileC), C.POINTER(ChoiceC), _i32p, _i32p]
@@ -428,6 +449,8 @@ class Block:
     an 8-bit checkpoint, it is a uint8 tensor [tokens, ckpt_pitch(columns)]."""
 
     def __init__(self, hidden, *, device=0, eps=0.0, residual_scale=0.0, gate="none", gate_sigmoid=False, flags=0, n_lanes=0):
+        if not _marshal:
+            raise ImportError(_no_marshal + ": build it with `python -m paper_2609_33133_b200.build` (a C++ compiler and torch's headers)")
         if any(x and not C.c_float(x).value for x in (eps, residual_scale)):   # (zero stands for the default there)
             raise ValueError(f"eps {eps}, residual_scale {residual_scale}: too small for fp32")
         if gate not in GATES:

@@ -2,6 +2,9 @@
 import gc
 import os
 import re
+import shutil
+import subprocess
+import sys
 import weakref
 
 import pytest
@@ -112,3 +115,29 @@ def test_a_product_whose_gradient_cannot_be_made_is_refused_at_once(B):
             product(**bad)
     with torch.autocast("cpu", BF16):      # the product's type counts, not its operands'
         assert product(weight=F32).dtype is BF16
+
+
+# ------------------------------------------------------------------------------------------------ the extension that checks arguments
+@pytest.mark.parametrize("broken", [False, True])
+def test_only_the_block_handle_needs_the_argument_checks(B, tmp_path, broken):
+    """Without csrc/marshal.cpp's extension, or with one that does not load, plans and vocabulary handles work and a block handle says what to do."""
+    from paper_2609_33133_b200 import build
+    package = os.path.basename(build.HERE)
+    shutil.copytree(build.HERE, tmp_path / package, ignore=shutil.ignore_patterns("_marshal*", "__pycache__"))
+    if broken:
+        (tmp_path / package / os.path.basename(build.marshal_path())).write_bytes(b"not a library")
+    code = ("from paper_2609_33133_b200 import binding as B\n"
+            "plan, lm = B.Plan([5], [[3]], 2, 1, 64, device=None, n_lanes=4), B.LM(503, 64, device=None, n_lanes=4)\n"
+            "try:\n    B.Block(64, device=None, n_lanes=4)\n"
+            "except ImportError as err:\n    print(plan.total_p, lm.vocab, err)\n")
+    run = subprocess.run([sys.executable, "-c", code], cwd=tmp_path, env={**os.environ, "PYTHONPATH": str(tmp_path)}, capture_output=True, text=True)
+    assert run.returncode == 0 and run.stdout.startswith("5 503 "), run.stdout + run.stderr
+    assert ("does not load" if broken else "is missing") in run.stdout and "paper_2609_33133_b200.build" in run.stdout
+
+
+def test_another_torch_gets_an_extension_of_its_own(B, monkeypatch):
+    from paper_2609_33133_b200 import build
+    here = build.marshal_path()
+    assert os.path.exists(here) and not build._stale(here, build.MARSHAL_SOURCES)
+    monkeypatch.setattr(torch, "__version__", "99.0")
+    assert build.marshal_path() != here and build._stale(build.marshal_path(), build.MARSHAL_SOURCES)
