@@ -563,8 +563,9 @@ int augtree_block_bwd(const augtree_block_t *block, const void *dy, int x_dtype,
 
 /*
  * Checkpoints: [n_tokens] rows of *pitch bytes: ceil16(cols) integers -127 .. 127, then ceil16(ceil(cols / 32)) bytes e + 127.  32 neighbouring
- * columns share 2^e, the smallest power of two with max |x| < 127.5 2^e and e >= -126; a value stands for its integer times 2^e (the nearest,
- * ties to even).  A group with a NaN or an infinity (byte 255) stands for NaN.  Bytes behind the last column and group are not defined.
+ * columns share 2^e, the smallest power of two with max |x| < 127.5 2^e, but -126 <= e <= 121; a value stands for its integer times 2^e (the nearest,
+ * ties to even; magnitudes from 127.5 2^121 on, the last 0.4 % of fp32's range, stand for 127 2^121).  A group with a NaN or an infinity (byte 255)
+ * stands for NaN.  Bytes behind the last column and group are not defined.
  * unpack: out = 2^e q, times row[t] (fp32) and then col[c] where they are not NULL, in fp32, rounded to out's type.
  */
 int augtree_ckpt_pitch(int64_t cols, int64_t *pitch);

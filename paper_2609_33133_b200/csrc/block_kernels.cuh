@@ -108,9 +108,9 @@ __device__ __forceinline__ void block_store8(uint8_t *row, int vec, int type, co
   else Row8<__half>::store(reinterpret_cast<__half *>(row + vec * 16), x);
 }
 // A thread's kParts pieces of a row into its checkpoint.  The four lanes of a quad hold a group of 32 columns in each part; two parts' exponents go
-// through one pair of shuffles, and each lane of the quad writes one part's.
+// through one pair of shuffles, and each lane of the quad writes one part's.  Returns the largest of the thread's bytes, for block_cut.
 template <int kParts>
-__device__ __forceinline__ void block_keep(uint8_t *row, int v0, int step, int vecs, int scales, const V8 (&x)[kParts]) {
+__device__ __forceinline__ uint32_t block_keep(uint8_t *row, int v0, int step, int vecs, int scales, const V8 (&x)[kParts]) {
   uint32_t byte[kParts];
 #pragma unroll
   for (int k = 0; k < kParts; ++k) byte[k] = ckpt_byte(max_magnitude(x[k]));
@@ -134,6 +134,28 @@ __device__ __forceinline__ void block_keep(uint8_t *row, int v0, int step, int v
   }
   const int v = (v0 - quad) + quad * step;     // the group's first piece in part `quad`
   if (quad < kParts && v < vecs) row[scales + (v >> 2)] = (uint8_t)mine;
+  uint32_t top = byte[0];
+#pragma unroll
+  for (int k = 1; k < kParts; ++k) top = max(top, byte[k]);
+  return top;
+}
+// Makes the groups of a kept row again whose largest values have to be cut (ckpt_cut), from where the row still stands.  Behind everything else of the row and hardly ever: with the
+// cut in block_keep, whose arithmetic runs among that of the rest of the row, the forward pass of 16384 x 3584 bf16 with checkpoints takes 119 to 138 us instead of 108.
+template <int kParts, int T>
+__device__ __forceinline__ void block_cut(uint8_t *row, const uint8_t *from, int type, int v0, int step, int vecs, int scales) {
+  const uint32_t quad = threadIdx.x & 3, mask = 15u << (threadIdx.x & 28);     // (the four lanes of a quad come here together)
+#pragma unroll 1
+  for (int k = 0; k < kParts; ++k) {
+    const int v = v0 + k * step;
+    V8 x = only_if(v < vecs, block_load8<T>(from, min(v, vecs - 1), type, 0));
+    uint32_t byte = ckpt_byte(max_magnitude(x));
+    byte = max(byte, __shfl_xor_sync(mask, byte, 1));
+    byte = max(byte, __shfl_xor_sync(mask, byte, 2));
+    if (byte <= kCkptTop || byte == 255u) continue;
+    ckpt_cut(x, byte);
+    if (v < vecs) *reinterpret_cast<uint2 *>(row + v * 8) = ckpt_integers(x, ckpt_per(byte));
+    if (quad == k && v - quad < vecs) row[scales + (v >> 2)] = (uint8_t)byte;      // (the lane that has written it before)
+  }
 }
 // row t of a matrix in global memory
 template <int T>
@@ -343,6 +365,7 @@ block_fwd_kernel(const __grid_constant__ BlockParams p) {
         }
         // Straight through, without a branch for the pieces behind the row's end: their threads work on the last piece (at[k]) and count for nothing.
         V8 y[kParts];
+        uint32_t top_o = 0, top_y = 0;
         if (branch) {
           // (o is read twice rather than kept: registers are warps)
           float r_o = 1.f;
@@ -354,7 +377,7 @@ block_fwd_kernel(const __grid_constant__ BlockParams p) {
               o[k] = only_if(there[k], block_load8<OT>(ro, at[k], p.o_type, 0));
               ss = dot2(o[k], o[k], ss);
             }
-            if (p.ckpt_o.base) block_keep(p.ckpt_o.base + (size_t)t * (unsigned)p.ckpt_o.pitch, v0, step, vecs, (int)p.ckpt_o.scales, o);
+            if (p.ckpt_o.base) top_o = block_keep(p.ckpt_o.base + (size_t)t * (unsigned)p.ckpt_o.pitch, v0, step, vecs, (int)p.ckpt_o.scales, o);
             if (norm_out) {
               r_o = rsqrtf(fmaf(g.sum(ss.x + ss.y), p.inv_hidden, p.eps));
               if (p.r_out && writer) p.r_out[t] = r_o;
@@ -392,7 +415,13 @@ block_fwd_kernel(const __grid_constant__ BlockParams p) {
         if (p.ckpt_y.base) {
 #pragma unroll
           for (int k = 0; k < kParts; ++k) y[k] = block_round<XT>(y[k], p.x_type);
-          block_keep(p.ckpt_y.base + (size_t)t * (unsigned)p.ckpt_y.pitch, v0, step, vecs, (int)p.ckpt_y.scales, y);
+          top_y = block_keep(p.ckpt_y.base + (size_t)t * (unsigned)p.ckpt_y.pitch, v0, step, vecs, (int)p.ckpt_y.scales, y);
+        }
+        if (max(top_o, top_y) > kCkptTop) {
+          if (top_o > kCkptTop) block_cut<kParts, OT>(p.ckpt_o.base + (size_t)t * (unsigned)p.ckpt_o.pitch, ro, p.o_type, v0, step, vecs, (int)p.ckpt_o.scales);
+          if (top_y > kCkptTop)
+            block_cut<kParts, XT>(p.ckpt_y.base + (size_t)t * (unsigned)p.ckpt_y.pitch, branch ? block_row<XT>(p.y, t, hidden, p.x_type) : rx, p.x_type, v0, step, vecs,
+                                  (int)p.ckpt_y.scales);
         }
       }
       warp_arrive(c.bar_empty + 8 * st);

@@ -2,8 +2,9 @@
 //
 // A row of `cols` values is kept as ceil16(cols) bytes of integers and ceil16(ceil(cols / 32)) bytes of exponents (what lies behind
 // the last column or group is not defined).  32 neighbouring columns share 2^e, kept as the byte e + 127: the smallest power of two with max |x| < 127.5 2^e,
-// e >= -126; each value is x / 2^e rounded to the nearest integer (ties to even), which is then within -127 .. 127, and off by at most
-// half of 2^e, 1 / 127.5 of the group's largest value.  A group that holds a NaN or an infinity gets the byte 255 and reads as NaN.
+// but -126 <= e <= 121; each value is x / 2^e rounded to the nearest integer (ties to even) within -127 .. 127, and off by at most
+// half of 2^e, 1 / 127.5 of the group's largest value.  (With e = 122 the largest integer, 64, would stand for 2^128.  So magnitudes from 127.5 2^121 = 1.992 2^127 on, the
+// last 0.4 % of the range, read as 127 2^121 and are off by less than 2^121.)  A group that holds a NaN or an infinity gets the byte 255 and reads as NaN.
 // Why so: with a power of two both directions are exact but for the one rounding, so the form of a tensor does not depend on which
 // kernel made it, and what it stands for fits bf16 exactly (8 significant bits), which the tensor core takes as an operand without
 // a second rounding.  For normal values 32 of which share an exponent the error is 0.0075 of their deviation (rms); 8-bit floating
@@ -113,13 +114,21 @@ __device__ __forceinline__ float max_magnitude(float a, float b, float c) {
   return d;
 }
 // The exponent byte of a group whose largest magnitude is `top` (magnitudes order like their bits, infinity and NaN on top).  It grows with
-// `top`, so the byte of a group is also the largest of its parts' bytes.
+// `top`, so the byte of a group is also the largest of its parts' bytes.  One more than kCkptTop if the group's largest values have to be cut (ckpt_cut).
 __device__ __forceinline__ uint32_t ckpt_byte(float top) {
   const uint32_t m = __float_as_uint(top);
   // m = f 2^k, 1 <= f < 2: e = k - 6, one more from f = 127.5 / 64 on, where the added bits carry into the exponent
   return m < 0x7f800000u ? (uint32_t)max((int)((m + 0x10000u) >> 23) - 6, 1) : 255u;
 }
 __device__ __forceinline__ float ckpt_per(uint32_t byte) { return byte == 255u ? 0.f : __uint_as_float((254u - byte) << 23); }   // 2^-e
+constexpr uint32_t kCkptTop = 121 + 127;     // the byte of the largest power of two
+// Values of a group whose byte is above that: finite ones (the byte says 2^122) are cut to 127 2^121.
+__device__ __forceinline__ void ckpt_cut(V8 &x, uint32_t &byte) {
+  if (byte <= kCkptTop || byte == 255u) return;
+  byte = kCkptTop;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = fminf(fmaxf(x[i], -127.f * 0x1p121f), 127.f * 0x1p121f);
+}
 __device__ __forceinline__ uint2 ckpt_integers(const V8 &x, float per) {
   const V8 b = fma(x, per, v8(12582912.f));    // + 1.5 2^23: the integer in the low bits
   uint32_t q[2];
@@ -141,9 +150,14 @@ __device__ __forceinline__ float max_magnitude(const V8 &x) {
   return top;
 }
 // 16 columns of a thread; a lane pair holds a group.  Every lane of the warp takes part; columns behind the row's end are zero.
-__device__ __forceinline__ void ckpt_encode(const V8 &lo, const V8 &hi, uint4 &q, uint32_t &byte) {
+__device__ __forceinline__ void ckpt_encode(V8 lo, V8 hi, uint4 &q, uint32_t &byte) {
   byte = ckpt_byte(max_magnitude(max_magnitude(lo), max_magnitude(hi), 0.f));
   byte = max(byte, __shfl_xor_sync(0xffffffffu, byte, 1));
+  if (__builtin_expect(byte > kCkptTop, 0)) {
+    uint32_t same = byte;
+    ckpt_cut(lo, same);
+    ckpt_cut(hi, byte);
+  }
   const float per = ckpt_per(byte);
   const uint2 a = ckpt_integers(lo, per), b = ckpt_integers(hi, per);
   q = make_uint4(a.x, a.y, b.x, b.y);

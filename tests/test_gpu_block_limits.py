@@ -116,3 +116,73 @@ def test_the_widest_rows_through_autograd(B, kind, c, x_grad):
         if t.grad is not None:
             bu.check(t.grad, (val, bound + 1000 * bu.U * val.abs().max()), name)
     assert blk.device_status() == (0, 0)
+
+
+def test_the_largest_values_stay_finite(B):
+    """The power of two stops at 2^121: with 2^122 the integer 64 would stand for 2^128.  Integers stop at 127, so that a finite value never reads as an infinity; either
+    side of the border, both signs, alone and beside zeros, small values and values that are the largest already."""
+    top, border = torch.finfo(F32).max, 127.5 * 2.0 ** 121
+    below = torch.nextafter(torch.tensor(border), torch.tensor(0.0)).item()
+    x = torch.zeros(8, 96)
+    x[0, :4] = torch.tensor([top, -top, 1.0, 2.0 ** 121 * 64.5])
+    x[1, 32] = border
+    x[2, 31], x[2, 32], x[2, 95] = -border, below, -below
+    x[3] = torch.finfo(BF16).max
+    x[4] = -torch.finfo(BF16).max
+    x[5] = torch.linspace(-1, 1, 96) * top
+    x[6, ::2], x[6, 5] = 2.0 ** 127, 2.0 ** 120
+    x[7, 40], x[7, 70] = float("inf"), top
+
+    def want(t):
+        v = t.to(F64).view(8, 3, 32)
+        bad = ~torch.isfinite(v).all(2, keepdim=True)
+        _, byte = bu.encode(torch.where(bad.expand_as(v), 0.0, v).reshape(8, 96))
+        e = (byte - 127).clamp(max=121)[:, :, None]
+        return torch.where(bad, float("nan"), torch.round(v / torch.exp2(e)).clamp(-127, 127) * torch.exp2(e)).view(8, 96)
+    blk = B.Block(96, device=0)
+    for dtype in (F32, BF16):
+        t = x.to(dtype) if dtype is F32 else x.clamp(-torch.finfo(BF16).max, torch.finfo(BF16).max).to(BF16)
+        t[7, 40] = float("inf")
+        ckpt = torch.full((8, B.ckpt_pitch(96)), 173, device="cuda", dtype=U8)
+        blk.pack(t.cuda(), ckpt)
+        for out in (torch.empty(8, 96, device="cuda"), torch.empty(8, 96, device="cuda", dtype=BF16)):
+            blk.unpack(ckpt, out)
+            assert torch.equal(out.cpu().double().nan_to_num(nan=7.0), want(t).nan_to_num(nan=7.0))
+            assert torch.isfinite(out[:7]).all()
+        # the block end and the gated MLP keep the same bytes
+        z, h, fused = torch.zeros_like(t).cuda(), torch.empty(8, 96, device="cuda", dtype=BF16), torch.full_like(ckpt, 173)
+        one = torch.ones(96, device="cuda")
+        blk.fwd(t.cuda(), z.to(BF16), None, None, one, torch.empty_like(z), h, None, torch.empty(8, device="cuda"), fused, None)
+        used = slice(0, 99)                # 96 integers, three exponents
+        assert torch.equal(fused[:, used], ckpt[:, used])
+        for k in (torch.full_like(ckpt, 173), torch.full_like(ckpt, 173)):
+            blk.glu_fwd(t.cuda(), t.cuda(), torch.empty_like(z), fused, k)
+            assert torch.equal(fused[:, used], ckpt[:, used]) and torch.equal(k[:, used], ckpt[:, used])
+    assert blk.device_status() == (0, 0)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,c", [(40, 248), (700, 1032), (9, 8192)])
+@pytest.mark.parametrize("branch", [False, True])
+def test_block_ends_keep_the_largest_values_as_pack_does(B, dtype, n, c, branch):
+    """Rows with groups at the end of the range among ordinary ones: the fused checkpoints of y and of o are those of pack to the byte, and read as finite values."""
+    gen = torch.Generator(device="cuda").manual_seed(c)
+    draw = lambda t: torch.randn(n, c, generator=gen, device="cuda").to(t)
+    big = lambda t: torch.where(torch.rand(n, c, generator=gen, device="cuda") < 0.002, torch.finfo(t).max * torch.randn(n, c, generator=gen, device="cuda").sign(), draw(F32)).to(t)
+    blk = B.Block(c, device=0, residual_scale=1e-30)
+    new = lambda: torch.full((n, B.ckpt_pitch(c)), 173, device="cuda", dtype=U8)
+    x, o, one = big(dtype), big(BF16) if branch else None, torch.ones(c, device="cuda")
+    y, h, r = torch.empty_like(x) if branch else None, torch.empty(n, c, device="cuda", dtype=BF16), torch.empty(n, device="cuda")
+    for w_out in (None, one) if branch else (None,):
+        ky, ko = new(), new() if branch else None
+        blk.fwd(x, o, None, w_out, one, y, h, None, r, ky, ko)
+        at = -(-c // 16) * 16
+        for kept, t in ((ky, y if branch else x), (ko, o)):
+            if t is None:
+                continue
+            same, out = new(), torch.empty(n, c, device="cuda")
+            blk.pack(t, same)
+            blk.unpack(kept, out)
+            assert torch.equal(kept[:, :c], same[:, :c]) and torch.equal(kept[:, at:at + -(-c // 32)], same[:, at:at + -(-c // 32)])
+            assert (t.float().abs() == torch.finfo(t.dtype).max).any() and torch.isfinite(t).all() and torch.isfinite(out).all()
+    assert blk.device_status() == (0, 0)
