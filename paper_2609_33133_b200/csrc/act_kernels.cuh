@@ -95,7 +95,7 @@ template <typename T> __device__ __forceinline__ Raw16<T> raw16(const T *p, int 
 template <typename T> __device__ __forceinline__ V8 values(const Raw16<T> &r, int run) { return Row8<T>::load(reinterpret_cast<const T *>(&r) + run * 8); }
 template <typename T> __device__ __forceinline__ void store16(T *p, int there, bool wide, const V8 &lo, const V8 &hi) {
   if (sizeof(T) == 2 && wide && there == 2) {
-    T v[16];
+    alignas(16) T v[16];
     Row8<T>::store(v, lo);
     Row8<T>::store(v + 8, hi);
     uint32_t w[8];
