@@ -39,6 +39,7 @@ namespace augtree {
 enum : int { LM_STATS = 0, LM_GRAD = 1, LM_DH = 2, LM_DW = 3 };
 enum : int { WAIT_LM_FULL = 80, WAIT_LM_EMPTY = 81, WAIT_LM_ACC_FULL = 82, WAIT_LM_ACC_EMPTY = 83 };
 
+constexpr int kLmThreads = 320;
 constexpr int kLmMaxJobs = 2;
 
 // One product.  Rows of the compacted token block (their number is known on the device only) take part in every
@@ -75,6 +76,15 @@ struct LmParams {
   int *status;
   long long wait_budget;
   int test_flags;
+};
+
+struct LmSmem {
+  static constexpr int kABytes = 128 * 128, kBBytes = 128 * 128;  // this CTA's share of a stage
+  static constexpr int kStageBytes = kABytes + kBBytes;
+  static constexpr int kStages = 6;
+  static constexpr int kOffOut = kStages * kStageBytes;   // 4 KB a warp on their way out
+  static constexpr int kOffBar = kOffOut + 8 * 4096;
+  static constexpr int kBytes = kOffBar + 256;
 };
 
 // Walks the tiles of one CTA pair: tile t0, t0 + step, .. of all jobs in a row.

@@ -1,20 +1,10 @@
-// What the products of CTA pairs share (256 x 256 output tiles, tcgen05 cta_group::2): sizes, shared memory, the way results leave.
+// What the products of CTA pairs share (256 x 256 output tiles, tcgen05 cta_group::2): the tile, the way results leave.
 #pragma once
 #include "ptx.cuh"
 
 namespace augtree {
 
 constexpr int kLmTile = 256;     // tile rows and columns of a CTA pair
-constexpr int kLmThreads = 320;
-
-struct LmSmem {
-  static constexpr int kABytes = 128 * 128, kBBytes = 128 * 128;  // this CTA's share of a stage
-  static constexpr int kStageBytes = kABytes + kBBytes;
-  static constexpr int kStages = 6;
-  static constexpr int kOffOut = kStages * kStageBytes;   // 4 KB a warp on their way out
-  static constexpr int kOffBar = kOffOut + 8 * 4096;
-  static constexpr int kBytes = kOffBar + 256;
-};
 
 // A row's columns into the warp's 4 KB block, in the 128-byte swizzle (16-byte chunk j of row r sits at j ^ (r % 8)): 32 columns
 // of 16 bits as the chunks from `chunk`, or 32 columns of 32 bits.
