@@ -164,6 +164,27 @@ def wgrad(dy, x, row, col, dtype):
     return val, adds * U * mag + (2.0 ** -8 * mag if row is not None else 0.0) + 4 * U * val.abs() + rounding(dtype, val)
 
 
+def wgrad_exact_operand(dy, x, row, col, dtype, chain=128):
+    """As wgrad, from the operand that the tensor core is given: a token's factor rounds it once, to a number that can be formed exactly here, so that what is left are the
+    additions, of which `chain` come in a row inside the tensor core.  Returns the value before its delivery and the bound of that."""
+    n = dy.shape[0]
+    x = x.to(F32)
+    if row is not None:
+        x = (x * row.to(F32)[:, None]).to(BF16)
+    dy, x = dy.to(F64), x.to(F64)
+    f = col.to(F64) if col is not None else torch.ones(x.shape[1], dtype=F64)
+    val = dy.T @ x * f
+    return val, (2 * min(n / 16 + 1, chain) + n / 2048 + 44) * U * (dy.abs().T @ x.abs() * f.abs())
+
+
+def check_delivered(got, want, what=""):
+    """A rounding of a value within the bound: rounding keeps the order, so what is delivered lies between the roundings of the interval's ends."""
+    (val, bound), got = want, got.detach().cpu()
+    lo, hi = (val - bound).to(got.dtype), (val + bound).to(got.dtype)
+    bad = ~((lo <= got) & (got <= hi))      # (NaN is bad)
+    assert got.shape == val.shape and not bad.any(), (what, int(bad.sum()), float((got.to(F64) - val).abs()[bad].max()), bad.nonzero()[0].tolist())
+
+
 def check(got, want, what=""):
     val, bound = want
     got = got.detach().cpu().to(F64)

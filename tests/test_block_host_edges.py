@@ -10,6 +10,8 @@ import weakref
 import pytest
 import torch
 
+from tests import block_util as bu
+
 CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2609_33133_b200", "csrc")
 
 
@@ -141,3 +143,20 @@ def test_another_torch_gets_an_extension_of_its_own(B, monkeypatch):
     assert os.path.exists(here) and not build._stale(here, build.MARSHAL_SOURCES)
     monkeypatch.setattr(torch, "__version__", "99.0")
     assert build.marshal_path() != here and build._stale(build.marshal_path(), build.MARSHAL_SOURCES)
+
+
+# ------------------------------------------------------------------------------------------------ the weight gradient's bounds
+@pytest.mark.parametrize("n", [65, 743, 2183, 5000])
+def test_the_bounds_see_mistakes_in_the_tokens_factors(n):
+    """A rounding too many of the factors, a scale, the last token with its neighbour's factor, two tokens swapped, the last token left out."""
+    gen = torch.Generator().manual_seed(n)
+    randn = lambda *s: torch.randn(*s, generator=gen)
+    dy, x, row, col = randn(n, 72).to(torch.bfloat16), bu.in_8_bits(2 * randn(n, 64)), randn(n).abs() + 0.1, 1 + 0.2 * randn(64)
+    want = bu.wgrad_exact_operand(dy, x, row, col, torch.float32)
+    bu.check_delivered(want[0].float(), want)
+    last, swapped = row.clone(), row.clone()
+    last[-1], swapped[3], swapped[17] = row[-2], row[17], row[3]
+    for other in ((dy, x, row.to(torch.bfloat16).float(), col), (dy, x, 1.003 * row, col), (dy, x, last, col), (dy, x, swapped, col), (dy[:-1], x[:-1], row[:-1], col),
+                  (dy, x * row[:, None], None, col)):
+        with pytest.raises(AssertionError):
+            bu.check_delivered(bu.wgrad_exact_operand(*other, torch.float32)[0].float(), want)

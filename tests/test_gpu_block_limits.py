@@ -59,13 +59,6 @@ def test_memory_after_the_backward_pass_while_the_loss_is_held(B):
         del s
 
 
-def between(got, val, off):
-    """A rounding of some value within `off` of `val`: rounding keeps the order, so its bounds are the roundings of the interval's ends."""
-    lo, hi = (val - off).to(got.dtype), (val + off).to(got.dtype)
-    bad = ~((lo <= got) & (got <= hi))
-    assert not bad.any(), (int(bad.sum()), ((got.double() - val) / val)[bad].mean().item())
-
-
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("n,lanes", [(32768, 2), (32769, 2), ((1 << 20) + 37, 2), ((1 << 20) + 37, 0)])
 def test_a_weight_gradient_over_many_tokens_of_one_sign(B, n, lanes, dtype):
@@ -86,7 +79,7 @@ def test_a_weight_gradient_over_many_tokens_of_one_sign(B, n, lanes, dtype):
     val *= col.double()
     one = dtype is BF16 and n <= 32768 and lanes == 2
     adds = 2 * 2049 if one else 2 * 128 + n / 2048 + 40
-    between(dw, val, (adds + 4) * bu.U * val)
+    bu.check_delivered(dw, (val.cpu(), (adds + 4) * bu.U * val.cpu()))
     assert blk.device_status() == (0, 0)
 
 
@@ -185,4 +178,22 @@ def test_block_ends_keep_the_largest_values_as_pack_does(B, dtype, n, c, branch)
             blk.unpack(kept, out)
             assert torch.equal(kept[:, :c], same[:, :c]) and torch.equal(kept[:, at:at + -(-c // 32)], same[:, at:at + -(-c // 32)])
             assert (t.float().abs() == torch.finfo(t.dtype).max).any() and torch.isfinite(t).all() and torch.isfinite(out).all()
+    assert blk.device_status() == (0, 0)
+
+
+@pytest.mark.parametrize("n,out,c,lanes", [(1, 8, 8, 0), (65, 264, 200, 0), (129, 256, 512, 0), (743, 520, 1032, 0), (2183, 512, 136, 0), (5000, 72, 328, 0), (4160, 640, 576, 0),
+                                           (700, 520, 328, 2), (2200, 72, 264, 2), (5000, 328, 520, 4)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_a_tokens_factor_rounds_the_operand_once(B, n, out, c, lanes, dtype):
+    """From the bits (all lanes) and by way of bf16 scratch (few): against the very operand, so that the additions' bound alone is left."""
+    blk = B.Block(64, device=0, n_lanes=lanes)
+    gen = torch.Generator().manual_seed(n + c)
+    randn = lambda *s: torch.randn(*s, generator=gen)
+    dy, x, row, col = randn(n, out).to(BF16), (2 * randn(n, c) * torch.exp(0.5 * randn(c))).to(BF16), randn(n).abs() + 0.1, 1 + 0.2 * randn(c)
+    ckpt, dw = torch.full((n, B.ckpt_pitch(c)), 173, device="cuda", dtype=U8), torch.full((out, c), float("nan"), device="cuda", dtype=dtype)
+    blk.pack(x.cuda(), ckpt)
+    ws = torch.empty(blk.wgrad_workspace_bytes(n, out, c), device="cuda", dtype=U8)
+    for r, f in ((row, col), (row, None)):
+        blk.wgrad(dy.cuda(), ckpt, dw, ws, r.cuda(), None if f is None else f.cuda())
+        bu.check_delivered(dw, bu.wgrad_exact_operand(dy, bu.in_8_bits(x), r, f, dtype, chain=128 if dtype is F32 else n / 16 + 1))
     assert blk.device_status() == (0, 0)
