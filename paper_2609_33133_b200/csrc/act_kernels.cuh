@@ -109,8 +109,15 @@ template <typename T> __device__ __forceinline__ void store16(T *p, int there, b
 }
 
 // e^-g by the special-function unit (2 units in the last place of g log2(e) and of 2^x), the quotient by its reciprocal: relative
-// error below 1e-6 for |g| < 8 and absolute below 1e-6 everywhere, far under the rounding of 16-bit results.
+// error below 1e-6 for |g| < 8 and absolute below 1e-6 everywhere, far under the rounding of 16-bit results.  An fp32 result carries it, up to 17 of its half steps, beside
+// inputs that mostly come from 16-bit products; the exact exponential and quotient take some 20 instructions more a value.
 __device__ __forceinline__ float logistic(float g) { return __fdividef(1.f, 1.f + __expf(-g)); }
+// With its derivative a (1 - a), as e^-|g| a^2 or the like: the difference would lose all its figures where a is near one.
+struct Logistic { float a, slope; };
+__device__ __forceinline__ Logistic logistic_pair(float g) {
+  const float t = __expf(-fabsf(g)), s = __fdividef(1.f, 1.f + t), ts = t * s;
+  return {g < 0.f ? ts : s, ts * s};
+}
 
 __device__ __forceinline__ V8 logistic(const V8 &g) {
   V8 s;

@@ -536,14 +536,21 @@ block_bwd_kernel(const __grid_constant__ BlockParams p) {
             u[k] = only_if(there[k], block_load8_times<ST>(ro, at[k], p.o_type, scales, r_o));
             const V8 q = d[k] * p.scale;
             if (gate >= GATE_CHANNEL) {
-              V8 a = gate == GATE_FULL ? block_load8<OT>(row(at_g), at[k], p.gate_type, 0) : block_weight(g_ch, at[k], vecs);
-              if (p.sigmoid) a = logistic(a);
+              V8 a = gate == GATE_FULL ? block_load8<OT>(row(at_g), at[k], p.gate_type, 0) : block_weight(g_ch, at[k], vecs), slope = v8(1.f);
+              if (p.sigmoid) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                  const Logistic l = logistic_pair(a[i]);
+                  a[i] = l.a;
+                  slope[i] = l.slope;
+                }
+              }
               const V8 qa = q * a, w = norm_out ? block_weight(w_out, at[k], vecs) : v8(1.f);
               acc_out[k] = fma(gate == GATE_CHANNEL ? q : qa, u[k], acc_out[k]);
               d[k] = w * qa;
               if (gate == GATE_FULL && p.dg && there[k]) {
                 V8 dg = q * (w * u[k]);
-                if (p.sigmoid) dg = dg * (a * fma(a, -1.f, v8(1.f)));
+                if (p.sigmoid) dg = dg * slope;
                 block_store8<OT>(block_row<OT>(p.dg, t, hidden, p.gate_type), at[k], p.gate_type, dg);
               }
             } else {
@@ -556,7 +563,10 @@ block_bwd_kernel(const __grid_constant__ BlockParams p) {
           if (norm_out || gate == GATE_TOKEN) {
             const float total = g.sum(dot.x + dot.y);
             mean = -total * p.inv_hidden;
-            if (gate == GATE_TOKEN && p.dg && writer) block_scalar_store(p.dg, t, p.gate_type, total * (p.sigmoid ? gate_t * (1.f - gate_t) : 1.f));
+            // (the slope from the gate once more, by the one thread that needs it: 16384 x 3584 bf16 with checkpoints 136 us; kept over the row in a register 138, in
+            // shared memory 137)
+            if (gate == GATE_TOKEN && p.dg && writer)
+              block_scalar_store(p.dg, t, p.gate_type, total * (p.sigmoid ? logistic_pair(block_scalar(p.gate_ptr, t, p.gate_type)).slope : 1.f));
           }
           if (put_do) {
             const float f = r_o * gate_t;      // (1 without a norm, 1 without a gate of one number a token)
@@ -643,7 +653,7 @@ __global__ void __launch_bounds__(1024) block_sums_kernel(const BlockSums p) {
   float a = 1.f, slope = 1.f;
   if (p.gate) {
     a = block_scalar(p.gate, c, p.gate_type);
-    if (p.sigmoid) { a = logistic(a); slope = a * (1.f - a); }
+    if (p.sigmoid) { const Logistic l = logistic_pair(a); a = l.a; slope = l.slope; }
     if (p.dg) put(p.dg, p.gate_type, v * slope * (p.w_out ? block_scalar(p.w_out, c, p.w_type) : 1.f));
   }
   if (p.dw_out) put(p.dw_out, p.w_type, v * a);

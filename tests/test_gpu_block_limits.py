@@ -197,3 +197,32 @@ def test_a_tokens_factor_rounds_the_operand_once(B, n, out, c, lanes, dtype):
         blk.wgrad(dy.cuda(), ckpt, dw, ws, r.cuda(), None if f is None else f.cuda())
         bu.check_delivered(dw, bu.wgrad_exact_operand(dy, bu.in_8_bits(x), r, f, dtype, chain=128 if dtype is F32 else n / 16 + 1))
     assert blk.device_status() == (0, 0)
+
+
+@pytest.mark.parametrize("kind", ["token", "channel", "full"])
+def test_saturated_gates_keep_a_gradient(B, kind):
+    """Logits up to 80 either way: the slope e^-|g| / (1 + e^-|g|)^2 is within a relative error that grows with |g| alone (its exponent is rounded, 2^-24 |g| log2(e) and 2 units of
+    2^x), like the gate's value for negative logits.  Everything in fp32, residual stream's gradient alone, so that d_gate = s dy o slope summed over what shares it."""
+    n, c, scale = 64, 264, 0.7
+    gen = torch.Generator().manual_seed(5)
+    blk = B.Block(c, device=0, residual_scale=scale, gate=kind, gate_sigmoid=True)
+    shape = {"token": (n,), "channel": (c,), "full": (n, c)}[kind]
+    g = torch.linspace(-80, 80, torch.Size(shape).numel()).view(shape)
+    dy, o = torch.randn(n, c, generator=gen).abs() + 0.1, torch.randn(n, c, generator=gen).abs() + 0.1      # (terms of one sign)
+    d_o, d_gate = torch.empty(n, c, device="cuda"), torch.empty(shape, device="cuda")
+    ws = torch.empty(blk.workspace_bytes(n), device="cuda", dtype=U8)
+    blk.bwd(dy.cuda(), None, None, o.cuda(), g.cuda(), None, None, None, None, None, d_o, d_gate, None, None, ws)
+    wide = g.double()
+    wide = wide[:, None].expand(n, c) if kind == "token" else wide.expand(n, c)
+    t = torch.exp(-wide.abs())
+    a, slope = torch.where(wide < 0, t, torch.ones_like(t)) / (1 + t), t / (1 + t) ** 2
+    rel = (4 * wide.abs() + 40) * bu.U
+    term = scale * dy.double() * o.double() * slope
+    chain = 0 if kind == "full" else 120
+    off = (rel + chain * bu.U) * term
+    if kind != "full":
+        term, off = term.sum(1 if kind == "token" else 0), off.sum(1 if kind == "token" else 0)
+    bu.check(d_gate, (term, off + 2.0 ** -149), "d_gate")
+    v = scale * dy.double() * a
+    bu.check(d_o, (v, rel * v + 2.0 ** -149), "d_o")
+    assert blk.device_status() == (0, 0)
