@@ -566,7 +566,8 @@ int augtree_block_bwd(const augtree_block_t *block, const void *dy, int x_dtype,
  * columns share 2^e, the smallest power of two with max |x| < 127.5 2^e, but -126 <= e <= 121; a value stands for its integer times 2^e (the nearest,
  * ties to even; magnitudes from 127.5 2^121 on, the last 0.4 % of fp32's range, stand for 127 2^121).  A group with a NaN or an infinity (byte 255)
  * stands for NaN.  Bytes behind the last column and group are not defined.
- * unpack: out = 2^e q, times row[t] (fp32) and then col[c] where they are not NULL, in fp32, rounded to out's type.
+ * unpack: out = 2^e q, times row[t] (fp32) and then col[c] where they are not NULL, in fp32, rounded to out's type.  (2^e row[t] has to stay finite, as it does with a
+ * norm's factor: a zero beside values that overflow reads as NaN otherwise.  The same holds for the weight gradient below.)
  */
 int augtree_ckpt_pitch(int64_t cols, int64_t *pitch);
 int augtree_ckpt_pack(const augtree_block_t *block, const void *x, int dtype, int64_t ld, int64_t n_tokens, int64_t cols, void *ckpt, void *stream);

@@ -8,7 +8,7 @@
 //           written.  No launch and no memory beside it, but every row of tiles does it again, and with 92 instructions for 16 values it
 //           keeps the tensor core waiting: 740 cycles a stage instead of 512.
 //   other   ckpt_unpack_kernel has left X in bf16 in scratch, from where the copy engine loads it.
-// Measured (us, kBits against other): 129 tokens x 256 -> 256 6.9 against 8.2; 4096 x 3584 -> 512 23 against 27; 4096 x 3584 -> 3584 91 against 84;
+// Measured (us, kBits against other): 129 tokens x 256 -> 256 6.9 against 8.2; 4096 x 3584 -> 512 24 against 27; 4096 x 3584 -> 3584 91 against 84;
 // 16384 x 3584 -> 18944 1705 against 1450 to 1540.  wgrad_way (block.cu) chooses.
 // Without kBits the tensor pipe is 95.9 % active (4096 x 3584 -> 18944: 343 us, 1621 TFLOP/s); in a long run the board's power decides: 16384 x 3584 -> 18944 takes
 // 1770 us, 1257 TFLOP/s, and the library's product of the same sizes 1610.
