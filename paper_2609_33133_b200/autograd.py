@@ -231,6 +231,7 @@ def linear(blk: B.Block, h, weight, kept=None):
                              f"{got(h)} and {got(weight)}, product {y.dtype}")
         if kept.ckpt.shape != (h.shape[0], B.ckpt_pitch(h.shape[1])):
             raise ValueError(f"linear: h is {got(h)}, the checkpoint is of another tensor: {got(kept.ckpt)}")
+        blk.wgrad_workspace_bytes(h.shape[0], *weight.shape)      # (raises for sizes beyond the product's limits)
     return y
 
 

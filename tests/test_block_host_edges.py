@@ -104,9 +104,9 @@ def test_a_product_whose_gradient_cannot_be_made_is_refused_at_once(B):
     BF16, F16, F32 = torch.bfloat16, torch.float16, torch.float32
     blk = Still(64)
 
-    def product(n=6, out=72, h=BF16, weight=BF16, shape=None, rows=None, wanted=True):
+    def product(n=6, out=72, h=BF16, weight=BF16, shape=None, rows=None, wanted=True, device="cpu"):
         kept = A.Kept(torch.zeros(rows or n, B.ckpt_pitch(64), dtype=torch.uint8), torch.ones(rows or n), torch.ones(64))
-        return A.linear(blk, torch.ones(shape or (n, 64), dtype=h), torch.ones(out, 64, dtype=weight, requires_grad=wanted), kept)
+        return A.linear(blk, torch.ones(shape or (n, 64), dtype=h, device=device), torch.ones(out, 64, dtype=weight, requires_grad=wanted, device=device), kept)
     product().float().sum().backward()
     assert [name for name, _, _ in blk.calls] == ["wgrad"]
     for bad in (dict(h=F16, weight=F16), dict(h=F32, weight=F32), dict(out=60), dict(shape=(2, 3, 64)), dict(shape=(64,)), dict(rows=5)):
@@ -115,6 +115,10 @@ def test_a_product_whose_gradient_cannot_be_made_is_refused_at_once(B):
         product(**bad, wanted=False)       # (nobody wants the weight's gradient)
         with torch.no_grad():
             product(**bad)
+    blk = B.Block(64, device=None, n_lanes=4)
+    with pytest.raises(B.AugtreeError) as err:      # more features than the product takes
+        product(out=(1 << 20) + 8, device="meta")
+    assert err.value.code == B.ERR_UNSUPPORTED
     with torch.autocast("cpu", BF16):      # the product's type counts, not its operands'
         assert product(weight=F32).dtype is BF16
 
