@@ -15,7 +15,7 @@
 // A group's sum over a row: shuffles, then the warps' sums through shared memory behind one named barrier.
 // The sums over tokens stay in registers (every thread owns its columns for all rows of its group), go over the groups through shared memory
 // and from CTA to CTA through scratch and a second kernel, in an order that depends on the sizes alone: no atomics, bitwise repeatable.
-// Measured (share of the bytes' time at 6.56 TB/s): 24576 x 3584 with an fp32 stream, forward and backward 411 to 420 us (97 %; a loop of one direction alone takes
+// Measured (share of the bytes' time at 6.56 TB/s): 24576 x 3584 with an fp32 stream, forward and backward 411 to 421 us (97 %; a loop of one direction alone takes
 // 181 and 260, 89 and 93 %); 16384 x 3584 with a bf16 stream and checkpoints, which has 10 bytes a value for about the same arithmetic, forward 108 to 115 us (80 %),
 // backward 134 us (67 %; 136 with a logistic gate of a token): 37 and 36 instructions a value, of which half are arithmetic on the values, issue slots 60 % busy.  Forward 16 warps, backward 14 of 128 registers
 // are all that fit, and the rest is waits for fixed latencies, shared memory and the row's sums.  (Both means of the backward pass from three sums behind
